@@ -49,6 +49,18 @@ typedef struct kvc_ctx kvc_ctx;
 
 /* Element types. */
 enum { KVC_F32 = 0, KVC_BF16 = 1 };
+/* Flag on kvc_config.dtype: K and V are held in 4 bits, for 3.6 (bfloat16) or 7.1 (binary32) times
+ * as many positions in the same memory; what the calls take and give stays in the element type.
+ * Each row (the K or V of one position and KV head; K after its rotation) is held in groups of 32
+ * elements x with a scale s = max|x| / 7, rounded to 7 significant bits and to a multiple of 2^-20
+ * at the finest, 9344 at most, and codes c = x / s rounded to an integer of -7 .. 7 (ties to even).
+ * It stands for s * c: elements beyond 65408 are held as 65408, groups below 3.5 * 2^-20 as 0.  A
+ * group that holds an infinity or a NaN stands for NaN.
+ * Every call takes such a context but kvc_attn_decode_noalloc, which returns KVC_EINVAL.  Attention
+ * runs over the numbers that the codes stand for, in binary32 with exact K and V operands; for
+ * bfloat16 q (scaled by a power of two) and P are rounded to binary16 for the tensor cores, for
+ * binary32 each is split into two such pieces. */
+#define KVC_KV4 0x10
 
 /* Token type tags (low 7 bits of a type byte).  Sec. 3.3: ACOUSTIC (unit
  * marker, audio tokens, native decision, terminators) and ASR_DELIM are
@@ -98,7 +110,7 @@ typedef struct kvc_config {
   int32_t page_size;             /* positions per page; 16 */
   int64_t budget;                /* B (Sec. 3.3); < 0 means unbounded */
   int32_t window;                /* W >= 0 most recent units are never evicted */
-  int32_t dtype;                 /* KVC_F32 or KVC_BF16 */
+  int32_t dtype;                 /* KVC_F32 or KVC_BF16, each with or without KVC_KV4 */
   double rope_base;              /* rotary base, e.g. 10000 */
   int64_t n_pages;               /* pool capacity in pages */
   int32_t max_pages_per_session; /* capacity of each of a session's two page lists */
@@ -111,7 +123,7 @@ typedef struct kvc_config {
 } kvc_config;
 
 /* Supported shapes: (KVC_BF16, head_dim 128) and (KVC_F32, head_dim 64), with
- * G = Hq / Hkv = 4 and page_size 16. */
+ * G = Hq / Hkv = 4 and page_size 16; each with or without KVC_KV4. */
 
 typedef struct kvc_session_info {
   int32_t pos_next;       /* next position id (= positions fed so far) */
@@ -127,7 +139,8 @@ typedef struct kvc_session_info {
 } kvc_session_info;
 
 /* Bytes of pool and metadata workspace a configuration needs.
- * Pool layout: page-major, [n_pages][L][2 (K,V)][Hkv][page_size][D] elements.
+ * Pool layout: page-major, [n_pages][L][2 (K,V)][Hkv][page_size][D] elements; with KVC_KV4
+ * [n_pages][L][Hkv][2 (K,V)] tiles of page_size rows of D / 2 + D / 16 bytes.
  * Returns KVC_EINVAL for unsupported or inconsistent configurations. */
 int kvc_query_sizes(const kvc_config* cfg, size_t* pool_bytes, size_t* meta_bytes);
 
@@ -290,7 +303,7 @@ int kvc_export_state(kvc_ctx* ctx, int session, kvc_session_info* h_info,
                      uint8_t* h_type, int32_t* h_unit, int64_t cap);
 
 /* Copy the stored (rotated) K and V of one layer of one session, in retained
- * order, to host buffers [cap][Hkv][D] each (synchronises). */
+ * order, to host buffers [cap][Hkv][D] each in the element type (synchronises). */
 int kvc_export_kv(kvc_ctx* ctx, int session, int layer, void* h_k, void* h_v, int64_t cap);
 
 /* Transcript export for query-time re-encoding (Sec. 4.2: task queries use
@@ -309,6 +322,22 @@ int kvc_export_kv(kvc_ctx* ctx, int session, int layer, void* h_k, void* h_v, in
  *              min(count, cap) of them are written */
 int kvc_export_transcript(kvc_ctx* ctx, int session, int64_t cap, int32_t* d_pos_out,
                           void* d_k_out, void* d_v_out, int32_t* d_count, void* stream);
+
+/* Read rows back: retained positions of the listed sessions, K (rotated at the original position)
+ * and V of n_layers layers from layer0 on, in the element type (with KVC_KV4 what the codes stand
+ * for, rounded once).  Asynchronous on stream; leaves the cache and its queries unchanged.
+ *   n_seq, h_sessions  as for kvc_append_chunk
+ *   h_first     host [n_seq] first retained position (0 = the oldest one that is still resident)
+ *   h_cu_rows   host [n_seq+1] offsets of the sessions' rows in the outputs, h_cu_rows[0] = 0,
+ *               ascending; a session may have none
+ *   d_k_out, d_v_out  device [n_layers][h_cu_rows[n_seq]][Hkv][D], 16-byte aligned; rows past the
+ *               positions that a session holds are zeros
+ *   d_resident_out  optional device [n_seq] int64: resident counts
+ * After kvc_append_chunk without K/V the new positions' rows of a layer are what their slots held
+ * before until the layer is written. */
+int kvc_read_kv(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, const int32_t* h_first,
+                const int32_t* h_cu_rows, int layer0, int n_layers, void* d_k_out, void* d_v_out,
+                int64_t* d_resident_out, void* stream);
 
 /* Free pages in the pool and the device error word (synchronises). */
 int kvc_device_status(kvc_ctx* ctx, int64_t* h_free_pages, int32_t* h_error_bits);

@@ -16,6 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libkvc.so")
 
 KVC_F32, KVC_BF16 = 0, 1
+KVC_KV4 = 0x10
 KVC_ACOUSTIC, KVC_ASR_DELIM, KVC_TRANSCRIPT, KVC_TEXT = 0, 1, 2, 3
 KVC_UNIT_BEGIN = 0x80
 KVC_POLICY_UNIT, KVC_POLICY_POSITION, KVC_POLICY_SINK_RECENT = 0, 1, 2
@@ -30,7 +31,8 @@ EXPORTED = ["kvc_query_sizes", "kvc_create", "kvc_destroy", "kvc_append_chunk",
             "kvc_attn_decode_kv",
             "kvc_attn_decode_noalloc",
             "kvc_resident_size", "kvc_release",
-            "kvc_export_state", "kvc_export_kv", "kvc_export_transcript", "kvc_device_status",
+            "kvc_export_state", "kvc_export_kv", "kvc_export_transcript", "kvc_read_kv",
+            "kvc_device_status",
             "kvc_last_error"]
 
 
@@ -91,6 +93,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                                      p_i32, ctypes.POINTER(ctypes.c_uint8), p_i32, i64]
     lib.kvc_export_kv.argtypes = [vp, ctypes.c_int, ctypes.c_int, vp, vp, i64]
     lib.kvc_export_transcript.argtypes = [vp, ctypes.c_int, i64, vp, vp, vp, vp, vp]
+    lib.kvc_read_kv.argtypes = [vp, ctypes.c_int, p_i32, p_i32, p_i32, ctypes.c_int, ctypes.c_int,
+                                vp, vp, vp, vp]
     lib.kvc_device_status.argtypes = [vp, ctypes.POINTER(i64), ctypes.POINTER(i32)]
     lib.kvc_last_error.restype = ctypes.c_char_p
     for name in EXPORTED:
@@ -151,11 +155,15 @@ class KVCache:
                  max_pages_per_session: int, max_positions: int, max_seq_per_call: int,
                  max_tokens_per_call: int, page_size: int = 16, rope_base: float = 10000.0,
                  policy: str = "unit", sink: int = 0, recent: int = 0,
-                 device: str = "cuda", stream=None):
+                 device: str = "cuda", stream=None, kv_bits: int | None = None):
+        """kv_bits: None holds K and V in `dtype`, 4 in 4 bits (KVC_KV4)."""
         import torch
+        if kv_bits not in (None, 4):
+            raise ValueError(f"kv_bits must be None or 4, not {kv_bits!r}")
         self.lib = load_library()
         self.cfg = Config(n_sessions, layers, q_heads, kv_heads, head_dim, page_size, budget,
-                          window, KVC_BF16 if dtype == "bf16" else KVC_F32, rope_base, n_pages,
+                          window, (KVC_BF16 if dtype == "bf16" else KVC_F32) |
+                          (KVC_KV4 if kv_bits == 4 else 0), rope_base, n_pages,
                           max_pages_per_session, max_positions, max_seq_per_call,
                           max_tokens_per_call, POLICIES[policy], sink, recent)
         self.dtype = dtype
@@ -240,6 +248,39 @@ class KVCache:
     def attn_decode(self, layer: int, q, out, stream=None) -> None:
         _check(self.lib.kvc_attn_decode(self.ctx, layer, q.data_ptr(), out.data_ptr(),
                                         _stream(stream)))
+
+    def read_kv(self, sessions, first, cu_rows, layer0: int = 0, n_layers: int | None = None,
+                k=None, v=None, resident_out=None, stream=None):
+        """Retained rows of the listed sessions, from retained position first[i] on, in the
+        element type: device tensors K and V [n_layers][cu_rows[-1]][Hkv][D] (made here unless
+        given), filled asynchronously on the stream."""
+        import torch
+        s, f, cu = _i32(sessions), _i32(first), _i32(cu_rows)
+        if len(f) != len(s) or len(cu) != len(s) + 1:
+            raise ValueError("first needs an entry per session, cu_rows one more")
+        n = self.cfg.layers - layer0 if n_layers is None else n_layers
+        if n < 1 or not 0 <= layer0 <= self.cfg.layers - n:
+            raise ValueError(f"layers {layer0}..{layer0 + n - 1} outside 0..{self.cfg.layers - 1}")
+        shape = (n, max(0, int(cu[-1])), self.cfg.kv_heads, self.cfg.head_dim)
+        if k is None:
+            k = torch.empty(shape, dtype=self.torch_dtype, device=self.pool.device)
+        if v is None:
+            v = torch.empty(shape, dtype=self.torch_dtype, device=self.pool.device)
+        for x in (k, v):
+            if x.shape != shape or x.dtype != self.torch_dtype or not x.is_contiguous():
+                raise ValueError(f"k and v must be contiguous {self.torch_dtype} of shape {shape}")
+        _check(self.lib.kvc_read_kv(self.ctx, len(s), _ptr_i32(s), _ptr_i32(f), _ptr_i32(cu),
+                                    layer0, n, k.data_ptr(), v.data_ptr(),
+                                    None if resident_out is None else resident_out.data_ptr(),
+                                    _stream(stream)))
+        return k, v
+
+    def read_kv_raw(self, n_seq, sess_p, first_p, cu_p, layer0, n_layers, k_ptr, v_ptr,
+                    resident_ptr, stream) -> None:
+        rc = self.lib.kvc_read_kv(self.ctx, n_seq, sess_p, first_p, cu_p, layer0, n_layers, k_ptr,
+                                  v_ptr, resident_ptr, stream)
+        if rc:
+            _check(rc)
 
     def release(self, sessions, stream=None) -> None:
         s = _i32(sessions)

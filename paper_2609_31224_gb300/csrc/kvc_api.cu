@@ -7,7 +7,10 @@
 #include <string>
 #include <vector>
 
+#include <cuda_fp16.h>
+
 #include "kvc_estimate.h"
+#include "kvc_kv4.h"
 #include "kvc_launch.cuh"
 #include "kvc_order.h"
 
@@ -36,6 +39,9 @@ int fail(int code, const char* fmt, ...) {
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+int element_type(const kvc_config& c) { return c.dtype & ~KVC_KV4; }
+bool holds_4_bits(const kvc_config& c) { return (c.dtype & KVC_KV4) != 0; }
+
 struct Sizes {
   int max_moves, max_alloc, dec_slots, dec_tag_slots, pf_slots;
 };
@@ -48,9 +54,10 @@ Sizes derive_sizes(const kvc_config& c) {
   // Decode partial slots: two per CTA of the stream-K split (grid <= 2048 CTAs).
   s.dec_slots = 4096;
   // Tagged partial slots of the pair-split decode (one per CTA of its one-wave grid).
-  s.dec_tag_slots = 2048;
+  s.dec_tag_slots = c.dtype & KVC_KV4 ? 0 : 2048;
   // Prefill partial slots: two per CTA of the bfloat16 kernel's stream-K split.
-  s.pf_slots = c.dtype == KVC_BF16 ? 512 : 0;
+  // (Of both kernels over 4-bit rows too, as many as fit in the same bytes.)
+  s.pf_slots = c.dtype == KVC_F32 ? 0 : 512;
   return s;
 }
 
@@ -130,8 +137,11 @@ int check_config(const kvc_config* c) {
   if (c->q_heads != 4 * c->kv_heads)
     return fail(KVC_EINVAL, "q_heads must be 4 * kv_heads (GQA group of 4)");
   if (c->page_size != PS) return fail(KVC_EINVAL, "page_size must be 16");
-  if (!((c->dtype == KVC_BF16 && c->head_dim == 128) || (c->dtype == KVC_F32 && c->head_dim == 64)))
-    return fail(KVC_EINVAL, "supported (dtype, head_dim): (KVC_BF16, 128), (KVC_F32, 64)");
+  const int type = element_type(*c);
+  if (!((type == KVC_BF16 && c->head_dim == 128) || (type == KVC_F32 && c->head_dim == 64)))
+    return fail(KVC_EINVAL,
+                "supported (dtype, head_dim): (KVC_BF16, 128), (KVC_F32, 64), each with or without "
+                "KVC_KV4");
   if (c->window < 0) return fail(KVC_EINVAL, "window must be >= 0");
   if (c->policy < KVC_POLICY_UNIT || c->policy > KVC_POLICY_SINK_RECENT)
     return fail(KVC_EINVAL, "policy must be one of KVC_POLICY_UNIT, _POSITION, _SINK_RECENT");
@@ -139,8 +149,11 @@ int check_config(const kvc_config* c) {
     return fail(KVC_EINVAL, "sink and recent must be >= 0");
   if (!(c->rope_base > 0.0)) return fail(KVC_EINVAL, "rope_base must be > 0");
   if (c->n_pages < 1) return fail(KVC_EINVAL, "n_pages must be >= 1");
-  const int64_t rows = c->n_pages * c->layers * 2 * c->kv_heads * PS;
-  if (rows >= (1LL << 31)) return fail(KVC_EINVAL, "pool too large for 32-bit row coordinates");
+  // Tensor copies count rows of all pages in 32 bits; 4-bit rows are found by 64-bit offsets, and
+  // slots of a page and position in 32 bits remain.
+  const int64_t rows_per_slot = holds_4_bits(*c) ? 1 : c->layers * 2 * c->kv_heads;
+  if (c->n_pages >= (1LL << 31) || c->n_pages * PS * rows_per_slot >= (1LL << 31))
+    return fail(KVC_EINVAL, "pool too large for 32-bit row coordinates");
   if (c->max_pages_per_session < 1) return fail(KVC_EINVAL, "max_pages_per_session must be >= 1");
   if (c->max_positions < 1 || c->max_positions > (1 << 24))
     return fail(KVC_EINVAL, "max_positions must be in 1..2^24");
@@ -158,6 +171,7 @@ int check_config(const kvc_config* c) {
 struct kvc_ctx {
   kvc_config cfg;
   Dev d;
+  bool kv4 = false;  // rows held in 4 bits
   // Host mirrors.
   std::vector<int32_t> tail_mod;  // (live_head + n_live) % PS, exact
   std::vector<int32_t> pos_next;  // exact
@@ -261,6 +275,30 @@ void enqueue_readback(kvc_ctx* ctx, cudaStream_t s) {
   ctx->delta_since_readback = 0;
 }
 
+// One layer's K/V of the last append, in a launch of their own.
+cudaError_t write_layer(kvc_ctx* ctx, int layer, const void* k, const void* v, cudaStream_t s) {
+  return ctx->kv4 ? launch_append_layers_kv4(ctx->d, ctx->last_total, layer, 1, k, v, false, s)
+                  : launch_append_layers(ctx->d, ctx->last_total, layer, 1, k, v, false, s);
+}
+
+// A row of a host copy of a tile of 4-bit rows, in the element type (esz bytes each).
+void row_back(const uint8_t* tile, int D, int kv, int slot, int esz, uint8_t* out) {
+  for (int dim = 0; dim < D; ++dim) {
+    const int at = (kv ? kv4::v_codes(D, slot, dim & ~7) : kv4::k_codes(D, slot, dim & ~7)) + dim % 8 / 2;
+    const int sc = kv ? kv4::v_scale(D, slot, dim / kv4::GROUP) : kv4::k_scale(D, slot, dim / kv4::GROUP);
+    __half_raw m;
+    memcpy(&m.x, tile + sc, 2);
+    const int code = (tile[at] >> (4 * (dim & 1)) & 15) - 8;
+    const float x = (float)code * (__half2float(__half(m)) * 16.f);
+    if (esz == 4) {
+      memcpy(out + 4 * dim, &x, 4);
+    } else {
+      const __nv_bfloat16_raw b = __float2bfloat16_rn(x);
+      memcpy(out + 2 * dim, &b.x, 2);
+    }
+  }
+}
+
 int sync_and_check(kvc_ctx* ctx) {
   KVC_CUDA(cudaDeviceSynchronize());
   int32_t err = 0;
@@ -278,9 +316,12 @@ const char* kvc_last_error(void) { return g_err.c_str(); }
 int kvc_query_sizes(const kvc_config* cfg, size_t* pool_bytes, size_t* meta_bytes) {
   int rc = check_config(cfg);
   if (rc) return rc;
-  const size_t esz = cfg->dtype == KVC_BF16 ? 2 : 4;
+  const size_t esz = element_type(*cfg) == KVC_BF16 ? 2 : 4;
   if (pool_bytes)
-    *pool_bytes = (size_t)cfg->n_pages * cfg->layers * 2 * cfg->kv_heads * PS * cfg->head_dim * esz;
+    *pool_bytes = (size_t)cfg->n_pages *
+                  (holds_4_bits(*cfg)
+                       ? kv4::page_bytes(cfg->head_dim, cfg->layers, cfg->kv_heads)
+                       : (size_t)cfg->layers * 2 * cfg->kv_heads * PS * cfg->head_dim * esz);
   if (meta_bytes) *meta_bytes = layout_meta(*cfg, nullptr, nullptr);
   return KVC_OK;
 }
@@ -312,7 +353,8 @@ int kvc_create(kvc_ctx** out, const kvc_config* cfg, void* d_pool, size_t pool_b
   d.kv_heads = cfg->kv_heads;
   d.head_dim = cfg->head_dim;
   d.group = cfg->q_heads / cfg->kv_heads;
-  d.esz = cfg->dtype == KVC_BF16 ? 2 : 4;
+  d.esz = element_type(*cfg) == KVC_BF16 ? 2 : 4;
+  ctx->kv4 = holds_4_bits(*cfg);
   d.max_pages_per_session = cfg->max_pages_per_session;
   d.max_positions = cfg->max_positions;
   d.max_seq = cfg->max_seq_per_call;
@@ -405,7 +447,7 @@ int kvc_append_chunk(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, const i
   for (int i = 0; i < n_seq; ++i) a.sessions[i] = h_sessions[i];
   for (int i = 0; i <= n_seq; ++i) a.cu[i] = h_cu_tokens[i];
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  KVC_CUDA(launch_append(ctx->d, a, d_types, d_k, d_v, single, s));
+  KVC_CUDA(launch_append(ctx->d, ctx->kv4, a, d_types, d_k, d_v, single, s));
   for (int i = 0; i < n_seq; ++i) {
     const int sid = h_sessions[i];
     const int t = h_cu_tokens[i + 1] - h_cu_tokens[i];
@@ -440,8 +482,7 @@ int kvc_append_kv_layer(kvc_ctx* ctx, int layer, const void* d_k, const void* d_
   if (!aligned16(d_k) || !aligned16(d_v)) return fail(KVC_EINVAL, "d_k / d_v must be 16-byte aligned");
   if (!ctx->attn_valid)
     return fail(KVC_ESTATE, "kvc_append_kv_layer needs a preceding kvc_append_chunk (no evict/release after it)");
-  KVC_CUDA(launch_append_layers(ctx->d, ctx->last_total, layer, 1, d_k, d_v, false,
-                                static_cast<cudaStream_t>(stream)));
+  KVC_CUDA(write_layer(ctx, layer, d_k, d_v, static_cast<cudaStream_t>(stream)));
   // The next attention launch must not read early: its prologue loads pages
   // this write may still be filling.
   ctx->order.layer_write(layer);
@@ -458,7 +499,7 @@ int kvc_evict(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, int64_t* d_res
   a.n_seq = n_seq;
   for (int i = 0; i < n_seq; ++i) a.sessions[i] = h_sessions[i];
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  KVC_CUDA(launch_evict(ctx->d, a, d_resident_out, ctx->h_readback, ctx->lim.sms, s));
+  KVC_CUDA(launch_evict(ctx->d, ctx->kv4, a, d_resident_out, ctx->h_readback, ctx->lim.sms, s));
   for (int i = 0; i < n_seq; ++i) ctx->resident[h_sessions[i]].evict(ctx->cfg);
   ctx->used_ub += n_seq;  // an evict adds at most one page per session, net
   ctx->delta_since_readback += n_seq;
@@ -508,6 +549,11 @@ int kvc_attn_decode(kvc_ctx* ctx, int layer, const void* d_q, void* d_out, void*
   if (rc) return rc;
   if (!ctx->last_single)
     return fail(KVC_ESTATE, "decode needs exactly one appended token per session");
+  if (ctx->kv4) {
+    KVC_CUDA(launch_attn_kv4(ctx->d, ctx->lim, &ctx->order, layer, nullptr, nullptr, d_q, d_out,
+                             ctx->last_total, ctx->last_max_t, static_cast<cudaStream_t>(stream)));
+    return KVC_OK;
+  }
   bool capturing = false;
   KVC_CUDA(is_capturing(static_cast<cudaStream_t>(stream), &capturing));
   uint32_t epoch = 0;
@@ -528,6 +574,11 @@ int kvc_attn_decode_kv(kvc_ctx* ctx, int layer, const void* d_k, const void* d_v
   if (!aligned16(d_k) || !aligned16(d_v)) return fail(KVC_EINVAL, "d_k / d_v must be 16-byte aligned");
   if (!ctx->last_single)
     return fail(KVC_ESTATE, "decode needs exactly one appended token per session");
+  if (ctx->kv4) {
+    KVC_CUDA(launch_attn_kv4(ctx->d, ctx->lim, &ctx->order, layer, d_k, d_v, d_q, d_out,
+                             ctx->last_total, ctx->last_max_t, static_cast<cudaStream_t>(stream)));
+    return KVC_OK;
+  }
   // (An early launch may load the page while a launch before it writes the new row's slot:
   // the row goes into the tile after its load.)
   bool capturing = false;
@@ -548,6 +599,8 @@ int kvc_attn_decode_noalloc(kvc_ctx* ctx, int layer, const void* d_q, void* d_ou
   if (rc) return rc;
   if (!ctx->last_single)
     return fail(KVC_ESTATE, "decode needs exactly one appended token per session");
+  if (ctx->kv4)
+    return fail(KVC_EINVAL, "kvc_attn_decode_noalloc does not take rows held in 4 bits (KVC_KV4)");
   const int pairs = ctx->last_n_seq * ctx->cfg.kv_heads;
   if (pairs > noalloc_max_pairs())
     return fail(KVC_EINVAL,
@@ -566,6 +619,11 @@ int kvc_attn_prefill_chunk(kvc_ctx* ctx, int layer, const void* d_q, void* d_out
   if (ctx->last_max_t > PF_MAX_TOKENS)
     return fail(KVC_EINVAL, "prefill chunks are limited to %d tokens per session", PF_MAX_TOKENS);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (ctx->kv4) {
+    KVC_CUDA(launch_attn_kv4(ctx->d, ctx->lim, &ctx->order, layer, nullptr, nullptr, d_q, d_out,
+                             ctx->last_total, ctx->last_max_t, s));
+    return KVC_OK;
+  }
   bool capturing = false;
   KVC_CUDA(is_capturing(s, &capturing));
   const PageHint pages = page_hint(ctx, capturing);
@@ -586,6 +644,11 @@ int kvc_attn_prefill_chunk_kv(kvc_ctx* ctx, int layer, const void* d_k, const vo
   if (ctx->last_max_t > PF_MAX_TOKENS)
     return fail(KVC_EINVAL, "prefill chunks are limited to %d tokens per session", PF_MAX_TOKENS);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (ctx->kv4) {
+    KVC_CUDA(launch_attn_kv4(ctx->d, ctx->lim, &ctx->order, layer, d_k, d_v, d_q, d_out,
+                             ctx->last_total, ctx->last_max_t, s));
+    return KVC_OK;
+  }
   bool capturing = false;
   KVC_CUDA(is_capturing(s, &capturing));
   const PageHint pages = page_hint(ctx, capturing);
@@ -696,8 +759,43 @@ int kvc_export_transcript(kvc_ctx* ctx, int session, int64_t cap, int32_t* d_pos
     return fail(KVC_EINVAL, "output buffers are NULL");
   if (cap > 0 && (!aligned16(d_k_out) || !aligned16(d_v_out)))
     return fail(KVC_EINVAL, "d_k_out / d_v_out must be 16-byte aligned");
-  KVC_CUDA(launch_transcript(ctx->d, session, (int)cap, d_pos_out, d_k_out, d_v_out, d_count,
+  KVC_CUDA(launch_transcript(ctx->d, ctx->kv4, session, (int)cap, d_pos_out, d_k_out, d_v_out, d_count,
                              static_cast<cudaStream_t>(stream)));
+  return KVC_OK;
+}
+
+int kvc_read_kv(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, const int32_t* h_first,
+                const int32_t* h_cu_rows, int layer0, int n_layers, void* d_k_out, void* d_v_out,
+                int64_t* d_resident_out, void* stream) {
+  g_err.clear();
+  if (!ctx) return fail(KVC_EINVAL, "ctx is NULL");
+  int rc = check_sessions(ctx, n_seq, h_sessions);
+  if (rc) return rc;
+  if (!h_first || !h_cu_rows) return fail(KVC_EINVAL, "h_first / h_cu_rows is NULL");
+  if (n_layers < 1 || layer0 < 0 || layer0 > ctx->cfg.layers - n_layers)
+    return fail(KVC_EINVAL, "layers %d..%d + %d outside 0..%d", layer0, layer0, n_layers,
+                ctx->cfg.layers - 1);
+  if (h_cu_rows[0] != 0) return fail(KVC_EINVAL, "h_cu_rows[0] must be 0");
+  for (int i = 0; i < n_seq; ++i) {
+    if (h_first[i] < 0) return fail(KVC_EINVAL, "h_first[%d] = %d is negative", i, h_first[i]);
+    if (h_cu_rows[i + 1] < h_cu_rows[i])
+      return fail(KVC_EINVAL, "h_cu_rows decreases at %d", i);
+  }
+  const int total = h_cu_rows[n_seq];
+  if (total > 0 && (!d_k_out || !d_v_out)) return fail(KVC_EINVAL, "output buffers are NULL");
+  if (total > 0 && (!aligned16(d_k_out) || !aligned16(d_v_out)))
+    return fail(KVC_EINVAL, "d_k_out / d_v_out must be 16-byte aligned");
+  if (total == 0 && !d_resident_out) return KVC_OK;
+  ReadArgs a;
+  a.n_seq = n_seq;
+  a.total = total;
+  for (int i = 0; i < n_seq; ++i) {
+    a.sessions[i] = h_sessions[i];
+    a.first[i] = h_first[i];
+  }
+  for (int i = 0; i <= n_seq; ++i) a.cu[i] = h_cu_rows[i];
+  KVC_CUDA(launch_read_kv(ctx->d, ctx->kv4, a, layer0, n_layers, d_k_out, d_v_out, d_resident_out,
+                          ctx->lim.sms, static_cast<cudaStream_t>(stream)));
   return KVC_OK;
 }
 
@@ -721,6 +819,30 @@ int kvc_export_kv(kvc_ctx* ctx, int session, int layer, void* h_k, void* h_v, in
   if (st.n_live_pages)
     KVC_CUDA(cudaMemcpy(lp.data(), d.live_pt + row, lp.size() * 4, cudaMemcpyDeviceToHost));
   const size_t vec = (size_t)d.head_dim * d.esz;              // one head row
+  if (ctx->kv4) {
+    const size_t tile = kv4::tile_bytes(d.head_dim);
+    std::vector<uint8_t> page(2 * d.kv_heads * tile);         // one page-layer
+    int i = 0;
+    auto emit = [&](int p, int s_lo, int s_hi) -> int {
+      KVC_CUDA(cudaMemcpy(page.data(),
+                          d.pool + kv4::tile_at(d.head_dim, d.layers, d.kv_heads, p, layer, 0, 0),
+                          page.size(), cudaMemcpyDeviceToHost));
+      for (int s = s_lo; s < s_hi; ++s, ++i)
+        for (int h = 0; h < d.kv_heads; ++h)
+          for (int kv = 0; kv < 2; ++kv)
+            row_back(page.data() + (2 * h + kv) * tile, d.head_dim, kv, s, d.esz,
+                     static_cast<uint8_t*>(kv ? h_v : h_k) + ((size_t)i * d.kv_heads + h) * vec);
+      return KVC_OK;
+    };
+    for (int b = 0; b < st.n_hist_pages; ++b)
+      if ((rc = emit(hp[b], 0, std::min(PS, st.n_hist - b * PS)))) return rc;
+    for (int b = 0; b < st.n_live_pages; ++b) {
+      const int lo = std::max(0, st.live_head - b * PS);
+      const int hi = std::min(PS, st.live_head + st.n_live - b * PS);
+      if (hi > lo && (rc = emit(lp[b], lo, hi))) return rc;
+    }
+    return KVC_OK;
+  }
   const size_t blk = (size_t)d.kv_heads * PS * vec;           // K (or V) of one page-layer
   std::vector<uint8_t> kb(blk), vb(blk);
   uint8_t* ko = static_cast<uint8_t*>(h_k);

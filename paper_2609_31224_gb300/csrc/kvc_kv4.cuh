@@ -1,0 +1,89 @@
+// Device code shared by the kernels on 4-bit rows (kvc_kv4.h): a group's scale and codes, the
+// rotation of a key that is held in 4 bits, and a row's chunk back from its bytes.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "kvc_kv4.h"
+#include "kvc_launch.cuh"
+#include "kvc_rope.cuh"
+
+namespace kvc {
+
+namespace kv4 {
+
+// Bits of |x|: they order as the numbers do, infinities above them and NaN on top.
+__device__ inline uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+// The scale of a group whose largest |x| has these bits.
+__device__ inline float scale_of(uint32_t most) {
+  if (most >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
+  const float s = __fdiv_rn(__uint_as_float(most), (float)CODE_MAX);
+  // Multiples of 2^e: the seventh significant bit of s, 2^-20 at the finest.
+  const int e = max((int)(__float_as_uint(s) >> 23) - 127 - (SCALE_BITS - 1), SCALE_FINEST_EXP);
+  const float step = __uint_as_float((uint32_t)(127 + e) << 23);
+  const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+  return fminf(rintf(s * inv) * step, SCALE_MAX);
+}
+__device__ inline __half stored_scale(float s) { return __float2half_rn(s * 0.0625f); }
+
+// Nibbles of 8 elements of a group of scale s (rounded to nearest, ties to even, of the quotient).
+__device__ inline uint32_t codes_of(const float (&x)[8], float s) {
+  const float by = s > 0.f ? s : 1.f;
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int c = max(-CODE_MAX, min(CODE_MAX, __float2int_rn(__fdiv_rn(x[i], by))));
+    w |= (uint32_t)(c + 8) << (4 * i);
+  }
+  return w;
+}
+
+// Rotate-half of one pair, every product and sum rounded (rope_pair fuses one of each): codes
+// next to a rounding boundary depend on the last bit.
+__device__ inline void turn_pair(float x1, float x2, float2 c, float& y1, float& y2) {
+  y1 = __fsub_rn(__fmul_rn(x1, c.x), __fmul_rn(x2, c.y));
+  y2 = __fadd_rn(__fmul_rn(x2, c.x), __fmul_rn(x1, c.y));
+}
+
+// 8 elements of T as binary32 and back.
+template <typename T>
+struct Eight;
+template <>
+struct Eight<__nv_bfloat16> {
+  uint4 w;
+  __device__ void load(const __nv_bfloat16* p) { w = __ldcs(reinterpret_cast<const uint4*>(p)); }
+  __device__ void get(float (&f)[8]) const { Chunk16<__nv_bfloat16>::unpack(w, f); }
+  __device__ static void store(__nv_bfloat16* p, const float (&f)[8]) {
+    *reinterpret_cast<uint4*>(p) = Chunk16<__nv_bfloat16>::pack(f);
+  }
+};
+template <>
+struct Eight<float> {
+  uint4 a, b;
+  __device__ void load(const float* p) {
+    a = __ldcs(reinterpret_cast<const uint4*>(p));
+    b = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+  }
+  __device__ void get(float (&f)[8]) const {
+    f[0] = __uint_as_float(a.x); f[1] = __uint_as_float(a.y);
+    f[2] = __uint_as_float(a.z); f[3] = __uint_as_float(a.w);
+    f[4] = __uint_as_float(b.x); f[5] = __uint_as_float(b.y);
+    f[6] = __uint_as_float(b.z); f[7] = __uint_as_float(b.w);
+  }
+  __device__ static void store(float* p, const float (&f)[8]) {
+    *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    *(reinterpret_cast<float4*>(p) + 1) = make_float4(f[4], f[5], f[6], f[7]);
+  }
+};
+
+// Values of 8 nibbles of a group whose stored scale is m.
+__device__ inline void values_of(uint32_t w, __half m, float (&f)[8]) {
+  const float s = __half2float(m) * 16.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = (float)((int)(w >> (4 * i) & 15u) - 8) * s;
+}
+
+}  // namespace kv4
+
+}  // namespace kvc

@@ -4,6 +4,7 @@
 
 #include "kvc_decode_slices.h"
 #include "kvc_internal.cuh"
+#include "kvc_order.h"
 
 namespace kvc {
 
@@ -29,10 +30,23 @@ struct SeqArgsT {
 };
 using SeqArgs = SeqArgsT<MAX_SEQ>;
 
+// Rows to read back: rows [cu[i], cu[i + 1]) of the outputs are session i's retained positions from
+// first[i] on.
+template <int N>
+struct ReadArgsT {
+  int32_t n_seq;
+  int32_t total;
+  int32_t sessions[N];
+  int32_t first[N];
+  int32_t cu[N + 1];
+};
+using ReadArgs = ReadArgsT<MAX_SEQ>;
+
 // What the device runs at once, for each kernel whose launch shape follows from it.  kvc_create
 // looks it up for the current CUDA context; the first time for a context and element type (about
 // 3 ms) that also sets the kernels' attributes, which belong to the CUDA context too.
 constexpr int PF_MAX_SLICES = 8;  // CTAs of a bfloat16 prefill cluster, at most
+constexpr int KV4_PF_WARPS = 6;   // warps that share a page in the prefill over 4-bit rows, at most
 struct Limits {
   int sms;                         // SMs
   int dec_stream_k;                // CTAs of the stream-K decode's grid
@@ -40,6 +54,8 @@ struct Limits {
   int pf_stream_k;                 // CTAs of the stream-K prefill (bfloat16)
   int pf_clusters[PF_MAX_SLICES + 1];  // [k] clusters of k CTAs of the prefill's pair split
   int f32_cluster[2][2];           // largest cluster of the binary32 prefill: [rows][spread]
+  int kv4_decode;                  // CTAs of the decode over 4-bit rows
+  int kv4_prefill[KV4_PF_WARPS + 1];  // [w] CTAs of the prefill with w warps to a page
 };
 cudaError_t query_limits(const Dev& d, Limits* lim);
 // Id of the current CUDA context (never reused: a context that replaces a destroyed one at the
@@ -49,16 +65,34 @@ cudaError_t current_context_id(unsigned long long* id);
 cudaError_t launch_init(const Dev& d, double rope_base, cudaStream_t s);
 // single: every session of the call gets exactly one token (one session: plan and K/V write in
 // one launch).
-cudaError_t launch_append(const Dev& d, const AppendArgs& a, const uint8_t* types, const void* k,
-                          const void* v, bool single, cudaStream_t s);
+// kv4: the rows are held in 4 bits.
+cudaError_t launch_append(const Dev& d, bool kv4, const AppendArgs& a, const uint8_t* types,
+                          const void* k, const void* v, bool single, cudaStream_t s);
 // after_plan: launched right behind the plan kernel of the same append.
 cudaError_t launch_append_layers(const Dev& d, int total, int layer0, int n_layers, const void* k,
                                  const void* v, bool after_plan, cudaStream_t s);
-cudaError_t launch_evict(const Dev& d, const SeqArgs& a, int64_t* resident_out, int64_t* used_out,
-                         int sms, cudaStream_t s);
+cudaError_t launch_evict(const Dev& d, bool kv4, const SeqArgs& a, int64_t* resident_out,
+                         int64_t* used_out, int sms, cudaStream_t s);
 cudaError_t launch_release(const Dev& d, const SeqArgs& a, int64_t* used_out, cudaStream_t s);
-cudaError_t launch_transcript(const Dev& d, int session, int cap, int32_t* pos_out, void* k_out,
-                              void* v_out, int32_t* count, cudaStream_t s);
+cudaError_t launch_transcript(const Dev& d, bool kv4, int session, int cap, int32_t* pos_out,
+                              void* k_out, void* v_out, int32_t* count, cudaStream_t s);
+cudaError_t launch_read_kv(const Dev& d, bool kv4, const ReadArgs& a, int layer0, int n_layers,
+                           void* k_out, void* v_out, int64_t* resident_out, int sms,
+                           cudaStream_t s);
+// The parts of those calls that touch 4-bit rows (kvc_kv4_rows.cu), and the attention over them
+// (kvc_kv4_attn.cu): chunks of up to max_t tokens.
+cudaError_t launch_append_layers_kv4(const Dev& d, int total, int layer0, int n_layers,
+                                     const void* k, const void* v, bool after_plan,
+                                     cudaStream_t s);
+cudaError_t launch_evict_copy_kv4(const Dev& d, int sms, cudaStream_t s);
+cudaError_t launch_transcript_copy_kv4(const Dev& d, int cap, void* k_out, void* v_out, int sms,
+                                       cudaStream_t s);
+cudaError_t kv4_limits(int esz, Limits* lim);  // sets its attributes
+// new_k / new_v (optional): the layer's rows of the append, written first.  Asks `order` when it may
+// read early, and reports its launches to it.
+cudaError_t launch_attn_kv4(const Dev& d, const Limits& lim, LaunchOrder* order, int layer,
+                            const void* new_k, const void* new_v, const void* q, void* out,
+                            int total, int max_t, cudaStream_t s);
 // Attention launches may start while the kernel before them in the stream finishes.  early:
 // they may also read what the append wrote before that (an attention launch of the same
 // append came before, so the append is complete).

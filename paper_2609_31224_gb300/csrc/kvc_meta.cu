@@ -1128,13 +1128,13 @@ cudaError_t launch_init(const Dev& d, double rope_base, cudaStream_t s) {
 // Every kernel below may start while the one before it in the stream finishes (it waits for
 // that one before it reads anything but the caller's inputs), so that a chain of short
 // kernels does not pay a full launch each.
-cudaError_t launch_append(const Dev& d, const AppendArgs& a, const uint8_t* types, const void* k,
-                          const void* v, bool single, cudaStream_t s) {
+cudaError_t launch_append(const Dev& d, bool kv4, const AppendArgs& a, const uint8_t* types,
+                          const void* k, const void* v, bool single, cudaStream_t s) {
   cudaError_t e;
   if (single && a.n_seq <= FEW) {
     // One CTA writes the K/V rows only for a one-session call (a few hundred KiB at
     // most); larger calls spread the rows over append_kv_kernel's grid.
-    const bool fuse_kv = a.n_seq == 1 && k != nullptr;
+    const bool fuse_kv = a.n_seq == 1 && k != nullptr && !kv4;
     const dim3 block(fuse_kv ? META_THREADS : 32);
     SeqArgsT<FEW> few;
     few.n_seq = a.n_seq;
@@ -1161,7 +1161,8 @@ cudaError_t launch_append(const Dev& d, const AppendArgs& a, const uint8_t* type
     e = launch_ex(&append_plan_kernel<MAX_SEQ>, dim3(1), dim3(META_THREADS), 0, s, true, d, a, types);
   }
   if (e != cudaSuccess || k == nullptr) return e;  // plan only: layers follow one by one
-  return launch_append_layers(d, a.total, 0, d.layers, k, v, true, s);
+  return kv4 ? launch_append_layers_kv4(d, a.total, 0, d.layers, k, v, true, s)
+             : launch_append_layers(d, a.total, 0, d.layers, k, v, true, s);
 }
 
 cudaError_t launch_append_layers(const Dev& d, int total, int layer0, int n_layers, const void* k,
@@ -1178,8 +1179,8 @@ cudaError_t launch_append_layers(const Dev& d, int total, int layer0, int n_laye
 }
 
 // used_out: the pages in use afterwards are written there (pinned host memory).
-cudaError_t launch_evict(const Dev& d, const SeqArgs& a, int64_t* resident_out, int64_t* used_out,
-                         int sms, cudaStream_t s) {
+cudaError_t launch_evict(const Dev& d, bool kv4, const SeqArgs& a, int64_t* resident_out,
+                         int64_t* used_out, int sms, cudaStream_t s) {
   cudaError_t e;
   if (a.n_seq <= FEW) {
     SeqArgsT<FEW> few;
@@ -1192,17 +1193,19 @@ cudaError_t launch_evict(const Dev& d, const SeqArgs& a, int64_t* resident_out, 
                   resident_out, used_out);
   }
   if (e != cudaSuccess) return e;
+  if (kv4) return launch_evict_copy_kv4(d, sms, s);
   return launch_ex(&evict_copy_kernel, dim3(sms * 4), dim3(256), 0, s, true, d);
 }
 
-cudaError_t launch_transcript(const Dev& d, int session, int cap, int32_t* pos_out, void* k_out,
-                              void* v_out, int32_t* count, cudaStream_t s) {
+cudaError_t launch_transcript(const Dev& d, bool kv4, int session, int cap, int32_t* pos_out,
+                              void* k_out, void* v_out, int32_t* count, cudaStream_t s) {
   cudaError_t e = launch_ex(&transcript_gather_kernel, dim3(1), dim3(META_THREADS), 0, s, true, d,
                             session, cap, pos_out, count);
   if (e != cudaSuccess) return e;
   int dev = 0, sms = 0;
   cudaGetDevice(&dev);
   cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (kv4) return launch_transcript_copy_kv4(d, cap, k_out, v_out, sms, s);
   return launch_ex(&transcript_copy_kernel, dim3(sms * 4), dim3(256), 0, s, true, d, cap,
                    static_cast<uint8_t*>(k_out), static_cast<uint8_t*>(v_out));
 }
