@@ -281,6 +281,17 @@ cudaError_t write_layer(kvc_ctx* ctx, int layer, const void* k, const void* v, c
                   : launch_append_layers(ctx->d, ctx->last_total, layer, 1, k, v, false, s);
 }
 
+// Attention of the last append's queries over rows held in 4 bits.
+int attend_kv4(kvc_ctx* ctx, int layer, const void* k, const void* v, const void* q, void* out,
+               void* stream) {
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  bool capturing = false;
+  KVC_CUDA(is_capturing(s, &capturing));
+  KVC_CUDA(launch_attn_kv4(ctx->d, ctx->lim, &ctx->order, layer, k, v, q, out, ctx->last_total,
+                           ctx->last_max_t, page_hint(ctx, capturing).sum * ctx->cfg.kv_heads, s));
+  return KVC_OK;
+}
+
 // A row of a host copy of a tile of 4-bit rows, in the element type (esz bytes each).
 void row_back(const uint8_t* tile, int D, int kv, int slot, int esz, uint8_t* out) {
   for (int dim = 0; dim < D; ++dim) {
@@ -549,11 +560,7 @@ int kvc_attn_decode(kvc_ctx* ctx, int layer, const void* d_q, void* d_out, void*
   if (rc) return rc;
   if (!ctx->last_single)
     return fail(KVC_ESTATE, "decode needs exactly one appended token per session");
-  if (ctx->kv4) {
-    KVC_CUDA(launch_attn_kv4(ctx->d, ctx->lim, &ctx->order, layer, nullptr, nullptr, d_q, d_out,
-                             ctx->last_total, ctx->last_max_t, static_cast<cudaStream_t>(stream)));
-    return KVC_OK;
-  }
+  if (ctx->kv4) return attend_kv4(ctx, layer, nullptr, nullptr, d_q, d_out, stream);
   bool capturing = false;
   KVC_CUDA(is_capturing(static_cast<cudaStream_t>(stream), &capturing));
   uint32_t epoch = 0;
@@ -574,11 +581,7 @@ int kvc_attn_decode_kv(kvc_ctx* ctx, int layer, const void* d_k, const void* d_v
   if (!aligned16(d_k) || !aligned16(d_v)) return fail(KVC_EINVAL, "d_k / d_v must be 16-byte aligned");
   if (!ctx->last_single)
     return fail(KVC_ESTATE, "decode needs exactly one appended token per session");
-  if (ctx->kv4) {
-    KVC_CUDA(launch_attn_kv4(ctx->d, ctx->lim, &ctx->order, layer, d_k, d_v, d_q, d_out,
-                             ctx->last_total, ctx->last_max_t, static_cast<cudaStream_t>(stream)));
-    return KVC_OK;
-  }
+  if (ctx->kv4) return attend_kv4(ctx, layer, d_k, d_v, d_q, d_out, stream);
   // (An early launch may load the page while a launch before it writes the new row's slot:
   // the row goes into the tile after its load.)
   bool capturing = false;
@@ -619,11 +622,7 @@ int kvc_attn_prefill_chunk(kvc_ctx* ctx, int layer, const void* d_q, void* d_out
   if (ctx->last_max_t > PF_MAX_TOKENS)
     return fail(KVC_EINVAL, "prefill chunks are limited to %d tokens per session", PF_MAX_TOKENS);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (ctx->kv4) {
-    KVC_CUDA(launch_attn_kv4(ctx->d, ctx->lim, &ctx->order, layer, nullptr, nullptr, d_q, d_out,
-                             ctx->last_total, ctx->last_max_t, s));
-    return KVC_OK;
-  }
+  if (ctx->kv4) return attend_kv4(ctx, layer, nullptr, nullptr, d_q, d_out, stream);
   bool capturing = false;
   KVC_CUDA(is_capturing(s, &capturing));
   const PageHint pages = page_hint(ctx, capturing);
@@ -644,11 +643,7 @@ int kvc_attn_prefill_chunk_kv(kvc_ctx* ctx, int layer, const void* d_k, const vo
   if (ctx->last_max_t > PF_MAX_TOKENS)
     return fail(KVC_EINVAL, "prefill chunks are limited to %d tokens per session", PF_MAX_TOKENS);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (ctx->kv4) {
-    KVC_CUDA(launch_attn_kv4(ctx->d, ctx->lim, &ctx->order, layer, d_k, d_v, d_q, d_out,
-                             ctx->last_total, ctx->last_max_t, s));
-    return KVC_OK;
-  }
+  if (ctx->kv4) return attend_kv4(ctx, layer, d_k, d_v, d_q, d_out, stream);
   bool capturing = false;
   KVC_CUDA(is_capturing(s, &capturing));
   const PageHint pages = page_hint(ctx, capturing);

@@ -125,7 +125,8 @@ cudaError_t query_limits(const Dev& d, Limits* lim) {
   lim->dec_wide = decode_split_slots(d.esz, true, lim->sms);
   lim->dec_narrow = decode_split_slots(d.esz, false, lim->sms);
   e = d.esz == 2 ? prefill_tc_limits(lim) : prefill_f32_limits(lim);
-  if (e == cudaSuccess) e = kv4_limits(d.esz, lim);
+  if (e == cudaSuccess) e = kv4_decode_limits(d, lim);
+  if (e == cudaSuccess) e = kv4_prefill_limits(d, lim);
   // A full table only means that later contexts repeat this for every kvc_create.
   if (e == cudaSuccess && known && g_n_known < MAX_KNOWN) g_known[g_n_known++] = {id, d.esz, *lim};
   return e;

@@ -84,6 +84,81 @@ __device__ inline void values_of(uint32_t w, __half m, float (&f)[8]) {
   for (int i = 0; i < 8; ++i) f[i] = (float)((int)(w >> (4 * i) & 15u) - 8) * s;
 }
 
+// -- tensor cores ------------------------------------------------------------------------------
+__device__ inline uint32_t h2_bits(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
+__device__ inline __half2 bits_h2(uint32_t u) { return *reinterpret_cast<const __half2*>(&u); }
+
+__device__ inline void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                               uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// d = a b + c.
+__device__ inline void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                               uint32_t b0, uint32_t b1, const float (&c)[4]) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%10,%11,%12,%13};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]),
+        "f"(c[3]));
+}
+
+// Transpose of an 8 x 8 matrix of binary16 numbers held as accumulators are (lane (g, t): row g,
+// columns 2t and 2t + 1).
+__device__ inline uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+// (x & a) | b in one instruction.
+__device__ inline uint32_t and_or(uint32_t x, uint32_t a, uint32_t b) {
+  uint32_t y;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(y) : "r"(x), "r"(a), "r"(b));
+  return y;
+}
+
+// The pairs of a word as binary16 numbers (n - 8) m, exact: pair p is nibbles p and p + 4, m a scale
+// for each of the two, neg72m = -72 m.  Bits 4..7 of a half are (64 + n) m - 72 m in one step; bits
+// 0..3 are (1024 + n) - 1032, then times m: as many instructions as a shift would take, but the
+// pipes of shifts and of products then have about the same to do.
+__device__ inline void pairs_of(uint32_t w, __half2 m, __half2 neg72m, uint32_t (&v)[4]) {
+  const __half2 k1032 = __float2half2_rn(-1032.f);
+  const uint32_t x = w >> 8;
+  v[0] = h2_bits(__hmul2(__hadd2(bits_h2(and_or(w, 0x000F000Fu, 0x64006400u)), k1032), m));
+  v[1] = h2_bits(__hfma2(bits_h2(and_or(w, 0x00F000F0u, 0x54005400u)), m, neg72m));
+  v[2] = h2_bits(__hmul2(__hadd2(bits_h2(and_or(x, 0x000F000Fu, 0x64006400u)), k1032), m));
+  v[3] = h2_bits(__hfma2(bits_h2(and_or(x, 0x00F000F0u, 0x54005400u)), m, neg72m));
+}
+
+// Words of shared memory (32-bit address).
+__device__ inline void lds(uint32_t at, uint32_t (&w)[4]) {
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+               : "r"(at));
+}
+__device__ inline void lds(uint32_t at, uint32_t (&w)[2]) {
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
+}
+__device__ inline void lds(uint32_t at, uint32_t (&w)[1]) {
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(at));
+}
+__device__ inline void lds(uint32_t at, uint32_t& w) {
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(at));
+}
+
+// bulk_g2s with an L2 policy.
+__device__ inline void bulk_g2s_hint(void* dst_smem, const void* src_gmem, uint32_t bytes,
+                                     uint64_t* bar, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], "
+      "%2, [%3], %4;" ::"r"(smem_u32(dst_smem)),
+      "l"(src_gmem), "r"(bytes), "r"(smem_u32(bar)), "l"(policy)
+      : "memory");
+}
+
 }  // namespace kv4
 
 }  // namespace kvc

@@ -12,9 +12,10 @@
 // A group with an infinity or a NaN gets a NaN scale and stands for NaN.
 //
 // A tile is the 16 rows of one (page, layer, KV head) of K or of V, 9 D bytes: codes, then scales.
-//   K: row-major; the codes of row `slot` are D / 2 bytes, dim d in nibble d; scales [slot][D / 32].
-//      Lane (g, t) of a warp takes dims [t D / 4, (t + 1) D / 4) of rows g and g + 8: one 16-byte
-//      (D = 128) or 8-byte (D = 64) load each, one group each.
+//   K: row-major, D / 2 bytes of codes a row; scales [slot][D / 32].  Lane (g, t) of a warp takes 8
+//      dims of each group, [32 w + 8 t, 32 w + 8 t + 8) as its word w, of rows g and g + 8: its
+//      D / 32 words side by side, one 16-byte (D = 128) or 8-byte (D = 64) load a row.  A step of
+//      the product then stays within a group, so that a scale can come in behind it.
 //   V: dims in 8 pieces of D / 8; a piece of one row is D / 16 bytes, dim d in nibble d % (D / 8).
 //      Lane (g, t) takes piece g of rows 2t, 2t + 1 and of rows 2t + 8, 2t + 9, each pair side by
 //      side; scales [D / 32][slot], so that those of a pair are one 4-byte load.
@@ -47,9 +48,13 @@ KV4_FN size_t tile_at(int D, int layers, int heads, int page, int layer, int hea
   return ((((size_t)page * layers + layer) * heads + head) * 2 + kv) * tile_bytes(D);
 }
 
-// Byte offsets within a tile.
+// Byte offsets within a tile; 8 codes are a 32-bit word, dim d in nibble d % 8.
 // 8 codes (4 bytes) from dim d (a multiple of 8) of a K row.
-KV4_FN int k_codes(int D, int slot, int d) { return slot * (D / 2) + d / 2; }
+KV4_FN int k_codes(int D, int slot, int d) {
+  return slot * (D / 2) + (d % GROUP / 8 * (D / GROUP) + d / GROUP) * 4;
+}
+// Piece p of the 8 (D / 16 bytes each) that make up the codes of a K row.
+KV4_FN int k_piece(int D, int slot, int p) { return slot * (D / 2) + p * (D / 16); }
 KV4_FN int k_scale(int D, int slot, int group) { return ROWS * D / 2 + (slot * (D / GROUP) + group) * 2; }
 // Piece g (dims [g D / 8, (g + 1) D / 8)) of a V row.
 KV4_FN int v_piece(int D, int slot, int g) {

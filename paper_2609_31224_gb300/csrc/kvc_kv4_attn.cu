@@ -35,7 +35,6 @@ constexpr unsigned FULL = 0xFFFFFFFFu;
 constexpr int G = 4;               // query heads per KV head
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float P_SHIFT = 8.f;     // log2 of the largest weight P
-constexpr int MAX_PARTS = 64;      // CTAs that share a (session, KV head) pair, at most
 
 // Shape of one kernel: element type, head dim, column tiles per warp, ring depth.
 template <typename T_, int D_, int NT_, int STAGES_>
@@ -68,33 +67,6 @@ struct Layout {
     total = bars + wp * C::STAGES * 2 * 8;
   }
 };
-
-__device__ inline uint32_t h2_bits(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
-__device__ inline __half2 bits_h2(uint32_t u) { return *reinterpret_cast<const __half2*>(&u); }
-
-__device__ inline void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
-                               uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
-      "{%0,%1,%2,%3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
-// Transpose of an 8 x 8 matrix of binary16 numbers held as accumulators are (lane (g, t): row g,
-// columns 2t and 2t + 1).
-__device__ inline uint32_t transpose8(uint32_t x) {
-  uint32_t y;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-  return y;
-}
-
-// Values of nibbles p and p + 4 of w (nibble p of each half) times m: (64 + n) m - 72 m, exact.
-template <int P>
-__device__ inline uint32_t pair_of(uint32_t w, __half2 m, __half2 neg72m) {
-  const uint32_t s = P == 0 ? w << 4 : P == 1 ? w : P == 2 ? w >> 4 : w >> 8;
-  return h2_bits(__hfma2(bits_h2((s & 0x00F000F0u) | 0x54005400u), m, neg72m));
-}
 
 // Weight of a state with running maximum x against the maximum m of both, 0 where there is no key.
 // Maxima are of the raw products S, c is the row's softmax scale: S - max is rounded before c comes
@@ -147,8 +119,8 @@ __device__ void build_queries(const Dev& d, const SeqInfo& si, int head, int n_c
     const int tile = col / 8, n = col % 8;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      const int dim = half * (D / 2) + 8 * c;           // first of eight dims
-      const int t = dim / (D / 4), w = dim % (D / 4) / 8;  // lane (n, t), word w
+      const int dim = half * (D / 2) + 8 * c;                // first of eight dims
+      const int t = dim % GROUP / 8, w = dim / GROUP;        // lane (n, t), word w
       float y[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) y[j] = (half ? yb[j] : ya[j]) * inv;
@@ -256,17 +228,16 @@ __device__ inline void page_step(const uint8_t* page, const uint8_t* frag, const
       wa[0] = a.x; wa[1] = a.y;
       wb[0] = b.x; wb[1] = b.y;
     }
-    const int group = t * (D / 4) / GROUP;
-    const __half2 ma = __half2half2(*reinterpret_cast<const __half*>(kt + k_scale(D, g, group)));
-    const __half2 mb = __half2half2(*reinterpret_cast<const __half*>(kt + k_scale(D, g + 8, group)));
     const __half2 m72 = __float2half2_rn(-72.f);
-    const __half2 na = __hmul2(ma, m72), nb = __hmul2(mb, m72);
 #pragma unroll
     for (int w = 0; w < C::WORDS; ++w) {
-      const uint32_t a[8] = {pair_of<0>(wa[w], ma, na), pair_of<0>(wb[w], mb, nb),
-                             pair_of<1>(wa[w], ma, na), pair_of<1>(wb[w], mb, nb),
-                             pair_of<2>(wa[w], ma, na), pair_of<2>(wb[w], mb, nb),
-                             pair_of<3>(wa[w], ma, na), pair_of<3>(wb[w], mb, nb)};
+      const __half2 ma = __half2half2(*reinterpret_cast<const __half*>(kt + k_scale(D, g, w)));
+      const __half2 mb = __half2half2(*reinterpret_cast<const __half*>(kt + k_scale(D, g + 8, w)));
+      const __half2 na = __hmul2(ma, m72), nb = __hmul2(mb, m72);
+      uint32_t pa[4], pb[4];
+      pairs_of(wa[w], ma, na, pa);
+      pairs_of(wb[w], mb, nb, pb);
+      const uint32_t a[8] = {pa[0], pb[0], pa[1], pb[1], pa[2], pb[2], pa[3], pb[3]};
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const uint8_t* qf = frag + (size_t)(tile0 + nt) * C::Q_TILE + (w * 32 + lane) * 16;
@@ -397,10 +368,10 @@ __device__ inline void page_step(const uint8_t* page, const uint8_t* frag, const
       const uint32_t sel = half ? 0x7632u : 0x5410u;
       const uint32_t lo = __byte_perm(v[0][0][w], v[0][1][w], sel);
       const uint32_t hi = __byte_perm(v[1][0][w], v[1][1][w], sel);
-      const uint32_t a[8] = {pair_of<0>(lo, ml, nl), pair_of<1>(lo, ml, nl),
-                             pair_of<0>(hi, mh, nh), pair_of<1>(hi, mh, nh),
-                             pair_of<2>(lo, ml, nl), pair_of<3>(lo, ml, nl),
-                             pair_of<2>(hi, mh, nh), pair_of<3>(hi, mh, nh)};
+      uint32_t pl[4], ph[4];
+      pairs_of(lo, ml, nl, pl);
+      pairs_of(hi, mh, nh, ph);
+      const uint32_t a[8] = {pl[0], pl[1], ph[0], ph[1], pl[2], pl[3], ph[2], ph[3]};
       const int mt = 4 * w + 2 * half;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -668,12 +639,8 @@ __global__ void __launch_bounds__(C::MOST_THREADS, 1) attn_kv4_kernel(
   }
 }
 
-// Shapes: decode (and chunks of up to two tokens, which fit one column tile) has a warp per page
-// group; chunks have ceil(rows / 24) warps per group.
-constexpr int DEC_NT = 1, DEC_STAGES = 4, DEC_WP = 4;
+// Chunks have ceil(rows / 24) warps per page group.
 constexpr int PF_NT = 3, PF_STAGES = 4, PF_PARTS = 32;
-template <typename T, int D>
-using DecCfg = Cfg<T, D, DEC_NT, DEC_STAGES>;
 template <typename T, int D>
 using PfCfg = Cfg<T, D, PF_NT, PF_STAGES>;
 
@@ -692,67 +659,53 @@ cudaError_t grid_of(int wc, int wp, int parts, int sms, int* grid) {
 
 template <typename T, int D>
 cudaError_t limits_of(Limits* lim) {
-  constexpr int MOST = 227 * 1024;
-  cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(&attn_kv4_kernel<DecCfg<T, D>>),
-                                       cudaFuncAttributeMaxDynamicSharedMemorySize, MOST - 1024);
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(reinterpret_cast<const void*>(&attn_kv4_kernel<PfCfg<T, D>>),
-                             cudaFuncAttributeMaxDynamicSharedMemorySize, MOST - 1024);
-  if (e == cudaSuccess) e = grid_of<DecCfg<T, D>>(1, DEC_WP, MAX_PARTS, lim->sms, &lim->kv4_decode);
+  constexpr int MOST = 226 * 1024;
+  cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(&attn_kv4_kernel<PfCfg<T, D>>),
+                                       cudaFuncAttributeMaxDynamicSharedMemorySize, MOST);
   for (int wc = 1; wc <= KV4_PF_WARPS && e == cudaSuccess; ++wc)
     e = grid_of<PfCfg<T, D>>(wc, pf_groups(wc), PF_PARTS, lim->sms, &lim->kv4_prefill[wc]);
   return e;
 }
 
-template <class C>
-cudaError_t launch(const Dev& d, int layer, const void* q, void* out, int wc, int wp, int min_units,
-                   int parts, int grid, float* part_o, float2* part_ml, int64_t part_floats,
-                   int64_t part_rows, int* count, bool early, cudaStream_t s) {
-  using T = typename C::T;
-  const Layout<C> lay(wc, wp, parts);
-  // Each CTA of the split may leave two partial states.
-  const int64_t cols = (int64_t)wc * C::NT * 8;
-  const int64_t slots = std::min(part_floats / (cols * C::D), part_rows / cols);
-  const int n = (int)std::min<int64_t>(grid, slots / 2);
-  if (n < 1) return cudaErrorInvalidConfiguration;
-  const float scale = 16.f * LOG2E / sqrtf((float)C::D);
-  return launch_ex(&attn_kv4_kernel<C>, dim3(n), dim3(32 * wc * wp), lay.total, s, true, d, layer,
-                   static_cast<const T*>(q), static_cast<T*>(out), scale, wc, wp, min_units, parts,
-                   part_o, part_ml, count, (int)early);
-}
-
 template <typename T, int D>
 cudaError_t launch_any(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
                        int max_t, bool early, cudaStream_t s) {
-  if (max_t * G <= 8)
-    return launch<DecCfg<T, D>>(d, layer, q, out, 1, DEC_WP, DEC_WP, MAX_PARTS, lim.kv4_decode,
-                                d.dec_part_o, d.dec_part_ml, (int64_t)d.dec_slots * G * D,
-                                (int64_t)d.dec_slots * G, d.dec_count, early, s);
-  const int wc = pf_warps(max_t);
-  return launch<PfCfg<T, D>>(d, layer, q, out, wc, pf_groups(wc), pf_groups(wc), PF_PARTS,
-                             lim.kv4_prefill[wc], d.pf_part_o, d.pf_part_ml,
-                             (int64_t)d.pf_slots * PF_MAX_TOKENS * G * 128,
-                             (int64_t)d.pf_slots * PF_MAX_TOKENS * G, d.pf_count, early, s);
+  using C = PfCfg<T, D>;
+  const int wc = pf_warps(max_t), wp = pf_groups(wc);
+  const Layout<C> lay(wc, wp, PF_PARTS);
+  // Each CTA of the split may leave two partial states.
+  const int cols = wc * C::NT * 8;
+  const int64_t slots = (int64_t)d.pf_slots * PF_MAX_TOKENS * G * 128 / (cols * D);
+  const int grid = (int)std::min<int64_t>(
+      lim.kv4_prefill[wc], std::min<int64_t>(slots, (int64_t)d.pf_slots * PF_MAX_TOKENS * G / cols) / 2);
+  const float scale = 16.f * LOG2E / sqrtf((float)D);
+  return launch_ex(&attn_kv4_kernel<C>, dim3(grid), dim3(32 * wc * wp), lay.total, s, true, d, layer,
+                   static_cast<const T*>(q), static_cast<T*>(out), scale, wc, wp, wp, PF_PARTS,
+                   d.pf_part_o, d.pf_part_ml, d.pf_count, (int)early);
 }
 
 }  // namespace
 
-cudaError_t kv4_limits(int esz, Limits* lim) {
-  return esz == 2 ? limits_of<__nv_bfloat16, 128>(lim) : limits_of<float, 64>(lim);
+cudaError_t kv4_prefill_limits(const Dev& d, Limits* lim) {
+  return d.esz == 2 ? limits_of<__nv_bfloat16, 128>(lim) : limits_of<float, 64>(lim);
 }
 
 cudaError_t launch_attn_kv4(const Dev& d, const Limits& lim, LaunchOrder* order, int layer,
                             const void* new_k, const void* new_v, const void* q, void* out,
-                            int total, int max_t, cudaStream_t s) {
+                            int total, int max_t, int64_t units, cudaStream_t s) {
   if (new_k != nullptr) {
     const cudaError_t e = launch_append_layers_kv4(d, total, layer, 1, new_k, new_v, false, s);
     if (e != cudaSuccess) return e;
     order->layer_write(layer);
   }
   const bool early = order->early(layer, false);
-  const cudaError_t e =
-      d.esz == 2 ? launch_any<__nv_bfloat16, 128>(d, lim, layer, q, out, max_t, early, s)
-                 : launch_any<float, 64>(d, lim, layer, q, out, max_t, early, s);
+  cudaError_t e;
+  if (max_t == 1)
+    e = launch_decode_kv4(d, lim, layer, q, out, units, early, s);
+  else if (d.esz == 2)
+    e = launch_any<__nv_bfloat16, 128>(d, lim, layer, q, out, max_t, early, s);
+  else
+    e = launch_any<float, 64>(d, lim, layer, q, out, max_t, early, s);
   if (e == cudaSuccess) order->launched(layer, false);
   return e;
 }

@@ -1,0 +1,642 @@
+// Single-token decode attention over a cache held in 4 bits (KVC_KV4).
+//
+// For each session of the last append (one token each), KV head and its G = 4 query heads:
+// out = softmax(RoPE(q) . k / sqrt(D)) v over every resident key, k and v the numbers that the codes
+// stand for.
+//
+// A warp takes a page of 16 keys at a time, as one step of mma.sync m16n8k16 (binary16 in, binary32
+// accumulate) with the keys as M:
+//   S^T [16 keys x 8] = K [16 x D] . Q^T [D x 8],   O^T [D x 8] += V^T [D x 16] . P^T [16 x 8].
+// The eight columns are two binary16 pieces of each of the four heads (column 2h: q rounded, 2h + 1:
+// what the rounding left), so that lane (g, t) ends with both pieces of head t for keys g and g + 8:
+// their sum is a score with about 22 bits of q, one softmax state per lane, no lane idle.  binary32
+// calls split P the same way; for bfloat16 the rounding of P to 11 bits stays.
+//
+// What bounds it: 18 D bytes a page against about 260 warp instructions, most of them the way from
+// nibble to operand (one AND-OR, a shift for three pairs of four, and a fused multiply-add for each
+// pair of elements).  So everything else is kept small: the query's operands stay in registers, the
+// softmax reference lags (it moves only when a score passes it by 2^6), page lists are looked up 32
+// at a time, and only pages with masked slots look at their range.
+#include "kvc_kv4.cuh"
+
+namespace kvc {
+
+namespace {
+
+using namespace kv4;
+
+constexpr unsigned FULL = 0xFFFFFFFFu;
+constexpr int G = 4;               // query heads per KV head
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float P_SHIFT = 8.f;     // log2 of the weight P of a key at the reference
+constexpr float P_LAG = 6.f;       // and of how far above it a weight may be: 2^14 in all
+constexpr int MAX_PARTS = 64;      // CTAs that share a (session, KV head) pair, at most
+
+// Shape of a CTA: WARPS warps, each with its own ring of STAGES pages.
+template <typename T_, int D_, int WARPS_, int STAGES_>
+struct Cfg {
+  using T = T_;
+  static constexpr int D = D_, WARPS = WARPS_, STAGES = STAGES_, THREADS = 32 * WARPS_;
+  static constexpr bool SPLIT_P = sizeof(T) == 4;  // P in two binary16 pieces
+  static constexpr bool SCALE_BEHIND = !SPLIT_P;   // K's scales come in behind the product
+  static constexpr int PAGE = 18 * D;              // bytes of a page of one head, K and V
+  static constexpr int KW = D / 32;                // 32-bit words of K codes per lane and row
+  static constexpr int VW = D / 64;                // and of V codes per lane and row
+  static constexpr int MT = D / 16;                // row tiles of O^T
+  // Shared memory: rings, the warps' states, weights of parts, barriers.
+  static constexpr int RING = WARPS * STAGES * PAGE;
+  static constexpr int STATE_O = RING;                          // [WARPS][G][D] floats
+  static constexpr int STATE_ML = STATE_O + WARPS * G * D * 4;  // [WARPS][G] (m, l)
+  static constexpr int WEIGHT = STATE_ML + WARPS * G * 8;       // [max(WARPS, MAX_PARTS)][G]
+  static constexpr int TOTAL = WEIGHT + (WARPS > MAX_PARTS ? WARPS : MAX_PARTS) * G * 4;  // [G] (m, l)
+  static constexpr int BARS = TOTAL + G * 8;
+  static constexpr int SMEM = BARS + WARPS * STAGES * 8;
+  static_assert(PAGE % 16 == 0 && RING % 16 == 0 && BARS % 8 == 0, "alignment");
+};
+
+__device__ inline float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// Weight of a state with reference m against the reference M of several, 0 where it has no key.
+// References are of the raw products S, c is the row's softmax scale: S - m is rounded before c
+// comes in, so that logits of any size leave exponents that are exact near 0.
+__device__ inline float weight2(float m, float M, float c) {
+  return m == -INFINITY ? 0.f : ex2((m - M) * c);
+}
+
+// The query of a pair in this warp's registers.
+template <class C>
+struct Query {
+  // Lane (n, t) holds, for column n (head n / 2, piece n % 2), the pairs (p, p + 4) of dims
+  // [32 w + 8 t, 32 w + 8 t + 8); where the scales come in behind the product, pairs 1 and 3 (whose
+  // nibbles are read 16 times too large) over 16.
+  uint32_t b[C::KW][4];
+  float c;        // softmax scale of head t
+  // What a group's product starts from, -8 times the sum of its dims of head t: takes the 8 off the
+  // nibbles.
+  float zero[C::KW][4];
+};
+
+constexpr int Q_EXP = 9;        // a row's largest element is in [2^9, 2^10)
+constexpr int RAW_EXP = -24;    // a nibble's bits 0..3 as a binary16 number are n 2^-24
+
+template <class C>
+__device__ inline void load_query(const Dev& d, const SeqInfo& si, int head, const typename C::T* q,
+                                  int lane, Query<C>& qr) {
+  using T = typename C::T;
+  constexpr int D = C::D, KW = C::KW, HALF = D / 2;
+  const int n = lane >> 2, t = lane & 3;
+  const T* row = q + ((size_t)si.q_row0 * d.q_heads + head * G + n / 2) * D + 8 * t;
+  Eight<T> in[KW];
+#pragma unroll
+  for (int w = 0; w < KW; ++w) in[w].load(row + GROUP * w);
+  const float4* t4 = reinterpret_cast<const float4*>(d.rope + (size_t)si.pos_first * HALF + 8 * t);
+  float y[KW][8];
+  uint32_t most = 0;
+#pragma unroll
+  for (int w = 0; w < KW / 2; ++w) {
+    float x1[8], x2[8];
+    in[w].get(x1);
+    in[w + KW / 2].get(x2);                           // the rotate-half partners
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const float4 cs = t4[(GROUP * w + e) / 2];
+      turn_pair(x1[e], x2[e], make_float2(cs.x, cs.y), y[w][e], y[w + KW / 2][e]);
+      turn_pair(x1[e + 1], x2[e + 1], make_float2(cs.z, cs.w), y[w][e + 1], y[w + KW / 2][e + 1]);
+    }
+  }
+#pragma unroll
+  for (int w = 0; w < KW; ++w)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = max(most, abs_bits(y[w][e]));
+  most = max(most, __shfl_xor_sync(FULL, most, 1));
+  most = max(most, __shfl_xor_sync(FULL, most, 2));
+  // The row over 2^e.  Infinities and NaN pass through.
+  int e = (int)(most >> 23) - 127 - Q_EXP;
+  e = most >= 0x7F800000u ? 0 : max(e, -126);
+  const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+  float sum[KW];
+#pragma unroll
+  for (int w = 0; w < KW; ++w) {
+    sum[w] = 0.f;
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const float lo = y[w][p] * inv, hi = y[w][p + 4] * inv;
+      __half2 v = __floats2half2_rn(lo, hi);
+      if (n & 1) v = __floats2half2_rn(lo - __low2float(v), hi - __high2float(v));
+      if constexpr (C::SCALE_BEHIND)
+        if (p & 1) v = __hmul2(v, __float2half2_rn(0.0625f));
+      const float back = C::SCALE_BEHIND && (p & 1) ? 16.f : 1.f;
+      sum[w] += (__low2float(v) + __high2float(v)) * back;
+      qr.b[w][p] = h2_bits(v);
+    }
+  }
+  // 16: scales are stored over 16; and the softmax takes exponents of 2.
+  const float scale = 16.f * LOG2E * (D == 128 ? 0.08838834764831845f : 0.125f);
+  const float c = scale * __uint_as_float((uint32_t)(127 + e) << 23) *
+                  (C::SCALE_BEHIND ? (float)(1 << -RAW_EXP) : 1.f);
+  // Of head t, from lane (2t, 0).  (Beyond binary32 it is large enough to single out a maximum.)
+  qr.c = __shfl_sync(FULL, fminf(c, 3.4e38f), 8 * t);
+  if constexpr (C::SCALE_BEHIND) {
+#pragma unroll
+    for (int w = 0; w < KW; ++w) {
+      float z = sum[w];
+      z += __shfl_xor_sync(FULL, z, 1);
+      z += __shfl_xor_sync(FULL, z, 2);
+      z += __shfl_xor_sync(FULL, z, 4);               // both pieces
+      z = __shfl_sync(FULL, z, 8 * t) * (-8.f / (float)(1 << -RAW_EXP));
+      qr.zero[w][0] = qr.zero[w][2] = z;
+      qr.zero[w][1] = qr.zero[w][3] = 0.f;
+    }
+  }
+}
+
+// Which pages of a session need no look at their slots: full pages of the compacted region and live
+// pages between the consumed front and the partly filled end.
+struct OpenPages {
+  int hist_full, live_first, live_last;
+  __device__ explicit OpenPages(const SeqInfo& si) {
+    hist_full = si.n_hist / PS;
+    live_first = si.n_hist_pages + (si.live_head + PS - 1) / PS;
+    live_last = si.n_hist_pages + (si.live_head + si.n_live) / PS - 1;
+  }
+  __device__ bool has(int b) const { return b < hist_full || (b >= live_first && b <= live_last); }
+};
+
+// A warp's running state: head t, this lane's keys (l) and its 16 (8) dims of piece g (o).
+template <class C>
+struct State {
+  float o[C::MT][4];
+  float m, l;
+};
+
+template <class C>
+__device__ inline void page_step(const uint32_t page, const Query<C>& qr, bool open,
+                                 const SeqInfo& si, int blk, State<C>& st, int lane) {
+  constexpr int D = C::D, KW = C::KW, VW = C::VW;
+  const int g = lane >> 2, t = lane & 3;
+  const uint32_t kt = page, vt = page + 9 * D;
+  const __half2 m72 = __float2half2_rn(-72.f);
+
+  float s0, s1;  // scores of keys g and g + 8
+  {
+    uint32_t wa[KW], wb[KW], ma[KW / 2], mb[KW / 2];
+    lds(kt + g * (D / 2) + t * (D / 8), wa);
+    lds(kt + (g + 8) * (D / 2) + t * (D / 8), wb);
+    lds(kt + k_scale(D, g, 0), ma);
+    lds(kt + k_scale(D, g + 8, 0), mb);
+    float x[KW][4];
+    if constexpr (C::SCALE_BEHIND) {
+      // Nibbles as they are: bits 0..3 of a half are n 2^-24, bits 4..7 n 2^-20.
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        const uint32_t ha = wa[w] >> 8, hb = wb[w] >> 8;
+        mma_f16(x[w], wa[w] & 0x000F000Fu, wb[w] & 0x000F000Fu, wa[w] & 0x00F000F0u,
+                wb[w] & 0x00F000F0u, qr.b[w][0], qr.b[w][1], qr.zero[w]);
+        mma_f16(x[w], ha & 0x000F000Fu, hb & 0x000F000Fu, ha & 0x00F000F0u, hb & 0x00F000F0u,
+                qr.b[w][2], qr.b[w][3]);
+      }
+      s0 = s1 = 0.f;
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        const float2 a = __half22float2(bits_h2(ma[w / 2])), b = __half22float2(bits_h2(mb[w / 2]));
+        s0 = fmaf(x[w][0] + x[w][1], w % 2 ? a.y : a.x, s0);
+        s1 = fmaf(x[w][2] + x[w][3], w % 2 ? b.y : b.x, s1);
+      }
+    } else {
+      // Exact values of the keys, and a sum for every 16 dims: the tensor cores cut off what they
+      // add to an accumulator.
+      float z[KW][4];
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        const uint32_t da = __byte_perm(ma[w / 2], 0, w % 2 ? 0x3232u : 0x1010u);
+        const uint32_t db = __byte_perm(mb[w / 2], 0, w % 2 ? 0x3232u : 0x1010u);
+        uint32_t a[4], b[4];
+        pairs_of(wa[w], bits_h2(da), __hmul2(bits_h2(da), m72), a);
+        pairs_of(wb[w], bits_h2(db), __hmul2(bits_h2(db), m72), b);
+        x[w][0] = x[w][1] = x[w][2] = x[w][3] = z[w][0] = z[w][1] = z[w][2] = z[w][3] = 0.f;
+        mma_f16(x[w], a[0], b[0], a[1], b[1], qr.b[w][0], qr.b[w][1]);
+        mma_f16(z[w], a[2], b[2], a[3], b[3], qr.b[w][2], qr.b[w][3]);
+      }
+      s0 = s1 = 0.f;
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        s0 += x[w][1] + z[w][1];
+        s1 += x[w][3] + z[w][3];
+      }
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        s0 += x[w][0] + z[w][0];
+        s1 += x[w][2] + z[w][2];
+      }
+    }
+  }
+  BlockRange br;
+  if (!open) {
+    br = block_range(si, blk);
+    if (g < br.lo || g >= br.hi) s0 = -INFINITY;
+    if (g + 8 < br.lo || g + 8 >= br.hi) s1 = -INFINITY;
+  }
+  float a0 = fmaf(s0 - st.m, qr.c, P_SHIFT), a1 = fmaf(s1 - st.m, qr.c, P_SHIFT);
+  // (At the first page m is -infinity: every valid key asks for a new reference.)
+  if (__any_sync(FULL, fmaxf(a0, a1) > P_SHIFT + P_LAG)) {
+    float mx = fmaxf(s0, s1);
+#pragma unroll
+    for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(FULL, mx, off));
+    const float mn = fmaxf(st.m, mx);
+    const float alpha = weight2(st.m, mn, qr.c);
+    st.l *= alpha;
+#pragma unroll
+    for (int mt = 0; mt < C::MT; ++mt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) st.o[mt][j] *= alpha;
+    st.m = mn;
+    a0 = fmaf(s0 - mn, qr.c, P_SHIFT);
+    a1 = fmaf(s1 - mn, qr.c, P_SHIFT);
+  }
+  if (!open) {
+    // (Where no key was valid so far s - m is no number.)
+    if (s0 == -INFINITY) a0 = -INFINITY;
+    if (s1 == -INFINITY) a1 = -INFINITY;
+  }
+  const float p0 = ex2(a0), p1 = ex2(a1);
+  st.l += p0 + p1;
+  uint32_t b0, b1;
+  if constexpr (C::SPLIT_P) {
+    const float h0 = __half2float(__float2half_rn(p0)), h1 = __half2float(__float2half_rn(p1));
+    b0 = transpose8(h2_bits(__floats2half2_rn(h0, p0 - h0)));
+    b1 = transpose8(h2_bits(__floats2half2_rn(h1, p1 - h1)));
+  } else {
+    b0 = transpose8(h2_bits(__floats2half2_rn(p0, 0.f)));
+    b1 = transpose8(h2_bits(__floats2half2_rn(p1, 0.f)));
+  }
+
+  // V^T: lane (g, t) takes piece g of rows 2t, 2t + 1 (lo) and 2t + 8, 2t + 9 (hi).
+  uint32_t lo[2 * VW], hi[2 * VW], sl, sh;  // [row of the pair][word]
+  lds(vt + lane * (D / 8), lo);
+  lds(vt + D * 4 + lane * (D / 8), hi);
+  const uint32_t sc = vt + v_scale(D, 2 * t, g * (D / 8) / GROUP);
+  lds(sc, sl);
+  lds(sc + 16, sh);
+  if (!open) {
+    // Invalid slots stand for 0, whatever the page held there before.
+    const int i = 2 * t;
+    if (i < br.lo || i >= br.hi) sl &= 0xFFFF0000u;
+    if (i + 1 < br.lo || i + 1 >= br.hi) sl &= 0x0000FFFFu;
+    if (i + 8 < br.lo || i + 8 >= br.hi) sh &= 0xFFFF0000u;
+    if (i + 9 < br.lo || i + 9 >= br.hi) sh &= 0x0000FFFFu;
+  }
+  const __half2 ml = bits_h2(sl), mh = bits_h2(sh);
+  const __half2 nl = __hmul2(ml, m72), nh = __hmul2(mh, m72);
+#pragma unroll
+  for (int w = 0; w < VW; ++w)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      // Dims 8 w + 4 half + 0..3 of the piece: nibble p of both halves of a word, the pair's rows.
+      const uint32_t sel = half ? 0x7632u : 0x5410u;
+      uint32_t a[4], b[4];
+      pairs_of(__byte_perm(lo[w], lo[VW + w], sel), ml, nl, a);
+      pairs_of(__byte_perm(hi[w], hi[VW + w], sel), mh, nh, b);
+      const int mt = 4 * w + 2 * half;
+      if constexpr (C::SPLIT_P) {
+        // A page's sums by themselves, then added rounded (as above).
+        float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
+        mma_f16(x, a[0], a[1], b[0], b[1], b0, b1);
+        mma_f16(y, a[2], a[3], b[2], b[3], b0, b1);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          st.o[mt][j] += x[j];
+          st.o[mt + 1][j] += y[j];
+        }
+      } else {
+        mma_f16(st.o[mt], a[0], a[1], b[0], b[1], b0, b1);
+        mma_f16(st.o[mt + 1], a[2], a[3], b[2], b[3], b0, b1);
+      }
+    }
+}
+
+// The pages of one warp and segment (every WARPS-th block), through the warp's ring.
+template <class C>
+struct Ring {
+  uint8_t* slots;
+  uint64_t* full;
+  const uint8_t* tiles;      // of the layer and head in page 0
+  size_t page_stride;
+  const int32_t* hrow;
+  const int32_t* lrow;
+  int n_hist_pages, first, n_my, win, pid;
+
+  __device__ void open(const Dev& d, int layer, const UnitSeg& seg, int warp) {
+    tiles = d.pool + tile_at(C::D, d.layers, d.kv_heads, 0, layer, seg.head, 0);
+    hrow = d.hist_pt + (size_t)seg.si.sid * d.max_pages_per_session;
+    lrow = d.live_pt + (size_t)seg.si.sid * d.max_pages_per_session;
+    n_hist_pages = seg.si.n_hist_pages;
+    first = seg.blk_begin() + warp;
+    const int n = seg.end - seg.u;
+    n_my = n > warp ? (n - warp + C::WARPS - 1) / C::WARPS : 0;
+    win = -32;
+    pid = 0;
+  }
+  // Copy the warp's k-th page in, as its n-th of the launch; the whole warp.
+  __device__ void issue(int k, uint32_t n, uint64_t policy, int lane) {
+    if (k >= win + 32) {
+      win = k & ~31;
+      const int j = win + lane, b = first + j * C::WARPS;
+      pid = j < n_my ? (b < n_hist_pages ? hrow[b] : lrow[b - n_hist_pages]) : 0;
+    }
+    const int page = __shfl_sync(FULL, pid, k - win);
+    if (lane == 0) {
+      const uint32_t st = n % C::STAGES;
+      fence_proxy_async_smem();
+      mbar_arrive_expect_tx(&full[st], C::PAGE);
+      bulk_g2s_hint(slots + st * C::PAGE, tiles + page * page_stride, C::PAGE, &full[st], policy);
+    }
+  }
+};
+
+// Rows of a pair from the parts that cover it, by every thread of the last CTA to arrive: part i is
+// in slot part(i), [G][D] outputs and (m, l) per head.
+template <class C, typename PartFn>
+__device__ void merge_parts(const float* part_o, const float2* part_ml, int parts, PartFn part,
+                            const float* scale, float* weight, typename C::T* out, int tid) {
+  using T = typename C::T;
+  constexpr int D = C::D, E = G * D, EPT = (E + C::THREADS - 1) / C::THREADS;
+  constexpr int BATCH = 32 / EPT > 16 ? 16 : 32 / EPT;  // parts whose loads are in flight together
+  const int lane = tid & 31, warp = tid >> 5;
+  float x[BATCH][EPT];
+  auto load = [&](int i0) {
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+      for (int j = 0; j < EPT; ++j) {
+        const int e = tid + j * C::THREADS;
+        x[i][j] = i0 + i < parts && e < E ? __ldcg(part_o + (size_t)part(i0 + i) * E + e) : 0.f;
+      }
+  };
+  load(0);
+  if (warp < G) {
+    constexpr int PL = MAX_PARTS / 32;
+    float2 ml[PL];
+    float M = -INFINITY, L = 0.f, w[PL];
+#pragma unroll
+    for (int i = 0; i < PL; ++i) {
+      ml[i] = lane + 32 * i < parts ? __ldcg(&part_ml[(size_t)part(lane + 32 * i) * G + warp])
+                                    : make_float2(-INFINITY, 0.f);
+      M = fmaxf(M, ml[i].x);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(FULL, M, o));
+#pragma unroll
+    for (int i = 0; i < PL; ++i) {
+      w[i] = weight2(ml[i].x, M, scale[warp]);
+      L += ml[i].y * w[i];
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(FULL, L, o);
+    const float inv = 16.f / L;
+#pragma unroll
+    for (int i = 0; i < PL; ++i)
+      if (lane + 32 * i < parts) weight[(lane + 32 * i) * G + warp] = w[i] * inv;
+  }
+  __syncthreads();
+  float acc[EPT] = {};
+  for (int i0 = 0;;) {
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      if (i0 + i >= parts) break;
+#pragma unroll
+      for (int j = 0; j < EPT; ++j) {
+        const int e = tid + j * C::THREADS;
+        if (e < E) acc[j] += x[i][j] * weight[(i0 + i) * G + e / D];
+      }
+    }
+    i0 += BATCH;
+    if (i0 >= parts) break;
+    load(i0);
+  }
+#pragma unroll
+  for (int j = 0; j < EPT; ++j) {
+    const int e = tid + j * C::THREADS;
+    if (e < E) out[e] = from_float<T>(acc[j]);
+  }
+}
+
+template <class C>
+__global__ void __launch_bounds__(C::THREADS, C::WARPS == 4 ? 4 : 1) decode_kv4_kernel(
+    Dev d, int layer, const typename C::T* __restrict__ q, typename C::T* __restrict__ out,
+    int min_units, int max_parts, int early) {
+  using T = typename C::T;
+  constexpr int D = C::D, E = G * D;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int s_last, s_abort;
+  __shared__ float s_scale[G];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  float* state_o = reinterpret_cast<float*>(smem + C::STATE_O);
+  float2* state_ml = reinterpret_cast<float2*>(smem + C::STATE_ML);
+  float* weight = reinterpret_cast<float*>(smem + C::WEIGHT);
+  float2* total = reinterpret_cast<float2*>(smem + C::TOTAL);
+  Ring<C> ring;
+  ring.slots = smem + warp * C::STAGES * C::PAGE;
+  ring.full = reinterpret_cast<uint64_t*>(smem + C::BARS) + warp * C::STAGES;
+  ring.page_stride = page_bytes(D, d.layers, d.kv_heads);
+  if (lane == 0) {
+    for (int i = 0; i < C::STAGES; ++i) mbar_init(&ring.full[i], 1);
+    fence_mbar_init();
+  }
+  if (tid == 0) s_abort = 0;
+  __syncthreads();
+  // Before the wait below an early launch reads only what the append wrote (work list, page tables,
+  // pages); q, outputs, partial states and counters come after it.
+  if (!early) pdl_wait();
+  pdl_launch_dependents();
+  bool waited = false;
+
+  const int H = d.kv_heads;
+  const UnitSplit us = unit_split(d, gridDim.x, min_units, max_parts);
+  if ((int)blockIdx.x >= us.n_cta) return;
+  const int cta = blockIdx.x;
+  const int u_begin = us.start_of(cta), u_end = us.start_of(cta + 1);
+  if (u_begin >= u_end) return;
+  const uint64_t policy = evict_first_policy();
+  const uint32_t slots = smem_u32(ring.slots);
+  uint32_t loads = 0;  // pages of this warp, over all segments before
+  UnitSeg seg = unit_segment(d, u_begin, u_end);
+  ring.open(d, layer, seg, warp);
+  for (int k = 0; k < min(C::STAGES, ring.n_my); ++k) ring.issue(k, k, policy, lane);
+
+  for (;;) {
+    const SeqInfo& si = seg.si;
+    if (!waited) {
+      pdl_wait();
+      waited = true;
+    }
+    Query<C> qr;
+    load_query<C>(d, si, seg.head, q, lane, qr);
+    State<C> st;
+    st.m = -INFINITY;
+    st.l = 0.f;
+#pragma unroll
+    for (int mt = 0; mt < C::MT; ++mt) st.o[mt][0] = st.o[mt][1] = st.o[mt][2] = st.o[mt][3] = 0.f;
+    const OpenPages open(si);
+    const int n_my = ring.n_my;
+    int failed_at = -1;
+    for (int k = 0; k < n_my; ++k) {
+      const uint32_t n = loads + k, stage = n % C::STAGES;
+      if (!__all_sync(FULL, mbar_wait(d, &ring.full[stage], (n / C::STAGES) & 1))) {
+        failed_at = k;
+        break;
+      }
+      const int blk = ring.first + k * C::WARPS;
+      page_step<C>(slots + stage * C::PAGE, qr, open.has(blk), si, blk, st, lane);
+      __syncwarp();
+      if (k + C::STAGES < n_my) ring.issue(k + C::STAGES, n + C::STAGES, policy, lane);
+    }
+    if (failed_at >= 0 && lane == 0) s_abort = 1;
+
+    // This warp's state for the CTA's merge.
+    {
+      const int g = lane >> 2, t = lane & 3;
+      float l = st.l;
+#pragma unroll
+      for (int off = 4; off < 32; off <<= 1) l += __shfl_xor_sync(FULL, l, off);
+      if (g == 0) {
+        state_ml[warp * G + t] = make_float2(st.m, l);
+        if (warp == 0) s_scale[t] = qr.c;
+      }
+      float* to = state_o + (warp * G + t) * D + g * (D / 8);
+#pragma unroll
+      for (int mt = 0; mt < C::MT; mt += 2) {
+        float4 x = make_float4(st.o[mt][0], st.o[mt][2], st.o[mt + 1][0], st.o[mt + 1][2]);
+        if constexpr (C::SPLIT_P)
+          x = make_float4(x.x + st.o[mt][1], x.y + st.o[mt][3], x.z + st.o[mt + 1][1],
+                          x.w + st.o[mt + 1][3]);
+        *reinterpret_cast<float4*>(to + 2 * mt) = x;
+      }
+    }
+    __syncthreads();
+    if (s_abort) {
+      // A wait gave up: each warp drains the copies that it still has in flight (bounded), then the
+      // whole CTA stops.
+      if (failed_at >= 0)
+        for (int k = failed_at; k < min(n_my, failed_at + C::STAGES); ++k)
+          mbar_wait(d, &ring.full[(loads + k) % C::STAGES], ((loads + k) / C::STAGES) & 1);
+      return;
+    }
+    loads += n_my;
+    const UnitSeg cur = seg;
+    const bool more = cur.end < u_end;
+    // The next segment's first pages are on their way while this one is merged.
+    if (more) {
+      seg = unit_segment(d, cur.end, u_end);
+      ring.open(d, layer, seg, warp);
+      for (int k = 0; k < min(C::STAGES, ring.n_my); ++k) ring.issue(k, loads + k, policy, lane);
+    }
+    if (warp < G) {
+      float m = -INFINITY, l = 0.f;
+      if (lane < C::WARPS) {
+        const float2 ml = state_ml[lane * G + warp];
+        m = ml.x;
+        l = ml.y;
+      }
+      float M = m;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(FULL, M, o));
+      const float w = weight2(m, M, s_scale[warp]);
+      float L = l * w;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(FULL, L, o);
+      if (lane < C::WARPS) weight[lane * G + warp] = w;
+      if (lane == 0) total[warp] = make_float2(M, L);
+    }
+    __syncthreads();
+    const bool whole = cur.whole();
+    const int slot = 2 * cta + (cur.u == u_begin ? 0 : 1);
+    T* orow = out + ((size_t)cur.si.q_row0 * d.q_heads + cur.head * G) * D;
+    for (int e = tid; e < E; e += C::THREADS) {
+      const int h = e / D;
+      float o = 0.f;
+#pragma unroll
+      for (int w = 0; w < C::WARPS; ++w) o += state_o[w * E + e] * weight[w * G + h];
+      if (whole) orow[e] = from_float<T>(o * (16.f / total[h].y));
+      else d.dec_part_o[(size_t)slot * E + e] = o;
+    }
+    if (!whole) {
+      if (tid < G) d.dec_part_ml[(size_t)slot * G + tid] = total[tid];
+      // The CTAs cf..cl own the pair's units; the last of them to arrive merges.
+      const int cf = us.owner(cur.pair_start), cl = us.owner(cur.pair_end - 1);
+      const int parts = cl - cf + 1;
+      int* counter = &d.dec_count[cur.seq * H + cur.head];
+      __syncthreads();
+      if (tid == 0) s_last = arrive_acq_rel(counter, parts);
+      __syncthreads();
+      if (s_last) {
+        const int first_slot = us.slot_of(cf, cf, cur.pair_start);
+        merge_parts<C>(d.dec_part_o, d.dec_part_ml, parts,
+                       [&](int i) { return i ? 2 * (cf + i) : first_slot; }, s_scale, weight, orow,
+                       tid);
+        if (tid == 0) *counter = 0;
+      }
+    }
+    if (!more) break;
+    __syncthreads();
+  }
+}
+
+template <typename T, int D>
+using Narrow = Cfg<T, D, 4, 4>;
+template <typename T, int D>
+using Wide = Cfg<T, D, 16, 2>;
+
+template <class C>
+cudaError_t grid_of(int sms, int dec_slots, int* grid) {
+  const void* fn = reinterpret_cast<const void*>(&decode_kv4_kernel<C>);
+  cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  int per_sm = 0;
+  if (e == cudaSuccess)
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, fn, C::THREADS, C::SMEM);
+  // Every CTA of the split may write two partial states.
+  *grid = min(per_sm * sms, dec_slots / 2);
+  return e;
+}
+
+template <class C>
+cudaError_t launch(const Dev& d, int layer, const void* q, void* out, int grid, int min_units,
+                   int parts, bool early, cudaStream_t s) {
+  using T = typename C::T;
+  return launch_ex(&decode_kv4_kernel<C>, dim3(grid), dim3(C::THREADS), C::SMEM, s, true, d, layer,
+                   static_cast<const T*>(q), static_cast<T*>(out), min_units, parts,
+                   (int)early);
+}
+
+template <typename T, int D>
+cudaError_t launch_any(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
+                       int64_t units, bool early, cudaStream_t s) {
+  const char* w = getenv("KV4_WIDE");
+  const bool wide = w ? atoi(w) : units <= 16 * 16 * lim.kv4_decode_wide;
+  if (wide)
+    return launch<Wide<T, D>>(d, layer, q, out, lim.kv4_decode_wide, 16, MAX_PARTS, early, s);
+  return launch<Narrow<T, D>>(d, layer, q, out, lim.kv4_decode, 8, MAX_PARTS, early, s);
+}
+
+template <typename T, int D>
+cudaError_t limits_of(int dec_slots, Limits* lim) {
+  const cudaError_t e = grid_of<Narrow<T, D>>(lim->sms, dec_slots, &lim->kv4_decode);
+  return e != cudaSuccess ? e : grid_of<Wide<T, D>>(lim->sms, dec_slots, &lim->kv4_decode_wide);
+}
+
+}  // namespace
+
+cudaError_t kv4_decode_limits(const Dev& d, Limits* lim) {
+  return d.esz == 2 ? limits_of<__nv_bfloat16, 128>(d.dec_slots, lim)
+                    : limits_of<float, 64>(d.dec_slots, lim);
+}
+
+cudaError_t launch_decode_kv4(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
+                              int64_t units, bool early, cudaStream_t s) {
+  return d.esz == 2 ? launch_any<__nv_bfloat16, 128>(d, lim, layer, q, out, units, early, s)
+                    : launch_any<float, 64>(d, lim, layer, q, out, units, early, s);
+}
+
+}  // namespace kvc

@@ -100,8 +100,8 @@ __global__ void __launch_bounds__(THREADS) evict_copy_kv4_kernel(Dev d) {
     const int ss = mv.x % PS, ds = mv.y % PS;
     const uint8_t* src = d.pool + tile_at(D, d.layers, d.kv_heads, mv.x / PS, layer, h, kv);
     uint8_t* dst = d.pool + tile_at(D, d.layers, d.kv_heads, mv.y / PS, layer, h, kv);
-    const int so = kv ? v_piece(D, ss, p) : k_codes(D, ss, p * (D / 8));
-    const int to = kv ? v_piece(D, ds, p) : k_codes(D, ds, p * (D / 8));
+    const int so = kv ? v_piece(D, ss, p) : k_piece(D, ss, p);
+    const int to = kv ? v_piece(D, ds, p) : k_piece(D, ds, p);
     if constexpr (D == 128)
       *reinterpret_cast<uint2*>(dst + to) = *reinterpret_cast<const uint2*>(src + so);
     else

@@ -54,7 +54,7 @@ struct Limits {
   int pf_stream_k;                 // CTAs of the stream-K prefill (bfloat16)
   int pf_clusters[PF_MAX_SLICES + 1];  // [k] clusters of k CTAs of the prefill's pair split
   int f32_cluster[2][2];           // largest cluster of the binary32 prefill: [rows][spread]
-  int kv4_decode;                  // CTAs of the decode over 4-bit rows
+  int kv4_decode, kv4_decode_wide; // CTAs of the decode over 4-bit rows, of 4 and of 16 warps
   int kv4_prefill[KV4_PF_WARPS + 1];  // [w] CTAs of the prefill with w warps to a page
 };
 cudaError_t query_limits(const Dev& d, Limits* lim);
@@ -79,20 +79,24 @@ cudaError_t launch_transcript(const Dev& d, bool kv4, int session, int cap, int3
 cudaError_t launch_read_kv(const Dev& d, bool kv4, const ReadArgs& a, int layer0, int n_layers,
                            void* k_out, void* v_out, int64_t* resident_out, int sms,
                            cudaStream_t s);
-// The parts of those calls that touch 4-bit rows (kvc_kv4_rows.cu), and the attention over them
-// (kvc_kv4_attn.cu): chunks of up to max_t tokens.
+// The parts of those calls that touch 4-bit rows (kvc_kv4_rows.cu), and the attention over them.
 cudaError_t launch_append_layers_kv4(const Dev& d, int total, int layer0, int n_layers,
                                      const void* k, const void* v, bool after_plan,
                                      cudaStream_t s);
 cudaError_t launch_evict_copy_kv4(const Dev& d, int sms, cudaStream_t s);
 cudaError_t launch_transcript_copy_kv4(const Dev& d, int cap, void* k_out, void* v_out, int sms,
                                        cudaStream_t s);
-cudaError_t kv4_limits(int esz, Limits* lim);  // sets its attributes
-// new_k / new_v (optional): the layer's rows of the append, written first.  Asks `order` when it may
-// read early, and reports its launches to it.
+// new_k / new_v (optional): the layer's rows of the append, written first.  Chunks of up to max_t
+// tokens; units: estimate of the call's (session, KV head, page) units, for the choice of the shape
+// only.  Asks `order` when it may read early, and reports its launches to it.
 cudaError_t launch_attn_kv4(const Dev& d, const Limits& lim, LaunchOrder* order, int layer,
                             const void* new_k, const void* new_v, const void* q, void* out,
-                            int total, int max_t, cudaStream_t s);
+                            int total, int max_t, int64_t units, cudaStream_t s);
+// Single tokens (kvc_kv4_decode.cu).
+cudaError_t launch_decode_kv4(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
+                              int64_t units, bool early, cudaStream_t s);
+cudaError_t kv4_decode_limits(const Dev& d, Limits* lim);  // both set their kernels' attributes
+cudaError_t kv4_prefill_limits(const Dev& d, Limits* lim);
 // Attention launches may start while the kernel before them in the stream finishes.  early:
 // they may also read what the append wrote before that (an attention launch of the same
 // append came before, so the append is complete).

@@ -39,11 +39,10 @@ int main() {
           const int at = kv ? v_scale(D, slot, g) : k_scale(D, slot, g);
           if (at % 2 || !take(at, slot) || !take(at + 1, slot)) return 3;
         }
-        // The pieces that an eviction moves are the row's codes in order.
-        for (int g = 0; g < 8; ++g)
-          if ((kv ? v_piece(D, slot, g) : k_codes(D, slot, g * (D / 8))) !=
-              (kv ? v_codes(D, slot, g * (D / 8)) : slot * (D / 2) + g * (D / 16)))
-            return 4;
+        // The pieces that an eviction moves are the row's codes.
+        for (int p = 0; p < 8; ++p)
+          for (int i = 0; i < D / 16; ++i)
+            if (owner[(kv ? v_piece(D, slot, p) : k_piece(D, slot, p)) + i] != slot) return 4;
       }
       for (int o : owner)
         if (o < 0) return 5;
@@ -54,7 +53,8 @@ int main() {
           if (v_piece(D, 2 * t + 1, g) != v_piece(D, 2 * t, g) + D / 16) return 7;
           if (v_piece(D, 2 * t + 8, g) != v_piece(D, 2 * t, g) + 4 * D) return 8;
           if (v_scale(D, 2 * t + 1, 0) != v_scale(D, 2 * t, 0) + 2 || v_scale(D, 2 * t, 0) % 4) return 9;
-          if (k_codes(D, g, t * (D / 4)) != g * (D / 2) + t * (D / 8)) return 10;
+          for (int w = 0; w < D / 32; ++w)
+            if (k_codes(D, g, 32 * w + 8 * t) != g * (D / 2) + t * (D / 8) + 4 * w) return 10;
         }
     }
   // Tiles do not overlap, K and V of a head side by side, 16-byte aligned, past 32 bits too.
