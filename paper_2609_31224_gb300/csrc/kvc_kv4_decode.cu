@@ -32,7 +32,7 @@ constexpr float P_SHIFT = 8.f;     // log2 of the weight P of a key at the refer
 constexpr float P_LAG = 6.f;       // and of how far above it a weight may be: 2^14 in all
 constexpr int MAX_PARTS = 64;      // CTAs that share a (session, KV head) pair, at most
 
-// Shape of a CTA: WARPS warps, each with its own ring of STAGES pages.
+// Shape of a CTA: WARPS warps, each with its own ring of STAGES pairs of pages.
 template <typename T_, int D_, int WARPS_, int STAGES_>
 struct Cfg {
   using T = T_;
@@ -44,7 +44,7 @@ struct Cfg {
   static constexpr int VW = D / 64;                // and of V codes per lane and row
   static constexpr int MT = D / 16;                // row tiles of O^T
   // Shared memory: rings, the warps' states, weights of parts, barriers.
-  static constexpr int RING = WARPS * STAGES * PAGE;
+  static constexpr int RING = WARPS * STAGES * 2 * PAGE;
   static constexpr int STATE_O = RING;                          // [WARPS][G][D] floats
   static constexpr int STATE_ML = STATE_O + WARPS * G * D * 4;  // [WARPS][G] (m, l)
   static constexpr int WEIGHT = STATE_ML + WARPS * G * 8;       // [max(WARPS, MAX_PARTS)][G]
@@ -172,107 +172,71 @@ struct State {
   float m, l;
 };
 
+// Scores of keys g and g + 8 of a page for head t.
 template <class C>
-__device__ inline void page_step(const uint32_t page, const Query<C>& qr, bool open,
-                                 const SeqInfo& si, int blk, State<C>& st, int lane) {
-  constexpr int D = C::D, KW = C::KW, VW = C::VW;
+__device__ inline void page_scores(uint32_t kt, const Query<C>& qr, int lane, float& s0, float& s1) {
+  constexpr int D = C::D, KW = C::KW;
   const int g = lane >> 2, t = lane & 3;
-  const uint32_t kt = page, vt = page + 9 * D;
+  uint32_t wa[KW], wb[KW], ma[KW / 2], mb[KW / 2];
+  lds(kt + g * (D / 2) + t * (D / 8), wa);
+  lds(kt + (g + 8) * (D / 2) + t * (D / 8), wb);
+  lds(kt + k_scale(D, g, 0), ma);
+  lds(kt + k_scale(D, g + 8, 0), mb);
+  float x[KW][4];
   const __half2 m72 = __float2half2_rn(-72.f);
-
-  float s0, s1;  // scores of keys g and g + 8
-  {
-    uint32_t wa[KW], wb[KW], ma[KW / 2], mb[KW / 2];
-    lds(kt + g * (D / 2) + t * (D / 8), wa);
-    lds(kt + (g + 8) * (D / 2) + t * (D / 8), wb);
-    lds(kt + k_scale(D, g, 0), ma);
-    lds(kt + k_scale(D, g + 8, 0), mb);
-    float x[KW][4];
-    if constexpr (C::SCALE_BEHIND) {
-      // Nibbles as they are: bits 0..3 of a half are n 2^-24, bits 4..7 n 2^-20.
+  if constexpr (C::SCALE_BEHIND) {
+    // Nibbles as they are: bits 0..3 of a half are n 2^-24, bits 4..7 n 2^-20.
 #pragma unroll
-      for (int w = 0; w < KW; ++w) {
-        const uint32_t ha = wa[w] >> 8, hb = wb[w] >> 8;
-        mma_f16(x[w], wa[w] & 0x000F000Fu, wb[w] & 0x000F000Fu, wa[w] & 0x00F000F0u,
-                wb[w] & 0x00F000F0u, qr.b[w][0], qr.b[w][1], qr.zero[w]);
-        mma_f16(x[w], ha & 0x000F000Fu, hb & 0x000F000Fu, ha & 0x00F000F0u, hb & 0x00F000F0u,
-                qr.b[w][2], qr.b[w][3]);
-      }
-      s0 = s1 = 0.f;
+    for (int w = 0; w < KW; ++w) {
+      const uint32_t ha = wa[w] >> 8, hb = wb[w] >> 8;
+      mma_f16(x[w], wa[w] & 0x000F000Fu, wb[w] & 0x000F000Fu, wa[w] & 0x00F000F0u,
+              wb[w] & 0x00F000F0u, qr.b[w][0], qr.b[w][1], qr.zero[w]);
+      mma_f16(x[w], ha & 0x000F000Fu, hb & 0x000F000Fu, ha & 0x00F000F0u, hb & 0x00F000F0u,
+              qr.b[w][2], qr.b[w][3]);
+    }
+    s0 = s1 = 0.f;
 #pragma unroll
-      for (int w = 0; w < KW; ++w) {
-        const float2 a = __half22float2(bits_h2(ma[w / 2])), b = __half22float2(bits_h2(mb[w / 2]));
-        s0 = fmaf(x[w][0] + x[w][1], w % 2 ? a.y : a.x, s0);
-        s1 = fmaf(x[w][2] + x[w][3], w % 2 ? b.y : b.x, s1);
-      }
-    } else {
-      // Exact values of the keys, and a sum for every 16 dims: the tensor cores cut off what they
-      // add to an accumulator.
-      float z[KW][4];
+    for (int w = 0; w < KW; ++w) {
+      const float2 a = __half22float2(bits_h2(ma[w / 2])), b = __half22float2(bits_h2(mb[w / 2]));
+      s0 = fmaf(x[w][0] + x[w][1], w % 2 ? a.y : a.x, s0);
+      s1 = fmaf(x[w][2] + x[w][3], w % 2 ? b.y : b.x, s1);
+    }
+  } else {
+    // Exact values of the keys, and a sum for every 16 dims: the tensor cores cut off what they
+    // add to an accumulator.
+    float z[KW][4];
 #pragma unroll
-      for (int w = 0; w < KW; ++w) {
-        const uint32_t da = __byte_perm(ma[w / 2], 0, w % 2 ? 0x3232u : 0x1010u);
-        const uint32_t db = __byte_perm(mb[w / 2], 0, w % 2 ? 0x3232u : 0x1010u);
-        uint32_t a[4], b[4];
-        pairs_of(wa[w], bits_h2(da), __hmul2(bits_h2(da), m72), a);
-        pairs_of(wb[w], bits_h2(db), __hmul2(bits_h2(db), m72), b);
-        x[w][0] = x[w][1] = x[w][2] = x[w][3] = z[w][0] = z[w][1] = z[w][2] = z[w][3] = 0.f;
-        mma_f16(x[w], a[0], b[0], a[1], b[1], qr.b[w][0], qr.b[w][1]);
-        mma_f16(z[w], a[2], b[2], a[3], b[3], qr.b[w][2], qr.b[w][3]);
-      }
-      s0 = s1 = 0.f;
+    for (int w = 0; w < KW; ++w) {
+      const uint32_t da = __byte_perm(ma[w / 2], 0, w % 2 ? 0x3232u : 0x1010u);
+      const uint32_t db = __byte_perm(mb[w / 2], 0, w % 2 ? 0x3232u : 0x1010u);
+      uint32_t a[4], b[4];
+      pairs_of(wa[w], bits_h2(da), __hmul2(bits_h2(da), m72), a);
+      pairs_of(wb[w], bits_h2(db), __hmul2(bits_h2(db), m72), b);
+      x[w][0] = x[w][1] = x[w][2] = x[w][3] = z[w][0] = z[w][1] = z[w][2] = z[w][3] = 0.f;
+      mma_f16(x[w], a[0], b[0], a[1], b[1], qr.b[w][0], qr.b[w][1]);
+      mma_f16(z[w], a[2], b[2], a[3], b[3], qr.b[w][2], qr.b[w][3]);
+    }
+    s0 = s1 = 0.f;
 #pragma unroll
-      for (int w = 0; w < KW; ++w) {
-        s0 += x[w][1] + z[w][1];
-        s1 += x[w][3] + z[w][3];
-      }
+    for (int w = 0; w < KW; ++w) {
+      s0 += x[w][1] + z[w][1];
+      s1 += x[w][3] + z[w][3];
+    }
 #pragma unroll
-      for (int w = 0; w < KW; ++w) {
-        s0 += x[w][0] + z[w][0];
-        s1 += x[w][2] + z[w][2];
-      }
+    for (int w = 0; w < KW; ++w) {
+      s0 += x[w][0] + z[w][0];
+      s1 += x[w][2] + z[w][2];
     }
   }
-  BlockRange br;
-  if (!open) {
-    br = block_range(si, blk);
-    if (g < br.lo || g >= br.hi) s0 = -INFINITY;
-    if (g + 8 < br.lo || g + 8 >= br.hi) s1 = -INFINITY;
-  }
-  float a0 = fmaf(s0 - st.m, qr.c, P_SHIFT), a1 = fmaf(s1 - st.m, qr.c, P_SHIFT);
-  // (At the first page m is -infinity: every valid key asks for a new reference.)
-  if (__any_sync(FULL, fmaxf(a0, a1) > P_SHIFT + P_LAG)) {
-    float mx = fmaxf(s0, s1);
-#pragma unroll
-    for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(FULL, mx, off));
-    const float mn = fmaxf(st.m, mx);
-    const float alpha = weight2(st.m, mn, qr.c);
-    st.l *= alpha;
-#pragma unroll
-    for (int mt = 0; mt < C::MT; ++mt)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) st.o[mt][j] *= alpha;
-    st.m = mn;
-    a0 = fmaf(s0 - mn, qr.c, P_SHIFT);
-    a1 = fmaf(s1 - mn, qr.c, P_SHIFT);
-  }
-  if (!open) {
-    // (Where no key was valid so far s - m is no number.)
-    if (s0 == -INFINITY) a0 = -INFINITY;
-    if (s1 == -INFINITY) a1 = -INFINITY;
-  }
-  const float p0 = ex2(a0), p1 = ex2(a1);
-  st.l += p0 + p1;
-  uint32_t b0, b1;
-  if constexpr (C::SPLIT_P) {
-    const float h0 = __half2float(__float2half_rn(p0)), h1 = __half2float(__float2half_rn(p1));
-    b0 = transpose8(h2_bits(__floats2half2_rn(h0, p0 - h0)));
-    b1 = transpose8(h2_bits(__floats2half2_rn(h1, p1 - h1)));
-  } else {
-    b0 = transpose8(h2_bits(__floats2half2_rn(p0, 0.f)));
-    b1 = transpose8(h2_bits(__floats2half2_rn(p1, 0.f)));
-  }
+}
 
+// O^T += V^T P^T of a page; b0, b1: P^T of rows 2t, 2t + 1 and 2t + 8, 2t + 9 for column g.
+template <class C>
+__device__ inline void page_values(uint32_t vt, uint32_t b0, uint32_t b1, bool open,
+                                   const BlockRange& br, State<C>& st, int lane) {
+  constexpr int D = C::D, VW = C::VW;
+  const int g = lane >> 2, t = lane & 3;
+  const __half2 m72 = __float2half2_rn(-72.f);
   // V^T: lane (g, t) takes piece g of rows 2t, 2t + 1 (lo) and 2t + 8, 2t + 9 (hi).
   uint32_t lo[2 * VW], hi[2 * VW], sl, sh;  // [row of the pair][word]
   lds(vt + lane * (D / 8), lo);
@@ -317,6 +281,83 @@ __device__ inline void page_step(const uint32_t page, const Query<C>& qr, bool o
     }
 }
 
+// Weights of two keys (g and g + 8 of a page) as the B operand of page_values; adds them to l.
+template <class C>
+__device__ inline void weights_of(float a0, float a1, float& l, uint32_t& b0, uint32_t& b1) {
+  const float p0 = ex2(a0), p1 = ex2(a1);
+  l += p0 + p1;
+  if constexpr (C::SPLIT_P) {
+    const float h0 = __half2float(__float2half_rn(p0)), h1 = __half2float(__float2half_rn(p1));
+    b0 = transpose8(h2_bits(__floats2half2_rn(h0, p0 - h0)));
+    b1 = transpose8(h2_bits(__floats2half2_rn(h1, p1 - h1)));
+  } else {
+    b0 = transpose8(h2_bits(__floats2half2_rn(p0, 0.f)));
+    b1 = transpose8(h2_bits(__floats2half2_rn(p1, 0.f)));
+  }
+}
+
+// N pages (in shared memory at `at`, blocks blk and blk + WARPS): scores, running softmax, P V.
+template <class C, int N>
+__device__ inline void pages_step(uint32_t at, const Query<C>& qr, const OpenPages& pages,
+                                  const SeqInfo& si, int blk, State<C>& st, int lane) {
+  const int g = lane >> 2;
+  float s[N][2];
+  bool open[N];
+  BlockRange br[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    page_scores<C>(at + i * C::PAGE, qr, lane, s[i][0], s[i][1]);
+    open[i] = pages.has(blk + i * C::WARPS);
+    if (!open[i]) {
+      br[i] = block_range(si, blk + i * C::WARPS);
+      if (g < br[i].lo || g >= br[i].hi) s[i][0] = -INFINITY;
+      if (g + 8 < br[i].lo || g + 8 >= br[i].hi) s[i][1] = -INFINITY;
+    }
+  }
+  float a[N][2], most = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      a[i][j] = fmaf(s[i][j] - st.m, qr.c, P_SHIFT);
+      most = fmaxf(most, a[i][j]);
+    }
+  // (At the first page m is -infinity: every valid key asks for a new reference.)
+  if (__any_sync(FULL, most > P_SHIFT + P_LAG)) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < N; ++i) mx = fmaxf(mx, fmaxf(s[i][0], s[i][1]));
+#pragma unroll
+    for (int off = 4; off < 32; off <<= 1) mx = fmaxf(mx, __shfl_xor_sync(FULL, mx, off));
+    const float mn = fmaxf(st.m, mx);
+    const float alpha = weight2(st.m, mn, qr.c);
+    st.l *= alpha;
+#pragma unroll
+    for (int mt = 0; mt < C::MT; ++mt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) st.o[mt][j] *= alpha;
+    st.m = mn;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) a[i][j] = fmaf(s[i][j] - mn, qr.c, P_SHIFT);
+  }
+  uint32_t b[N][2];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (!open[i]) {
+      // (Where no key was valid so far s - m is no number.)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (s[i][j] == -INFINITY) a[i][j] = -INFINITY;
+    }
+    weights_of<C>(a[i][0], a[i][1], st.l, b[i][0], b[i][1]);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    page_values<C>(at + i * C::PAGE + 9 * C::D, b[i][0], b[i][1], open[i], br[i], st, lane);
+}
+
 // The pages of one warp and segment (every WARPS-th block), through the warp's ring.
 template <class C>
 struct Ring {
@@ -339,19 +380,23 @@ struct Ring {
     win = -32;
     pid = 0;
   }
-  // Copy the warp's k-th page in, as its n-th of the launch; the whole warp.
+  __device__ int steps() const { return (n_my + 1) / 2; }
+  // Copy the warp's k-th pair of pages in, as its n-th of the launch; the whole warp.
   __device__ void issue(int k, uint32_t n, uint64_t policy, int lane) {
-    if (k >= win + 32) {
-      win = k & ~31;
+    if (2 * k >= win + 32) {
+      win = (2 * k) & ~31;
       const int j = win + lane, b = first + j * C::WARPS;
       pid = j < n_my ? (b < n_hist_pages ? hrow[b] : lrow[b - n_hist_pages]) : 0;
     }
-    const int page = __shfl_sync(FULL, pid, k - win);
+    const int p0 = __shfl_sync(FULL, pid, 2 * k - win), p1 = __shfl_sync(FULL, pid, 2 * k + 1 - win);
     if (lane == 0) {
       const uint32_t st = n % C::STAGES;
+      uint8_t* to = slots + st * 2 * C::PAGE;
+      const bool two = 2 * k + 1 < n_my;
       fence_proxy_async_smem();
-      mbar_arrive_expect_tx(&full[st], C::PAGE);
-      bulk_g2s_hint(slots + st * C::PAGE, tiles + page * page_stride, C::PAGE, &full[st], policy);
+      mbar_arrive_expect_tx(&full[st], two ? 2 * C::PAGE : C::PAGE);
+      bulk_g2s_hint(to, tiles + p0 * page_stride, C::PAGE, &full[st], policy);
+      if (two) bulk_g2s_hint(to + C::PAGE, tiles + p1 * page_stride, C::PAGE, &full[st], policy);
     }
   }
 };
@@ -438,7 +483,7 @@ __global__ void __launch_bounds__(C::THREADS, C::WARPS == 4 ? 4 : 1) decode_kv4_
   float* weight = reinterpret_cast<float*>(smem + C::WEIGHT);
   float2* total = reinterpret_cast<float2*>(smem + C::TOTAL);
   Ring<C> ring;
-  ring.slots = smem + warp * C::STAGES * C::PAGE;
+  ring.slots = smem + warp * C::STAGES * 2 * C::PAGE;
   ring.full = reinterpret_cast<uint64_t*>(smem + C::BARS) + warp * C::STAGES;
   ring.page_stride = page_bytes(D, d.layers, d.kv_heads);
   if (lane == 0) {
@@ -461,10 +506,10 @@ __global__ void __launch_bounds__(C::THREADS, C::WARPS == 4 ? 4 : 1) decode_kv4_
   if (u_begin >= u_end) return;
   const uint64_t policy = evict_first_policy();
   const uint32_t slots = smem_u32(ring.slots);
-  uint32_t loads = 0;  // pages of this warp, over all segments before
+  uint32_t loads = 0;  // steps of this warp, over all segments before
   UnitSeg seg = unit_segment(d, u_begin, u_end);
   ring.open(d, layer, seg, warp);
-  for (int k = 0; k < min(C::STAGES, ring.n_my); ++k) ring.issue(k, k, policy, lane);
+  for (int k = 0; k < min(C::STAGES, ring.steps()); ++k) ring.issue(k, k, policy, lane);
 
   for (;;) {
     const SeqInfo& si = seg.si;
@@ -480,18 +525,20 @@ __global__ void __launch_bounds__(C::THREADS, C::WARPS == 4 ? 4 : 1) decode_kv4_
 #pragma unroll
     for (int mt = 0; mt < C::MT; ++mt) st.o[mt][0] = st.o[mt][1] = st.o[mt][2] = st.o[mt][3] = 0.f;
     const OpenPages open(si);
-    const int n_my = ring.n_my;
+    const int n_my = ring.n_my, n_steps = ring.steps();
     int failed_at = -1;
-    for (int k = 0; k < n_my; ++k) {
+    for (int k = 0; k < n_steps; ++k) {
       const uint32_t n = loads + k, stage = n % C::STAGES;
       if (!__all_sync(FULL, mbar_wait(d, &ring.full[stage], (n / C::STAGES) & 1))) {
         failed_at = k;
         break;
       }
-      const int blk = ring.first + k * C::WARPS;
-      page_step<C>(slots + stage * C::PAGE, qr, open.has(blk), si, blk, st, lane);
+      const uint32_t at = slots + stage * 2 * C::PAGE;
+      const int blk = ring.first + 2 * k * C::WARPS;
+      if (2 * k + 1 < n_my) pages_step<C, 2>(at, qr, open, si, blk, st, lane);
+      else pages_step<C, 1>(at, qr, open, si, blk, st, lane);
       __syncwarp();
-      if (k + C::STAGES < n_my) ring.issue(k + C::STAGES, n + C::STAGES, policy, lane);
+      if (k + C::STAGES < n_steps) ring.issue(k + C::STAGES, n + C::STAGES, policy, lane);
     }
     if (failed_at >= 0 && lane == 0) s_abort = 1;
 
@@ -520,18 +567,18 @@ __global__ void __launch_bounds__(C::THREADS, C::WARPS == 4 ? 4 : 1) decode_kv4_
       // A wait gave up: each warp drains the copies that it still has in flight (bounded), then the
       // whole CTA stops.
       if (failed_at >= 0)
-        for (int k = failed_at; k < min(n_my, failed_at + C::STAGES); ++k)
+        for (int k = failed_at; k < min(n_steps, failed_at + C::STAGES); ++k)
           mbar_wait(d, &ring.full[(loads + k) % C::STAGES], ((loads + k) / C::STAGES) & 1);
       return;
     }
-    loads += n_my;
+    loads += n_steps;
     const UnitSeg cur = seg;
     const bool more = cur.end < u_end;
     // The next segment's first pages are on their way while this one is merged.
     if (more) {
       seg = unit_segment(d, cur.end, u_end);
       ring.open(d, layer, seg, warp);
-      for (int k = 0; k < min(C::STAGES, ring.n_my); ++k) ring.issue(k, loads + k, policy, lane);
+      for (int k = 0; k < min(C::STAGES, ring.steps()); ++k) ring.issue(k, loads + k, policy, lane);
     }
     if (warp < G) {
       float m = -INFINITY, l = 0.f;
@@ -585,9 +632,9 @@ __global__ void __launch_bounds__(C::THREADS, C::WARPS == 4 ? 4 : 1) decode_kv4_
 }
 
 template <typename T, int D>
-using Narrow = Cfg<T, D, 4, 4>;
+using Narrow = Cfg<T, D, 4, 2>;
 template <typename T, int D>
-using Wide = Cfg<T, D, 16, 2>;
+using Wide = Cfg<T, D, 16, 1>;
 
 template <class C>
 cudaError_t grid_of(int sms, int dec_slots, int* grid) {
