@@ -287,8 +287,8 @@ int attend_kv4(kvc_ctx* ctx, int layer, const void* k, const void* v, const void
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   bool capturing = false;
   KVC_CUDA(is_capturing(s, &capturing));
-  KVC_CUDA(launch_attn_kv4(ctx->d, ctx->lim, &ctx->order, layer, k, v, q, out, ctx->last_total,
-                           ctx->last_max_t, page_hint(ctx, capturing).sum * ctx->cfg.kv_heads, s));
+  KVC_CUDA(launch_attn_kv4(ctx->d, ctx->lim, &ctx->order, layer, k, v, q, out, ctx->last_n_seq,
+                           ctx->last_total, ctx->last_max_t, page_hint(ctx, capturing).sum * ctx->cfg.kv_heads, s));
   return KVC_OK;
 }
 

@@ -27,12 +27,13 @@ __device__ inline float scale_of(uint32_t most) {
 }
 __device__ inline __half stored_scale(float s) { return __float2half_rn(s * 0.0625f); }
 
-// Nibbles of 8 elements of a group of scale s (rounded to nearest, ties to even, of the quotient).
-__device__ inline uint32_t codes_of(const float (&x)[8], float s) {
+// Nibbles of N <= 8 elements of a group of scale s (rounded to nearest, ties to even, of the quotient).
+template <int N>
+__device__ inline uint32_t codes_of(const float (&x)[N], float s) {
   const float by = s > 0.f ? s : 1.f;
   uint32_t w = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < N; ++i) {
     const int c = max(-CODE_MAX, min(CODE_MAX, __float2int_rn(__fdiv_rn(x[i], by))));
     w |= (uint32_t)(c + 8) << (4 * i);
   }

@@ -692,20 +692,23 @@ cudaError_t kv4_prefill_limits(const Dev& d, Limits* lim) {
 
 cudaError_t launch_attn_kv4(const Dev& d, const Limits& lim, LaunchOrder* order, int layer,
                             const void* new_k, const void* new_v, const void* q, void* out,
-                            int total, int max_t, int64_t units, cudaStream_t s) {
-  if (new_k != nullptr) {
+                            int n_seq, int total, int max_t, int64_t units, cudaStream_t s) {
+  const bool fused = new_k != nullptr;
+  if (max_t == 1) {
+    const cudaError_t e = launch_decode_kv4(d, lim, layer, q, out, new_k, new_v, n_seq * d.kv_heads,
+                                            units, order->early(layer, fused), s);
+    if (e == cudaSuccess) order->launched(layer, fused);
+    return e;
+  }
+  if (fused) {
     const cudaError_t e = launch_append_layers_kv4(d, total, layer, 1, new_k, new_v, false, s);
     if (e != cudaSuccess) return e;
     order->layer_write(layer);
   }
   const bool early = order->early(layer, false);
-  cudaError_t e;
-  if (max_t == 1)
-    e = launch_decode_kv4(d, lim, layer, q, out, units, early, s);
-  else if (d.esz == 2)
-    e = launch_any<__nv_bfloat16, 128>(d, lim, layer, q, out, max_t, early, s);
-  else
-    e = launch_any<float, 64>(d, lim, layer, q, out, max_t, early, s);
+  const cudaError_t e =
+      d.esz == 2 ? launch_any<__nv_bfloat16, 128>(d, lim, layer, q, out, max_t, early, s)
+                 : launch_any<float, 64>(d, lim, layer, q, out, max_t, early, s);
   if (e == cudaSuccess) order->launched(layer, false);
   return e;
 }

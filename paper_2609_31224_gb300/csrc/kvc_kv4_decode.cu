@@ -17,6 +17,8 @@
 // pair of elements).  So everything else is kept small: the query's operands stay in registers, the
 // softmax reference lags (it moves only when a score passes it by 2^6), page lists are looked up 32
 // at a time, and only pages with masked slots look at their range.
+#include <algorithm>
+
 #include "kvc_kv4.cuh"
 
 namespace kvc {
@@ -358,6 +360,60 @@ __device__ inline void pages_step(uint32_t at, const Query<C>& qr, const OpenPag
     page_values<C>(at + i * C::PAGE + 9 * C::D, b[i][0], b[i][1], open[i], br[i], st, lane);
 }
 
+// The new token's K (rotated at its position) and V of this layer and head, from the caller's rows,
+// into their slot of the pool and of the page just loaded from it (whose copy may be older), as the
+// write kernel would have them.  By the warp that has the pair's last block.
+template <class C>
+__device__ void write_new_row(const Dev& d, int layer, const SeqInfo& si, int head,
+                              const typename C::T* nk, const typename C::T* nv, uint8_t* page,
+                              int lane) {
+  using T = typename C::T;
+  constexpr int D = C::D, HALF = D / 2, E = D / 32, LANES = GROUP / E;  // elements, lanes of a group
+  const int gs = d.tok_slot[si.q_row0], slot = gs % PS, d0 = lane * E;
+  const size_t row = ((size_t)si.q_row0 * d.kv_heads + head) * D;
+  float x[E], partner[E], y[2][E];
+  float2 cs[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    x[e] = to_float<T>(nk[row + d0 + e]);
+    partner[e] = to_float<T>(nk[row + (d0 ^ HALF) + e]);
+    y[1][e] = to_float<T>(nv[row + d0 + e]);
+    cs[e] = d.rope[(size_t)si.pos_first * HALF + (d0 & (HALF - 1)) + e];
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    float other;
+    if (d0 < HALF) turn_pair(x[e], partner[e], cs[e], y[0][e], other);
+    else turn_pair(partner[e], x[e], cs[e], other, y[0][e]);
+  }
+  uint8_t* tiles = d.pool + tile_at(D, d.layers, d.kv_heads, gs / PS, layer, head, 0);
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) most = max(most, abs_bits(y[kv][e]));
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1) most = max(most, __shfl_xor_sync(FULL, most, o));
+    const float s = scale_of(most);
+    const uint32_t codes = codes_of(y[kv], s);
+    const int at = kv * 9 * D + (kv ? v_codes(D, slot, d0 & ~7) : k_codes(D, slot, d0 & ~7)) +
+                   d0 % 8 / 2;
+    if constexpr (E == 4) {
+      *reinterpret_cast<uint16_t*>(tiles + at) = (uint16_t)codes;
+      *reinterpret_cast<uint16_t*>(page + at) = (uint16_t)codes;
+    } else {
+      tiles[at] = page[at] = (uint8_t)codes;
+    }
+    if (lane % LANES == 0) {
+      const int group = lane / LANES;
+      const int sc = kv * 9 * D + (kv ? v_scale(D, slot, group) : k_scale(D, slot, group));
+      *reinterpret_cast<__half*>(tiles + sc) = stored_scale(s);
+      *reinterpret_cast<__half*>(page + sc) = stored_scale(s);
+    }
+  }
+  __syncwarp();
+}
+
 // The pages of one warp and segment (every WARPS-th block), through the warp's ring.
 template <class C>
 struct Ring {
@@ -468,10 +524,29 @@ __device__ void merge_parts(const float* part_o, const float2* part_ml, int part
   }
 }
 
+// How a call's pages reach the CTAs: slices >= 1 cuts each (session, KV head) pair into as many
+// slices, one CTA each (no more than it has pages); 0 cuts the call's units evenly over the grid
+// (stream-K), at least min_units to a CTA.
+struct Cut {
+  int slices, min_units;
+};
+
+// Query rows and rotary row of a pair into L2 (what later loads observe does not depend on it).
 template <class C>
+__device__ inline void prefetch_query(const Dev& d, const SeqInfo& si, int head,
+                                      const typename C::T* q, int lane) {
+  constexpr int QL = G * C::D * (int)sizeof(typename C::T) / 128, RL = C::D * 4 / 128;
+  const uint8_t* qa = reinterpret_cast<const uint8_t*>(q + ((size_t)si.q_row0 * d.q_heads + head * G) * C::D);
+  const uint8_t* ra = reinterpret_cast<const uint8_t*>(d.rope + (size_t)si.pos_first * (C::D / 2));
+  if (lane < QL) prefetch_l2(qa + 128 * lane);
+  else if (lane >= 16 && lane < 16 + RL) prefetch_l2(ra + 128 * (lane - 16));
+}
+
+template <class C, bool FUSED>
 __global__ void __launch_bounds__(C::THREADS, C::WARPS == 4 ? 4 : 1) decode_kv4_kernel(
     Dev d, int layer, const typename C::T* __restrict__ q, typename C::T* __restrict__ out,
-    int min_units, int max_parts, int early) {
+    const typename C::T* __restrict__ new_k, const typename C::T* __restrict__ new_v, Cut cut,
+    int early) {
   using T = typename C::T;
   constexpr int D = C::D, E = G * D;
   extern __shared__ __align__(128) uint8_t smem[];
@@ -498,18 +573,36 @@ __global__ void __launch_bounds__(C::THREADS, C::WARPS == 4 ? 4 : 1) decode_kv4_
   pdl_launch_dependents();
   bool waited = false;
 
-  const int H = d.kv_heads;
-  const UnitSplit us = unit_split(d, gridDim.x, min_units, max_parts);
-  if ((int)blockIdx.x >= us.n_cta) return;
-  const int cta = blockIdx.x;
-  const int u_begin = us.start_of(cta), u_end = us.start_of(cta + 1);
-  if (u_begin >= u_end) return;
+  const int H = d.kv_heads, cta = blockIdx.x;
+  UnitSplit us = {};
+  UnitSeg seg;
+  int u_begin, u_end, slices = 0;
+  if (cut.slices > 0) {
+    const int pair = cta / cut.slices, slice = cta % cut.slices;
+    seg.seq = pair / H;
+    seg.head = pair % H;
+    seg.si = d.seq[seg.seq];
+    const int nb = seg.si.n_blocks;
+    slices = min(cut.slices, nb);
+    if (slice >= slices) return;
+    seg.pair_start = seg.si.unit_base + seg.head * nb;
+    seg.pair_end = seg.pair_start + nb;
+    seg.u = u_begin = seg.pair_start + (int)((int64_t)slice * nb / slices);
+    seg.end = u_end = seg.pair_start + (int)((int64_t)(slice + 1) * nb / slices);
+  } else {
+    us = unit_split(d, gridDim.x, cut.min_units, MAX_PARTS);
+    if (cta >= us.n_cta) return;
+    u_begin = us.start_of(cta);
+    u_end = us.start_of(cta + 1);
+    if (u_begin >= u_end) return;
+    seg = unit_segment(d, u_begin, u_end);
+  }
   const uint64_t policy = evict_first_policy();
   const uint32_t slots = smem_u32(ring.slots);
   uint32_t loads = 0;  // steps of this warp, over all segments before
-  UnitSeg seg = unit_segment(d, u_begin, u_end);
   ring.open(d, layer, seg, warp);
   for (int k = 0; k < min(C::STAGES, ring.steps()); ++k) ring.issue(k, k, policy, lane);
+  if (!waited && warp == 0) prefetch_query<C>(d, seg.si, seg.head, q, lane);
 
   for (;;) {
     const SeqInfo& si = seg.si;
@@ -535,6 +628,12 @@ __global__ void __launch_bounds__(C::THREADS, C::WARPS == 4 ? 4 : 1) decode_kv4_
       }
       const uint32_t at = slots + stage * 2 * C::PAGE;
       const int blk = ring.first + 2 * k * C::WARPS;
+      if constexpr (FUSED) {
+        const int last = si.n_blocks - 1;
+        if (blk == last || (blk + C::WARPS == last && 2 * k + 1 < n_my))
+          write_new_row<C>(d, layer, si, seg.head, new_k, new_v,
+                           ring.slots + (stage * 2 + (blk != last)) * C::PAGE, lane);
+      }
       if (2 * k + 1 < n_my) pages_step<C, 2>(at, qr, open, si, blk, st, lane);
       else pages_step<C, 1>(at, qr, open, si, blk, st, lane);
       __syncwarp();
@@ -599,7 +698,8 @@ __global__ void __launch_bounds__(C::THREADS, C::WARPS == 4 ? 4 : 1) decode_kv4_
     }
     __syncthreads();
     const bool whole = cur.whole();
-    const int slot = 2 * cta + (cur.u == u_begin ? 0 : 1);
+    // Slots of a pair's parts: its slices one after the other, or two of each CTA of the split.
+    const int slot = slices ? cta : 2 * cta + (cur.u == u_begin ? 0 : 1);
     T* orow = out + ((size_t)cur.si.q_row0 * d.q_heads + cur.head * G) * D;
     for (int e = tid; e < E; e += C::THREADS) {
       const int h = e / D;
@@ -611,18 +711,19 @@ __global__ void __launch_bounds__(C::THREADS, C::WARPS == 4 ? 4 : 1) decode_kv4_
     }
     if (!whole) {
       if (tid < G) d.dec_part_ml[(size_t)slot * G + tid] = total[tid];
-      // The CTAs cf..cl own the pair's units; the last of them to arrive merges.
-      const int cf = us.owner(cur.pair_start), cl = us.owner(cur.pair_end - 1);
-      const int parts = cl - cf + 1;
+      // The last CTA of the pair to arrive merges (stream-K: CTAs cf..cl own its units).
+      const int cf = slices ? cta - cta % cut.slices : us.owner(cur.pair_start);
+      const int parts = slices ? slices : us.owner(cur.pair_end - 1) - cf + 1;
       int* counter = &d.dec_count[cur.seq * H + cur.head];
       __syncthreads();
       if (tid == 0) s_last = arrive_acq_rel(counter, parts);
       __syncthreads();
       if (s_last) {
-        const int first_slot = us.slot_of(cf, cf, cur.pair_start);
+        const int first_slot = slices ? cf : us.slot_of(cf, cf, cur.pair_start);
+        const int next_slot = slices ? cf : 2 * cf, step = slices ? 1 : 2;
         merge_parts<C>(d.dec_part_o, d.dec_part_ml, parts,
-                       [&](int i) { return i ? 2 * (cf + i) : first_slot; }, s_scale, weight, orow,
-                       tid);
+                       [&](int i) { return i ? next_slot + step * i : first_slot; }, s_scale,
+                       weight, orow, tid);
         if (tid == 0) *counter = 0;
       }
     }
@@ -638,8 +739,11 @@ using Wide = Cfg<T, D, 16, 1>;
 
 template <class C>
 cudaError_t grid_of(int sms, int dec_slots, int* grid) {
-  const void* fn = reinterpret_cast<const void*>(&decode_kv4_kernel<C>);
+  const void* fn = reinterpret_cast<const void*>(&decode_kv4_kernel<C, false>);
   cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(reinterpret_cast<const void*>(&decode_kv4_kernel<C, true>),
+                             cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   int per_sm = 0;
   if (e == cudaSuccess)
     e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, fn, C::THREADS, C::SMEM);
@@ -649,22 +753,29 @@ cudaError_t grid_of(int sms, int dec_slots, int* grid) {
 }
 
 template <class C>
-cudaError_t launch(const Dev& d, int layer, const void* q, void* out, int grid, int min_units,
-                   int parts, bool early, cudaStream_t s) {
+cudaError_t launch(const Dev& d, int layer, const void* q, void* out, const void* new_k,
+                   const void* new_v, int grid, Cut cut, bool early, cudaStream_t s) {
   using T = typename C::T;
-  return launch_ex(&decode_kv4_kernel<C>, dim3(grid), dim3(C::THREADS), C::SMEM, s, true, d, layer,
-                   static_cast<const T*>(q), static_cast<T*>(out), min_units, parts,
-                   (int)early);
+  return launch_ex(new_k != nullptr ? &decode_kv4_kernel<C, true> : &decode_kv4_kernel<C, false>,
+                   dim3(grid), dim3(C::THREADS), C::SMEM, s, true, d, layer,
+                   static_cast<const T*>(q), static_cast<T*>(out), static_cast<const T*>(new_k),
+                   static_cast<const T*>(new_v), cut, (int)early);
 }
 
 template <typename T, int D>
 cudaError_t launch_any(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
-                       int64_t units, bool early, cudaStream_t s) {
+                       const void* new_k, const void* new_v, int n_pairs, int64_t units, bool early,
+                       cudaStream_t s) {
   const char* w = getenv("KV4_WIDE");
-  const bool wide = w ? atoi(w) : units <= 16 * 16 * lim.kv4_decode_wide;
-  if (wide)
-    return launch<Wide<T, D>>(d, layer, q, out, lim.kv4_decode_wide, 16, MAX_PARTS, early, s);
-  return launch<Narrow<T, D>>(d, layer, q, out, lim.kv4_decode, 8, MAX_PARTS, early, s);
+  const int mode = w ? atoi(w) : 0;
+  if (mode == 1) {
+    const int k = std::min(MAX_PARTS, lim.kv4_decode_wide / n_pairs);
+    if (k >= 1) return launch<Wide<T, D>>(d, layer, q, out, new_k, new_v, n_pairs * k, {k, 0}, early, s);
+  } else if (mode == 0) {
+    const int k = std::min(MAX_PARTS, lim.kv4_decode / n_pairs);
+    if (k >= 1) return launch<Narrow<T, D>>(d, layer, q, out, new_k, new_v, n_pairs * k, {k, 0}, early, s);
+  }
+  return launch<Narrow<T, D>>(d, layer, q, out, new_k, new_v, lim.kv4_decode, {0, 8}, early, s);
 }
 
 template <typename T, int D>
@@ -681,9 +792,11 @@ cudaError_t kv4_decode_limits(const Dev& d, Limits* lim) {
 }
 
 cudaError_t launch_decode_kv4(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
-                              int64_t units, bool early, cudaStream_t s) {
-  return d.esz == 2 ? launch_any<__nv_bfloat16, 128>(d, lim, layer, q, out, units, early, s)
-                    : launch_any<float, 64>(d, lim, layer, q, out, units, early, s);
+                              const void* new_k, const void* new_v, int n_pairs, int64_t units,
+                              bool early, cudaStream_t s) {
+  return d.esz == 2
+             ? launch_any<__nv_bfloat16, 128>(d, lim, layer, q, out, new_k, new_v, n_pairs, units, early, s)
+             : launch_any<float, 64>(d, lim, layer, q, out, new_k, new_v, n_pairs, units, early, s);
 }
 
 }  // namespace kvc

@@ -91,10 +91,11 @@ cudaError_t launch_transcript_copy_kv4(const Dev& d, int cap, void* k_out, void*
 // only.  Asks `order` when it may read early, and reports its launches to it.
 cudaError_t launch_attn_kv4(const Dev& d, const Limits& lim, LaunchOrder* order, int layer,
                             const void* new_k, const void* new_v, const void* q, void* out,
-                            int total, int max_t, int64_t units, cudaStream_t s);
-// Single tokens (kvc_kv4_decode.cu).
+                            int n_seq, int total, int max_t, int64_t units, cudaStream_t s);
+// Single tokens (kvc_kv4_decode.cu); with new_k / new_v their rows are written by the launch itself.
 cudaError_t launch_decode_kv4(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
-                              int64_t units, bool early, cudaStream_t s);
+                              const void* new_k, const void* new_v, int n_pairs, int64_t units,
+                              bool early, cudaStream_t s);
 cudaError_t kv4_decode_limits(const Dev& d, Limits* lim);  // both set their kernels' attributes
 cudaError_t kv4_prefill_limits(const Dev& d, Limits* lim);
 // Attention launches may start while the kernel before them in the stream finishes.  early:
