@@ -12,11 +12,15 @@
 // their sum is a score with about 22 bits of q, one softmax state per lane, no lane idle.  binary32
 // calls split P the same way; for bfloat16 the rounding of P to 11 bits stays.
 //
-// What bounds it: 18 D bytes a page against about 260 warp instructions, most of them the way from
-// nibble to operand (one AND-OR, a shift for three pairs of four, and a fused multiply-add for each
-// pair of elements).  So everything else is kept small: the query's operands stay in registers, the
-// softmax reference lags (it moves only when a score passes it by 2^6), page lists are looked up 32
-// at a time, and only pages with masked slots look at their range.
+// What bounds it: 18 D bytes a page (44.6 us for 64 sessions of 4,100 positions) against about 330
+// warp instructions, most of them the way from nibble to operand.  K's nibbles go in as they are (an
+// AND each: bits 0..3 and 4..7 of a half are binary16 numbers n 2^-24 and n 2^-20) with scale and
+// zero behind the product, which a group of 32 dims does not cross; V's take an AND-OR and one or two
+// products each.  The rest is kept small: the query's operands stay in registers, the softmax
+// reference lags (it moves only when a score passes it by 2^6), two pages make a step, page lists are
+// looked up 32 at a time, and only pages with masked slots look at their range.  64 sessions: 58.0 us
+// (77 % of the bytes' rate; 105 us as first written, 517 instructions), against 159 us for bfloat16
+// rows.  Issue is at about 60 % there; 16 warps an SM is what 128 registers leave.
 #include <algorithm>
 
 #include "kvc_kv4.cuh"
@@ -76,9 +80,7 @@ struct Query {
   // nibbles are read 16 times too large) over 16.
   uint32_t b[C::KW][4];
   float c;        // softmax scale of head t
-  // What a group's product starts from, -8 times the sum of its dims of head t: takes the 8 off the
-  // nibbles.
-  float zero[C::KW][4];
+  float zero[C::KW];  // -8 times the sum of a group's dims of head t: takes the 8 off its nibbles
 };
 
 constexpr int Q_EXP = 9;        // a row's largest element is in [2^9, 2^10)
@@ -148,9 +150,7 @@ __device__ inline void load_query(const Dev& d, const SeqInfo& si, int head, con
       z += __shfl_xor_sync(FULL, z, 1);
       z += __shfl_xor_sync(FULL, z, 2);
       z += __shfl_xor_sync(FULL, z, 4);               // both pieces
-      z = __shfl_sync(FULL, z, 8 * t) * (-8.f / (float)(1 << -RAW_EXP));
-      qr.zero[w][0] = qr.zero[w][2] = z;
-      qr.zero[w][1] = qr.zero[w][3] = 0.f;
+      qr.zero[w] = __shfl_sync(FULL, z, 8 * t) * (-8.f / (float)(1 << -RAW_EXP));
     }
   }
 }
@@ -187,12 +187,13 @@ __device__ inline void page_scores(uint32_t kt, const Query<C>& qr, int lane, fl
   float x[KW][4];
   const __half2 m72 = __float2half2_rn(-72.f);
   if constexpr (C::SCALE_BEHIND) {
+    const float none[4] = {0.f, 0.f, 0.f, 0.f};
     // Nibbles as they are: bits 0..3 of a half are n 2^-24, bits 4..7 n 2^-20.
 #pragma unroll
     for (int w = 0; w < KW; ++w) {
       const uint32_t ha = wa[w] >> 8, hb = wb[w] >> 8;
       mma_f16(x[w], wa[w] & 0x000F000Fu, wb[w] & 0x000F000Fu, wa[w] & 0x00F000F0u,
-              wb[w] & 0x00F000F0u, qr.b[w][0], qr.b[w][1], qr.zero[w]);
+              wb[w] & 0x00F000F0u, qr.b[w][0], qr.b[w][1], none);
       mma_f16(x[w], ha & 0x000F000Fu, hb & 0x000F000Fu, ha & 0x00F000F0u, hb & 0x00F000F0u,
               qr.b[w][2], qr.b[w][3]);
     }
@@ -200,8 +201,8 @@ __device__ inline void page_scores(uint32_t kt, const Query<C>& qr, int lane, fl
 #pragma unroll
     for (int w = 0; w < KW; ++w) {
       const float2 a = __half22float2(bits_h2(ma[w / 2])), b = __half22float2(bits_h2(mb[w / 2]));
-      s0 = fmaf(x[w][0] + x[w][1], w % 2 ? a.y : a.x, s0);
-      s1 = fmaf(x[w][2] + x[w][3], w % 2 ? b.y : b.x, s1);
+      s0 = fmaf(x[w][0] + qr.zero[w] + x[w][1], w % 2 ? a.y : a.x, s0);
+      s1 = fmaf(x[w][2] + qr.zero[w] + x[w][3], w % 2 ? b.y : b.x, s1);
     }
   } else {
     // Exact values of the keys, and a sum for every 16 dims: the tensor cores cut off what they
@@ -543,7 +544,7 @@ __device__ inline void prefetch_query(const Dev& d, const SeqInfo& si, int head,
 }
 
 template <class C, bool FUSED>
-__global__ void __launch_bounds__(C::THREADS, C::WARPS == 4 ? 4 : 1) decode_kv4_kernel(
+__global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
     Dev d, int layer, const typename C::T* __restrict__ q, typename C::T* __restrict__ out,
     const typename C::T* __restrict__ new_k, const typename C::T* __restrict__ new_v, Cut cut,
     int early) {
@@ -611,7 +612,7 @@ __global__ void __launch_bounds__(C::THREADS, C::WARPS == 4 ? 4 : 1) decode_kv4_
       waited = true;
     }
     Query<C> qr;
-    load_query<C>(d, si, seg.head, q, lane, qr);
+    if (ring.n_my > 0) load_query<C>(d, si, seg.head, q, lane, qr);  // (the first warp has a page)
     State<C> st;
     st.m = -INFINITY;
     st.l = 0.f;
@@ -735,53 +736,100 @@ __global__ void __launch_bounds__(C::THREADS, C::WARPS == 4 ? 4 : 1) decode_kv4_
 template <typename T, int D>
 using Narrow = Cfg<T, D, 4, 2>;
 template <typename T, int D>
-using Wide = Cfg<T, D, 16, 1>;
+using Wide = Cfg<T, D, 8, 2>;
+// One CTA to an SM: the block scheduler fills an SM with several CTAs of a small grid while others
+// stay empty (96 CTAs of 4 warps: 23.5 us against 14.2), so that these ask for more shared memory.
+constexpr int ALONE_SMEM = 120 * 1024;
 
 template <class C>
+cudaError_t set_smem() {
+  const int most = std::max(C::SMEM, ALONE_SMEM);
+  const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(&decode_kv4_kernel<C, false>),
+                                             cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(reinterpret_cast<const void*>(&decode_kv4_kernel<C, true>),
+                              cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+}
+
+// CTAs of the stream-K split: as many as run at once; each may write two partial states.
+template <class C>
 cudaError_t grid_of(int sms, int dec_slots, int* grid) {
-  const void* fn = reinterpret_cast<const void*>(&decode_kv4_kernel<C, false>);
-  cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(reinterpret_cast<const void*>(&decode_kv4_kernel<C, true>),
-                             cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
   int per_sm = 0;
+  cudaError_t e = set_smem<C>();
   if (e == cudaSuccess)
-    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, fn, C::THREADS, C::SMEM);
-  // Every CTA of the split may write two partial states.
-  *grid = min(per_sm * sms, dec_slots / 2);
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(
+        &per_sm, reinterpret_cast<const void*>(&decode_kv4_kernel<C, false>), C::THREADS, C::SMEM);
+  *grid = std::min(per_sm * sms, dec_slots / 2);
   return e;
 }
 
 template <class C>
 cudaError_t launch(const Dev& d, int layer, const void* q, void* out, const void* new_k,
-                   const void* new_v, int grid, Cut cut, bool early, cudaStream_t s) {
+                   const void* new_v, int grid, bool alone, Cut cut, bool early, cudaStream_t s) {
   using T = typename C::T;
   return launch_ex(new_k != nullptr ? &decode_kv4_kernel<C, true> : &decode_kv4_kernel<C, false>,
-                   dim3(grid), dim3(C::THREADS), C::SMEM, s, true, d, layer,
-                   static_cast<const T*>(q), static_cast<T*>(out), static_cast<const T*>(new_k),
-                   static_cast<const T*>(new_v), cut, (int)early);
+                   dim3(grid), dim3(C::THREADS), alone ? std::max(C::SMEM, ALONE_SMEM) : C::SMEM, s,
+                   true, d, layer, static_cast<const T*>(q), static_cast<T*>(out),
+                   static_cast<const T*>(new_k), static_cast<const T*>(new_v), cut, (int)early);
+}
+
+// How a call is cut, by what a launch takes in us: a fixed chain, then times in units of a page's
+// work (binary32 pages, half as long, take 0.7 of it): the pages of a warp one after the other, each
+// the longer the more warps share an SM, and 2 for the merge of a pair's slices.  Measured (us,
+// 8 KV heads; Mk, Nk: k slices of 8 and 4 warps, S: stream-K; the first is the one chosen):
+//   pages      1 session                4                     14                     38, 64
+//       7   M1 3.8  N4 5.1  S 9.4   M1 3.8  N2 5.2        M1 4.4  N4 6.2        N1 4.6, 6.0  S 18.6
+//      25   M1 4.9  N8 5.3          M1 5.1  N3 5.9        M1 5.8  N4 7.6        M1 8.1, N1 10.2
+//      94   M15 6.1 N12 6.4 S 12.6  M4 7.4  N4 7.6        M1 10.6 N5 10.5       M1 15.0, N1 25.5 S 29.7
+//     257   M15 6.9 N14 7.3 S 16.1  M9 10.0 M4 10.2       N5 18.3 M2 20.6       M1 32.7, S 58.0 N1 61.6
+// One slice each and no merge wins up to about 40 pages; then as many slices as give a warp a page or
+// two; stream-K where pairs outnumber the SMs' room and their last CTAs would leave most SMs empty.
+struct Choice {
+  bool wide;
+  int slices;  // 0: stream-K
+};
+Choice choose(int sms, int n_pairs, int64_t units, int esz) {
+  const float page = esz == 2 ? 1.f : 0.7f;
+  const int pages = (int)((units + n_pairs - 1) / n_pairs);
+  Choice best = {false, 0};
+  float least = 3.4f + page * (8.4f + 0.0534f * units / sms);
+  for (int wide = 0; wide < 2; ++wide) {
+    const int warps = wide ? 8 : 4;
+    const int most = std::max(1, std::min(std::min(MAX_PARTS, pages), sms * (16 / warps) / n_pairs));
+    for (int k = 1; k <= most; ++k) {
+      const int64_t ctas = (int64_t)n_pairs * k;
+      const bool alone = ctas <= sms;
+      const float each = !alone ? 0.85f : wide ? 0.56f : 0.43f;
+      const int64_t room = sms * (16 / warps), waves = (ctas + room - 1) / room;
+      const int64_t steps = waves * ((pages + k * warps - 1) / (k * warps));
+      const float t = 3.4f + page * (steps * each + (k > 1 ? 2.f + 0.03f * k : 0.f) +
+                                     (alone ? ctas / (float)sms : 1.5f));
+      if (t < least) {
+        least = t;
+        best = {wide != 0, k};
+      }
+    }
+  }
+  return best;
 }
 
 template <typename T, int D>
 cudaError_t launch_any(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
                        const void* new_k, const void* new_v, int n_pairs, int64_t units, bool early,
                        cudaStream_t s) {
-  const char* w = getenv("KV4_WIDE");
-  const int mode = w ? atoi(w) : 0;
-  if (mode == 1) {
-    const int k = std::min(MAX_PARTS, lim.kv4_decode_wide / n_pairs);
-    if (k >= 1) return launch<Wide<T, D>>(d, layer, q, out, new_k, new_v, n_pairs * k, {k, 0}, early, s);
-  } else if (mode == 0) {
-    const int k = std::min(MAX_PARTS, lim.kv4_decode / n_pairs);
-    if (k >= 1) return launch<Narrow<T, D>>(d, layer, q, out, new_k, new_v, n_pairs * k, {k, 0}, early, s);
-  }
-  return launch<Narrow<T, D>>(d, layer, q, out, new_k, new_v, lim.kv4_decode, {0, 8}, early, s);
+  const Choice c = choose(lim.sms, n_pairs, units, d.esz);
+  if (c.slices == 0)
+    return launch<Narrow<T, D>>(d, layer, q, out, new_k, new_v, lim.kv4_decode, false, {0, 8}, early, s);
+  const int grid = n_pairs * c.slices;
+  const bool alone = grid <= lim.sms;
+  return c.wide ? launch<Wide<T, D>>(d, layer, q, out, new_k, new_v, grid, alone, {c.slices, 0}, early, s)
+                : launch<Narrow<T, D>>(d, layer, q, out, new_k, new_v, grid, alone, {c.slices, 0}, early, s);
 }
 
 template <typename T, int D>
 cudaError_t limits_of(int dec_slots, Limits* lim) {
-  const cudaError_t e = grid_of<Narrow<T, D>>(lim->sms, dec_slots, &lim->kv4_decode);
-  return e != cudaSuccess ? e : grid_of<Wide<T, D>>(lim->sms, dec_slots, &lim->kv4_decode_wide);
+  const cudaError_t e = set_smem<Wide<T, D>>();
+  return e != cudaSuccess ? e : grid_of<Narrow<T, D>>(lim->sms, dec_slots, &lim->kv4_decode);
 }
 
 }  // namespace

@@ -54,7 +54,7 @@ struct Limits {
   int pf_stream_k;                 // CTAs of the stream-K prefill (bfloat16)
   int pf_clusters[PF_MAX_SLICES + 1];  // [k] clusters of k CTAs of the prefill's pair split
   int f32_cluster[2][2];           // largest cluster of the binary32 prefill: [rows][spread]
-  int kv4_decode, kv4_decode_wide; // CTAs of the decode over 4-bit rows, of 4 and of 16 warps
+  int kv4_decode;                  // CTAs of the stream-K decode over 4-bit rows
   int kv4_prefill[KV4_PF_WARPS + 1];  // [w] CTAs of the prefill with w warps to a page
 };
 cudaError_t query_limits(const Dev& d, Limits* lim);
