@@ -687,7 +687,7 @@ cudaError_t launch_any(const Dev& d, const Limits& lim, int layer, const void* q
 }  // namespace
 
 cudaError_t kv4_prefill_limits(const Dev& d, Limits* lim) {
-  return d.esz == 2 ? limits_of<__nv_bfloat16, 128>(lim) : limits_of<float, 64>(lim);
+  return d.esz == 2 ? kv4_prefill_tc_limits(lim) : limits_of<float, 64>(lim);
 }
 
 cudaError_t launch_attn_kv4(const Dev& d, const Limits& lim, LaunchOrder* order, int layer,
@@ -707,7 +707,7 @@ cudaError_t launch_attn_kv4(const Dev& d, const Limits& lim, LaunchOrder* order,
   }
   const bool early = order->early(layer, false);
   const cudaError_t e =
-      d.esz == 2 ? launch_any<__nv_bfloat16, 128>(d, lim, layer, q, out, max_t, early, s)
+      d.esz == 2 ? launch_prefill_kv4_tc(d, lim, layer, q, out, n_seq * d.kv_heads, units, early, s)
                  : launch_any<float, 64>(d, lim, layer, q, out, max_t, early, s);
   if (e == cudaSuccess) order->launched(layer, false);
   return e;

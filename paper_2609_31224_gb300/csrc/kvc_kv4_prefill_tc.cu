@@ -1,0 +1,712 @@
+// Chunked-prefill attention over a cache held in 4 bits (KVC_KV4), bfloat16 calls, on the
+// 5th-generation tensor cores (tcgen05 + TMEM).
+//
+// The T * G query rows of a (session, KV head) pair (T <= 32 tokens, G = 4 heads) are the M = 128
+// rows of the products S = Q K^T and O += P V, 128 keys (8 pages) a stage.  Operands are binary16:
+// K and V exactly the numbers that the codes stand for (over 16, kvc_kv4.h), q and P rounded to 11
+// bits; accumulation and softmax in binary32.  Rounding and masks are those of kvc_kv4_decode.cu:
+// q rows over a power of two, P = exp2(s - m + 8) with a lagging reference m, masked keys of weight
+// 0, invalid slots of value 0.  A V group that stands for NaN and that not every row sees is held as
+// 0 and its first place noted; the rows that see it get NaN when they are written.
+//
+// Each pair's pages are cut into k slices of whole stages, one CTA each; the k CTAs of a pair are a
+// thread-block cluster and merge their partial rows through distributed shared memory.
+//
+// Warps of a CTA (480 threads, one CTA per SM):
+//   0-3    softmax: a thread owns a TMEM lane, that is a query row; rotates it into TMEM, then turns
+//          rows of S into rows of P (written over them), keeps maximum and sum, writes the output;
+//   4-11   operands: warp 4 + i unpacks page i of a stage, K and V, into 128-byte-swizzled tiles.
+//          Dims and nibbles keep their stored order (the query's dims take K's, the output's are put
+//          back in order), so that a word of eight codes becomes one 16-byte store; the order of the
+//          stores of a warp is chosen so that eight lanes in a row hit all banks;
+//   12     copies the raw pages (18 D bytes each, K and V) into a ring of 3 stages;
+//   13, 14 issue S = Q K^T (Q from TMEM) and O += P V (P from TMEM, V read along its keys).
+// Every wait is bounded; a timeout records KVC_DERR_WAIT and the CTA stops.
+#include <cuda.h>
+
+#include <algorithm>
+
+#include "kvc_kv4.cuh"
+#include "kvc_prefill_tc.cuh"
+
+namespace kvc {
+
+namespace {
+
+using namespace kv4;
+
+constexpr int KEYS = 128;                       // of a stage
+constexpr int PAGES = KEYS / PS;
+constexpr int PAGE = 18 * D;                    // raw bytes of a page of one head, K and V
+constexpr int PANEL = KEYS * 128;               // 128 rows of 64 binary16 numbers
+constexpr int TILE = 2 * PANEL;                 // K or V of a stage
+constexpr int RAW = 3;                          // raw stages in the ring
+constexpr int SM_WARPS = 4, OP_WARPS = PAGES;
+constexpr int W_OP = SM_WARPS, W_LOAD = W_OP + OP_WARPS, W_S = W_LOAD + 1, W_PV = W_S + 1;
+constexpr int THREADS = (W_PV + 1) * 32;
+constexpr float P_SHIFT = 8.f, P_LAG = 6.f;     // as in the decode kernel
+
+// Tensor memory: S of even and odd stages (128 fp32 columns each; P, 64 columns of pairs, over
+// their first half), O (128), Q (64).
+constexpr int TMEM_COLS = 512, S_COL = 0, O_COL = 256, Q_COL = 384;
+
+enum {
+  B_RAW_FULL = 0,                  // [RAW] raw pages of a stage copied
+  B_RAW_EMPTY = B_RAW_FULL + RAW,  // [RAW] ... and unpacked
+  B_K_FULL = B_RAW_EMPTY + RAW,    // [2] K tile of a stage written
+  B_K_EMPTY = B_K_FULL + 2,        // [2] ... and read by S = Q K^T
+  B_V_FULL = B_K_EMPTY + 2,
+  B_V_EMPTY = B_V_FULL + 2,
+  B_S_FULL = B_V_EMPTY + 2,        // [2] scores complete
+  B_P_FULL = B_S_FULL + 2,         // [2] weights written
+  B_PV = B_P_FULL + 2,             // [2] O += P V complete (and S, P of the stage free)
+  B_Q = B_PV + 2,                  // query rows in TMEM
+  B_FINAL = B_Q + 1,               // [2] the products of an issuer complete
+  N_BARS = B_FINAL + 2
+};
+// Shared memory from a 1024-aligned base: K tiles, V tiles, raw ring, barriers.  The partial rows of
+// a slice take the place of the tiles when its products are complete.
+constexpr int OFF_K = 0, OFF_V = OFF_K + 2 * TILE, OFF_RAW = OFF_V + 2 * TILE;
+constexpr int OFF_BAR = OFF_RAW + RAW * PAGES * PAGE;
+constexpr int OFF_TMEM = OFF_BAR + N_BARS * 8;
+constexpr int OFF_NAN = OFF_TMEM + 8;           // [D / GROUP] first retained index of a NaN group
+constexpr int SMEM = 1024 + OFF_NAN + D / GROUP * 4;
+constexpr int ROW_PITCH = (D + 4) * 4;          // a partial row: D values, then (m, l, c)
+static_assert(OFF_BAR % 8 == 0 && PAGE % 16 == 0 && M * ROW_PITCH <= 4 * TILE, "layout");
+static_assert(SMEM <= 227 * 1024 - 256, "fits");
+
+// Instruction descriptor, kind::f16: D fp32, A and B binary16, A K-major, B K- or MN-major.
+__host__ __device__ constexpr uint32_t f16_desc(int n, int m, bool b_mn_major) {
+  return (1u << 4) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
+         ((uint32_t)(m >> 4) << 24);
+}
+
+__device__ inline void sts128(uint32_t at, const uint32_t (&v)[4]) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+               "r"(v[3])
+               : "memory");
+}
+
+// The pages of a slice: blocks [blk0, blk0 + nblk) of a pair.
+struct Slice {
+  SeqInfo si;
+  int seq, head, blk0, nblk;
+  __device__ int stages() const { return (nblk + PAGES - 1) / PAGES; }
+  __device__ int last0() const { return si.n_hist + si.n_live - si.t; }  // of the first token
+};
+
+// K tile rows of page i of a stage from its raw tile (shared addresses): lane (x, t) takes words
+// [4 t, 4 t + 4) of rows r and r + 8.
+__device__ inline void unpack_k(uint32_t raw, uint32_t tile, int i, bool open, const BlockRange& br,
+                                int lane) {
+  const int x = lane >> 2, t = lane & 3;
+  const int r0 = (x & 4) | (x & 1) << 1 | (x >> 1 & 1);  // rows two apart side by side
+  const int turn = t >> 1;                               // this lane's words in the order w ^ turn
+  const __half2 m72 = __float2half2_rn(-72.f);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int row = r0 + 8 * j;
+    uint32_t w[4], m[2];
+    lds(raw + k_codes(D, row, 8 * t), w);
+    lds(raw + k_scale(D, row, 0), m);
+    if (!open && (row < br.lo || row >= br.hi)) m[0] = m[1] = 0u;
+    const uint32_t to = tile + turn * PANEL + (PS * i + row) * 128;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      // (w ^ turn of a register array would go through memory: both are picked.)
+      const uint32_t word = turn ? w[s ^ 1] : w[s];
+      const uint32_t mm = __byte_perm(m[s / 2], 0, (s & 1) != turn ? 0x3232u : 0x1010u);
+      uint32_t v[4];
+      pairs_of(word, bits_h2(mm), __hmul2(bits_h2(mm), m72), v);
+      sts128(to + (((4 * (t & 1) + (s ^ turn)) ^ (row & 7)) << 4), v);
+    }
+  }
+}
+
+// V tile rows of page i of a stage: lane (g, t) takes piece g of rows 2t, 2t + 1 (+ 8).
+__device__ inline void unpack_v(uint32_t raw, uint32_t tile, int i, bool open, const BlockRange& br,
+                                int last0, int* nan_at, int lane) {
+  const int g = lane >> 2, t = lane & 3, turn = g & 1;   // this lane's rows in the order k ^ turn
+  const __half2 m72 = __float2half2_rn(-72.f);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int row0 = 2 * t + 8 * h, group = g * (D / 8) / GROUP;
+    uint32_t w[4], m;
+    lds(raw + v_piece(D, row0, g), w);
+    lds(raw + v_scale(D, row0, group), m);
+    if (!open) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const bool valid = row0 + k >= br.lo && row0 + k < br.hi;
+        const bool is_nan = (m >> (16 * k) & 0x7FFFu) > 0x7C00u;
+        if (valid && is_nan && br.base + PS - 1 > last0) atomicMin(&nan_at[group], br.base + row0 + k);
+        if (!valid || (is_nan && br.base + PS - 1 > last0)) m &= k ? 0x0000FFFFu : 0xFFFF0000u;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int row = row0 + (k ^ turn);
+      const uint32_t mm = __byte_perm(m, 0, k != turn ? 0x3232u : 0x1010u);
+      const uint32_t to = tile + (g >> 2) * PANEL + (PS * i + row) * 128;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        uint32_t v[4];
+        pairs_of(turn ? w[2 * (k ^ 1) + s] : w[2 * k + s], bits_h2(mm), __hmul2(bits_h2(mm), m72), v);
+        sts128(to + (((2 * (g & 3) + s) ^ (row & 7)) << 4), v);
+      }
+    }
+  }
+}
+
+// A query row into TMEM (every lane of the warp; rows that are not live are zeros): its rotated
+// elements over a power of two, largest in [1, 2), dims in K's stored order.  Returns the row's
+// softmax scale.
+__device__ inline float query_row(const __nv_bfloat16* row, const float2* rope, bool live,
+                                  uint32_t tq) {
+  constexpr int HALF = D / 2;
+  uint32_t most = 0;
+  // Words w and w + 2 of t hold rotate-half partners.
+  auto rotated = [&](int t, int w, float (&y1)[8], float (&y2)[8]) {
+    const int at = GROUP * w + 8 * t;
+    float x1[8], x2[8];
+    Chunk16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(row + at), x1);
+    Chunk16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(row + at + HALF), x2);
+    const float4* t4 = reinterpret_cast<const float4*>(rope + at);
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const float4 cs = t4[e / 2];
+      turn_pair(x1[e], x2[e], make_float2(cs.x, cs.y), y1[e], y2[e]);
+      turn_pair(x1[e + 1], x2[e + 1], make_float2(cs.z, cs.w), y1[e + 1], y2[e + 1]);
+    }
+  };
+  if (live) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        float y1[8], y2[8];
+        rotated(t, w, y1, y2);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most = max(most, max(abs_bits(y1[e]), abs_bits(y2[e])));
+      }
+  }
+  int e = (int)(most >> 23) - 127;
+  e = e > 126 ? (e == 128 ? 0 : 126) : max(e, -126);   // (infinities and NaN pass through)
+  const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    uint32_t u[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) u[i] = 0u;
+    if (live) {
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        float y1[8], y2[8];
+        rotated(t, w, y1, y2);
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          u[4 * w + p] = h2_bits(__floats2half2_rn(y1[p] * inv, y1[p + 4] * inv));
+          u[4 * (w + 2) + p] = h2_bits(__floats2half2_rn(y2[p] * inv, y2[p + 4] * inv));
+        }
+      }
+    }
+    __syncwarp();
+    tmem_st16(tq + 16 * t, u);
+  }
+  // 16: scales are stored over 16.
+  return 16.f * LOG2E * 0.08838834764831845f * __uint_as_float((uint32_t)(127 + e) << 23);
+}
+
+// Weight of a state with reference m against the reference m2 of several.
+__device__ inline float weight2(float m, float m2, float c) {
+  return m == -INFINITY ? 0.f : ex2((m - m2) * c);
+}
+
+__device__ inline void cluster_arrive() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ inline void cluster_wait() {
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ inline uint32_t cluster_map(uint32_t saddr, int rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(rank));
+  return r;
+}
+__device__ inline float4 ld_cluster(uint32_t at) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(at)
+               : "memory");
+  return v;
+}
+
+// Dims [8 c, 8 c + 8) of an output row from its columns in the tiles' order.
+__device__ inline void in_order(const float* o, float f, float (&y)[8]) {
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    y[p] = o[2 * p] * f;
+    y[p + 4] = o[2 * p + 1] * f;
+  }
+}
+
+__global__ void __launch_bounds__(THREADS, 1) prefill_kv4_kernel(
+    Dev d, int layer, const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out,
+    int k_slices, int early) {
+  extern __shared__ uint8_t smem_raw[];
+  // (The same offset in every CTA, so that cluster_map() of an address finds the peer's.)
+  uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + OFF_BAR);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + OFF_TMEM);
+  int* nan_at = reinterpret_cast<int*>(smem + OFF_NAN);
+  __shared__ int s_abort_flag;
+  volatile int& s_abort = s_abort_flag;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  // The first call after an append waits for it (and lets nothing else start before that).
+  if (!early) pdl_wait();
+  if (d.g->n_units == 0) {  // the append failed: nothing to do for any CTA
+    pdl_wait();
+    return;
+  }
+  if (tid == 0) {
+    for (int i = 0; i < RAW; ++i) {
+      mbar_init(&bars[B_RAW_FULL + i], 1);
+      mbar_init(&bars[B_RAW_EMPTY + i], OP_WARPS);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&bars[B_K_FULL + i], OP_WARPS);
+      mbar_init(&bars[B_K_EMPTY + i], 1);
+      mbar_init(&bars[B_V_FULL + i], OP_WARPS);
+      mbar_init(&bars[B_V_EMPTY + i], 1);
+      mbar_init(&bars[B_S_FULL + i], 1);
+      mbar_init(&bars[B_P_FULL + i], SM_WARPS);
+      mbar_init(&bars[B_PV + i], 1);
+      mbar_init(&bars[B_FINAL + i], 1);
+    }
+    mbar_init(&bars[B_Q], SM_WARPS);
+    fence_mbar_init();
+    s_abort = 0;
+  }
+  if (tid < D / GROUP) nan_at[tid] = 1 << 30;
+  __syncwarp();
+  if (warp == W_S) tmem_alloc(tmem_slot, TMEM_COLS);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  pdl_launch_dependents();
+  const uint32_t sbase = smem_u32(smem);
+
+  Slice sl;
+  const int pair = blockIdx.x / k_slices, slice = blockIdx.x % k_slices;
+  sl.seq = pair / d.kv_heads;
+  sl.head = pair % d.kv_heads;
+  sl.si = d.seq[sl.seq];
+  const SeqInfo& si = sl.si;
+  {
+    const int all = (si.n_blocks + PAGES - 1) / PAGES;
+    sl.blk0 = min(si.n_blocks, PAGES * (int)((int64_t)slice * all / k_slices));
+    sl.nblk = min(si.n_blocks, PAGES * (int)((int64_t)(slice + 1) * all / k_slices)) - sl.blk0;
+  }
+  const int n_st = sl.stages(), last0 = sl.last0(), R = si.t * G;
+  // A wait that gives up stops its warp; the others follow when their own waits do.
+  auto wait = [&](int bar, uint32_t parity) {
+    const bool ok = __all_sync(FULL, mbar_wait(d, &bars[bar], parity & 1));
+    if (!ok && lane == 0) s_abort = 1;
+    return ok;
+  };
+  // This thread's partial row: reference, sum, softmax scale (softmax warps).
+  float m = -INFINITY, l = 0.f, c = 0.f;
+  bool dead = false;
+
+  if (warp < SM_WARPS) {
+    // ---------------- softmax ----------------
+    const int r = tid;
+    const bool live = r < R, idle = warp * 32 >= R;
+    const uint32_t trow = tmem + ((uint32_t)(warp * 32) << 16);
+    pdl_wait();
+    {
+      const __nv_bfloat16* row =
+          q + ((size_t)(si.q_row0 + r / G) * d.q_heads + sl.head * G + r % G) * D;
+      c = query_row(row, d.rope + (size_t)(si.pos_first + r / G) * (D / 2), live, trow + Q_COL);
+    }
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&bars[B_Q]);
+    const int last = last0 + r / G;  // retained index of the last key that the row sees
+    for (int i = 0; i < n_st; ++i) {
+      const int b = i & 1;
+      if (!wait(B_S_FULL + b, i >> 1)) {
+        dead = true;
+        break;
+      }
+      tc_fence_after();
+      if (idle) {  // padding rows: whatever their P is, it stays in their rows of O
+        if (lane == 0) mbar_arrive(&bars[B_P_FULL + b]);
+        continue;
+      }
+      const uint32_t ts = trow + S_COL + KEYS * b;
+      const int b0 = sl.blk0 + PAGES * i, npg = min(PAGES, sl.nblk - PAGES * i);
+      // Pages of the stage with a key that some row must not see.
+      unsigned edge = 0;
+#pragma unroll
+      for (int pg = 0; pg < PAGES; ++pg) {
+        const BlockRange br = block_range(si, b0 + min(pg, npg - 1));
+        if (pg >= npg || br.lo > 0 || br.hi < PS || br.base + PS - 1 > last0) edge |= 1u << pg;
+      }
+      uint32_t pw[KEYS / 2];
+      float sum = 0.f, most = -INFINITY;
+      auto weigh = [&] {
+        sum = 0.f;
+        most = -INFINITY;
+        float2 rs[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        const float2 c2 = make_float2(c, c), sh = make_float2(P_SHIFT, P_SHIFT);
+        const float2 nm = make_float2(-m, -m);
+#pragma unroll
+        for (int part = 0; part < 4; ++part) {
+          float s[32];
+          tmem_ld32(ts + 32 * part, s);
+#pragma unroll
+          for (int k = 0; k < 32; k += 2) {
+            float2 a = __ffma2_rn(__fadd2_rn(make_float2(s[k], s[k + 1]), nm), c2, sh);
+            s[k] = a.x;
+            s[k + 1] = a.y;
+          }
+          if (edge >> (2 * part) & 3u) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int pg = 2 * part + h;
+              const BlockRange br = block_range(si, b0 + min(pg, npg - 1));
+              const int hi = pg < npg ? min(br.hi, last - br.base + 1) : 0;
+#pragma unroll
+              for (int k = 0; k < PS; ++k)
+                if (k < br.lo || k >= hi) s[PS * h + k] = -INFINITY;
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < 32; k += 2) {
+            most = fmaxf(most, fmaxf(s[k], s[k + 1]));
+            const float2 p = make_float2(ex2(s[k]), ex2(s[k + 1]));
+            rs[(k / 2) & 1] = __fadd2_rn(rs[(k / 2) & 1], p);
+            pw[16 * part + k / 2] = h2_bits(__floats2half2_rn(p.x, p.y));
+          }
+        }
+        sum = (rs[0].x + rs[1].x) + (rs[0].y + rs[1].y);
+      };
+      weigh();
+      if (!live) most = -INFINITY;
+      // (At the first stage with a key that the row sees m is -infinity: a new reference.)
+      if (__any_sync(FULL, most > P_SHIFT + P_LAG)) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int part = 0; part < 4; ++part) {
+          float s[32];
+          tmem_ld32(ts + 32 * part, s);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int pg = 2 * part + h;
+            const BlockRange br = block_range(si, b0 + min(pg, npg - 1));
+            const int hi = pg < npg ? min(br.hi, last - br.base + 1) : 0;
+#pragma unroll
+            for (int k = 0; k < PS; ++k)
+              if (k >= br.lo && k < hi) mx = fmaxf(mx, s[PS * h + k]);
+          }
+        }
+        const float mn = most > P_SHIFT + P_LAG ? fmaxf(m, mx) : m;
+        const float f = mn == m ? 1.f : weight2(m, mn, c);
+        if (i > 0) {
+          // The products so far are complete: their rows may be scaled.
+          if (!wait(B_PV + (b ^ 1), (i - 1) >> 1)) {
+            dead = true;
+            break;
+          }
+          tc_fence_after();
+#pragma unroll 1
+          for (int x = 0; x < D / 16; ++x) {
+            float o[16];
+            tmem_ld16(trow + O_COL + 16 * x, o);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) o[k] *= f;
+            tmem_st16(trow + O_COL + 16 * x, o);
+          }
+        }
+        l *= f;
+        m = mn;
+        weigh();
+      }
+      l += sum;
+      __syncwarp();
+      tmem_st32(ts, pw);
+      tmem_st32(ts + 32, pw + 32);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars[B_P_FULL + b]);
+    }
+    if (n_st > 0 && !dead) dead = !wait(B_PV + ((n_st - 1) & 1), (n_st - 1) >> 1);
+    tc_fence_after();
+  } else if (warp < W_LOAD) {
+    // ---------------- operands ----------------
+    const int pg = warp - W_OP;
+    for (int i = 0; i < n_st; ++i) {
+      const int slot = i % RAW, b = i & 1;
+      if (!wait(B_RAW_FULL + slot, i / RAW)) break;
+      const uint32_t raw = sbase + OFF_RAW + (slot * PAGES + pg) * PAGE;
+      const int blk = sl.blk0 + PAGES * i + pg;
+      const bool here = blk < sl.blk0 + sl.nblk;
+      const BlockRange br = block_range(si, here ? blk : sl.blk0);
+      const bool open = br.lo == 0 && br.hi == PS && br.base + PS - 1 <= last0;
+      if (i >= 2 && !wait(B_K_EMPTY + b, (i >> 1) - 1)) break;
+      // (A page that is not there: its scores are masked whatever K holds.)
+      if (here) unpack_k(raw, sbase + OFF_K + b * TILE, pg, open, br, lane);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars[B_K_FULL + b]);
+      if (i >= 2 && !wait(B_V_EMPTY + b, (i >> 1) - 1)) break;
+      if (here) {
+        unpack_v(raw + 9 * D, sbase + OFF_V + b * TILE, pg, open, br, last0, nan_at, lane);
+      } else {
+        // Weight 0 times what the tile held must be 0.
+        const uint32_t zero[4] = {0u, 0u, 0u, 0u};
+        const uint32_t at = sbase + OFF_V + b * TILE + PS * pg * 128 + lane * 16;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          sts128(at + x * 512, zero);
+          sts128(at + PANEL + x * 512, zero);
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&bars[B_V_FULL + b]);
+        mbar_arrive(&bars[B_RAW_EMPTY + slot]);
+      }
+    }
+  } else if (warp == W_LOAD) {
+    // ---------------- raw pages ----------------
+    const int32_t* hrow = d.hist_pt + (size_t)si.sid * d.max_pages_per_session;
+    const int32_t* lrow = d.live_pt + (size_t)si.sid * d.max_pages_per_session;
+    const uint8_t* tiles = d.pool + tile_at(D, d.layers, d.kv_heads, 0, layer, sl.head, 0);
+    const size_t stride = page_bytes(D, d.layers, d.kv_heads);
+    const uint64_t policy = evict_first_policy();
+    auto page_at = [&](int b) {
+      return lane < PAGES && b < sl.nblk ? block_page(si, hrow, lrow, sl.blk0 + b) : 0;
+    };
+    int done = 0, page = page_at(lane);
+    for (int i = 0; i < n_st; ++i) {
+      const int slot = i % RAW, npg = min(PAGES, sl.nblk - PAGES * i);
+      const int next = page_at(PAGES * (i + 1) + lane);
+      if (i >= RAW && !wait(B_RAW_EMPTY + slot, i / RAW - 1)) break;
+      if (lane == 0) mbar_arrive_expect_tx(&bars[B_RAW_FULL + slot], npg * PAGE);
+      __syncwarp();
+      if (lane < npg) {
+        fence_proxy_async_smem();
+        bulk_g2s_hint(smem + OFF_RAW + (slot * PAGES + lane) * PAGE, tiles + page * stride, PAGE,
+                      &bars[B_RAW_FULL + slot], policy);
+      }
+      page = next;
+      done = i + 1;
+    }
+    // No copy may still be in flight when the CTA ends.
+    for (int i = max(0, done - RAW); i < done; ++i)
+      mbar_wait(d, &bars[B_RAW_FULL + i % RAW], i / RAW & 1);
+  } else if (lane == 0) {
+    // ---------------- MMA issuers ----------------
+    bool ok = true;
+    if (warp == W_S) {
+      constexpr uint32_t ID = f16_desc(KEYS, M, false);
+      ok = mbar_wait(d, &bars[B_Q], 0);
+      for (int i = 0; i < n_st && ok; ++i) {
+        const int b = i & 1;
+        ok = mbar_wait(d, &bars[B_K_FULL + b], i >> 1 & 1) &&
+             (i < 2 || mbar_wait(d, &bars[B_PV + b], (i >> 1) - 1 & 1));
+        if (!ok) break;
+        tc_fence_after();
+        const uint64_t k_desc = smem_desc(sbase + OFF_K + b * TILE, 0, 1024);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk)
+          tc_mma_ts(tmem + S_COL + KEYS * b, tmem + Q_COL + 8 * kk,
+                    desc_at(k_desc, (kk >> 2) * PANEL + (kk & 3) * 32), ID, kk > 0);
+        tc_commit(&bars[B_S_FULL + b]);
+        tc_commit(&bars[B_K_EMPTY + b]);
+      }
+    } else {
+      constexpr uint32_t ID = f16_desc(D, M, true);
+      for (int i = 0; i < n_st && ok; ++i) {
+        const int b = i & 1;
+        ok = mbar_wait(d, &bars[B_V_FULL + b], i >> 1 & 1) &&
+             mbar_wait(d, &bars[B_P_FULL + b], i >> 1 & 1);
+        if (!ok) break;
+        tc_fence_after();
+        const uint64_t v_desc = smem_desc(sbase + OFF_V + b * TILE, PANEL, 1024);
+#pragma unroll
+        for (int kk = 0; kk < KEYS / 16; ++kk)
+          tc_mma_ts(tmem + O_COL, tmem + S_COL + KEYS * b + 8 * kk, desc_at(v_desc, kk * 16 * 128),
+                    ID, i > 0 || kk > 0);
+        tc_commit(&bars[B_PV + b]);
+        tc_commit(&bars[B_V_EMPTY + b]);
+      }
+    }
+    if (!ok) s_abort = 1;
+    // No MMA may still be running when the tensor memory is released.
+    tc_commit(&bars[B_FINAL + (warp - W_S)]);
+    mbar_wait(d, &bars[B_FINAL + (warp - W_S)], 0);
+  }
+  __syncwarp();
+  if (warp >= SM_WARPS) pdl_wait();
+  tc_fence_before();
+  __syncthreads();  // every product and copy is complete
+  tc_fence_after();
+
+  // ---------------- output ----------------
+  if (warp < SM_WARPS && warp * 32 < R) {
+    const int r = tid;
+    const bool live = r < R;
+    const uint32_t trow = tmem + ((uint32_t)(warp * 32) << 16) + O_COL;
+    const int last = last0 + r / G;
+    const float f = k_slices == 1 ? 16.f / l : 1.f;
+    __nv_bfloat16* orow =
+        out + ((size_t)(si.q_row0 + r / G) * d.q_heads + sl.head * G + r % G) * D;
+    float* prow = reinterpret_cast<float*>(smem + OFF_K + r * ROW_PITCH);
+#pragma unroll 1
+    for (int x = 0; x < D / GROUP; ++x) {
+      float o[32];
+      __syncwarp();
+      if (n_st > 0) {
+        tmem_ld32(trow + GROUP * x, o);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 32; ++k) o[k] = 0.f;
+      }
+      if (!live || s_abort) continue;
+      const bool is_nan = last >= nan_at[x];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float y[8];
+        in_order(o + 8 * j, is_nan ? __uint_as_float(0x7FC00000u) : f, y);
+        if (k_slices == 1) {
+          Eight<__nv_bfloat16>::store(orow + GROUP * x + 8 * j, y);
+        } else {
+          float* to = prow + GROUP * x + 8 * j;
+          *reinterpret_cast<float4*>(to) = make_float4(y[0], y[1], y[2], y[3]);
+          *reinterpret_cast<float4*>(to + 4) = make_float4(y[4], y[5], y[6], y[7]);
+        }
+      }
+    }
+    if (live && k_slices > 1)
+      *reinterpret_cast<float4*>(prow + D) = make_float4(dead ? -INFINITY : m, l, c, 0.f);
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == W_S) tmem_dealloc(tmem, TMEM_COLS);
+  if (k_slices == 1) return;
+
+  // Rows [slice R / k, (slice + 1) R / k) of the pair are this CTA's to merge and write.
+  __syncwarp();
+  cluster_arrive();
+  cluster_wait();  // every part is in its CTA's shared memory
+  const int k = k_slices, r0 = slice * R / k, n_rows = (slice + 1) * R / k - r0;
+  for (int i = tid; i < n_rows * (D / 4); i += THREADS) {
+    const int r = r0 + i / (D / 4), x = i % (D / 4);
+    const uint32_t at = sbase + OFF_K + r * ROW_PITCH;
+    float4 ml[PF_MAX_SLICES], o[PF_MAX_SLICES];
+#pragma unroll
+    for (int p = 0; p < PF_MAX_SLICES; ++p) {
+      if (p >= k) break;
+      const uint32_t there = cluster_map(at, p);
+      ml[p] = ld_cluster(there + D * 4);
+      o[p] = ld_cluster(there + x * 16);
+    }
+    float mx = -INFINITY, L = 0.f;
+#pragma unroll
+    for (int p = 0; p < PF_MAX_SLICES; ++p)
+      if (p < k) mx = fmaxf(mx, ml[p].x);
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int p = 0; p < PF_MAX_SLICES; ++p) {
+      if (p >= k) break;
+      const float w = weight2(ml[p].x, mx, ml[p].z);
+      L += ml[p].y * w;
+      a.x = fmaf(o[p].x, w, a.x);
+      a.y = fmaf(o[p].y, w, a.y);
+      a.z = fmaf(o[p].z, w, a.z);
+      a.w = fmaf(o[p].w, w, a.w);
+    }
+    const float f = 16.f / L;
+    __nv_bfloat16* to = out + ((size_t)(si.q_row0 + r / G) * d.q_heads + sl.head * G + r % G) * D + 4 * x;
+    *reinterpret_cast<uint2*>(to) =
+        make_uint2(pack_bf16(a.x * f, a.y * f), pack_bf16(a.z * f, a.w * f));
+  }
+  __syncwarp();
+  cluster_arrive();
+  cluster_wait();  // no CTA still reads this one's rows
+}
+
+}  // namespace
+
+cudaError_t kv4_prefill_tc_limits(Limits* lim) {
+  cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(&prefill_kv4_kernel),
+                                       cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
+  if (e != cudaSuccess) return e;
+  for (int k = 1; k <= PF_MAX_SLICES; ++k) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(k);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = SMEM;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = k;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, &prefill_kv4_kernel, &cfg);
+    lim->kv4_clusters[k] = e == cudaSuccess ? n : 0;
+    if (e != cudaSuccess) cudaGetLastError();  // (a size that the device does not take: no error)
+  }
+  return cudaSuccess;
+}
+
+cudaError_t launch_prefill_kv4_tc(const Dev& d, const Limits& lim, int layer, const void* q,
+                                  void* out, int n_pairs, int64_t units, bool early,
+                                  cudaStream_t s) {
+  // Slices of a pair: a CTA takes 5.5 us beside its stages of 0.6 us, a merge 1.5 us.
+  const int pages = (int)std::max<int64_t>(1, (units + n_pairs - 1) / n_pairs);
+  const int stages = (pages + PAGES - 1) / PAGES;
+  int k = 1;
+  float least = 1e30f;
+  for (int x = 1; x <= std::min(PF_MAX_SLICES, stages); ++x) {
+    if (lim.kv4_clusters[x] < 1) continue;
+    const int waves = (n_pairs + lim.kv4_clusters[x] - 1) / lim.kv4_clusters[x];
+    const float t = waves * (5.5f + 0.6f * ((stages + x - 1) / x)) + (x > 1 ? 1.5f : 0.f);
+    if (t < least) {
+      least = t;
+      k = x;
+    }
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(n_pairs * k);
+  cfg.blockDim = dim3(THREADS);
+  cfg.dynamicSmemBytes = SMEM;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  int n = 0;
+  if (k > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = k;
+    attr[n].val.clusterDim.y = 1;
+    attr[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[n].val.programmaticStreamSerializationAllowed = 1;
+  ++n;
+  cfg.attrs = attr;
+  cfg.numAttrs = n;
+  return cudaLaunchKernelEx(&cfg, &prefill_kv4_kernel, d, layer, static_cast<const __nv_bfloat16*>(q),
+                            static_cast<__nv_bfloat16*>(out), k, (int)early);
+}
+
+}  // namespace kvc

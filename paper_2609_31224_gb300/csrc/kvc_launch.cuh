@@ -56,6 +56,7 @@ struct Limits {
   int f32_cluster[2][2];           // largest cluster of the binary32 prefill: [rows][spread]
   int kv4_decode;                  // CTAs of the stream-K decode over 4-bit rows
   int kv4_prefill[KV4_PF_WARPS + 1];  // [w] CTAs of the prefill with w warps to a page
+  int kv4_clusters[PF_MAX_SLICES + 1];  // [k] clusters of k CTAs of the bfloat16 prefill over them
 };
 cudaError_t query_limits(const Dev& d, Limits* lim);
 // Id of the current CUDA context (never reused: a context that replaces a destroyed one at the
@@ -98,6 +99,11 @@ cudaError_t launch_decode_kv4(const Dev& d, const Limits& lim, int layer, const 
                               bool early, cudaStream_t s);
 cudaError_t kv4_decode_limits(const Dev& d, Limits* lim);  // both set their kernels' attributes
 cudaError_t kv4_prefill_limits(const Dev& d, Limits* lim);
+// Chunks of bfloat16 calls (kvc_kv4_prefill_tc.cu).
+cudaError_t launch_prefill_kv4_tc(const Dev& d, const Limits& lim, int layer, const void* q,
+                                  void* out, int n_pairs, int64_t units, bool early,
+                                  cudaStream_t s);
+cudaError_t kv4_prefill_tc_limits(Limits* lim);
 // Attention launches may start while the kernel before them in the stream finishes.  early:
 // they may also read what the append wrote before that (an attention launch of the same
 // append came before, so the append is complete).
