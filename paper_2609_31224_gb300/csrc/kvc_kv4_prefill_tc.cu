@@ -12,15 +12,18 @@
 // Each pair's pages are cut into k slices of whole stages, one CTA each; the k CTAs of a pair are a
 // thread-block cluster and merge their partial rows through distributed shared memory.
 //
-// Warps of a CTA (480 threads, one CTA per SM):
-//   0-3    softmax: a thread owns a TMEM lane, that is a query row; rotates it into TMEM, then turns
-//          rows of S into rows of P (written over them), keeps maximum and sum, writes the output;
-//   4-11   operands: warp 4 + i unpacks page i of a stage, K and V, into 128-byte-swizzled tiles.
+// Warps of a CTA (608 threads, one CTA per SM):
+//   0-7    softmax: warps w and w + 4 own TMEM lanes 32 w .. 32 w + 31, a query row per lane; warp
+//          w takes the first 64 keys of a stage, warp w + 4 the others.  They rotate the rows into
+//          TMEM, then turn rows of S into rows of P (written over them), keep maximum and sum, and
+//          write the output.  The two threads of a row share its reference m: a flag between their
+//          warps tells each stage whether it still holds;
+//   8-15   operands: warp 8 + i unpacks page i of a stage, K and V, into 128-byte-swizzled tiles.
 //          Dims and nibbles keep their stored order (the query's dims take K's, the output's are put
 //          back in order), so that a word of eight codes becomes one 16-byte store; the order of the
 //          stores of a warp is chosen so that eight lanes in a row hit all banks;
-//   12     copies the raw pages (18 D bytes each, K and V) into a ring of 3 stages;
-//   13, 14 issue S = Q K^T (Q from TMEM) and O += P V (P from TMEM, V read along its keys).
+//   16     copies the raw pages (18 D bytes each, K and V) into a ring of 3 stages;
+//   17, 18 issue S = Q K^T (Q from TMEM) and O += P V (P from TMEM, V read along its keys).
 // Every wait is bounded; a timeout records KVC_DERR_WAIT and the CTA stops.
 #include <cuda.h>
 
@@ -41,13 +44,13 @@ constexpr int PAGE = 18 * D;                    // raw bytes of a page of one he
 constexpr int PANEL = KEYS * 128;               // 128 rows of 64 binary16 numbers
 constexpr int TILE = 2 * PANEL;                 // K or V of a stage
 constexpr int RAW = 3;                          // raw stages in the ring
-constexpr int SM_WARPS = 4, OP_WARPS = PAGES;
+constexpr int SM_WARPS = 8, OP_WARPS = PAGES, SM_THREADS = 32 * SM_WARPS;
 constexpr int W_OP = SM_WARPS, W_LOAD = W_OP + OP_WARPS, W_S = W_LOAD + 1, W_PV = W_S + 1;
 constexpr int THREADS = (W_PV + 1) * 32;
 constexpr float P_SHIFT = 8.f, P_LAG = 6.f;     // as in the decode kernel
 
-// Tensor memory: S of even and odd stages (128 fp32 columns each; P, 64 columns of pairs, over
-// their first half), O (128), Q (64).
+// Tensor memory: S of even and odd stages (128 fp32 columns each; P of each 64 keys, 32 columns of
+// pairs, over their first half), O (128), Q (64).
 constexpr int TMEM_COLS = 512, S_COL = 0, O_COL = 256, Q_COL = 384;
 
 enum {
@@ -67,7 +70,12 @@ enum {
 // Shared memory from a 1024-aligned base: K tiles, V tiles, raw ring, barriers.  The partial rows of
 // a slice take the place of the tiles when its products are complete.
 constexpr int OFF_K = 0, OFF_V = OFF_K + 2 * TILE, OFF_RAW = OFF_V + 2 * TILE;
-constexpr int OFF_BAR = OFF_RAW + RAW * PAGES * PAGE;
+// Query rows on their way to TMEM (padded: 8 lanes read 8 rows without a conflict).
+constexpr int Q_PITCH = 2 * D + 16;
+constexpr int OFF_Q = OFF_RAW + RAW * PAGES * PAGE;
+constexpr int OFF_ROW = OFF_Q + M * Q_PITCH;    // [M] softmax scales, then [2][M] exchanged values
+constexpr int OFF_FLAG = OFF_ROW + 3 * M * 4;   // [3][2][4] flags of the softmax warps
+constexpr int OFF_BAR = OFF_FLAG + 24 * 4;
 constexpr int OFF_TMEM = OFF_BAR + N_BARS * 8;
 constexpr int OFF_NAN = OFF_TMEM + 8;           // [D / GROUP] first retained index of a NaN group
 constexpr int SMEM = 1024 + OFF_NAN + D / GROUP * 4;
@@ -158,63 +166,65 @@ __device__ inline void unpack_v(uint32_t raw, uint32_t tile, int i, bool open, c
   }
 }
 
-// A query row into TMEM (every lane of the warp; rows that are not live are zeros): its rotated
-// elements over a power of two, largest in [1, 2), dims in K's stored order.  Returns the row's
-// softmax scale.
-__device__ inline float query_row(const __nv_bfloat16* row, const float2* rope, bool live,
-                                  uint32_t tq) {
-  constexpr int HALF = D / 2;
-  uint32_t most = 0;
-  // Words w and w + 2 of t hold rotate-half partners.
-  auto rotated = [&](int t, int w, float (&y1)[8], float (&y2)[8]) {
-    const int at = GROUP * w + 8 * t;
-    float x1[8], x2[8];
-    Chunk16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(row + at), x1);
-    Chunk16<__nv_bfloat16>::unpack(*reinterpret_cast<const uint4*>(row + at + HALF), x2);
-    const float4* t4 = reinterpret_cast<const float4*>(rope + at);
+// The chunk's query rows into their staging rows: rotated, over a power of two (largest element in
+// [1, 2); infinities and NaN pass through), dims in K's stored order; a row's softmax scale beside.
+// Item (row, c): dims [8c, 8c + 8) and their rotate-half partners; 8 lanes a row.
+__device__ inline void stage_queries(const Dev& d, const SeqInfo& si, int head,
+                                     const __nv_bfloat16* q, uint8_t* rows, float* scale, int tid) {
+  constexpr int HALF = D / 2, KC = D / 16, BATCH = 2;
+  const int n = si.t * G * KC;
+  for (int i0 = 0; i0 < n; i0 += BATCH * SM_THREADS) {
+    uint4 a[BATCH], b[BATCH];
+    float4 cs[BATCH][4];
 #pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      const float4 cs = t4[e / 2];
-      turn_pair(x1[e], x2[e], make_float2(cs.x, cs.y), y1[e], y2[e]);
-      turn_pair(x1[e + 1], x2[e + 1], make_float2(cs.z, cs.w), y1[e + 1], y2[e + 1]);
+    for (int u = 0; u < BATCH; ++u) {
+      const int i = min(i0 + u * SM_THREADS + tid, n - 1), r = i / KC, c = i % KC;
+      const uint4* row = reinterpret_cast<const uint4*>(
+          q + ((size_t)(si.q_row0 + r / G) * d.q_heads + head * G + r % G) * D);
+      a[u] = row[c];
+      b[u] = row[c + KC];
+      const float4* t4 = reinterpret_cast<const float4*>(d.rope + (size_t)(si.pos_first + r / G) * HALF + 8 * c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) cs[u][e] = t4[e];
     }
-  };
-  if (live) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int u = 0; u < BATCH; ++u) {
+      const int i = i0 + u * SM_THREADS + tid, r = min(i, n - 1) / KC, c = min(i, n - 1) % KC;
+      float x1[8], x2[8], y1[8], y2[8];
+      Chunk16<__nv_bfloat16>::unpack(a[u], x1);
+      Chunk16<__nv_bfloat16>::unpack(b[u], x2);
+      uint32_t most = 0;
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        float y1[8], y2[8];
-        rotated(t, w, y1, y2);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) most = max(most, max(abs_bits(y1[e]), abs_bits(y2[e])));
+      for (int e = 0; e < 8; e += 2) {
+        const float4 t = cs[u][e / 2];
+        turn_pair(x1[e], x2[e], make_float2(t.x, t.y), y1[e], y2[e]);
+        turn_pair(x1[e + 1], x2[e + 1], make_float2(t.z, t.w), y1[e + 1], y2[e + 1]);
       }
-  }
-  int e = (int)(most >> 23) - 127;
-  e = e > 126 ? (e == 128 ? 0 : 126) : max(e, -126);   // (infinities and NaN pass through)
-  const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    uint32_t u[16];
+      for (int e = 0; e < 8; ++e) most = max(most, max(abs_bits(y1[e]), abs_bits(y2[e])));
+      // (Rows are whole within a warp, and n is a multiple of 32: lanes past it repeat the last
+      // item together.)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) u[i] = 0u;
-    if (live) {
+      for (int o = 1; o < KC; o <<= 1) most = max(most, __shfl_xor_sync(FULL, most, o));
+      int e = (int)(most >> 23) - 127;
+      e = e > 126 ? (e == 128 ? 0 : 126) : max(e, -126);
+      const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+      if (i >= n) continue;
+      // 16: scales are stored over 16; the softmax takes exponents of 2.
+      if (c == 0)
+        scale[r] = 16.f * LOG2E * 0.08838834764831845f * __uint_as_float((uint32_t)(127 + e) << 23);
+      uint32_t u1[4], u2[4];
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        float y1[8], y2[8];
-        rotated(t, w, y1, y2);
-#pragma unroll
-        for (int p = 0; p < 4; ++p) {
-          u[4 * w + p] = h2_bits(__floats2half2_rn(y1[p] * inv, y1[p + 4] * inv));
-          u[4 * (w + 2) + p] = h2_bits(__floats2half2_rn(y2[p] * inv, y2[p + 4] * inv));
-        }
+      for (int p = 0; p < 4; ++p) {
+        u1[p] = h2_bits(__floats2half2_rn(y1[p] * inv, y1[p + 4] * inv));
+        u2[p] = h2_bits(__floats2half2_rn(y2[p] * inv, y2[p + 4] * inv));
       }
+      // Dims 8 c are word w = c / 4 of t = c % 4, the partners word w + 2.
+      uint8_t* to = rows + r * Q_PITCH + (4 * (c % 4) + c / 4) * 16;
+      *reinterpret_cast<uint4*>(to) = make_uint4(u1[0], u1[1], u1[2], u1[3]);
+      *reinterpret_cast<uint4*>(to + 32) = make_uint4(u2[0], u2[1], u2[2], u2[3]);
     }
-    __syncwarp();
-    tmem_st16(tq + 16 * t, u);
   }
-  // 16: scales are stored over 16.
-  return 16.f * LOG2E * 0.08838834764831845f * __uint_as_float((uint32_t)(127 + e) << 23);
 }
 
 // Weight of a state with reference m against the reference m2 of several.
@@ -316,72 +326,97 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_kv4_kernel(
     if (!ok && lane == 0) s_abort = 1;
     return ok;
   };
-  // This thread's partial row: reference, sum, softmax scale (softmax warps).
+  // This thread's partial row: reference, sum of its keys, softmax scale (softmax warps).
   float m = -INFINITY, l = 0.f, c = 0.f;
   bool dead = false;
+  const int quarter = warp & 3, half = warp >> 2 & 1;
+  float* s_row = reinterpret_cast<float*>(smem + OFF_ROW);
+  volatile int* s_flag = reinterpret_cast<volatile int*>(smem + OFF_FLAG);
+  // The two warps of a quarter (named barriers 1-4), all softmax warps (5).
+  auto sync_quarter = [&] {
+    __syncwarp();
+    asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");
+  };
 
   if (warp < SM_WARPS) {
     // ---------------- softmax ----------------
-    const int r = tid;
-    const bool live = r < R, idle = warp * 32 >= R;
-    const uint32_t trow = tmem + ((uint32_t)(warp * 32) << 16);
+    const int r = 32 * quarter + lane;
+    const bool live = r < R, idle = 32 * quarter >= R;
+    const uint32_t trow = tmem + ((uint32_t)(32 * quarter) << 16);
     pdl_wait();
+    stage_queries(d, si, sl.head, q, smem + OFF_Q, s_row, tid);
+    __syncwarp();
+    asm volatile("bar.sync 5, %0;" ::"n"(SM_THREADS) : "memory");
     {
-      const __nv_bfloat16* row =
-          q + ((size_t)(si.q_row0 + r / G) * d.q_heads + sl.head * G + r % G) * D;
-      c = query_row(row, d.rope + (size_t)(si.pos_first + r / G) * (D / 2), live, trow + Q_COL);
+      // This thread's half of its row's 64 columns of pairs; padding rows are zeros.
+      uint32_t u[32];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const uint4 w = live ? *reinterpret_cast<const uint4*>(smem + OFF_Q + r * Q_PITCH + 128 * half + 16 * x)
+                             : make_uint4(0, 0, 0, 0);
+        u[4 * x] = w.x;
+        u[4 * x + 1] = w.y;
+        u[4 * x + 2] = w.z;
+        u[4 * x + 3] = w.w;
+      }
+      __syncwarp();
+      tmem_st32(trow + Q_COL + 32 * half, u);
+      c = live ? s_row[r] : 0.f;
     }
     tc_fence_before();
     __syncwarp();
     if (lane == 0) mbar_arrive(&bars[B_Q]);
     const int last = last0 + r / G;  // retained index of the last key that the row sees
+    constexpr int HK = KEYS / 2, HP = PAGES / 2;
     for (int i = 0; i < n_st; ++i) {
       const int b = i & 1;
-      if (!wait(B_S_FULL + b, i >> 1)) {
-        dead = true;
-        break;
-      }
+      dead = dead || !wait(B_S_FULL + b, i >> 1);
       tc_fence_after();
       if (idle) {  // padding rows: whatever their P is, it stays in their rows of O
+        if (dead) break;
         if (lane == 0) mbar_arrive(&bars[B_P_FULL + b]);
         continue;
       }
-      const uint32_t ts = trow + S_COL + KEYS * b;
-      const int b0 = sl.blk0 + PAGES * i, npg = min(PAGES, sl.nblk - PAGES * i);
-      // Pages of the stage with a key that some row must not see.
+      const uint32_t ts = trow + S_COL + KEYS * b + HK * half;
+      const int b0 = sl.blk0 + PAGES * i + HP * half, npg = sl.nblk - PAGES * i - HP * half;
+      // Pages of the half with a key that some row must not see.
       unsigned edge = 0;
 #pragma unroll
-      for (int pg = 0; pg < PAGES; ++pg) {
+      for (int pg = 0; pg < HP; ++pg) {
         const BlockRange br = block_range(si, b0 + min(pg, npg - 1));
         if (pg >= npg || br.lo > 0 || br.hi < PS || br.base + PS - 1 > last0) edge |= 1u << pg;
       }
-      uint32_t pw[KEYS / 2];
+      // Slots of page pg that the row sees.
+      auto seen = [&](int pg, int& lo, int& hi) {
+        const BlockRange br = block_range(si, b0 + pg);
+        lo = br.lo;
+        hi = pg < npg ? min(br.hi, last - br.base + 1) : 0;
+      };
+      uint32_t pw[HK / 2];
       float sum = 0.f, most = -INFINITY;
       auto weigh = [&] {
-        sum = 0.f;
         most = -INFINITY;
         float2 rs[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
         const float2 c2 = make_float2(c, c), sh = make_float2(P_SHIFT, P_SHIFT);
         const float2 nm = make_float2(-m, -m);
 #pragma unroll
-        for (int part = 0; part < 4; ++part) {
+        for (int part = 0; part < 2; ++part) {
           float s[32];
           tmem_ld32(ts + 32 * part, s);
 #pragma unroll
           for (int k = 0; k < 32; k += 2) {
-            float2 a = __ffma2_rn(__fadd2_rn(make_float2(s[k], s[k + 1]), nm), c2, sh);
+            const float2 a = __ffma2_rn(__fadd2_rn(make_float2(s[k], s[k + 1]), nm), c2, sh);
             s[k] = a.x;
             s[k + 1] = a.y;
           }
           if (edge >> (2 * part) & 3u) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const int pg = 2 * part + h;
-              const BlockRange br = block_range(si, b0 + min(pg, npg - 1));
-              const int hi = pg < npg ? min(br.hi, last - br.base + 1) : 0;
+              int lo, hi;
+              seen(2 * part + h, lo, hi);
 #pragma unroll
               for (int k = 0; k < PS; ++k)
-                if (k < br.lo || k >= hi) s[PS * h + k] = -INFINITY;
+                if (k < lo || k >= hi) s[PS * h + k] = -INFINITY;
             }
           }
 #pragma unroll
@@ -394,57 +429,72 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_kv4_kernel(
         }
         sum = (rs[0].x + rs[1].x) + (rs[0].y + rs[1].y);
       };
-      weigh();
-      if (!live) most = -INFINITY;
-      // (At the first stage with a key that the row sees m is -infinity: a new reference.)
-      if (__any_sync(FULL, most > P_SHIFT + P_LAG)) {
+      // A new reference where a weight would pass 2^(P_SHIFT + P_LAG), and at the first stage.  Both
+      // warps take every barrier of a stage, and leave together when a wait of either gave up.
+      bool need = false;
+      if (i > 0 && !dead) {
+        weigh();
+        need = __any_sync(FULL, live && most > P_SHIFT + P_LAG);
+      }
+      if (lane == 0) s_flag[8 * b + 4 * half + quarter] = dead ? 2 : need;
+      sync_quarter();
+      const int flags = s_flag[8 * b + quarter] | s_flag[8 * b + 4 + quarter];
+      dead = flags & 2;
+      if (dead) break;
+      const bool fresh = i == 0 || flags;
+      if (fresh) {
         float mx = -INFINITY;
 #pragma unroll
-        for (int part = 0; part < 4; ++part) {
+        for (int part = 0; part < 2; ++part) {
           float s[32];
           tmem_ld32(ts + 32 * part, s);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const int pg = 2 * part + h;
-            const BlockRange br = block_range(si, b0 + min(pg, npg - 1));
-            const int hi = pg < npg ? min(br.hi, last - br.base + 1) : 0;
+            int lo, hi;
+            seen(2 * part + h, lo, hi);
 #pragma unroll
             for (int k = 0; k < PS; ++k)
-              if (k >= br.lo && k < hi) mx = fmaxf(mx, s[PS * h + k]);
+              if (k >= lo && k < hi) mx = fmaxf(mx, s[PS * h + k]);
           }
         }
-        const float mn = most > P_SHIFT + P_LAG ? fmaxf(m, mx) : m;
-        const float f = mn == m ? 1.f : weight2(m, mn, c);
+        s_row[M * (1 + half) + r] = mx;
+        sync_quarter();
+        const float mn = fmaxf(m, fmaxf(mx, s_row[M * (2 - half) + r]));
+        const float f = weight2(m, mn, c);
         if (i > 0) {
-          // The products so far are complete: their rows may be scaled.
-          if (!wait(B_PV + (b ^ 1), (i - 1) >> 1)) {
-            dead = true;
-            break;
-          }
+          // The products so far are complete: this thread's half of the row's columns is scaled.
+          dead = !wait(B_PV + (b ^ 1), (i - 1) >> 1);
           tc_fence_after();
+          if (!dead) {
 #pragma unroll 1
-          for (int x = 0; x < D / 16; ++x) {
-            float o[16];
-            tmem_ld16(trow + O_COL + 16 * x, o);
+            for (int x = 0; x < D / 32; ++x) {
+              float o[16];
+              tmem_ld16(trow + O_COL + D / 2 * half + 16 * x, o);
 #pragma unroll
-            for (int k = 0; k < 16; ++k) o[k] *= f;
-            tmem_st16(trow + O_COL + 16 * x, o);
+              for (int k = 0; k < 16; ++k) o[k] *= f;
+              tmem_st16(trow + O_COL + D / 2 * half + 16 * x, o);
+            }
           }
         }
         l *= f;
         m = mn;
-        weigh();
+        if (!dead) weigh();
+        // (Both have read the other's maximum before either writes one again.)
+        if (lane == 0) s_flag[16 + 4 * half + quarter] = dead;
+        sync_quarter();
+        dead = s_flag[16 + quarter] | s_flag[16 + 4 + quarter];
+        if (dead) break;
       }
       l += sum;
       __syncwarp();
       tmem_st32(ts, pw);
-      tmem_st32(ts + 32, pw + 32);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars[B_P_FULL + b]);
     }
     if (n_st > 0 && !dead) dead = !wait(B_PV + ((n_st - 1) & 1), (n_st - 1) >> 1);
     tc_fence_after();
+    s_row[M * (1 + half) + r] = l;
   } else if (warp < W_LOAD) {
     // ---------------- operands ----------------
     const int pg = warp - W_OP;
@@ -493,6 +543,16 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_kv4_kernel(
       return lane < PAGES && b < sl.nblk ? block_page(si, hrow, lrow, sl.blk0 + b) : 0;
     };
     int done = 0, page = page_at(lane);
+    {
+      // The query rows (1 KiB a token) and rotary rows (512 B) into L2 ahead of the softmax warps.
+      const char* qb = reinterpret_cast<const char*>(q + ((size_t)si.q_row0 * d.q_heads + sl.head * G) * D);
+      const char* rb = reinterpret_cast<const char*>(d.rope + (size_t)si.pos_first * (D / 2));
+      for (int x = lane; x < si.t * 12; x += 32) {
+        const int t = x / 12, line = x % 12;
+        prefetch_l2(line < 8 ? qb + (size_t)t * d.q_heads * D * 2 + line * 128
+                             : rb + (size_t)t * 512 + (line - 8) * 128);
+      }
+    }
     for (int i = 0; i < n_st; ++i) {
       const int slot = i % RAW, npg = min(PAGES, sl.nblk - PAGES * i);
       const int next = page_at(PAGES * (i + 1) + lane);
@@ -541,8 +601,9 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_kv4_kernel(
         const uint64_t v_desc = smem_desc(sbase + OFF_V + b * TILE, PANEL, 1024);
 #pragma unroll
         for (int kk = 0; kk < KEYS / 16; ++kk)
-          tc_mma_ts(tmem + O_COL, tmem + S_COL + KEYS * b + 8 * kk, desc_at(v_desc, kk * 16 * 128),
-                    ID, i > 0 || kk > 0);
+          tc_mma_ts(tmem + O_COL, tmem + S_COL + KEYS * b + (kk >> 2) * (KEYS / 2) + (kk & 3) * 8,
+                    desc_at(v_desc, kk * 16 * 128), ID,
+                    i > 0 || kk > 0);
         tc_commit(&bars[B_PV + b]);
         tc_commit(&bars[B_V_EMPTY + b]);
       }
@@ -559,17 +620,18 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_kv4_kernel(
   tc_fence_after();
 
   // ---------------- output ----------------
-  if (warp < SM_WARPS && warp * 32 < R) {
-    const int r = tid;
+  if (warp < SM_WARPS && 32 * quarter < R) {
+    const int r = 32 * quarter + lane;
     const bool live = r < R;
-    const uint32_t trow = tmem + ((uint32_t)(warp * 32) << 16) + O_COL;
+    const uint32_t trow = tmem + ((uint32_t)(32 * quarter) << 16) + O_COL;
     const int last = last0 + r / G;
+    l = s_row[M + r] + s_row[2 * M + r];
     const float f = k_slices == 1 ? 16.f / l : 1.f;
     __nv_bfloat16* orow =
         out + ((size_t)(si.q_row0 + r / G) * d.q_heads + sl.head * G + r % G) * D;
     float* prow = reinterpret_cast<float*>(smem + OFF_K + r * ROW_PITCH);
 #pragma unroll 1
-    for (int x = 0; x < D / GROUP; ++x) {
+    for (int x = 2 * half; x < 2 * half + 2; ++x) {  // this thread's half of the row
       float o[32];
       __syncwarp();
       if (n_st > 0) {
@@ -593,7 +655,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_kv4_kernel(
         }
       }
     }
-    if (live && k_slices > 1)
+    if (live && k_slices > 1 && half == 0)
       *reinterpret_cast<float4*>(prow + D) = make_float4(dead ? -INFINITY : m, l, c, 0.f);
   }
   tc_fence_before();
