@@ -687,7 +687,7 @@ cudaError_t launch_any(const Dev& d, const Limits& lim, int layer, const void* q
 }  // namespace
 
 cudaError_t kv4_prefill_limits(const Dev& d, Limits* lim) {
-  return d.esz == 2 ? kv4_prefill_tc_limits(d, lim) : limits_of<float, 64>(lim);
+  return d.esz == 2 ? kv4_prefill_tc_limits(lim) : limits_of<float, 64>(lim);
 }
 
 cudaError_t launch_attn_kv4(const Dev& d, const Limits& lim, LaunchOrder* order, int layer,

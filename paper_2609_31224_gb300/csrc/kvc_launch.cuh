@@ -56,7 +56,6 @@ struct Limits {
   int f32_cluster[2][2];           // largest cluster of the binary32 prefill: [rows][spread]
   int kv4_decode;                  // CTAs of the stream-K decode over 4-bit rows
   int kv4_prefill[KV4_PF_WARPS + 1];  // [w] CTAs of the prefill with w warps to a page
-  int kv4_prefill_stream_k;        // CTAs of the stream-K split of the bfloat16 prefill over them
   int kv4_clusters[PF_MAX_SLICES + 1];  // [k] clusters of k CTAs of the bfloat16 prefill over them
 };
 cudaError_t query_limits(const Dev& d, Limits* lim);
@@ -104,7 +103,7 @@ cudaError_t kv4_prefill_limits(const Dev& d, Limits* lim);
 cudaError_t launch_prefill_kv4_tc(const Dev& d, const Limits& lim, int layer, const void* q,
                                   void* out, int n_pairs, int64_t units, bool early,
                                   cudaStream_t s);
-cudaError_t kv4_prefill_tc_limits(const Dev& d, Limits* lim);
+cudaError_t kv4_prefill_tc_limits(Limits* lim);
 // Attention launches may start while the kernel before them in the stream finishes.  early:
 // they may also read what the append wrote before that (an attention launch of the same
 // append came before, so the append is complete).
