@@ -27,16 +27,57 @@ __device__ inline float scale_of(uint32_t most) {
 }
 __device__ inline __half stored_scale(float s) { return __float2half_rn(s * 0.0625f); }
 
-// Nibbles of N <= 8 elements of a group of scale s (rounded to nearest, ties to even, of the quotient).
+// Largest |x| of three, NaN if one is.
+__device__ inline float most_of(float a, float b, float c) {
+  float y;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
 template <int N>
-__device__ inline uint32_t codes_of(const float (&x)[N], float s) {
-  const float by = s > 0.f ? s : 1.f;
+__device__ inline uint32_t most_of(const float (&x)[N]) {
+  float y = 0.f;
+#pragma unroll
+  for (int i = 0; i + 1 < N; i += 2) y = most_of(y, x[i], x[i + 1]);
+  if constexpr (N % 2 == 1) y = most_of(y, x[N - 1], 0.f);
+  return __float_as_uint(y);
+}
+
+// What a group's elements are divided by (its scale, 1 where that is 0 or NaN), and the reciprocal in
+// two words: inv to nearest, rest = 1 / by - inv from the remainder 1 - inv by, which one fma gives
+// exactly.  x inv + x rest is then the quotient but for 2^-48 of it, and its rounding to binary32 is
+// that of x / by wherever the nearest integer depends on it: `by` has 7 significant bits, so the
+// quotient of a number next to (k + 1/2) by is at least 2^-33 away from what rounds to k + 1/2.
+struct Divisor {
+  float by, inv, rest;
+  __device__ explicit Divisor(float s) {
+    by = s > 0.f ? s : 1.f;
+    inv = __frcp_rn(by);
+    rest = __fmaf_rn(-inv, by, 1.f) * inv;
+  }
+  // Whether a code of the group whose largest |x| has these bits can pass CODE_MAX (its scale is the
+  // finest, the largest or none).
+  __device__ bool passes(uint32_t most) const { return most > __float_as_uint(7.4f * by); }
+};
+// Elements of a group whose codes may pass CODE_MAX, at what CODE_MAX stands for (NaN at 0).
+template <int N>
+__device__ inline void hold_codes(float (&x)[N], float by) {
+  const float lim = CODE_MAX * by;
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = isnan(x[i]) ? 0.f : fminf(fmaxf(x[i], -lim), lim);
+}
+
+// Nibbles of N <= 8 elements (rounded to nearest, ties to even, of the quotient; none passes
+// CODE_MAX).  1.5 2^23 + 8 puts code + 8 in the low bits of the sum; the bits above them add up to a
+// constant that the word starts without.
+template <int N>
+__device__ inline uint32_t codes_of(const float (&x)[N], float inv, float rest) {
+  constexpr uint32_t MAGIC = 0x4B400000u;  // 1.5 2^23
   uint32_t w = 0;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int c = max(-CODE_MAX, min(CODE_MAX, __float2int_rn(__fdiv_rn(x[i], by))));
-    w |= (uint32_t)(c + 8) << (4 * i);
-  }
+  for (int i = 0; i < N; ++i) w -= MAGIC << (4 * i);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    w += __float_as_uint(__fmaf_rn(x[i], inv, x[i] * rest) + (12582912.f + 8.f)) << (4 * i);
   return w;
 }
 

@@ -390,13 +390,13 @@ __device__ void write_new_row(const Dev& d, int layer, const SeqInfo& si, int he
   uint8_t* tiles = d.pool + tile_at(D, d.layers, d.kv_heads, gs / PS, layer, head, 0);
 #pragma unroll
   for (int kv = 0; kv < 2; ++kv) {
-    uint32_t most = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) most = max(most, abs_bits(y[kv][e]));
+    uint32_t most = most_of(y[kv]);
 #pragma unroll
     for (int o = 1; o < LANES; o <<= 1) most = max(most, __shfl_xor_sync(FULL, most, o));
     const float s = scale_of(most);
-    const uint32_t codes = codes_of(y[kv], s);
+    const Divisor div(s);
+    if (div.passes(most)) hold_codes(y[kv], div.by);
+    const uint32_t codes = codes_of(y[kv], div.inv, div.rest);
     const int at = kv * 9 * D + (kv ? v_codes(D, slot, d0 & ~7) : k_codes(D, slot, d0 & ~7)) +
                    d0 % 8 / 2;
     if constexpr (E == 4) {

@@ -9,14 +9,17 @@ namespace {
 using namespace kv4;
 
 constexpr int THREADS = 256;
+constexpr unsigned FULL = 0xFFFFFFFFu;
 
 // K rotated at its position and V, quantised into the page slots of the plan kernel.  Input
 // [L][total][Hkv][D]; blockIdx.y is the input layer, cache layer layer0 + blockIdx.y.
 // A thread takes 8 dims of the first half of a K row with their rotate-half partners, and the
-// same dims of the V row; the 4 threads of a group find its largest |x| by shuffles.
+// same dims of the V row.  Its 4 x 8 elements lie in four groups, which it shares with three other
+// threads: each of the four finds the scale and the reciprocal of one group and hands them out.
+// `early`: the caller's rows were complete before the kernel in front could start.
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS) append_kv4_kernel(Dev d, int total, int layer0,
-                                                             const T* k, const T* v) {
+                                                             const T* k, const T* v, int early) {
   constexpr int KC = D / 16, HALF = D / 2, NG = D / GROUP;
   static_assert(GROUP == 32 && KC % 4 == 0, "four threads of eight dims share a scale");
   const int H = d.kv_heads;
@@ -25,6 +28,7 @@ __global__ void __launch_bounds__(THREADS) append_kv4_kernel(Dev d, int total, i
   const int64_t row = idx / KC;
   const int g = (int)(row / H), h = (int)(row % H);
   const bool in = g < total;
+  if (!early) pdl_wait();
   pdl_launch_dependents();
   Eight<T> ka = {}, kb = {}, va = {}, vb = {};
   if (in) {
@@ -45,42 +49,48 @@ __global__ void __launch_bounds__(THREADS) append_kv4_kernel(Dev d, int total, i
   va.get(wa);
   vb.get(wb);
   const float4* t4 = reinterpret_cast<const float4*>(d.rope + (size_t)pos * HALF + c * 8);
-  uint32_t most[4] = {0, 0, 0, 0};
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
     const float4 cs = t4[e / 2];
     turn_pair(x1[e], x2[e], make_float2(cs.x, cs.y), ya[e], yb[e]);
     turn_pair(x1[e + 1], x2[e + 1], make_float2(cs.z, cs.w), ya[e + 1], yb[e + 1]);
   }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    most[0] = max(most[0], abs_bits(ya[e]));
-    most[1] = max(most[1], abs_bits(yb[e]));
-    most[2] = max(most[2], abs_bits(wa[e]));
-    most[3] = max(most[3], abs_bits(wb[e]));
+  // Largest |x| of group i to the quad's thread i.
+  const int own = c % 4, lane = threadIdx.x & 31;
+  const uint32_t most[4] = {most_of(ya), most_of(yb), most_of(wa), most_of(wb)};
+  uint32_t mx;
+  {
+    const bool b1 = own & 2, b0 = own & 1;
+    const uint32_t p = max(b1 ? most[2] : most[0], __shfl_xor_sync(FULL, b1 ? most[0] : most[2], 2));
+    const uint32_t r = max(b1 ? most[3] : most[1], __shfl_xor_sync(FULL, b1 ? most[1] : most[3], 2));
+    mx = max(b0 ? r : p, __shfl_xor_sync(FULL, b0 ? p : r, 1));
   }
+  const float s = scale_of(mx);
+  const Divisor div(s);
+  const bool passes = __any_sync(FULL, div.passes(mx));
+  float inv[4], rest[4];
 #pragma unroll
-  for (int o = 1; o < 4; o <<= 1)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) most[i] = max(most[i], __shfl_xor_sync(0xFFFFFFFFu, most[i], o));
+  for (int i = 0; i < 4; ++i) {
+    inv[i] = __shfl_sync(FULL, div.inv, lane & ~3 | i);
+    rest[i] = __shfl_sync(FULL, div.rest, lane & ~3 | i);
+  }
+  if (passes) {
+    hold_codes(ya, __shfl_sync(FULL, div.by, lane & ~3));
+    hold_codes(yb, __shfl_sync(FULL, div.by, lane & ~3 | 1));
+    hold_codes(wa, __shfl_sync(FULL, div.by, lane & ~3 | 2));
+    hold_codes(wb, __shfl_sync(FULL, div.by, lane & ~3 | 3));
+  }
   if (!live) return;
-  float s[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) s[i] = scale_of(most[i]);
   const int page = gs / PS, slot = gs % PS, layer = layer0 + blockIdx.y;
   uint8_t* kt = d.pool + tile_at(D, d.layers, H, page, layer, h, 0);
   uint8_t* vt = kt + tile_bytes(D);
-  *reinterpret_cast<uint32_t*>(kt + k_codes(D, slot, 8 * c)) = codes_of(ya, s[0]);
-  *reinterpret_cast<uint32_t*>(kt + k_codes(D, slot, HALF + 8 * c)) = codes_of(yb, s[1]);
-  *reinterpret_cast<uint32_t*>(vt + v_codes(D, slot, 8 * c)) = codes_of(wa, s[2]);
-  *reinterpret_cast<uint32_t*>(vt + v_codes(D, slot, HALF + 8 * c)) = codes_of(wb, s[3]);
-  if (c % 4 == 0) {
-    const int group = c / 4;
-    *reinterpret_cast<__half*>(kt + k_scale(D, slot, group)) = stored_scale(s[0]);
-    *reinterpret_cast<__half*>(kt + k_scale(D, slot, NG / 2 + group)) = stored_scale(s[1]);
-    *reinterpret_cast<__half*>(vt + v_scale(D, slot, group)) = stored_scale(s[2]);
-    *reinterpret_cast<__half*>(vt + v_scale(D, slot, NG / 2 + group)) = stored_scale(s[3]);
-  }
+  *reinterpret_cast<uint32_t*>(kt + k_codes(D, slot, 8 * c)) = codes_of(ya, inv[0], rest[0]);
+  *reinterpret_cast<uint32_t*>(kt + k_codes(D, slot, HALF + 8 * c)) = codes_of(yb, inv[1], rest[1]);
+  *reinterpret_cast<uint32_t*>(vt + v_codes(D, slot, 8 * c)) = codes_of(wa, inv[2], rest[2]);
+  *reinterpret_cast<uint32_t*>(vt + v_codes(D, slot, HALF + 8 * c)) = codes_of(wb, inv[3], rest[3]);
+  const int group = c / 4 + (own & 1) * (NG / 2);
+  const int at = own & 2 ? tile_bytes(D) + v_scale(D, slot, group) : k_scale(D, slot, group);
+  *reinterpret_cast<__half*>(kt + at) = stored_scale(s);
 }
 
 // Survivors of an eviction (the move list of evict_plan_kernel), every layer, K and V, and head.
@@ -234,11 +244,11 @@ cudaError_t launch_append_layers_kv4(const Dev& d, int total, int layer0, int n_
   const int64_t threads = (int64_t)total * d.kv_heads * (d.head_dim / 16);
   const dim3 grid((unsigned)((threads + THREADS - 1) / THREADS), n_layers);
   if (d.esz == 2)
-    return launch_ex(&append_kv4_kernel<__nv_bfloat16, 128>, grid, dim3(THREADS), 0, s, after_plan,
-                     d, total, layer0, static_cast<const __nv_bfloat16*>(k),
-                     static_cast<const __nv_bfloat16*>(v));
-  return launch_ex(&append_kv4_kernel<float, 64>, grid, dim3(THREADS), 0, s, after_plan, d, total,
-                   layer0, static_cast<const float*>(k), static_cast<const float*>(v));
+    return launch_ex(&append_kv4_kernel<__nv_bfloat16, 128>, grid, dim3(THREADS), 0, s, true, d,
+                     total, layer0, static_cast<const __nv_bfloat16*>(k),
+                     static_cast<const __nv_bfloat16*>(v), (int)after_plan);
+  return launch_ex(&append_kv4_kernel<float, 64>, grid, dim3(THREADS), 0, s, true, d, total, layer0,
+                   static_cast<const float*>(k), static_cast<const float*>(v), (int)after_plan);
 }
 
 cudaError_t launch_evict_copy_kv4(const Dev& d, int sms, cudaStream_t s) {

@@ -510,3 +510,21 @@ def test_refusals():
     q = torch.zeros((33, 8, 128), dtype=torch.bfloat16, device="cuda")
     refused(lambda: c.attn_prefill_chunk(0, q, q), "32 tokens")
     p.check_rows([0, 1])                      # nothing of it changed the cache
+
+
+@pytest.mark.parametrize("exp", [-14, -3, 0, 6])
+def test_numbers_next_to_half_a_step(exp):
+    """Every scale of an octave, its half steps and their neighbours on both sides: codes are those of
+    the rounded quotient, ties to even."""
+    half, f = [], np.float32
+    for m in range(64, 128):
+        s = f(m) * f(2.0 ** (exp - 6))
+        at = [(2 * j + 1) * s / f(2) for j in range(7)]
+        near = [np.nextafter(x, f(y)) for x in at for y in (0, np.inf)]
+        half.append([7 * s] + at + near + [-x for x in at + near][:10])
+    half = np.array(half, f)                                 # [64 scales, 32]
+    p = Pair("f32", 2, 1, layers=1)
+    rows = half.reshape(16, 1, 2, 64)
+    assert (np.abs(rows).reshape(-1, 32).max(-1) == half[:, 0]).all()
+    p.append([0], [16], kv=(p.normal(16, 1, 2, 64), rows))
+    p.check_rows([0])
