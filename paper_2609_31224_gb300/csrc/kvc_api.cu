@@ -277,7 +277,8 @@ void enqueue_readback(kvc_ctx* ctx, cudaStream_t s) {
 
 // One layer's K/V of the last append, in a launch of their own.
 cudaError_t write_layer(kvc_ctx* ctx, int layer, const void* k, const void* v, cudaStream_t s) {
-  return ctx->kv4 ? launch_append_layers_kv4(ctx->d, ctx->last_total, layer, 1, k, v, false, s)
+  return ctx->kv4 ? launch_append_layers_kv4(ctx->d, ctx->last_total, layer, 1, k, v, false,
+                                             ctx->order.planned(), ctx->lim.sms, s)
                   : launch_append_layers(ctx->d, ctx->last_total, layer, 1, k, v, false, s);
 }
 
@@ -458,7 +459,7 @@ int kvc_append_chunk(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, const i
   for (int i = 0; i < n_seq; ++i) a.sessions[i] = h_sessions[i];
   for (int i = 0; i <= n_seq; ++i) a.cu[i] = h_cu_tokens[i];
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  KVC_CUDA(launch_append(ctx->d, ctx->kv4, a, d_types, d_k, d_v, single, s));
+  KVC_CUDA(launch_append(ctx->d, ctx->kv4, a, d_types, d_k, d_v, single, ctx->lim.sms, s));
   for (int i = 0; i < n_seq; ++i) {
     const int sid = h_sessions[i];
     const int t = h_cu_tokens[i + 1] - h_cu_tokens[i];

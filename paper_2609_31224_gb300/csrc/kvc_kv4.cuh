@@ -18,7 +18,10 @@ __device__ inline uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FF
 // The scale of a group whose largest |x| has these bits.
 __device__ inline float scale_of(uint32_t most) {
   if (most >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
-  const float s = __fdiv_rn(__uint_as_float(most), (float)CODE_MAX);
+  // most / 7 by the two words of 1 / 7 (the nearest binary32 number and what is left): rounded as the
+  // quotient is, for every most.
+  constexpr float SEVENTH = (float)(1. / CODE_MAX), REST = (float)(1. / CODE_MAX - (double)SEVENTH);
+  const float s = __fmaf_rn(__uint_as_float(most), SEVENTH, __uint_as_float(most) * REST);
   // Multiples of 2^e: the seventh significant bit of s, 2^-20 at the finest.
   const int e = max((int)(__float_as_uint(s) >> 23) - 127 - (SCALE_BITS - 1), SCALE_FINEST_EXP);
   const float step = __uint_as_float((uint32_t)(127 + e) << 23);
@@ -43,15 +46,15 @@ __device__ inline uint32_t most_of(const float (&x)[N]) {
 }
 
 // What a group's elements are divided by (its scale, 1 where that is 0 or NaN), and the reciprocal in
-// two words: inv to nearest, rest = 1 / by - inv from the remainder 1 - inv by, which one fma gives
-// exactly.  x inv + x rest is then the quotient but for 2^-48 of it, and its rounding to binary32 is
-// that of x / by wherever the nearest integer depends on it: `by` has 7 significant bits, so the
-// quotient of a number next to (k + 1/2) by is at least 2^-33 away from what rounds to k + 1/2.
+// two words: inv within a unit in the last place, rest = 1 / by - inv from the remainder 1 - inv by,
+// which one fma gives exactly.  x inv + x rest is then the quotient but for 2^-44 of it, and its rounding
+// to binary32 is that of x / by wherever the nearest integer depends on it: `by` has 7 significant bits,
+// so the quotient of a number next to (k + 1/2) by is at least 2^-33 away from what rounds to k + 1/2.
 struct Divisor {
   float by, inv, rest;
   __device__ explicit Divisor(float s) {
     by = s > 0.f ? s : 1.f;
-    inv = __frcp_rn(by);
+    asm("rcp.approx.f32 %0, %1;" : "=f"(inv) : "f"(by));
     rest = __fmaf_rn(-inv, by, 1.f) * inv;
   }
   // Whether a code of the group whose largest |x| has these bits can pass CODE_MAX (its scale is the
@@ -75,9 +78,18 @@ __device__ inline uint32_t codes_of(const float (&x)[N], float inv, float rest) 
   uint32_t w = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) w -= MAGIC << (4 * i);
+  if constexpr (N % 2 == 1) {
+    w += __float_as_uint(__fmaf_rn(x[N - 1], inv, x[N - 1] * rest) + (12582912.f + 8.f)) << (4 * (N - 1));
+  }
+  const float2 inv2 = make_float2(inv, inv), rest2 = make_float2(rest, rest);
+  const float2 up = make_float2(12582912.f + 8.f, 12582912.f + 8.f);
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-    w += __float_as_uint(__fmaf_rn(x[i], inv, x[i] * rest) + (12582912.f + 8.f)) << (4 * i);
+  for (int i = 0; i + 1 < N; i += 2) {
+    const float2 y = make_float2(x[i], x[i + 1]);
+    const float2 z = __fadd2_rn(__ffma2_rn(y, inv2, __fmul2_rn(y, rest2)), up);
+    w += __float_as_uint(z.x) << (4 * i);
+    w += __float_as_uint(z.y) << (4 * i + 4);
+  }
   return w;
 }
 

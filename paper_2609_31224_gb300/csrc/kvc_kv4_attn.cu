@@ -701,7 +701,8 @@ cudaError_t launch_attn_kv4(const Dev& d, const Limits& lim, LaunchOrder* order,
     return e;
   }
   if (fused) {
-    const cudaError_t e = launch_append_layers_kv4(d, total, layer, 1, new_k, new_v, false, s);
+    const cudaError_t e = launch_append_layers_kv4(d, total, layer, 1, new_k, new_v, false,
+                                                   order->planned(), lim.sms, s);
     if (e != cudaSuccess) return e;
     order->layer_write(layer);
   }

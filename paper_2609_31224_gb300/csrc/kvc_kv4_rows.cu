@@ -10,87 +10,130 @@ using namespace kv4;
 
 constexpr int THREADS = 256;
 constexpr unsigned FULL = 0xFFFFFFFFu;
+constexpr int APPEND_CTAS = 4;  // CTAs of the write per SM
 
 // K rotated at its position and V, quantised into the page slots of the plan kernel.  Input
-// [L][total][Hkv][D]; blockIdx.y is the input layer, cache layer layer0 + blockIdx.y.
-// A thread takes 8 dims of the first half of a K row with their rotate-half partners, and the
-// same dims of the V row.  Its 4 x 8 elements lie in four groups, which it shares with three other
-// threads: each of the four finds the scale and the reciprocal of one group and hands them out.
-// `early`: the caller's rows were complete before the kernel in front could start.
+// [L][total][Hkv][D]; blockIdx.y is the input layer, cache layer layer0 + blockIdx.y.  The first
+// half of the CTAs takes K, the other V (in turn they would leave every second SM the rotations), each
+// several blocks of rows: the next block's rows and slots are on their way while one is worked on.
+// A thread takes 8 dims of the first half of a row and their rotate-half partners.  Its 2 x 8 elements
+// lie in two groups, which it shares with three other threads: two of the four find the scale and the
+// reciprocal of either group and hand them out.
+// Before the kernel in front is complete, `early` launches read the caller's rows (complete before
+// that kernel could start), `planned` ones the slots (the plan kernel was complete by then).
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS) append_kv4_kernel(Dev d, int total, int layer0,
-                                                             const T* k, const T* v, int early) {
+                                                             const T* k, const T* v, bool early,
+                                                             bool planned) {
   constexpr int KC = D / 16, HALF = D / 2, NG = D / GROUP;
   static_assert(GROUP == 32 && KC % 4 == 0, "four threads of eight dims share a scale");
-  const int H = d.kv_heads;
-  const int64_t idx = (int64_t)blockIdx.x * THREADS + threadIdx.x;
-  const int c = (int)(idx % KC);
-  const int64_t row = idx / KC;
-  const int g = (int)(row / H), h = (int)(row % H);
-  const bool in = g < total;
-  if (!early) pdl_wait();
-  pdl_launch_dependents();
-  Eight<T> ka = {}, kb = {}, va = {}, vb = {};
-  if (in) {
-    const size_t off = (((size_t)blockIdx.y * total + g) * H + h) * D + c * 8;
-    ka.load(k + off);
-    kb.load(k + off + HALF);
-    va.load(v + off);
-    vb.load(v + off + HALF);
+  const int H = d.kv_heads, n_cta = gridDim.x >> 1, kv = (int)blockIdx.x >= n_cta, layer = layer0 + blockIdx.y;
+  const T* from = (kv ? v : k) + (size_t)blockIdx.y * total * H * D;
+  // (A call has 2^20 tokens at most: rows count in 32 bits.)  A row's token and head are
+  // carried along, not divided out.
+  const int step = n_cta * (THREADS / KC), n = total * H;
+  const int c = threadIdx.x % KC, lane = threadIdx.x & 31, step_g = step / H, step_h = step % H;
+  struct Block {
+    Eight<T> a, b;
+    int g, h, gs, pos;
+    bool live;
+  };
+  int n_tok = 0;
+  auto ask_rows = [&](Block& x) {
+    x.a = {};
+    x.b = {};
+    if (x.g >= total) return;
+    const T* p = from + ((size_t)x.g * H + x.h) * D + c * 8;
+    x.a.load(p);
+    x.b.load(p + HALF);
+  };
+  auto ask_slots = [&](Block& x) {
+    // (Nothing to do where the plan kernel failed: error recorded.  All threads stay for the
+    // shuffles.)
+    x.live = x.g < n_tok;
+    x.gs = x.live ? d.tok_slot[x.g] : 0;
+    x.pos = x.live && !kv ? d.tok_pos[x.g] : 0;
+  };
+  int first = ((int)blockIdx.x - kv * n_cta) * (THREADS / KC);
+  Block cur, next;
+  cur.g = (first + (int)threadIdx.x / KC) / H;
+  cur.h = (first + (int)threadIdx.x / KC) % H;
+  if (early) {
+    ask_rows(cur);
+    pdl_launch_dependents();
+  }
+  if (planned) {
+    n_tok = min(total, d.g->total_tokens);
+    ask_slots(cur);
   }
   pdl_wait();
-  // (Nothing to do where the plan kernel failed: error recorded.  All threads stay for the
-  // shuffles.)
-  const bool live = in && g < d.g->total_tokens;
-  const int gs = live ? d.tok_slot[g] : 0, pos = live ? d.tok_pos[g] : 0;
-  float x1[8], x2[8], ya[8], yb[8], wa[8], wb[8];
-  ka.get(x1);
-  kb.get(x2);
-  va.get(wa);
-  vb.get(wb);
-  const float4* t4 = reinterpret_cast<const float4*>(d.rope + (size_t)pos * HALF + c * 8);
+  if (!planned) {
+    n_tok = min(total, d.g->total_tokens);
+    ask_slots(cur);
+  }
+  if (!early) {
+    pdl_launch_dependents();
+    ask_rows(cur);
+  }
+  for (; first < n; first += step, cur = next) {
+    float xa[8], xb[8];
+    next.g = cur.g + step_g;
+    next.h = cur.h + step_h;
+    if (next.h >= H) {
+      next.h -= H;
+      ++next.g;
+    }
+    if (kv == 0) {
+      float4 t4[4];
 #pragma unroll
-  for (int e = 0; e < 8; e += 2) {
-    const float4 cs = t4[e / 2];
-    turn_pair(x1[e], x2[e], make_float2(cs.x, cs.y), ya[e], yb[e]);
-    turn_pair(x1[e + 1], x2[e + 1], make_float2(cs.z, cs.w), ya[e + 1], yb[e + 1]);
-  }
-  // Largest |x| of group i to the quad's thread i.
-  const int own = c % 4, lane = threadIdx.x & 31;
-  const uint32_t most[4] = {most_of(ya), most_of(yb), most_of(wa), most_of(wb)};
-  uint32_t mx;
-  {
-    const bool b1 = own & 2, b0 = own & 1;
-    const uint32_t p = max(b1 ? most[2] : most[0], __shfl_xor_sync(FULL, b1 ? most[0] : most[2], 2));
-    const uint32_t r = max(b1 ? most[3] : most[1], __shfl_xor_sync(FULL, b1 ? most[1] : most[3], 2));
-    mx = max(b0 ? r : p, __shfl_xor_sync(FULL, b0 ? p : r, 1));
-  }
-  const float s = scale_of(mx);
-  const Divisor div(s);
-  const bool passes = __any_sync(FULL, div.passes(mx));
-  float inv[4], rest[4];
+      for (int e = 0; e < 4; ++e)
+        t4[e] = reinterpret_cast<const float4*>(d.rope + (size_t)cur.pos * HALF + c * 8)[e];
+      ask_rows(next);
+      ask_slots(next);
+      float x1[8], x2[8];
+      cur.a.get(x1);
+      cur.b.get(x2);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    inv[i] = __shfl_sync(FULL, div.inv, lane & ~3 | i);
-    rest[i] = __shfl_sync(FULL, div.rest, lane & ~3 | i);
+      for (int e = 0; e < 8; e += 2) {
+        const float4 cs = t4[e / 2];
+        turn_pair(x1[e], x2[e], make_float2(cs.x, cs.y), xa[e], xb[e]);
+        turn_pair(x1[e + 1], x2[e + 1], make_float2(cs.z, cs.w), xa[e + 1], xb[e + 1]);
+      }
+    } else {
+      ask_rows(next);
+      ask_slots(next);
+      cur.a.get(xa);
+      cur.b.get(xb);
+    }
+    // Largest |x| of the first group to threads 0 and 1 of the four, of the second to 2 and 3.
+    const bool second = lane & 2;
+    uint32_t mx;
+    {
+      const uint32_t ma = most_of(xa), mb = most_of(xb);
+      mx = max(second ? mb : ma, __shfl_xor_sync(FULL, second ? ma : mb, 2));
+      mx = max(mx, __shfl_xor_sync(FULL, mx, 1));
+    }
+    const float s = scale_of(mx);
+    const Divisor div(s);
+    if (__any_sync(FULL, div.passes(mx))) {
+      hold_codes(xa, __shfl_sync(FULL, div.by, lane & ~3));
+      hold_codes(xb, __shfl_sync(FULL, div.by, lane & ~3 | 2));
+    }
+    const uint32_t wa = codes_of(xa, __shfl_sync(FULL, div.inv, lane & ~3), __shfl_sync(FULL, div.rest, lane & ~3));
+    const uint32_t wb = codes_of(xb, __shfl_sync(FULL, div.inv, lane & ~3 | 2),
+                                 __shfl_sync(FULL, div.rest, lane & ~3 | 2));
+    if (!cur.live) continue;
+    const int page = cur.gs / PS, slot = cur.gs % PS;
+    uint8_t* tile = d.pool + tile_at(D, d.layers, H, page, layer, cur.h, kv);
+    *reinterpret_cast<uint32_t*>(tile + (kv ? v_codes(D, slot, 8 * c) : k_codes(D, slot, 8 * c))) = wa;
+    *reinterpret_cast<uint32_t*>(tile + (kv ? v_codes(D, slot, HALF + 8 * c)
+                                            : k_codes(D, slot, HALF + 8 * c))) = wb;
+    if (lane % 2 == 0) {
+      const int group = c / 4 + (second ? NG / 2 : 0);
+      *reinterpret_cast<__half*>(tile + (kv ? v_scale(D, slot, group) : k_scale(D, slot, group))) =
+          stored_scale(s);
+    }
   }
-  if (passes) {
-    hold_codes(ya, __shfl_sync(FULL, div.by, lane & ~3));
-    hold_codes(yb, __shfl_sync(FULL, div.by, lane & ~3 | 1));
-    hold_codes(wa, __shfl_sync(FULL, div.by, lane & ~3 | 2));
-    hold_codes(wb, __shfl_sync(FULL, div.by, lane & ~3 | 3));
-  }
-  if (!live) return;
-  const int page = gs / PS, slot = gs % PS, layer = layer0 + blockIdx.y;
-  uint8_t* kt = d.pool + tile_at(D, d.layers, H, page, layer, h, 0);
-  uint8_t* vt = kt + tile_bytes(D);
-  *reinterpret_cast<uint32_t*>(kt + k_codes(D, slot, 8 * c)) = codes_of(ya, inv[0], rest[0]);
-  *reinterpret_cast<uint32_t*>(kt + k_codes(D, slot, HALF + 8 * c)) = codes_of(yb, inv[1], rest[1]);
-  *reinterpret_cast<uint32_t*>(vt + v_codes(D, slot, 8 * c)) = codes_of(wa, inv[2], rest[2]);
-  *reinterpret_cast<uint32_t*>(vt + v_codes(D, slot, HALF + 8 * c)) = codes_of(wb, inv[3], rest[3]);
-  const int group = c / 4 + (own & 1) * (NG / 2);
-  const int at = own & 2 ? tile_bytes(D) + v_scale(D, slot, group) : k_scale(D, slot, group);
-  *reinterpret_cast<__half*>(kt + at) = stored_scale(s);
 }
 
 // Survivors of an eviction (the move list of evict_plan_kernel), every layer, K and V, and head.
@@ -124,50 +167,91 @@ __global__ void __launch_bounds__(THREADS) evict_copy_kv4_kernel(Dev d) {
   }
 }
 
-// 8 elements from dim dd of a stored row, as they are given back.
-template <typename T, int D, bool KV4>
-__device__ inline void copy_eight(const Dev& d, int gs, int layer, int kv, int h, int dd, T* to) {
-  const int page = gs / PS, slot = gs % PS;
-  if constexpr (KV4) {
-    const uint8_t* tile = d.pool + tile_at(D, d.layers, d.kv_heads, page, layer, h, kv);
-    const uint32_t w =
-        *reinterpret_cast<const uint32_t*>(tile + (kv ? v_codes(D, slot, dd) : k_codes(D, slot, dd)));
-    const __half m = *reinterpret_cast<const __half*>(
-        tile + (kv ? v_scale(D, slot, dd / GROUP) : k_scale(D, slot, dd / GROUP)));
+// 8 elements as they are given back, from their word and scale.  bfloat16: 128 + code + 8 is its pattern
+// 0x4300 | nibble, so the code comes exactly and the product with the scale (7 bits, exact too) is
+// rounded once.
+template <typename T>
+__device__ inline void give_eight(uint32_t w, __half m, T* to) {
+  if constexpr (sizeof(T) == 2) {
+    const __nv_bfloat162 s = __float2bfloat162_rn(__half2float(m) * 16.f), k136 = __float2bfloat162_rn(136.f);
+    uint32_t v[4];
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {  // dims p and p + 4
+      const uint32_t u = and_or(w >> (4 * p), 0x000F000Fu, 0x43004300u);
+      const __nv_bfloat162 y = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&u), k136), s);
+      v[p] = *reinterpret_cast<const uint32_t*>(&y);
+    }
+    *reinterpret_cast<uint4*>(to) =
+        make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410),
+                   __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632));
+  } else {
     float f[8];
     values_of(w, m, f);
     Eight<T>::store(to, f);
-  } else {
-    const uint4* src = reinterpret_cast<const uint4*>(
-        reinterpret_cast<const T*>(d.pool) + pool_offset_elems(d, page, layer, kv, h, slot) + dd);
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(to)[i] = src[i];
   }
 }
 
-// One warp's share of a row: all heads of K and of V, `row` their place in the outputs.
+// One warp's share of a row: all heads of K and of V, `row` their place in the outputs.  A lane keeps
+// its 8 dims and takes every STEP-th head, four of them on their way at a time.
 template <typename T, int D, bool KV4>
 __device__ inline void read_row(const Dev& d, int gs, int layer, size_t row, T* k_out, T* v_out,
                                 int lane) {
-  const int chunks = d.kv_heads * (D / 8);
-  for (int i = lane; i < 2 * chunks; i += 32) {
-    const int kv = i >= chunks, j = kv ? i - chunks : i;
-    T* to = (kv ? v_out : k_out) + (row * chunks + j) * 8;
-    if (gs >= 0) {
-      copy_eight<T, D, KV4>(d, gs, layer, kv, j / (D / 8), j % (D / 8) * 8, to);
-    } else {
-      const float zero[8] = {};
-      Eight<T>::store(to, zero);
+  constexpr int CHUNKS = D / 8, STEP = 32 / CHUNKS, BATCH = 4;
+  const int H = d.kv_heads, dd = lane % CHUNKS * 8, h0 = lane / CHUNKS;
+  k_out += row * H * D + dd;
+  v_out += row * H * D + dd;
+  if (gs < 0) {
+    const float zero[8] = {};
+    for (int h = h0; h < H; h += STEP) {
+      Eight<T>::store(k_out + h * D, zero);
+      Eight<T>::store(v_out + h * D, zero);
+    }
+    return;
+  }
+  const int page = gs / PS, slot = gs % PS;
+  if constexpr (KV4) {
+    const uint8_t* tile = d.pool + tile_at(D, d.layers, H, page, layer, 0, 0);
+    const int TB = (int)tile_bytes(D);
+    const int kc = k_codes(D, slot, dd), ks = k_scale(D, slot, dd / GROUP);
+    const int vc = TB + v_codes(D, slot, dd), vs = TB + v_scale(D, slot, dd / GROUP);
+    for (int h = h0; h < H; h += BATCH * STEP) {
+      uint32_t w[BATCH][2];
+      __half m[BATCH][2];
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) {
+        const uint8_t* at = tile + (size_t)min(h + u * STEP, H - 1) * 2 * TB;
+        w[u][0] = *reinterpret_cast<const uint32_t*>(at + kc);
+        w[u][1] = *reinterpret_cast<const uint32_t*>(at + vc);
+        m[u][0] = *reinterpret_cast<const __half*>(at + ks);
+        m[u][1] = *reinterpret_cast<const __half*>(at + vs);
+      }
+#pragma unroll
+      for (int u = 0; u < BATCH; ++u) {
+        if (h + u * STEP >= H) break;
+        give_eight(w[u][0], m[u][0], k_out + (h + u * STEP) * D);
+        give_eight(w[u][1], m[u][1], v_out + (h + u * STEP) * D);
+      }
+    }
+  } else {
+    for (int h = h0; h < H; h += STEP) {
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        const uint4* src = reinterpret_cast<const uint4*>(
+            reinterpret_cast<const T*>(d.pool) + pool_offset_elems(d, page, layer, kv, h, slot) + dd);
+        uint4* to = reinterpret_cast<uint4*>((kv ? v_out : k_out) + h * D);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) to[i] = src[i];
+      }
     }
   }
 }
 
-// Rows of the listed sessions (kvc_read_kv): output row r of layer blockIdx.y belongs to the
-// session i with cu[i] <= r < cu[i + 1] and is its retained position first[i] + r - cu[i]; zeros
-// where it holds no such position.
+// Rows of the listed sessions (kvc_read_kv): output row r of a layer belongs to the session i with
+// cu[i] <= r < cu[i + 1] and is its retained position first[i] + r - cu[i]; zeros where it holds no
+// such position.  A warp finds a row's slot once and gives it back for `per` layers, blockIdx.y per on.
 template <typename T, int D, bool KV4, int N>
 __global__ void __launch_bounds__(THREADS) read_kv_kernel(Dev d, ReadArgsT<N> a, int layer0,
-                                                          T* k_out, T* v_out,
+                                                          int n_layers, int per, T* k_out, T* v_out,
                                                           int64_t* resident_out) {
   pdl_wait();
   pdl_launch_dependents();
@@ -196,8 +280,9 @@ __global__ void __launch_bounds__(THREADS) read_kv_kernel(Dev d, ReadArgsT<N> a,
       const int j = st.live_head + (int)(i - st.n_hist);
       gs = d.live_pt[pt + j / PS] * PS + j % PS;
     }
-    read_row<T, D, KV4>(d, gs, layer0 + blockIdx.y, (size_t)blockIdx.y * a.total + r, k_out, v_out,
-                        lane);
+    const int end = min(n_layers, ((int)blockIdx.y + 1) * per);
+    for (int l = blockIdx.y * per; l < end; ++l)
+      read_row<T, D, KV4>(d, gs, layer0 + l, (size_t)l * a.total + r, k_out, v_out, lane);
   }
 }
 
@@ -218,11 +303,13 @@ __global__ void __launch_bounds__(THREADS) transcript_copy_kv4_kernel(Dev d, int
 template <typename T, int D, bool KV4, int N>
 cudaError_t launch_read(const Dev& d, const ReadArgsT<N>& a, int layer0, int n_layers, void* k_out,
                         void* v_out, int64_t* resident_out, int sms, cudaStream_t s) {
-  // As many warps as rows, up to a few CTAs per SM; one CTA for the counts alone.
+  // A warp to a row, in up to a few CTAs per SM, and to as many layers as leave two rounds of them; one
+  // CTA for the counts alone.
   const int rows = (a.total + THREADS / 32 - 1) / (THREADS / 32);
-  const dim3 grid(max(1, min(rows, sms * 8)), a.total > 0 ? n_layers : 1);
+  const int per = (int)max((int64_t)1, min((int64_t)n_layers, (int64_t)rows * n_layers / (sms * 16)));
+  const dim3 grid(max(1, min(rows, sms * 8)), a.total > 0 ? (n_layers + per - 1) / per : 1);
   return launch_ex(&read_kv_kernel<T, D, KV4, N>, grid, dim3(THREADS), 0, s, true, d, a, layer0,
-                   static_cast<T*>(k_out), static_cast<T*>(v_out), resident_out);
+                   n_layers, per, static_cast<T*>(k_out), static_cast<T*>(v_out), resident_out);
 }
 
 template <int N>
@@ -239,16 +326,19 @@ cudaError_t launch_read_of(const Dev& d, bool kv4, const ReadArgsT<N>& a, int la
 }  // namespace
 
 cudaError_t launch_append_layers_kv4(const Dev& d, int total, int layer0, int n_layers,
-                                     const void* k, const void* v, bool after_plan,
+                                     const void* k, const void* v, bool early, bool planned, int sms,
                                      cudaStream_t s) {
-  const int64_t threads = (int64_t)total * d.kv_heads * (d.head_dim / 16);
-  const dim3 grid((unsigned)((threads + THREADS - 1) / THREADS), n_layers);
+  const int rows = THREADS / (d.head_dim / 16);  // of a block
+  const int blocks = (total * d.kv_heads + rows - 1) / rows;
+  // Two blocks of rows a CTA or more where there are enough of them.
+  const int per_layer = max(1, sms * APPEND_CTAS / 2 / n_layers);
+  const dim3 grid(2 * (unsigned)min(blocks, per_layer), n_layers);
   if (d.esz == 2)
     return launch_ex(&append_kv4_kernel<__nv_bfloat16, 128>, grid, dim3(THREADS), 0, s, true, d,
                      total, layer0, static_cast<const __nv_bfloat16*>(k),
-                     static_cast<const __nv_bfloat16*>(v), (int)after_plan);
+                     static_cast<const __nv_bfloat16*>(v), early, planned);
   return launch_ex(&append_kv4_kernel<float, 64>, grid, dim3(THREADS), 0, s, true, d, total, layer0,
-                   static_cast<const float*>(k), static_cast<const float*>(v), (int)after_plan);
+                   static_cast<const float*>(k), static_cast<const float*>(v), early, planned);
 }
 
 cudaError_t launch_evict_copy_kv4(const Dev& d, int sms, cudaStream_t s) {

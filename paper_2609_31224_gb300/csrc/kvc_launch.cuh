@@ -68,7 +68,7 @@ cudaError_t launch_init(const Dev& d, double rope_base, cudaStream_t s);
 // one launch).
 // kv4: the rows are held in 4 bits.
 cudaError_t launch_append(const Dev& d, bool kv4, const AppendArgs& a, const uint8_t* types,
-                          const void* k, const void* v, bool single, cudaStream_t s);
+                          const void* k, const void* v, bool single, int sms, cudaStream_t s);
 // after_plan: launched right behind the plan kernel of the same append.
 cudaError_t launch_append_layers(const Dev& d, int total, int layer0, int n_layers, const void* k,
                                  const void* v, bool after_plan, cudaStream_t s);
@@ -81,8 +81,9 @@ cudaError_t launch_read_kv(const Dev& d, bool kv4, const ReadArgs& a, int layer0
                            void* k_out, void* v_out, int64_t* resident_out, int sms,
                            cudaStream_t s);
 // The parts of those calls that touch 4-bit rows (kvc_kv4_rows.cu), and the attention over them.
+// early: k and v were complete before the kernel in front could start; planned: the plan was.
 cudaError_t launch_append_layers_kv4(const Dev& d, int total, int layer0, int n_layers,
-                                     const void* k, const void* v, bool after_plan,
+                                     const void* k, const void* v, bool early, bool planned, int sms,
                                      cudaStream_t s);
 cudaError_t launch_evict_copy_kv4(const Dev& d, int sms, cudaStream_t s);
 cudaError_t launch_transcript_copy_kv4(const Dev& d, int cap, void* k_out, void* v_out, int sms,

@@ -1129,7 +1129,7 @@ cudaError_t launch_init(const Dev& d, double rope_base, cudaStream_t s) {
 // that one before it reads anything but the caller's inputs), so that a chain of short
 // kernels does not pay a full launch each.
 cudaError_t launch_append(const Dev& d, bool kv4, const AppendArgs& a, const uint8_t* types,
-                          const void* k, const void* v, bool single, cudaStream_t s) {
+                          const void* k, const void* v, bool single, int sms, cudaStream_t s) {
   cudaError_t e;
   if (single && a.n_seq <= FEW) {
     // One CTA writes the K/V rows only for a one-session call (a few hundred KiB at
@@ -1161,7 +1161,7 @@ cudaError_t launch_append(const Dev& d, bool kv4, const AppendArgs& a, const uin
     e = launch_ex(&append_plan_kernel<MAX_SEQ>, dim3(1), dim3(META_THREADS), 0, s, true, d, a, types);
   }
   if (e != cudaSuccess || k == nullptr) return e;  // plan only: layers follow one by one
-  return kv4 ? launch_append_layers_kv4(d, a.total, 0, d.layers, k, v, true, s)
+  return kv4 ? launch_append_layers_kv4(d, a.total, 0, d.layers, k, v, true, false, sms, s)
              : launch_append_layers(d, a.total, 0, d.layers, k, v, true, s);
 }
 

@@ -18,14 +18,19 @@ class LaunchOrder {
  public:
   // An append: of all layers' K/V, or of none (layers follow one by one).
   void append(bool with_kv, int layers) {
+    planned_ = false;
     written_ = !with_kv ? 0 : layers >= 64 ? ~0ull : (1ull << layers) - 1;
     settle();
   }
   // A separate write of one layer's K/V, complete before the launch behind it starts.
   void layer_write(int layer) {
     written_ |= 1ull << layer;
+    planned_ = true;
     settle();
   }
+  // Whether the append's plan is complete before any launch behind can start: a launch since has
+  // waited for it before it let others start.
+  bool planned() const { return planned_; }
   bool layer_written(int layer) const { return (written_ >> layer) & 1; }
 
   bool early(int layer, bool fused) const {
@@ -38,7 +43,7 @@ class LaunchOrder {
       pending_ |= 1ull << layer;
       written_ |= 1ull << layer;
     }
-    waited_ = true;
+    waited_ = planned_ = true;
   }
 
  private:
@@ -48,6 +53,7 @@ class LaunchOrder {
   }
   uint64_t written_ = 0;  // layers whose K/V of the append are in the pool, or will be
   uint64_t pending_ = 0;  // layers with a fused write that no launch has waited for
+  bool planned_ = false;  // a launch or a layer write has waited for the append's plan
   bool waited_ = false;   // an attention launch has waited for the append (or layer write)
 };
 
