@@ -19,8 +19,8 @@ LIB = os.path.join(HERE, "libkvc.so")
 SOURCES = ["kvc_api.cu", "kvc_meta.cu", "kvc_attn_decode.cu", "kvc_attn_decode_split.cu",
            "kvc_decode_dispatch.cu",
            "kvc_attn_prefill.cu", "kvc_attn_prefill_tc.cu", "kvc_attn_prefill_f32.cu",
-           "kvc_noalloc.cu", "kvc_kv4_rows.cu", "kvc_kv4_attn.cu", "kvc_kv4_decode.cu",
-           "kvc_kv4_prefill_tc.cu"]
+           "kvc_noalloc.cu", "kvc_kv4_rows.cu", "kvc_kv4_attn.cu", "kvc_kv4_prefill_f32.cu",
+           "kvc_kv4_decode.cu", "kvc_kv4_prefill_tc.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -585,14 +585,20 @@ __global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
     seg.si = d.seq[seg.seq];
     const int nb = seg.si.n_blocks;
     slices = min(cut.slices, nb);
-    if (slice >= slices) return;
+    if (slice >= slices) {
+      pdl_wait();
+      return;
+    }
     seg.pair_start = seg.si.unit_base + seg.head * nb;
     seg.pair_end = seg.pair_start + nb;
     seg.u = u_begin = seg.pair_start + (int)((int64_t)slice * nb / slices);
     seg.end = u_end = seg.pair_start + (int)((int64_t)(slice + 1) * nb / slices);
   } else {
     us = unit_split(d, gridDim.x, cut.min_units, MAX_PARTS);
-    if (cta >= us.n_cta) return;
+    if (cta >= us.n_cta) {
+      pdl_wait();
+      return;
+    }
     u_begin = us.start_of(cta);
     u_end = us.start_of(cta + 1);
     if (u_begin >= u_end) return;
