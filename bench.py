@@ -10,6 +10,7 @@ follow, then K timed steps.  Per-step K/V traffic is hundreds of GB, far
 above the 129 MB L2, so no flush is needed between steps.
 
     python bench.py [--gpus N] [--steps K] [--warmup W] [--impl ours|reference]
+                    [--kv-bits 4]     (the same workload over a cache held in 4 bits)
 
 Prints one JSON line (rank 0).  N > 1 (torchrun): every rank runs an
 independent replica of the workload (sessions are independent; no
@@ -156,7 +157,8 @@ def step_bytes(w, drv, st, prev_resident: dict) -> tuple[float, float, int]:
     """(attention+append bytes of the step, bytes of its first full-batch decode round per
     layer launch, number of decode sessions in that round)."""
     esz = 2 if w.dtype == "bf16" else 4
-    per_pos_layer = w.kv_heads * w.head_dim * 2 * esz           # K+V of one position, one layer
+    # K+V of one position, one layer (in 4 bits: D / 2 bytes of codes, D / 16 of scales a row).
+    per_pos_layer = w.kv_heads * w.head_dim * 2 * (9 / 16 if drv.kv_bits == 4 else esz)
     q_row = w.q_heads * w.head_dim * esz
     total = 0.0
     n_now = {s: prev_resident.get(s, 0) for s, _ in st.pairs}
@@ -195,9 +197,11 @@ def job_throughput(units: float, elapsed_ms: float, world: int) -> tuple[float, 
     return units / (elapsed_ms / 1e3), elapsed_ms
 
 
-def workload_config(w, start: int, steps: int, world: int, per_layer: bool) -> dict:
+def workload_config(w, start: int, steps: int, world: int, per_layer: bool,
+                    kv_bits: int | None = None) -> dict:
     """The `config` object of the JSON line (both arms)."""
     return {
+        **({} if kv_bits is None else {"kv_bits": kv_bits}),
         "workload": w.name,
         "sessions": w.n_sessions, "layers": w.layers, "q_heads": w.q_heads,
         "kv_heads": w.kv_heads, "head_dim": w.head_dim, "page_size": w.page_size,
@@ -222,7 +226,7 @@ def run_ours(args, rank: int, world: int, local_rank: int):
                     name=f"{w.name}-reduced-{args.sessions or w.n_sessions}s-"
                          f"{args.layers or w.layers}L")
     scripts = S.workload_scripts(w)
-    drv = Driver(w, scripts)
+    drv = Driver(w, scripts, kv_bits=args.kv_bits)
     start = args.start if args.start is not None else S.steady_state_step(w, scripts)
     n_steps_total = len(drv.sched)
     assert start - args.warmup >= 0 and start + args.steps <= n_steps_total
@@ -335,7 +339,7 @@ def run_ours(args, rank: int, world: int, local_rank: int):
     #    one released) brought to the same state and warmed up the same way; then every
     #    step's inputs are copied from pinned host memory and its results (every call's
     #    output, resident counts) read back inside the timed region.
-    drv = Driver(w, scripts)
+    drv = Driver(w, scripts, kv_bits=args.kv_bits)
     drv.fast_forward(start - args.warmup)
     for _ in range(args.warmup):
         drv.run_step(drv.prepare_step())
@@ -359,19 +363,21 @@ def run_ours(args, rank: int, world: int, local_rank: int):
         "vs_baseline": None,
         "dtype": w.dtype,
         "data": "synthetic (seeded SplitMix64 Irwin-Hall values, PCG64 session scripts)",
-        "config": dict(workload_config(w, start, args.steps, world, args.per_layer_append),
+        "config": dict(workload_config(w, start, args.steps, world, args.per_layer_append,
+                                       args.kv_bits),
                        audio_seconds_timed_per_gpu=audio_s),
         "path_hbm_gbs": (tot_bytes / 1e9) / (elapsed_ms / 1e3),
         "path_frac_of_peak": (tot_bytes / 1e9) / (elapsed_ms / 1e3) / peak,
         "roofline": {
-            "kernel": decode_kernel_label(w),
+            "kernel": decode_kernel_label(w) if args.kv_bits is None else "decode_kv4_kernel",
             "bound": "hbm",
             "achieved": dec_gbs,
             "peak": peak,
             "peak_kind": f"{peak_kind} copy bandwidth",
             "unit": "GB/s",
             "frac": (dec_gbs / peak) if dec_gbs else None,
-            "traffic": decode_traffic((sum(dec_bytes) / len(dec_bytes)) if dec_bytes else None),
+            "traffic": (decode_traffic((sum(dec_bytes) / len(dec_bytes)) if dec_bytes else None)
+                        if args.kv_bits is None else None),
             "traffic_note": "ncu DRAM bytes per algorithmic byte of the stream-K kernel on "
                             "the 64-session two-layer case, times this launch's bytes",
             "algorithmic_bytes_per_launch": (sum(dec_bytes) / len(dec_bytes)) if dec_bytes else None,
@@ -780,6 +786,8 @@ def main():
     ap.add_argument("--per-layer-append", action="store_true",
                     help="the model's order: appends without K/V, each layer's K/V written "
                          "just before its attention")
+    ap.add_argument("--kv-bits", type=int, choices=[4], default=None,
+                    help="hold K and V in 4 bits (default: in the element type)")
     ap.add_argument("--budget-sweep", type=int, default=0, metavar="SESSIONS",
                     help="print the Table-3-shaped budget sweep over SESSIONS sessions and exit")
     ap.add_argument("--stress", default=None, metavar="B,W[,N]",

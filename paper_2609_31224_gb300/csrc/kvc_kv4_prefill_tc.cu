@@ -738,7 +738,9 @@ cudaError_t kv4_prefill_tc_limits(Limits* lim) {
 cudaError_t launch_prefill_kv4_tc(const Dev& d, const Limits& lim, int layer, const void* q,
                                   void* out, int n_pairs, int64_t units, bool early,
                                   cudaStream_t s) {
-  // Slices of a pair: a CTA takes 5.5 us beside its stages of 0.6 us, a merge 1.5 us.
+  // Slices of a pair, by what they were measured to take: a CTA 9 us beside its stages of 1.15 us, a merge
+  // 1 us.  (31 stages: one session 45 us in one slice, 28 in 2, 19 in 4, 15.7 in 8; 9 sessions 46, 30, 42
+  // and 81 us; 64 sessions 183 in one, 207 in 2.)
   const int pages = (int)std::max<int64_t>(1, (units + n_pairs - 1) / n_pairs);
   const int stages = (pages + PAGES - 1) / PAGES;
   int k = 1;
@@ -746,7 +748,7 @@ cudaError_t launch_prefill_kv4_tc(const Dev& d, const Limits& lim, int layer, co
   for (int x = 1; x <= std::min(PF_MAX_SLICES, stages); ++x) {
     if (lim.kv4_clusters[x] < 1) continue;
     const int waves = (n_pairs + lim.kv4_clusters[x] - 1) / lim.kv4_clusters[x];
-    const float t = waves * (5.5f + 0.6f * ((stages + x - 1) / x)) + (x > 1 ? 1.5f : 0.f);
+    const float t = waves * (9.f + 1.15f * ((stages + x - 1) / x)) + (x > 1 ? 1.f : 0.f);
     if (t < least) {
       least = t;
       k = x;

@@ -79,11 +79,13 @@ class Step:
 
 class Driver:
     def __init__(self, w: Workload, scripts: list[SessionScript], cache=None, device="cuda",
-                 sizing: dict | None = None):
+                 sizing: dict | None = None, kv_bits: int | None = None):
+        """kv_bits: as KVCache takes it (4 holds K and V in 4 bits)."""
         import torch
         from paper_2609_31224_gb300 import KVCache
         self.torch = torch
         self.w = w
+        self.kv_bits = kv_bits
         self.scripts = {s.session: s for s in scripts}
         self.sched = schedule(scripts)
         self.device = device
@@ -93,7 +95,8 @@ class Driver:
                                       head_dim=w.head_dim, budget=w.budget, window=w.window,
                                       dtype=w.dtype, rope_base=w.rope_base,
                                       page_size=w.page_size, policy=w.policy, sink=w.sink,
-                                      recent=w.recent, device=device, **self.sizing)
+                                      recent=w.recent, device=device, kv_bits=kv_bits,
+                                      **self.sizing)
         self.pos = np.zeros(w.n_sessions, dtype=np.int64)  # host copy of positions fed
         self.tdtype = torch.bfloat16 if w.dtype == "bf16" else torch.float32
         self.step_index = 0
@@ -199,7 +202,8 @@ class Driver:
                 fused = (cache.attn_decode_kv_raw if c.kind == "decode"
                          else cache.attn_prefill_kv_raw)
                 fused(layer, kl, vl, q_ptrs[layer], o_ptr, stream)
-                launches += 1 if (c.kind == "decode" or self.w.dtype == "bf16") else 2
+                one = c.kind == "decode" or (self.w.dtype == "bf16" and self.kv_bits is None)
+                launches += 1 if one else 2
                 if on_attention is not None:
                     on_attention(c, layer)
                 continue

@@ -79,3 +79,17 @@ def test_roofline_kernel_label_follows_the_dispatch(sessions, label, monkeypatch
                         lambda i: types.SimpleNamespace(multi_processor_count=152))
     w = types.SimpleNamespace(n_sessions=sessions, kv_heads=8)
     assert bench.decode_kernel_label(w) == label
+
+
+def test_step_bytes_of_a_cache_held_in_4_bits():
+    """Rows count with their codes and scales; queries and outputs in the element type as before."""
+    import numpy as np
+    call = types.SimpleNamespace(kind="decode", sessions=np.array([0, 1]), cu=np.array([0, 1, 2]))
+    step = types.SimpleNamespace(pairs=[(0, 3), (1, 3)], calls=[call])
+    w = types.SimpleNamespace(dtype="bf16", kv_heads=8, q_heads=32, head_dim=128, layers=4)
+    q = 32 * 128 * 2
+    for bits, row in ((None, 8 * 128 * 2 * 2), (4, 8 * 2 * (64 + 8))):
+        drv = types.SimpleNamespace(kv_bits=bits)
+        total, one, n = bench.step_bytes(w, drv, step, {0: 100, 1: 50})
+        assert one == 152 * row + 2 * 2 * q and n == 2
+        assert total == 4 * (one + 2 * row)

@@ -19,7 +19,11 @@ if not torch.cuda.is_available():
     pytest.skip("needs a CUDA GPU", allow_module_level=True)
 
 import kv4_reference as R  # noqa: E402
+from harness import Lockstep  # noqa: E402
 from paper_2609_31224_gb300 import KVCache, KvcError  # noqa: E402
+from synth import gpu as synth_gpu  # noqa: E402
+from synth import script as S  # noqa: E402
+from synth.driver import Driver  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -528,3 +532,50 @@ def test_numbers_next_to_half_a_step(exp):
     assert (np.abs(rows).reshape(-1, 32).max(-1) == half[:, 0]).all()
     p.append([0], [16], kv=(p.normal(16, 1, 2, 64), rows))
     p.check_rows([0])
+
+
+class Held(Lockstep):
+    """A workload run on a cache held in 4 bits beside the oracle: states as always, outputs against
+    attention over the numbers that the retained rows are held as."""
+
+    def held(self, s, layer, pos):
+        k, v = (x.astype(np.float32) for x in self.kv_source(s, layer, pos))
+        return R.held(R.rotate32(k, pos)), R.held(v)
+
+    def compare_call(self, c, layer, sessions=None, what=""):
+        out = c.out.float().cpu().numpy()
+        for i, s in enumerate(c.sessions.tolist()):
+            pos, mine = np.array(self.orc.state(s)["pos"]), np.array(c.positions[i])
+            k, v = self.held(s, layer, pos)
+            ref = R.attention(self.q_raw(s, layer, mine).astype(np.float32), mine, k, v,
+                              np.arange(len(pos) - len(mine) + 1, len(pos) + 1))
+            assert_attention(out[c.cu[i]:c.cu[i + 1]], ref, self.w.dtype, f"{what} {c.kind}")
+            self.n_compared += 1
+
+
+@pytest.mark.parametrize("policy", ["unit", "position", "sink_recent"])
+@pytest.mark.parametrize("per_layer", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_workload_over_rows_in_4_bits(dtype, per_layer, policy):
+    """Appends, prefill, decode, evictions and the read-back of what is left, as a user runs them."""
+    base = S.SINGLE_BF16 if dtype == "bf16" else S.TINY_F32
+    w = base.with_(layers=2, q_heads=8, kv_heads=2, n_sessions=3, units=24, budget=200, window=2,
+                   offset_max=4, policy=policy, sink=5 if policy == "sink_recent" else 0,
+                   recent=120 if policy == "sink_recent" else 0, seed=11)
+    synth_gpu.build()
+    drv = Driver(w, S.workload_scripts(w), kv_bits=4)
+    ls = Held(drv, w)
+    for _ in range(len(drv.sched)):
+        ls.run_step(attn_pred=lambda step, kind, call, layer: (step + layer) % 3 == 0,
+                    per_layer=per_layer)
+    assert ls.n_compared > 40
+    for s in range(3):
+        st = ls.orc.state(s)
+        assert st["n_evicted"] > 0
+        pos = np.array(st["pos"])
+        k, v = drv.cache.read_kv([s], [0], [0, len(pos)])
+        for layer in range(2):
+            for got, want in zip((k, v), ls.held(s, layer, pos)):
+                np.testing.assert_array_equal(got[layer].float().cpu().numpy(),
+                                              R.in_type(want, dtype))
+    assert drv.cache.device_status()[1] == 0
