@@ -164,7 +164,10 @@ struct OpenPages {
     live_first = si.n_hist_pages + (si.live_head + PS - 1) / PS;
     live_last = si.n_hist_pages + (si.live_head + si.n_live) / PS - 1;
   }
-  __device__ bool has(int b) const { return b < hist_full || (b >= live_first && b <= live_last); }
+  // Blocks b to e (those of a warp among them).
+  __device__ bool has(int b, int e) const {
+    return e < hist_full || (b >= live_first && e <= live_last);
+  }
 };
 
 // A warp's running state: head t, this lane's keys (l) and its 16 (8) dims of piece g (o).
@@ -197,13 +200,16 @@ __device__ inline void page_scores(uint32_t kt, const Query<C>& qr, int lane, fl
       mma_f16(x[w], ha & 0x000F000Fu, hb & 0x000F000Fu, ha & 0x00F000F0u, hb & 0x00F000F0u,
               qr.b[w][2], qr.b[w][3]);
     }
-    s0 = s1 = 0.f;
+    float2 z0 = make_float2(0.f, 0.f), z1 = z0;
 #pragma unroll
-    for (int w = 0; w < KW; ++w) {
+    for (int w = 0; w < KW; w += 2) {
       const float2 a = __half22float2(bits_h2(ma[w / 2])), b = __half22float2(bits_h2(mb[w / 2]));
-      s0 = fmaf(x[w][0] + qr.zero[w] + x[w][1], w % 2 ? a.y : a.x, s0);
-      s1 = fmaf(x[w][2] + qr.zero[w] + x[w][3], w % 2 ? b.y : b.x, s1);
+      const float2 zero = make_float2(qr.zero[w], qr.zero[w + 1]);
+      z0 = __ffma2_rn(__fadd2_rn(make_float2(x[w][0] + x[w][1], x[w + 1][0] + x[w + 1][1]), zero), a, z0);
+      z1 = __ffma2_rn(__fadd2_rn(make_float2(x[w][2] + x[w][3], x[w + 1][2] + x[w + 1][3]), zero), b, z1);
     }
+    s0 = z0.x + z0.y;
+    s1 = z1.x + z1.y;
   } else {
     // Exact values of the keys, and a sum for every 16 dims: the tensor cores cut off what they
     // add to an accumulator.
@@ -305,13 +311,12 @@ __device__ inline void pages_step(uint32_t at, const Query<C>& qr, const OpenPag
                                   const SeqInfo& si, int blk, State<C>& st, int lane) {
   const int g = lane >> 2;
   float s[N][2];
-  bool open[N];
+  const bool open = pages.has(blk, blk + (N - 1) * C::WARPS);
   BlockRange br[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     page_scores<C>(at + i * C::PAGE, qr, lane, s[i][0], s[i][1]);
-    open[i] = pages.has(blk + i * C::WARPS);
-    if (!open[i]) {
+    if (!open) {
       br[i] = block_range(si, blk + i * C::WARPS);
       if (g < br[i].lo || g >= br[i].hi) s[i][0] = -INFINITY;
       if (g + 8 < br[i].lo || g + 8 >= br[i].hi) s[i][1] = -INFINITY;
@@ -348,7 +353,7 @@ __device__ inline void pages_step(uint32_t at, const Query<C>& qr, const OpenPag
   uint32_t b[N][2];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    if (!open[i]) {
+    if (!open) {
       // (Where no key was valid so far s - m is no number.)
 #pragma unroll
       for (int j = 0; j < 2; ++j)
@@ -358,7 +363,7 @@ __device__ inline void pages_step(uint32_t at, const Query<C>& qr, const OpenPag
   }
 #pragma unroll
   for (int i = 0; i < N; ++i)
-    page_values<C>(at + i * C::PAGE + 9 * C::D, b[i][0], b[i][1], open[i], br[i], st, lane);
+    page_values<C>(at + i * C::PAGE + 9 * C::D, b[i][0], b[i][1], open, br[i], st, lane);
 }
 
 // The new token's K (rotated at its position) and V of this layer and head, from the caller's rows,
