@@ -270,7 +270,7 @@ __device__ inline void in_order(const float* o, float f, float (&y)[8]) {
 
 __global__ void __launch_bounds__(THREADS, 1) prefill_kv4_kernel(
     Dev d, int layer, const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out,
-    int k_slices, int early) {
+    int pair0, int k_slices, int early) {
   extern __shared__ uint8_t smem_raw[];
   // (The same offset in every CTA, so that cluster_map() of an address finds the peer's.)
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -316,7 +316,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_kv4_kernel(
   const uint32_t sbase = smem_u32(smem);
 
   Slice sl;
-  const int pair = blockIdx.x / k_slices, slice = blockIdx.x % k_slices;
+  const int pair = pair0 + blockIdx.x / k_slices, slice = blockIdx.x % k_slices;
   sl.seq = pair / d.kv_heads;
   sl.head = pair % d.kv_heads;
   sl.si = d.seq[sl.seq];
@@ -738,43 +738,64 @@ cudaError_t kv4_prefill_tc_limits(Limits* lim) {
 cudaError_t launch_prefill_kv4_tc(const Dev& d, const Limits& lim, int layer, const void* q,
                                   void* out, int n_pairs, int64_t units, bool early,
                                   cudaStream_t s) {
-  // Slices of a pair, by what they were measured to take: a CTA 9 us beside its stages of 1.15 us, a merge
+  // How the pairs are cut, by what was measured: a CTA takes 9 us beside its stages of 1.15 us, a merge
   // 1 us.  (31 stages: one session 45 us in one slice, 28 in 2, 19 in 4, 15.7 in 8; 9 sessions 46, 30, 42
-  // and 81 us; 64 sessions 183 in one, 207 in 2.)
+  // and 81 us; 64 sessions 183 in one, 207 in 2.)  Whole waves of uncut pairs may go first, the rest
+  // in slices of its own behind them, where one more wave would find most SMs without a pair.
   const int pages = (int)std::max<int64_t>(1, (units + n_pairs - 1) / n_pairs);
-  const int stages = (pages + PAGES - 1) / PAGES;
-  int k = 1;
-  float least = 1e30f;
-  for (int x = 1; x <= std::min(PF_MAX_SLICES, stages); ++x) {
-    if (lim.kv4_clusters[x] < 1) continue;
-    const int waves = (n_pairs + lim.kv4_clusters[x] - 1) / lim.kv4_clusters[x];
-    const float t = waves * (9.f + 1.15f * ((stages + x - 1) / x)) + (x > 1 ? 1.f : 0.f);
-    if (t < least) {
-      least = t;
-      k = x;
+  const int stages = (pages + PAGES - 1) / PAGES, per_wave = lim.kv4_clusters[1];
+  auto cut = [&](int n, float* least) {
+    int k = 1;
+    *least = n > 0 ? 1e30f : 0.f;
+    for (int x = 1; n > 0 && x <= std::min(PF_MAX_SLICES, stages); ++x) {
+      if (lim.kv4_clusters[x] < 1) continue;
+      const int waves = (n + lim.kv4_clusters[x] - 1) / lim.kv4_clusters[x];
+      const float t = waves * (9.f + 1.15f * ((stages + x - 1) / x)) + (x > 1 ? 1.f : 0.f);
+      if (t < *least) {
+        *least = t;
+        k = x;
+      }
+    }
+    return k;
+  };
+  float t_all, t_rest;
+  int first = 0, k = cut(n_pairs, &t_all);
+  if (per_wave > 0 && n_pairs > per_wave) {
+    const int waves = n_pairs / per_wave, k_rest = cut(n_pairs - waves * per_wave, &t_rest);
+    if (k_rest > 1 && waves * (9.f + 1.15f * stages) + t_rest < t_all) {
+      first = waves * per_wave;
+      k = k_rest;
     }
   }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(n_pairs * k);
-  cfg.blockDim = dim3(THREADS);
-  cfg.dynamicSmemBytes = SMEM;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  int n = 0;
-  if (k > 1) {
-    attr[n].id = cudaLaunchAttributeClusterDimension;
-    attr[n].val.clusterDim.x = k;
-    attr[n].val.clusterDim.y = 1;
-    attr[n].val.clusterDim.z = 1;
-    ++n;
+  for (int part = first > 0 ? 0 : 1; part < 2; ++part) {
+    const int kp = part == 0 ? 1 : k, n = part == 0 ? first : n_pairs - first;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(n * kp);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = SMEM;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    int a = 0;
+    if (kp > 1) {
+      attr[a].id = cudaLaunchAttributeClusterDimension;
+      attr[a].val.clusterDim.x = kp;
+      attr[a].val.clusterDim.y = 1;
+      attr[a].val.clusterDim.z = 1;
+      ++a;
+    }
+    attr[a].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[a].val.programmaticStreamSerializationAllowed = 1;
+    ++a;
+    cfg.attrs = attr;
+    cfg.numAttrs = a;
+    // (The second launch starts when the first has waited for the append, if it had to.)
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, &prefill_kv4_kernel, d, layer,
+                                             static_cast<const __nv_bfloat16*>(q),
+                                             static_cast<__nv_bfloat16*>(out), part == 0 ? 0 : first, kp,
+                                             (int)(early || (part == 1 && first > 0)));
+    if (e != cudaSuccess) return e;
   }
-  attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[n].val.programmaticStreamSerializationAllowed = 1;
-  ++n;
-  cfg.attrs = attr;
-  cfg.numAttrs = n;
-  return cudaLaunchKernelEx(&cfg, &prefill_kv4_kernel, d, layer, static_cast<const __nv_bfloat16*>(q),
-                            static_cast<__nv_bfloat16*>(out), k, (int)early);
+  return cudaSuccess;
 }
 
 }  // namespace kvc
