@@ -16,8 +16,8 @@
 //   0-7    softmax: warps w and w + 4 own TMEM lanes 32 w .. 32 w + 31, a query row per lane; warp
 //          w takes the first 64 keys of a stage, warp w + 4 the others.  They rotate the rows into
 //          TMEM, then turn rows of S into rows of P (written over them), keep maximum and sum, and
-//          write the output.  The two threads of a row share its reference m: a flag between their
-//          warps tells each stage whether it still holds;
+//          write the output.  The two threads of a row share its reference m: a vote of their warps
+//          tells each stage whether it still holds;
 //   8-15   operands: warp 8 + i unpacks page i of a stage, K and V, into 128-byte-swizzled tiles.
 //          Dims and nibbles keep their stored order (the query's dims take K's, the output's are put
 //          back in order), so that a word of eight codes becomes one 16-byte store; the order of the
@@ -74,8 +74,7 @@ constexpr int OFF_K = 0, OFF_V = OFF_K + 2 * TILE, OFF_RAW = OFF_V + 2 * TILE;
 constexpr int Q_PITCH = 2 * D + 16;
 constexpr int OFF_Q = OFF_RAW + RAW * PAGES * PAGE;
 constexpr int OFF_ROW = OFF_Q + M * Q_PITCH;    // [M] softmax scales, then [2][M] exchanged values
-constexpr int OFF_FLAG = OFF_ROW + 3 * M * 4;   // [3][2][4] flags of the softmax warps
-constexpr int OFF_BAR = OFF_FLAG + 24 * 4;
+constexpr int OFF_BAR = OFF_ROW + 3 * M * 4;
 constexpr int OFF_TMEM = OFF_BAR + N_BARS * 8;
 constexpr int OFF_NAN = OFF_TMEM + 8;           // [D / GROUP] first retained index of a NaN group
 constexpr int SMEM = 1024 + OFF_NAN + D / GROUP * 4;
@@ -338,11 +337,27 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_kv4_kernel(
   bool dead = false;
   const int quarter = warp & 3, half = warp >> 2 & 1;
   float* s_row = reinterpret_cast<float*>(smem + OFF_ROW);
-  volatile int* s_flag = reinterpret_cast<volatile int*>(smem + OFF_FLAG);
   // The two warps of a quarter (named barriers 1-4), all softmax warps (5).
   auto sync_quarter = [&] {
     __syncwarp();
     asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");
+  };
+
+  // ... and whether a thread of either has x.
+  auto quarter_any = [&](bool x) {
+    uint32_t any;
+    __syncwarp();
+    asm volatile(
+        "{\n"
+        ".reg .pred p, q;\n"
+        "setp.ne.u32 p, %1, 0;\n"
+        "bar.red.or.pred q, %2, 64, p;\n"
+        "selp.u32 %0, 1, 0, q;\n"
+        "}"
+        : "=r"(any)
+        : "r"((uint32_t)x), "r"(1 + quarter)
+        : "memory");
+    return any != 0;
   };
 
   if (warp < SM_WARPS) {
@@ -435,14 +450,12 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_kv4_kernel(
       bool need = false;
       if (i > 0 && !dead) {
         weigh();
-        need = __any_sync(FULL, live && sum > 32768.f);
+        need = live && sum > 32768.f;
       }
-      if (lane == 0) s_flag[8 * b + 4 * half + quarter] = dead ? 2 : need;
-      sync_quarter();
-      const int flags = s_flag[8 * b + quarter] | s_flag[8 * b + 4 + quarter];
-      dead = flags & 2;
+      const bool any = quarter_any(dead || need);
+      if (any) dead = quarter_any(dead);
       if (dead) break;
-      const bool fresh = i == 0 || flags;
+      const bool fresh = i == 0 || any;
       if (fresh) {
         float mx = -INFINITY;
 #pragma unroll
@@ -481,9 +494,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_kv4_kernel(
         m = mn;
         if (!dead) weigh();
         // (Both have read the other's maximum before either writes one again.)
-        if (lane == 0) s_flag[16 + 4 * half + quarter] = dead;
-        sync_quarter();
-        dead = s_flag[16 + quarter] | s_flag[16 + 4 + quarter];
+        dead = quarter_any(dead);
         if (dead) break;
       }
       l += sum;
