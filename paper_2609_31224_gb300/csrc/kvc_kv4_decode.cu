@@ -420,45 +420,46 @@ __device__ void write_new_row(const Dev& d, int layer, const SeqInfo& si, int he
   __syncwarp();
 }
 
-// The pages of one warp and segment (every WARPS-th block), through the warp's ring.
+// The pages of one warp and segment (every WARPS-th block), through the warp's ring.  What is looked at
+// once in 16 steps stays in the warp's copy of the segment in shared memory: the registers of the main
+// loop are all taken (with 20 of these in registers instead, spills were 25 instructions a page).
 template <class C>
 struct Ring {
   uint8_t* slots;
   uint64_t* full;
   const uint8_t* tiles;      // of the layer and head in page 0
-  size_t page_stride;
-  const int32_t* hrow;
-  const int32_t* lrow;
-  int n_hist_pages, first, n_my, win, pid;
+  const UnitSeg* seg;
+  int first, n_my, win, pid;
 
-  __device__ void open(const Dev& d, int layer, const UnitSeg& seg, int warp) {
-    tiles = d.pool + tile_at(C::D, d.layers, d.kv_heads, 0, layer, seg.head, 0);
-    hrow = d.hist_pt + (size_t)seg.si.sid * d.max_pages_per_session;
-    lrow = d.live_pt + (size_t)seg.si.sid * d.max_pages_per_session;
-    n_hist_pages = seg.si.n_hist_pages;
-    first = seg.blk_begin() + warp;
-    const int n = seg.end - seg.u;
+  __device__ void open(const Dev& d, int layer, const UnitSeg* s, int warp) {
+    seg = s;
+    tiles = d.pool + tile_at(C::D, d.layers, d.kv_heads, 0, layer, s->head, 0);
+    first = s->blk_begin() + warp;
+    const int n = s->end - s->u;
     n_my = n > warp ? (n - warp + C::WARPS - 1) / C::WARPS : 0;
     win = -32;
     pid = 0;
   }
   __device__ int steps() const { return (n_my + 1) / 2; }
   // Copy the warp's k-th pair of pages in, as its n-th of the launch; the whole warp.
-  __device__ void issue(int k, uint32_t n, uint64_t policy, int lane) {
+  __device__ void issue(const Dev& d, int k, uint32_t n, int lane) {
     if (2 * k >= win + 32) {
       win = (2 * k) & ~31;
-      const int j = win + lane, b = first + j * C::WARPS;
-      pid = j < n_my ? (b < n_hist_pages ? hrow[b] : lrow[b - n_hist_pages]) : 0;
+      const int j = win + lane, b = first + j * C::WARPS, nh = seg->si.n_hist_pages;
+      const size_t row = (size_t)seg->si.sid * d.max_pages_per_session;
+      pid = j < n_my ? (b < nh ? d.hist_pt[row + b] : d.live_pt[row + b - nh]) : 0;
     }
     const int p0 = __shfl_sync(FULL, pid, 2 * k - win), p1 = __shfl_sync(FULL, pid, 2 * k + 1 - win);
     if (lane == 0) {
       const uint32_t st = n % C::STAGES;
+      const size_t stride = page_bytes(C::D, d.layers, d.kv_heads);
+      const uint64_t policy = evict_first_policy();
       uint8_t* to = slots + st * 2 * C::PAGE;
       const bool two = 2 * k + 1 < n_my;
       fence_proxy_async_smem();
       mbar_arrive_expect_tx(&full[st], two ? 2 * C::PAGE : C::PAGE);
-      bulk_g2s_hint(to, tiles + p0 * page_stride, C::PAGE, &full[st], policy);
-      if (two) bulk_g2s_hint(to + C::PAGE, tiles + p1 * page_stride, C::PAGE, &full[st], policy);
+      bulk_g2s_hint(to, tiles + p0 * stride, C::PAGE, &full[st], policy);
+      if (two) bulk_g2s_hint(to + C::PAGE, tiles + p1 * stride, C::PAGE, &full[st], policy);
     }
   }
 };
@@ -557,6 +558,7 @@ __global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
   constexpr int D = C::D, E = G * D;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int s_last, s_abort;
+  __shared__ UnitSeg s_seg[2][C::WARPS];
   __shared__ float s_scale[G];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   float* state_o = reinterpret_cast<float*>(smem + C::STATE_O);
@@ -566,7 +568,6 @@ __global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
   Ring<C> ring;
   ring.slots = smem + warp * C::STAGES * 2 * C::PAGE;
   ring.full = reinterpret_cast<uint64_t*>(smem + C::BARS) + warp * C::STAGES;
-  ring.page_stride = page_bytes(D, d.layers, d.kv_heads);
   if (lane == 0) {
     for (int i = 0; i < C::STAGES; ++i) mbar_init(&ring.full[i], 1);
     fence_mbar_init();
@@ -581,8 +582,8 @@ __global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
 
   const int H = d.kv_heads, cta = blockIdx.x;
   UnitSplit us = {};
-  UnitSeg seg;
-  int u_begin, u_end, slices = 0;
+  UnitSeg seg;  // (the one to come; the warp's copy of the current one is in shared memory)
+  int u_begin, u_end, slices = 0, turn = 0;
   if (cut.slices > 0) {
     const int pair = cta / cut.slices, slice = cta % cut.slices;
     seg.seq = pair / H;
@@ -609,21 +610,27 @@ __global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
     if (u_begin >= u_end) return;
     seg = unit_segment(d, u_begin, u_end);
   }
-  const uint64_t policy = evict_first_policy();
+  auto keep = [&] {
+    __syncwarp();
+    if (lane == 0) s_seg[turn][warp] = seg;
+    __syncwarp();
+    return &s_seg[turn][warp];
+  };
   const uint32_t slots = smem_u32(ring.slots);
   uint32_t loads = 0;  // steps of this warp, over all segments before
-  ring.open(d, layer, seg, warp);
-  for (int k = 0; k < min(C::STAGES, ring.steps()); ++k) ring.issue(k, k, policy, lane);
+  ring.open(d, layer, keep(), warp);
+  for (int k = 0; k < min(C::STAGES, ring.steps()); ++k) ring.issue(d, k, k, lane);
   if (!waited && warp == 0) prefetch_query<C>(d, seg.si, seg.head, q, lane);
 
   for (;;) {
-    const SeqInfo& si = seg.si;
+    const UnitSeg& cur = *ring.seg;
+    const SeqInfo& si = cur.si;
     if (!waited) {
       pdl_wait();
       waited = true;
     }
     Query<C> qr;
-    if (ring.n_my > 0) load_query<C>(d, si, seg.head, q, lane, qr);  // (the first warp has a page)
+    if (ring.n_my > 0) load_query<C>(d, si, cur.head, q, lane, qr);  // (the first warp has a page)
     State<C> st;
     st.m = -INFINITY;
     st.l = 0.f;
@@ -643,13 +650,13 @@ __global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
       if constexpr (FUSED) {
         const int last = si.n_blocks - 1;
         if (blk == last || (blk + C::WARPS == last && 2 * k + 1 < n_my))
-          write_new_row<C>(d, layer, si, seg.head, new_k, new_v,
+          write_new_row<C>(d, layer, si, cur.head, new_k, new_v,
                            ring.slots + (stage * 2 + (blk != last)) * C::PAGE, lane);
       }
       if (2 * k + 1 < n_my) pages_step<C, 2>(at, qr, open, si, blk, st, lane);
       else pages_step<C, 1>(at, qr, open, si, blk, st, lane);
       __syncwarp();
-      if (k + C::STAGES < n_steps) ring.issue(k + C::STAGES, n + C::STAGES, policy, lane);
+      if (k + C::STAGES < n_steps) ring.issue(d, k + C::STAGES, n + C::STAGES, lane);
     }
     if (failed_at >= 0 && lane == 0) s_abort = 1;
 
@@ -683,13 +690,13 @@ __global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
       return;
     }
     loads += n_steps;
-    const UnitSeg cur = seg;
     const bool more = cur.end < u_end;
     // The next segment's first pages are on their way while this one is merged.
     if (more) {
       seg = unit_segment(d, cur.end, u_end);
-      ring.open(d, layer, seg, warp);
-      for (int k = 0; k < min(C::STAGES, ring.steps()); ++k) ring.issue(k, loads + k, policy, lane);
+      turn ^= 1;
+      ring.open(d, layer, keep(), warp);
+      for (int k = 0; k < min(C::STAGES, ring.steps()); ++k) ring.issue(d, k, loads + k, lane);
     }
     if (warp < G) {
       float m = -INFINITY, l = 0.f;
