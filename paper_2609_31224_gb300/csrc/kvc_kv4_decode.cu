@@ -86,73 +86,77 @@ struct Query {
 constexpr int Q_EXP = 9;        // a row's largest element is in [2^9, 2^10)
 constexpr int RAW_EXP = -24;    // a nibble's bits 0..3 as a binary16 number are n 2^-24
 
+// The query of a pair as it is staged for all warps of a CTA.
 template <class C>
-__device__ inline void load_query(const Dev& d, const SeqInfo& si, int head, const typename C::T* q,
-                                  int lane, Query<C>& qr) {
-  using T = typename C::T;
+struct StagedQuery {
+  uint32_t b[C::KW][32][4];
+  float zero[G][C::KW];
+  float c[G];
+};
+
+// Head h of the pair, by one warp: lane (w, t, p) takes dims a = 32 w + 8 t + p and a + 4 and the
+// rotate-half partners of both, which are pair p of words w and w + D / 64.  (Every warp for itself took
+// 450 instructions before its first page.)
+template <class C>
+__device__ inline void stage_query(const Dev& d, const SeqInfo& si, int head, int h,
+                                   const typename C::T* q, int lane, StagedQuery<C>& sq) {
   constexpr int D = C::D, KW = C::KW, HALF = D / 2;
-  const int n = lane >> 2, t = lane & 3;
-  const T* row = q + ((size_t)si.q_row0 * d.q_heads + head * G + n / 2) * D + 8 * t;
-  Eight<T> in[KW];
+  const int w = lane / 16 % (KW / 2), t = lane / 4 % 4, p = lane % 4, a = GROUP * w + 8 * t + p;
+  const typename C::T* row = q + ((size_t)si.q_row0 * d.q_heads + head * G + h) * D + a;
+  const float x[4] = {to_float<typename C::T>(row[0]), to_float<typename C::T>(row[4]),
+                      to_float<typename C::T>(row[HALF]), to_float<typename C::T>(row[HALF + 4])};
+  const float2* cs = d.rope + (size_t)si.pos_first * HALF + a;
+  float y[2][2];  // [word w, its partner][dim a, dim a + 4]
+  turn_pair(x[0], x[2], cs[0], y[0][0], y[1][0]);
+  turn_pair(x[1], x[3], cs[4], y[0][1], y[1][1]);
+  uint32_t most = max(max(abs_bits(y[0][0]), abs_bits(y[0][1])), max(abs_bits(y[1][0]), abs_bits(y[1][1])));
 #pragma unroll
-  for (int w = 0; w < KW; ++w) in[w].load(row + GROUP * w);
-  const float4* t4 = reinterpret_cast<const float4*>(d.rope + (size_t)si.pos_first * HALF + 8 * t);
-  float y[KW][8];
-  uint32_t most = 0;
-#pragma unroll
-  for (int w = 0; w < KW / 2; ++w) {
-    float x1[8], x2[8];
-    in[w].get(x1);
-    in[w + KW / 2].get(x2);                           // the rotate-half partners
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-      const float4 cs = t4[(GROUP * w + e) / 2];
-      turn_pair(x1[e], x2[e], make_float2(cs.x, cs.y), y[w][e], y[w + KW / 2][e]);
-      turn_pair(x1[e + 1], x2[e + 1], make_float2(cs.z, cs.w), y[w][e + 1], y[w + KW / 2][e + 1]);
-    }
-  }
-#pragma unroll
-  for (int w = 0; w < KW; ++w)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) most = max(most, abs_bits(y[w][e]));
-  most = max(most, __shfl_xor_sync(FULL, most, 1));
-  most = max(most, __shfl_xor_sync(FULL, most, 2));
+  for (int o = 1; o < 32; o <<= 1) most = max(most, __shfl_xor_sync(FULL, most, o));
   // The row over 2^e.  Infinities and NaN pass through.
   int e = (int)(most >> 23) - 127 - Q_EXP;
   e = most >= 0x7F800000u ? 0 : max(e, -126);
   const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-  float sum[KW];
+  float sum[2];
 #pragma unroll
-  for (int w = 0; w < KW; ++w) {
-    sum[w] = 0.f;
-#pragma unroll
-    for (int p = 0; p < 4; ++p) {
-      const float lo = y[w][p] * inv, hi = y[w][p + 4] * inv;
-      __half2 v = __floats2half2_rn(lo, hi);
-      if (n & 1) v = __floats2half2_rn(lo - __low2float(v), hi - __high2float(v));
-      if constexpr (C::SCALE_BEHIND)
-        if (p & 1) v = __hmul2(v, __float2half2_rn(0.0625f));
-      const float back = C::SCALE_BEHIND && (p & 1) ? 16.f : 1.f;
-      sum[w] += (__low2float(v) + __high2float(v)) * back;
-      qr.b[w][p] = h2_bits(v);
-    }
+  for (int i = 0; i < 2; ++i) {
+    const float y0 = y[i][0] * inv, y1 = y[i][1] * inv;
+    const __half2 hi = __floats2half2_rn(y0, y1);
+    const __half2 lo = __floats2half2_rn(y0 - __low2float(hi), y1 - __high2float(hi));
+    // (Where the scales come in behind the product; exact but for the last bits of small numbers.)
+    const bool over16 = C::SCALE_BEHIND && (p & 1);
+    const __half2 f = __float2half2_rn(over16 ? 0.0625f : 1.f), vh = __hmul2(hi, f), vl = __hmul2(lo, f);
+    sum[i] = ((__low2float(vh) + __high2float(vh)) + (__low2float(vl) + __high2float(vl))) *
+             (over16 ? 16.f : 1.f);
+    sq.b[w + i * (KW / 2)][8 * h + t][p] = h2_bits(vh);
+    sq.b[w + i * (KW / 2)][8 * h + 4 + t][p] = h2_bits(vl);
   }
-  // 16: scales are stored over 16; and the softmax takes exponents of 2.
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) sum[i] += __shfl_xor_sync(FULL, sum[i], o);
+  if (lane % 16 == 0)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) sq.zero[h][w + i * (KW / 2)] = sum[i] * (-8.f / (float)(1 << -RAW_EXP));
+  // 16: scales are stored over 16; and the softmax takes exponents of 2.  (Beyond binary32 it is large
+  // enough to single out a maximum.)
   const float scale = 16.f * LOG2E * (D == 128 ? 0.08838834764831845f : 0.125f);
   const float c = scale * __uint_as_float((uint32_t)(127 + e) << 23) *
                   (C::SCALE_BEHIND ? (float)(1 << -RAW_EXP) : 1.f);
-  // Of head t, from lane (2t, 0).  (Beyond binary32 it is large enough to single out a maximum.)
-  qr.c = __shfl_sync(FULL, fminf(c, 3.4e38f), 8 * t);
-  if constexpr (C::SCALE_BEHIND) {
+  if (lane == 0) sq.c[h] = fminf(c, 3.4e38f);
+}
+
+template <class C>
+__device__ inline void load_query(const StagedQuery<C>& sq, int lane, Query<C>& qr) {
 #pragma unroll
-    for (int w = 0; w < KW; ++w) {
-      float z = sum[w];
-      z += __shfl_xor_sync(FULL, z, 1);
-      z += __shfl_xor_sync(FULL, z, 2);
-      z += __shfl_xor_sync(FULL, z, 4);               // both pieces
-      qr.zero[w] = __shfl_sync(FULL, z, 8 * t) * (-8.f / (float)(1 << -RAW_EXP));
-    }
+  for (int w = 0; w < C::KW; ++w) {
+    const uint4 v = *reinterpret_cast<const uint4*>(sq.b[w][lane]);
+    qr.b[w][0] = v.x;
+    qr.b[w][1] = v.y;
+    qr.b[w][2] = v.z;
+    qr.b[w][3] = v.w;
+    qr.zero[w] = sq.zero[lane & 3][w];
   }
+  qr.c = sq.c[lane & 3];
 }
 
 // Which pages of a session need no look at their slots: full pages of the compacted region and live
@@ -559,7 +563,8 @@ __global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int s_last, s_abort;
   __shared__ UnitSeg s_seg[2][C::WARPS];
-  __shared__ float s_scale[G];
+  __shared__ __align__(16) StagedQuery<C> s_query;
+  const float* s_scale = s_query.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   float* state_o = reinterpret_cast<float*>(smem + C::STATE_O);
   float2* state_ml = reinterpret_cast<float2*>(smem + C::STATE_ML);
@@ -629,8 +634,10 @@ __global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
       pdl_wait();
       waited = true;
     }
+    if (warp < G) stage_query<C>(d, si, cur.head, warp, q, lane, s_query);
+    __syncthreads();
     Query<C> qr;
-    if (ring.n_my > 0) load_query<C>(d, si, cur.head, q, lane, qr);  // (the first warp has a page)
+    load_query<C>(s_query, lane, qr);
     State<C> st;
     st.m = -INFINITY;
     st.l = 0.f;
@@ -668,7 +675,6 @@ __global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
       for (int off = 4; off < 32; off <<= 1) l += __shfl_xor_sync(FULL, l, off);
       if (g == 0) {
         state_ml[warp * G + t] = make_float2(st.m, l);
-        if (warp == 0) s_scale[t] = qr.c;
       }
       float* to = state_o + (warp * G + t) * D + g * (D / 8);
 #pragma unroll
