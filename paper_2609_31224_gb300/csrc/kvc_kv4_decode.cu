@@ -12,15 +12,17 @@
 // their sum is a score with about 22 bits of q, one softmax state per lane, no lane idle.  binary32
 // calls split P the same way; for bfloat16 the rounding of P to 11 bits stays.
 //
-// What bounds it: 18 D bytes a page (44.6 us for 64 sessions of 4,100 positions) against about 330
-// warp instructions, most of them the way from nibble to operand.  K's nibbles go in as they are (an
-// AND each: bits 0..3 and 4..7 of a half are binary16 numbers n 2^-24 and n 2^-20) with scale and
-// zero behind the product, which a group of 32 dims does not cross; V's take an AND-OR and one or two
-// products each.  The rest is kept small: the query's operands stay in registers, the softmax
-// reference lags (it moves only when a score passes it by 2^6), two pages make a step, page lists are
-// looked up 32 at a time, and only pages with masked slots look at their range.  64 sessions: 58.0 us
-// (77 % of the bytes' rate; 105 us as first written, 517 instructions), against 159 us for bfloat16
-// rows.  Issue is at about 60 % there; 16 warps an SM is what 128 registers leave.
+// What bounds it: 18 D bytes a page (44 us for 64 sessions of 4,096 positions) against about 280
+// warp instructions, 80 for the scores, 125 for P V (most of both the way from nibble to operand) and
+// the rest ring, masks and softmax.  K's nibbles go in as they are (an AND each: bits 0..3 and 4..7 of
+// a half are binary16 numbers n 2^-24 and n 2^-20) with scale and zero behind the product, which a
+// group of 32 dims does not cross; V's take an AND-OR and one or two products each.  The rest is kept
+// small: the query's operands stay in registers, the softmax reference lags (it moves only when a
+// score passes it by 2^6), two pages make a step, page lists are looked up 32 at a time, and only
+// pages with masked slots look at their range.  64 sessions: 60.9 us (72 % of the bytes' rate; 105 us
+// as first written, 517 instructions), against 159 us for bfloat16 rows; issue is at 55 %, and 16 warps
+// an SM is what 128 registers leave.  One session: 6.9 us against 0.7 us for its bytes, a chain of the
+// launch's release, the query's staging, two pages a warp and two merges.
 #include <algorithm>
 
 #include "kvc_kv4.cuh"
@@ -802,10 +804,10 @@ cudaError_t launch(const Dev& d, int layer, const void* q, void* out, const void
 // the longer the more warps share an SM, and 2 for the merge of a pair's slices.  Measured (us,
 // 8 KV heads; Mk, Nk: k slices of 8 and 4 warps, S: stream-K; the first is the one chosen):
 //   pages      1 session                4                     14                     38, 64
-//       7   M1 3.8  N4 5.1  S 9.4   M1 3.8  N2 5.2        M1 4.4  N4 6.2        N1 4.6, 6.0  S 18.6
-//      25   M1 4.9  N8 5.3          M1 5.1  N3 5.9        M1 5.8  N4 7.6        M1 8.1, N1 10.2
-//      94   M15 6.1 N12 6.4 S 12.6  M4 7.4  N4 7.6        M1 10.6 N5 10.5       M1 15.0, N1 25.5 S 29.7
-//     257   M15 6.9 N14 7.3 S 16.1  M9 10.0 M4 10.2       N5 18.3 M2 20.6       M1 32.7, S 58.0 N1 61.6
+//    to 7   M1 3.6  N4 5.0  S 8.7   M1 3.5  N2 4.7        M1 3.9  N4 5.9        M1 4.8 N1 4.2, N1 5.3 S 12.9
+//      25   M1 4.4  N8 5.0          M1 4.4  N3 5.2        M1 5.2  N4 6.7        M1 7.1, N1 9.2
+//      94   M15 5.6 N14 5.8 S 10.3  M4 6.7  N14 6.9       M1 9.7  N5 9.6        M1 13.7, N1 23.8 S 27.6
+//     257   M15 6.2 N14 6.6 S 12.4  M8 8.7  M4 9.3        N5 17.2 M2 19.1       M1 30.8, S 54.7 N1 58.5
 // One slice each and no merge wins up to about 40 pages; then as many slices as give a warp a page or
 // two; stream-K where pairs outnumber the SMs' room and their last CTAs would leave most SMs empty.
 struct Choice {
