@@ -25,11 +25,11 @@ cudaError_t launch_attn_kv4(const Dev& d, const Limits& lim, LaunchOrder* order,
     if (e != cudaSuccess) return e;
     order->layer_write(layer);
   }
-  const bool early = order->early(layer, false);
+  const Early early = order->early_pages(layer);
   const cudaError_t e =
       d.esz == 2 ? launch_prefill_kv4_tc(d, lim, layer, q, out, n_seq * d.kv_heads, units, early, s)
                  : launch_prefill_kv4_f32(d, lim, layer, q, out, n_seq * d.kv_heads, max_t, units, early, s);
-  if (e == cudaSuccess) order->launched(layer, false);
+  if (e == cudaSuccess) order->launched_pages(layer, early);
   return e;
 }
 

@@ -375,6 +375,7 @@ struct Ring {
   SeqInfo si;
   int head, blk_begin, n_my, wp;
   int win, pid;
+  int first_new;  // block whose copy, and of those behind it, waits for the kernels in front
 
   // Copy the group's k-th page in; the whole warp.
   __device__ bool issue(const Dev& d, int layer, int k, int wc_count, int group, int lane) {
@@ -383,6 +384,7 @@ struct Ring {
       const int j = win + lane;
       pid = j < n_my ? block_page(si, hrow, lrow, blk_begin + group + j * wp) : 0;
     }
+    if (blk_begin + group + k * wp >= first_new) pdl_wait();
     const int page = __shfl_sync(FULL, pid, k - win);
     const int st = k % STAGES;
     bool ok = true;
@@ -467,7 +469,7 @@ __device__ void merge_parts(const float* part_o, const float2* part_ml, int cols
 
 __global__ void __launch_bounds__(384, 1) prefill_kv4_f32_kernel(
     Dev d, int layer, const float* __restrict__ q, float* __restrict__ out, float qk_scale, int wc_count,
-    int wp_count, int k_slices, float* part_o, float2* part_ml, int* count, int early) {
+    int wp_count, int k_slices, float* part_o, float2* part_ml, int* count, Early early) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int s_last, s_abort;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_threads = blockDim.x;
@@ -488,7 +490,7 @@ __global__ void __launch_bounds__(384, 1) prefill_kv4_f32_kernel(
   __syncthreads();
   // Before the wait below an early launch reads only what the append wrote (sessions, page tables,
   // pages); q, outputs, partial states and counters come after it.
-  if (!early) pdl_wait();
+  if (early == EARLY_NONE) pdl_wait();
   pdl_launch_dependents();
 
   const int H = d.kv_heads, pair = blockIdx.x / k_slices, slice = blockIdx.x % k_slices;
@@ -513,6 +515,7 @@ __global__ void __launch_bounds__(384, 1) prefill_kv4_f32_kernel(
   ring.n_my = nblk > group ? (nblk - group + wp_count - 1) / wp_count : 0;
   ring.win = -32;
   ring.pid = 0;
+  ring.first_new = early == EARLY_OLD ? si.n_hist_pages + (si.live_head + si.n_live - si.t) / PS : si.n_blocks;
   int issued = 0;  // pages copied or in flight (loader warp)
   bool ok = true;
   if (wc == 0)
@@ -610,7 +613,7 @@ cudaError_t kv4_prefill_f32_limits(Limits* lim) {
 }
 
 cudaError_t launch_prefill_kv4_f32(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
-                                   int n_pairs, int max_t, int64_t units, bool early, cudaStream_t s) {
+                                   int n_pairs, int max_t, int64_t units, Early early, cudaStream_t s) {
   const int wc = warps_of(max_t), wp = groups_of(wc), cols = wc * NT * 8, grid = lim.kv4_prefill[wc];
   // Slots of partial states, one to a CTA.
   const int64_t floats = (int64_t)d.pf_slots * PF_MAX_TOKENS * G * 128;
@@ -632,7 +635,7 @@ cudaError_t launch_prefill_kv4_f32(const Dev& d, const Limits& lim, int layer, c
   const float scale = 16.f * LOG2E / sqrtf((float)D);
   return launch_ex(&prefill_kv4_f32_kernel, dim3(n_pairs * k), dim3(32 * wc * wp), Layout(wc, wp).total,
                    s, true, d, layer, static_cast<const float*>(q), static_cast<float*>(out), scale, wc,
-                   wp, k, d.pf_part_o, d.pf_part_ml, d.pf_count, (int)early);
+                   wp, k, d.pf_part_o, d.pf_part_ml, d.pf_count, early);
 }
 
 }  // namespace kvc

@@ -107,6 +107,7 @@ struct Slice {
   int seq, head, blk0, nblk;
   __device__ int stages() const { return (nblk + PAGES - 1) / PAGES; }
   __device__ int last0() const { return si.n_hist + si.n_live - si.t; }  // of the first token
+  __device__ int first_new() const { return si.n_hist_pages + (si.live_head + si.n_live - si.t) / PS; }
   // Whether every row sees every slot of pages [b, b + n) of the pair: full pages of the history, or
   // full pages of the live part up to the first token's key.
   __device__ bool open(int b, int n) const {
@@ -276,7 +277,7 @@ __device__ inline void in_order(const float* o, float f, float (&y)[8]) {
 
 __global__ void __launch_bounds__(THREADS, 1) prefill_kv4_kernel(
     Dev d, int layer, const __nv_bfloat16* __restrict__ q, __nv_bfloat16* __restrict__ out,
-    int pair0, int k_slices, int early) {
+    int pair0, int k_slices, Early early) {
   extern __shared__ uint8_t smem_raw[];
   // (The same offset in every CTA, so that cluster_map() of an address finds the peer's.)
   uint8_t* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -287,7 +288,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_kv4_kernel(
   volatile int& s_abort = s_abort_flag;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   // The first call after an append waits for it (and lets nothing else start before that).
-  if (!early) pdl_wait();
+  if (early == EARLY_NONE) pdl_wait();
   if (d.g->n_units == 0) {  // the append failed: nothing to do for any CTA
     pdl_wait();
     return;
@@ -579,6 +580,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_kv4_kernel(
         ahead = ids_at(PAGES * i + 32 + lane);
       }
       const int page = __shfl_sync(FULL, ids, PAGES * (i % PER) + lane % PAGES);
+      if (early == EARLY_OLD && sl.blk0 + PAGES * i + npg > sl.first_new()) pdl_wait();
       if (i >= RAW && !wait(B_RAW_EMPTY + slot, i / RAW - 1)) break;
       if (lane == 0) mbar_arrive_expect_tx(&bars[B_RAW_FULL + slot], npg * PAGE);
       __syncwarp();
@@ -754,7 +756,7 @@ cudaError_t kv4_prefill_tc_limits(Limits* lim) {
 }
 
 cudaError_t launch_prefill_kv4_tc(const Dev& d, const Limits& lim, int layer, const void* q,
-                                  void* out, int n_pairs, int64_t units, bool early,
+                                  void* out, int n_pairs, int64_t units, Early early,
                                   cudaStream_t s) {
   // How the pairs are cut, by what was measured: a CTA takes 9 us beside its stages of 1.15 us, a merge
   // 1 us.  (31 stages: one session 45 us in one slice, 28 in 2, 19 in 4, 15.7 in 8; 9 sessions 46, 30, 42
@@ -810,7 +812,7 @@ cudaError_t launch_prefill_kv4_tc(const Dev& d, const Limits& lim, int layer, co
     const cudaError_t e = cudaLaunchKernelEx(&cfg, &prefill_kv4_kernel, d, layer,
                                              static_cast<const __nv_bfloat16*>(q),
                                              static_cast<__nv_bfloat16*>(out), part == 0 ? 0 : first, kp,
-                                             (int)(early || (part == 1 && first > 0)));
+                                             part == 1 && first > 0 && early == EARLY_NONE ? EARLY_ALL : early);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;

@@ -102,10 +102,10 @@ cudaError_t kv4_decode_limits(const Dev& d, Limits* lim);  // both set their ker
 cudaError_t kv4_prefill_limits(const Dev& d, Limits* lim);
 // Chunks of bfloat16 calls (kvc_kv4_prefill_tc.cu).
 cudaError_t launch_prefill_kv4_tc(const Dev& d, const Limits& lim, int layer, const void* q,
-                                  void* out, int n_pairs, int64_t units, bool early,
+                                  void* out, int n_pairs, int64_t units, Early early,
                                   cudaStream_t s);
 cudaError_t launch_prefill_kv4_f32(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
-                                   int n_pairs, int max_t, int64_t units, bool early, cudaStream_t s);
+                                   int n_pairs, int max_t, int64_t units, Early early, cudaStream_t s);
 cudaError_t kv4_prefill_tc_limits(Limits* lim);
 cudaError_t kv4_prefill_f32_limits(Limits* lim);
 // Attention launches may start while the kernel before them in the stream finishes.  early:

@@ -14,6 +14,10 @@
 
 namespace kvc {
 
+// What a launch may read before the kernels in front of it are complete: nothing, the pages without a row
+// of the last append, or all pages.
+enum Early { EARLY_NONE, EARLY_OLD, EARLY_ALL };
+
 class LaunchOrder {
  public:
   // An append: of all layers' K/V, or of none (layers follow one by one).
@@ -44,6 +48,17 @@ class LaunchOrder {
       written_ |= 1ull << layer;
     }
     waited_ = planned_ = true;
+  }
+
+
+  // Plain launches that know EARLY_OLD: behind a complete plan, but not yet behind the write of the append's
+  // rows, they read early all pages but those.  Such a launch lets others start before it has waited
+  // itself, so that it changes nothing here: none of them may take the rows for complete.
+  Early early_pages(int layer) const {
+    return early(layer, false) ? EARLY_ALL : planned_ ? EARLY_OLD : EARLY_NONE;
+  }
+  void launched_pages(int layer, Early e) {
+    if (e != EARLY_OLD) launched(layer, false);
   }
 
  private:

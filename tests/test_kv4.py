@@ -152,3 +152,84 @@ def test_kv_bits_values():
         L.KVCache(n_sessions=1, layers=1, q_heads=4, kv_heads=1, head_dim=64, budget=-1, window=1,
                   dtype="f32", n_pages=4, max_pages_per_session=4, max_positions=64,
                   max_seq_per_call=1, max_tokens_per_call=16, kv_bits=8)
+
+
+ORDER = r"""
+#include "kvc_order.h"
+#include <cstdio>
+
+// Launches in stream order.  `complete`: what is surely complete when the next launch can start;
+// `flight`: what launches before it write.  Bits 0 and 1: rows of two layers, bit 2: the plan.  A launch
+// that waits before it lets others start moves all of `flight` over; one that does not, nothing.
+struct Model {
+  kvc::LaunchOrder order;
+  unsigned complete = 0, flight = 0;
+  void wait() {
+    complete |= flight;
+    flight = 0;
+  }
+  bool op(int o) {
+    if (o < 2) {  // an append with and without rows: lets others start before it has waited
+      order.append(o == 0, 2);
+      complete = 0;
+      flight = o == 0 ? 7 : 4;
+      return true;
+    }
+    const int l = o & 1;
+    if (o < 4) {  // a layer's rows: reads the plan's slots early, waits, lets others start
+      const bool ok = !order.planned() || (complete & 4);
+      wait();
+      flight = 1u << l;
+      complete &= ~flight;
+      order.layer_write(l);
+      return ok;
+    }
+    if (!order.layer_written(l)) return true;  // (refused by the library)
+    const kvc::Early e = order.early_pages(l);
+    if (e == kvc::EARLY_NONE) wait();
+    order.launched_pages(l, e);
+    if (e == kvc::EARLY_NONE) return true;
+    if (!(complete & 4)) return false;
+    return e == kvc::EARLY_OLD || (complete & (1u << l));
+  }
+};
+
+int main() {
+  for (int len = 1; len <= 7; ++len) {
+    long n = 1;
+    for (int i = 0; i < len; ++i) n *= 6;
+    for (long s = 0; s < 2 * n; ++s) {
+      Model m;
+      m.op(s & 1);
+      long x = s / 2;
+      for (int i = 0; i < len; ++i, x /= 6)
+        if (!m.op((int)(x % 6))) {
+          std::printf("sequence %ld of length %d fails at call %d\n", s, len, i);
+          return 1;
+        }
+    }
+  }
+  // A model's order, layer by layer: every write behind the first finds the plan complete, every attention
+  // reads the old pages early.
+  kvc::LaunchOrder o;
+  o.append(false, 8);
+  for (int l = 0; l < 8; ++l) {
+    if (o.planned() != (l > 0)) return 2;
+    o.layer_write(l);
+    const kvc::Early e = o.early_pages(l);
+    if (e != kvc::EARLY_OLD) return 3;
+    o.launched_pages(l, e);
+  }
+  return 0;
+}
+"""
+
+
+def test_no_early_read_of_a_chunk_in_flight(tmp_path):
+    """csrc/kvc_order.h over every short sequence of appends, layer writes and chunked attention."""
+    src, exe = tmp_path / "order.cpp", tmp_path / "order"
+    src.write_text(ORDER)
+    inc = os.path.join(ROOT, "paper_2609_31224_gb300", "csrc")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", inc, str(src), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0, (r.returncode, r.stdout)
