@@ -23,8 +23,8 @@
 // (session, KV head) pair's pages are cut into slices, one CTA each, whose states merge in global
 // memory, by the last CTA of a pair to arrive.  What bounds a small call is the chain of phases of a
 // CTA (queries, pages, merges), not its 0.25 instructions a cycle: one slice a CTA keeps that short
-// where an even cut of all units would leave most CTAs two pairs.  Three sessions of 1,100 positions (4
-// heads, 23 tokens): 13 us a layer, 20 with that cut; the bytes are 0.3 us.
+// where an even cut of all units would leave most CTAs two pairs.  Three sessions of 1,100 positions (8
+// heads, up to 23 tokens): 13 us a layer, 20 with that cut; the bytes are 0.3 us.
 #include <algorithm>
 
 #include "kvc_kv4.cuh"

@@ -26,8 +26,8 @@
 //   17, 18 issue S = Q K^T (Q from TMEM) and O += P V (P from TMEM, V read along its keys).
 // Every wait is bounded; a timeout records KVC_DERR_WAIT and the CTA stops.
 //
-// What bounds it: 64 sessions of 4,096 positions and 17 tokens read 47 us of bytes, the products (68 of
-// their 128 rows are tokens) are 45 us at the measured rate, and about 6,000 warp instructions a stage,
+// What bounds it: 64 sessions of 4,096 positions and 17 tokens read 47 us of bytes, the products are
+// 73 us at the measured rate (68 of their 128 rows are tokens), and about 6,000 warp instructions a stage,
 // 2,000 of them the unpacking, 1,300 the weights, hold 53 % of the issue slots: 1.15 us a stage.  Measured
 // 169 us a layer (233 as first written; 168 over bfloat16 rows, whose operands need no unpacking), one
 // session 15.7 us, 9 sessions 30 us.  Larger stages pay: at 96 keys the hops between the roles cost

@@ -579,3 +579,61 @@ def test_a_workload_over_rows_in_4_bits(dtype, per_layer, policy):
                 np.testing.assert_array_equal(got[layer].float().cpu().numpy(),
                                               R.in_type(want, dtype))
     assert drv.cache.device_status()[1] == 0
+
+
+def test_pages_past_four_gib():
+    """A session whose pages lie past 2^32 bytes of the pool: write, read-back, decode, prefill."""
+    before = 7400                                   # pages, of 589,824 bytes each
+    p = Pair("bf16", 8, 2, layers=32, n_pages=before + 60, most=120000, tokens=before * 16)
+    n = before * 16
+    p.cache.append_chunk([0], [0, n], torch.full((n,), TEXT, dtype=torch.uint8, device="cuda"),
+                         None, None)
+    p.append([1], [45])
+    p.append([1], [1])
+    p.check_attention([1], [1], "decode", layers=[0, 31])
+    p.append([1], [17])
+    p.check_attention([1], [17], "prefill", layers=[0, 31])
+    p.check_rows([1])
+    kv = p.append([1], [19], per_layer=True, hold=False)
+    q = p.queries([19])
+    for layer in range(32):
+        out = p.attend([1], [19], q, layer, "prefill", kv)
+        if layer % 31 == 0:
+            assert_attention(out.float().cpu().numpy(), p.reference([1], [19], q, layer), "bf16")
+    p.check_rows([1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("turn", ["layers first", "one by one", "mixed"])
+def test_orders_of_writes_and_attention(dtype, turn):
+    """Chunks whose rows are written layer by layer, in several orders with the attention over them, call
+    after call: old pages may be read before the write is complete, new ones may not."""
+    p = Pair(dtype, 3, 5, layers=4, n_pages=2000)
+    s = [0, 1, 2, 3, 4]
+    p.append(s, [300, 1, 33, 700, 16])
+    for lens in ([17, 1, 2, 32, 16], [5, 31, 17, 3, 1], [32, 32, 32, 32, 32]):
+        kv = p.append(s, lens, per_layer=True, hold=False)
+        q = p.queries(lens)
+        outs = {}
+        write = lambda l: p.cache.append_kv_layer(l, kv[0][l], kv[1][l])
+        read = lambda l: outs.__setitem__(l, p.attend(s, lens, q, l, "prefill"))
+        if turn == "layers first":
+            for l in range(4):
+                write(l)
+            for l in range(4):
+                read(l)
+        elif turn == "one by one":
+            for l in range(4):
+                outs[l] = p.attend(s, lens, q, l, "prefill", kv)
+        else:
+            write(2)
+            read(2)
+            outs[0] = p.attend(s, lens, q, 0, "prefill", kv)
+            read(2)
+            write(3)
+            read(0)
+            read(3)
+            outs[1] = p.attend(s, lens, q, 1, "prefill", kv)
+        for l, out in outs.items():
+            assert_attention(out.float().cpu().numpy(), p.reference(s, lens, q, l), dtype, f"{turn} {l}")
+    p.check_rows(s)
