@@ -2,10 +2,10 @@
 // survivors of an eviction, and the read-back of rows of either kind of cache in the element type.
 //
 // All move bytes.  A layer of 5,500 bfloat16 positions (8 heads) is 30 MB, 4.4 us at the copy rate, and
-// its write takes 11 us: 18 instructions an element (rotation, largest |x|, two products, a sum and a
-// shifted add a code) in one wave of CTAs whose loads are one block of rows ahead (23 us with a
-// division a code).  Its read-back, 16 layers in a launch, takes 74 us for 460 MB (6.2 TB/s).  A token
-// or two take what a launch takes, 2.6 us behind another one.
+// its write takes 9.5 us behind another one: 12 instructions an element (rotation, largest |x|, two
+// products, a sum and a shifted add a code) in one wave of CTAs whose loads are one block of rows ahead
+// (17 us with a division a code; 11 us a head a thread, 18 instructions).  Its read-back, 16 layers in a
+// launch, takes 74 us for 460 MB (6.2 TB/s).  A token or two take what a launch takes, 2.6 us.
 #include "kvc_kv4.cuh"
 
 namespace kvc {
@@ -16,15 +16,15 @@ using namespace kv4;
 
 constexpr int THREADS = 256;
 constexpr unsigned FULL = 0xFFFFFFFFu;
-constexpr int APPEND_CTAS = 4;  // CTAs of the write per SM
+constexpr int APPEND_CTAS = 2;  // CTAs of the write per SM: what its 105 registers let run at once
 
 // K rotated at its position and V, quantised into the page slots of the plan kernel.  Input
 // [L][total][Hkv][D]; blockIdx.y is the input layer, cache layer layer0 + blockIdx.y.  The first
 // half of the CTAs takes K, the other V (in turn they would leave every second SM the rotations), each
 // several blocks of rows: the next block's rows and slots are on their way while one is worked on.
-// A thread takes 8 dims of the first half of a row and their rotate-half partners.  Its 2 x 8 elements
-// lie in two groups, which it shares with three other threads: two of the four find the scale and the
-// reciprocal of either group and hand them out.
+// A thread takes 8 dims of the first half of a row and their rotate-half partners, of two heads of a
+// token, which share slot and rotation.  Its 4 x 8 elements lie in four groups, which it shares with three
+// other threads: each of the four finds the scale and the reciprocal of one and hands them out.
 // Before the kernel in front is complete, `early` launches read the caller's rows (complete before
 // that kernel could start), `planned` ones the slots (the plan kernel was complete by then).
 template <typename T, int D>
@@ -33,25 +33,29 @@ __global__ void __launch_bounds__(THREADS) append_kv4_kernel(Dev d, int total, i
                                                              bool planned) {
   constexpr int KC = D / 16, HALF = D / 2, NG = D / GROUP;
   static_assert(GROUP == 32 && KC % 4 == 0, "four threads of eight dims share a scale");
-  const int H = d.kv_heads, n_cta = gridDim.x >> 1, kv = (int)blockIdx.x >= n_cta, layer = layer0 + blockIdx.y;
+  const int H = d.kv_heads, HP = (H + 1) / 2;
+  const int n_cta = gridDim.x >> 1, kv = (int)blockIdx.x >= n_cta, layer = layer0 + blockIdx.y;
   const T* from = (kv ? v : k) + (size_t)blockIdx.y * total * H * D;
   // (A call has 2^20 tokens at most: rows count in 32 bits.)  A row's token and head are
   // carried along, not divided out.
-  const int step = n_cta * (THREADS / KC), n = total * H;
-  const int c = threadIdx.x % KC, lane = threadIdx.x & 31, step_g = step / H, step_h = step % H;
+  const int step = n_cta * (THREADS / KC), n = total * HP;
+  const int c = threadIdx.x % KC, lane = threadIdx.x & 31, step_g = step / HP, step_h = step % HP;
   struct Block {
-    Eight<T> a, b;
+    Eight<T> x[2][2];  // [head][half]
     int g, h, gs, pos;
     bool live;
   };
   int n_tok = 0;
   auto ask_rows = [&](Block& x) {
-    x.a = {};
-    x.b = {};
-    if (x.g >= total) return;
-    const T* p = from + ((size_t)x.g * H + x.h) * D + c * 8;
-    x.a.load(p);
-    x.b.load(p + HALF);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      x.x[i][0] = {};
+      x.x[i][1] = {};
+      if (x.g >= total || x.h + i * HP >= H) continue;
+      const T* p = from + ((size_t)x.g * H + x.h + i * HP) * D + c * 8;
+      x.x[i][0].load(p);
+      x.x[i][1].load(p + HALF);
+    }
   };
   auto ask_slots = [&](Block& x) {
     // (Nothing to do where the plan kernel failed: error recorded.  All threads stay for the
@@ -62,8 +66,8 @@ __global__ void __launch_bounds__(THREADS) append_kv4_kernel(Dev d, int total, i
   };
   int first = ((int)blockIdx.x - kv * n_cta) * (THREADS / KC);
   Block cur, next;
-  cur.g = (first + (int)threadIdx.x / KC) / H;
-  cur.h = (first + (int)threadIdx.x / KC) % H;
+  cur.g = (first + (int)threadIdx.x / KC) / HP;
+  cur.h = (first + (int)threadIdx.x / KC) % HP;
   if (early) {
     ask_rows(cur);
     pdl_launch_dependents();
@@ -82,62 +86,75 @@ __global__ void __launch_bounds__(THREADS) append_kv4_kernel(Dev d, int total, i
     ask_rows(cur);
   }
   for (; first < n; first += step, cur = next) {
-    float xa[8], xb[8];
+    float x[2][2][8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      cur.x[i][0].get(x[i][0]);
+      cur.x[i][1].get(x[i][1]);
+    }
     next.g = cur.g + step_g;
     next.h = cur.h + step_h;
-    if (next.h >= H) {
-      next.h -= H;
+    if (next.h >= HP) {
+      next.h -= HP;
       ++next.g;
     }
     if (kv == 0) {
-      float4 t4[4];
+      const float4* t4 = reinterpret_cast<const float4*>(d.rope + (size_t)cur.pos * HALF + c * 8);
+      float4 cs[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        t4[e] = reinterpret_cast<const float4*>(d.rope + (size_t)cur.pos * HALF + c * 8)[e];
+      for (int e = 0; e < 4; ++e) cs[e] = t4[e];
       ask_rows(next);
       ask_slots(next);
-      float x1[8], x2[8];
-      cur.a.get(x1);
-      cur.b.get(x2);
 #pragma unroll
-      for (int e = 0; e < 8; e += 2) {
-        const float4 cs = t4[e / 2];
-        turn_pair(x1[e], x2[e], make_float2(cs.x, cs.y), xa[e], xb[e]);
-        turn_pair(x1[e + 1], x2[e + 1], make_float2(cs.z, cs.w), xa[e + 1], xb[e + 1]);
-      }
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float2 t = e % 2 ? make_float2(cs[e / 2].z, cs[e / 2].w) : make_float2(cs[e / 2].x, cs[e / 2].y);
+          float y0, y1;
+          turn_pair(x[i][0][e], x[i][1][e], t, y0, y1);
+          x[i][0][e] = y0;
+          x[i][1][e] = y1;
+        }
     } else {
       ask_rows(next);
       ask_slots(next);
-      cur.a.get(xa);
-      cur.b.get(xb);
     }
-    // Largest |x| of the first group to threads 0 and 1 of the four, of the second to 2 and 3.
-    const bool second = lane & 2;
+    // Largest |x| of group i (head i / 2, half i % 2) to thread i of the four.
+    const int own = lane & 3;
     uint32_t mx;
     {
-      const uint32_t ma = most_of(xa), mb = most_of(xb);
-      mx = max(second ? mb : ma, __shfl_xor_sync(FULL, second ? ma : mb, 2));
-      mx = max(mx, __shfl_xor_sync(FULL, mx, 1));
+      const uint32_t m[4] = {most_of(x[0][0]), most_of(x[0][1]), most_of(x[1][0]), most_of(x[1][1])};
+      const bool b1 = own & 2, b0 = own & 1;
+      const uint32_t p = max(b1 ? m[2] : m[0], __shfl_xor_sync(FULL, b1 ? m[0] : m[2], 2));
+      const uint32_t r = max(b1 ? m[3] : m[1], __shfl_xor_sync(FULL, b1 ? m[1] : m[3], 2));
+      mx = max(b0 ? r : p, __shfl_xor_sync(FULL, b0 ? p : r, 1));
     }
     const float s = scale_of(mx);
     const Divisor div(s);
     if (__any_sync(FULL, div.passes(mx))) {
-      hold_codes(xa, __shfl_sync(FULL, div.by, lane & ~3));
-      hold_codes(xb, __shfl_sync(FULL, div.by, lane & ~3 | 2));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) hold_codes(x[i / 2][i % 2], __shfl_sync(FULL, div.by, lane & ~3 | i));
     }
-    const uint32_t wa = codes_of(xa, __shfl_sync(FULL, div.inv, lane & ~3), __shfl_sync(FULL, div.rest, lane & ~3));
-    const uint32_t wb = codes_of(xb, __shfl_sync(FULL, div.inv, lane & ~3 | 2),
-                                 __shfl_sync(FULL, div.rest, lane & ~3 | 2));
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = codes_of(x[i / 2][i % 2], __shfl_sync(FULL, div.inv, lane & ~3 | i),
+                      __shfl_sync(FULL, div.rest, lane & ~3 | i));
     if (!cur.live) continue;
     const int page = cur.gs / PS, slot = cur.gs % PS;
     uint8_t* tile = d.pool + tile_at(D, d.layers, H, page, layer, cur.h, kv);
-    *reinterpret_cast<uint32_t*>(tile + (kv ? v_codes(D, slot, 8 * c) : k_codes(D, slot, 8 * c))) = wa;
-    *reinterpret_cast<uint32_t*>(tile + (kv ? v_codes(D, slot, HALF + 8 * c)
-                                            : k_codes(D, slot, HALF + 8 * c))) = wb;
-    if (lane % 2 == 0) {
-      const int group = c / 4 + (second ? NG / 2 : 0);
-      *reinterpret_cast<__half*>(tile + (kv ? v_scale(D, slot, group) : k_scale(D, slot, group))) =
-          stored_scale(s);
+    const int at[2] = {kv ? v_codes(D, slot, 8 * c) : k_codes(D, slot, 8 * c),
+                       kv ? v_codes(D, slot, HALF + 8 * c) : k_codes(D, slot, HALF + 8 * c)};
+    const int to_second = HP * 2 * (int)tile_bytes(D);
+    const bool second = cur.h + HP < H;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < 2 || second)
+        *reinterpret_cast<uint32_t*>(tile + (i / 2) * to_second + at[i % 2]) = w[i];
+    if (own < 2 || second) {
+      const int group = c / 4 + (own & 1) * (NG / 2);
+      *reinterpret_cast<__half*>(tile + (own >> 1) * to_second +
+                                 (kv ? v_scale(D, slot, group) : k_scale(D, slot, group))) = stored_scale(s);
     }
   }
 }
@@ -335,7 +352,7 @@ cudaError_t launch_append_layers_kv4(const Dev& d, int total, int layer0, int n_
                                      const void* k, const void* v, bool early, bool planned, int sms,
                                      cudaStream_t s) {
   const int rows = THREADS / (d.head_dim / 16);  // of a block
-  const int blocks = (total * d.kv_heads + rows - 1) / rows;
+  const int blocks = (total * ((d.kv_heads + 1) / 2) + rows - 1) / rows;
   // Two blocks of rows a CTA or more where there are enough of them.
   const int per_layer = max(1, sms * APPEND_CTAS / 2 / n_layers);
   const dim3 grid(2 * (unsigned)min(blocks, per_layer), n_layers);
