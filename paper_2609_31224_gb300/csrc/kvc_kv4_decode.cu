@@ -598,7 +598,8 @@ __global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
     seg.si = d.seq[seg.seq];
     const int nb = seg.si.n_blocks;
     slices = min(cut.slices, nb);
-    if (slice >= slices) {
+    // (The append failed: what d.seq holds is an older one's.)
+    if (d.g->n_units == 0 || slice >= slices) {
       pdl_wait();
       return;
     }

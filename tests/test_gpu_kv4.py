@@ -637,3 +637,44 @@ def test_orders_of_writes_and_attention(dtype, turn):
         for l, out in outs.items():
             assert_attention(out.float().cpu().numpy(), p.reference(s, lens, q, l), dtype, f"{turn} {l}")
     p.check_rows(s)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_replayed_append_that_fails_changes_nothing(dtype):
+    """A graph of a decode step, replayed past the pool's last page: the error is recorded, and the step
+    that found no page leaves rows, outputs and counts as they were."""
+    p = Pair(dtype, 2, 2, layers=2, n_pages=10)
+    p.append([0, 1], [30, 15])
+    d = p.d
+    k, v = (torch.empty(2, 2, 2, d, dtype=TD[dtype], device="cuda") for _ in range(2))  # [layer][session]
+    q, out = p.device(p.normal(2, 8, d)), torch.zeros(2, 2, 8, d, dtype=TD[dtype], device="cuda")
+    types = torch.full((2,), TEXT, dtype=torch.uint8, device="cuda")
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+
+    def rows(n):
+        got = p.cache.read_kv([0, 1], [0, 0], [0, n, 2 * n])
+        return [x.clone() for x in got]
+
+    with torch.cuda.stream(stream):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            p.cache.append_chunk([0, 1], [0, 1, 2], types, None, None, stream=stream)
+            for layer in range(2):
+                p.cache.attn_decode_kv_raw(layer, k[layer].data_ptr(), v[layer].data_ptr(),
+                                           q.data_ptr(), out[layer].data_ptr(), stream.cuda_stream)
+        for step in range(200):
+            before = rows(200)
+            k.fill_(step + 1)
+            v.fill_(-step - 1)
+            out.fill_(7.0)
+            graph.replay()
+            stream.synchronize()
+            if p.cache.device_status()[1] != 0:
+                break
+            assert (out != 7.0).any()
+    # After 50 steps 80 and 65 positions take five pages each; the next needs an eleventh.
+    assert step == 50, step
+    for a, b in zip(before, rows(200)):
+        assert torch.equal(a, b)
+    assert (out == 7.0).all()
