@@ -55,9 +55,8 @@ struct Cfg {
   static constexpr int RING = WARPS * STAGES * 2 * PAGE;
   static constexpr int STATE_O = RING;                          // [WARPS][G][D] floats
   static constexpr int STATE_ML = STATE_O + WARPS * G * D * 4;  // [WARPS][G] (m, l)
-  static constexpr int WEIGHT = STATE_ML + WARPS * G * 8;       // [max(WARPS, MAX_PARTS)][G]
-  static constexpr int TOTAL = WEIGHT + (WARPS > MAX_PARTS ? WARPS : MAX_PARTS) * G * 4;  // [G] (m, l)
-  static constexpr int BARS = TOTAL + G * 8;
+  static constexpr int WEIGHT = STATE_ML + WARPS * G * 8;       // [MAX_PARTS][G], of parts
+  static constexpr int BARS = WEIGHT + MAX_PARTS * G * 4;
   static constexpr int SMEM = BARS + WARPS * STAGES * 8;
   static_assert(PAGE % 16 == 0 && RING % 16 == 0 && BARS % 8 == 0, "alignment");
 };
@@ -470,6 +469,53 @@ struct Ring {
   }
 };
 
+// N floats as one access (N = 1, 2 or 4).
+template <int N>
+struct Floats {
+  float v[N];
+  __device__ static Floats load(const float* p) {  // of global memory, past L1
+    Floats f;
+    if constexpr (N == 4) {
+      const float4 x = __ldcg(reinterpret_cast<const float4*>(p));
+      f.v[0] = x.x; f.v[1] = x.y; f.v[2] = x.z; f.v[3] = x.w;
+    } else if constexpr (N == 2) {
+      const float2 x = __ldcg(reinterpret_cast<const float2*>(p));
+      f.v[0] = x.x; f.v[1] = x.y;
+    } else {
+      f.v[0] = __ldcg(p);
+    }
+    return f;
+  }
+  __device__ static Floats load_shared(const float* p) {
+    Floats f;
+    if constexpr (N == 4) {
+      const float4 x = *reinterpret_cast<const float4*>(p);
+      f.v[0] = x.x; f.v[1] = x.y; f.v[2] = x.z; f.v[3] = x.w;
+    } else if constexpr (N == 2) {
+      const float2 x = *reinterpret_cast<const float2*>(p);
+      f.v[0] = x.x; f.v[1] = x.y;
+    } else {
+      f.v[0] = *p;
+    }
+    return f;
+  }
+  __device__ void store(float* p) const {
+    if constexpr (N == 4) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    else if constexpr (N == 2) *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+    else *p = v[0];
+  }
+  template <typename T>
+  __device__ void store_row(T* p) const {
+    if constexpr (sizeof(T) == 4) {
+      store(reinterpret_cast<float*>(p));
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; i += 2)
+        *reinterpret_cast<__nv_bfloat162*>(p + i) = __floats2bfloat162_rn(v[i], v[i + 1]);
+    }
+  }
+};
+
 // Rows of a pair from the parts that cover it, by every thread of the last CTA to arrive: part i is
 // in slot part(i), [G][D] outputs and (m, l) per head.
 template <class C, typename PartFn>
@@ -477,7 +523,8 @@ __device__ void merge_parts(const float* part_o, const float2* part_ml, int part
                             const float* scale, float* weight, typename C::T* out, int tid) {
   using T = typename C::T;
   constexpr int D = C::D, E = G * D, EPT = (E + C::THREADS - 1) / C::THREADS;
-  constexpr int BATCH = 32 / EPT > 16 ? 16 : 32 / EPT;  // parts whose loads are in flight together
+  // Parts whose loads are in flight together: more than the 17 that one session's pairs are cut into.
+  constexpr int BATCH = C::WARPS == 8 ? 20 : 32 / EPT;
   const int lane = tid & 31, warp = tid >> 5;
   float x[BATCH][EPT];
   auto load = [&](int i0) {
@@ -571,7 +618,6 @@ __global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
   float* state_o = reinterpret_cast<float*>(smem + C::STATE_O);
   float2* state_ml = reinterpret_cast<float2*>(smem + C::STATE_ML);
   float* weight = reinterpret_cast<float*>(smem + C::WEIGHT);
-  float2* total = reinterpret_cast<float2*>(smem + C::TOTAL);
   Ring<C> ring;
   ring.slots = smem + warp * C::STAGES * 2 * C::PAGE;
   ring.full = reinterpret_cast<uint64_t*>(smem + C::BARS) + warp * C::STAGES;
@@ -707,38 +753,42 @@ __global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
       ring.open(d, layer, keep(), warp);
       for (int k = 0; k < min(C::STAGES, ring.steps()); ++k) ring.issue(d, k, loads + k, lane);
     }
-    if (warp < G) {
-      float m = -INFINITY, l = 0.f;
-      if (lane < C::WARPS) {
-        const float2 ml = state_ml[lane * G + warp];
-        m = ml.x;
-        l = ml.y;
-      }
-      float M = m;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(FULL, M, o));
-      const float w = weight2(m, M, s_scale[warp]);
-      float L = l * w;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(FULL, L, o);
-      if (lane < C::WARPS) weight[lane * G + warp] = w;
-      if (lane == 0) total[warp] = make_float2(M, L);
-    }
-    __syncthreads();
     const bool whole = cur.whole();
     // Slots of a pair's parts: its slices one after the other, or two of each CTA of the split.
     const int slot = slices ? cta : 2 * cta + (cur.u == u_begin ? 0 : 1);
     T* orow = out + ((size_t)cur.si.q_row0 * d.q_heads + cur.head * G) * D;
-    for (int e = tid; e < E; e += C::THREADS) {
-      const int h = e / D;
-      float o = 0.f;
+    // The warps' states: each thread finds the weights of its elements' head by itself, which is sooner
+    // done than handed out.
+    // (The thread's number is hidden from the compiler, which would hold what follows from it in registers
+    // throughout the pages' loop.)
+    int id = tid;
+    asm volatile("" : "+r"(id));
+    constexpr int EPT = E / C::THREADS;
+    const int e0 = id * EPT, h = e0 / D;
+    float2 ml[C::WARPS];
+    float M = -INFINITY, L = 0.f;
 #pragma unroll
-      for (int w = 0; w < C::WARPS; ++w) o += state_o[w * E + e] * weight[w * G + h];
-      if (whole) orow[e] = from_float<T>(o * (16.f / total[h].y));
-      else d.dec_part_o[(size_t)slot * E + e] = o;
+    for (int w = 0; w < C::WARPS; ++w) {
+      ml[w] = state_ml[w * G + h];
+      M = fmaxf(M, ml[w].x);
     }
-    if (!whole) {
-      if (tid < G) d.dec_part_ml[(size_t)slot * G + tid] = total[tid];
+    Floats<EPT> o = {};
+#pragma unroll
+    for (int w = 0; w < C::WARPS; ++w) {
+      const float f = weight2(ml[w].x, M, s_scale[h]);
+      const Floats<EPT> x = Floats<EPT>::load_shared(state_o + w * E + e0);
+      L += ml[w].y * f;
+#pragma unroll
+      for (int k = 0; k < EPT; ++k) o.v[k] += x.v[k] * f;
+    }
+    if (whole) {
+      const float inv = 16.f / L;
+#pragma unroll
+      for (int k = 0; k < EPT; ++k) o.v[k] *= inv;
+      o.store_row(orow + e0);
+    } else {
+      o.store(d.dec_part_o + (size_t)slot * E + e0);
+      if (e0 % D == 0) d.dec_part_ml[(size_t)slot * G + h] = make_float2(M, L);
       // The last CTA of the pair to arrive merges (stream-K: CTAs cf..cl own its units).
       const int cf = slices ? cta - cta % cut.slices : us.owner(cur.pair_start);
       const int parts = slices ? slices : us.owner(cur.pair_end - 1) - cf + 1;
@@ -751,7 +801,7 @@ __global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
         const int next_slot = slices ? cf : 2 * cf, step = slices ? 1 : 2;
         merge_parts<C>(d.dec_part_o, d.dec_part_ml, parts,
                        [&](int i) { return i ? next_slot + step * i : first_slot; }, s_scale,
-                       weight, orow, tid);
+                       weight, orow, id);
         if (tid == 0) *counter = 0;
       }
     }
