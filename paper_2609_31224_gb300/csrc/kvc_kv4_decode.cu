@@ -55,8 +55,10 @@ struct Cfg {
   static constexpr int RING = WARPS * STAGES * 2 * PAGE;
   static constexpr int STATE_O = RING;                          // [WARPS][G][D] floats
   static constexpr int STATE_ML = STATE_O + WARPS * G * D * 4;  // [WARPS][G] (m, l)
-  static constexpr int WEIGHT = STATE_ML + WARPS * G * 8;       // [MAX_PARTS][G], of parts
-  static constexpr int BARS = WEIGHT + MAX_PARTS * G * 4;
+  static constexpr int PARTS_ROOM = 96;                         // parts and a batch past them
+  static constexpr int WEIGHT = STATE_ML + WARPS * G * 8;       // [PARTS_ROOM][G], of parts
+  static constexpr int BARS = WEIGHT + PARTS_ROOM * G * 4;
+  static_assert(PARTS_ROOM >= MAX_PARTS + 20, "room for zeros");
   static constexpr int SMEM = BARS + WARPS * STAGES * 8;
   static_assert(PAGE % 16 == 0 && RING % 16 == 0 && BARS % 8 == 0, "alignment");
 };
@@ -516,35 +518,37 @@ struct Floats {
   }
 };
 
-// Rows of a pair from the parts that cover it, by every thread of the last CTA to arrive: part i is
-// in slot part(i), [G][D] outputs and (m, l) per head.
-template <class C, typename PartFn>
-__device__ void merge_parts(const float* part_o, const float2* part_ml, int parts, PartFn part,
-                            const float* scale, float* weight, typename C::T* out, int tid) {
-  using T = typename C::T;
-  constexpr int D = C::D, E = G * D, EPT = (E + C::THREADS - 1) / C::THREADS;
+// Rows of a pair from the parts that cover it, by every thread of the last CTA to arrive: part 0 is in
+// slot `first`, part i in next + step i; [G][D] outputs and (m, l) per head.  A thread takes EPT elements
+// side by side; parts that are not there have weight 0 (the chain of instructions is what this costs).
+template <class C>
+__device__ void merge_parts(const float* part_o, const float2* part_ml, int parts, int first, int next,
+                            int step, const float* scale, float* weight, typename C::T* out, int tid) {
+  constexpr int D = C::D, E = G * D, EPT = E / C::THREADS;
   // Parts whose loads are in flight together: more than the 17 that one session's pairs are cut into.
   constexpr int BATCH = C::WARPS == 8 ? 20 : 32 / EPT;
-  const int lane = tid & 31, warp = tid >> 5;
-  float x[BATCH][EPT];
+  const int lane = tid & 31, warp = tid >> 5, e0 = tid * EPT, h = e0 / D;
+  const float* p = part_o + (size_t)next * E + e0;
+  const uint32_t stride = step * E;
+  const Floats<EPT> x0 = Floats<EPT>::load(part_o + (size_t)first * E + e0);
+  Floats<EPT> x[BATCH];
   auto load = [&](int i0) {
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i)
-#pragma unroll
-      for (int j = 0; j < EPT; ++j) {
-        const int e = tid + j * C::THREADS;
-        x[i][j] = i0 + i < parts && e < E ? __ldcg(part_o + (size_t)part(i0 + i) * E + e) : 0.f;
-      }
+    for (int i = 0; i < BATCH; ++i) {
+      x[i] = {};
+      if (i0 + i < parts) x[i] = Floats<EPT>::load(p + (i0 + i) * stride);
+    }
   };
-  load(0);
+  load(1);
   if (warp < G) {
-    constexpr int PL = MAX_PARTS / 32;
+    constexpr int PL = C::PARTS_ROOM / 32;
     float2 ml[PL];
     float M = -INFINITY, L = 0.f, w[PL];
 #pragma unroll
     for (int i = 0; i < PL; ++i) {
-      ml[i] = lane + 32 * i < parts ? __ldcg(&part_ml[(size_t)part(lane + 32 * i) * G + warp])
-                                    : make_float2(-INFINITY, 0.f);
+      const int k = lane + 32 * i;
+      ml[i] = k < parts ? __ldcg(&part_ml[(size_t)(k ? next + step * k : first) * G + warp])
+                        : make_float2(-INFINITY, 0.f);
       M = fmaxf(M, ml[i].x);
     }
 #pragma unroll
@@ -558,30 +562,23 @@ __device__ void merge_parts(const float* part_o, const float2* part_ml, int part
     for (int o = 16; o > 0; o >>= 1) L += __shfl_xor_sync(FULL, L, o);
     const float inv = 16.f / L;
 #pragma unroll
-    for (int i = 0; i < PL; ++i)
-      if (lane + 32 * i < parts) weight[(lane + 32 * i) * G + warp] = w[i] * inv;
+    for (int i = 0; i < PL; ++i) weight[(lane + 32 * i) * G + warp] = w[i] * inv;
   }
   __syncthreads();
-  float acc[EPT] = {};
-  for (int i0 = 0;;) {
+  const float* w = weight + h;
+  Floats<EPT> acc;
 #pragma unroll
-    for (int i = 0; i < BATCH; ++i) {
-      if (i0 + i >= parts) break;
+  for (int k = 0; k < EPT; ++k) acc.v[k] = x0.v[k] * w[0];
+  for (int i0 = 1;;) {
 #pragma unroll
-      for (int j = 0; j < EPT; ++j) {
-        const int e = tid + j * C::THREADS;
-        if (e < E) acc[j] += x[i][j] * weight[(i0 + i) * G + e / D];
-      }
-    }
+    for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+      for (int k = 0; k < EPT; ++k) acc.v[k] += x[i].v[k] * w[(i0 + i) * G];
     i0 += BATCH;
     if (i0 >= parts) break;
     load(i0);
   }
-#pragma unroll
-  for (int j = 0; j < EPT; ++j) {
-    const int e = tid + j * C::THREADS;
-    if (e < E) out[e] = from_float<T>(acc[j]);
-  }
+  acc.store_row(out + e0);
 }
 
 // How a call's pages reach the CTAs: slices >= 1 cuts each (session, KV head) pair into as many
@@ -799,9 +796,8 @@ __global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
       if (s_last) {
         const int first_slot = slices ? cf : us.slot_of(cf, cf, cur.pair_start);
         const int next_slot = slices ? cf : 2 * cf, step = slices ? 1 : 2;
-        merge_parts<C>(d.dec_part_o, d.dec_part_ml, parts,
-                       [&](int i) { return i ? next_slot + step * i : first_slot; }, s_scale,
-                       weight, orow, id);
+        merge_parts<C>(d.dec_part_o, d.dec_part_ml, parts, first_slot, next_slot, step, s_scale, weight,
+                       orow, id);
         if (tid == 0) *counter = 0;
       }
     }
