@@ -21,8 +21,9 @@
 // score passes it by 2^6), two pages make a step, page lists are looked up 32 at a time, and only
 // pages with masked slots look at their range.  64 sessions: 60.9 us (72 % of the bytes' rate; 105 us
 // as first written, 517 instructions), against 159 us for bfloat16 rows; issue is at 55 %, and 16 warps
-// an SM is what 128 registers leave.  One session: 6.9 us against 0.7 us for its bytes, a chain of the
-// launch's release, the query's staging, two pages a warp and two merges.
+// an SM is what 128 registers leave.  One session: 5.7 us against 0.7 us for its bytes, a chain (release
+// by the launch before 0.9, query 0.5, two pages a warp 1.3, the CTA's merge 0.9, arrival 0.7, the pair's
+// merge 1.3), in which the number of instructions one after the other is what counts.
 #include <algorithm>
 
 #include "kvc_kv4.cuh"
@@ -851,10 +852,10 @@ cudaError_t launch(const Dev& d, int layer, const void* q, void* out, const void
 // the longer the more warps share an SM, and 2 for the merge of a pair's slices.  Measured (us,
 // 8 KV heads; Mk, Nk: k slices of 8 and 4 warps, S: stream-K; the first is the one chosen):
 //   pages      1 session                4                     14                     38, 64
-//    to 7   M1 3.6  N4 5.0  S 8.7   M1 3.5  N2 4.7        M1 3.9  N4 5.9        M1 4.8 N1 4.2, N1 5.3 S 12.9
-//      25   M1 4.4  N8 5.0          M1 4.4  N3 5.2        M1 5.2  N4 6.7        M1 7.1, N1 9.2
-//      94   M15 5.6 N14 5.8 S 10.3  M4 6.7  N14 6.9       M1 9.7  N5 9.6        M1 13.7, N1 23.8 S 27.6
-//     257   M15 6.2 N14 6.6 S 12.4  M8 8.7  M4 9.3        N5 17.2 M2 19.1       M1 30.8, S 54.7 N1 58.5
+//    to 7   N1 3.0  M1 3.2  S 7.9   M1 3.0  N1 3.1        M1 3.7  N1 3.8        M1 4.5 N1 3.8, N1 4.9 S 12.4
+//      25   M1 3.9  N8 4.5  S 8.8   M1 4.0  N1 4.6        M1 4.8  N1 5.4        M1 6.7 N1 6.8, N1 9.0 S 15.8
+//      94   M11 5.1 M14 4.9 S 9.5   M4 6.4  M8 6.2        M1 9.3  N5 9.3        M1 13.5, N1 23.8 S 27.4
+//     288   M17 5.7 N16 6.2 S 11.0  M8 8.8  N17 9.2       N5 18.3 M2 20.6       M1 33.7, S 60.1 M1 63.0
 // One slice each and no merge wins up to about 40 pages; then as many slices as give a warp a page or
 // two; stream-K where pairs outnumber the SMs' room and their last CTAs would leave most SMs empty.
 struct Choice {
