@@ -266,9 +266,17 @@ class KVCache:
             k = torch.empty(shape, dtype=self.torch_dtype, device=self.pool.device)
         if v is None:
             v = torch.empty(shape, dtype=self.torch_dtype, device=self.pool.device)
+        dev = self.pool.device
         for x in (k, v):
-            if x.shape != shape or x.dtype != self.torch_dtype or not x.is_contiguous():
-                raise ValueError(f"k and v must be contiguous {self.torch_dtype} of shape {shape}")
+            if (x.shape != shape or x.dtype != self.torch_dtype or not x.is_contiguous()
+                    or x.device != dev):
+                raise ValueError(f"k and v must be contiguous {self.torch_dtype} of shape {shape} "
+                                 f"on {dev}")
+        if resident_out is not None and (
+                resident_out.dtype != torch.int64 or not resident_out.is_contiguous()
+                or resident_out.numel() < len(s) or resident_out.device != dev):
+            raise ValueError(f"resident_out must be contiguous torch.int64 on {dev}, an entry per "
+                             f"session")
         _check(self.lib.kvc_read_kv(self.ctx, len(s), _ptr_i32(s), _ptr_i32(f), _ptr_i32(cu),
                                     layer0, n, k.data_ptr(), v.data_ptr(),
                                     None if resident_out is None else resident_out.data_ptr(),
