@@ -7,6 +7,7 @@ library is missing or the device is not a CUDA GPU, the calls raise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -140,6 +141,29 @@ def _stream(stream):
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
+@contextlib.contextmanager
+def _made_for(stream, device):
+    """Tensors made inside are filled by a call on `stream`: they are allocated on that stream, so that
+    neither a kernel in flight on the current one still uses their memory nor the allocator hands it
+    out before the call is through.  Yields what is to be told of each of them, so that readers on
+    the current stream count as well."""
+    import torch
+    handle = _stream(stream)
+    current = torch.cuda.current_stream(device) if device.type == "cuda" else None
+    if current is None or handle == current.cuda_stream:
+        yield lambda tensor: tensor
+        return
+
+    def told(tensor):
+        tensor.record_stream(current)
+        return tensor
+
+    side = (torch.cuda.ExternalStream(handle, device=device) if handle
+            else torch.cuda.default_stream(device))
+    with torch.cuda.stream(side):
+        yield told
+
+
 def query_sizes(cfg: Config) -> tuple[int, int]:
     lib = load_library()
     pool, meta = ctypes.c_size_t(), ctypes.c_size_t()
@@ -253,7 +277,7 @@ class KVCache:
                 k=None, v=None, resident_out=None, stream=None):
         """Retained rows of the listed sessions, from retained position first[i] on, in the
         element type: device tensors K and V [n_layers][cu_rows[-1]][Hkv][D] (made here unless
-        given), filled asynchronously on the stream."""
+        given), filled asynchronously on the stream.  What is made here belongs to that stream."""
         import torch
         s, f, cu = _i32(sessions), _i32(first), _i32(cu_rows)
         if len(f) != len(s) or len(cu) != len(s) + 1:
@@ -262,11 +286,11 @@ class KVCache:
         if n < 1 or not 0 <= layer0 <= self.cfg.layers - n:
             raise ValueError(f"layers {layer0}..{layer0 + n - 1} outside 0..{self.cfg.layers - 1}")
         shape = (n, max(0, int(cu[-1])), self.cfg.kv_heads, self.cfg.head_dim)
-        if k is None:
-            k = torch.empty(shape, dtype=self.torch_dtype, device=self.pool.device)
-        if v is None:
-            v = torch.empty(shape, dtype=self.torch_dtype, device=self.pool.device)
         dev = self.pool.device
+        if k is None or v is None:
+            with _made_for(stream, dev) as told:
+                k, v = (told(torch.empty(shape, dtype=self.torch_dtype, device=dev)) if x is None
+                        else x for x in (k, v))
         for x in (k, v):
             if (x.shape != shape or x.dtype != self.torch_dtype or not x.is_contiguous()
                     or x.device != dev):
