@@ -364,14 +364,15 @@ class KVCache:
     def export_transcript(self, session: int, cap: int, stream=None):
         """Retained TRANSCRIPT positions of a session (Sec. 4.2), with their stored K and V
         of every layer: device tensors (positions [cap] int32, K and V [L][cap][Hkv][D],
-        count [1] int32), filled asynchronously on the stream."""
+        count [1] int32), filled asynchronously on the stream, to which they belong."""
         import torch
         dev = self.pool.device
         shape = (self.cfg.layers, max(1, cap), self.cfg.kv_heads, self.cfg.head_dim)
-        pos = torch.zeros(max(1, cap), dtype=torch.int32, device=dev)
-        k = torch.zeros(shape, dtype=self.torch_dtype, device=dev)
-        v = torch.zeros(shape, dtype=self.torch_dtype, device=dev)
-        count = torch.zeros(1, dtype=torch.int32, device=dev)
+        with _made_for(stream, dev) as told:
+            pos = told(torch.zeros(max(1, cap), dtype=torch.int32, device=dev))
+            k = told(torch.zeros(shape, dtype=self.torch_dtype, device=dev))
+            v = told(torch.zeros(shape, dtype=self.torch_dtype, device=dev))
+            count = told(torch.zeros(1, dtype=torch.int32, device=dev))
         _check(self.lib.kvc_export_transcript(self.ctx, session, cap, pos.data_ptr(), k.data_ptr(),
                                               v.data_ptr(), count.data_ptr(), _stream(stream)))
         return pos, k, v, count

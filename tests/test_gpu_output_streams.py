@@ -43,7 +43,7 @@ def outputs(cache, call, stream):
     return k, v, pos, count
 
 
-CALLS = ["read"]
+CALLS = ["read", "transcript"]
 
 
 @pytest.mark.parametrize("call", CALLS)
@@ -103,3 +103,13 @@ def test_memory_still_in_use_on_the_current_stream_is_not_taken(call):
     assert torch.equal(outs[1], v)
     torch.cuda.synchronize()
     assert torch.equal(outs[1], v)
+
+
+def test_a_transcript_is_not_cleared_behind_its_export():
+    """The current stream is busy: what clears the outputs runs in front of the export all the same."""
+    cache, v = filled()
+    side = torch.cuda.Stream()
+    torch.cuda._sleep(BUSY)
+    pos, k, got, count = cache.export_transcript(0, N, stream=side)
+    torch.cuda.synchronize()
+    assert int(count) == N and pos.tolist() == list(range(N)) and torch.equal(got, v)
