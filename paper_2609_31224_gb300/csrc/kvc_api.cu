@@ -55,9 +55,10 @@ Sizes derive_sizes(const kvc_config& c) {
   s.dec_slots = 4096;
   // Tagged partial slots of the pair-split decode (one per CTA of its one-wave grid).
   s.dec_tag_slots = c.dtype & KVC_KV4 ? 0 : 2048;
-  // Prefill partial slots: two per CTA of the bfloat16 kernel's stream-K split.
-  // (Of both kernels over 4-bit rows too, as many as fit in the same bytes.)
-  s.pf_slots = c.dtype == KVC_F32 ? 0 : 512;
+  // Prefill partial slots: two per CTA of the stream-K split over bfloat16 rows; of the slices over
+  // binary32 rows in 4 bits as many as fit in the same bytes.  (The other two prefill kernels merge
+  // within thread-block clusters.)
+  s.pf_slots = c.dtype == KVC_BF16 || c.dtype == (KVC_F32 | KVC_KV4) ? 512 : 0;
   return s;
 }
 

@@ -76,7 +76,7 @@ struct Dev {
   int32_t bitmap_words;
   int32_t max_moves;
   int32_t dec_slots;           // decode partial slots (two per CTA of a split)
-  int32_t pf_slots;            // prefill partial slots (two per CTA of a split; bfloat16)
+  int32_t pf_slots;            // prefill partial slots (bfloat16, and binary32 held in 4 bits)
   // memory
   uint8_t* pool;
   SessState* sess;
@@ -98,7 +98,7 @@ struct Dev {
   float2* dec_part_ml;         // [dec_slots][G] (m, l) in log2 units
   unsigned long long* dec_tagged;  // [dec_tag_slots][G * D + 2 G] tagged partial states
   int32_t dec_tag_slots;
-  float* pf_part_o;            // [pf_slots][D / 4][128 query rows][4]
+  float* pf_part_o;            // [pf_slots][D / 4][128 query rows][4] (in 4 bits: [slot][row][D])
   float2* pf_part_ml;          // [pf_slots][128]
   int32_t* dec_count;          // [max_seq * kv_heads] arrival counters
   int32_t* pf_count;           // [max_seq * kv_heads]

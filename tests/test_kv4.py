@@ -233,3 +233,16 @@ def test_no_early_read_of_a_chunk_in_flight(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-O1", "-I", inc, str(src), "-o", str(exe)], check=True)
     r = subprocess.run([str(exe)], capture_output=True, text=True)
     assert r.returncode == 0, (r.returncode, r.stdout)
+
+
+def test_a_bfloat16_cache_in_4_bits_has_no_slots_for_prefill_parts():
+    """Its prefill merges within clusters: of the workspace of 16-bit rows, neither the prefill's partial
+    rows (512 slots of 128 rows with their maximum and sum) nor the tagged ones of its decode."""
+    B.build()
+    of = lambda **kw: L.query_sizes(_cfg(**kw))[1]
+    prefill, tagged = 512 * 128 * (128 * 4 + 8), 2048 * (4 * 128 + 8) * 8
+    assert of(dtype=L.KVC_BF16) - of() == prefill + tagged
+    # binary32 in 4 bits keeps them (its slices meet in memory), binary32 has only the tagged ones.
+    f32 = dict(head_dim=64)
+    assert of(dtype=L.KVC_F32 | L.KVC_KV4, **f32) - of(dtype=L.KVC_F32, **f32) == \
+        prefill - 2048 * (4 * 64 + 8) * 8
