@@ -397,7 +397,7 @@ int kvc_create(kvc_ctx** out, const kvc_config* cfg, void* d_pool, size_t pool_b
       launch_init(d, cfg->rope_base, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess)
     return cleanup(fail(KVC_ECUDA, "initialisation failed: %s",
                         cudaGetErrorString(cudaGetLastError())));
-  const cudaError_t le = query_limits(d, &ctx->lim);
+  const cudaError_t le = query_limits(d, ctx->kv4, &ctx->lim);
   if (le != cudaSuccess)
     return cleanup(fail(KVC_ECUDA, "device query failed: %s", cudaGetErrorString(le)));
   *out = ctx;

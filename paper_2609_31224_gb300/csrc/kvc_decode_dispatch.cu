@@ -98,6 +98,7 @@ namespace {
 struct KnownLimits {
   unsigned long long ctx_id;
   int esz;
+  bool kv4;
   Limits lim;
 };
 constexpr int MAX_KNOWN = 64;
@@ -105,14 +106,28 @@ KnownLimits g_known[MAX_KNOWN];
 int g_n_known = 0;
 std::mutex g_known_mu;
 
+// Of the kernels over rows in the element type.
+cudaError_t own_type_limits(const Dev& d, Limits* lim) {
+  lim->dec_stream_k = decode_stream_k_grid(d);
+  lim->dec_wide = decode_split_slots(d.esz, true, lim->sms);
+  lim->dec_narrow = decode_split_slots(d.esz, false, lim->sms);
+  return d.esz == 2 ? prefill_tc_limits(lim) : prefill_f32_limits(lim);
+}
+
+// Of those over rows in 4 bits.
+cudaError_t kv4_limits(const Dev& d, Limits* lim) {
+  const cudaError_t e = kv4_decode_limits(d, lim);
+  return e != cudaSuccess ? e : kv4_prefill_limits(d, lim);
+}
+
 }  // namespace
 
-cudaError_t query_limits(const Dev& d, Limits* lim) {
+cudaError_t query_limits(const Dev& d, bool kv4, Limits* lim) {
   std::lock_guard<std::mutex> lock(g_known_mu);
   unsigned long long id = 0;
   const bool known = current_context_id(&id) == cudaSuccess;  // (else worked out each time)
   for (int i = 0; known && i < g_n_known; ++i)
-    if (g_known[i].ctx_id == id && g_known[i].esz == d.esz) {
+    if (g_known[i].ctx_id == id && g_known[i].esz == d.esz && g_known[i].kv4 == kv4) {
       *lim = g_known[i].lim;
       return cudaSuccess;
     }
@@ -120,15 +135,10 @@ cudaError_t query_limits(const Dev& d, Limits* lim) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&lim->sms, cudaDevAttrMultiProcessorCount, dev);
-  if (e != cudaSuccess) return e;
-  lim->dec_stream_k = decode_stream_k_grid(d);
-  lim->dec_wide = decode_split_slots(d.esz, true, lim->sms);
-  lim->dec_narrow = decode_split_slots(d.esz, false, lim->sms);
-  e = d.esz == 2 ? prefill_tc_limits(lim) : prefill_f32_limits(lim);
-  if (e == cudaSuccess) e = kv4_decode_limits(d, lim);
-  if (e == cudaSuccess) e = kv4_prefill_limits(d, lim);
+  if (e == cudaSuccess) e = kv4 ? kv4_limits(d, lim) : own_type_limits(d, lim);
   // A full table only means that later contexts repeat this for every kvc_create.
-  if (e == cudaSuccess && known && g_n_known < MAX_KNOWN) g_known[g_n_known++] = {id, d.esz, *lim};
+  if (e == cudaSuccess && known && g_n_known < MAX_KNOWN)
+    g_known[g_n_known++] = {id, d.esz, kv4, *lim};
   return e;
 }
 

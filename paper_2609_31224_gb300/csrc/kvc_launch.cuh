@@ -43,8 +43,10 @@ struct ReadArgsT {
 using ReadArgs = ReadArgsT<MAX_SEQ>;
 
 // What the device runs at once, for each kernel whose launch shape follows from it.  kvc_create
-// looks it up for the current CUDA context; the first time for a context and element type (about
-// 3 ms) that also sets the kernels' attributes, which belong to the CUDA context too.
+// looks it up for the current CUDA context; the first time for a context, element type and way of
+// holding the rows that also sets the attributes of the kernels over them, which belong to the CUDA
+// context too (about 2 ms in a process's first kvc_create, 0.5 to 1 ms for another kind).  What it
+// does not look up is 0.
 constexpr int PF_MAX_SLICES = 8;  // CTAs of a bfloat16 prefill cluster, at most
 constexpr int KV4_PF_WARPS = 6;   // warps that share a page in the prefill over 4-bit rows, at most
 struct Limits {
@@ -58,7 +60,7 @@ struct Limits {
   int kv4_prefill[KV4_PF_WARPS + 1];  // [w] CTAs of the prefill with w warps to a page
   int kv4_clusters[PF_MAX_SLICES + 1];  // [k] clusters of k CTAs of the bfloat16 prefill over them
 };
-cudaError_t query_limits(const Dev& d, Limits* lim);
+cudaError_t query_limits(const Dev& d, bool kv4, Limits* lim);  // kv4: rows in 4 bits
 // Id of the current CUDA context (never reused: a context that replaces a destroyed one at the
 // same address has another).
 cudaError_t current_context_id(unsigned long long* id);
