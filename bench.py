@@ -787,7 +787,8 @@ def main():
                     help="the model's order: appends without K/V, each layer's K/V written "
                          "just before its attention")
     ap.add_argument("--kv-bits", type=int, choices=[4], default=None,
-                    help="hold K and V in 4 bits (default: in the element type)")
+                    help="hold K and V in 4 bits (default: in the element type); for the "
+                         "64-session workload only")
     ap.add_argument("--budget-sweep", type=int, default=0, metavar="SESSIONS",
                     help="print the Table-3-shaped budget sweep over SESSIONS sessions and exit")
     ap.add_argument("--stress", default=None, metavar="B,W[,N]",
@@ -798,6 +799,12 @@ def main():
     ap.add_argument("--layers", type=int, default=None,
                     help="reduced case for profiler captures (default: the full 32)")
     args = ap.parse_args()
+    others = [name for name, on in (("--impl reference", args.impl == "reference"),
+                                    ("--compare-unbounded", args.compare_unbounded),
+                                    ("--budget-sweep", args.budget_sweep),
+                                    ("--stress", args.stress)) if on]
+    if args.kv_bits is not None and others:
+        ap.error(f"--kv-bits does not go with {others[0]}, which runs rows in the element type")
     if args.warmup < 3 and args.impl == "ours":
         print("warning: fewer than 3 warm-up steps", file=sys.stderr)
 

@@ -93,3 +93,14 @@ def test_step_bytes_of_a_cache_held_in_4_bits():
         total, one, n = bench.step_bytes(w, drv, step, {0: 100, 1: 50})
         assert one == 152 * row + 2 * 2 * q and n == 2
         assert total == 4 * (one + 2 * row)
+
+
+@pytest.mark.parametrize("mode", [["--impl", "reference"], ["--compare-unbounded"],
+                                  ["--budget-sweep", "2"], ["--stress", "64,2"]])
+def test_kv_bits_is_refused_where_it_would_be_ignored(mode):
+    """Modes over rows in the element type (or the oracle) print no figures for --kv-bits 4."""
+    r = subprocess.run([sys.executable, "bench.py", "--kv-bits", "4", "--steps", "1", "--warmup", "0"]
+                       + mode, cwd=ROOT, capture_output=True, text=True, timeout=600,
+                       env=dict(os.environ, CUDA_VISIBLE_DEVICES=""))
+    assert r.returncode == 2 and not r.stdout.strip()
+    assert "--kv-bits does not go with " + mode[0] in r.stderr
