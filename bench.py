@@ -77,6 +77,17 @@ def decode_traffic(alg_bytes_per_launch):
     return DECODE_TRAFFIC_RATIO * alg_bytes_per_launch
 
 
+def traffic_fields(alg_bytes_per_launch, kv_bits) -> dict:
+    """The roofline's DRAM traffic, with the note of where it comes from if there is one: the ratio was
+    taken of the stream-K kernel over rows in the element type."""
+    traffic = decode_traffic(alg_bytes_per_launch) if kv_bits is None else None
+    if traffic is None:
+        return {"traffic": None}
+    return {"traffic": traffic,
+            "traffic_note": "ncu DRAM bytes per algorithmic byte of the stream-K kernel on "
+                            "the 64-session two-layer case, times this launch's bytes"}
+
+
 def decode_kernel_label(w) -> str:
     """Kernel that the library's dispatch gives a full-batch decode call of `w` (sessions
     at full budget): the 16-warp pair split while every (session, KV head) pair gets six
@@ -376,10 +387,7 @@ def run_ours(args, rank: int, world: int, local_rank: int):
             "peak_kind": f"{peak_kind} copy bandwidth",
             "unit": "GB/s",
             "frac": (dec_gbs / peak) if dec_gbs else None,
-            "traffic": (decode_traffic((sum(dec_bytes) / len(dec_bytes)) if dec_bytes else None)
-                        if args.kv_bits is None else None),
-            "traffic_note": "ncu DRAM bytes per algorithmic byte of the stream-K kernel on "
-                            "the 64-session two-layer case, times this launch's bytes",
+            **traffic_fields((sum(dec_bytes) / len(dec_bytes)) if dec_bytes else None, args.kv_bits),
             "algorithmic_bytes_per_launch": (sum(dec_bytes) / len(dec_bytes)) if dec_bytes else None,
             "avg_launch_us": (1e3 * sum(dec_times) / len(dec_times)) if dec_times else None,
         },

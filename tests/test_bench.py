@@ -104,3 +104,12 @@ def test_kv_bits_is_refused_where_it_would_be_ignored(mode):
                        env=dict(os.environ, CUDA_VISIBLE_DEVICES=""))
     assert r.returncode == 2 and not r.stdout.strip()
     assert "--kv-bits does not go with " + mode[0] in r.stderr
+
+
+def test_a_traffic_note_stands_beside_a_figure_only(monkeypatch):
+    """No figure of the decode over rows in 4 bits, and none of other sources than the captured ones."""
+    monkeypatch.setattr(bench, "decode_traffic", lambda b: None if b is None else 1.008 * b)
+    got = bench.traffic_fields(1000.0, None)
+    assert got["traffic"] == pytest.approx(1008.0) and "stream-K" in got["traffic_note"]
+    assert bench.traffic_fields(1000.0, 4) == {"traffic": None}
+    assert bench.traffic_fields(None, None) == {"traffic": None}
