@@ -274,7 +274,7 @@ def run_ours(args, rank: int, world: int, local_rank: int):
     dec_ev = [(torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True))
               for _ in timed]
     t0, t1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-    launches = 0
+    launched_before = drv.cache.launches()
     clocks = Clocks(local_rank)
     if world > 1:
         torch.distributed.barrier()
@@ -295,7 +295,6 @@ def run_ours(args, rank: int, world: int, local_rank: int):
                 for layer in range(w.layers):
                     drv.cache.attn_decode_raw(layer, q_ptrs[layer], o_ptr, drv.stream)
                 dec_ev[i][1].record(stream)
-                launches += 2 + w.layers
             elif c is first_dec:
                 # The model's order: each layer's K/V written by its own decode launch
                 # (fused); each launch is timed on its own.
@@ -314,14 +313,13 @@ def run_ours(args, rank: int, world: int, local_rank: int):
                     e1.record(stream)
                     evs.append((e0, e1))
                 dec_ev[i] = evs
-                launches += 1 + w.layers
             else:
-                launches += drv.run_call(c, per_layer=per_layer)
+                drv.run_call(c, per_layer=per_layer)
         drv.cache.evict(st.evict_sessions, drv.resident_out)
-        launches += 2
         snapshot_resident(i + 1, st)
     t1.record(stream)
     host_submit_s = time.perf_counter() - host0
+    launches = drv.cache.launches() - launched_before
     torch.cuda.nvtx.range_pop()
     torch.cuda.synchronize()
     if world > 1:

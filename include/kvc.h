@@ -339,6 +339,10 @@ int kvc_read_kv(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, const int32_
                 const int32_t* h_cu_rows, int layer0, int n_layers, void* d_k_out, void* d_v_out,
                 int64_t* d_resident_out, void* stream);
 
+/* Kernels that the calls on ctx have launched since kvc_create, those captured into graphs counted once
+ * (their replays are the caller's).  Host bookkeeping: neither waits nor launches. */
+int kvc_launches(const kvc_ctx* ctx, int64_t* h_out);
+
 /* Free pages in the pool and the device error word (synchronises). */
 int kvc_device_status(kvc_ctx* ctx, int64_t* h_free_pages, int32_t* h_error_bits);
 

@@ -33,7 +33,7 @@ EXPORTED = ["kvc_query_sizes", "kvc_create", "kvc_destroy", "kvc_append_chunk",
             "kvc_attn_decode_noalloc",
             "kvc_resident_size", "kvc_release",
             "kvc_export_state", "kvc_export_kv", "kvc_export_transcript", "kvc_read_kv",
-            "kvc_device_status",
+            "kvc_launches", "kvc_device_status",
             "kvc_last_error"]
 
 
@@ -96,6 +96,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.kvc_export_transcript.argtypes = [vp, ctypes.c_int, i64, vp, vp, vp, vp, vp]
     lib.kvc_read_kv.argtypes = [vp, ctypes.c_int, p_i32, p_i32, p_i32, ctypes.c_int, ctypes.c_int,
                                 vp, vp, vp, vp]
+    lib.kvc_launches.argtypes = [vp, ctypes.POINTER(i64)]
     lib.kvc_device_status.argtypes = [vp, ctypes.POINTER(i64), ctypes.POINTER(i32)]
     lib.kvc_last_error.restype = ctypes.c_char_p
     for name in EXPORTED:
@@ -317,6 +318,12 @@ class KVCache:
     def release(self, sessions, stream=None) -> None:
         s = _i32(sessions)
         _check(self.lib.release_addr(self.ctx, len(s), s.ctypes.data, _stream(stream)))
+
+    def launches(self) -> int:
+        """Kernels that the calls on this cache have launched so far."""
+        out = ctypes.c_int64()
+        _check(self.lib.kvc_launches(self.ctx, ctypes.byref(out)))
+        return out.value
 
     # -- synchronising queries -------------------------------------------------------
     def resident_size(self, session: int) -> int:

@@ -193,6 +193,7 @@ struct kvc_ctx {
   int64_t est_pages_sum = 0;
   LaunchOrder order;       // of the attention launches since the last append
   bool last_single = false;
+  int64_t launches = 0;    // kernels launched by the calls so far
   uint32_t dec_epoch = 0;  // tag of the last decode launch's partial states
 };
 
@@ -290,7 +291,8 @@ int attend_kv4(kvc_ctx* ctx, int layer, const void* k, const void* v, const void
   bool capturing = false;
   KVC_CUDA(is_capturing(s, &capturing));
   KVC_CUDA(launch_attn_kv4(ctx->d, ctx->lim, &ctx->order, layer, k, v, q, out, ctx->last_n_seq,
-                           ctx->last_total, ctx->last_max_t, page_hint(ctx, capturing).sum * ctx->cfg.kv_heads, s));
+                           ctx->last_total, ctx->last_max_t, page_hint(ctx, capturing).sum * ctx->cfg.kv_heads, s,
+                           &ctx->launches));
   return KVC_OK;
 }
 
@@ -460,7 +462,8 @@ int kvc_append_chunk(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, const i
   for (int i = 0; i < n_seq; ++i) a.sessions[i] = h_sessions[i];
   for (int i = 0; i <= n_seq; ++i) a.cu[i] = h_cu_tokens[i];
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  KVC_CUDA(launch_append(ctx->d, ctx->kv4, a, d_types, d_k, d_v, single, ctx->lim.sms, s));
+  KVC_CUDA(launch_append(ctx->d, ctx->kv4, a, d_types, d_k, d_v, single, ctx->lim.sms, s,
+                         &ctx->launches));
   for (int i = 0; i < n_seq; ++i) {
     const int sid = h_sessions[i];
     const int t = h_cu_tokens[i + 1] - h_cu_tokens[i];
@@ -496,6 +499,7 @@ int kvc_append_kv_layer(kvc_ctx* ctx, int layer, const void* d_k, const void* d_
   if (!ctx->attn_valid)
     return fail(KVC_ESTATE, "kvc_append_kv_layer needs a preceding kvc_append_chunk (no evict/release after it)");
   KVC_CUDA(write_layer(ctx, layer, d_k, d_v, static_cast<cudaStream_t>(stream)));
+  ++ctx->launches;
   // The next attention launch must not read early: its prologue loads pages
   // this write may still be filling.
   ctx->order.layer_write(layer);
@@ -513,6 +517,7 @@ int kvc_evict(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, int64_t* d_res
   for (int i = 0; i < n_seq; ++i) a.sessions[i] = h_sessions[i];
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   KVC_CUDA(launch_evict(ctx->d, ctx->kv4, a, d_resident_out, ctx->h_readback, ctx->lim.sms, s));
+  ctx->launches += 2;  // plan and copy
   for (int i = 0; i < n_seq; ++i) ctx->resident[h_sessions[i]].evict(ctx->cfg);
   ctx->used_ub += n_seq;  // an evict adds at most one page per session, net
   ctx->delta_since_readback += n_seq;
@@ -531,6 +536,7 @@ int kvc_release(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, void* stream
   for (int i = 0; i < n_seq; ++i) a.sessions[i] = h_sessions[i];
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   KVC_CUDA(launch_release(ctx->d, a, ctx->h_readback, s));
+  ++ctx->launches;
   for (int i = 0; i < n_seq; ++i) {
     ctx->tail_mod[h_sessions[i]] = 0;
     ctx->pos_next[h_sessions[i]] = 0;
@@ -570,6 +576,7 @@ int kvc_attn_decode(kvc_ctx* ctx, int layer, const void* d_q, void* d_out, void*
   KVC_CUDA(launch_attn_decode(ctx->d, ctx->lim, layer, d_q, d_out, ctx->last_n_seq,
                               page_hint(ctx, capturing).max, ctx->order.early(layer, false),
                               static_cast<cudaStream_t>(stream), epoch));
+  ++ctx->launches;
   ctx->order.launched(layer, false);
   return KVC_OK;
 }
@@ -593,6 +600,7 @@ int kvc_attn_decode_kv(kvc_ctx* ctx, int layer, const void* d_k, const void* d_v
   KVC_CUDA(launch_attn_decode(ctx->d, ctx->lim, layer, d_q, d_out, ctx->last_n_seq,
                               page_hint(ctx, capturing).max, ctx->order.early(layer, true),
                               static_cast<cudaStream_t>(stream), epoch, d_k, d_v));
+  ++ctx->launches;
   ctx->order.launched(layer, true);
   return KVC_OK;
 }
@@ -614,6 +622,7 @@ int kvc_attn_decode_noalloc(kvc_ctx* ctx, int layer, const void* d_q, void* d_ou
                 noalloc_max_pairs(), ctx->last_n_seq, ctx->cfg.kv_heads, pairs);
   KVC_CUDA(launch_attn_decode_noalloc(ctx->d, layer, d_q, d_out, ctx->last_n_seq,
                                       static_cast<cudaStream_t>(stream)));
+  ++ctx->launches;
   return KVC_OK;
 }
 
@@ -631,6 +640,7 @@ int kvc_attn_prefill_chunk(kvc_ctx* ctx, int layer, const void* d_q, void* d_out
   KVC_CUDA(launch_attn_prefill(ctx->d, ctx->lim, layer, d_q, d_out, ctx->last_n_seq,
                                ctx->last_max_t, pages.max, pages.sum,
                                ctx->order.early(layer, false), s));
+  ++ctx->launches;
   ctx->order.launched(layer, false);
   return KVC_OK;
 }
@@ -654,14 +664,17 @@ int kvc_attn_prefill_chunk_kv(kvc_ctx* ctx, int layer, const void* d_k, const vo
     KVC_CUDA(launch_attn_prefill(ctx->d, ctx->lim, layer, d_q, d_out, ctx->last_n_seq,
                                  ctx->last_max_t, pages.max, pages.sum,
                                  ctx->order.early(layer, true), s, d_k, d_v));
+    ++ctx->launches;
     ctx->order.launched(layer, true);
   } else {
     // Binary32 (CUDA-core prefill): the rows first, then the attention, unoverlapped.
     KVC_CUDA(launch_append_layers(ctx->d, ctx->last_total, layer, 1, d_k, d_v, false, s));
+    ++ctx->launches;
     ctx->order.layer_write(layer);
     KVC_CUDA(launch_attn_prefill(ctx->d, ctx->lim, layer, d_q, d_out, ctx->last_n_seq,
                                  ctx->last_max_t, pages.max, pages.sum,
                                  ctx->order.early(layer, false), s));
+    ++ctx->launches;
     ctx->order.launched(layer, false);
   }
   return KVC_OK;
@@ -758,6 +771,7 @@ int kvc_export_transcript(kvc_ctx* ctx, int session, int64_t cap, int32_t* d_pos
     return fail(KVC_EINVAL, "d_k_out / d_v_out must be 16-byte aligned");
   KVC_CUDA(launch_transcript(ctx->d, ctx->kv4, session, (int)cap, d_pos_out, d_k_out, d_v_out, d_count,
                              static_cast<cudaStream_t>(stream)));
+  ctx->launches += 2;  // gather and copy
   return KVC_OK;
 }
 
@@ -793,6 +807,7 @@ int kvc_read_kv(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, const int32_
   for (int i = 0; i <= n_seq; ++i) a.cu[i] = h_cu_rows[i];
   KVC_CUDA(launch_read_kv(ctx->d, ctx->kv4, a, layer0, n_layers, d_k_out, d_v_out, d_resident_out,
                           ctx->lim.sms, static_cast<cudaStream_t>(stream)));
+  ++ctx->launches;
   return KVC_OK;
 }
 
@@ -863,6 +878,13 @@ int kvc_export_kv(kvc_ctx* ctx, int session, int layer, void* h_k, void* h_v, in
     const int hi = std::min(PS, st.live_head + st.n_live - b * PS);
     if (hi > lo && (rc = emit(lp[b], lo, hi))) return rc;
   }
+  return KVC_OK;
+}
+
+int kvc_launches(const kvc_ctx* ctx, int64_t* h_out) {
+  g_err.clear();
+  if (!ctx || !h_out) return fail(KVC_EINVAL, "ctx / h_out is NULL");
+  *h_out = ctx->launches;
   return KVC_OK;
 }
 

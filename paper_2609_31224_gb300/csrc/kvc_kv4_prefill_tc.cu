@@ -757,7 +757,7 @@ cudaError_t kv4_prefill_tc_limits(Limits* lim) {
 
 cudaError_t launch_prefill_kv4_tc(const Dev& d, const Limits& lim, int layer, const void* q,
                                   void* out, int n_pairs, int64_t units, Early early,
-                                  cudaStream_t s) {
+                                  cudaStream_t s, int64_t* launches) {
   // How the pairs are cut, by what was measured: a CTA takes 9 us beside its stages of 1.15 us, a merge
   // 1 us.  (31 stages: one session 45 us in one slice, 28 in 2, 19 in 4, 15.7 in 8; 9 sessions 46, 30, 42
   // and 81 us; 64 sessions 183 in one, 207 in 2.)  Whole waves of uncut pairs may go first, the rest
@@ -814,6 +814,7 @@ cudaError_t launch_prefill_kv4_tc(const Dev& d, const Limits& lim, int layer, co
                                              static_cast<__nv_bfloat16*>(out), part == 0 ? 0 : first, kp,
                                              part == 1 && first > 0 && early == EARLY_NONE ? EARLY_ALL : early);
     if (e != cudaSuccess) return e;
+    ++*launches;
   }
   return cudaSuccess;
 }

@@ -68,9 +68,10 @@ cudaError_t current_context_id(unsigned long long* id);
 cudaError_t launch_init(const Dev& d, double rope_base, cudaStream_t s);
 // single: every session of the call gets exactly one token (one session: plan and K/V write in
 // one launch).
-// kv4: the rows are held in 4 bits.
+// kv4: the rows are held in 4 bits.  Adds its launches to *launches, as the others that take it do.
 cudaError_t launch_append(const Dev& d, bool kv4, const AppendArgs& a, const uint8_t* types,
-                          const void* k, const void* v, bool single, int sms, cudaStream_t s);
+                          const void* k, const void* v, bool single, int sms, cudaStream_t s,
+                          int64_t* launches);
 // after_plan: launched right behind the plan kernel of the same append.
 cudaError_t launch_append_layers(const Dev& d, int total, int layer0, int n_layers, const void* k,
                                  const void* v, bool after_plan, cudaStream_t s);
@@ -95,7 +96,8 @@ cudaError_t launch_transcript_copy_kv4(const Dev& d, int cap, void* k_out, void*
 // only.  Asks `order` when it may read early, and reports its launches to it.
 cudaError_t launch_attn_kv4(const Dev& d, const Limits& lim, LaunchOrder* order, int layer,
                             const void* new_k, const void* new_v, const void* q, void* out,
-                            int n_seq, int total, int max_t, int64_t units, cudaStream_t s);
+                            int n_seq, int total, int max_t, int64_t units, cudaStream_t s,
+                            int64_t* launches);
 // Single tokens (kvc_kv4_decode.cu); with new_k / new_v their rows are written by the launch itself.
 cudaError_t launch_decode_kv4(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
                               const void* new_k, const void* new_v, int n_pairs, int64_t units,
@@ -105,7 +107,7 @@ cudaError_t kv4_prefill_limits(const Dev& d, Limits* lim);
 // Chunks of bfloat16 calls (kvc_kv4_prefill_tc.cu).
 cudaError_t launch_prefill_kv4_tc(const Dev& d, const Limits& lim, int layer, const void* q,
                                   void* out, int n_pairs, int64_t units, Early early,
-                                  cudaStream_t s);
+                                  cudaStream_t s, int64_t* launches);
 cudaError_t launch_prefill_kv4_f32(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
                                    int n_pairs, int max_t, int64_t units, Early early, cudaStream_t s);
 cudaError_t kv4_prefill_tc_limits(Limits* lim);

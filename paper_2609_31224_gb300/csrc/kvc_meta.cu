@@ -1129,7 +1129,8 @@ cudaError_t launch_init(const Dev& d, double rope_base, cudaStream_t s) {
 // that one before it reads anything but the caller's inputs), so that a chain of short
 // kernels does not pay a full launch each.
 cudaError_t launch_append(const Dev& d, bool kv4, const AppendArgs& a, const uint8_t* types,
-                          const void* k, const void* v, bool single, int sms, cudaStream_t s) {
+                          const void* k, const void* v, bool single, int sms, cudaStream_t s,
+                          int64_t* launches) {
   cudaError_t e;
   if (single && a.n_seq <= FEW) {
     // One CTA writes the K/V rows only for a one-session call (a few hundred KiB at
@@ -1147,7 +1148,10 @@ cudaError_t launch_append(const Dev& d, bool kv4, const AppendArgs& a, const uin
       e = launch_ex(&append_few_kernel<float>, dim3(1), block, 0, s, true, d, few, types,
                     static_cast<const float*>(fuse_kv ? k : nullptr),
                     static_cast<const float*>(fuse_kv ? v : nullptr));
-    if (fuse_kv) return e;
+    if (fuse_kv) {
+      *launches += e == cudaSuccess;
+      return e;
+    }
   } else if (single) {
     e = launch_ex(&append_many_kernel, dim3(1), dim3(META_THREADS), 0, s, true, d, a, types);
   } else if (a.n_seq <= FEW) {
@@ -1160,9 +1164,12 @@ cudaError_t launch_append(const Dev& d, bool kv4, const AppendArgs& a, const uin
   } else {
     e = launch_ex(&append_plan_kernel<MAX_SEQ>, dim3(1), dim3(META_THREADS), 0, s, true, d, a, types);
   }
+  *launches += e == cudaSuccess;
   if (e != cudaSuccess || k == nullptr) return e;  // plan only: layers follow one by one
-  return kv4 ? launch_append_layers_kv4(d, a.total, 0, d.layers, k, v, true, false, sms, s)
-             : launch_append_layers(d, a.total, 0, d.layers, k, v, true, s);
+  e = kv4 ? launch_append_layers_kv4(d, a.total, 0, d.layers, k, v, true, false, sms, s)
+          : launch_append_layers(d, a.total, 0, d.layers, k, v, true, s);
+  *launches += e == cudaSuccess;
+  return e;
 }
 
 cudaError_t launch_append_layers(const Dev& d, int total, int layer0, int n_layers, const void* k,

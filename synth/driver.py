@@ -185,13 +185,13 @@ class Driver:
         kvc_attn_prefill_chunk_kv), or, for calls without attention, just before it
         would run (kvc_append_kv_layer)."""
         cache = self.cache
+        before = cache.launches()
         _, s_p, _, c_p, t_ptr, k_ptr, v_ptr, q_ptrs, o_ptr = c.raw
         stream = self.stream
         cache.append_chunk_raw(len(c.sessions), s_p, c_p, t_ptr, None if per_layer else k_ptr,
                                None if per_layer else v_ptr, stream)
         if on_append is not None:
             on_append(c)
-        launches = 1 if per_layer else 2
         do_attn = attention and c.q is not None and c.kind != "prefix"
         fn = cache.attn_prefill_raw if c.kind == "prefill" else cache.attn_decode_raw
         kv_stride = c.k.stride(0) * c.k.element_size()
@@ -202,32 +202,28 @@ class Driver:
                 fused = (cache.attn_decode_kv_raw if c.kind == "decode"
                          else cache.attn_prefill_kv_raw)
                 fused(layer, kl, vl, q_ptrs[layer], o_ptr, stream)
-                one = c.kind == "decode" or (self.w.dtype == "bf16" and self.kv_bits is None)
-                launches += 1 if one else 2
                 if on_attention is not None:
                     on_attention(c, layer)
                 continue
             if per_layer:
                 cache.append_kv_layer_raw(layer, kl, vl, stream)
-                launches += 1
             if do_attn:
                 fn(layer, q_ptrs[layer], o_ptr, stream)
-                launches += 1
                 if on_attention is not None:
                     on_attention(c, layer)
-        return launches
+        return cache.launches() - before
 
     def run_step(self, st: Step, attention: bool = True, on_attention=None,
                  on_evict=None, on_append=None, per_layer: bool = False) -> int:
-        launches = 0
+        """Every call of a step. Returns kernels launched."""
+        before = self.cache.launches()
         for c in st.calls:
-            launches += self.run_call(c, attention, on_attention, on_append, per_layer)
+            self.run_call(c, attention, on_attention, on_append, per_layer)
         if st.evict_sessions is not None and len(st.evict_sessions):
             self.cache.evict(st.evict_sessions, self.resident_out)
-            launches += 2
             if on_evict is not None:
                 on_evict(st)
-        return launches
+        return self.cache.launches() - before
 
     def release(self, sessions) -> None:
         """End sessions (kvc_release): their positions start over at 0; later steps feed

@@ -246,3 +246,9 @@ def test_a_bfloat16_cache_in_4_bits_has_no_slots_for_prefill_parts():
     f32 = dict(head_dim=64)
     assert of(dtype=L.KVC_F32 | L.KVC_KV4, **f32) - of(dtype=L.KVC_F32, **f32) == \
         prefill - 2048 * (4 * 64 + 8) * 8
+
+
+def test_launches_refuses_null():
+    lib = L.load_library()
+    out = ctypes.c_int64()
+    assert lib.kvc_launches(None, ctypes.byref(out)) == -1 and b"NULL" in lib.kvc_last_error()
