@@ -27,6 +27,7 @@
 #include <algorithm>
 
 #include "kvc_kv4.cuh"
+#include "kvc_kv4_cuts.h"
 
 namespace kvc {
 
@@ -39,7 +40,6 @@ constexpr int G = 4;               // query heads per KV head
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float P_SHIFT = 8.f;     // log2 of the weight P of a key at the reference
 constexpr float P_LAG = 6.f;       // and of how far above it a weight may be: 2^14 in all
-constexpr int MAX_PARTS = 64;      // CTAs that share a (session, KV head) pair, at most
 
 // Shape of a CTA: WARPS warps, each with its own ring of STAGES pairs of pages.
 template <typename T_, int D_, int WARPS_, int STAGES_>
@@ -59,7 +59,7 @@ struct Cfg {
   static constexpr int PARTS_ROOM = 96;                         // parts and a batch past them
   static constexpr int WEIGHT = STATE_ML + WARPS * G * 8;       // [PARTS_ROOM][G], of parts
   static constexpr int BARS = WEIGHT + PARTS_ROOM * G * 4;
-  static_assert(PARTS_ROOM >= MAX_PARTS + 20, "room for zeros");
+  static_assert(PARTS_ROOM >= DECODE_MAX_PARTS + 20, "room for zeros");
   static constexpr int SMEM = BARS + WARPS * STAGES * 8;
   static_assert(PAGE % 16 == 0 && RING % 16 == 0 && BARS % 8 == 0, "alignment");
 };
@@ -652,7 +652,7 @@ __global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
     seg.u = u_begin = seg.pair_start + (int)((int64_t)slice * nb / slices);
     seg.end = u_end = seg.pair_start + (int)((int64_t)(slice + 1) * nb / slices);
   } else {
-    us = unit_split(d, gridDim.x, cut.min_units, MAX_PARTS);
+    us = unit_split(d, gridDim.x, cut.min_units, DECODE_MAX_PARTS);
     if (cta >= us.n_cta) {
       pdl_wait();
       return;
@@ -847,51 +847,11 @@ cudaError_t launch(const Dev& d, int layer, const void* q, void* out, const void
                    static_cast<const T*>(new_k), static_cast<const T*>(new_v), cut, (int)early);
 }
 
-// How a call is cut, by what a launch takes in us: a fixed chain, then times in units of a page's
-// work (binary32 pages, half as long, take 0.7 of it): the pages of a warp one after the other, each
-// the longer the more warps share an SM, and 2 for the merge of a pair's slices.  Measured (us,
-// 8 KV heads; Mk, Nk: k slices of 8 and 4 warps, S: stream-K; the first is the one chosen):
-//   pages      1 session                4                     14                     38, 64
-//    to 7   N1 3.0  M1 3.2  S 7.9   M1 3.0  N1 3.1        M1 3.7  N1 3.8        M1 4.5 N1 3.8, N1 4.9 S 12.4
-//      25   M1 3.9  N8 4.5  S 8.8   M1 4.0  N1 4.6        M1 4.8  N1 5.4        M1 6.7 N1 6.8, N1 9.0 S 15.8
-//      94   M11 5.1 M14 4.9 S 9.5   M4 6.4  M8 6.2        M1 9.3  N5 9.3        M1 13.5, N1 23.8 S 27.4
-//     288   M17 5.7 N16 6.2 S 11.0  M8 8.8  N17 9.2       N5 18.3 M2 20.6       M1 33.7, S 60.1 M1 63.0
-// One slice each and no merge wins up to about 40 pages; then as many slices as give a warp a page or
-// two; stream-K where pairs outnumber the SMs' room and their last CTAs would leave most SMs empty.
-struct Choice {
-  bool wide;
-  int slices;  // 0: stream-K
-};
-Choice choose(int sms, int n_pairs, int64_t units, int esz) {
-  const float page = esz == 2 ? 1.f : 0.7f;
-  const int pages = (int)((units + n_pairs - 1) / n_pairs);
-  Choice best = {false, 0};
-  float least = 3.4f + page * (8.4f + 0.0534f * units / sms);
-  for (int wide = 0; wide < 2; ++wide) {
-    const int warps = wide ? 8 : 4;
-    const int most = std::max(1, std::min(std::min(MAX_PARTS, pages), sms * (16 / warps) / n_pairs));
-    for (int k = 1; k <= most; ++k) {
-      const int64_t ctas = (int64_t)n_pairs * k;
-      const bool alone = ctas <= sms;
-      const float each = !alone ? 0.85f : wide ? 0.56f : 0.43f;
-      const int64_t room = sms * (16 / warps), waves = (ctas + room - 1) / room;
-      const int64_t steps = waves * ((pages + k * warps - 1) / (k * warps));
-      const float t = 3.4f + page * (steps * each + (k > 1 ? 2.f + 0.03f * k : 0.f) +
-                                     (alone ? ctas / (float)sms : 1.5f));
-      if (t < least) {
-        least = t;
-        best = {wide != 0, k};
-      }
-    }
-  }
-  return best;
-}
-
 template <typename T, int D>
 cudaError_t launch_any(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
                        const void* new_k, const void* new_v, int n_pairs, int64_t units, bool early,
                        cudaStream_t s) {
-  const Choice c = choose(lim.sms, n_pairs, units, d.esz);
+  const DecodeCut c = decode_cut(lim.sms, n_pairs, units, d.esz);
   if (c.slices == 0)
     return launch<Narrow<T, D>>(d, layer, q, out, new_k, new_v, lim.kv4_decode, false, {0, 8}, early, s);
   const int grid = n_pairs * c.slices;
