@@ -4,7 +4,9 @@
 //
 // Every attention launch lets the next one start before it has finished, so a chain of early
 // launches may overlap.  The first launch after an append, or after a layer write, waits for
-// it before it lets anything else start.  A fused launch writes its layer's rows itself and
+// it before it lets anything else start, but for those that know EARLY_OLD: behind a complete
+// plan they let others start at once, read the older pages, and wait before the first page that
+// holds a row of the append.  What they let start knows no more than they did.  A fused launch writes its layer's rows itself and
 // reads them from the caller's buffers, so launches on other layers may overlap it, and so may
 // a fused launch on the same layer; a plain launch on that layer reads the rows from the pool
 // and has to wait, after which no fused write is pending any more.
@@ -14,8 +16,8 @@
 
 namespace kvc {
 
-// What a launch may read before the kernels in front of it are complete: nothing, the pages without a row
-// of the last append, or all pages.
+// What a launch may read before the kernels in front of it are complete: nothing, the pages
+// without a row of the last append, or all pages.
 enum Early { EARLY_NONE, EARLY_OLD, EARLY_ALL };
 
 class LaunchOrder {
@@ -26,7 +28,9 @@ class LaunchOrder {
     written_ = !with_kv ? 0 : layers >= 64 ? ~0ull : (1ull << layers) - 1;
     settle();
   }
-  // A separate write of one layer's K/V, complete before the launch behind it starts.
+  // A separate write of one layer's K/V.  It waits for everything in front of it before it lets the
+  // launch behind it start: the plan and all older rows are complete by then.  Its own rows are not,
+  // until that launch has waited.
   void layer_write(int layer) {
     written_ |= 1ull << layer;
     planned_ = true;
@@ -50,10 +54,9 @@ class LaunchOrder {
     waited_ = planned_ = true;
   }
 
-
-  // Plain launches that know EARLY_OLD: behind a complete plan, but not yet behind the write of the append's
-  // rows, they read early all pages but those.  Such a launch lets others start before it has waited
-  // itself, so that it changes nothing here: none of them may take the rows for complete.
+  // Plain launches that know EARLY_OLD: behind a complete plan, but not yet behind the write of the
+  // append's rows, they read early all pages but those.  Such a launch lets others start before it
+  // has waited itself, so that it changes nothing here: none of them may take the rows for complete.
   Early early_pages(int layer) const {
     return early(layer, false) ? EARLY_ALL : planned_ ? EARLY_OLD : EARLY_NONE;
   }
