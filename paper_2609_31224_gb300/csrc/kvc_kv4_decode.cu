@@ -672,7 +672,7 @@ __global__ void __launch_bounds__(C::THREADS, 16 / C::WARPS) decode_kv4_kernel(
   uint32_t loads = 0;  // steps of this warp, over all segments before
   ring.open(d, layer, keep(), warp);
   for (int k = 0; k < min(C::STAGES, ring.steps()); ++k) ring.issue(d, k, k, lane);
-  if (!waited && warp == 0) prefetch_query<C>(d, seg.si, seg.head, q, lane);
+  if (warp == 0) prefetch_query<C>(d, seg.si, seg.head, q, lane);
 
   for (;;) {
     const UnitSeg& cur = *ring.seg;
