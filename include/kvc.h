@@ -57,9 +57,10 @@ enum { KVC_F32 = 0, KVC_BF16 = 1 };
  * It stands for s * c: elements beyond 65408 are held as 65408, groups below 3.5 * 2^-20 as 0.  A
  * group that holds an infinity or a NaN stands for NaN.
  * Every call takes such a context but kvc_attn_decode_noalloc, which returns KVC_EINVAL.  Attention
- * runs over the numbers that the codes stand for, in binary32 with exact K and V operands; for
- * bfloat16 q (scaled by a power of two) and P are rounded to binary16 for the tensor cores, for
- * binary32 each is split into two such pieces. */
+ * runs over the numbers that the codes stand for, in binary32 with exact K and V operands.  For the
+ * tensor cores q is scaled by a power of two: for bfloat16 P, and in chunks of several tokens q, are
+ * rounded to binary16 (single tokens keep q in two such pieces), for binary32 both are split into
+ * two.  (The precision that the attention calls below state is that of rows in the element type.) */
 #define KVC_KV4 0x10
 
 /* Token type tags (low 7 bits of a type byte).  Sec. 3.3: ACOUSTIC (unit
@@ -231,7 +232,8 @@ int kvc_attn_prefill_chunk(kvc_ctx* ctx, int layer, const void* d_q, void* d_out
  * chunk's K (rotated at its positions) and V of the layer are written into their
  * slots and attended in the same call.  Same results and stored bytes as
  * kvc_append_kv_layer followed by kvc_attn_prefill_chunk.  For bfloat16 the write
- * happens inside the attention launch; for binary32 it is a separate launch first.
+ * happens inside the attention launch; for binary32, and with KVC_KV4 (but in chunks
+ * of one token), it is a separate launch first.
  *   d_k, d_v   device [total][Hkv][D], the layer's rows of the appended chunk,
  *              total and order as in the last append; 16-byte aligned
  *   other arguments as for kvc_attn_prefill_chunk */

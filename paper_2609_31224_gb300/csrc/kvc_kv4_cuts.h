@@ -21,6 +21,7 @@ constexpr int DECODE_MAX_PARTS = 64;  // CTAs that share a (session, KV head) pa
 //     288   M17 5.7 N16 6.2 S 11.0  M8 8.8  N17 9.2       N5 18.3 M2 20.6       M1 33.7, S 60.1 M1 63.0
 // One slice each and no merge wins up to about 40 pages; then as many slices as give a warp a page or
 // two; stream-K where pairs outnumber the SMs' room and their last CTAs would leave most SMs empty.
+// A launch counts as if it stood alone: one layer's CTAs leave no room for the next one's.
 // n_pairs (session, KV head) pairs with `units` pages in all.
 struct DecodeCut {
   bool wide;   // 8 warps a CTA (else 4)

@@ -30,7 +30,9 @@
 // 73 us at the measured rate (68 of their 128 rows are tokens), and about 6,000 warp instructions a stage,
 // 2,000 of them the unpacking, 1,300 the weights, hold 53 % of the issue slots: 1.15 us a stage.  Measured
 // 169 us a layer (233 as first written; 168 over bfloat16 rows, whose operands need no unpacking), one
-// session 15.7 us, 9 sessions 30 us.  Larger stages pay: at 96 keys the hops between the roles cost
+// session 15.7 us (12.5), 9 sessions 30 us (30).  Few sessions take 2 to 3 us more than over bfloat16
+// rows whatever their length (one of 100 positions 7.6 and 5.8, of 8,000 18.9 and 16.3): not the stages,
+// but what each CTA does once.  Larger stages pay: at 96 keys the hops between the roles cost
 // 15 % more; softmax warps of 64 columns each beat four of 128 by a seventh.
 #include <cuda.h>
 
