@@ -288,9 +288,55 @@ int kvc_attn_decode(kvc_ctx* ctx, int layer, const void* d_q, void* d_out, void*
  *     contexts over the same CUDA context) race on it, so serialise them. */
 int kvc_attn_decode_noalloc(kvc_ctx* ctx, int layer, const void* d_q, void* d_out, void* stream);
 
+/* GQA attention of one layer for the queries of the last append, chunks of any length (a system
+ * prompt, a document, a session fed back from its tokens): query t of a session sees every resident
+ * key at or before its own position.  Calls of single tokens, and of chunks of at most 32, are
+ * kvc_attn_decode and kvc_attn_prefill_chunk.  Longer bfloat16 chunks run on tensor cores with q and P
+ * rounded to bfloat16, binary32 accumulation and softmax; binary32 ones stay in binary32 on CUDA cores.
+ *   d_q, d_out  device [total][Hq][D], as for kvc_attn_prefill_chunk
+ * KVC_EINVAL with KVC_KV4 for chunks of more than 32 tokens. */
+int kvc_attn_prompt(kvc_ctx* ctx, int layer, const void* d_q, void* d_out, void* stream);
+
+/* Attention weights that the resident positions draw from the queries of the last append in one layer:
+ * softmax(RoPE(q, p_t) . k / sqrt(D)) summed over the chunk's tokens t and all query heads is added to
+ * each resident position's weight (others are left as they are).  Chunks of any length; same order of
+ * calls as the attention, which it neither needs nor changes.  Binary32 throughout (bfloat16 rows: q
+ * is held in pieces that keep 16 bits or more); results repeat bit for bit.
+ *   d_q        device [total][Hq][D] un-rotated queries
+ *   d_weights  device [n_sessions][max_positions] binary32, by session id and position, 16-byte
+ *              aligned; the caller clears a session's row when it ends (kvc_release)
+ *   d_work     device scratch of at least kvc_weights_workspace bytes, 256-byte aligned; its
+ *              contents need not last between calls, calls that share it must be ordered
+ * KVC_EINVAL with KVC_KV4. */
+int kvc_attn_weights(kvc_ctx* ctx, int layer, const void* d_q, float* d_weights, void* d_work,
+                     size_t work_bytes, void* stream);
+
+/* Bytes of scratch that kvc_attn_weights needs for a configuration. */
+int kvc_weights_workspace(const kvc_config* cfg, size_t* bytes);
+
 /* Resident count of one session (n_hist + n_live), including the system
  * prefix and text (Sec. 3.3).  Synchronises the device. */
 int kvc_resident_size(kvc_ctx* ctx, int session, int64_t* h_out);
+
+/* Eviction by weight, for each listed session: while more than h_keep[i] positions are resident, the
+ * candidate of the smallest weight is dropped, of equal ones the one of the lowest position (-0 counts
+ * as 0, a NaN as -infinity); it stops when none is left.  Candidates are resident positions of a type
+ * in `kinds`, at a position >= sink and < pos_next - recent, those that earlier evictions kept
+ * included; units, the window, the budget and the policy play no part.  What stays keeps its order,
+ * positions and rows (all layers), packed in place; consumed pages are freed.
+ *   h_keep      host [n_seq] positions to leave, >= 0
+ *   d_weights   device [n_sessions][max_positions] binary32, by session id and position (what
+ *               kvc_attn_weights adds up); read at the candidates only
+ *   kinds       bit t: positions of type t may go (1 << KVC_ACOUSTIC, ...)
+ *   d_resident_out  optional device [n_seq] int64: resident count afterwards
+ *   d_kept      optional device [n_seq][max_positions] bytes: 1 at positions that are resident
+ *               afterwards, 0 at the others below pos_next; the rest is left as it is
+ * May need one new page for each session before pages are freed; where the pool has none (or a page
+ * list would overflow) the device error word records it and no session of the call changes.
+ * Invalidates the last append's queries for attention.  With KVC_KV4 the 4-bit rows move as they are. */
+int kvc_evict_weighted(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, const int32_t* h_keep,
+                       const float* d_weights, int kinds, int sink, int recent,
+                       int64_t* d_resident_out, uint8_t* d_kept, void* stream);
 
 /* End sessions: free all their pages and reset them to position 0. */
 int kvc_release(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, void* stream);

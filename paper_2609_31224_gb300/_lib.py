@@ -30,7 +30,8 @@ EXPORTED = ["kvc_query_sizes", "kvc_create", "kvc_destroy", "kvc_append_chunk",
             "kvc_append_kv_layer", "kvc_evict",
             "kvc_attn_prefill_chunk", "kvc_attn_prefill_chunk_kv", "kvc_attn_decode",
             "kvc_attn_decode_kv",
-            "kvc_attn_decode_noalloc",
+            "kvc_attn_decode_noalloc", "kvc_attn_prompt", "kvc_attn_weights",
+            "kvc_weights_workspace", "kvc_evict_weighted",
             "kvc_resident_size", "kvc_release",
             "kvc_export_state", "kvc_export_kv", "kvc_export_transcript", "kvc_read_kv",
             "kvc_launches", "kvc_device_status",
@@ -88,6 +89,11 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.kvc_attn_decode_kv.argtypes = [vp, ctypes.c_int, vp, vp, vp, vp, vp]
     lib.kvc_attn_prefill_chunk_kv.argtypes = [vp, ctypes.c_int, vp, vp, vp, vp, vp]
     lib.kvc_attn_decode_noalloc.argtypes = [vp, ctypes.c_int, vp, vp, vp]
+    lib.kvc_attn_prompt.argtypes = [vp, ctypes.c_int, vp, vp, vp]
+    lib.kvc_attn_weights.argtypes = [vp, ctypes.c_int, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.kvc_weights_workspace.argtypes = [ctypes.POINTER(Config), ctypes.POINTER(ctypes.c_size_t)]
+    lib.kvc_evict_weighted.argtypes = [vp, ctypes.c_int, vp, vp, vp, ctypes.c_int, ctypes.c_int,
+                                       ctypes.c_int, vp, vp, vp]
     lib.kvc_resident_size.argtypes = [vp, ctypes.c_int, ctypes.POINTER(i64)]
     lib.kvc_release.argtypes = [vp, ctypes.c_int, p_i32, vp]
     lib.kvc_export_state.argtypes = [vp, ctypes.c_int, ctypes.POINTER(SessionInfo), p_i32, p_i32,
@@ -243,6 +249,17 @@ class KVCache:
         if rc:
             _check(rc)
 
+    def attn_prompt_raw(self, layer, q_ptr, out_ptr, stream) -> None:
+        rc = self.lib.kvc_attn_prompt(self.ctx, layer, q_ptr, out_ptr, stream)
+        if rc:
+            _check(rc)
+
+    def attn_weights_raw(self, layer, q_ptr, weights_ptr, work_ptr, work_bytes, stream) -> None:
+        rc = self.lib.kvc_attn_weights(self.ctx, layer, q_ptr, weights_ptr, work_ptr, work_bytes,
+                                       stream)
+        if rc:
+            _check(rc)
+
     # -- hot path -------------------------------------------------------------------
     def append_chunk(self, sessions, cu_tokens, types, k, v, stream=None) -> None:
         s, cu = _i32(sessions), _i32(cu_tokens)
@@ -273,6 +290,63 @@ class KVCache:
     def attn_decode(self, layer: int, q, out, stream=None) -> None:
         _check(self.lib.kvc_attn_decode(self.ctx, layer, q.data_ptr(), out.data_ptr(),
                                         _stream(stream)))
+
+    def attn_prompt(self, layer: int, q, out, stream=None) -> None:
+        """Attention of the last append's queries, chunks of any length."""
+        _check(self.lib.kvc_attn_prompt(self.ctx, layer, q.data_ptr(), out.data_ptr(),
+                                        _stream(stream)))
+
+    # -- attention weights and eviction by them --------------------------------------
+    def make_weights(self):
+        """Zeros [n_sessions][max_positions]: what each position of each session weighs so far."""
+        import torch
+        return torch.zeros((self.cfg.n_sessions, self.cfg.max_positions), dtype=torch.float32,
+                           device=self.pool.device)
+
+    def make_weights_workspace(self):
+        """Scratch for attn_weights; one for each set of calls that are not ordered."""
+        import torch
+        out = ctypes.c_size_t()
+        _check(self.lib.kvc_weights_workspace(ctypes.byref(self.cfg), ctypes.byref(out)))
+        return torch.empty(out.value, dtype=torch.uint8, device=self.pool.device)
+
+    def _check_by_position(self, name, x, rows, dtype) -> None:
+        shape = (rows, self.cfg.max_positions)
+        if (x.shape != shape or x.dtype != dtype or not x.is_contiguous()
+                or x.device != self.pool.device):
+            raise ValueError(f"{name} must be contiguous {dtype} of shape {shape} on "
+                             f"{self.pool.device}")
+
+    def attn_weights(self, layer: int, q, weights, work, stream=None) -> None:
+        """Adds to `weights` (make_weights) what each resident position draws from the last append's
+        queries in one layer; `work`: make_weights_workspace."""
+        import torch
+        self._check_by_position("weights", weights, self.cfg.n_sessions, torch.float32)
+        _check(self.lib.kvc_attn_weights(self.ctx, layer, q.data_ptr(), weights.data_ptr(),
+                                         work.data_ptr(), work.numel() * work.element_size(),
+                                         _stream(stream)))
+
+    def evict_weighted(self, sessions, keep, weights, *, kinds: int = 0xF, sink: int = 0,
+                       recent: int = 0, resident_out=None, kept=None, stream=None) -> None:
+        """Drops each session's lightest positions (of the types in the bit mask `kinds`, outside the
+        first `sink` and the last `recent` positions) until keep[i] are left.  kept (optional): bool
+        [len(sessions)][max_positions], set where a position stays."""
+        import torch
+        s, k = _i32(sessions), _i32(keep)
+        if len(k) != len(s):
+            raise ValueError("keep needs an entry per session")
+        self._check_by_position("weights", weights, self.cfg.n_sessions, torch.float32)
+        if kept is not None:
+            self._check_by_position("kept", kept, len(s), torch.bool)
+        if resident_out is not None and (
+                resident_out.dtype != torch.int64 or not resident_out.is_contiguous()
+                or resident_out.numel() < len(s) or resident_out.device != self.pool.device):
+            raise ValueError(f"resident_out must be contiguous torch.int64 on {self.pool.device}, an "
+                             f"entry per session")
+        _check(self.lib.kvc_evict_weighted(
+            self.ctx, len(s), s.ctypes.data, k.ctypes.data, weights.data_ptr(), kinds, sink, recent,
+            None if resident_out is None else resident_out.data_ptr(),
+            None if kept is None else kept.data_ptr(), _stream(stream)))
 
     def read_kv(self, sessions, first, cu_rows, layer0: int = 0, n_layers: int | None = None,
                 k=None, v=None, resident_out=None, stream=None):

@@ -63,7 +63,7 @@ Sizes derive_sizes(const kvc_config& c) {
 }
 
 // Lay out the metadata workspace; with base == nullptr only the size is computed.
-size_t layout_meta(const kvc_config& c, uint8_t* base, Dev* d) {
+size_t layout_meta(const kvc_config& c, uint8_t* base, Dev* d, WeighDev* w) {
   const Sizes z = derive_sizes(c);
   const int G = c.q_heads / c.kv_heads;
   size_t off = 0;
@@ -97,6 +97,11 @@ size_t layout_meta(const kvc_config& c, uint8_t* base, Dev* d) {
   uint8_t* ppm = take((size_t)z.pf_slots * PF_MAX_TOKENS * G * sizeof(float2));
   uint8_t* dc = take((size_t)c.max_seq_per_call * c.kv_heads * 4);
   uint8_t* pc = take((size_t)c.max_seq_per_call * c.kv_heads * 4);
+  // A session's positions fill two page lists at most, all sessions' together the pool.
+  const int64_t listed = std::min<int64_t>(2LL * c.max_seq_per_call * c.max_pages_per_session, c.n_pages);
+  uint8_t* wp = take((size_t)c.max_seq_per_call * sizeof(WeighPlan));
+  uint8_t* wl = take((size_t)listed * PS * sizeof(uint2));
+  uint8_t* wc = take(4);
   off = align_up(off, 256);
   if (d) {
     d->sess = reinterpret_cast<SessState*>(sess);
@@ -121,6 +126,9 @@ size_t layout_meta(const kvc_config& c, uint8_t* base, Dev* d) {
     d->pf_part_ml = reinterpret_cast<float2*>(ppm);
     d->dec_count = reinterpret_cast<int32_t*>(dc);
     d->pf_count = reinterpret_cast<int32_t*>(pc);
+    w->plan = reinterpret_cast<WeighPlan*>(wp);
+    w->list = reinterpret_cast<uint2*>(wl);
+    w->count = reinterpret_cast<int32_t*>(wc);
     d->max_moves = z.max_moves;
     d->max_alloc = z.max_alloc;
     d->dec_slots = z.dec_slots;
@@ -172,6 +180,7 @@ int check_config(const kvc_config* c) {
 struct kvc_ctx {
   kvc_config cfg;
   Dev d;
+  WeighDev weigh = {};
   bool kv4 = false;  // rows held in 4 bits
   // Host mirrors.
   std::vector<int32_t> tail_mod;  // (live_head + n_live) % PS, exact
@@ -337,7 +346,7 @@ int kvc_query_sizes(const kvc_config* cfg, size_t* pool_bytes, size_t* meta_byte
                   (holds_4_bits(*cfg)
                        ? kv4::page_bytes(cfg->head_dim, cfg->layers, cfg->kv_heads)
                        : (size_t)cfg->layers * 2 * cfg->kv_heads * PS * cfg->head_dim * esz);
-  if (meta_bytes) *meta_bytes = layout_meta(*cfg, nullptr, nullptr);
+  if (meta_bytes) *meta_bytes = layout_meta(*cfg, nullptr, nullptr, nullptr);
   return KVC_OK;
 }
 
@@ -381,7 +390,7 @@ int kvc_create(kvc_ctx** out, const kvc_config* cfg, void* d_pool, size_t pool_b
   d.recent = cfg->recent;
   d.n_pages = cfg->n_pages;
   d.pool = static_cast<uint8_t*>(d_pool);
-  layout_meta(*cfg, static_cast<uint8_t*>(d_meta), &d);
+  layout_meta(*cfg, static_cast<uint8_t*>(d_meta), &d, &ctx->weigh);
   ctx->tail_mod.assign(cfg->n_sessions, 0);
   ctx->pos_next.assign(cfg->n_sessions, 0);
   ctx->resident.assign(cfg->n_sessions, ResidentEstimate());
@@ -399,7 +408,8 @@ int kvc_create(kvc_ctx** out, const kvc_config* cfg, void* d_pool, size_t pool_b
       launch_init(d, cfg->rope_base, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess)
     return cleanup(fail(KVC_ECUDA, "initialisation failed: %s",
                         cudaGetErrorString(cudaGetLastError())));
-  const cudaError_t le = query_limits(d, ctx->kv4, &ctx->lim);
+  cudaError_t le = query_limits(d, ctx->kv4, &ctx->lim);
+  if (le == cudaSuccess && !ctx->kv4) le = prompt_attributes(d);
   if (le != cudaSuccess)
     return cleanup(fail(KVC_ECUDA, "device query failed: %s", cudaGetErrorString(le)));
   *out = ctx;
@@ -519,6 +529,39 @@ int kvc_evict(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, int64_t* d_res
   KVC_CUDA(launch_evict(ctx->d, ctx->kv4, a, d_resident_out, ctx->h_readback, ctx->lim.sms, s));
   ctx->launches += 2;  // plan and copy
   for (int i = 0; i < n_seq; ++i) ctx->resident[h_sessions[i]].evict(ctx->cfg);
+  ctx->used_ub += n_seq;  // an evict adds at most one page per session, net
+  ctx->delta_since_readback += n_seq;
+  enqueue_readback(ctx, s);
+  ctx->attn_valid = false;
+  return KVC_OK;
+}
+
+int kvc_evict_weighted(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, const int32_t* h_keep,
+                       const float* d_weights, int kinds, int sink, int recent,
+                       int64_t* d_resident_out, uint8_t* d_kept, void* stream) {
+  g_err.clear();
+  if (!ctx) return fail(KVC_EINVAL, "ctx is NULL");
+  int rc = check_sessions(ctx, n_seq, h_sessions);
+  if (rc) return rc;
+  if (!h_keep || !d_weights) return fail(KVC_EINVAL, "h_keep / d_weights is NULL");
+  if (reinterpret_cast<uintptr_t>(d_weights) & 3)
+    return fail(KVC_EINVAL, "d_weights must be 4-byte aligned");
+  if (kinds < 0 || kinds > 15) return fail(KVC_EINVAL, "kinds must be in 0..15 (a bit for each type)");
+  if (sink < 0 || recent < 0) return fail(KVC_EINVAL, "sink and recent must be >= 0");
+  WeighArgs a;
+  a.n_seq = n_seq;
+  a.kinds = kinds;
+  a.sink = sink;
+  a.recent = recent;
+  for (int i = 0; i < n_seq; ++i) {
+    if (h_keep[i] < 0) return fail(KVC_EINVAL, "h_keep[%d] = %d is negative", i, h_keep[i]);
+    a.sessions[i] = h_sessions[i];
+    a.keep[i] = h_keep[i];
+  }
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  KVC_CUDA(launch_evict_weighted(ctx->d, ctx->weigh, ctx->kv4, a, d_weights, d_resident_out, d_kept,
+                                 ctx->h_readback, s, &ctx->launches));
+  for (int i = 0; i < n_seq; ++i) ctx->resident[h_sessions[i]].thin(h_keep[i]);
   ctx->used_ub += n_seq;  // an evict adds at most one page per session, net
   ctx->delta_since_readback += n_seq;
   enqueue_readback(ctx, s);
@@ -677,6 +720,50 @@ int kvc_attn_prefill_chunk_kv(kvc_ctx* ctx, int layer, const void* d_k, const vo
     ++ctx->launches;
     ctx->order.launched(layer, false);
   }
+  return KVC_OK;
+}
+
+int kvc_attn_prompt(kvc_ctx* ctx, int layer, const void* d_q, void* d_out, void* stream) {
+  g_err.clear();
+  int rc = check_attn(ctx, layer, d_q, d_out);
+  if (rc) return rc;
+  if (ctx->last_single) return kvc_attn_decode(ctx, layer, d_q, d_out, stream);
+  if (ctx->last_max_t <= PF_MAX_TOKENS) return kvc_attn_prefill_chunk(ctx, layer, d_q, d_out, stream);
+  if (ctx->kv4)
+    return fail(KVC_EINVAL, "chunks of more than %d tokens over rows held in 4 bits (KVC_KV4)",
+                PF_MAX_TOKENS);
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  bool capturing = false;
+  KVC_CUDA(is_capturing(s, &capturing));
+  const PageHint pages = page_hint(ctx, capturing);
+  KVC_CUDA(launch_attn_prompt(ctx->d, ctx->lim, layer, d_q, d_out, ctx->last_n_seq, ctx->last_max_t,
+                              pages.max, pages.sum, &ctx->order, s, &ctx->launches));
+  return KVC_OK;
+}
+
+int kvc_weights_workspace(const kvc_config* cfg, size_t* bytes) {
+  g_err.clear();
+  int rc = check_config(cfg);
+  if (rc) return rc;
+  if (!bytes) return fail(KVC_EINVAL, "bytes is NULL");
+  *bytes = weights_work_bytes(*cfg);
+  return KVC_OK;
+}
+
+int kvc_attn_weights(kvc_ctx* ctx, int layer, const void* d_q, float* d_weights, void* d_work,
+                     size_t work_bytes, void* stream) {
+  g_err.clear();
+  int rc = check_attn(ctx, layer, d_q, d_weights);
+  if (rc) return rc;
+  if (ctx->kv4)
+    return fail(KVC_EINVAL, "kvc_attn_weights does not take rows held in 4 bits (KVC_KV4)");
+  if (!d_work || (reinterpret_cast<uintptr_t>(d_work) & 255))
+    return fail(KVC_EINVAL, "d_work must be a 256-byte aligned device pointer");
+  const size_t need = weights_work_bytes(ctx->cfg);
+  if (work_bytes < need) return fail(KVC_EINVAL, "work_bytes %zu < required %zu", work_bytes, need);
+  KVC_CUDA(launch_attn_weights(ctx->d, ctx->lim, layer, d_q, d_weights, d_work, ctx->last_n_seq,
+                               ctx->last_total, ctx->last_max_t, &ctx->order,
+                               static_cast<cudaStream_t>(stream), &ctx->launches));
   return KVC_OK;
 }
 

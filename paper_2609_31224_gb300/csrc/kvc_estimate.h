@@ -24,6 +24,8 @@ class ResidentEstimate {
     resident_ += tokens;
   }
   void evict(const kvc_config& c) { resident_ = std::min(resident_, kept(c, fed_)); }
+  // An eviction that drops positions by other rules until `keep` are left.
+  void thin(int64_t keep) { resident_ = std::min(resident_, keep); }
   void release() { fed_ = resident_ = 0; }
 
   // Positions that an eviction leaves of a session of `fed`, as far as it has as many.

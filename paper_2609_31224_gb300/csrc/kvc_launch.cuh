@@ -42,6 +42,43 @@ struct ReadArgsT {
 };
 using ReadArgs = ReadArgsT<MAX_SEQ>;
 
+// Sessions to evict by weight, and what is left of each.
+template <int N>
+struct WeighArgsT {
+  int32_t n_seq;
+  int32_t kinds, sink, recent;
+  int32_t sessions[N];
+  int32_t keep[N];
+};
+using WeighArgs = WeighArgsT<MAX_SEQ>;
+
+// What an eviction by weight does to one session of the call (kvc_evict_weighted.cu).
+struct WeighPlan {
+  int64_t list_at;     // its entries in the list
+  uint32_t key;        // positions of smaller keys go, and of equal ones
+  int32_t tie_last;    // those up to this retained index
+  int32_t drop;        // positions that go
+  int32_t first;       // retained index of the first of them
+  int32_t end;         // live positions consumed
+  int32_t stay;        // compacted positions afterwards
+  int32_t pages;       // and their pages
+  int32_t taken;       // of them live pages taken over
+  int32_t extra;       // 1: the last one is new
+  int32_t extra_page;
+  int32_t freed;       // consumed or compacted pages that are free again
+  int32_t moves;       // rows that move
+  int32_t ok;          // 0: the call failed, nothing changes
+  int32_t pad;
+};
+static_assert(sizeof(WeighPlan) == 64, "WeighPlan size");
+
+// Its part of the metadata workspace.
+struct WeighDev {
+  WeighPlan* plan;     // [max_seq]
+  uint2* list;         // [positions of max_seq sessions] (key, slot), then moves (from, to)
+  int32_t* count;      // arrival counter
+};
+
 // What the device runs at once, for each kernel whose launch shape follows from it.  kvc_create
 // looks it up for the current CUDA context; the first time for a context, element type and way of
 // holding the rows that also sets the attributes of the kernels over them, which belong to the CUDA
@@ -77,6 +114,9 @@ cudaError_t launch_append_layers(const Dev& d, int total, int layer0, int n_laye
                                  const void* v, bool after_plan, cudaStream_t s);
 cudaError_t launch_evict(const Dev& d, bool kv4, const SeqArgs& a, int64_t* resident_out,
                          int64_t* used_out, int sms, cudaStream_t s);
+cudaError_t launch_evict_weighted(const Dev& d, const WeighDev& wd, bool kv4, const WeighArgs& a,
+                                  const float* weights, int64_t* resident_out, uint8_t* kept,
+                                  int64_t* used_out, cudaStream_t s, int64_t* launches);
 cudaError_t launch_release(const Dev& d, const SeqArgs& a, int64_t* used_out, cudaStream_t s);
 cudaError_t launch_transcript(const Dev& d, bool kv4, int session, int cap, int32_t* pos_out,
                               void* k_out, void* v_out, int32_t* count, cudaStream_t s);
@@ -165,6 +205,19 @@ cudaError_t launch_attn_prefill_f32(const Dev& d, const Limits& lim, int layer, 
 // 64-127), 16-row boxes, 128-byte swizzle; cached per pool.  False if the driver
 // entry point is missing or the encoding fails.
 bool pool_tensor_maps(const Dev& d, CUtensorMap* lo, CUtensorMap* hi);
+// Whole prompts (kvc_prompt.cu): chunks of any length, rows in the element type.
+cudaError_t launch_attn_prompt(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
+                               int n_seq, int max_t, int pages_max, int64_t pages_sum,
+                               LaunchOrder* order, cudaStream_t s, int64_t* launches);
+// Attention weights of the last append's queries, added to weights (kvc_weights.cu).  work: bytes as
+// weights_work_bytes says.
+size_t weights_work_bytes(const kvc_config& c);
+// Attributes of the kernels of both, in the current CUDA context.
+cudaError_t prompt_attributes(const Dev& d);
+cudaError_t weights_attributes(const Dev& d);
+cudaError_t launch_attn_weights(const Dev& d, const Limits& lim, int layer, const void* q,
+                                float* weights, void* work, int n_seq, int total, int max_t,
+                                LaunchOrder* order, cudaStream_t s, int64_t* launches);
 int noalloc_max_pairs();
 cudaError_t launch_attn_decode_noalloc(const Dev& d, int layer, const void* q, void* out,
                                        int n_seq, cudaStream_t s);
