@@ -4,6 +4,7 @@
 // One pass over the keys with a running maximum and sum a row, in binary32.
 #include <cmath>
 
+#include "kvc_prompt.h"
 #include "kvc_prompt_tile.cuh"
 
 namespace kvc {
@@ -144,7 +145,7 @@ cudaError_t attributes() {
 }  // namespace
 
 cudaError_t prompt_attributes(const Dev& d) {
-  const cudaError_t e = d.esz == 2 ? attributes<__nv_bfloat16, 128>() : attributes<float, 64>();
+  const cudaError_t e = d.esz == 2 ? prompt_tc_attributes() : attributes<float, 64>();
   return e != cudaSuccess ? e : weights_attributes(d);
 }
 
@@ -152,7 +153,7 @@ cudaError_t launch_attn_prompt(const Dev& d, const Limits& lim, int layer, const
                                int n_seq, int max_t, int pages_max, int64_t pages_sum,
                                LaunchOrder* order, cudaStream_t s, int64_t* launches) {
   // (The kernel waits for the one before it before it lets the next one start.)
-  const cudaError_t e = d.esz == 2 ? launch<__nv_bfloat16, 128>(d, lim, layer, q, out, s)
+  const cudaError_t e = d.esz == 2 ? launch_prompt_tc(d, lim, layer, q, out, s)
                                    : launch<float, 64>(d, lim, layer, q, out, s);
   *launches += e == cudaSuccess;
   order->launched(layer, false);

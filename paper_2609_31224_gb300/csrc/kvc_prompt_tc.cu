@@ -1,0 +1,676 @@
+// Attention over whole prompts on the 5th-generation tensor cores (tcgen05 + TMEM): bfloat16 K, V and
+// q, binary32 softmax and accumulation.
+//
+// An item is 64 tokens of one session and KV head: two tiles A and B of 32 tokens x G = 4 query heads =
+// 128 rows each, against the session's pages up to the last one that its last token sees, 128 keys (8
+// pages) a step.  Items go to the CTAs (one per SM) from a counter, a session's last tokens, which see
+// most, first.  A step has four products of 128^3: S_A, S_B (Q K^T) and O_A, O_B += P V; while the
+// softmax of one tile runs, the tensor cores have the other tile's.
+// Warp roles (512 threads):
+//   warp 0      items from the counter; K and V by TMA (128-byte swizzle, a box of 16 rows x 64 columns a
+//               lane) into a ring of five 32 KiB stages, K and V in turn
+//   warp 1      one thread issues the products
+//   warps 4-7   query rows, rotated, scaled and rounded, into shared memory, the next item's as soon as
+//               this one's last score product of the tile is complete; V rows that have to be zero (below)
+//   warps 8-15  softmax, four warps a tile: a thread has one row of S, from tensor memory to registers in
+//               one go, and writes P over it; O is rescaled in tensor memory when the row's maximum has
+//               grown by more than 2^8
+// Tensor memory: S_A, S_B (P over the first half of each), O_A, O_B, 128 columns each: all 512.
+//
+// A key that no row of a product may see has P = 0, but 0 times a value that is not finite is not 0.  So
+// the V rows of slots that hold no resident position are zeroed in shared memory, and those of the
+// chunk's own tokens that some rows of the item see and others do not, where they are not finite: the
+// rows that do see such a one add it by themselves at the end (add_odd_values).
+//
+// All waits are bounded; a timeout records KVC_DERR_WAIT and the CTA stops.
+#include <cuda.h>
+
+#include <cmath>
+
+#include "kvc_prefill_tc.cuh"
+#include "kvc_prompt.h"
+
+namespace kvc {
+
+namespace {
+
+constexpr int KEYS = 128, PAGES = KEYS / PS;       // of a step
+constexpr int TOKENS = 32;                         // of a tile
+constexpr int PANEL = KEYS * 128;                  // 128 rows x 64 columns
+constexpr int SLOT = 2 * PANEL;                    // a K or V stage, or a query tile
+constexpr int RING = 5;
+constexpr int EDGES = 4;
+constexpr int TC_THREADS = 512;
+constexpr int S_COL = 0, O_COL = 256, ALL_COLS = 512;
+constexpr int FEW_REGS = 96, MANY_REGS = 160;      // 256 threads each: what 128 a thread make together
+
+enum {
+  B_FULL = 0,                    // [RING] a stage has landed
+  B_EMPTY = B_FULL + RING,       // [RING] and was read
+  B_Q_FULL = B_EMPTY + RING,     // [2] a tile's query rows are there
+  B_Q_EMPTY = B_Q_FULL + 2,      // [2] and its last scores of the item complete
+  B_S = B_Q_EMPTY + 2,           // [2] scores complete (and every product before them)
+  B_P = B_S + 2,                 // [2] P written, O rescaled
+  B_O = B_P + 2,                 // [2] the item's output complete
+  B_O_EMPTY = B_O + 2,           // [2] and read
+  // V stages of edge steps land here instead (their B_FULL phase completes at once), and have their
+  // rows zeroed: the e-th such stage of the CTA, at e % EDGES.  A ring holds fewer.
+  B_EDGE = B_O_EMPTY + 2,        // [EDGES]
+  B_FIX = B_EDGE + EDGES,        // [EDGES]
+  B_ITEM = B_FIX + EDGES,        // [2] an item is known
+  B_ITEM_EMPTY = B_ITEM + 2,     // [2] and every warp is through with it
+  B_FINAL = B_ITEM_EMPTY + 2,    // every product of the CTA complete
+  N_BARS = B_FINAL + 1
+};
+constexpr int ITEM_READERS = 1 + 4 + 8;            // warps that arrive at B_ITEM_EMPTY
+
+// What every role knows of an item.
+struct Item {
+  SeqInfo si;
+  int32_t seq, head, t0, steps;  // steps = 0: no more items
+  int32_t odd;                   // some V row was zeroed because it is not finite
+  int32_t pad[11];
+};
+static_assert(sizeof(Item) == 128, "Item size");
+
+constexpr int OFF_BARS = 0;
+constexpr int OFF_ITEM = 512;                      // [2]
+constexpr int OFF_TMEM = OFF_ITEM + 2 * 128;
+constexpr int OFF_STOP = OFF_TMEM + 4;
+constexpr int OFF_FIRST = OFF_STOP + 4;            // [MAX_SEQ + 1] first item of each session
+constexpr int OFF_TILES = 3072;                    // query tiles A, B, then the ring
+constexpr int SMEM_BYTES = OFF_TILES + (2 + RING) * SLOT;
+static_assert(N_BARS * 8 <= OFF_ITEM && OFF_FIRST + (MAX_SEQ + 1) * 4 <= OFF_TILES, "header fits");
+static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of a CTA");
+
+__device__ inline void tc_mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                 uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ inline void tma_load_2d(void* dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_u32(bar))
+      : "memory");
+}
+template <int N>
+__device__ inline void give_registers() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ inline void take_registers() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+// Bounded wait that also ends when another warp has given up.
+__device__ inline bool wait_or_stop(const Dev& d, uint64_t* bar, uint32_t parity, volatile int* stop) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity)) {
+    if (*stop) return false;
+    if (clock64() - t0 > WAIT_LIMIT_CYCLES) {
+      set_error(d, KVC_DERR_WAIT);
+      *stop = 1;
+      return false;
+    }
+  }
+  return true;
+}
+
+// Blocks that the tokens up to `tok` of the chunk see.
+__device__ inline int blocks_seen(const SeqInfo& si, int tok) {
+  return si.n_hist_pages + (si.live_head + si.n_live - si.t + tok) / PS + 1;
+}
+
+// Whether a step (blocks [b0, b0 + PAGES)) has slots that some row of the item starting at token t0 does
+// not see: a partly filled page, pages past the end, keys behind the item's first token.
+__device__ inline bool is_edge(const SeqInfo& si, int t0, int b0) {
+  const int nhp = si.n_hist_pages;
+  const int first = nhp + (si.live_head + si.n_live - si.t + t0) / PS;  // block of the first token
+  if (b0 + PAGES > first) return true;
+  const int b_hist = (si.n_hist % PS) ? nhp - 1 : -1, b_live = si.live_head ? nhp : -1;
+  return (b_hist >= b0 && b_hist < b0 + PAGES) || (b_live >= b0 && b_live < b0 + PAGES);
+}
+
+// Slots [lo, hi) of block b that hold a position with index <= q_log.
+__device__ inline uint32_t slots_seen(const SeqInfo& si, int b, int n_blocks, int q_log) {
+  if (b >= n_blocks) return 0;
+  const BlockRange br = block_range(si, b);
+  const int hi = min(br.hi, q_log - br.base + 1);
+  return hi <= br.lo ? 0u : ((1u << hi) - 1u) & ~((1u << br.lo) - 1u);
+}
+
+__device__ inline bool not_finite(uint32_t two) {
+  return (two & 0x7F80u) == 0x7F80u || (two & 0x7F800000u) == 0x7F800000u;
+}
+
+// What a row draws of the V rows that were zeroed because they are not finite (rare: slow and
+// simple), dims [c0, c0 + 32), unnormalised.  Keys behind the item's first token up to the row's own.
+__device__ __noinline__ void odd_value(const Dev& d, const SeqInfo& si, int layer, int head, int t0, int tok,
+                                       int g, const __nv_bfloat16* q, float qk_scale, float m, int c0,
+                                       float* o) {
+  const int32_t* hrow = d.hist_pt + (size_t)si.sid * d.max_pages_per_session;
+  const int32_t* lrow = d.live_pt + (size_t)si.sid * d.max_pages_per_session;
+  const __nv_bfloat16* pool = reinterpret_cast<const __nv_bfloat16*>(d.pool);
+  const __nv_bfloat16* row = q + ((size_t)(si.q_row0 + tok) * d.q_heads + head * G + g) * D;
+  const float2* cs = d.rope + (size_t)(si.pos_first + tok) * (D / 2);
+  for (int i = 0; i < 32; ++i) o[i] = 0.f;
+  for (int key = t0 + 1; key <= tok; ++key) {
+    const int slot = si.live_head + si.n_live - si.t + key;
+    const int page = block_page(si, hrow, lrow, si.n_hist_pages + slot / PS);
+    const __nv_bfloat16* v = pool + pool_offset_elems(d, page, layer, 1, head, slot % PS);
+    bool odd = false;
+    for (int i = 0; i < D / 2; ++i) odd |= not_finite(reinterpret_cast<const uint32_t*>(v)[i]);
+    if (!odd) continue;
+    const __nv_bfloat16* k = pool + pool_offset_elems(d, page, layer, 0, head, slot % PS);
+    float s = 0.f;
+    for (int i = 0; i < D / 2; ++i) {
+      float a, b;
+      rope_pair(__bfloat162float(row[i]), __bfloat162float(row[i + D / 2]), cs[i], a, b);
+      s = fmaf(__bfloat162float(__float2bfloat16_rn(a * qk_scale)), __bfloat162float(k[i]), s);
+      s = fmaf(__bfloat162float(__float2bfloat16_rn(b * qk_scale)), __bfloat162float(k[i + D / 2]), s);
+    }
+    const float p = __bfloat162float(__float2bfloat16_rn(exp2f(s - m)));
+    for (int i = 0; i < 32; ++i) o[i] = fmaf(p, __bfloat162float(v[c0 + i]), o[i]);
+  }
+}
+
+__global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
+    Dev d, int layer, const __grid_constant__ CUtensorMap map_lo,
+    const __grid_constant__ CUtensorMap map_hi, const __nv_bfloat16* __restrict__ q,
+    __nv_bfloat16* __restrict__ out, float qk_scale) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + OFF_BARS);
+  Item* items = reinterpret_cast<Item*>(smem + OFF_ITEM);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + OFF_TMEM);
+  int* s_first = reinterpret_cast<int*>(smem + OFF_FIRST);
+  volatile int* stop = reinterpret_cast<int*>(smem + OFF_STOP);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int H = d.kv_heads, L = d.layers;
+  uint8_t* s_q = smem + OFF_TILES;
+  uint8_t* s_ring = s_q + 2 * SLOT;
+  pdl_wait();
+  pdl_launch_dependents();
+  const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;  // (no units: the append failed)
+  if (tid == 0) {
+    for (int i = 0; i < N_BARS; ++i) {
+      const int count = i >= B_Q_FULL && i < B_Q_EMPTY ? 4
+                        : i >= B_P && i < B_O          ? 4
+                        : i >= B_O_EMPTY && i < B_EDGE ? 4
+                        : i >= B_FIX && i < B_ITEM     ? 4
+                        : i >= B_ITEM_EMPTY && i < B_FINAL ? ITEM_READERS
+                                                           : 1;
+      mbar_init(&bars[i], count);
+    }
+    fence_mbar_init();
+    *stop = 0;
+  }
+  // First item of each session: 64-token tiles of its chunk, for each KV head (one warp).
+  if (warp == 2) {
+    int sum = 0;
+    for (int i0 = 0; i0 < n_seq; i0 += 32) {
+      const int i = i0 + lane;
+      const int n = i < n_seq ? (d.seq[i].t + 2 * TOKENS - 1) / (2 * TOKENS) * H : 0;
+      int x = n;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(FULL, x, o);
+        if (lane >= o) x += y;
+      }
+      if (i < n_seq) s_first[i] = sum + x - n;
+      sum += __shfl_sync(FULL, x, 31);
+    }
+    if (lane == 0) s_first[n_seq] = sum;
+  }
+  __syncwarp();
+  if (warp == 1) tmem_alloc(tmem_slot, ALL_COLS);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp < 4) {
+  give_registers<FEW_REGS>();
+  if (warp == 0) {
+    // ---------------- items, K and V ----------------
+    const int total = s_first[n_seq];
+    const int pg = lane >> 1 & 7;
+    const CUtensorMap* map = (lane & 1) ? &map_hi : &map_lo;
+    uint32_t seq_no = 0, edges = 0;  // stages so far, and V stages of edge steps
+    bool ok = true;
+    for (int n = 0; ok; ++n) {
+      Item* it = items + (n & 1);
+      if (n >= 2) ok = __all_sync(FULL, wait_or_stop(d, &bars[B_ITEM_EMPTY + (n & 1)], ((n >> 1) & 1) ^ 1, stop));
+      if (!ok) break;
+      int at = 0;
+      if (lane == 0) at = atomicAdd(&d.pf_count[0], 1);
+      at = __shfl_sync(FULL, at, 0);
+      if (at >= total) {
+        if (lane == 0) {
+          it->steps = 0;
+          mbar_arrive(&bars[B_ITEM + (n & 1)]);
+        }
+        break;
+      }
+      int lo = 0, hi = n_seq - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (s_first[mid] <= at) lo = mid;
+        else hi = mid - 1;
+      }
+      const int seq = lo, in = at - s_first[seq];
+      if (lane < 16)
+        reinterpret_cast<int*>(&it->si)[lane] = reinterpret_cast<const int*>(d.seq + seq)[lane];
+      __syncwarp();
+      const SeqInfo& si = it->si;
+      const int n_t = (si.t + 2 * TOKENS - 1) / (2 * TOKENS), head = in % H;
+      const int t0 = (n_t - 1 - in / H) * 2 * TOKENS;
+      const int nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1), steps = (nb + PAGES - 1) / PAGES;
+      if (lane == 0) {
+        it->seq = seq;
+        it->head = head;
+        it->t0 = t0;
+        it->steps = steps;
+        it->odd = 0;
+        mbar_arrive(&bars[B_ITEM + (n & 1)]);
+      }
+      const int32_t* hrow = d.hist_pt + (size_t)si.sid * d.max_pages_per_session;
+      const int32_t* lrow = d.live_pt + (size_t)si.sid * d.max_pages_per_session;
+      auto page_at = [&](int b) { return b < nb ? block_page(si, hrow, lrow, b) : 0; };
+      int pid = page_at(lane), pid_next = page_at(32 + lane);
+      for (int j = 0; j < steps && ok; ++j) {
+        if (j > 0 && (j & 3) == 0) {
+          pid = pid_next;
+          pid_next = page_at(PAGES * j + 32 + lane);
+        }
+        const int page = __shfl_sync(FULL, pid, PAGES * (j & 3) + pg);
+        const int n_pg = min(PAGES, nb - PAGES * j);
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv, ++seq_no) {
+          const int st = seq_no % RING;
+          if (seq_no >= RING) {
+            ok = __all_sync(FULL, wait_or_stop(d, &bars[B_EMPTY + st], ((seq_no / RING) & 1) ^ 1, stop));
+            if (!ok) break;
+          }
+          uint64_t* bar = &bars[B_FULL + st];
+          if (kv == 1 && is_edge(si, t0, PAGES * j)) {
+            if (lane == 0) mbar_arrive(bar);
+            bar = &bars[B_EDGE + edges % EDGES];
+            ++edges;
+          }
+          if (lane == 0) mbar_arrive_expect_tx(bar, n_pg * PS * D * 2);
+          __syncwarp();
+          if (lane < 16 && pg < n_pg)
+            tma_load_2d(s_ring + st * SLOT + (lane & 1) * PANEL + pg * 2048, map, 0,
+                        (((page * L + layer) * 2 + kv) * H + head) * PS, bar);
+        }
+      }
+    }
+    // Copies still in flight land before the CTA ends.
+    for (uint32_t s = seq_no > RING ? seq_no - RING : 0; s < seq_no; ++s)
+      mbar_wait(d, &bars[B_FULL + s % RING], (s / RING) & 1);
+    for (uint32_t e = edges > EDGES ? edges - EDGES : 0; e < edges; ++e)
+      mbar_wait(d, &bars[B_EDGE + e % EDGES], (e / EDGES) & 1);
+  } else if (warp == 1) {
+    // ---------------- products ----------------
+    if (lane == 0) {
+      constexpr uint32_t ID_S = instr_desc(KEYS, M, false), ID_O = instr_desc(D, M, true);
+      const uint32_t a_q = smem_u32(s_q), a_ring = smem_u32(s_ring);
+      bool ok = true;
+      auto wait = [&](int bar, uint32_t parity) {
+        ok = ok && wait_or_stop(d, &bars[bar], parity, stop);
+        return ok;
+      };
+      // S_x = Q_x K^T of stage `s` (a count of stages).
+      auto scores = [&](int x, uint32_t s) {
+        const uint64_t qd = smem_desc(a_q + x * SLOT, 0, 1024);
+        const uint64_t kd = smem_desc(a_ring + (s % RING) * SLOT, 0, 1024);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+          const uint32_t at = (kk >> 2) * PANEL + (kk & 3) * 32;
+          tc_mma_ss(tmem + S_COL + x * KEYS, desc_at(qd, at), desc_at(kd, at), ID_S, kk > 0);
+        }
+        tc_commit(&bars[B_S + x]);
+      };
+      auto outputs = [&](int x, uint32_t s, bool first) {
+        const uint64_t vd = smem_desc(a_ring + (s % RING) * SLOT, PANEL, 1024);
+#pragma unroll
+        for (int kk = 0; kk < KEYS / 16; ++kk)
+          tc_mma_ts(tmem + O_COL + x * D, tmem + S_COL + x * KEYS + kk * 8, desc_at(vd, kk * 16 * 128),
+                    ID_O, !first || kk > 0);
+      };
+      auto full = [&](uint32_t s) { return wait(B_FULL + s % RING, (s / RING) & 1); };
+      uint32_t s0 = 0;                       // stages before this item
+      uint32_t p_no[2] = {0, 0};             // steps of a tile so far
+      uint32_t q_no[2] = {0, 0};             // items of a tile whose scores have begun
+      uint32_t o_no[2] = {0, 0};             // and whose output has
+      uint32_t edges = 0;
+      // The first scores of item n, tile x: its K is stage s.
+      auto begin = [&](int x, uint32_t s, int steps) {
+        if (!wait(B_Q_FULL + x, q_no[x] & 1) || !full(s)) return;
+        ++q_no[x];
+        tc_fence_after();
+        scores(x, s);
+        if (steps == 1) tc_commit(&bars[B_Q_EMPTY + x]);
+      };
+      int n = 0;
+      if (!wait(B_ITEM, 0)) n = -1;
+      int steps = ok ? items[0].steps : 0;
+      bool two = steps > 0 && items[0].t0 + TOKENS < items[0].si.t;
+      if (steps > 0) {
+        begin(0, 0, steps);
+        if (ok && two) begin(1, 0, steps);
+        tc_commit(&bars[B_EMPTY + 0]);
+      }
+      while (ok && steps > 0) {
+        const Item& it = items[n & 1];
+        const SeqInfo& si = it.si;
+        const int t0 = it.t0;
+        int steps_next = 0;
+        bool two_next = false;
+        for (int j = 0; j < steps && ok; ++j) {
+          const uint32_t sv = s0 + 2 * j + 1, sk = sv + 1;  // V of this step, K of the next one
+          const bool last = j == steps - 1;
+          if (last) {
+            if (!wait(B_ITEM + ((n + 1) & 1), ((n + 1) >> 1) & 1)) break;
+            const Item& nx = items[(n + 1) & 1];
+            steps_next = nx.steps;
+            two_next = steps_next > 0 && nx.t0 + TOKENS < nx.si.t;
+          }
+          if (!full(sv)) break;
+          if (is_edge(si, t0, PAGES * j)) {
+            if (!wait(B_FIX + edges % EDGES, (edges / EDGES) & 1)) break;
+            ++edges;
+          }
+          for (int x = 0; x < 2 && ok; ++x) {
+            if (x == 0 || two) {
+              if (!wait(B_P + x, p_no[x] & 1)) break;
+              ++p_no[x];
+              if (j == 0) {
+                if (o_no[x] > 0 && !wait(B_O_EMPTY + x, (o_no[x] - 1) & 1)) break;
+                ++o_no[x];
+              }
+              tc_fence_after();
+              outputs(x, sv, j == 0);
+              if (last) tc_commit(&bars[B_O + x]);
+            }
+            if (x == (two ? 1 : 0)) tc_commit(&bars[B_EMPTY + sv % RING]);
+            if (!last) {
+              if (x == 0 || two) {
+                if (!full(sk)) break;
+                tc_fence_after();
+                scores(x, sk);
+                if (j + 2 == steps) tc_commit(&bars[B_Q_EMPTY + x]);
+              }
+              if (x == (two ? 1 : 0)) tc_commit(&bars[B_EMPTY + sk % RING]);
+            } else if (steps_next > 0) {
+              if (x == 0 || two_next) begin(x, sk, steps_next);
+              if (x == (two_next ? 1 : 0)) tc_commit(&bars[B_EMPTY + sk % RING]);
+            }
+          }
+        }
+        if (!ok) break;
+        mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
+        s0 += 2 * steps;
+        steps = steps_next;
+        two = two_next;
+        ++n;
+      }
+      // No product may still be running when the tensor memory is released.
+      tc_commit(&bars[B_FINAL]);
+      mbar_wait(d, &bars[B_FINAL], 0);
+    }
+  }
+  } else if (warp < 8) {
+    give_registers<FEW_REGS>();
+    // ---------------- query rows, V rows to zero ----------------
+    const int ts = tid - 4 * 32;
+    bool ok = true;
+    auto wait = [&](int bar, uint32_t parity) {
+      ok = ok && __all_sync(FULL, wait_or_stop(d, &bars[bar], parity, stop));
+      return ok;
+    };
+    uint32_t s0 = 0, edges = 0, q_no[2] = {0, 0};
+    for (int n = 0; ok; ++n) {
+      if (!wait(B_ITEM + (n & 1), (n >> 1) & 1)) break;
+      Item& it = items[n & 1];
+      if (it.steps == 0) break;
+      const SeqInfo& si = it.si;
+      const int head = it.head, t0 = it.t0, steps = it.steps;
+      const int tiles = t0 + TOKENS < si.t ? 2 : 1;
+      // A thread takes 16-byte chunks c and c + 8 (which rotate together) of a token's G rows.
+      const int c = ts & 7;
+      for (int x = 0; x < tiles; ++x) {
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          const int tl = (ts >> 3) + 16 * h, tok = t0 + x * TOKENS + tl;
+          uint4 a[G], b[G];
+          float4 cs[4];
+          const bool in = tok < si.t;
+          if (in) {
+            const uint4* row = reinterpret_cast<const uint4*>(
+                q + ((size_t)(si.q_row0 + tok) * d.q_heads + head * G) * D) + c;
+            const float4* t4 = reinterpret_cast<const float4*>(d.rope + (size_t)(si.pos_first + tok) * (D / 2) + c * 8);
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+              a[g] = row[g * 16];
+              b[g] = row[g * 16 + 8];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) cs[e] = t4[e];
+          }
+          if (h == 0 && q_no[x] > 0 && !wait(B_Q_EMPTY + x, (q_no[x] - 1) & 1)) break;
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            uint32_t ya[4] = {0, 0, 0, 0}, yb[4] = {0, 0, 0, 0};
+            if (in) {
+              const uint32_t ua[4] = {a[g].x, a[g].y, a[g].z, a[g].w};
+              const uint32_t ub[4] = {b[g].x, b[g].y, b[g].z, b[g].w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const float a0 = bf16lo(ua[e]), a1 = bf16hi(ua[e]), b0 = bf16lo(ub[e]), b1 = bf16hi(ub[e]);
+                ya[e] = pack_bf16(fmaf(a0, cs[e].x, -b0 * cs[e].y) * qk_scale,
+                                  fmaf(a1, cs[e].z, -b1 * cs[e].w) * qk_scale);
+                yb[e] = pack_bf16(fmaf(b0, cs[e].x, a0 * cs[e].y) * qk_scale,
+                                  fmaf(b1, cs[e].z, a1 * cs[e].w) * qk_scale);
+              }
+            }
+            const int r = tl * G + g;
+            uint8_t* at = s_q + x * SLOT + r * 128 + ((c ^ (r & 7)) << 4);
+            *reinterpret_cast<uint4*>(at) = make_uint4(ya[0], ya[1], ya[2], ya[3]);
+            *reinterpret_cast<uint4*>(at + PANEL) = make_uint4(yb[0], yb[1], yb[2], yb[3]);
+          }
+        }
+        if (!ok) break;
+        ++q_no[x];
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars[B_Q_FULL + x]);
+      }
+      // Thread ts has row ts of each such step's V.
+      const int nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1);
+      const int q_log0 = si.n_hist + si.n_live - si.t;
+      for (int j = 0; j < steps && ok; ++j) {
+        const int b = PAGES * j + ts / PS;
+        if (!is_edge(si, t0, PAGES * j)) continue;
+        const uint32_t s = s0 + 2 * j + 1;
+        if (!wait(B_EDGE + edges % EDGES, (edges / EDGES) & 1)) break;
+        uint8_t* row = s_ring + (s % RING) * SLOT + ts * 128;
+        const uint32_t bit = 1u << (ts % PS);
+        bool zero = !(slots_seen(si, b, nb, q_log0 + si.t) & bit);
+        if (!zero && !(slots_seen(si, b, nb, q_log0 + t0) & bit)) {  // some rows see it
+          bool odd = false;
+          for (int i = 0; i < 16; ++i) {
+            const uint4 v = *reinterpret_cast<const uint4*>(row + (i >> 3) * PANEL + ((i & 7) ^ (ts & 7)) * 16);
+            odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
+          }
+          if (odd) {
+            it.odd = 1;
+            zero = true;
+          }
+        }
+        if (zero)
+          for (int i = 0; i < 16; ++i)
+            *reinterpret_cast<uint4*>(row + (i >> 3) * PANEL + ((i & 7) ^ (ts & 7)) * 16) = make_uint4(0, 0, 0, 0);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars[B_FIX + edges % EDGES]);
+        ++edges;
+      }
+      s0 += 2 * steps;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
+    }
+  } else {
+    take_registers<MANY_REGS>();
+    // ---------------- softmax ----------------
+    const int x = (warp - 8) >> 2;             // tile
+    const int r = (warp & 3) * 32 + lane;      // row
+    const uint32_t trow = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t t_s = trow + S_COL + x * KEYS, t_o = trow + O_COL + x * D;
+    bool ok = true;
+    auto wait = [&](int bar, uint32_t parity) {
+      ok = ok && __all_sync(FULL, wait_or_stop(d, &bars[bar], parity, stop));
+      return ok;
+    };
+    uint32_t s_no = 0, o_no = 0;
+    for (int n = 0; ok; ++n) {
+      if (!wait(B_ITEM + (n & 1), (n >> 1) & 1)) break;
+      const Item& it = items[n & 1];
+      const int steps = it.steps;
+      if (steps == 0) break;
+      const SeqInfo& si = it.si;
+      const int t0 = it.t0, tok = t0 + x * TOKENS + r / G;
+      if (t0 + x * TOKENS < si.t) {
+        const int nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1);
+        const int q_log = si.n_hist + si.n_live - si.t + tok;
+        float m = -INFINITY, l = 0.f;
+        for (int j = 0; j < steps; ++j, ++s_no) {
+          if (!wait(B_S + x, s_no & 1)) break;
+          tc_fence_after();
+          float s[KEYS];
+          tmem_ld64(t_s, s);
+          tmem_ld64(t_s + 64, s + 64);
+          if (is_edge(si, t0, PAGES * j)) {
+#pragma unroll
+            for (int p = 0; p < PAGES; ++p) {
+              const uint32_t seen = slots_seen(si, PAGES * j + p, nb, q_log);
+#pragma unroll
+              for (int i = 0; i < PS; ++i) s[p * PS + i] = (seen >> i & 1) ? s[p * PS + i] : -INFINITY;
+            }
+          }
+          float m8[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) m8[i] = s[i];
+#pragma unroll
+          for (int i = 8; i < KEYS; i += 16)
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+              m8[c] = i + 8 < KEYS ? fmaxf(fmaxf(m8[c], s[i + c]), s[i + 8 + c]) : fmaxf(m8[c], s[i + c]);
+          const float mx = fmaxf(fmaxf(fmaxf(m8[0], m8[1]), fmaxf(m8[2], m8[3])),
+                                 fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7])));
+          // The scores' barrier says that the products before them are complete too, the last O += P V
+          // among them, so O may be rescaled.
+          const bool need = mx > m + RESCALE_LOG2;
+          if (__any_sync(FULL, need && j > 0)) {
+            const float f = need ? exp2_safe(m, mx) : 1.f;
+            l *= f;
+#pragma unroll 1
+            for (int c = 0; c < D / 16; ++c) {
+              float o[16];
+              tmem_ld16(t_o + c * 16, o);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[i] *= f;
+              tmem_st16(t_o + c * 16, o);
+            }
+          }
+          if (need) m = mx;
+          const float ref = m == -INFINITY ? 0.f : m;  // (a row that has seen no key yet)
+          const float2 nref = make_float2(-ref, -ref);
+          float2 rs[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f),
+                          make_float2(0.f, 0.f)};
+          uint32_t pw[KEYS / 2];
+#pragma unroll
+          for (int i = 0; i < KEYS; i += 2) {
+            const float2 y = __fadd2_rn(make_float2(s[i], s[i + 1]), nref);
+            const float2 p = make_float2(ex2(y.x), ex2(y.y));
+            rs[(i / 2) & 3] = __fadd2_rn(rs[(i / 2) & 3], p);
+            pw[i / 2] = pack_bf16(p.x, p.y);
+          }
+          const float2 r2 = __fadd2_rn(__fadd2_rn(rs[0], rs[1]), __fadd2_rn(rs[2], rs[3]));
+          l += r2.x + r2.y;
+          __syncwarp();
+          tmem_st32(t_s, pw);
+          tmem_st32(t_s + 32, pw + 32);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars[B_P + x]);
+        }
+        if (!ok || !wait(B_O + x, o_no & 1)) break;
+        ++o_no;
+        tc_fence_after();
+        const float inv = 1.f / l;
+        const bool odd = *reinterpret_cast<volatile const int*>(&it.odd) != 0;
+        __nv_bfloat16* row = out + ((size_t)(si.q_row0 + tok) * d.q_heads + it.head * G + r % G) * D;
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          float o[32];
+          tmem_ld32(t_o + c * 32, o);
+          if (odd && tok < si.t) {
+            float more[32];
+            odd_value(d, si, layer, it.head, t0, tok, r % G, q, qk_scale, m == -INFINITY ? 0.f : m, c * 32, more);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] += more[i];
+          }
+          if (tok < si.t) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 8)
+              *reinterpret_cast<uint4*>(row + c * 32 + i) =
+                  make_uint4(pack_bf16(o[i] * inv, o[i + 1] * inv), pack_bf16(o[i + 2] * inv, o[i + 3] * inv),
+                             pack_bf16(o[i + 4] * inv, o[i + 5] * inv), pack_bf16(o[i + 6] * inv, o[i + 7] * inv));
+          }
+          __syncwarp();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars[B_O_EMPTY + x]);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc(tmem, ALL_COLS);
+  // The last CTA leaves the counters as it found them.
+  if (tid == 0 && atomicAdd(&d.dec_count[0], 1) == (int)gridDim.x - 1) {
+    d.pf_count[0] = 0;
+    d.dec_count[0] = 0;
+  }
+}
+
+}  // namespace
+
+cudaError_t prompt_tc_attributes() {
+  return cudaFuncSetAttribute(prompt_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              SMEM_BYTES);
+}
+
+cudaError_t launch_prompt_tc(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
+                             cudaStream_t s) {
+  CUtensorMap lo, hi;
+  if (!pool_tensor_maps(d, &lo, &hi)) return cudaErrorInvalidValue;
+  return launch_ex(&prompt_tc_kernel, dim3(lim.sms), dim3(TC_THREADS), SMEM_BYTES, s, true, d,
+                   layer, lo, hi, static_cast<const __nv_bfloat16*>(q), static_cast<__nv_bfloat16*>(out),
+                   LOG2E / sqrtf((float)D));
+}
+
+}  // namespace kvc
