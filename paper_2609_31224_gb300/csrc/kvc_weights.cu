@@ -9,23 +9,16 @@
 #include <cmath>
 
 #include "kvc_prompt_tile.cuh"
+#include "kvc_weights.h"
 
 namespace kvc {
 
 namespace {
 
-// Workspace: sums by KV head and slot of the pool, then lse by call row and query head.
-__host__ __device__ inline size_t sums_bytes(int64_t n_pages, int q_heads) {
-  return (size_t)n_pages * PS * q_heads * 4;
-}
-__device__ inline float* lse_of(const Dev& d, void* work) {
-  return reinterpret_cast<float*>(static_cast<uint8_t*>(work) + sums_bytes(d.n_pages, d.q_heads));
-}
-
 // lse of every row: a CTA takes 16 tokens of one session and KV head at a time.
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS) weights_lse_kernel(Dev d, int layer, const T* q, float scale,
-                                                              void* work) {
+                                                              WeightsWork work) {
   extern __shared__ __align__(16) float sm[];
   using TL = Tile<T, D>;
   float *s_q = sm, *s_k = sm + RT * TL::PITCH;
@@ -33,7 +26,7 @@ __global__ void __launch_bounds__(THREADS) weights_lse_kernel(Dev d, int layer, 
   pdl_wait();
   pdl_launch_dependents();
   if (d.g->n_units == 0) return;  // the append failed
-  float* lse = lse_of(d, work);
+  float* lse = work.lse;
   int item = blockIdx.x;
   for (int i = 0; i < d.g->n_seq; ++i) {
     const SeqInfo si = d.seq[i];
@@ -88,7 +81,7 @@ __global__ void __launch_bounds__(THREADS) weights_lse_kernel(Dev d, int layer, 
 // Sums over the rows of one KV head for each key: a CTA takes four pages of one session and head.
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS) weights_sum_kernel(Dev d, int layer, const T* q, float scale,
-                                                              void* work) {
+                                                              WeightsWork work) {
   extern __shared__ __align__(16) float sm[];
   using TL = Tile<T, D>;
   float *s_q = sm, *s_k = sm + RT * TL::PITCH;
@@ -97,8 +90,8 @@ __global__ void __launch_bounds__(THREADS) weights_sum_kernel(Dev d, int layer, 
   pdl_wait();
   pdl_launch_dependents();
   if (d.g->n_units == 0) return;
-  const float* lse = lse_of(d, work);
-  float* sums = static_cast<float*>(work);
+  const float* lse = work.lse;
+  float* sums = work.scores;
   int item = blockIdx.x;
   for (int i = 0; i < d.g->n_seq; ++i) {
     const SeqInfo si = d.seq[i];
@@ -150,11 +143,11 @@ __global__ void __launch_bounds__(THREADS) weights_sum_kernel(Dev d, int layer, 
 }
 
 // The heads' sums of each resident position, added to what it weighs.
-__global__ void __launch_bounds__(THREADS) weights_add_kernel(Dev d, const void* work, float* weights) {
+__global__ void __launch_bounds__(THREADS) weights_add_kernel(Dev d, WeightsWork work, float* weights) {
   pdl_wait();
   pdl_launch_dependents();
   if (d.g->n_units == 0) return;
-  const float* sums = static_cast<const float*>(work);
+  const float* sums = work.scores;
   int at = blockIdx.x * THREADS + threadIdx.x;
   for (int i = 0; i < d.g->n_seq; ++i) {
     const SeqInfo si = d.seq[i];
@@ -183,8 +176,8 @@ cudaError_t attributes() {
 }
 
 template <typename T, int D>
-cudaError_t launch(const Dev& d, const Limits& lim, int layer, const void* q, float* weights, void* work,
-                   cudaStream_t s, int64_t* launches) {
+cudaError_t launch(const Dev& d, const Limits& lim, int layer, const void* q, float* weights,
+                   const WeightsWork& work, cudaStream_t s, int64_t* launches) {
   const float scale = LOG2E / sqrtf((float)D);
   const dim3 grid(lim.sms * 3);
   cudaError_t e = launch_ex(&weights_lse_kernel<T, D>, grid, dim3(THREADS), Tile<T, D>::SMEM, s, true, d,
@@ -202,21 +195,51 @@ cudaError_t launch(const Dev& d, const Limits& lim, int layer, const void* q, fl
 
 }  // namespace
 
+namespace {
+
+// The parts of a scratch area, from its start; their bytes.
+size_t lay_out(uint8_t* base, int64_t n_pages, int q_heads, int max_tokens, int max_seq, WeightsWork* w) {
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    uint8_t* p = base ? base + off : nullptr;
+    off += (bytes + 255) / 256 * 256;
+    return p;
+  };
+  uint8_t* scores = take((size_t)n_pages * PS * q_heads * sizeof(float));
+  uint8_t* lse = take((size_t)max_tokens * q_heads * sizeof(float));
+  uint8_t* whole = take((size_t)max_seq * q_heads * sizeof(float2));
+  uint8_t* parts = take((size_t)WEIGHTS_PARTS * G * sizeof(float2));
+  if (w) {
+    w->scores = reinterpret_cast<float*>(scores);
+    w->lse = reinterpret_cast<float*>(lse);
+    w->whole = reinterpret_cast<float2*>(whole);
+    w->parts = reinterpret_cast<float2*>(parts);
+  }
+  return off;
+}
+
+}  // namespace
+
 size_t weights_work_bytes(const kvc_config& c) {
-  return sums_bytes(c.n_pages, c.q_heads) + (size_t)c.max_tokens_per_call * c.q_heads * 4;
+  return lay_out(nullptr, c.n_pages, c.q_heads, c.max_tokens_per_call, c.max_seq_per_call, nullptr);
 }
 
 cudaError_t weights_attributes(const Dev& d) {
-  return d.esz == 2 ? attributes<__nv_bfloat16, 128>() : attributes<float, 64>();
+  const cudaError_t e = d.esz == 2 ? attributes<__nv_bfloat16, 128>() : attributes<float, 64>();
+  return e != cudaSuccess ? e : weights_token_attributes(d);
 }
 
 cudaError_t launch_attn_weights(const Dev& d, const Limits& lim, int layer, const void* q,
                                 float* weights, void* work, int n_seq, int total, int max_t,
                                 LaunchOrder* order, cudaStream_t s, int64_t* launches) {
-  // (Each kernel waits for the one before it before it lets the next one start.)
+  WeightsWork w;
+  lay_out(static_cast<uint8_t*>(work), d.n_pages, d.q_heads, d.max_tokens, d.max_seq, &w);
+  // (Each kernel but an early one waits for the one before it before it lets the next one start.)
+  const bool early = order->early(layer, false);
   order->launched(layer, false);
-  return d.esz == 2 ? launch<__nv_bfloat16, 128>(d, lim, layer, q, weights, work, s, launches)
-                    : launch<float, 64>(d, lim, layer, q, weights, work, s, launches);
+  if (max_t == 1) return launch_weights_token(d, lim, layer, q, weights, w, n_seq, early, s, launches);
+  return d.esz == 2 ? launch<__nv_bfloat16, 128>(d, lim, layer, q, weights, w, s, launches)
+                    : launch<float, 64>(d, lim, layer, q, weights, w, s, launches);
 }
 
 }  // namespace kvc
