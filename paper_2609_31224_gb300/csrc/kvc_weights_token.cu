@@ -24,7 +24,7 @@ constexpr int TOKEN_WARPS = 4, TOKEN_THREADS = TOKEN_WARPS * 32;
 constexpr int TOKEN_STAGES = 6;                    // 4 KiB each, a warp
 constexpr int UNIT_BYTES = 4096;                   // the keys of a unit, in either type
 constexpr int TOKEN_SMEM = TOKEN_WARPS * TOKEN_STAGES * UNIT_BYTES + 1024;
-constexpr int TOKEN_MIN_UNITS = 8;                 // of a CTA, at least
+constexpr int TOKEN_MIN_UNITS = 4;                 // of a CTA, at least
 constexpr int TOKEN_NO_LIMIT = 1 << 16;
 
 // Copy of a unit's keys into a stage (one lane).
@@ -66,6 +66,16 @@ __device__ inline void q_pieces(const Dev& d, const SeqInfo& si, int head, const
       qb[ks][j] = piece(a0 * qk_scale, a1 * qk_scale);
       qb[ks + 4][j] = piece(b0 * qk_scale, b1 * qk_scale);
     }
+}
+
+// A head's query rows and rotary row into L2 (either type: 1 KiB and 512 bytes).
+template <typename T>
+__device__ inline void prefetch_q_rows(const Dev& d, const SeqInfo& si, int head, const T* q, int lane) {
+  const char* rows = reinterpret_cast<const char*>(
+      q + ((size_t)si.q_row0 * d.q_heads + (size_t)head * G) * d.head_dim);
+  const char* cs = reinterpret_cast<const char*>(d.rope + (size_t)si.pos_first * (d.head_dim / 2));
+  if (lane < 8) prefetch_l2(rows + lane * 128);
+  else if (lane < 8 + d.head_dim / 32) prefetch_l2(cs + (lane - 8) * 128);
 }
 
 // The running (max, sum) of two states.
@@ -126,6 +136,7 @@ __global__ void __launch_bounds__(TOKEN_THREADS) weights_token_kernel(
       if (lane == 0) load_unit<T>(d, layer, page, head, ring + s * UNIT_BYTES, &bars[s], &map_lo, &map_hi, policy);
     }
     if (!waited) {
+      if (warp == 0) prefetch_q_rows(d, si, head, q, lane);
       pdl_wait();
       waited = true;
     }
@@ -268,63 +279,99 @@ __global__ void __launch_bounds__(TOKEN_THREADS) weights_token_kernel(
   }
 }
 
-// Pages of one session, eight at a time: blockIdx.y is the session of the call.
+// Pages of one session, eight at a time: blockIdx.y is the session of the call.  (Everything that the
+// append wrote is complete before the kernel in front lets this one start.)
 __global__ void __launch_bounds__(TOKEN_THREADS) weights_token_add_kernel(Dev d, int grid,
                                                                           WeightsWork work,
                                                                           float* weights) {
-  __shared__ float s_lse[64 * G];
+  __shared__ __align__(16) float s_lse[64 * G];
+  constexpr int AT_ONCE = TOKEN_THREADS / PS, HEADS = 8;  // pages; heads' scores on their way
   const int tid = threadIdx.x, H = d.kv_heads, seq = blockIdx.y;
-  pdl_wait();
   pdl_launch_dependents();
   const UnitSplit us = unit_split(d, grid, TOKEN_MIN_UNITS, TOKEN_NO_LIMIT);
-  if (us.U == 0) return;
   const SeqInfo si = d.seq[seq];
-  const int nb = si.n_blocks;
-  if ((int)blockIdx.x * (TOKEN_THREADS / PS) >= nb) return;
-  // lse of each query head's row: eight lanes share its parts.
+  const int nb = si.n_blocks, slot = tid % PS;
+  if (us.U == 0 || (int)blockIdx.x * AT_ONCE >= nb) {
+    pdl_wait();
+    return;
+  }
+  const int32_t* hrow = d.hist_pt + (size_t)si.sid * d.max_pages_per_session;
+  const int32_t* lrow = d.live_pt + (size_t)si.sid * d.max_pages_per_session;
+  int b = blockIdx.x * AT_ONCE + tid / PS, page = 0, pos = 0;
+  bool in = false;
+  auto find = [&] {  // this thread's slot of its page b
+    in = false;
+    if (b >= nb) return;
+    const BlockRange br = block_range(si, b);
+    in = slot >= br.lo && slot < br.hi;
+    if (!in) return;
+    page = block_page(si, hrow, lrow, b);
+    pos = d.meta_pos[page * PS + slot];
+  };
+  find();
   const int lane = tid & 31;
-  for (int r0 = 0; r0 < H * G; r0 += TOKEN_THREADS / 8) {
-    const int r = min(r0 + tid / 8, H * G - 1), head = r / G, start = si.unit_base + head * nb;
-    const int cf = us.owner(start), cl = us.owner(start + nb - 1);
+  // A row of lse, eight lanes to its parts.
+  int r = min(tid / 8, H * G - 1), start = si.unit_base + r / G * nb;
+  int cf = us.owner(start), cl = us.owner(start + nb - 1), first = us.slot_of(cf, cf, start);
+  pdl_wait();
+  float4 x[HEADS];
+  float before = 0.f;
+  const float4* scores = reinterpret_cast<const float4*>(work.scores) + slot;
+  auto fetch = [&](int h0) {
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h)
+      if (in && h0 + h < H) x[h] = scores[((size_t)page * H + h0 + h) * PS];
+  };
+  float* at = weights + (size_t)si.sid * d.max_positions;
+  fetch(0);
+  if (in) before = at[pos];
+  for (int r0 = 0;;) {
     float2 a = make_float2(-INFINITY, 0.f);
     if (cf == cl) {
-      if (lane % 8 == 0) a = work.whole[((size_t)seq * H + head) * G + r % G];
+      if (lane % 8 == 0) a = work.whole[(size_t)seq * H * G + r];
     } else {
-      const int first = us.slot_of(cf, cf, start);
       for (int c = cf + lane % 8; c <= cl; c += 32) {  // four loads in flight
-        float2 b[4];
+        float2 o[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          b[i] = c + 8 * i <= cl ? work.parts[(size_t)(c + 8 * i == cf ? first : 2 * (c + 8 * i)) * G + r % G]
+          o[i] = c + 8 * i <= cl ? work.parts[(size_t)(c + 8 * i == cf ? first : 2 * (c + 8 * i)) * G + r % G]
                                  : make_float2(-INFINITY, 0.f);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) join(a.x, a.y, b[i].x, b[i].y);
+        for (int i = 0; i < 4; ++i) join(a.x, a.y, o[i].x, o[i].y);
       }
     }
 #pragma unroll
     for (int o = 4; o > 0; o >>= 1)
       join(a.x, a.y, __shfl_xor_sync(FULL, a.x, o), __shfl_xor_sync(FULL, a.y, o));
     if (lane % 8 == 0) s_lse[r] = a.x + log2f(a.y);
+    r0 += TOKEN_THREADS / 8;
+    if (r0 >= H * G) break;
+    r = min(r0 + tid / 8, H * G - 1);
+    start = si.unit_base + r / G * nb;
+    cf = us.owner(start);
+    cl = us.owner(start + nb - 1);
+    first = us.slot_of(cf, cf, start);
   }
   __syncthreads();
-  const int32_t* hrow = d.hist_pt + (size_t)si.sid * d.max_pages_per_session;
-  const int32_t* lrow = d.live_pt + (size_t)si.sid * d.max_pages_per_session;
-  const int slot = tid % PS;
-  for (int b = blockIdx.x * (TOKEN_THREADS / PS) + tid / PS; b < nb; b += gridDim.x * (TOKEN_THREADS / PS)) {
-    const BlockRange br = block_range(si, b);
-    if (slot < br.lo || slot >= br.hi) continue;
-    const int page = block_page(si, hrow, lrow, b);
-    const float4* s = reinterpret_cast<const float4*>(work.scores) + (size_t)page * H * PS + slot;
-    float* at = weights + (size_t)si.sid * d.max_positions + d.meta_pos[page * PS + slot];
-    const float before = *at;
+  for (;;) {
     float w = 0.f;
-#pragma unroll 8
-    for (int h = 0; h < H; ++h) {
-      const float4 x = s[h * PS];
-      const float* lse = s_lse + h * G;
-      w += (exp2f(x.x - lse[0]) + exp2f(x.y - lse[1])) + (exp2f(x.z - lse[2]) + exp2f(x.w - lse[3]));
+    for (int h0 = 0;;) {
+#pragma unroll
+      for (int h = 0; h < HEADS; ++h)
+        if (h0 + h < H) {
+          const float4 lse = reinterpret_cast<const float4*>(s_lse)[h0 + h];
+          w += (exp2f(x[h].x - lse.x) + exp2f(x[h].y - lse.y)) + (exp2f(x[h].z - lse.z) + exp2f(x[h].w - lse.w));
+        }
+      h0 += HEADS;
+      if (h0 >= H) break;
+      fetch(h0);
     }
-    *at = before + w;
+    if (in) at[pos] = before + w;
+    b += gridDim.x * AT_ONCE;
+    if (b - tid / PS >= nb) break;
+    find();
+    fetch(0);
+    if (in) before = at[pos];
   }
 }
 
@@ -339,7 +386,7 @@ cudaError_t launch(const Dev& d, const Limits& lim, int layer, const void* q, fl
                             work, (int)early);
   *launches += e == cudaSuccess;
   if (e != cudaSuccess) return e;
-  const int per = max(1, min(64, 4 * lim.sms / n_seq));
+  const int per = max(1, min(64, 16 * lim.sms / n_seq));
   e = launch_ex(&weights_token_add_kernel, dim3(per, n_seq), dim3(TOKEN_THREADS), 0, s, true, d, grid,
                 work, weights);
   *launches += e == cudaSuccess;
