@@ -217,7 +217,7 @@ cudaError_t prompt_attributes(const Dev& d);
 cudaError_t weights_attributes(const Dev& d);
 cudaError_t launch_attn_weights(const Dev& d, const Limits& lim, int layer, const void* q,
                                 float* weights, void* work, int n_seq, int total, int max_t,
-                                LaunchOrder* order, cudaStream_t s, int64_t* launches);
+                                int pages_max, int64_t pages_sum, LaunchOrder* order, cudaStream_t s, int64_t* launches);
 int noalloc_max_pairs();
 cudaError_t launch_attn_decode_noalloc(const Dev& d, int layer, const void* q, void* out,
                                        int n_seq, cudaStream_t s);

@@ -27,22 +27,16 @@
 
 #include <cmath>
 
-#include "kvc_prefill_tc.cuh"
 #include "kvc_prompt.h"
+#include "kvc_prompt_tc.cuh"
 
 namespace kvc {
 
 namespace {
 
-constexpr int KEYS = 128, PAGES = KEYS / PS;       // of a step
-constexpr int TOKENS = 32;                         // of a tile
-constexpr int PANEL = KEYS * 128;                  // 128 rows x 64 columns
-constexpr int SLOT = 2 * PANEL;                    // a K or V stage, or a query tile
 constexpr int RING = 5;
 constexpr int EDGES = 4;
-constexpr int TC_THREADS = 512;
 constexpr int S_COL = 0, O_COL = 256, ALL_COLS = 512;
-constexpr int FEW_REGS = 96, MANY_REGS = 160;      // 256 threads each: what 128 a thread make together
 
 enum {
   B_FULL = 0,                    // [RING] a stage has landed
@@ -82,69 +76,6 @@ constexpr int OFF_TILES = 3072;                    // query tiles A, B, then the
 constexpr int SMEM_BYTES = OFF_TILES + (2 + RING) * SLOT;
 static_assert(N_BARS * 8 <= OFF_ITEM && OFF_FIRST + (MAX_SEQ + 1) * 4 <= OFF_TILES, "header fits");
 static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of a CTA");
-
-__device__ inline void tc_mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
-                                 uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-__device__ inline void tma_load_2d(void* dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_u32(bar))
-      : "memory");
-}
-template <int N>
-__device__ inline void give_registers() {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
-}
-template <int N>
-__device__ inline void take_registers() {
-  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
-}
-
-// Bounded wait that also ends when another warp has given up.
-__device__ inline bool wait_or_stop(const Dev& d, uint64_t* bar, uint32_t parity, volatile int* stop) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const long long t0 = clock64();
-  while (!mbar_try_wait(bar, parity)) {
-    if (*stop) return false;
-    if (clock64() - t0 > WAIT_LIMIT_CYCLES) {
-      set_error(d, KVC_DERR_WAIT);
-      *stop = 1;
-      return false;
-    }
-  }
-  return true;
-}
-
-// Blocks that the tokens up to `tok` of the chunk see.
-__device__ inline int blocks_seen(const SeqInfo& si, int tok) {
-  return si.n_hist_pages + (si.live_head + si.n_live - si.t + tok) / PS + 1;
-}
-
-// Whether a step (blocks [b0, b0 + PAGES)) has slots that some row of the item starting at token t0 does
-// not see: a partly filled page, pages past the end, keys behind the item's first token.
-__device__ inline bool is_edge(const SeqInfo& si, int t0, int b0) {
-  const int nhp = si.n_hist_pages;
-  const int first = nhp + (si.live_head + si.n_live - si.t + t0) / PS;  // block of the first token
-  if (b0 + PAGES > first) return true;
-  const int b_hist = (si.n_hist % PS) ? nhp - 1 : -1, b_live = si.live_head ? nhp : -1;
-  return (b_hist >= b0 && b_hist < b0 + PAGES) || (b_live >= b0 && b_live < b0 + PAGES);
-}
-
-// Slots [lo, hi) of block b that hold a position with index <= q_log.
-__device__ inline uint32_t slots_seen(const SeqInfo& si, int b, int n_blocks, int q_log) {
-  if (b >= n_blocks) return 0;
-  const BlockRange br = block_range(si, b);
-  const int hi = min(br.hi, q_log - br.base + 1);
-  return hi <= br.lo ? 0u : ((1u << hi) - 1u) & ~((1u << br.lo) - 1u);
-}
 
 __device__ inline bool not_finite(uint32_t two) {
   return (two & 0x7F80u) == 0x7F80u || (two & 0x7F800000u) == 0x7F800000u;
@@ -192,7 +123,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
   int* s_first = reinterpret_cast<int*>(smem + OFF_FIRST);
   volatile int* stop = reinterpret_cast<int*>(smem + OFF_STOP);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int H = d.kv_heads, L = d.layers;
+  const int H = d.kv_heads;
   uint8_t* s_q = smem + OFF_TILES;
   uint8_t* s_ring = s_q + 2 * SLOT;
   pdl_wait();
@@ -211,23 +142,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
     fence_mbar_init();
     *stop = 0;
   }
-  // First item of each session: 64-token tiles of its chunk, for each KV head (one warp).
-  if (warp == 2) {
-    int sum = 0;
-    for (int i0 = 0; i0 < n_seq; i0 += 32) {
-      const int i = i0 + lane;
-      const int n = i < n_seq ? (d.seq[i].t + 2 * TOKENS - 1) / (2 * TOKENS) * H : 0;
-      int x = n;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(FULL, x, o);
-        if (lane >= o) x += y;
-      }
-      if (i < n_seq) s_first[i] = sum + x - n;
-      sum += __shfl_sync(FULL, x, 31);
-    }
-    if (lane == 0) s_first[n_seq] = sum;
-  }
+  // First item of each session: 64-token tiles of its chunk, for each KV head.
+  if (warp == 2)
+    first_items(n_seq, lane, s_first, [&](int i) { return (d.seq[i].t + 2 * TOKENS - 1) / (2 * TOKENS) * H; });
   __syncwarp();
   if (warp == 1) tmem_alloc(tmem_slot, ALL_COLS);
   tc_fence_before();
@@ -258,13 +175,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
         }
         break;
       }
-      int lo = 0, hi = n_seq - 1;
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (s_first[mid] <= at) lo = mid;
-        else hi = mid - 1;
-      }
-      const int seq = lo, in = at - s_first[seq];
+      const int seq = session_of(n_seq, s_first, at), in = at - s_first[seq];
       if (lane < 16)
         reinterpret_cast<int*>(&it->si)[lane] = reinterpret_cast<const int*>(d.seq + seq)[lane];
       __syncwarp();
@@ -306,9 +217,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
           }
           if (lane == 0) mbar_arrive_expect_tx(bar, n_pg * PS * D * 2);
           __syncwarp();
-          if (lane < 16 && pg < n_pg)
-            tma_load_2d(s_ring + st * SLOT + (lane & 1) * PANEL + pg * 2048, map, 0,
-                        (((page * L + layer) * 2 + kv) * H + head) * PS, bar);
+          load_tile(d, layer, kv, head, page, n_pg, s_ring + st * SLOT, map, bar, lane);
         }
       }
     }
@@ -444,49 +353,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
       const SeqInfo& si = it.si;
       const int head = it.head, t0 = it.t0, steps = it.steps;
       const int tiles = t0 + TOKENS < si.t ? 2 : 1;
-      // A thread takes 16-byte chunks c and c + 8 (which rotate together) of a token's G rows.
-      const int c = ts & 7;
-      for (int x = 0; x < tiles; ++x) {
-#pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
-          const int tl = (ts >> 3) + 16 * h, tok = t0 + x * TOKENS + tl;
-          uint4 a[G], b[G];
-          float4 cs[4];
-          const bool in = tok < si.t;
-          if (in) {
-            const uint4* row = reinterpret_cast<const uint4*>(
-                q + ((size_t)(si.q_row0 + tok) * d.q_heads + head * G) * D) + c;
-            const float4* t4 = reinterpret_cast<const float4*>(d.rope + (size_t)(si.pos_first + tok) * (D / 2) + c * 8);
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-              a[g] = row[g * 16];
-              b[g] = row[g * 16 + 8];
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) cs[e] = t4[e];
-          }
-          if (h == 0 && q_no[x] > 0 && !wait(B_Q_EMPTY + x, (q_no[x] - 1) & 1)) break;
-#pragma unroll
-          for (int g = 0; g < G; ++g) {
-            uint32_t ya[4] = {0, 0, 0, 0}, yb[4] = {0, 0, 0, 0};
-            if (in) {
-              const uint32_t ua[4] = {a[g].x, a[g].y, a[g].z, a[g].w};
-              const uint32_t ub[4] = {b[g].x, b[g].y, b[g].z, b[g].w};
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float a0 = bf16lo(ua[e]), a1 = bf16hi(ua[e]), b0 = bf16lo(ub[e]), b1 = bf16hi(ub[e]);
-                ya[e] = pack_bf16(fmaf(a0, cs[e].x, -b0 * cs[e].y) * qk_scale,
-                                  fmaf(a1, cs[e].z, -b1 * cs[e].w) * qk_scale);
-                yb[e] = pack_bf16(fmaf(b0, cs[e].x, a0 * cs[e].y) * qk_scale,
-                                  fmaf(b1, cs[e].z, a1 * cs[e].w) * qk_scale);
-              }
-            }
-            const int r = tl * G + g;
-            uint8_t* at = s_q + x * SLOT + r * 128 + ((c ^ (r & 7)) << 4);
-            *reinterpret_cast<uint4*>(at) = make_uint4(ya[0], ya[1], ya[2], ya[3]);
-            *reinterpret_cast<uint4*>(at + PANEL) = make_uint4(yb[0], yb[1], yb[2], yb[3]);
-          }
-        }
+      for (int x = 0; x < tiles && ok; ++x) {
+        stage_q<1>(d, si, head, t0 + x * TOKENS, q, qk_scale, s_q + x * SLOT, ts,
+                   [&] { return q_no[x] == 0 || wait(B_Q_EMPTY + x, (q_no[x] - 1) & 1); });
         if (!ok) break;
         ++q_no[x];
         fence_proxy_async_smem();

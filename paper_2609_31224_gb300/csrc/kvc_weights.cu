@@ -6,6 +6,7 @@
 // A weight needs its row's sum first, so the scores are formed twice: the first kernel forms lse, the
 // second the sums over rows, for a key tile and KV head each; a third adds the heads up in their order,
 // so that results repeat.
+#include <algorithm>
 #include <cmath>
 
 #include "kvc_prompt_tile.cuh"
@@ -142,27 +143,35 @@ __global__ void __launch_bounds__(THREADS) weights_sum_kernel(Dev d, int layer, 
   }
 }
 
-// The heads' sums of each resident position, added to what it weighs.
-__global__ void __launch_bounds__(THREADS) weights_add_kernel(Dev d, WeightsWork work, float* weights) {
+// The planes' sums of each resident position, added to what it weighs: blockIdx.y is the session of the
+// call.
+__global__ void __launch_bounds__(THREADS) weights_add_kernel(Dev d, int planes, WeightsWork work,
+                                                              float* weights) {
   pdl_wait();
   pdl_launch_dependents();
   if (d.g->n_units == 0) return;
-  const float* sums = work.scores;
-  int at = blockIdx.x * THREADS + threadIdx.x;
-  for (int i = 0; i < d.g->n_seq; ++i) {
-    const SeqInfo si = d.seq[i];
-    for (; at < si.n_blocks * PS; at += gridDim.x * THREADS) {
-      int index;
-      if (!key_index(si, at / PS, at % PS, &index)) continue;
-      const int page = block_page(si, d.hist_pt + (size_t)si.sid * d.max_pages_per_session,
-                                  d.live_pt + (size_t)si.sid * d.max_pages_per_session, at / PS);
-      const int gs = page * PS + at % PS;
-      float w = 0.f;
-      for (int h = 0; h < d.kv_heads; ++h) w += sums[(size_t)h * d.n_pages * PS + gs];
-      weights[(size_t)si.sid * d.max_positions + d.meta_pos[gs]] += w;
-    }
-    at -= si.n_blocks * PS;
+  const SeqInfo si = d.seq[blockIdx.y];
+  const size_t plane = (size_t)d.n_pages * PS;
+  for (int at = blockIdx.x * THREADS + threadIdx.x; at < si.n_blocks * PS; at += gridDim.x * THREADS) {
+    int index;
+    if (!key_index(si, at / PS, at % PS, &index)) continue;
+    const int page = block_page(si, d.hist_pt + (size_t)si.sid * d.max_pages_per_session,
+                                d.live_pt + (size_t)si.sid * d.max_pages_per_session, at / PS);
+    const int gs = page * PS + at % PS;
+    float w = 0.f;
+#pragma unroll 8
+    for (int h = 0; h < planes; ++h) w += work.scores[h * plane + gs];
+    weights[(size_t)si.sid * d.max_positions + d.meta_pos[gs]] += w;
   }
+}
+
+cudaError_t launch_add(const Dev& d, const Limits& lim, int planes, const WeightsWork& work, float* weights,
+                       int n_seq, cudaStream_t s, int64_t* launches) {
+  const dim3 grid(std::max(1, std::min(64, 8 * lim.sms / n_seq)), n_seq);
+  const cudaError_t e = launch_ex(&weights_add_kernel, grid, dim3(THREADS), 0, s, true, d, planes, work,
+                                  weights);
+  *launches += e == cudaSuccess;
+  return e;
 }
 
 template <typename T, int D>
@@ -176,8 +185,8 @@ cudaError_t attributes() {
 }
 
 template <typename T, int D>
-cudaError_t launch(const Dev& d, const Limits& lim, int layer, const void* q, float* weights,
-                   const WeightsWork& work, cudaStream_t s, int64_t* launches) {
+cudaError_t launch(const Dev& d, const Limits& lim, int layer, const void* q, const WeightsWork& work,
+                   cudaStream_t s, int64_t* launches) {
   const float scale = LOG2E / sqrtf((float)D);
   const dim3 grid(lim.sms * 3);
   cudaError_t e = launch_ex(&weights_lse_kernel<T, D>, grid, dim3(THREADS), Tile<T, D>::SMEM, s, true, d,
@@ -186,9 +195,6 @@ cudaError_t launch(const Dev& d, const Limits& lim, int layer, const void* q, fl
   if (e != cudaSuccess) return e;
   e = launch_ex(&weights_sum_kernel<T, D>, grid, dim3(THREADS), Tile<T, D>::SMEM, s, true, d, layer,
                 static_cast<const T*>(q), scale, work);
-  *launches += e == cudaSuccess;
-  if (e != cudaSuccess) return e;
-  e = launch_ex(&weights_add_kernel, dim3(lim.sms), dim3(THREADS), 0, s, true, d, work, weights);
   *launches += e == cudaSuccess;
   return e;
 }
@@ -207,11 +213,13 @@ size_t lay_out(uint8_t* base, int64_t n_pages, int q_heads, int max_tokens, int 
   };
   uint8_t* scores = take((size_t)n_pages * PS * q_heads * sizeof(float));
   uint8_t* lse = take((size_t)max_tokens * q_heads * sizeof(float));
+  uint8_t* stats = take(((size_t)max_tokens * q_heads + WEIGHTS_STATS) * sizeof(float2));
   uint8_t* whole = take((size_t)max_seq * q_heads * sizeof(float2));
   uint8_t* parts = take((size_t)WEIGHTS_PARTS * G * sizeof(float2));
   if (w) {
     w->scores = reinterpret_cast<float*>(scores);
     w->lse = reinterpret_cast<float*>(lse);
+    w->stats = reinterpret_cast<float2*>(stats);
     w->whole = reinterpret_cast<float2*>(whole);
     w->parts = reinterpret_cast<float2*>(parts);
   }
@@ -225,21 +233,35 @@ size_t weights_work_bytes(const kvc_config& c) {
 }
 
 cudaError_t weights_attributes(const Dev& d) {
-  const cudaError_t e = d.esz == 2 ? attributes<__nv_bfloat16, 128>() : attributes<float, 64>();
+  const cudaError_t e = d.esz == 2 ? weights_tc_attributes() : attributes<float, 64>();
   return e != cudaSuccess ? e : weights_token_attributes(d);
 }
 
 cudaError_t launch_attn_weights(const Dev& d, const Limits& lim, int layer, const void* q,
                                 float* weights, void* work, int n_seq, int total, int max_t,
-                                LaunchOrder* order, cudaStream_t s, int64_t* launches) {
+                                int pages_max, int64_t pages_sum, LaunchOrder* order, cudaStream_t s, int64_t* launches) {
   WeightsWork w;
   lay_out(static_cast<uint8_t*>(work), d.n_pages, d.q_heads, d.max_tokens, d.max_seq, &w);
   // (Each kernel but an early one waits for the one before it before it lets the next one start.)
   const bool early = order->early(layer, false);
   order->launched(layer, false);
   if (max_t == 1) return launch_weights_token(d, lim, layer, q, weights, w, n_seq, early, s, launches);
-  return d.esz == 2 ? launch<__nv_bfloat16, 128>(d, lim, layer, q, weights, w, s, launches)
-                    : launch<float, 64>(d, lim, layer, q, weights, w, s, launches);
+  int shares = 1;
+  cudaError_t e;
+  if (d.esz == 2) {
+    // Where the chunk's rows alone are too few items, the keys are cut into parts; where the keys are,
+    // the tokens into shares.
+    const int64_t rows = ((int64_t)total + 63 * n_seq) / 64 * d.kv_heads;
+    const int64_t stats = (int64_t)d.max_tokens * d.q_heads + WEIGHTS_STATS;
+    int64_t parts = std::max<int64_t>(1, std::min<int64_t>(2 * lim.sms / rows, (pages_max + 7) / 8));
+    parts = std::max<int64_t>(1, std::min(parts, stats / ((int64_t)total * d.q_heads)));
+    const int64_t keys = (pages_sum / 16 + n_seq) * d.kv_heads;
+    while (shares < WEIGHTS_SHARES && keys * shares < 4 * lim.sms && max_t / 32 > 4 * shares) shares *= 2;
+    e = launch_weights_tc(d, lim, layer, q, w, (int)parts, shares, s, launches);
+  } else {
+    e = launch<float, 64>(d, lim, layer, q, w, s, launches);
+  }
+  return e != cudaSuccess ? e : launch_add(d, lim, d.kv_heads * shares, w, weights, n_seq, s, launches);
 }
 
 }  // namespace kvc

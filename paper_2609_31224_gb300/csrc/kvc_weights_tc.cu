@@ -1,0 +1,614 @@
+// Attention weights of chunks (kvc_attn_weights) over bfloat16 rows, on the 5th-generation tensor cores.
+//
+// Weights are sums of probabilities in binary32, so the scores keep more of q than bfloat16 has: q is
+// held in two bfloat16 pieces, q_up = bf16(q) and bf16(q - q_up), and S = K q_up + K q_low adds up both
+// products in one accumulator; what is left out is below 2^-17 of q.  K is what the cache holds, exact.
+// Two passes over the scores, since a weight needs its row's sum:
+//   weights_stat_kernel   S = Q K^T, a thread has a query row: running (max, sum), of `parts` ranges of
+//                         the keys where the chunk alone has too few rows for all SMs
+//   weights_sums_kernel   S^T = K Q^T, a thread has a key and adds up 2^(s - lse) along its row, for 256
+//                         keys of one (session, KV head) and a share of the chunk's tokens an item; no
+//                         sum crosses threads
+// The sums of heads and shares are added up by weights_add_kernel (kvc_weights.cu) in their order.
+// Both are bound by the products, 2 x 512 cycles a tile of 128 x 128; its exponentials take half of that.
+// Warp roles as in kvc_prompt_tc.cu: warp 0 items and K by TMA, warp 1 the products, warps 4-7 query
+// tiles, warps 8-15 what becomes of the scores.  All waits are bounded.
+#include <cuda.h>
+
+#include <cmath>
+
+#include "kvc_prompt_tc.cuh"
+#include "kvc_weights.h"
+
+namespace kvc {
+
+namespace {
+
+constexpr int K_RING = 3;
+constexpr int LSE_RING = 4;                        // query tiles whose lse is kept
+constexpr int ALL_COLS = 512;                      // two tiles' scores, twice each: 4 x 128 columns
+constexpr int OFF_ITEM = 512;                      // [2]
+constexpr int OFF_TMEM = OFF_ITEM + 2 * 128;
+constexpr int OFF_STOP = OFF_TMEM + 4;
+constexpr int OFF_FIRST = OFF_STOP + 4;            // first items, see each kernel
+constexpr int OFF_TILES = 3072;
+constexpr int SMEM_BYTES = OFF_TILES + 7 * SLOT;
+static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of a CTA");
+
+enum {
+  B_FULL = 0,                        // [K_RING] a K tile has landed
+  B_EMPTY = B_FULL + K_RING,         // [K_RING] and was read
+  B_Q_FULL = B_EMPTY + K_RING,       // [2] a query tile is there
+  B_Q_EMPTY = B_Q_FULL + 2,          // [2] and was read
+  B_S = B_Q_EMPTY + 2,               // [2 tiles][2] scores complete
+  B_S_EMPTY = B_S + 4,               // [2 tiles][2] and read
+  B_ITEM = B_S_EMPTY + 4,            // [2] an item is known
+  B_ITEM_EMPTY = B_ITEM + 2,         // [2] and every warp is through with it
+  B_LSE_EMPTY = B_ITEM_EMPTY + 2,    // sums: [LSE_RING] lse of a query tile was read
+  B_FINAL = B_LSE_EMPTY + LSE_RING,
+  N_BARS = B_FINAL + 1
+};
+static_assert(N_BARS * 8 <= OFF_ITEM, "barriers fit");
+constexpr int ITEM_READERS = 1 + 4 + 8;
+
+struct Item {
+  SeqInfo si;
+  int32_t valid;          // 0: no more items
+  int32_t head;
+  int32_t at;             // stat: first token; sums: first page
+  int32_t part;           // stat: part of the keys; sums: share of the tokens
+  int32_t begin, end;     // stat: steps of keys; sums: tiles of tokens
+  int32_t pad[10];
+};
+static_assert(sizeof(Item) == 128, "Item size");
+
+__device__ inline void init_barriers(uint64_t* bars) {
+  for (int i = 0; i < N_BARS; ++i) {
+    const int count = i >= B_Q_FULL && i < B_Q_EMPTY         ? 4
+                      : i >= B_S_EMPTY && i < B_ITEM         ? 4
+                      : i >= B_ITEM_EMPTY && i < B_LSE_EMPTY ? ITEM_READERS
+                      : i >= B_LSE_EMPTY && i < B_FINAL      ? 8
+                                                             : 1;
+    mbar_init(&bars[i], count);
+  }
+  fence_mbar_init();
+}
+
+// The last CTA leaves the counters as it found them.
+__device__ inline void leave_counters(const Dev& d) {
+  if (threadIdx.x == 0 && atomicAdd(&d.dec_count[0], 1) == (int)gridDim.x - 1) {
+    d.pf_count[0] = 0;
+    d.dec_count[0] = 0;
+  }
+}
+
+// Both pieces' products of a tile: A the rows at a (a_step bytes to its other piece), B at b likewise.
+__device__ inline void piece_products(uint32_t to, uint32_t a, uint32_t a_step, uint32_t b, uint32_t b_step,
+                                      uint32_t idesc) {
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    const uint64_t ad = smem_desc(a + p * a_step, 0, 1024), bd = smem_desc(b + p * b_step, 0, 1024);
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      const uint32_t at = (kk >> 2) * PANEL + (kk & 3) * 32;
+      tc_mma_ss(to, desc_at(ad, at), desc_at(bd, at), idesc, p > 0 || kk > 0);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Row statistics: an item is 64 tokens (tiles A and B) of one (session, KV head) and a part of the keys.
+// ---------------------------------------------------------------------------
+__global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
+    Dev d, int layer, const __grid_constant__ CUtensorMap map_lo,
+    const __grid_constant__ CUtensorMap map_hi, const __nv_bfloat16* __restrict__ q, float qk_scale,
+    int parts, WeightsWork work) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem);
+  Item* items = reinterpret_cast<Item*>(smem + OFF_ITEM);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + OFF_TMEM);
+  volatile int* stop = reinterpret_cast<int*>(smem + OFF_STOP);
+  int* s_first = reinterpret_cast<int*>(smem + OFF_FIRST);
+  static_assert(OFF_FIRST + (MAX_SEQ + 1) * 4 <= OFF_TILES, "header fits");
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = d.kv_heads;
+  uint8_t* s_q = smem + OFF_TILES;      // A upper, A lower, B upper, B lower
+  uint8_t* s_k = s_q + 4 * SLOT;
+  pdl_wait();
+  pdl_launch_dependents();
+  const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;
+  if (tid == 0) {
+    init_barriers(bars);
+    *stop = 0;
+  }
+  if (warp == 2)
+    first_items(n_seq, lane, s_first,
+                [&](int i) { return (d.seq[i].t + 2 * TOKENS - 1) / (2 * TOKENS) * H * parts; });
+  __syncwarp();
+  if (warp == 1) tmem_alloc(tmem_slot, ALL_COLS);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  bool ok = true;
+  auto wait_warp = [&](int bar, uint32_t parity) {
+    ok = ok && __all_sync(FULL, wait_or_stop(d, &bars[bar], parity, stop));
+    return ok;
+  };
+
+  if (warp < 4) {
+    give_registers<FEW_REGS>();
+    if (warp == 0) {
+      const int total = s_first[n_seq];
+      const CUtensorMap* map = (lane & 1) ? &map_hi : &map_lo;
+      uint32_t k_no = 0;
+      for (int n = 0; ok; ++n) {
+        Item* it = items + (n & 1);
+        if (n >= 2 && !wait_warp(B_ITEM_EMPTY + (n & 1), ((n >> 1) & 1) ^ 1)) break;
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&d.pf_count[0], 1);
+        at = __shfl_sync(FULL, at, 0);
+        if (at >= total) {
+          if (lane == 0) {
+            it->valid = 0;
+            mbar_arrive(&bars[B_ITEM + (n & 1)]);
+          }
+          break;
+        }
+        const int seq = session_of(n_seq, s_first, at), in = at - s_first[seq];
+        if (lane < 16)
+          reinterpret_cast<int*>(&it->si)[lane] = reinterpret_cast<const int*>(d.seq + seq)[lane];
+        __syncwarp();
+        const SeqInfo& si = it->si;
+        const int n_t = (si.t + 2 * TOKENS - 1) / (2 * TOKENS), head = in % H, part = in / H % parts;
+        const int t0 = (n_t - 1 - in / H / parts) * 2 * TOKENS;
+        const int nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1), steps = (nb + PAGES - 1) / PAGES;
+        const int j0 = (int)((int64_t)steps * part / parts), j1 = (int)((int64_t)steps * (part + 1) / parts);
+        if (lane == 0) {
+          it->valid = 1;
+          it->head = head;
+          it->at = t0;
+          it->part = part;
+          it->begin = j0;
+          it->end = j1;
+          mbar_arrive(&bars[B_ITEM + (n & 1)]);
+        }
+        const int32_t* hrow = d.hist_pt + (size_t)si.sid * d.max_pages_per_session;
+        const int32_t* lrow = d.live_pt + (size_t)si.sid * d.max_pages_per_session;
+        auto page_at = [&](int b) { return b < nb ? block_page(si, hrow, lrow, b) : 0; };
+        int pid = page_at(PAGES * j0 + lane), pid_next = page_at(PAGES * j0 + 32 + lane);
+        for (int j = j0; j < j1; ++j, ++k_no) {
+          if (j > j0 && ((j - j0) & 3) == 0) {
+            pid = pid_next;
+            pid_next = page_at(PAGES * j + 32 + lane);
+          }
+          const int page = __shfl_sync(FULL, pid, PAGES * ((j - j0) & 3) + (lane >> 1 & 7));
+          const int n_pg = min(PAGES, nb - PAGES * j), st = k_no % K_RING;
+          if (k_no >= K_RING && !wait_warp(B_EMPTY + st, ((k_no / K_RING) & 1) ^ 1)) break;
+          if (lane == 0) mbar_arrive_expect_tx(&bars[B_FULL + st], n_pg * PS * D * 2);
+          __syncwarp();
+          load_tile(d, layer, 0, head, page, n_pg, s_k + st * SLOT, map, &bars[B_FULL + st], lane);
+        }
+      }
+      for (uint32_t s = k_no > K_RING ? k_no - K_RING : 0; s < k_no; ++s)
+        mbar_wait(d, &bars[B_FULL + s % K_RING], (s / K_RING) & 1);
+    } else if (warp == 1) {
+      if (lane == 0) {
+        constexpr uint32_t ID = instr_desc(KEYS, M, false);
+        const uint32_t a_q = smem_u32(s_q), a_k = smem_u32(s_k);
+        auto wait = [&](int bar, uint32_t parity) {
+          ok = ok && wait_or_stop(d, &bars[bar], parity, stop);
+          return ok;
+        };
+        uint32_t k_no = 0, q_no[2] = {0, 0}, s_no[2] = {0, 0};
+        for (int n = 0; ok; ++n) {
+          if (!wait(B_ITEM + (n & 1), (n >> 1) & 1)) break;
+          const Item& it = items[n & 1];
+          if (!it.valid) break;
+          const int tiles = it.at + TOKENS < it.si.t ? 2 : 1, j0 = it.begin, j1 = it.end;
+          for (int j = j0; j < j1 && ok; ++j, ++k_no) {
+            if (!wait(B_FULL + k_no % K_RING, (k_no / K_RING) & 1)) break;
+            for (int x = 0; x < tiles && ok; ++x) {
+              if (j == j0) {
+                if (!wait(B_Q_FULL + x, q_no[x] & 1)) break;
+                ++q_no[x];
+              }
+              const int b = 2 * x + (s_no[x] & 1);
+              if (s_no[x] >= 2 && !wait(B_S_EMPTY + b, ((s_no[x] >> 1) & 1) ^ 1)) break;
+              ++s_no[x];
+              tc_fence_after();
+              piece_products(tmem + b * KEYS, a_q + 2 * x * SLOT, SLOT, a_k + (k_no % K_RING) * SLOT, 0, ID);
+              tc_commit(&bars[B_S + b]);
+              if (j == j1 - 1) tc_commit(&bars[B_Q_EMPTY + x]);
+            }
+            tc_commit(&bars[B_EMPTY + k_no % K_RING]);
+          }
+          mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
+        }
+        tc_commit(&bars[B_FINAL]);
+        mbar_wait(d, &bars[B_FINAL], 0);
+      }
+    }
+  } else if (warp < 8) {
+    give_registers<FEW_REGS>();
+    const int ts = tid - 4 * 32;
+    uint32_t q_no[2] = {0, 0};
+    for (int n = 0; ok; ++n) {
+      if (!wait_warp(B_ITEM + (n & 1), (n >> 1) & 1)) break;
+      const Item& it = items[n & 1];
+      if (!it.valid) break;
+      const int tiles = it.at + TOKENS < it.si.t ? 2 : 1;
+      for (int x = 0; x < tiles && ok && it.begin < it.end; ++x) {
+        stage_q<2>(d, it.si, it.head, it.at + x * TOKENS, q, qk_scale, s_q + 2 * x * SLOT, ts,
+                   [&] { return q_no[x] == 0 || wait_warp(B_Q_EMPTY + x, (q_no[x] - 1) & 1); });
+        if (!ok) break;
+        ++q_no[x];
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars[B_Q_FULL + x]);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
+    }
+  } else {
+    take_registers<MANY_REGS>();
+    const int x = (warp - 8) >> 2, r = (warp & 3) * 32 + lane;
+    const uint32_t trow = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    uint32_t s_no = 0;
+    for (int n = 0; ok; ++n) {
+      if (!wait_warp(B_ITEM + (n & 1), (n >> 1) & 1)) break;
+      const Item& it = items[n & 1];
+      if (!it.valid) break;
+      const SeqInfo& si = it.si;
+      const int t0 = it.at, tok = t0 + x * TOKENS + r / G;
+      if (t0 + x * TOKENS < si.t) {
+        const int nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1);
+        const int q_log = si.n_hist + si.n_live - si.t + tok;
+        float m = -INFINITY, l = 0.f;
+        for (int j = it.begin; j < it.end; ++j, ++s_no) {
+          const int b = 2 * x + (s_no & 1);
+          if (!wait_warp(B_S + b, (s_no >> 1) & 1)) break;
+          tc_fence_after();
+          float s[KEYS];
+          tmem_ld64(trow + b * KEYS, s);
+          tmem_ld64(trow + b * KEYS + 64, s + 64);
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars[B_S_EMPTY + b]);
+          if (is_edge(si, t0, PAGES * j)) {
+#pragma unroll
+            for (int p = 0; p < PAGES; ++p) {
+              const uint32_t seen = slots_seen(si, PAGES * j + p, nb, q_log);
+#pragma unroll
+              for (int i = 0; i < PS; ++i) s[p * PS + i] = (seen >> i & 1) ? s[p * PS + i] : -INFINITY;
+            }
+          }
+          float m8[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) m8[i] = s[i];
+#pragma unroll
+          for (int i = 8; i < KEYS; i += 8)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) m8[c] = fmaxf(m8[c], s[i + c]);
+          const float mx = fmaxf(fmaxf(fmaxf(m8[0], m8[1]), fmaxf(m8[2], m8[3])),
+                                 fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7])));
+          const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.f : mn;
+          const float2 nref = make_float2(-ref, -ref);
+          float2 rs[4] = {};
+#pragma unroll
+          for (int i = 0; i < KEYS; i += 2) {
+            const float2 y = __fadd2_rn(make_float2(s[i], s[i + 1]), nref);
+            rs[(i / 2) & 3] = __fadd2_rn(rs[(i / 2) & 3], make_float2(ex2(y.x), ex2(y.y)));
+          }
+          const float2 r2 = __fadd2_rn(__fadd2_rn(rs[0], rs[1]), __fadd2_rn(rs[2], rs[3]));
+          l = l * exp2_safe(m, ref) + (r2.x + r2.y);
+          m = mn;
+        }
+        if (ok && tok < si.t)
+          work.stats[((size_t)it.part * d.g->total_tokens + si.q_row0 + tok) * d.q_heads + it.head * G + r % G] =
+              make_float2(m, l);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc(tmem, ALL_COLS);
+  leave_counters(d);
+}
+
+// ---------------------------------------------------------------------------
+// Sums by key: an item is 256 keys (tiles A and B) of one (session, KV head) and a share of the tokens.
+// ---------------------------------------------------------------------------
+constexpr int GROUP_SEQ = 16;        // sessions of a group of the work list
+constexpr int OFF_LSE = OFF_FIRST + 136;
+static_assert(OFF_LSE % 16 == 0 && MAX_SEQ / GROUP_SEQ <= 32 &&
+                  OFF_LSE + LSE_RING * M * 4 <= OFF_TILES, "header fits");
+
+__global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
+    Dev d, int layer, const __grid_constant__ CUtensorMap map_lo,
+    const __grid_constant__ CUtensorMap map_hi, const __nv_bfloat16* __restrict__ q, float qk_scale,
+    int parts, int shares, WeightsWork work) {
+  extern __shared__ __align__(1024) uint8_t smem[];
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem);
+  Item* items = reinterpret_cast<Item*>(smem + OFF_ITEM);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + OFF_TMEM);
+  volatile int* stop = reinterpret_cast<int*>(smem + OFF_STOP);
+  int* s_group = reinterpret_cast<int*>(smem + OFF_FIRST);  // first item of each group of sessions
+  float* s_lse = reinterpret_cast<float*>(smem + OFF_LSE);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = d.kv_heads;
+  uint8_t* s_k = smem + OFF_TILES;
+  uint8_t* s_q = s_k + K_RING * SLOT;   // two tiles of two pieces
+  pdl_wait();
+  pdl_launch_dependents();
+  const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;
+  const int n_groups = (n_seq + GROUP_SEQ - 1) / GROUP_SEQ;
+  auto items_of = [&](int i) {
+    return i < n_seq ? (d.seq[i].n_blocks + 2 * PAGES - 1) / (2 * PAGES) * H * shares : 0;
+  };
+  if (tid == 0) {
+    init_barriers(bars);
+    *stop = 0;
+  }
+  if (warp == 2)
+    first_items(n_groups, lane, s_group, [&](int g) {
+      int n = 0;
+      for (int i = 0; i < GROUP_SEQ; ++i) n += items_of(g * GROUP_SEQ + i);
+      return n;
+    });
+  __syncwarp();
+  if (warp == 1) tmem_alloc(tmem_slot, ALL_COLS);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  bool ok = true;
+  auto wait_warp = [&](int bar, uint32_t parity) {
+    ok = ok && __all_sync(FULL, wait_or_stop(d, &bars[bar], parity, stop));
+    return ok;
+  };
+
+  if (warp < 4) {
+    give_registers<FEW_REGS>();
+    if (warp == 0) {
+      const int total = s_group[n_groups];
+      const CUtensorMap* map = (lane & 1) ? &map_hi : &map_lo;
+      uint32_t k_no = 0;
+      for (int n = 0; ok; ++n) {
+        Item* it = items + (n & 1);
+        if (n >= 2 && !wait_warp(B_ITEM_EMPTY + (n & 1), ((n >> 1) & 1) ^ 1)) break;
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&d.pf_count[0], 1);
+        at = __shfl_sync(FULL, at, 0);
+        if (at >= total) {
+          if (lane == 0) {
+            it->valid = 0;
+            mbar_arrive(&bars[B_ITEM + (n & 1)]);
+          }
+          break;
+        }
+        // Its group of sessions, then the session: lane i has the group's session i.
+        const int group = session_of(n_groups, s_group, at);
+        const int count = lane < GROUP_SEQ ? items_of(group * GROUP_SEQ + lane) : 0;
+        int upto = count;
+#pragma unroll
+        for (int o = 1; o < GROUP_SEQ; o <<= 1) {
+          const int y = __shfl_up_sync(FULL, upto, o);
+          if (lane >= o) upto += y;
+        }
+        const int rest = at - s_group[group];
+        const int mine = __ffs(__ballot_sync(FULL, lane < GROUP_SEQ && rest < upto)) - 1;
+        const int seq = group * GROUP_SEQ + mine;
+        const int in = rest - __shfl_sync(FULL, upto - count, mine);
+        if (lane < 16)
+          reinterpret_cast<int*>(&it->si)[lane] = reinterpret_cast<const int*>(d.seq + seq)[lane];
+        __syncwarp();
+        const SeqInfo& si = it->si;
+        const int head = in % H, share = in / H % shares, b0 = in / H / shares * 2 * PAGES;
+        const int n_t = (si.t + TOKENS - 1) / TOKENS, q_log0 = si.n_hist + si.n_live - si.t;
+        const int first = max(0, block_range(si, b0).base - q_log0) / TOKENS;
+        const int i0 = max((int)((int64_t)n_t * share / shares), first);
+        const int i1 = max(i0, (int)((int64_t)n_t * (share + 1) / shares));
+        if (lane == 0) {
+          it->valid = 1;
+          it->head = head;
+          it->at = b0;
+          it->part = share;
+          it->begin = i0;
+          it->end = i1;
+          mbar_arrive(&bars[B_ITEM + (n & 1)]);
+        }
+        if (i0 == i1) continue;
+        const int32_t* hrow = d.hist_pt + (size_t)si.sid * d.max_pages_per_session;
+        const int32_t* lrow = d.live_pt + (size_t)si.sid * d.max_pages_per_session;
+        const int b = b0 + (lane & 15);
+        const int pid = b < si.n_blocks ? block_page(si, hrow, lrow, b) : 0;
+        for (int x = 0; x < 2 && b0 + x * PAGES < si.n_blocks; ++x, ++k_no) {
+          const int page = __shfl_sync(FULL, pid, PAGES * x + (lane >> 1 & 7));
+          const int n_pg = min(PAGES, si.n_blocks - b0 - x * PAGES), st = k_no % K_RING;
+          if (k_no >= K_RING && !wait_warp(B_EMPTY + st, ((k_no / K_RING) & 1) ^ 1)) break;
+          if (lane == 0) mbar_arrive_expect_tx(&bars[B_FULL + st], n_pg * PS * D * 2);
+          __syncwarp();
+          load_tile(d, layer, 0, head, page, n_pg, s_k + st * SLOT, map, &bars[B_FULL + st], lane);
+        }
+      }
+      for (uint32_t s = k_no > K_RING ? k_no - K_RING : 0; s < k_no; ++s)
+        mbar_wait(d, &bars[B_FULL + s % K_RING], (s / K_RING) & 1);
+    } else if (warp == 1) {
+      if (lane == 0) {
+        const uint32_t a_q = smem_u32(s_q), a_k = smem_u32(s_k);
+        auto wait = [&](int bar, uint32_t parity) {
+          ok = ok && wait_or_stop(d, &bars[bar], parity, stop);
+          return ok;
+        };
+        uint32_t k_no = 0, q_no = 0, s_no[2] = {0, 0};
+        for (int n = 0; ok; ++n) {
+          if (!wait(B_ITEM + (n & 1), (n >> 1) & 1)) break;
+          const Item& it = items[n & 1];
+          if (!it.valid) break;
+          const int tiles = it.at + PAGES < it.si.n_blocks ? 2 : 1, i0 = it.begin, i1 = it.end, t = it.si.t;
+          for (int i = i0; i < i1 && ok; ++i, ++q_no) {
+            if (!wait(B_Q_FULL + (q_no & 1), (q_no >> 1) & 1)) break;
+            const int rows = min(TOKENS, t - i * TOKENS) * G;
+            const uint32_t id = instr_desc((rows + 31) / 32 * 32, M, false);
+            for (int x = 0; x < tiles && ok; ++x) {
+              const uint32_t k = k_no + x;
+              if (i == i0 && !wait(B_FULL + k % K_RING, (k / K_RING) & 1)) break;
+              const int b = 2 * x + (s_no[x] & 1);
+              if (s_no[x] >= 2 && !wait(B_S_EMPTY + b, ((s_no[x] >> 1) & 1) ^ 1)) break;
+              ++s_no[x];
+              tc_fence_after();
+              piece_products(tmem + b * KEYS, a_k + (k % K_RING) * SLOT, 0, a_q + (q_no & 1) * 2 * SLOT, SLOT, id);
+              tc_commit(&bars[B_S + b]);
+              if (i == i1 - 1) tc_commit(&bars[B_EMPTY + k % K_RING]);
+            }
+            tc_commit(&bars[B_Q_EMPTY + (q_no & 1)]);
+          }
+          if (i0 < i1) k_no += tiles;
+          mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
+        }
+        tc_commit(&bars[B_FINAL]);
+        mbar_wait(d, &bars[B_FINAL], 0);
+      }
+    }
+  } else if (warp < 8) {
+    give_registers<FEW_REGS>();
+    const int ts = tid - 4 * 32;
+    uint32_t q_no = 0;
+    const int total = d.g->total_tokens;
+    for (int n = 0; ok; ++n) {
+      if (!wait_warp(B_ITEM + (n & 1), (n >> 1) & 1)) break;
+      const Item& it = items[n & 1];
+      if (!it.valid) break;
+      const SeqInfo& si = it.si;
+      for (int i = it.begin; i < it.end && ok; ++i, ++q_no) {
+        // Row ts of the tile: its parts' (max, sum) joined; rows past the chunk draw nothing.
+        const int tok = i * TOKENS + ts / G;
+        float m = INFINITY, l = 1.f;
+        if (tok < si.t) {
+          const float2* row = work.stats + (size_t)(si.q_row0 + tok) * d.q_heads + it.head * G + ts % G;
+          m = row->x;
+          l = row->y;
+          for (int p = 1; p < parts; ++p) {
+            const float2 o = row[(size_t)p * total * d.q_heads];
+            const float mn = fmaxf(m, o.x);
+            l = l * exp2_safe(m, mn) + o.y * exp2_safe(o.x, mn);
+            m = mn;
+          }
+        }
+        stage_q<2>(d, si, it.head, i * TOKENS, q, qk_scale, s_q + (q_no & 1) * 2 * SLOT, ts,
+                   [&] { return q_no < 2 || wait_warp(B_Q_EMPTY + (q_no & 1), ((q_no >> 1) & 1) ^ 1); });
+        if (!ok) break;
+        if (q_no >= LSE_RING && !wait_warp(B_LSE_EMPTY + q_no % LSE_RING, ((q_no / LSE_RING) & 1) ^ 1)) break;
+        s_lse[(q_no % LSE_RING) * M + ts] = m + log2f(l);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars[B_Q_FULL + (q_no & 1)]);
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
+    }
+  } else {
+    take_registers<MANY_REGS>();
+    const int x = (warp - 8) >> 2, r = (warp & 3) * 32 + lane;
+    const uint32_t trow = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    uint32_t s_no = 0, q_no = 0;
+    for (int n = 0; ok; ++n) {
+      if (!wait_warp(B_ITEM + (n & 1), (n >> 1) & 1)) break;
+      const Item& it = items[n & 1];
+      if (!it.valid) break;
+      const SeqInfo& si = it.si;
+      const int i0 = it.begin, i1 = it.end, blk = it.at + x * PAGES + r / PS, slot = r % PS;
+      const bool alone = it.at + PAGES >= si.n_blocks;  // no tile B: its arrivals are tile A's to make
+      if (it.at + x * PAGES < si.n_blocks) {
+        const BlockRange br = blk < si.n_blocks ? block_range(si, blk) : BlockRange{0, 0, 0};
+        const bool in = slot >= br.lo && slot < br.hi;
+        const int seen_from = in ? br.base + slot - (si.n_hist + si.n_live - si.t) : 0;  // first token
+        float sum = 0.f, rest = 0.f;  // (what additions to the sum rounded off)
+        for (int i = i0; i < i1; ++i, ++s_no, ++q_no) {
+          const int b = 2 * x + (s_no & 1);
+          if (!wait_warp(B_S + b, (s_no >> 1) & 1)) break;
+          tc_fence_after();
+          const float4* lse = reinterpret_cast<const float4*>(s_lse + (q_no % LSE_RING) * M);
+          const int first = seen_from - i * TOKENS;  // first token of the tile that sees the key
+          const bool edge = __any_sync(FULL, first > 0);
+          const int rows = min(TOKENS, si.t - i * TOKENS) * G;
+          float2 a[2] = {};
+#pragma unroll 1
+          for (int c = 0; c < rows; c += 32) {
+            float s[32];
+            tmem_ld32(trow + b * KEYS + c, s);
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {  // a token's four heads
+              const float4 o = lse[c / 4 + g];
+              float2 u = __fadd2_rn(make_float2(s[4 * g], s[4 * g + 1]), make_float2(-o.x, -o.y));
+              float2 v = __fadd2_rn(make_float2(s[4 * g + 2], s[4 * g + 3]), make_float2(-o.z, -o.w));
+              u = make_float2(ex2(u.x), ex2(u.y));
+              v = make_float2(ex2(v.x), ex2(v.y));
+              if (edge && c / 4 + g < first) u = v = make_float2(0.f, 0.f);
+              a[0] = __fadd2_rn(a[0], u);
+              a[1] = __fadd2_rn(a[1], v);
+            }
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(&bars[B_S_EMPTY + b]);
+            mbar_arrive(&bars[B_LSE_EMPTY + q_no % LSE_RING]);
+            if (alone) mbar_arrive(&bars[B_LSE_EMPTY + q_no % LSE_RING]);
+          }
+          const float2 a2 = __fadd2_rn(a[0], a[1]);
+          const float add = (a2.x + a2.y) + rest, to = sum + add;
+          rest = add - (to - sum);
+          sum = to;
+        }
+        if (ok && in) {
+          const int page = block_page(si, d.hist_pt + (size_t)si.sid * d.max_pages_per_session,
+                                      d.live_pt + (size_t)si.sid * d.max_pages_per_session, blk);
+          work.scores[((size_t)(it.head * shares + it.part) * d.n_pages + page) * PS + slot] = sum;
+        }
+      } else {
+        q_no += i1 - i0;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc(tmem, ALL_COLS);
+  leave_counters(d);
+}
+
+}  // namespace
+
+cudaError_t weights_tc_attributes() {
+  const cudaError_t e = cudaFuncSetAttribute(weights_stat_kernel,
+                                             cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+  return e != cudaSuccess ? e
+                          : cudaFuncSetAttribute(weights_sums_kernel,
+                                                 cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
+}
+
+cudaError_t launch_weights_tc(const Dev& d, const Limits& lim, int layer, const void* q,
+                              const WeightsWork& work, int parts, int shares, cudaStream_t s,
+                              int64_t* launches) {
+  CUtensorMap lo, hi;
+  if (!pool_tensor_maps(d, &lo, &hi)) return cudaErrorInvalidValue;
+  const float scale = LOG2E / sqrtf((float)D);
+  const __nv_bfloat16* qt = static_cast<const __nv_bfloat16*>(q);
+  cudaError_t e = launch_ex(&weights_stat_kernel, dim3(lim.sms), dim3(TC_THREADS), SMEM_BYTES, s, true, d,
+                            layer, lo, hi, qt, scale, parts, work);
+  *launches += e == cudaSuccess;
+  if (e != cudaSuccess) return e;
+  e = launch_ex(&weights_sums_kernel, dim3(lim.sms), dim3(TC_THREADS), SMEM_BYTES, s, true, d, layer, lo,
+                hi, qt, scale, parts, shares, work);
+  *launches += e == cudaSuccess;
+  return e;
+}
+
+}  // namespace kvc
