@@ -45,8 +45,8 @@ EncodeTiledFn get_encode() {
 struct PoolMaps {
   const uint8_t* pool = nullptr;
   uint64_t rows = 0;
-  CUtensorMap lo, hi;
-  bool ok = false;
+  CUtensorMap lo, hi, tiles;
+  bool ok = false, tiles_ok = false;
 };
 
 uint64_t pool_rows(const Dev& d) {
@@ -67,7 +67,16 @@ bool make_pool_maps(const Dev& d, PoolMaps& m) {
   CUresult r2 = enc(&m.hi, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, (void*)(d.pool + 128), dims,
                     strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  // Whole (page, head) tiles: columns, rows of an 8-row group, halves of the columns, groups.
+  cuuint64_t t_dims[4] = {64, 8, 2, rows / 8};
+  cuuint64_t t_strides[3] = {(cuuint64_t)PF_D * 2, 128, (cuuint64_t)PF_D * 2 * 8};
+  cuuint32_t t_box[4] = {64, 8, 2, PS / 8};
+  cuuint32_t t_estr[4] = {1, 1, 1, 1};
+  CUresult r3 = enc(&m.tiles, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, (void*)d.pool, t_dims, t_strides,
+                    t_box, t_estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   m.ok = (r1 == CUDA_SUCCESS && r2 == CUDA_SUCCESS);
+  m.tiles_ok = r3 == CUDA_SUCCESS;
   m.pool = d.pool;
   m.rows = rows;
   return m.ok;
@@ -75,15 +84,32 @@ bool make_pool_maps(const Dev& d, PoolMaps& m) {
 
 }  // namespace
 
-bool pool_tensor_maps(const Dev& d, CUtensorMap* lo, CUtensorMap* hi) {
+namespace {
+
+const PoolMaps* pool_maps(const Dev& d) {
   // Keyed on the pool's address and extent: a later context may get the same address
   // for a pool of another shape.
   static thread_local PoolMaps maps;
   if (!maps.ok || maps.pool != d.pool || maps.rows != pool_rows(d)) {
-    if (!make_pool_maps(d, maps)) return false;
+    if (!make_pool_maps(d, maps)) return nullptr;
   }
-  *lo = maps.lo;
-  *hi = maps.hi;
+  return &maps;
+}
+
+}  // namespace
+
+bool pool_tensor_maps(const Dev& d, CUtensorMap* lo, CUtensorMap* hi) {
+  const PoolMaps* maps = pool_maps(d);
+  if (!maps) return false;
+  *lo = maps->lo;
+  *hi = maps->hi;
+  return true;
+}
+
+bool pool_tile_map(const Dev& d, CUtensorMap* tiles) {
+  const PoolMaps* maps = pool_maps(d);
+  if (!maps || !maps->tiles_ok) return false;
+  *tiles = maps->tiles;
   return true;
 }
 

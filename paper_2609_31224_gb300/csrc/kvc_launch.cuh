@@ -205,6 +205,9 @@ cudaError_t launch_attn_prefill_f32(const Dev& d, const Limits& lim, int layer, 
 // 64-127), 16-row boxes, 128-byte swizzle; cached per pool.  False if the driver
 // entry point is missing or the encoding fails.
 bool pool_tensor_maps(const Dev& d, CUtensorMap* lo, CUtensorMap* hi);
+// A 4-D view whose boxes are the 4 KiB of a (page, layer, K or V, head) in one copy: 8-row groups of 1 KiB,
+// 128-byte swizzle, columns 0-63 and 64-127 of a group side by side.  Coordinates (0, 0, 0, row / 8).
+bool pool_tile_map(const Dev& d, CUtensorMap* tiles);
 // Whole prompts (kvc_prompt.cu): chunks of any length, rows in the element type.
 cudaError_t launch_attn_prompt(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
                                int n_seq, int max_t, int pages_max, int64_t pages_sum,

@@ -7,14 +7,16 @@
 // most, first.  A step has four products of 128^3: S_A, S_B (Q K^T) and O_A, O_B += P V; while the
 // softmax of one tile runs, the tensor cores have the other tile's.
 // Warp roles (512 threads):
-//   warp 0      items from the counter; K and V by TMA (128-byte swizzle, a box of 16 rows x 64 columns a
-//               lane) into a ring of five 32 KiB stages, K and V in turn
-//   warp 1      one thread issues the products
+//   warp 0      items from the counter; K and V by TMA, a page's 4 KiB of a head a copy (twice as many of
+//               2 KiB took 2,600 cycles a step for 1,900), into a ring of five 32 KiB stages in turn
+//   warps 1, 2  one thread each issues the products of a tile
 //   warps 4-7   query rows, rotated, scaled and rounded, into shared memory, the next item's as soon as
 //               this one's last score product of the tile is complete; V rows that have to be zero (below)
 //   warps 8-15  softmax, four warps a tile: a thread has one row of S, from tensor memory to registers in
-//               one go, and writes P over it; O is rescaled in tensor memory when the row's maximum has
-//               grown by more than 2^8
+//               one go, and writes P over it.  P is taken against the maximum of the row's first step,
+//               for as long as a step's sum stays below 2^20 (sums and roundings do not depend on the
+//               scale): later steps look for no maximum, and O is rescaled in tensor memory only
+//               when a sum passes that
 // Tensor memory: S_A, S_B (P over the first half of each), O_A, O_B, 128 columns each: all 512.
 //
 // A key that no row of a product may see has P = 0, but 0 times a value that is not finite is not 0.  So
@@ -36,7 +38,12 @@ namespace {
 
 constexpr int RING = 5;
 constexpr int EDGES = 4;
+constexpr int HALF = KEYS / 2;                     // of a step's keys, and of a row's dims
+// 24 warps, 80 registers a thread at launch: issuing and query warps give some to the softmax.
+constexpr int TC_THREADS = 768, BASE_REGS = 80, FEW_REGS = 64, MANY_REGS = 88;
+static_assert(256 * FEW_REGS + 512 * MANY_REGS <= TC_THREADS * BASE_REGS, "registers of the launch");
 constexpr int S_COL = 0, O_COL = 256, ALL_COLS = 512;
+constexpr float SUM_LIMIT = 1048576.f;              // of a step's P in a row: 2^20
 
 enum {
   B_FULL = 0,                    // [RING] a stage has landed
@@ -56,7 +63,7 @@ enum {
   B_FINAL = B_ITEM_EMPTY + 2,    // every product of the CTA complete
   N_BARS = B_FINAL + 1
 };
-constexpr int ITEM_READERS = 1 + 4 + 8;            // warps that arrive at B_ITEM_EMPTY
+constexpr int ITEM_READERS = 2 + 4 + 16;           // warps that arrive at B_ITEM_EMPTY
 
 // What every role knows of an item.
 struct Item {
@@ -71,11 +78,28 @@ constexpr int OFF_BARS = 0;
 constexpr int OFF_ITEM = 512;                      // [2]
 constexpr int OFF_TMEM = OFF_ITEM + 2 * 128;
 constexpr int OFF_STOP = OFF_TMEM + 4;
-constexpr int OFF_FIRST = OFF_STOP + 4;            // [MAX_SEQ + 1] first item of each session
+constexpr int OFF_GROUP = OFF_STOP + 4;            // the work list
+constexpr int OFF_HALF = OFF_GROUP + 136;          // [2 tiles][2 halves][M] what halves of a row exchange
 constexpr int OFF_TILES = 3072;                    // query tiles A, B, then the ring
 constexpr int SMEM_BYTES = OFF_TILES + (2 + RING) * SLOT;
-static_assert(N_BARS * 8 <= OFF_ITEM && OFF_FIRST + (MAX_SEQ + 1) * 4 <= OFF_TILES, "header fits");
+static_assert(N_BARS * 8 <= OFF_ITEM && (GROUPS + 1) * 4 <= 136 && OFF_HALF + 4 * M * 4 <= OFF_TILES,
+              "header fits");
 static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of a CTA");
+
+// Barrier of the two warps that share rows: whether `say` holds in any of their threads.
+__device__ inline bool meet_any(int id, bool say) {
+  int any;
+  __syncwarp();
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.s32 p, %2, 0;\n\t"
+      "barrier.cta.red.or.pred.aligned q, %1, 64, p;\n\t"
+      "selp.s32 %0, 1, 0, q;\n\t}"
+      : "=r"(any)
+      : "r"(id), "r"((int)say)
+      : "memory");
+  return any != 0;
+}
 
 __device__ inline bool not_finite(uint32_t two) {
   return (two & 0x7F80u) == 0x7F80u || (two & 0x7F800000u) == 0x7F800000u;
@@ -113,14 +137,14 @@ __device__ __noinline__ void odd_value(const Dev& d, const SeqInfo& si, int laye
 }
 
 __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
-    Dev d, int layer, const __grid_constant__ CUtensorMap map_lo,
-    const __grid_constant__ CUtensorMap map_hi, const __nv_bfloat16* __restrict__ q,
+    Dev d, int layer, const __grid_constant__ CUtensorMap map,
+    const __nv_bfloat16* __restrict__ q,
     __nv_bfloat16* __restrict__ out, float qk_scale) {
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + OFF_BARS);
   Item* items = reinterpret_cast<Item*>(smem + OFF_ITEM);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + OFF_TMEM);
-  int* s_first = reinterpret_cast<int*>(smem + OFF_FIRST);
+  int* s_group = reinterpret_cast<int*>(smem + OFF_GROUP);
   volatile int* stop = reinterpret_cast<int*>(smem + OFF_STOP);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int H = d.kv_heads;
@@ -131,9 +155,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
   const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;  // (no units: the append failed)
   if (tid == 0) {
     for (int i = 0; i < N_BARS; ++i) {
-      const int count = i >= B_Q_FULL && i < B_Q_EMPTY ? 4
-                        : i >= B_P && i < B_O          ? 4
-                        : i >= B_O_EMPTY && i < B_EDGE ? 4
+      const int count = i >= B_EMPTY && i < B_Q_FULL || i == B_FINAL ? 2
+                        : i >= B_Q_FULL && i < B_Q_EMPTY             ? 4
+                        : i >= B_P && i < B_O          ? 8
+                        : i >= B_O_EMPTY && i < B_EDGE ? 8
                         : i >= B_FIX && i < B_ITEM     ? 4
                         : i >= B_ITEM_EMPTY && i < B_FINAL ? ITEM_READERS
                                                            : 1;
@@ -142,9 +167,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
     fence_mbar_init();
     *stop = 0;
   }
-  // First item of each session: 64-token tiles of its chunk, for each KV head.
-  if (warp == 2)
-    first_items(n_seq, lane, s_first, [&](int i) { return (d.seq[i].t + 2 * TOKENS - 1) / (2 * TOKENS) * H; });
+  // Items of a session: 64-token tiles of its chunk, for each KV head.
+  auto items_of = [&](int i) { return (d.seq[i].t + 2 * TOKENS - 1) / (2 * TOKENS) * H; };
+  if (warp == 3) list_items(n_seq, lane, s_group, items_of);
   __syncwarp();
   if (warp == 1) tmem_alloc(tmem_slot, ALL_COLS);
   tc_fence_before();
@@ -153,12 +178,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
   const uint32_t tmem = *tmem_slot;
 
   if (warp < 4) {
-  give_registers<FEW_REGS>();
+    set_registers<BASE_REGS, FEW_REGS>();
   if (warp == 0) {
     // ---------------- items, K and V ----------------
-    const int total = s_first[n_seq];
-    const int pg = lane >> 1 & 7;
-    const CUtensorMap* map = (lane & 1) ? &map_hi : &map_lo;
+    const int total = s_group[GROUPS];
     uint32_t seq_no = 0, edges = 0;  // stages so far, and V stages of edge steps
     bool ok = true;
     for (int n = 0; ok; ++n) {
@@ -175,7 +198,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
         }
         break;
       }
-      const int seq = session_of(n_seq, s_first, at), in = at - s_first[seq];
+      int in;
+      const int seq = find_item(n_seq, lane, s_group, at, items_of, &in);
       if (lane < 16)
         reinterpret_cast<int*>(&it->si)[lane] = reinterpret_cast<const int*>(d.seq + seq)[lane];
       __syncwarp();
@@ -194,13 +218,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
       const int32_t* hrow = d.hist_pt + (size_t)si.sid * d.max_pages_per_session;
       const int32_t* lrow = d.live_pt + (size_t)si.sid * d.max_pages_per_session;
       auto page_at = [&](int b) { return b < nb ? block_page(si, hrow, lrow, b) : 0; };
+      const EdgeSteps edge = edge_steps(si, t0);
       int pid = page_at(lane), pid_next = page_at(32 + lane);
       for (int j = 0; j < steps && ok; ++j) {
         if (j > 0 && (j & 3) == 0) {
           pid = pid_next;
           pid_next = page_at(PAGES * j + 32 + lane);
         }
-        const int page = __shfl_sync(FULL, pid, PAGES * (j & 3) + pg);
+        const int page = __shfl_sync(FULL, pid, PAGES * (j & 3) + (lane & 7));
         const int n_pg = min(PAGES, nb - PAGES * j);
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv, ++seq_no) {
@@ -210,14 +235,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
             if (!ok) break;
           }
           uint64_t* bar = &bars[B_FULL + st];
-          if (kv == 1 && is_edge(si, t0, PAGES * j)) {
+          if (kv == 1 && edge.at(j)) {
             if (lane == 0) mbar_arrive(bar);
             bar = &bars[B_EDGE + edges % EDGES];
             ++edges;
           }
           if (lane == 0) mbar_arrive_expect_tx(bar, n_pg * PS * D * 2);
           __syncwarp();
-          load_tile(d, layer, kv, head, page, n_pg, s_ring + st * SLOT, map, bar, lane);
+          load_tile(d, layer, kv, head, page, n_pg, s_ring + st * SLOT, &map, bar, lane);
         }
       }
     }
@@ -226,110 +251,107 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
       mbar_wait(d, &bars[B_FULL + s % RING], (s / RING) & 1);
     for (uint32_t e = edges > EDGES ? edges - EDGES : 0; e < edges; ++e)
       mbar_wait(d, &bars[B_EDGE + e % EDGES], (e / EDGES) & 1);
-  } else if (warp == 1) {
-    // ---------------- products ----------------
+  } else if (warp < 3) {
+    // ---------------- products: one thread a tile ----------------
     if (lane == 0) {
       constexpr uint32_t ID_S = instr_desc(KEYS, M, false), ID_O = instr_desc(D, M, true);
-      const uint32_t a_q = smem_u32(s_q), a_ring = smem_u32(s_ring);
+      const int x = warp - 1;
+      const uint32_t t_s = tmem + S_COL + x * KEYS, t_o = tmem + O_COL + x * D;
+      const uint64_t qd = desc_columns(smem_u32(s_q) + x * SLOT);
+      const uint64_t kd0 = desc_columns(smem_u32(s_ring)), vd0 = desc_rows(smem_u32(s_ring));
       bool ok = true;
       auto wait = [&](int bar, uint32_t parity) {
         ok = ok && wait_or_stop(d, &bars[bar], parity, stop);
         return ok;
       };
-      // S_x = Q_x K^T of stage `s` (a count of stages).
-      auto scores = [&](int x, uint32_t s) {
-        const uint64_t qd = smem_desc(a_q + x * SLOT, 0, 1024);
-        const uint64_t kd = smem_desc(a_ring + (s % RING) * SLOT, 0, 1024);
+      // Stages are counted on: `st` is the ring's slot of the next one, `pass` its pass over the ring.
+      int st = 0;
+      uint32_t pass = 0, edges = 0, p_no = 0, q_no = 0, o_no = 0;
+      auto full = [&] { return wait(B_FULL + st, pass & 1); };
+      auto next = [&] {
+        if (++st == RING) {
+          st = 0;
+          ++pass;
+        }
+      };
+      // S = Q K^T of the next stage; the last one of an item frees its query rows.
+      auto scores = [&](bool last) {
+        if (!full()) return;
+        tc_fence_after();
+        const uint64_t kd = desc_at(kd0, st * SLOT);
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) {
-          const uint32_t at = (kk >> 2) * PANEL + (kk & 3) * 32;
-          tc_mma_ss(tmem + S_COL + x * KEYS, desc_at(qd, at), desc_at(kd, at), ID_S, kk > 0);
+          const uint32_t at = step_columns(kk);
+          tc_mma_ss(t_s, desc_at(qd, at), desc_at(kd, at), ID_S, kk > 0);
         }
         tc_commit(&bars[B_S + x]);
+        if (last) tc_commit(&bars[B_Q_EMPTY + x]);
+        tc_commit(&bars[B_EMPTY + st]);
+        next();
       };
-      auto outputs = [&](int x, uint32_t s, bool first) {
-        const uint64_t vd = smem_desc(a_ring + (s % RING) * SLOT, PANEL, 1024);
-#pragma unroll
-        for (int kk = 0; kk < KEYS / 16; ++kk)
-          tc_mma_ts(tmem + O_COL + x * D, tmem + S_COL + x * KEYS + kk * 8, desc_at(vd, kk * 16 * 128),
-                    ID_O, !first || kk > 0);
+      // A stage that this tile has no use for.
+      auto skip = [&] {
+        if (!full()) return;
+        mbar_arrive(&bars[B_EMPTY + st]);
+        next();
       };
-      auto full = [&](uint32_t s) { return wait(B_FULL + s % RING, (s / RING) & 1); };
-      uint32_t s0 = 0;                       // stages before this item
-      uint32_t p_no[2] = {0, 0};             // steps of a tile so far
-      uint32_t q_no[2] = {0, 0};             // items of a tile whose scores have begun
-      uint32_t o_no[2] = {0, 0};             // and whose output has
-      uint32_t edges = 0;
-      // The first scores of item n, tile x: its K is stage s.
-      auto begin = [&](int x, uint32_t s, int steps) {
-        if (!wait(B_Q_FULL + x, q_no[x] & 1) || !full(s)) return;
-        ++q_no[x];
-        tc_fence_after();
-        scores(x, s);
-        if (steps == 1) tc_commit(&bars[B_Q_EMPTY + x]);
+      auto begin = [&](int steps, bool mine) {
+        if (!mine) return skip();
+        if (!wait(B_Q_FULL + x, q_no & 1)) return;
+        ++q_no;
+        scores(steps == 1);
       };
-      int n = 0;
-      if (!wait(B_ITEM, 0)) n = -1;
-      int steps = ok ? items[0].steps : 0;
-      bool two = steps > 0 && items[0].t0 + TOKENS < items[0].si.t;
-      if (steps > 0) {
-        begin(0, 0, steps);
-        if (ok && two) begin(1, 0, steps);
-        tc_commit(&bars[B_EMPTY + 0]);
-      }
-      while (ok && steps > 0) {
-        const Item& it = items[n & 1];
-        const SeqInfo& si = it.si;
-        const int t0 = it.t0;
-        int steps_next = 0;
-        bool two_next = false;
-        for (int j = 0; j < steps && ok; ++j) {
-          const uint32_t sv = s0 + 2 * j + 1, sk = sv + 1;  // V of this step, K of the next one
-          const bool last = j == steps - 1;
-          if (last) {
-            if (!wait(B_ITEM + ((n + 1) & 1), ((n + 1) >> 1) & 1)) break;
-            const Item& nx = items[(n + 1) & 1];
-            steps_next = nx.steps;
-            two_next = steps_next > 0 && nx.t0 + TOKENS < nx.si.t;
-          }
-          if (!full(sv)) break;
-          if (is_edge(si, t0, PAGES * j)) {
-            if (!wait(B_FIX + edges % EDGES, (edges / EDGES) & 1)) break;
-            ++edges;
-          }
-          for (int x = 0; x < 2 && ok; ++x) {
-            if (x == 0 || two) {
-              if (!wait(B_P + x, p_no[x] & 1)) break;
-              ++p_no[x];
+      if (wait(B_ITEM, 0)) {
+        int steps = items[0].steps;
+        bool mine = x == 0 || (steps > 0 && items[0].t0 + TOKENS < items[0].si.t);
+        if (steps > 0) begin(steps, mine);
+        for (int n = 0; ok && steps > 0; ++n) {
+          const Item& it = items[n & 1];
+          const EdgeSteps edge = edge_steps(it.si, it.t0);
+          int steps_next = 0;
+          bool mine_next = false;
+          for (int j = 0; j < steps && ok; ++j) {
+            const bool last = j == steps - 1;
+            if (!full()) break;
+            if (edge.at(j)) {
+              if (!wait(B_FIX + edges % EDGES, (edges / EDGES) & 1)) break;
+              ++edges;
+            }
+            if (mine) {
+              if (!wait(B_P + x, p_no & 1)) break;
+              ++p_no;
               if (j == 0) {
-                if (o_no[x] > 0 && !wait(B_O_EMPTY + x, (o_no[x] - 1) & 1)) break;
-                ++o_no[x];
+                if (o_no > 0 && !wait(B_O_EMPTY + x, (o_no - 1) & 1)) break;
+                ++o_no;
               }
               tc_fence_after();
-              outputs(x, sv, j == 0);
+              const uint64_t vd = desc_at(vd0, st * SLOT);
+#pragma unroll
+              for (int kk = 0; kk < KEYS / 16; ++kk)
+                tc_mma_ts(t_o, t_s + (kk >> 2) * HALF + (kk & 3) * 8, desc_at(vd, kk * 2 * ROW_GROUP), ID_O, j > 0 || kk > 0);
               if (last) tc_commit(&bars[B_O + x]);
+              tc_commit(&bars[B_EMPTY + st]);
+            } else {
+              mbar_arrive(&bars[B_EMPTY + st]);
             }
-            if (x == (two ? 1 : 0)) tc_commit(&bars[B_EMPTY + sv % RING]);
+            next();
             if (!last) {
-              if (x == 0 || two) {
-                if (!full(sk)) break;
-                tc_fence_after();
-                scores(x, sk);
-                if (j + 2 == steps) tc_commit(&bars[B_Q_EMPTY + x]);
-              }
-              if (x == (two ? 1 : 0)) tc_commit(&bars[B_EMPTY + sk % RING]);
-            } else if (steps_next > 0) {
-              if (x == 0 || two_next) begin(x, sk, steps_next);
-              if (x == (two_next ? 1 : 0)) tc_commit(&bars[B_EMPTY + sk % RING]);
+              if (mine) scores(j + 2 == steps);
+              else skip();
+            } else {
+              // The next item's first scores go ahead of this one's output.
+              if (!wait(B_ITEM + ((n + 1) & 1), ((n + 1) >> 1) & 1)) break;
+              const Item& nx = items[(n + 1) & 1];
+              steps_next = nx.steps;
+              mine_next = x == 0 || (steps_next > 0 && nx.t0 + TOKENS < nx.si.t);
+              if (steps_next > 0) begin(steps_next, mine_next);
             }
           }
+          if (!ok) break;
+          mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
+          steps = steps_next;
+          mine = mine_next;
         }
-        if (!ok) break;
-        mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
-        s0 += 2 * steps;
-        steps = steps_next;
-        two = two_next;
-        ++n;
       }
       // No product may still be running when the tensor memory is released.
       tc_commit(&bars[B_FINAL]);
@@ -337,7 +359,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
     }
   }
   } else if (warp < 8) {
-    give_registers<FEW_REGS>();
+    set_registers<BASE_REGS, FEW_REGS>();
     // ---------------- query rows, V rows to zero ----------------
     const int ts = tid - 4 * 32;
     bool ok = true;
@@ -354,7 +376,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
       const int head = it.head, t0 = it.t0, steps = it.steps;
       const int tiles = t0 + TOKENS < si.t ? 2 : 1;
       for (int x = 0; x < tiles && ok; ++x) {
-        stage_q<1>(d, si, head, t0 + x * TOKENS, q, qk_scale, s_q + x * SLOT, ts,
+        stage_q<1, 2>(d, si, head, t0 + x * TOKENS, q, qk_scale, s_q + x * SLOT, ts,
                    [&] { return q_no[x] == 0 || wait(B_Q_EMPTY + x, (q_no[x] - 1) & 1); });
         if (!ok) break;
         ++q_no[x];
@@ -365,18 +387,19 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
       // Thread ts has row ts of each such step's V.
       const int nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1);
       const int q_log0 = si.n_hist + si.n_live - si.t;
+      const EdgeSteps edge = edge_steps(si, t0);
       for (int j = 0; j < steps && ok; ++j) {
         const int b = PAGES * j + ts / PS;
-        if (!is_edge(si, t0, PAGES * j)) continue;
+        if (!edge.at(j)) continue;
         const uint32_t s = s0 + 2 * j + 1;
         if (!wait(B_EDGE + edges % EDGES, (edges / EDGES) & 1)) break;
-        uint8_t* row = s_ring + (s % RING) * SLOT + ts * 128;
+        uint8_t* tile = s_ring + (s % RING) * SLOT;
         const uint32_t bit = 1u << (ts % PS);
         bool zero = !(slots_seen(si, b, nb, q_log0 + si.t) & bit);
         if (!zero && !(slots_seen(si, b, nb, q_log0 + t0) & bit)) {  // some rows see it
           bool odd = false;
           for (int i = 0; i < 16; ++i) {
-            const uint4 v = *reinterpret_cast<const uint4*>(row + (i >> 3) * PANEL + ((i & 7) ^ (ts & 7)) * 16);
+            const uint4 v = *reinterpret_cast<const uint4*>(tile + tile_at(ts, i));
             odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
           }
           if (odd) {
@@ -386,7 +409,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
         }
         if (zero)
           for (int i = 0; i < 16; ++i)
-            *reinterpret_cast<uint4*>(row + (i >> 3) * PANEL + ((i & 7) ^ (ts & 7)) * 16) = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4*>(tile + tile_at(ts, i)) = make_uint4(0, 0, 0, 0);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars[B_FIX + edges % EDGES]);
@@ -397,20 +420,26 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
       if (lane == 0) mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
     }
   } else {
-    take_registers<MANY_REGS>();
+    set_registers<BASE_REGS, MANY_REGS>();
     // ---------------- softmax ----------------
-    const int x = (warp - 8) >> 2;             // tile
-    const int r = (warp & 3) * 32 + lane;      // row
-    const uint32_t trow = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    const uint32_t t_s = trow + S_COL + x * KEYS, t_o = trow + O_COL + x * D;
+    const int x = (warp - 8) >> 3, half = (warp - 8) >> 2 & 1;  // tile; keys [64 half, + 64) of a step
+    const int quarter = warp & 3, r = quarter * 32 + lane;      // row
+    const uint32_t trow = tmem + ((uint32_t)(quarter * 32) << 16);
+    const uint32_t t_s = trow + S_COL + x * KEYS + half * HALF, t_o = trow + O_COL + x * D + half * HALF;
+    float* mine = reinterpret_cast<float*>(smem + OFF_HALF) + (2 * x + half) * M + r;
+    const float* other = reinterpret_cast<float*>(smem + OFF_HALF) + (2 * x + (half ^ 1)) * M + r;
+    const int meet = 1 + x * 4 + quarter;                       // barrier of the two warps of a row
     bool ok = true;
     auto wait = [&](int bar, uint32_t parity) {
       ok = ok && __all_sync(FULL, wait_or_stop(d, &bars[bar], parity, stop));
       return ok;
     };
     uint32_t s_no = 0, o_no = 0;
-    for (int n = 0; ok; ++n) {
-      if (!wait(B_ITEM + (n & 1), (n >> 1) & 1)) break;
+    // A warp whose wait gave up goes on to the item's end without waiting or writing results, so that
+    // its partner never waits for it alone; then both stop.
+    for (int n = 0;; ++n) {
+      wait(B_ITEM + (n & 1), (n >> 1) & 1);
+      if (meet_any(meet, !ok)) break;
       const Item& it = items[n & 1];
       const int steps = it.steps;
       if (steps == 0) break;
@@ -419,88 +448,110 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
       if (t0 + x * TOKENS < si.t) {
         const int nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1);
         const int q_log = si.n_hist + si.n_live - si.t + tok;
-        float m = -INFINITY, l = 0.f;
+        const EdgeSteps edge = edge_steps(si, t0);
+        float m = 0.f, l = 0.f;
         for (int j = 0; j < steps; ++j, ++s_no) {
-          if (!wait(B_S + x, s_no & 1)) break;
+          wait(B_S + x, s_no & 1);
           tc_fence_after();
-          float s[KEYS];
-          tmem_ld64(t_s, s);
-          tmem_ld64(t_s + 64, s + 64);
-          if (is_edge(si, t0, PAGES * j)) {
+          float s[HALF];
+          auto load = [&] {
+            tmem_ld32(t_s, s);
+            tmem_ld32(t_s + 32, s + 32);
+            if (edge.at(j)) {
 #pragma unroll
-            for (int p = 0; p < PAGES; ++p) {
-              const uint32_t seen = slots_seen(si, PAGES * j + p, nb, q_log);
+              for (int p = 0; p < PAGES / 2; ++p) {
+                const uint32_t seen = slots_seen(si, PAGES * j + PAGES / 2 * half + p, nb, q_log);
 #pragma unroll
-              for (int i = 0; i < PS; ++i) s[p * PS + i] = (seen >> i & 1) ? s[p * PS + i] : -INFINITY;
+                for (int i = 0; i < PS; ++i) s[p * PS + i] = (seen >> i & 1) ? s[p * PS + i] : -INFINITY;
+              }
             }
+          };
+          // P = 2^(s - m), which goes over this half's S, and its sum.
+          float add = 0.f;
+          auto weigh = [&](bool check) {
+            uint32_t pw[HALF / 2];
+            const float2 nref = make_float2(-m, -m);
+            float2 rs[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+            for (int i = 0; i < HALF; i += 2) {
+              const float2 y = __fadd2_rn(make_float2(s[i], s[i + 1]), nref);
+              const float2 p = make_float2(ex2(y.x), ex2(y.y));
+              rs[(i / 2) & 1] = __fadd2_rn(rs[(i / 2) & 1], p);
+              pw[i / 2] = pack_bf16(p.x, p.y);
+            }
+            const float2 r2 = __fadd2_rn(rs[0], rs[1]);
+            add = r2.x + r2.y;
+            if (check && meet_any(meet, !(add < SUM_LIMIT))) return false;
+            __syncwarp();
+            tmem_st32(t_s, pw);
+            return true;
+          };
+          // The first step, and one where a sum is out of bounds against the reference so far (or NaN):
+          // the row's maximum becomes the reference.  (The scores' barrier says that the products
+          // before them are complete too, the last O += P V among them, so O may be rescaled.)
+          bool done = false;
+          if (j > 0) {
+            load();
+            done = weigh(true);
           }
-          float m8[8];
+          if (!done) {
+            load();
+            float m4[4];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) m8[i] = s[i];
+            for (int i = 0; i < 4; ++i) m4[i] = s[i];
 #pragma unroll
-          for (int i = 8; i < KEYS; i += 16)
+            for (int i = 4; i < HALF; i += 4)
 #pragma unroll
-            for (int c = 0; c < 8; ++c)
-              m8[c] = i + 8 < KEYS ? fmaxf(fmaxf(m8[c], s[i + c]), s[i + 8 + c]) : fmaxf(m8[c], s[i + c]);
-          const float mx = fmaxf(fmaxf(fmaxf(m8[0], m8[1]), fmaxf(m8[2], m8[3])),
-                                 fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7])));
-          // The scores' barrier says that the products before them are complete too, the last O += P V
-          // among them, so O may be rescaled.
-          const bool need = mx > m + RESCALE_LOG2;
-          if (__any_sync(FULL, need && j > 0)) {
-            const float f = need ? exp2_safe(m, mx) : 1.f;
-            l *= f;
+              for (int c = 0; c < 4; ++c) m4[c] = fmaxf(m4[c], s[i + c]);
+            *mine = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            meet_any(meet, false);
+            const float mx = fmaxf(*mine, *other);
+            const float to = j == 0 ? (mx == -INFINITY ? 0.f : mx) : fmaxf(m, mx);
+            if (j > 0) {
+              const float f = exp2f(m - to);
+              l *= f;
+              __syncwarp();
 #pragma unroll 1
-            for (int c = 0; c < D / 16; ++c) {
-              float o[16];
-              tmem_ld16(t_o + c * 16, o);
+              for (int c = 0; c < HALF / 16; ++c) {
+                float o[16];
+                tmem_ld16(t_o + c * 16, o);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) o[i] *= f;
-              tmem_st16(t_o + c * 16, o);
+                for (int i = 0; i < 16; ++i) o[i] *= f;
+                tmem_st16(t_o + c * 16, o);
+              }
             }
+            m = to;
+            weigh(false);
           }
-          if (need) m = mx;
-          const float ref = m == -INFINITY ? 0.f : m;  // (a row that has seen no key yet)
-          const float2 nref = make_float2(-ref, -ref);
-          float2 rs[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f),
-                          make_float2(0.f, 0.f)};
-          uint32_t pw[KEYS / 2];
-#pragma unroll
-          for (int i = 0; i < KEYS; i += 2) {
-            const float2 y = __fadd2_rn(make_float2(s[i], s[i + 1]), nref);
-            const float2 p = make_float2(ex2(y.x), ex2(y.y));
-            rs[(i / 2) & 3] = __fadd2_rn(rs[(i / 2) & 3], p);
-            pw[i / 2] = pack_bf16(p.x, p.y);
-          }
-          const float2 r2 = __fadd2_rn(__fadd2_rn(rs[0], rs[1]), __fadd2_rn(rs[2], rs[3]));
-          l += r2.x + r2.y;
-          __syncwarp();
-          tmem_st32(t_s, pw);
-          tmem_st32(t_s + 32, pw + 32);
+          l += add;
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(&bars[B_P + x]);
         }
-        if (!ok || !wait(B_O + x, o_no & 1)) break;
+        // The row's sum, then dims [64 half, + 64) of its output.
+        wait(B_O + x, o_no & 1);
         ++o_no;
         tc_fence_after();
-        const float inv = 1.f / l;
+        *mine = l;
+        meet_any(meet, false);
+        const float inv = 1.f / (l + *other);
+        meet_any(meet, false);  // (read before the next item's exchange)
         const bool odd = *reinterpret_cast<volatile const int*>(&it.odd) != 0;
-        __nv_bfloat16* row = out + ((size_t)(si.q_row0 + tok) * d.q_heads + it.head * G + r % G) * D;
+        __nv_bfloat16* row = out + ((size_t)(si.q_row0 + tok) * d.q_heads + it.head * G + r % G) * D + half * HALF;
 #pragma unroll 1
-        for (int c = 0; c < D / 32; ++c) {
+        for (int c = 0; c < HALF; c += 32) {
           float o[32];
-          tmem_ld32(t_o + c * 32, o);
+          tmem_ld32(t_o + c, o);
           if (odd && tok < si.t) {
             float more[32];
-            odd_value(d, si, layer, it.head, t0, tok, r % G, q, qk_scale, m == -INFINITY ? 0.f : m, c * 32, more);
+            odd_value(d, si, layer, it.head, t0, tok, r % G, q, qk_scale, m, half * HALF + c, more);
 #pragma unroll
             for (int i = 0; i < 32; ++i) o[i] += more[i];
           }
-          if (tok < si.t) {
+          if (ok && tok < si.t) {
 #pragma unroll
             for (int i = 0; i < 32; i += 8)
-              *reinterpret_cast<uint4*>(row + c * 32 + i) =
+              *reinterpret_cast<uint4*>(row + c + i) =
                   make_uint4(pack_bf16(o[i] * inv, o[i + 1] * inv), pack_bf16(o[i + 2] * inv, o[i + 3] * inv),
                              pack_bf16(o[i + 4] * inv, o[i + 5] * inv), pack_bf16(o[i + 6] * inv, o[i + 7] * inv));
           }
@@ -535,10 +586,10 @@ cudaError_t prompt_tc_attributes() {
 
 cudaError_t launch_prompt_tc(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
                              cudaStream_t s) {
-  CUtensorMap lo, hi;
-  if (!pool_tensor_maps(d, &lo, &hi)) return cudaErrorInvalidValue;
+  CUtensorMap map;
+  if (!pool_tile_map(d, &map)) return cudaErrorInvalidValue;
   return launch_ex(&prompt_tc_kernel, dim3(lim.sms), dim3(TC_THREADS), SMEM_BYTES, s, true, d,
-                   layer, lo, hi, static_cast<const __nv_bfloat16*>(q), static_cast<__nv_bfloat16*>(out),
+                   layer, map, static_cast<const __nv_bfloat16*>(q), static_cast<__nv_bfloat16*>(out),
                    LOG2E / sqrtf((float)D));
 }
 

@@ -10,11 +10,19 @@ namespace {
 
 constexpr int KEYS = 128, PAGES = KEYS / PS;       // of a step
 constexpr int TOKENS = 32;                         // of a tile
-constexpr int PANEL = KEYS * 128;                  // 128 rows x 64 columns
-constexpr int SLOT = 2 * PANEL;                    // a tile: 32 KiB
-constexpr int TC_THREADS = 512;
-constexpr int FEW_REGS = 96, MANY_REGS = 160;      // 256 threads each: what 128 a thread make together
-
+constexpr int SLOT = KEYS * D * 2;                 // a tile: 32 KiB
+// A tile is 16 groups of 8 rows; a group holds columns 0-63, then 64-127 of its rows, 1 KiB each with
+// 128-byte swizzle: what one copy brings of a page (16 rows) is then 4 KiB of the tile as it stands.
+constexpr int ATOM = 1024, ROW_GROUP = 2 * ATOM;
+// Byte offset in a tile of 16-byte chunk c (0 .. 15) of row r.
+__device__ inline uint32_t tile_at(int r, int c) {
+  return (r >> 3) * ROW_GROUP + (c >> 3) * ATOM + (r & 7) * 128 + (((c & 7) ^ (r & 7)) << 4);
+}
+// Descriptors of a tile as an operand whose K dimension is its columns (K-major), and whose K dimension
+// is its rows (MN-major); the 16 columns or rows of a step lie step_columns(kk) or 2 ROW_GROUP kk on.
+__device__ inline uint64_t desc_columns(uint32_t tile) { return smem_desc(tile, 0, ROW_GROUP); }
+__device__ inline uint64_t desc_rows(uint32_t tile) { return smem_desc(tile, ATOM, ROW_GROUP); }
+__host__ __device__ constexpr uint32_t step_columns(int kk) { return (kk >> 2) * ATOM + (kk & 3) * 32; }
 __device__ inline void tc_mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
                                  uint32_t accumulate) {
   asm volatile(
@@ -24,20 +32,18 @@ __device__ inline void tc_mma_ss(uint32_t d_tmem, uint64_t a_desc, uint64_t b_de
       "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-__device__ inline void tma_load_2d(void* dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
+__device__ inline void tma_load_tile(void* dst, const CUtensorMap* map, int group, uint64_t* bar) {
   asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%2, %3}], [%4];" ::"r"(smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_u32(bar))
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %2, %2, %3}], [%4];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(group), "r"(smem_u32(bar))
       : "memory");
 }
-template <int N>
-__device__ inline void give_registers() {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
-}
-template <int N>
-__device__ inline void take_registers() {
-  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+// To N registers a thread from the launch's BASE (a whole warpgroup).
+template <int BASE, int N>
+__device__ inline void set_registers() {
+  if constexpr (N < BASE) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+  if constexpr (N > BASE) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
 }
 
 // Bounded wait that also ends when another warp has given up.
@@ -60,14 +66,16 @@ __device__ inline int blocks_seen(const SeqInfo& si, int tok) {
   return si.n_hist_pages + (si.live_head + si.n_live - si.t + tok) / PS + 1;
 }
 
-// Whether a step (blocks [b0, b0 + PAGES)) has slots that some row of the item starting at token t0 does
-// not see: a partly filled page, pages past the end, keys behind the item's first token.
-__device__ inline bool is_edge(const SeqInfo& si, int t0, int b0) {
+// Steps (of PAGES blocks) with slots that some row of the item starting at token t0 does not see: a
+// partly filled page, pages past the end, keys behind the item's first token.
+struct EdgeSteps {
+  int diag, hist, live;
+  __device__ bool at(int j) const { return j >= diag || j == hist || j == live; }
+};
+__device__ inline EdgeSteps edge_steps(const SeqInfo& si, int t0) {
   const int nhp = si.n_hist_pages;
-  const int first = nhp + (si.live_head + si.n_live - si.t + t0) / PS;  // block of the first token
-  if (b0 + PAGES > first) return true;
-  const int b_hist = (si.n_hist % PS) ? nhp - 1 : -1, b_live = si.live_head ? nhp : -1;
-  return (b_hist >= b0 && b_hist < b0 + PAGES) || (b_live >= b0 && b_live < b0 + PAGES);
+  return {(nhp + (si.live_head + si.n_live - si.t + t0) / PS) / PAGES,
+          (si.n_hist % PS) ? (nhp - 1) / PAGES : -1, si.live_head ? nhp / PAGES : -1};
 }
 
 // Slots [lo, hi) of block b that hold a position with index <= q_log.
@@ -81,32 +89,32 @@ __device__ inline uint32_t slots_seen(const SeqInfo& si, int b, int n_blocks, in
 // Query rows of tokens [t0, t0 + TOKENS) of one KV head by the 128 threads `ts`: rotated, scaled and
 // rounded into the swizzled tile at `to`; PIECES = 2: what rounding left, rounded too, into the tile
 // behind it.  Rows past the chunk are zero.  `free` waits until the tile may be written (false: give up).
-// A thread takes 16-byte chunks c and c + 8 (which rotate together) of a token's G rows.
-template <int PIECES, typename FreeFn>
+// A thread takes 16-byte chunks c and c + 8 (which rotate together) of a token's G rows, HEADS at a time.
+template <int PIECES, int HEADS, typename FreeFn>
 __device__ inline void stage_q(const Dev& d, const SeqInfo& si, int head, int t0, const __nv_bfloat16* q,
                                float qk_scale, uint8_t* to, int ts, FreeFn free) {
   const int c = ts & 7;
 #pragma unroll 1
-  for (int h = 0; h < 2; ++h) {
-    const int tl = (ts >> 3) + 16 * h, tok = t0 + tl;
-    uint4 a[G], b[G];
+  for (int step = 0; step < 2 * G / HEADS; ++step) {
+    const int tl = (ts >> 3) + 16 * (step / (G / HEADS)), g0 = step % (G / HEADS) * HEADS, tok = t0 + tl;
+    uint4 a[HEADS], b[HEADS];
     float4 cs[4];
     const bool in = tok < si.t;
     if (in) {
       const uint4* row = reinterpret_cast<const uint4*>(
-          q + ((size_t)(si.q_row0 + tok) * d.q_heads + head * G) * D) + c;
+          q + ((size_t)(si.q_row0 + tok) * d.q_heads + head * G + g0) * D) + c;
       const float4* t4 = reinterpret_cast<const float4*>(d.rope + (size_t)(si.pos_first + tok) * (D / 2) + c * 8);
 #pragma unroll
-      for (int g = 0; g < G; ++g) {
+      for (int g = 0; g < HEADS; ++g) {
         a[g] = row[g * 16];
         b[g] = row[g * 16 + 8];
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) cs[e] = t4[e];
     }
-    if (h == 0 && !free()) return;
+    if (step == 0 && !free()) return;
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
+    for (int g = 0; g < HEADS; ++g) {
       uint32_t ya[PIECES][4] = {}, yb[PIECES][4] = {};
       if (in) {
         const uint32_t ua[4] = {a[g].x, a[g].y, a[g].z, a[g].w};
@@ -126,54 +134,61 @@ __device__ inline void stage_q(const Dev& d, const SeqInfo& si, int head, int t0
           }
         }
       }
-      const int r = tl * G + g;
+      const int r = tl * G + g0 + g;
 #pragma unroll
       for (int p = 0; p < PIECES; ++p) {
-        uint8_t* at = to + p * SLOT + r * 128 + ((c ^ (r & 7)) << 4);
+        uint8_t* at = to + p * SLOT + tile_at(r, c);
         *reinterpret_cast<uint4*>(at) = make_uint4(ya[p][0], ya[p][1], ya[p][2], ya[p][3]);
-        *reinterpret_cast<uint4*>(at + PANEL) = make_uint4(yb[p][0], yb[p][1], yb[p][2], yb[p][3]);
+        *reinterpret_cast<uint4*>(at + ATOM) = make_uint4(yb[p][0], yb[p][1], yb[p][2], yb[p][3]);
       }
     }
   }
 }
 
-// First item of each session, and the number of all behind the last: sums of count(session) (one warp).
+// Work lists: a session has count(session) items.  s_group holds the first item of each group of 16
+// sessions, and the number of all behind the last.
+constexpr int GROUP_SEQ = 16;
+constexpr int GROUPS = MAX_SEQ / GROUP_SEQ;
+static_assert(GROUPS <= 32, "a lane a group");
+
 template <typename CountFn>
-__device__ inline void first_items(int n_seq, int lane, int* first, CountFn count) {
-  int sum = 0;
-  for (int i0 = 0; i0 < n_seq; i0 += 32) {
-    const int i = i0 + lane, n = i < n_seq ? count(i) : 0;
-    int x = n;
+__device__ inline void list_items(int n_seq, int lane, int* s_group, CountFn count) {  // one warp
+  int n = 0;
+  for (int i = lane * GROUP_SEQ; i < min(n_seq, (lane + 1) * GROUP_SEQ); ++i) n += count(i);
+  int upto = n;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(FULL, x, o);
-      if (lane >= o) x += y;
-    }
-    if (i < n_seq) first[i] = sum + x - n;
-    sum += __shfl_sync(FULL, x, 31);
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(FULL, upto, o);
+    if (lane >= o) upto += y;
   }
-  if (lane == 0) first[n_seq] = sum;
+  if (lane < GROUPS) s_group[lane] = upto - n;
+  if (lane == 31) s_group[GROUPS] = upto;
 }
 
-// Session that item `at` belongs to.
-__device__ inline int session_of(int n_seq, const int* first, int at) {
-  int lo = 0, hi = n_seq - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (first[mid] <= at) lo = mid;
-    else hi = mid - 1;
+// Session of item `at`, and which of the session's items it is (one warp).
+template <typename CountFn>
+__device__ inline int find_item(int n_seq, int lane, const int* s_group, int at, CountFn count, int* which) {
+  const unsigned before = __ballot_sync(FULL, lane < GROUPS && s_group[min(lane, GROUPS)] <= at);
+  const int group = 31 - __clz(before);
+  const int i = group * GROUP_SEQ + lane, n = lane < GROUP_SEQ && i < n_seq ? count(i) : 0;
+  int upto = n;
+#pragma unroll
+  for (int o = 1; o < GROUP_SEQ; o <<= 1) {
+    const int y = __shfl_up_sync(FULL, upto, o);
+    if (lane >= o) upto += y;
   }
-  return lo;
+  const int rest = at - s_group[group];
+  const int mine = __ffs(__ballot_sync(FULL, lane < GROUP_SEQ && rest < upto)) - 1;
+  *which = rest - __shfl_sync(FULL, upto - n, mine);
+  return group * GROUP_SEQ + mine;
 }
 
-// Boxes of a tile of up to PAGES pages (16 rows x 64 columns each) by lanes 0 .. 15 of a warp: lane
-// 2 pg + h has half h of page pg, whose id it is given.
+// A tile of up to PAGES pages by lanes 0 .. 7 of a warp, which have the id of a page each.
 __device__ inline void load_tile(const Dev& d, int layer, int kv, int head, int page, int n_pg, uint8_t* to,
                                  const CUtensorMap* map, uint64_t* bar, int lane) {
-  const int pg = lane >> 1 & 7;
-  if (lane < 16 && pg < n_pg)
-    tma_load_2d(to + (lane & 1) * PANEL + pg * 2048, map, 0,
-                (((page * d.layers + layer) * 2 + kv) * d.kv_heads + head) * PS, bar);
+  if (lane < n_pg)
+    tma_load_tile(to + lane * PS * D * 2, map,
+                  (((page * d.layers + layer) * 2 + kv) * d.kv_heads + head) * (PS / 8), bar);
 }
 
 }  // namespace

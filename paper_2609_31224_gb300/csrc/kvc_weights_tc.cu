@@ -24,13 +24,16 @@ namespace kvc {
 
 namespace {
 
+constexpr int TC_THREADS = 512;
+// Registers a thread of the issuing and query warps, and of the last 256 threads (512 x 128 together).
+constexpr int FEW_REGS = 96, MANY_REGS = 160;
 constexpr int K_RING = 3;
 constexpr int LSE_RING = 4;                        // query tiles whose lse is kept
 constexpr int ALL_COLS = 512;                      // two tiles' scores, twice each: 4 x 128 columns
 constexpr int OFF_ITEM = 512;                      // [2]
 constexpr int OFF_TMEM = OFF_ITEM + 2 * 128;
 constexpr int OFF_STOP = OFF_TMEM + 4;
-constexpr int OFF_FIRST = OFF_STOP + 4;            // first items, see each kernel
+constexpr int OFF_GROUP = OFF_STOP + 4;            // the work list
 constexpr int OFF_TILES = 3072;
 constexpr int SMEM_BYTES = OFF_TILES + 7 * SLOT;
 static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of a CTA");
@@ -87,10 +90,10 @@ __device__ inline void piece_products(uint32_t to, uint32_t a, uint32_t a_step, 
                                       uint32_t idesc) {
 #pragma unroll
   for (int p = 0; p < 2; ++p) {
-    const uint64_t ad = smem_desc(a + p * a_step, 0, 1024), bd = smem_desc(b + p * b_step, 0, 1024);
+    const uint64_t ad = desc_columns(a + p * a_step), bd = desc_columns(b + p * b_step);
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) {
-      const uint32_t at = (kk >> 2) * PANEL + (kk & 3) * 32;
+      const uint32_t at = step_columns(kk);
       tc_mma_ss(to, desc_at(ad, at), desc_at(bd, at), idesc, p > 0 || kk > 0);
     }
   }
@@ -100,16 +103,15 @@ __device__ inline void piece_products(uint32_t to, uint32_t a, uint32_t a_step, 
 // Row statistics: an item is 64 tokens (tiles A and B) of one (session, KV head) and a part of the keys.
 // ---------------------------------------------------------------------------
 __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
-    Dev d, int layer, const __grid_constant__ CUtensorMap map_lo,
-    const __grid_constant__ CUtensorMap map_hi, const __nv_bfloat16* __restrict__ q, float qk_scale,
+    Dev d, int layer, const __grid_constant__ CUtensorMap map,
+    const __nv_bfloat16* __restrict__ q, float qk_scale,
     int parts, WeightsWork work) {
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem);
   Item* items = reinterpret_cast<Item*>(smem + OFF_ITEM);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + OFF_TMEM);
   volatile int* stop = reinterpret_cast<int*>(smem + OFF_STOP);
-  int* s_first = reinterpret_cast<int*>(smem + OFF_FIRST);
-  static_assert(OFF_FIRST + (MAX_SEQ + 1) * 4 <= OFF_TILES, "header fits");
+  int* s_group = reinterpret_cast<int*>(smem + OFF_GROUP);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = d.kv_heads;
   uint8_t* s_q = smem + OFF_TILES;      // A upper, A lower, B upper, B lower
   uint8_t* s_k = s_q + 4 * SLOT;
@@ -120,9 +122,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
     init_barriers(bars);
     *stop = 0;
   }
-  if (warp == 2)
-    first_items(n_seq, lane, s_first,
-                [&](int i) { return (d.seq[i].t + 2 * TOKENS - 1) / (2 * TOKENS) * H * parts; });
+  auto items_of = [&](int i) { return (d.seq[i].t + 2 * TOKENS - 1) / (2 * TOKENS) * H * parts; };
+  if (warp == 2) list_items(n_seq, lane, s_group, items_of);
   __syncwarp();
   if (warp == 1) tmem_alloc(tmem_slot, ALL_COLS);
   tc_fence_before();
@@ -136,11 +137,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
   };
 
   if (warp < 4) {
-    give_registers<FEW_REGS>();
+    set_registers<128, FEW_REGS>();
     if (warp == 0) {
-      const int total = s_first[n_seq];
-      const CUtensorMap* map = (lane & 1) ? &map_hi : &map_lo;
-      uint32_t k_no = 0;
+      const int total = s_group[GROUPS];
+        uint32_t k_no = 0;
       for (int n = 0; ok; ++n) {
         Item* it = items + (n & 1);
         if (n >= 2 && !wait_warp(B_ITEM_EMPTY + (n & 1), ((n >> 1) & 1) ^ 1)) break;
@@ -154,7 +154,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
           }
           break;
         }
-        const int seq = session_of(n_seq, s_first, at), in = at - s_first[seq];
+        int in;
+        const int seq = find_item(n_seq, lane, s_group, at, items_of, &in);
         if (lane < 16)
           reinterpret_cast<int*>(&it->si)[lane] = reinterpret_cast<const int*>(d.seq + seq)[lane];
         __syncwarp();
@@ -181,12 +182,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
             pid = pid_next;
             pid_next = page_at(PAGES * j + 32 + lane);
           }
-          const int page = __shfl_sync(FULL, pid, PAGES * ((j - j0) & 3) + (lane >> 1 & 7));
+          const int page = __shfl_sync(FULL, pid, PAGES * ((j - j0) & 3) + (lane & 7));
           const int n_pg = min(PAGES, nb - PAGES * j), st = k_no % K_RING;
           if (k_no >= K_RING && !wait_warp(B_EMPTY + st, ((k_no / K_RING) & 1) ^ 1)) break;
           if (lane == 0) mbar_arrive_expect_tx(&bars[B_FULL + st], n_pg * PS * D * 2);
           __syncwarp();
-          load_tile(d, layer, 0, head, page, n_pg, s_k + st * SLOT, map, &bars[B_FULL + st], lane);
+          load_tile(d, layer, 0, head, page, n_pg, s_k + st * SLOT, &map, &bars[B_FULL + st], lane);
         }
       }
       for (uint32_t s = k_no > K_RING ? k_no - K_RING : 0; s < k_no; ++s)
@@ -229,7 +230,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
       }
     }
   } else if (warp < 8) {
-    give_registers<FEW_REGS>();
+    set_registers<128, FEW_REGS>();
     const int ts = tid - 4 * 32;
     uint32_t q_no[2] = {0, 0};
     for (int n = 0; ok; ++n) {
@@ -238,7 +239,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
       if (!it.valid) break;
       const int tiles = it.at + TOKENS < it.si.t ? 2 : 1;
       for (int x = 0; x < tiles && ok && it.begin < it.end; ++x) {
-        stage_q<2>(d, it.si, it.head, it.at + x * TOKENS, q, qk_scale, s_q + 2 * x * SLOT, ts,
+        stage_q<2, G>(d, it.si, it.head, it.at + x * TOKENS, q, qk_scale, s_q + 2 * x * SLOT, ts,
                    [&] { return q_no[x] == 0 || wait_warp(B_Q_EMPTY + x, (q_no[x] - 1) & 1); });
         if (!ok) break;
         ++q_no[x];
@@ -250,7 +251,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
       if (lane == 0) mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
     }
   } else {
-    take_registers<MANY_REGS>();
+    set_registers<128, MANY_REGS>();
     const int x = (warp - 8) >> 2, r = (warp & 3) * 32 + lane;
     const uint32_t trow = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     uint32_t s_no = 0;
@@ -263,6 +264,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
       if (t0 + x * TOKENS < si.t) {
         const int nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1);
         const int q_log = si.n_hist + si.n_live - si.t + tok;
+        const EdgeSteps edge = edge_steps(si, t0);
         float m = -INFINITY, l = 0.f;
         for (int j = it.begin; j < it.end; ++j, ++s_no) {
           const int b = 2 * x + (s_no & 1);
@@ -274,7 +276,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(&bars[B_S_EMPTY + b]);
-          if (is_edge(si, t0, PAGES * j)) {
+          if (edge.at(j)) {
 #pragma unroll
             for (int p = 0; p < PAGES; ++p) {
               const uint32_t seen = slots_seen(si, PAGES * j + p, nb, q_log);
@@ -322,21 +324,20 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
 // ---------------------------------------------------------------------------
 // Sums by key: an item is 256 keys (tiles A and B) of one (session, KV head) and a share of the tokens.
 // ---------------------------------------------------------------------------
-constexpr int GROUP_SEQ = 16;        // sessions of a group of the work list
-constexpr int OFF_LSE = OFF_FIRST + 136;
-static_assert(OFF_LSE % 16 == 0 && MAX_SEQ / GROUP_SEQ <= 32 &&
-                  OFF_LSE + LSE_RING * M * 4 <= OFF_TILES, "header fits");
+constexpr int OFF_LSE = OFF_GROUP + 136;
+static_assert((GROUPS + 1) * 4 <= 136 && OFF_LSE % 16 == 0 && OFF_LSE + LSE_RING * M * 4 <= OFF_TILES,
+              "header fits");
 
 __global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
-    Dev d, int layer, const __grid_constant__ CUtensorMap map_lo,
-    const __grid_constant__ CUtensorMap map_hi, const __nv_bfloat16* __restrict__ q, float qk_scale,
+    Dev d, int layer, const __grid_constant__ CUtensorMap map,
+    const __nv_bfloat16* __restrict__ q, float qk_scale,
     int parts, int shares, WeightsWork work) {
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem);
   Item* items = reinterpret_cast<Item*>(smem + OFF_ITEM);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + OFF_TMEM);
   volatile int* stop = reinterpret_cast<int*>(smem + OFF_STOP);
-  int* s_group = reinterpret_cast<int*>(smem + OFF_FIRST);  // first item of each group of sessions
+  int* s_group = reinterpret_cast<int*>(smem + OFF_GROUP);
   float* s_lse = reinterpret_cast<float*>(smem + OFF_LSE);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, H = d.kv_heads;
   uint8_t* s_k = smem + OFF_TILES;
@@ -344,20 +345,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
   pdl_wait();
   pdl_launch_dependents();
   const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;
-  const int n_groups = (n_seq + GROUP_SEQ - 1) / GROUP_SEQ;
   auto items_of = [&](int i) {
-    return i < n_seq ? (d.seq[i].n_blocks + 2 * PAGES - 1) / (2 * PAGES) * H * shares : 0;
+    return (d.seq[i].n_blocks + 2 * PAGES - 1) / (2 * PAGES) * H * shares;
   };
   if (tid == 0) {
     init_barriers(bars);
     *stop = 0;
   }
-  if (warp == 2)
-    first_items(n_groups, lane, s_group, [&](int g) {
-      int n = 0;
-      for (int i = 0; i < GROUP_SEQ; ++i) n += items_of(g * GROUP_SEQ + i);
-      return n;
-    });
+  if (warp == 2) list_items(n_seq, lane, s_group, items_of);
   __syncwarp();
   if (warp == 1) tmem_alloc(tmem_slot, ALL_COLS);
   tc_fence_before();
@@ -371,11 +366,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
   };
 
   if (warp < 4) {
-    give_registers<FEW_REGS>();
+    set_registers<128, FEW_REGS>();
     if (warp == 0) {
-      const int total = s_group[n_groups];
-      const CUtensorMap* map = (lane & 1) ? &map_hi : &map_lo;
-      uint32_t k_no = 0;
+      const int total = s_group[GROUPS];
+        uint32_t k_no = 0;
       for (int n = 0; ok; ++n) {
         Item* it = items + (n & 1);
         if (n >= 2 && !wait_warp(B_ITEM_EMPTY + (n & 1), ((n >> 1) & 1) ^ 1)) break;
@@ -389,19 +383,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
           }
           break;
         }
-        // Its group of sessions, then the session: lane i has the group's session i.
-        const int group = session_of(n_groups, s_group, at);
-        const int count = lane < GROUP_SEQ ? items_of(group * GROUP_SEQ + lane) : 0;
-        int upto = count;
-#pragma unroll
-        for (int o = 1; o < GROUP_SEQ; o <<= 1) {
-          const int y = __shfl_up_sync(FULL, upto, o);
-          if (lane >= o) upto += y;
-        }
-        const int rest = at - s_group[group];
-        const int mine = __ffs(__ballot_sync(FULL, lane < GROUP_SEQ && rest < upto)) - 1;
-        const int seq = group * GROUP_SEQ + mine;
-        const int in = rest - __shfl_sync(FULL, upto - count, mine);
+        int in;
+        const int seq = find_item(n_seq, lane, s_group, at, items_of, &in);
         if (lane < 16)
           reinterpret_cast<int*>(&it->si)[lane] = reinterpret_cast<const int*>(d.seq + seq)[lane];
         __syncwarp();
@@ -426,12 +409,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
         const int b = b0 + (lane & 15);
         const int pid = b < si.n_blocks ? block_page(si, hrow, lrow, b) : 0;
         for (int x = 0; x < 2 && b0 + x * PAGES < si.n_blocks; ++x, ++k_no) {
-          const int page = __shfl_sync(FULL, pid, PAGES * x + (lane >> 1 & 7));
+          const int page = __shfl_sync(FULL, pid, PAGES * x + (lane & 7));
           const int n_pg = min(PAGES, si.n_blocks - b0 - x * PAGES), st = k_no % K_RING;
           if (k_no >= K_RING && !wait_warp(B_EMPTY + st, ((k_no / K_RING) & 1) ^ 1)) break;
           if (lane == 0) mbar_arrive_expect_tx(&bars[B_FULL + st], n_pg * PS * D * 2);
           __syncwarp();
-          load_tile(d, layer, 0, head, page, n_pg, s_k + st * SLOT, map, &bars[B_FULL + st], lane);
+          load_tile(d, layer, 0, head, page, n_pg, s_k + st * SLOT, &map, &bars[B_FULL + st], lane);
         }
       }
       for (uint32_t s = k_no > K_RING ? k_no - K_RING : 0; s < k_no; ++s)
@@ -474,7 +457,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
       }
     }
   } else if (warp < 8) {
-    give_registers<FEW_REGS>();
+    set_registers<128, FEW_REGS>();
     const int ts = tid - 4 * 32;
     uint32_t q_no = 0;
     const int total = d.g->total_tokens;
@@ -498,7 +481,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
             m = mn;
           }
         }
-        stage_q<2>(d, si, it.head, i * TOKENS, q, qk_scale, s_q + (q_no & 1) * 2 * SLOT, ts,
+        stage_q<2, G>(d, si, it.head, i * TOKENS, q, qk_scale, s_q + (q_no & 1) * 2 * SLOT, ts,
                    [&] { return q_no < 2 || wait_warp(B_Q_EMPTY + (q_no & 1), ((q_no >> 1) & 1) ^ 1); });
         if (!ok) break;
         if (q_no >= LSE_RING && !wait_warp(B_LSE_EMPTY + q_no % LSE_RING, ((q_no / LSE_RING) & 1) ^ 1)) break;
@@ -511,7 +494,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
       if (lane == 0) mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
     }
   } else {
-    take_registers<MANY_REGS>();
+    set_registers<128, MANY_REGS>();
     const int x = (warp - 8) >> 2, r = (warp & 3) * 32 + lane;
     const uint32_t trow = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     uint32_t s_no = 0, q_no = 0;
@@ -597,16 +580,16 @@ cudaError_t weights_tc_attributes() {
 cudaError_t launch_weights_tc(const Dev& d, const Limits& lim, int layer, const void* q,
                               const WeightsWork& work, int parts, int shares, cudaStream_t s,
                               int64_t* launches) {
-  CUtensorMap lo, hi;
-  if (!pool_tensor_maps(d, &lo, &hi)) return cudaErrorInvalidValue;
+  CUtensorMap map;
+  if (!pool_tile_map(d, &map)) return cudaErrorInvalidValue;
   const float scale = LOG2E / sqrtf((float)D);
   const __nv_bfloat16* qt = static_cast<const __nv_bfloat16*>(q);
   cudaError_t e = launch_ex(&weights_stat_kernel, dim3(lim.sms), dim3(TC_THREADS), SMEM_BYTES, s, true, d,
-                            layer, lo, hi, qt, scale, parts, work);
+                            layer, map, qt, scale, parts, work);
   *launches += e == cudaSuccess;
   if (e != cudaSuccess) return e;
-  e = launch_ex(&weights_sums_kernel, dim3(lim.sms), dim3(TC_THREADS), SMEM_BYTES, s, true, d, layer, lo,
-                hi, qt, scale, parts, shares, work);
+  e = launch_ex(&weights_sums_kernel, dim3(lim.sms), dim3(TC_THREADS), SMEM_BYTES, s, true, d, layer, map,
+                qt, scale, parts, shares, work);
   *launches += e == cudaSuccess;
   return e;
 }
