@@ -10,14 +10,17 @@
 //   warp 0      items from the counter; K and V by TMA, a page's 4 KiB of a head a copy (twice as many of
 //               2 KiB took 2,600 cycles a step for 1,900), into a ring of five 32 KiB stages in turn
 //   warps 1, 2  one thread each issues the products of a tile
-//   warps 4-7   query rows, rotated, scaled and rounded, into shared memory, the next item's as soon as
-//               this one's last score product of the tile is complete; V rows that have to be zero (below)
-//   warps 8-15  softmax, four warps a tile: a thread has one row of S, from tensor memory to registers in
-//               one go, and writes P over it.  P is taken against the maximum of the row's first step,
-//               for as long as a step's sum stays below 2^20 (sums and roundings do not depend on the
-//               scale): later steps look for no maximum, and O is rescaled in tensor memory only
-//               when a sum passes that
-// Tensor memory: S_A, S_B (P over the first half of each), O_A, O_B, 128 columns each: all 512.
+//   warp 3      V rows that have to be zero (below)
+//   warps 4-7   query rows, rotated, scaled and rounded, into three tiles of shared memory: an item's
+//               first one while the item before still runs
+//   warps 8-15  softmax, four warps a tile: a thread has one row of S, 32 keys at a time, and writes P over
+//               it.  P is taken against the maximum of the row's first keys, for as long as a sum of 32
+//               stays below 2^20 (sums and roundings do not depend on the scale): later ones look for no
+//               maximum, and O is rescaled in tensor memory only when a sum passes that
+// A step's keys come in halves, each with scores of its own: while the softmax of one half runs, the
+// tensor cores have the other half's O += P V and next scores, so that a row's warp need not wait.
+// Tensor memory: S_A, S_B (two halves each, P over the first part of a half), O_A, O_B, 128 columns each:
+// all 512.
 //
 // A key that no row of a product may see has P = 0, but 0 times a value that is not finite is not 0.  So
 // the V rows of slots that hold no resident position are zeroed in shared memory, and those of the
@@ -36,23 +39,24 @@ namespace kvc {
 
 namespace {
 
-constexpr int RING = 5;
+constexpr int RING = 4, Q_SLOTS = 3;
 constexpr int EDGES = 4;
-constexpr int HALF = KEYS / 2;                     // of a step's keys, and of a row's dims
-// 24 warps, 80 registers a thread at launch: issuing and query warps give some to the softmax.
-constexpr int TC_THREADS = 768, BASE_REGS = 80, FEW_REGS = 64, MANY_REGS = 88;
-static_assert(256 * FEW_REGS + 512 * MANY_REGS <= TC_THREADS * BASE_REGS, "registers of the launch");
+constexpr int TC_THREADS = 512;
 constexpr int S_COL = 0, O_COL = 256, ALL_COLS = 512;
-constexpr float SUM_LIMIT = 1048576.f;              // of a step's P in a row: 2^20
+constexpr int HALF = KEYS / 2;                     // of a step's keys
+constexpr int CHUNK = 32;                          // keys that a row takes at a time
+constexpr float SUM_LIMIT = 1048576.f;              // of a chunk's P in a row: 2^20
 
 enum {
   B_FULL = 0,                    // [RING] a stage has landed
   B_EMPTY = B_FULL + RING,       // [RING] and was read
-  B_Q_FULL = B_EMPTY + RING,     // [2] a tile's query rows are there
-  B_Q_EMPTY = B_Q_FULL + 2,      // [2] and its last scores of the item complete
-  B_S = B_Q_EMPTY + 2,           // [2] scores complete (and every product before them)
-  B_P = B_S + 2,                 // [2] P written, O rescaled
-  B_O = B_P + 2,                 // [2] the item's output complete
+  B_Q_FULL = B_EMPTY + RING,     // [Q_SLOTS] a tile's query rows are there
+  B_Q_EMPTY = B_Q_FULL + Q_SLOTS,  // [Q_SLOTS] and its last scores complete
+  // Halves of a step's keys: [2 tiles][2].  The first half's scores have one phase more an item, for
+  // the last step's first half of O += P V.
+  B_S = B_Q_EMPTY + Q_SLOTS,     // scores complete (and every product before them)
+  B_P = B_S + 4,                 // P written, O rescaled
+  B_O = B_P + 4,                 // [2] the item's output complete
   B_O_EMPTY = B_O + 2,           // [2] and read
   // V stages of edge steps land here instead (their B_FULL phase completes at once), and have their
   // rows zeroed: the e-th such stage of the CTA, at e % EDGES.  A ring holds fewer.
@@ -63,14 +67,14 @@ enum {
   B_FINAL = B_ITEM_EMPTY + 2,    // every product of the CTA complete
   N_BARS = B_FINAL + 1
 };
-constexpr int ITEM_READERS = 2 + 4 + 16;           // warps that arrive at B_ITEM_EMPTY
+constexpr int ITEM_READERS = 2 + 1 + 4 + 8;        // warps that arrive at B_ITEM_EMPTY
 
 // What every role knows of an item.
 struct Item {
   SeqInfo si;
-  int32_t seq, head, t0, steps;  // steps = 0: no more items
+  int32_t head, t0, steps;       // steps = 0: no more items
   int32_t odd;                   // some V row was zeroed because it is not finite
-  int32_t pad[11];
+  int32_t pad[12];
 };
 static_assert(sizeof(Item) == 128, "Item size");
 
@@ -79,26 +83,15 @@ constexpr int OFF_ITEM = 512;                      // [2]
 constexpr int OFF_TMEM = OFF_ITEM + 2 * 128;
 constexpr int OFF_STOP = OFF_TMEM + 4;
 constexpr int OFF_GROUP = OFF_STOP + 4;            // the work list
-constexpr int OFF_HALF = OFF_GROUP + 136;          // [2 tiles][2 halves][M] what halves of a row exchange
-constexpr int OFF_TILES = 3072;                    // query tiles A, B, then the ring
-constexpr int SMEM_BYTES = OFF_TILES + (2 + RING) * SLOT;
-static_assert(N_BARS * 8 <= OFF_ITEM && (GROUPS + 1) * 4 <= 136 && OFF_HALF + 4 * M * 4 <= OFF_TILES,
-              "header fits");
+constexpr int OFF_TILES = 3072;                    // query tiles, then the ring
+constexpr int SMEM_BYTES = OFF_TILES + (Q_SLOTS + RING) * SLOT;
+static_assert(N_BARS * 8 <= OFF_ITEM && OFF_GROUP + (GROUPS + 1) * 4 <= OFF_TILES, "header fits");
 static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of a CTA");
 
-// Barrier of the two warps that share rows: whether `say` holds in any of their threads.
-__device__ inline bool meet_any(int id, bool say) {
-  int any;
-  __syncwarp();
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.s32 p, %2, 0;\n\t"
-      "barrier.cta.red.or.pred.aligned q, %1, 64, p;\n\t"
-      "selp.s32 %0, 1, 0, q;\n\t}"
-      : "=r"(any)
-      : "r"(id), "r"((int)say)
-      : "memory");
-  return any != 0;
+// Page of block b of a session with nhp compacted pages.
+__device__ inline int page_of(const Dev& d, int sid, int nhp, int b) {
+  const size_t row = (size_t)sid * d.max_pages_per_session;
+  return b < nhp ? d.hist_pt[row + b] : d.live_pt[row + b - nhp];
 }
 
 __device__ inline bool not_finite(uint32_t two) {
@@ -149,17 +142,16 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int H = d.kv_heads;
   uint8_t* s_q = smem + OFF_TILES;
-  uint8_t* s_ring = s_q + 2 * SLOT;
+  uint8_t* s_ring = s_q + Q_SLOTS * SLOT;
   pdl_wait();
   pdl_launch_dependents();
   const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;  // (no units: the append failed)
   if (tid == 0) {
     for (int i = 0; i < N_BARS; ++i) {
-      const int count = i >= B_EMPTY && i < B_Q_FULL || i == B_FINAL ? 2
+      const int count = (i >= B_EMPTY && i < B_Q_FULL) || i == B_FINAL ? 2
                         : i >= B_Q_FULL && i < B_Q_EMPTY             ? 4
-                        : i >= B_P && i < B_O          ? 8
-                        : i >= B_O_EMPTY && i < B_EDGE ? 8
-                        : i >= B_FIX && i < B_ITEM     ? 4
+                        : i >= B_P && i < B_O          ? 4
+                        : i >= B_O_EMPTY && i < B_EDGE ? 4
                         : i >= B_ITEM_EMPTY && i < B_FINAL ? ITEM_READERS
                                                            : 1;
       mbar_init(&bars[i], count);
@@ -178,86 +170,104 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
   const uint32_t tmem = *tmem_slot;
 
   if (warp < 4) {
-    set_registers<BASE_REGS, FEW_REGS>();
-  if (warp == 0) {
-    // ---------------- items, K and V ----------------
-    const int total = s_group[GROUPS];
-    uint32_t seq_no = 0, edges = 0;  // stages so far, and V stages of edge steps
-    bool ok = true;
-    for (int n = 0; ok; ++n) {
-      Item* it = items + (n & 1);
-      if (n >= 2) ok = __all_sync(FULL, wait_or_stop(d, &bars[B_ITEM_EMPTY + (n & 1)], ((n >> 1) & 1) ^ 1, stop));
-      if (!ok) break;
-      int at = 0;
-      if (lane == 0) at = atomicAdd(&d.pf_count[0], 1);
-      at = __shfl_sync(FULL, at, 0);
-      if (at >= total) {
+    if (warp == 0) {
+      // ---------------- items, K and V ----------------
+      const int total = s_group[GROUPS];
+      uint32_t seq_no = 0, edges = 0;  // stages so far, and V stages of edge steps
+      bool ok = true;
+      auto wait = [&](int bar, uint32_t parity) {
+        ok = ok && __all_sync(FULL, wait_or_stop(d, &bars[bar], parity, stop));
+        return ok;
+      };
+      // The next item, taken from the counter and looked up while the stages of the one before are on
+      // their way.  (word: lane i has word i of its session's info.)
+      int word, sid, nhp, head, t0, nb, steps, pid, pid_next;
+      EdgeSteps edge;
+      auto fetch = [&] {
+        int at = 0, in;
+        if (lane == 0) at = atomicAdd(&d.pf_count[0], 1);
+        at = __shfl_sync(FULL, at, 0);
+        steps = 0;
+        if (at >= total) return;
+        const int seq = find_item(n_seq, lane, s_group, at, items_of, &in);
+        word = lane < 16 ? reinterpret_cast<const int*>(d.seq + seq)[lane] : 0;
+        const SeqInfo& si = d.seq[seq];
+        sid = si.sid;
+        nhp = si.n_hist_pages;
+        head = in % H;
+        t0 = ((si.t + 2 * TOKENS - 1) / (2 * TOKENS) - 1 - in / H) * 2 * TOKENS;
+        nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1);
+        steps = (nb + PAGES - 1) / PAGES;
+        edge = edge_steps(si, t0);
+        auto page_at = [&](int b) { return b < nb ? page_of(d, sid, nhp, b) : 0; };
+        pid = page_at(lane);
+        pid_next = page_at(32 + lane);
+      };
+      auto publish = [&](int n) {
+        Item* it = items + (n & 1);
+        if (lane < 16) reinterpret_cast<int*>(&it->si)[lane] = word;
         if (lane == 0) {
-          it->steps = 0;
-          mbar_arrive(&bars[B_ITEM + (n & 1)]);
+          it->head = head;
+          it->t0 = t0;
+          it->steps = steps;
+          it->odd = 0;
         }
-        break;
-      }
-      int in;
-      const int seq = find_item(n_seq, lane, s_group, at, items_of, &in);
-      if (lane < 16)
-        reinterpret_cast<int*>(&it->si)[lane] = reinterpret_cast<const int*>(d.seq + seq)[lane];
-      __syncwarp();
-      const SeqInfo& si = it->si;
-      const int n_t = (si.t + 2 * TOKENS - 1) / (2 * TOKENS), head = in % H;
-      const int t0 = (n_t - 1 - in / H) * 2 * TOKENS;
-      const int nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1), steps = (nb + PAGES - 1) / PAGES;
-      if (lane == 0) {
-        it->seq = seq;
-        it->head = head;
-        it->t0 = t0;
-        it->steps = steps;
-        it->odd = 0;
-        mbar_arrive(&bars[B_ITEM + (n & 1)]);
-      }
-      const int32_t* hrow = d.hist_pt + (size_t)si.sid * d.max_pages_per_session;
-      const int32_t* lrow = d.live_pt + (size_t)si.sid * d.max_pages_per_session;
-      auto page_at = [&](int b) { return b < nb ? block_page(si, hrow, lrow, b) : 0; };
-      const EdgeSteps edge = edge_steps(si, t0);
-      int pid = page_at(lane), pid_next = page_at(32 + lane);
-      for (int j = 0; j < steps && ok; ++j) {
-        if (j > 0 && (j & 3) == 0) {
-          pid = pid_next;
-          pid_next = page_at(PAGES * j + 32 + lane);
-        }
-        const int page = __shfl_sync(FULL, pid, PAGES * (j & 3) + (lane & 7));
-        const int n_pg = min(PAGES, nb - PAGES * j);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars[B_ITEM + (n & 1)]);
+      };
+      fetch();
+      publish(0);
+      for (int n = 0; ok && steps > 0; ++n) {
+        const int c_sid = sid, c_nhp = nhp, c_head = head, c_nb = nb, c_steps = steps;
+        const EdgeSteps c_edge = edge;
+        int c_pid = pid, c_pid_next = pid_next;
+        const int next_bar = B_ITEM_EMPTY + ((n + 1) & 1);
+        const uint32_t next_parity = (((n + 1) >> 1) & 1) ^ 1;
+        bool published = false;
+        for (int j = 0; j < c_steps && ok; ++j) {
+          if (j > 0 && (j & 3) == 0) {
+            c_pid = c_pid_next;
+            const int b = PAGES * j + 32 + lane;
+            c_pid_next = b < c_nb ? page_of(d, c_sid, c_nhp, b) : 0;
+          }
+          const int page = __shfl_sync(FULL, c_pid, PAGES * (j & 3) + (lane & 7));
+          const int n_pg = min(PAGES, c_nb - PAGES * j);
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv, ++seq_no) {
-          const int st = seq_no % RING;
-          if (seq_no >= RING) {
-            ok = __all_sync(FULL, wait_or_stop(d, &bars[B_EMPTY + st], ((seq_no / RING) & 1) ^ 1, stop));
-            if (!ok) break;
+          for (int kv = 0; kv < 2; ++kv, ++seq_no) {
+            const int st = seq_no % RING;
+            if (seq_no >= RING && !wait(B_EMPTY + st, ((seq_no / RING) & 1) ^ 1)) break;
+            uint64_t* bar = &bars[B_FULL + st];
+            if (kv == 1 && c_edge.at(j)) {
+              if (lane == 0) mbar_arrive(bar);
+              bar = &bars[B_EDGE + edges % EDGES];
+              ++edges;
+            }
+            if (lane == 0) mbar_arrive_expect_tx(bar, n_pg * PS * D * 2);
+            __syncwarp();
+            load_tile(d, layer, kv, c_head, page, n_pg, s_ring + st * SLOT, &map, bar, lane);
           }
-          uint64_t* bar = &bars[B_FULL + st];
-          if (kv == 1 && edge.at(j)) {
-            if (lane == 0) mbar_arrive(bar);
-            bar = &bars[B_EDGE + edges % EDGES];
-            ++edges;
+          if (j == min(1, c_steps - 1)) fetch();
+          if (j >= 1 && !published && (n == 0 || __all_sync(FULL, mbar_test(&bars[next_bar], next_parity)))) {
+            publish(n + 1);
+            published = true;
           }
-          if (lane == 0) mbar_arrive_expect_tx(bar, n_pg * PS * D * 2);
-          __syncwarp();
-          load_tile(d, layer, kv, head, page, n_pg, s_ring + st * SLOT, &map, bar, lane);
+        }
+        if (!published) {
+          if (n > 0 && !wait(next_bar, next_parity)) break;
+          publish(n + 1);
         }
       }
-    }
-    // Copies still in flight land before the CTA ends.
-    for (uint32_t s = seq_no > RING ? seq_no - RING : 0; s < seq_no; ++s)
-      mbar_wait(d, &bars[B_FULL + s % RING], (s / RING) & 1);
-    for (uint32_t e = edges > EDGES ? edges - EDGES : 0; e < edges; ++e)
-      mbar_wait(d, &bars[B_EDGE + e % EDGES], (e / EDGES) & 1);
-  } else if (warp < 3) {
-    // ---------------- products: one thread a tile ----------------
-    if (lane == 0) {
-      constexpr uint32_t ID_S = instr_desc(KEYS, M, false), ID_O = instr_desc(D, M, true);
+      // Copies still in flight land before the CTA ends.
+      for (uint32_t s = seq_no > RING ? seq_no - RING : 0; s < seq_no; ++s)
+        mbar_wait(d, &bars[B_FULL + s % RING], (s / RING) & 1);
+      for (uint32_t e = edges > EDGES ? edges - EDGES : 0; e < edges; ++e)
+        mbar_wait(d, &bars[B_EDGE + e % EDGES], (e / EDGES) & 1);
+    } else if (warp < 3 && lane == 0) {
+      // ---------------- products: one thread a tile ----------------
+      constexpr uint32_t ID_S = instr_desc(HALF, M, false), ID_O = instr_desc(D, M, true);
       const int x = warp - 1;
       const uint32_t t_s = tmem + S_COL + x * KEYS, t_o = tmem + O_COL + x * D;
-      const uint64_t qd = desc_columns(smem_u32(s_q) + x * SLOT);
+      const uint64_t qd0 = desc_columns(smem_u32(s_q));
       const uint64_t kd0 = desc_columns(smem_u32(s_ring)), vd0 = desc_rows(smem_u32(s_ring));
       bool ok = true;
       auto wait = [&](int bar, uint32_t parity) {
@@ -265,8 +275,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
         return ok;
       };
       // Stages are counted on: `st` is the ring's slot of the next one, `pass` its pass over the ring.
-      int st = 0;
-      uint32_t pass = 0, edges = 0, p_no = 0, q_no = 0, o_no = 0;
+      int st = 0, q_slot = 0;
+      uint32_t pass = 0, edges = 0, p_no = 0, o_no = 0;
+      uint32_t q_no = 0;  // query tiles of the items before
       auto full = [&] { return wait(B_FULL + st, pass & 1); };
       auto next = [&] {
         if (++st == RING) {
@@ -274,172 +285,181 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
           ++pass;
         }
       };
-      // S = Q K^T of the next stage; the last one of an item frees its query rows.
-      auto scores = [&](bool last) {
-        if (!full()) return;
+      // S = Q K^T of half h of the stage at `st`, which has landed.
+      auto scores = [&](int h) {
         tc_fence_after();
-        const uint64_t kd = desc_at(kd0, st * SLOT);
+        const uint64_t kd = desc_at(kd0, st * SLOT + h * (HALF / 8) * ROW_GROUP), qd = desc_at(qd0, q_slot * SLOT);
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          const uint32_t at = step_columns(kk);
-          tc_mma_ss(t_s, desc_at(qd, at), desc_at(kd, at), ID_S, kk > 0);
-        }
-        tc_commit(&bars[B_S + x]);
-        if (last) tc_commit(&bars[B_Q_EMPTY + x]);
-        tc_commit(&bars[B_EMPTY + st]);
-        next();
+        for (int kk = 0; kk < D / 16; ++kk)
+          tc_mma_ss(t_s + h * HALF, desc_at(qd, step_columns(kk)), desc_at(kd, step_columns(kk)), ID_S, kk > 0);
       };
-      // A stage that this tile has no use for.
-      auto skip = [&] {
+      // An item's first scores.
+      auto begin = [&](const Item& it, bool mine) {
         if (!full()) return;
-        mbar_arrive(&bars[B_EMPTY + st]);
+        if (mine) {
+          q_slot = (q_no + x) % Q_SLOTS;
+          if (!wait(B_Q_FULL + q_slot, ((q_no + x) / Q_SLOTS) & 1)) return;
+          scores(0);
+          tc_commit(&bars[B_S + 2 * x]);
+          scores(1);
+          tc_commit(&bars[B_S + 2 * x + 1]);
+          if (it.steps == 1) tc_commit(&bars[B_Q_EMPTY + q_slot]);
+          tc_commit(&bars[B_EMPTY + st]);
+        } else {
+          mbar_arrive(&bars[B_EMPTY + st]);
+        }
         next();
       };
-      auto begin = [&](int steps, bool mine) {
-        if (!mine) return skip();
-        if (!wait(B_Q_FULL + x, q_no & 1)) return;
-        ++q_no;
-        scores(steps == 1);
-      };
+      auto tiles_of = [](const Item& it) { return it.t0 + TOKENS < it.si.t ? 2 : 1; };
       if (wait(B_ITEM, 0)) {
-        int steps = items[0].steps;
-        bool mine = x == 0 || (steps > 0 && items[0].t0 + TOKENS < items[0].si.t);
-        if (steps > 0) begin(steps, mine);
+        int steps = items[0].steps, tiles = steps > 0 ? tiles_of(items[0]) : 0;
+        if (steps > 0) begin(items[0], x < tiles);
         for (int n = 0; ok && steps > 0; ++n) {
           const Item& it = items[n & 1];
           const EdgeSteps edge = edge_steps(it.si, it.t0);
-          int steps_next = 0;
-          bool mine_next = false;
+          const bool mine = x < tiles;
+          q_no += tiles;
           for (int j = 0; j < steps && ok; ++j) {
+            // What is there early is waited for first: V, then the next step's K.
             const bool last = j == steps - 1;
+            const int sv = st;
             if (!full()) break;
+            next();
+            if (!last && !full()) break;
             if (edge.at(j)) {
-              if (!wait(B_FIX + edges % EDGES, (edges / EDGES) & 1)) break;
+              if (mine && !wait(B_FIX + edges % EDGES, (edges / EDGES) & 1)) break;
               ++edges;
             }
             if (mine) {
-              if (!wait(B_P + x, p_no & 1)) break;
-              ++p_no;
-              if (j == 0) {
-                if (o_no > 0 && !wait(B_O_EMPTY + x, (o_no - 1) & 1)) break;
-                ++o_no;
-              }
-              tc_fence_after();
-              const uint64_t vd = desc_at(vd0, st * SLOT);
+              if (j == 0 && o_no++ > 0 && !wait(B_O_EMPTY + x, (o_no - 2) & 1)) break;
+              const uint64_t vd = desc_at(vd0, sv * SLOT);
+#pragma unroll 1
+              for (int h = 0; h < 2; ++h) {
+                if (!wait(B_P + 2 * x + h, p_no & 1)) break;
+                tc_fence_after();
 #pragma unroll
-              for (int kk = 0; kk < KEYS / 16; ++kk)
-                tc_mma_ts(t_o, t_s + (kk >> 2) * HALF + (kk & 3) * 8, desc_at(vd, kk * 2 * ROW_GROUP), ID_O, j > 0 || kk > 0);
-              if (last) tc_commit(&bars[B_O + x]);
-              tc_commit(&bars[B_EMPTY + st]);
+                for (int kk = 0; kk < HALF / 16; ++kk)
+                  tc_mma_ts(t_o, t_s + h * HALF + kk * 8, desc_at(vd, (h * (HALF / 16) + kk) * 2 * ROW_GROUP), ID_O,
+                            j > 0 || h > 0 || kk > 0);
+                if (!last) scores(h);
+                if (!last || h == 0) tc_commit(&bars[B_S + 2 * x + h]);
+                else tc_commit(&bars[B_O + x]);
+              }
+              ++p_no;
+              if (j + 2 == steps) tc_commit(&bars[B_Q_EMPTY + q_slot]);
+              tc_commit(&bars[B_EMPTY + sv]);
+              if (!last) tc_commit(&bars[B_EMPTY + st]);
             } else {
-              mbar_arrive(&bars[B_EMPTY + st]);
+              mbar_arrive(&bars[B_EMPTY + sv]);
+              if (!last) mbar_arrive(&bars[B_EMPTY + st]);
             }
-            next();
-            if (!last) {
-              if (mine) scores(j + 2 == steps);
-              else skip();
-            } else {
-              // The next item's first scores go ahead of this one's output.
-              if (!wait(B_ITEM + ((n + 1) & 1), ((n + 1) >> 1) & 1)) break;
-              const Item& nx = items[(n + 1) & 1];
-              steps_next = nx.steps;
-              mine_next = x == 0 || (steps_next > 0 && nx.t0 + TOKENS < nx.si.t);
-              if (steps_next > 0) begin(steps_next, mine_next);
-            }
+            if (!last) next();
           }
-          if (!ok) break;
+          // The next item's first scores go ahead of this one's output.
+          if (!wait(B_ITEM + ((n + 1) & 1), ((n + 1) >> 1) & 1)) break;
+          const Item& nx = items[(n + 1) & 1];
+          steps = nx.steps;
+          tiles = steps > 0 ? tiles_of(nx) : 0;
+          if (steps > 0) begin(nx, x < tiles);
           mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
-          steps = steps_next;
-          mine = mine_next;
         }
       }
       // No product may still be running when the tensor memory is released.
       tc_commit(&bars[B_FINAL]);
       mbar_wait(d, &bars[B_FINAL], 0);
+    } else if (warp == 3) {
+      // ---------------- V rows to zero ----------------
+      bool ok = true;
+      auto wait = [&](int bar, uint32_t parity) {
+        ok = ok && __all_sync(FULL, wait_or_stop(d, &bars[bar], parity, stop));
+        return ok;
+      };
+      uint32_t stages = 0, edges = 0;
+      for (int n = 0; ok; ++n) {
+        if (!wait(B_ITEM + (n & 1), (n >> 1) & 1)) break;
+        Item& it = items[n & 1];
+        if (it.steps == 0) break;
+        const SeqInfo& si = it.si;
+        const int t0 = it.t0, steps = it.steps, q_log0 = si.n_hist + si.n_live - si.t;
+        const int nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1);
+        const EdgeSteps edge = edge_steps(si, t0);
+        for (int j = 0; j < steps && ok; ++j) {
+          if (!edge.at(j)) continue;
+          uint8_t* tile = s_ring + (stages + 2 * j + 1) % RING * SLOT;
+          if (!wait(B_EDGE + edges % EDGES, (edges / EDGES) & 1)) break;
+#pragma unroll 1
+          for (int r = lane; r < KEYS; r += 32) {
+            const int b = PAGES * j + r / PS;
+            const uint32_t bit = 1u << (r % PS);
+            bool zero = !(slots_seen(si, b, nb, q_log0 + si.t) & bit);
+            if (!zero && !(slots_seen(si, b, nb, q_log0 + t0) & bit)) {  // some rows see it
+              bool odd = false;
+#pragma unroll 4
+              for (int i = 0; i < 16; ++i) {
+                const uint4 v = *reinterpret_cast<const uint4*>(tile + tile_at(r, i));
+                odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
+              }
+              if (odd) {
+                it.odd = 1;
+                zero = true;
+              }
+            }
+            if (zero)
+              for (int i = 0; i < 16; ++i)
+                *reinterpret_cast<uint4*>(tile + tile_at(r, i)) = make_uint4(0, 0, 0, 0);
+          }
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars[B_FIX + edges % EDGES]);
+          ++edges;
+        }
+        stages += 2 * steps;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
+      }
     }
-  }
   } else if (warp < 8) {
-    set_registers<BASE_REGS, FEW_REGS>();
-    // ---------------- query rows, V rows to zero ----------------
+    // ---------------- query rows ----------------
     const int ts = tid - 4 * 32;
     bool ok = true;
     auto wait = [&](int bar, uint32_t parity) {
       ok = ok && __all_sync(FULL, wait_or_stop(d, &bars[bar], parity, stop));
       return ok;
     };
-    uint32_t s0 = 0, edges = 0, q_no[2] = {0, 0};
+    uint32_t q_no = 0;
     for (int n = 0; ok; ++n) {
       if (!wait(B_ITEM + (n & 1), (n >> 1) & 1)) break;
-      Item& it = items[n & 1];
+      const Item& it = items[n & 1];
       if (it.steps == 0) break;
-      const SeqInfo& si = it.si;
-      const int head = it.head, t0 = it.t0, steps = it.steps;
-      const int tiles = t0 + TOKENS < si.t ? 2 : 1;
-      for (int x = 0; x < tiles && ok; ++x) {
-        stage_q<1, 2>(d, si, head, t0 + x * TOKENS, q, qk_scale, s_q + x * SLOT, ts,
-                   [&] { return q_no[x] == 0 || wait(B_Q_EMPTY + x, (q_no[x] - 1) & 1); });
+      const int tiles = it.t0 + TOKENS < it.si.t ? 2 : 1;
+      for (int x = 0; x < tiles; ++x, ++q_no) {
+        const int slot = q_no % Q_SLOTS;
+        stage_q<1, G>(d, it.si, it.head, it.t0 + x * TOKENS, q, qk_scale, s_q + slot * SLOT, ts,
+                      [&] { return q_no < Q_SLOTS || wait(B_Q_EMPTY + slot, ((q_no / Q_SLOTS) & 1) ^ 1); });
         if (!ok) break;
-        ++q_no[x];
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&bars[B_Q_FULL + x]);
+        if (lane == 0) mbar_arrive(&bars[B_Q_FULL + slot]);
       }
-      // Thread ts has row ts of each such step's V.
-      const int nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1);
-      const int q_log0 = si.n_hist + si.n_live - si.t;
-      const EdgeSteps edge = edge_steps(si, t0);
-      for (int j = 0; j < steps && ok; ++j) {
-        const int b = PAGES * j + ts / PS;
-        if (!edge.at(j)) continue;
-        const uint32_t s = s0 + 2 * j + 1;
-        if (!wait(B_EDGE + edges % EDGES, (edges / EDGES) & 1)) break;
-        uint8_t* tile = s_ring + (s % RING) * SLOT;
-        const uint32_t bit = 1u << (ts % PS);
-        bool zero = !(slots_seen(si, b, nb, q_log0 + si.t) & bit);
-        if (!zero && !(slots_seen(si, b, nb, q_log0 + t0) & bit)) {  // some rows see it
-          bool odd = false;
-          for (int i = 0; i < 16; ++i) {
-            const uint4 v = *reinterpret_cast<const uint4*>(tile + tile_at(ts, i));
-            odd |= not_finite(v.x) || not_finite(v.y) || not_finite(v.z) || not_finite(v.w);
-          }
-          if (odd) {
-            it.odd = 1;
-            zero = true;
-          }
-        }
-        if (zero)
-          for (int i = 0; i < 16; ++i)
-            *reinterpret_cast<uint4*>(tile + tile_at(ts, i)) = make_uint4(0, 0, 0, 0);
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bars[B_FIX + edges % EDGES]);
-        ++edges;
-      }
-      s0 += 2 * steps;
       __syncwarp();
       if (lane == 0) mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
     }
   } else {
-    set_registers<BASE_REGS, MANY_REGS>();
     // ---------------- softmax ----------------
-    const int x = (warp - 8) >> 3, half = (warp - 8) >> 2 & 1;  // tile; keys [64 half, + 64) of a step
-    const int quarter = warp & 3, r = quarter * 32 + lane;      // row
-    const uint32_t trow = tmem + ((uint32_t)(quarter * 32) << 16);
-    const uint32_t t_s = trow + S_COL + x * KEYS + half * HALF, t_o = trow + O_COL + x * D + half * HALF;
-    float* mine = reinterpret_cast<float*>(smem + OFF_HALF) + (2 * x + half) * M + r;
-    const float* other = reinterpret_cast<float*>(smem + OFF_HALF) + (2 * x + (half ^ 1)) * M + r;
-    const int meet = 1 + x * 4 + quarter;                       // barrier of the two warps of a row
+    // (Loops stay rolled: with a step's 128 keys in one piece the code of all roles did not fit the
+    // instruction caches, and a warp was without an instruction for as long as it issued one.)
+    const int x = (warp - 8) >> 2;             // tile
+    const int r = (warp & 3) * 32 + lane;      // row
+    const uint32_t trow = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t t_s = trow + S_COL + x * KEYS, t_o = trow + O_COL + x * D;
     bool ok = true;
     auto wait = [&](int bar, uint32_t parity) {
       ok = ok && __all_sync(FULL, wait_or_stop(d, &bars[bar], parity, stop));
       return ok;
     };
-    uint32_t s_no = 0, o_no = 0;
-    // A warp whose wait gave up goes on to the item's end without waiting or writing results, so that
-    // its partner never waits for it alone; then both stop.
-    for (int n = 0;; ++n) {
-      wait(B_ITEM + (n & 1), (n >> 1) & 1);
-      if (meet_any(meet, !ok)) break;
+    uint32_t s0_no = 0, s1_no = 0, o_no = 0;  // phases of the halves' scores so far, and of outputs
+    for (int n = 0; ok; ++n) {
+      if (!wait(B_ITEM + (n & 1), (n >> 1) & 1)) break;
       const Item& it = items[n & 1];
       const int steps = it.steps;
       if (steps == 0) break;
@@ -450,105 +470,119 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
         const int q_log = si.n_hist + si.n_live - si.t + tok;
         const EdgeSteps edge = edge_steps(si, t0);
         float m = 0.f, l = 0.f;
-        for (int j = 0; j < steps; ++j, ++s_no) {
-          wait(B_S + x, s_no & 1);
-          tc_fence_after();
-          float s[HALF];
-          auto load = [&] {
-            tmem_ld32(t_s, s);
-            tmem_ld32(t_s + 32, s + 32);
-            if (edge.at(j)) {
+        for (int j = 0; ok && j < steps; ++j) {
+          const bool masks = edge.at(j);
+          float add = 0.f;  // the step's part of l
+          // Chunk c of the row's scores: P = 2^(s - m) over what was read of S already.
+          auto weigh = [&](int c, uint32_t (&w)[CHUNK]) {
+            if (masks) {
 #pragma unroll
-              for (int p = 0; p < PAGES / 2; ++p) {
-                const uint32_t seen = slots_seen(si, PAGES * j + PAGES / 2 * half + p, nb, q_log);
+              for (int p = 0; p < CHUNK / PS; ++p) {
+                const uint32_t seen = slots_seen(si, PAGES * j + CHUNK / PS * c + p, nb, q_log);
 #pragma unroll
-                for (int i = 0; i < PS; ++i) s[p * PS + i] = (seen >> i & 1) ? s[p * PS + i] : -INFINITY;
+                for (int i = 0; i < PS; ++i) w[p * PS + i] = (seen >> i & 1) ? w[p * PS + i] : 0xFF800000u;
               }
             }
-          };
-          // P = 2^(s - m), which goes over this half's S, and its sum.
-          float add = 0.f;
-          auto weigh = [&](bool check) {
-            uint32_t pw[HALF / 2];
-            const float2 nref = make_float2(-m, -m);
-            float2 rs[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            auto most = [&] {
+              float a[4];
 #pragma unroll
-            for (int i = 0; i < HALF; i += 2) {
-              const float2 y = __fadd2_rn(make_float2(s[i], s[i + 1]), nref);
-              const float2 p = make_float2(ex2(y.x), ex2(y.y));
-              rs[(i / 2) & 1] = __fadd2_rn(rs[(i / 2) & 1], p);
-              pw[i / 2] = pack_bf16(p.x, p.y);
-            }
-            const float2 r2 = __fadd2_rn(rs[0], rs[1]);
-            add = r2.x + r2.y;
-            if (check && meet_any(meet, !(add < SUM_LIMIT))) return false;
-            __syncwarp();
-            tmem_st32(t_s, pw);
-            return true;
-          };
-          // The first step, and one where a sum is out of bounds against the reference so far (or NaN):
-          // the row's maximum becomes the reference.  (The scores' barrier says that the products
-          // before them are complete too, the last O += P V among them, so O may be rescaled.)
-          bool done = false;
-          if (j > 0) {
-            load();
-            done = weigh(true);
-          }
-          if (!done) {
-            load();
-            float m4[4];
+              for (int i = 0; i < 4; ++i) a[i] = __uint_as_float(w[i]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) m4[i] = s[i];
+              for (int i = 4; i < CHUNK; i += 4)
 #pragma unroll
-            for (int i = 4; i < HALF; i += 4)
+                for (int k = 0; k < 4; ++k) a[k] = fmaxf(a[k], __uint_as_float(w[i + k]));
+              return fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]));
+            };
+            uint32_t pw[CHUNK / 2];
+            auto sum_of = [&] {
+              const float2 nref = make_float2(-m, -m);
+              float2 rs[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-              for (int c = 0; c < 4; ++c) m4[c] = fmaxf(m4[c], s[i + c]);
-            *mine = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-            meet_any(meet, false);
-            const float mx = fmaxf(*mine, *other);
-            const float to = j == 0 ? (mx == -INFINITY ? 0.f : mx) : fmaxf(m, mx);
-            if (j > 0) {
-              const float f = exp2f(m - to);
+              for (int i = 0; i < CHUNK; i += 2) {
+                const float2 y = __fadd2_rn(make_float2(__uint_as_float(w[i]), __uint_as_float(w[i + 1])), nref);
+                const float2 p = make_float2(ex2(y.x), ex2(y.y));
+                rs[(i / 2) & 1] = __fadd2_rn(rs[(i / 2) & 1], p);
+                pw[i / 2] = pack_bf16(p.x, p.y);
+              }
+              const float2 r2 = __fadd2_rn(rs[0], rs[1]);
+              return r2.x + r2.y;
+            };
+            // The reference is the maximum of the row's first chunk (which holds position 0 of what is
+            // resident, so that each row sees a key of it), until a sum passes the limit (or is NaN):
+            // then it rises by a whole number, so that what was written of P scales exactly.  O may be
+            // rescaled behind the last O += P V: the other half's scores come after it, of the same step
+            // behind the second half's of the step before, of the next one behind the first half's.
+            if (j == 0 && c == 0) m = most();
+            float sum = sum_of();
+            if (!__all_sync(FULL, sum < SUM_LIMIT)) {
+              const float up = fmaxf(ceilf(most() - m), 0.f), f = exp2f(-up);
               l *= f;
-              __syncwarp();
+              add *= f;
+              const int h = c / 2;
+              wait(B_S + 2 * x + (h ^ 1), (h == 0 ? s1_no : s0_no) & 1);
+              tc_fence_after();
+              tmem_st_wait();
 #pragma unroll 1
-              for (int c = 0; c < HALF / 16; ++c) {
+              for (int k = 0; (j > 0 || h > 0) && k < D; k += 16) {
                 float o[16];
-                tmem_ld16(t_o + c * 16, o);
+                tmem_ld16(t_o + k, o);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[i] *= f;
-                tmem_st16(t_o + c * 16, o);
+                tmem_st16(t_o + k, o);
               }
+#pragma unroll 1
+              for (int k = 0; k < (c & 1); ++k) {
+                float o[16];
+                uint32_t to[16];
+                tmem_ld16(t_s + h * HALF, o);
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                  to[i] = pack_bf16(bf16lo(__float_as_uint(o[i])) * f, bf16hi(__float_as_uint(o[i])) * f);
+                tmem_st16(t_s + h * HALF, to);
+              }
+              m += up;
+              sum = sum_of();
             }
-            m = to;
-            weigh(false);
+            add += sum;
+            __syncwarp();
+            tmem_st16_begin(t_s + (c >> 1) * HALF + 16 * (c & 1), pw);
+          };
+#pragma unroll 1
+          for (int h = 0; h < 2; ++h) {
+            if (!wait(B_S + 2 * x + h, (h == 0 ? s0_no++ : s1_no++) & 1)) break;
+            tc_fence_after();
+            uint32_t wa[CHUNK], wb[CHUNK];
+            tmem_ld32_begin(t_s + h * HALF, wa);
+            tmem_ld32_begin(t_s + h * HALF + CHUNK, wb);
+            tmem_ld32_wait(wa);
+            tmem_ld32_wait(wb);
+            weigh(2 * h, wa);
+            weigh(2 * h + 1, wb);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars[B_P + 2 * x + h]);
           }
           l += add;
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&bars[B_P + x]);
         }
-        // The row's sum, then dims [64 half, + 64) of its output.
-        wait(B_O + x, o_no & 1);
+        wait(B_S + 2 * x, s0_no++ & 1);
+        if (!ok || !wait(B_O + x, o_no & 1)) break;
         ++o_no;
         tc_fence_after();
-        *mine = l;
-        meet_any(meet, false);
-        const float inv = 1.f / (l + *other);
-        meet_any(meet, false);  // (read before the next item's exchange)
+        const float inv = 1.f / l;
         const bool odd = *reinterpret_cast<volatile const int*>(&it.odd) != 0;
-        __nv_bfloat16* row = out + ((size_t)(si.q_row0 + tok) * d.q_heads + it.head * G + r % G) * D + half * HALF;
+        __nv_bfloat16* row = out + ((size_t)(si.q_row0 + tok) * d.q_heads + it.head * G + r % G) * D;
 #pragma unroll 1
-        for (int c = 0; c < HALF; c += 32) {
+        for (int c = 0; c < D; c += 32) {
           float o[32];
           tmem_ld32(t_o + c, o);
           if (odd && tok < si.t) {
             float more[32];
-            odd_value(d, si, layer, it.head, t0, tok, r % G, q, qk_scale, m, half * HALF + c, more);
+            odd_value(d, si, layer, it.head, t0, tok, r % G, q, qk_scale, m, c, more);
 #pragma unroll
             for (int i = 0; i < 32; ++i) o[i] += more[i];
           }
-          if (ok && tok < si.t) {
+          if (tok < si.t) {
 #pragma unroll
             for (int i = 0; i < 32; i += 8)
               *reinterpret_cast<uint4*>(row + c + i) =
