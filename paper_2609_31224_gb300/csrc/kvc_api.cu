@@ -732,12 +732,8 @@ int kvc_attn_prompt(kvc_ctx* ctx, int layer, const void* d_q, void* d_out, void*
   if (ctx->kv4)
     return fail(KVC_EINVAL, "chunks of more than %d tokens over rows held in 4 bits (KVC_KV4)",
                 PF_MAX_TOKENS);
-  const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  bool capturing = false;
-  KVC_CUDA(is_capturing(s, &capturing));
-  const PageHint pages = page_hint(ctx, capturing);
-  KVC_CUDA(launch_attn_prompt(ctx->d, ctx->lim, layer, d_q, d_out, ctx->last_n_seq, ctx->last_max_t,
-                              pages.max, pages.sum, &ctx->order, s, &ctx->launches));
+  KVC_CUDA(launch_attn_prompt(ctx->d, ctx->lim, layer, d_q, d_out, &ctx->order,
+                              static_cast<cudaStream_t>(stream), &ctx->launches));
   return KVC_OK;
 }
 

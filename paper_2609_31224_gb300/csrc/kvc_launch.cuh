@@ -210,7 +210,6 @@ bool pool_tensor_maps(const Dev& d, CUtensorMap* lo, CUtensorMap* hi);
 bool pool_tile_map(const Dev& d, CUtensorMap* tiles);
 // Whole prompts (kvc_prompt.cu): chunks of any length, rows in the element type.
 cudaError_t launch_attn_prompt(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
-                               int n_seq, int max_t, int pages_max, int64_t pages_sum,
                                LaunchOrder* order, cudaStream_t s, int64_t* launches);
 // Attention weights of the last append's queries, added to weights (kvc_weights.cu).  work: bytes as
 // weights_work_bytes says.

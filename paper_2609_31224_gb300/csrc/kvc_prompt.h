@@ -1,4 +1,4 @@
-// Kernels of whole prompts on the tensor cores (bfloat16), launched by kvc_prompt.cu and kvc_weights.cu.
+// Kernels of whole prompts, launched by kvc_prompt.cu: tensor cores for bfloat16 (tcgen05) and binary32.
 #pragma once
 
 #include "kvc_launch.cuh"
@@ -8,5 +8,8 @@ namespace kvc {
 cudaError_t prompt_tc_attributes();
 cudaError_t launch_prompt_tc(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
                              cudaStream_t s);
+cudaError_t prompt_f32_attributes();  // those of the weights too
+cudaError_t launch_prompt_f32(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
+                              cudaStream_t s);
 
 }  // namespace kvc

@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
       EdgeSteps edge;
       auto fetch = [&] {
         int at = 0, in;
-        if (lane == 0) at = atomicAdd(&d.pf_count[0], 1);
+        if (lane == 0) at = take_item(d);
         at = __shfl_sync(FULL, at, 0);
         steps = 0;
         if (at >= total) return;
@@ -604,11 +604,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
   __syncthreads();
   tc_fence_after();
   if (warp == 1) tmem_dealloc(tmem, ALL_COLS);
-  // The last CTA leaves the counters as it found them.
-  if (tid == 0 && atomicAdd(&d.dec_count[0], 1) == (int)gridDim.x - 1) {
-    d.pf_count[0] = 0;
-    d.dec_count[0] = 0;
-  }
+  if (tid == 0) leave_counters(d);
 }
 
 }  // namespace

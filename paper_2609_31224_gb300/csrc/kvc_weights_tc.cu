@@ -77,14 +77,6 @@ __device__ inline void init_barriers(uint64_t* bars) {
   fence_mbar_init();
 }
 
-// The last CTA leaves the counters as it found them.
-__device__ inline void leave_counters(const Dev& d) {
-  if (threadIdx.x == 0 && atomicAdd(&d.dec_count[0], 1) == (int)gridDim.x - 1) {
-    d.pf_count[0] = 0;
-    d.dec_count[0] = 0;
-  }
-}
-
 // Both pieces' products of a tile: A the rows at a (a_step bytes to its other piece), B at b likewise.
 __device__ inline void piece_products(uint32_t to, uint32_t a, uint32_t a_step, uint32_t b, uint32_t b_step,
                                       uint32_t idesc) {
@@ -145,7 +137,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
         Item* it = items + (n & 1);
         if (n >= 2 && !wait_warp(B_ITEM_EMPTY + (n & 1), ((n >> 1) & 1) ^ 1)) break;
         int at = 0;
-        if (lane == 0) at = atomicAdd(&d.pf_count[0], 1);
+        if (lane == 0) at = take_item(d);
         at = __shfl_sync(FULL, at, 0);
         if (at >= total) {
           if (lane == 0) {
@@ -318,7 +310,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
   __syncthreads();
   tc_fence_after();
   if (warp == 1) tmem_dealloc(tmem, ALL_COLS);
-  leave_counters(d);
+  if (tid == 0) leave_counters(d);
 }
 
 // ---------------------------------------------------------------------------
@@ -374,7 +366,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
         Item* it = items + (n & 1);
         if (n >= 2 && !wait_warp(B_ITEM_EMPTY + (n & 1), ((n >> 1) & 1) ^ 1)) break;
         int at = 0;
-        if (lane == 0) at = atomicAdd(&d.pf_count[0], 1);
+        if (lane == 0) at = take_item(d);
         at = __shfl_sync(FULL, at, 0);
         if (at >= total) {
           if (lane == 0) {
@@ -564,7 +556,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
   __syncthreads();
   tc_fence_after();
   if (warp == 1) tmem_dealloc(tmem, ALL_COLS);
-  leave_counters(d);
+  if (tid == 0) leave_counters(d);
 }
 
 }  // namespace
