@@ -9,8 +9,8 @@
 // Three products for one: a third of the TF32 rate of mma.sync (300 TFLOP/s measured), 100 against the
 // 76 TFLOP/s of the FMA pipes, which a kernel on them reaches a quarter to a half of.
 //
-// A tile is rows of 64 floats in shared memory.  A warp has 16 rows as the A operand in registers and
-// meets a tile of 64 rows as B.  Dims are taken in an order that makes every fragment a 16-byte load: dims
+// A tile is rows of 64 floats in shared memory.  A warp has 16 rows as the A operand, whose pieces lie in
+// shared memory, and meets a tile of 64 rows as B, which it takes apart itself.  Dims are taken in an order that makes every fragment a 16-byte load: dims
 // 16 c + 4 t .. + 3 of a row are lane t's for the steps 2c (first two) and 2c + 1 of the products; of P V
 // the keys 8 s + 2 t, + 1 are lane t's for step s, as the scores' fragments hold them, and output dims
 // 32 h + 4 g .. + 3 are column g of four products.
@@ -30,9 +30,10 @@ namespace {
 
 constexpr int G = 4, D = 64;
 constexpr int WARPS = 8, THREADS = WARPS * 32;
+constexpr int CTAS = 1;                          // of an SM
 constexpr int ROWS = 16 * WARPS;                 // of an item's A operand
 constexpr int TOKENS = ROWS / G;
-constexpr int KT = 64, PAGES = KT / PS;          // keys of a tile
+constexpr int KT = 64, PAGES = KT / PS, NT = KT / 8;  // keys of a tile, eight a product
 constexpr int TILE = KT * D;                     // floats
 constexpr unsigned FULL = 0xFFFFFFFFu;
 constexpr float LOG2E = 1.4426950408889634f;
@@ -58,68 +59,80 @@ struct Pieces {
 };
 __device__ inline Pieces pieces(float x) {
   Pieces p;
-  asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(p.up) : "f"(x));
+  // (Half a unit of the last place that stays, then cut: 10 % faster than the conversion instruction.)
+  p.up = (__float_as_uint(x) + 0x1000u) & 0xFFFFE000u;
   p.low = __float_as_uint(x - __uint_as_float(p.up));
   return p;
 }
 __device__ inline void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+  asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
       "{%0,%1,%2,%3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// A operand: a warp's 16 rows, both pieces, all eight steps of 8 dims.
-struct RowFrag {
-  uint32_t up[8][4], low[8][4];
-  // Rows r0 .. r0 + 15 of a K or Q tile.
-  __device__ void load(const float* tile, int r0, int lane) {
-    const int g = lane >> 2, t = lane & 3;
+// Products of the 16 rows from `rows` on (both pieces, in shared memory; the lower ones `low` floats behind)
+// with the rows 8 n .. 8 n + 7, n < NT, of a tile: s[n][0, 1] of row g and columns 8 n + 2 t, + 1; s[n][2, 3]
+// of row g + 8.
+__device__ inline void products(const float* rows, int low, int r0, const float* tile, int lane,
+                                float (&s)[NT][4]) {
+  const int g = lane >> 2, t = lane & 3;
+  float small[NT][4] = {};
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
+  for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {  // rows g, g + 8
-        const float4 x = *reinterpret_cast<const float4*>(tile + at_k(r0 + g + 8 * h, 4 * c + t));
-        const Pieces p[4] = {pieces(x.x), pieces(x.y), pieces(x.z), pieces(x.w)};
+    for (int i = 0; i < 4; ++i) s[n][i] = 0.f;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          up[2 * c + s][h] = p[2 * s].up;
-          up[2 * c + s][2 + h] = p[2 * s + 1].up;
-          low[2 * c + s][h] = p[2 * s].low;
-          low[2 * c + s][2 + h] = p[2 * s + 1].low;
-        }
-      }
-  }
-  // Products with the rows 8 n .. 8 n + 7, n = 0 .. 7, of a K or Q tile: s[n][0, 1] of row g and columns
-  // 8 n + 2 t, + 1; s[n][2, 3] of row g + 8.
-  __device__ void products(const float* tile, int lane, float (&s)[8][4]) const {
-    const int g = lane >> 2, t = lane & 3;
+  for (int c = 0; c < 4; ++c) {
+    const uint4 u0 = *reinterpret_cast<const uint4*>(rows + at_k(r0 + g, 4 * c + t));
+    const uint4 u1 = *reinterpret_cast<const uint4*>(rows + at_k(r0 + g + 8, 4 * c + t));
+    const uint4 l0 = *reinterpret_cast<const uint4*>(rows + low + at_k(r0 + g, 4 * c + t));
+    const uint4 l1 = *reinterpret_cast<const uint4*>(rows + low + at_k(r0 + g + 8, 4 * c + t));
+    const uint32_t up[2][4] = {{u0.x, u1.x, u0.y, u1.y}, {u0.z, u1.z, u0.w, u1.w}};
+    const uint32_t dn[2][4] = {{l0.x, l1.x, l0.y, l1.y}, {l0.z, l1.z, l0.w, l1.w}};
+    // (An accumulator's products lie four apart.)
 #pragma unroll
-    for (int n = 0; n < 8; ++n) {
-      float big[4] = {0.f, 0.f, 0.f, 0.f}, small[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int n0 = 0; n0 < NT; n0 += 4) {
+      Pieces p[4][4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const float4 x = *reinterpret_cast<const float4*>(tile + at_k(8 * n + g, 4 * c + t));
-        const Pieces p[4] = {pieces(x.x), pieces(x.y), pieces(x.z), pieces(x.w)};
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          mma(big, up[2 * c + i], p[2 * i].up, p[2 * i + 1].up);
-          mma(small, up[2 * c + i], p[2 * i].low, p[2 * i + 1].low);
-          mma(small, low[2 * c + i], p[2 * i].up, p[2 * i + 1].up);
-        }
+      for (int n = 0; n < 4; ++n) {
+        const float4 x = *reinterpret_cast<const float4*>(tile + at_k(8 * (n0 + n) + g, 4 * c + t));
+        p[n][0] = pieces(x.x);
+        p[n][1] = pieces(x.y);
+        p[n][2] = pieces(x.z);
+        p[n][3] = pieces(x.w);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[n][i] = big[i] + small[i];
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n) mma(s[n0 + n], up[i], p[n][2 * i].up, p[n][2 * i + 1].up);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) mma(small[n0 + n], up[i], p[n][2 * i].low, p[n][2 * i + 1].low);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) mma(small[n0 + n], dn[i], p[n][2 * i].up, p[n][2 * i + 1].up);
+      }
     }
   }
-};
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[n][i] += small[n][i];
+}
 
-// The same products in plain arithmetic (slow): a row of `rows` with a row of the tile.
-__device__ __noinline__ float plain_product(const float* rows, int r, const float* tile, int k) {
+// A chunk of a row into its pieces' places.
+__device__ inline void put_pieces(float4 x, float* to, int low) {
+  const Pieces a = pieces(x.x), b = pieces(x.y), c = pieces(x.z), d = pieces(x.w);
+  *reinterpret_cast<uint4*>(to) = make_uint4(a.up, b.up, c.up, d.up);
+  *reinterpret_cast<uint4*>(to + low) = make_uint4(a.low, b.low, c.low, d.low);
+}
+
+// The same in plain arithmetic (slow): a row of `rows` (the sum of its pieces is exact) with one of the tile.
+__device__ __noinline__ float plain_product(const float* rows, int low, int r, const float* tile, int k) {
   float s = 0.f;
   for (int c = 0; c < D / 4; ++c) {
-    const float4 a = *reinterpret_cast<const float4*>(rows + at_k(r, c));
+    float4 a = *reinterpret_cast<const float4*>(rows + at_k(r, c));
+    const float4 l = *reinterpret_cast<const float4*>(rows + low + at_k(r, c));
+    a = make_float4(a.x + l.x, a.y + l.y, a.z + l.z, a.w + l.w);
     const float4 b = *reinterpret_cast<const float4*>(tile + at_k(k, c));
     s = fmaf(a.x, b.x, s);
     s = fmaf(a.y, b.y, s);
@@ -129,57 +142,83 @@ __device__ __noinline__ float plain_product(const float* rows, int r, const floa
   return s;
 }
 
-// Query rows of tokens [t0, t0 + rows / G) of one KV head, rotated and scaled, into a tile; rows past the
-// chunk are zero.
-__device__ inline void stage_rows(const Dev& d, const SeqInfo& si, int head, int t0, int rows, const float* q,
-                                  float scale, float* tile) {
-  for (int i = threadIdx.x; i < rows * 8; i += THREADS) {
-    const int r = i >> 3, c = i & 7, tok = t0 + r / G;
-    float4 ya = make_float4(0.f, 0.f, 0.f, 0.f), yb = ya;
+// Query rows of tokens [t0, t0 + ROWS_ / G) of one KV head, rotated and scaled, into a tile (low: in pieces,
+// the lower ones that many floats behind; 0: as they are); rows past the chunk are zero.
+template <int ROWS_>
+__device__ inline void stage_rows(const Dev& d, const SeqInfo& si, int head, int t0, const float* __restrict__ q,
+                                  float scale, float* tile, int low) {
+  constexpr int PER = ROWS_ * 8 / THREADS;  // 16-byte chunks c and c + 8 (which rotate together) of a row
+  const int c = threadIdx.x & 7;
+  float4 a[PER], b[PER], c0[PER], c1[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int r = (threadIdx.x >> 3) + i * (THREADS / 8), tok = t0 + r / G;
+    a[i] = b[i] = c0[i] = c1[i] = make_float4(0.f, 0.f, 0.f, 0.f);
     if (tok < si.t) {
       const float* row = q + ((size_t)(si.q_row0 + tok) * d.q_heads + head * G + r % G) * D + c * 4;
-      const float4 a = *reinterpret_cast<const float4*>(row), b = *reinterpret_cast<const float4*>(row + D / 2);
       const float4* cs = reinterpret_cast<const float4*>(d.rope + (size_t)(si.pos_first + tok) * (D / 2) + c * 4);
-      const float4 c0 = cs[0], c1 = cs[1];
-      rope_pair(a.x, b.x, make_float2(c0.x, c0.y), ya.x, yb.x);
-      rope_pair(a.y, b.y, make_float2(c0.z, c0.w), ya.y, yb.y);
-      rope_pair(a.z, b.z, make_float2(c1.x, c1.y), ya.z, yb.z);
-      rope_pair(a.w, b.w, make_float2(c1.z, c1.w), ya.w, yb.w);
-      ya = make_float4(ya.x * scale, ya.y * scale, ya.z * scale, ya.w * scale);
-      yb = make_float4(yb.x * scale, yb.y * scale, yb.z * scale, yb.w * scale);
+      a[i] = *reinterpret_cast<const float4*>(row);
+      b[i] = *reinterpret_cast<const float4*>(row + D / 2);
+      c0[i] = cs[0];
+      c1[i] = cs[1];
     }
-    *reinterpret_cast<float4*>(tile + at_k(r, c)) = ya;
-    *reinterpret_cast<float4*>(tile + at_k(r, 8 + c)) = yb;
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int r = (threadIdx.x >> 3) + i * (THREADS / 8);
+    float4 ya, yb;
+    rope_pair(a[i].x, b[i].x, make_float2(c0[i].x, c0[i].y), ya.x, yb.x);
+    rope_pair(a[i].y, b[i].y, make_float2(c0[i].z, c0[i].w), ya.y, yb.y);
+    rope_pair(a[i].z, b[i].z, make_float2(c1[i].x, c1[i].y), ya.z, yb.z);
+    rope_pair(a[i].w, b[i].w, make_float2(c1[i].z, c1[i].w), ya.w, yb.w);
+    ya = make_float4(ya.x * scale, ya.y * scale, ya.z * scale, ya.w * scale);
+    yb = make_float4(yb.x * scale, yb.y * scale, yb.z * scale, yb.w * scale);
+    if (low) {
+      put_pieces(ya, tile + at_k(r, c), low);
+      put_pieces(yb, tile + at_k(r, 8 + c), low);
+    } else {
+      *reinterpret_cast<float4*>(tile + at_k(r, c)) = ya;
+      *reinterpret_cast<float4*>(tile + at_k(r, 8 + c)) = yb;
+    }
   }
 }
 
-// Blocks b0 .. b0 + n_pg - 1 of a session (below nb; zeros past it) into a tile of K and one of V (or none),
-// asynchronously: a thread has chunk tid % 16 of one slot of each page.
-__device__ inline void load_pages(const Dev& d, const SeqInfo& si, int layer, int head, int b0, int n_pg, int nb,
-                                  float* k, float* v) {
+// Pages of blocks b0 .. b0 + N - 1 of a session, -1 from block nb on.
+template <int N>
+__device__ inline void look_up(const Dev& d, const SeqInfo& si, int b0, int nb, int (&pages)[N]) {
   const int32_t* hrow = d.hist_pt + (size_t)si.sid * d.max_pages_per_session;
   const int32_t* lrow = d.live_pt + (size_t)si.sid * d.max_pages_per_session;
-  const int c = threadIdx.x & 15, slot = threadIdx.x >> 4;
-#pragma unroll 4
-  for (int p = 0; p < n_pg; ++p) {
-    const int r = p * PS + slot;
-    if (b0 + p < nb) {
-      const int page = block_page(si, hrow, lrow, b0 + p);
-      const float* src = reinterpret_cast<const float*>(d.pool) +
-                         pool_offset_elems(d, page, layer, 0, head, slot) + c * 4;
-      cp_async16(k + at_k(r, c), src);
-      if (v) cp_async16(v + at_v(r, c), src + (size_t)d.kv_heads * PS * D);
-    } else {
-      *reinterpret_cast<float4*>(k + at_k(r, c)) = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (v) *reinterpret_cast<float4*>(v + at_v(r, c)) = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int p = 0; p < N; ++p) pages[p] = b0 + p < nb ? block_page(si, hrow, lrow, b0 + p) : -1;
+}
+
+// Those pages (zeros for -1) into a tile of K and one of V (or none), asynchronously: a thread has chunk
+// tid % 16 of some slots of each page.
+template <int N>
+__device__ inline void load_pages(const Dev& d, int layer, int head, const int (&pages)[N], float* k, float* v) {
+  const int c = threadIdx.x & 15;
+#pragma unroll
+  for (int p = 0; p < N; ++p) {
+    const int page = pages[p];
+#pragma unroll
+    for (int slot = threadIdx.x >> 4; slot < PS; slot += THREADS / 16) {
+      const int r = p * PS + slot;
+      if (page >= 0) {
+        const float* src = reinterpret_cast<const float*>(d.pool) +
+                           pool_offset_elems(d, page, layer, 0, head, slot) + c * 4;
+        cp_async16(k + at_k(r, c), src);
+        if (v) cp_async16(v + at_v(r, c), src + (size_t)d.kv_heads * PS * D);
+      } else {
+        *reinterpret_cast<float4*>(k + at_k(r, c)) = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (v) *reinterpret_cast<float4*>(v + at_v(r, c)) = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
     }
   }
 }
-static_assert(THREADS == PS * (D / 4), "a thread a chunk of a page");
 
 // Whether one of the numbers that this thread brought is not finite.
 __device__ inline bool odd_pages(int n_pg, const float* k, const float* v) {
-  const int c = threadIdx.x & 15, slot = threadIdx.x >> 4;
+  const int c = threadIdx.x & 15;
   bool odd = false;
   auto look = [&](const float* x) {
     const uint4 w = *reinterpret_cast<const uint4*>(x);
@@ -187,9 +226,9 @@ __device__ inline bool odd_pages(int n_pg, const float* k, const float* v) {
     odd |= (w.x & e) == e || (w.y & e) == e || (w.z & e) == e || (w.w & e) == e;
   };
 #pragma unroll 4
-  for (int p = 0; p < n_pg; ++p) {
-    look(k + at_k(p * PS + slot, c));
-    if (v) look(v + at_v(p * PS + slot, c));
+  for (int r = threadIdx.x >> 4; r < n_pg * PS; r += THREADS / 16) {
+    look(k + at_k(r, c));
+    if (v) look(v + at_v(r, c));
   }
   return odd;
 }
@@ -216,18 +255,18 @@ __device__ inline Item next_item(const Dev& d, int n_seq, const int* s_group, It
 // Attention, and (STATS) the rows' (max, sum) alone.  An item is 32 tokens of one session and KV head,
 // the last ones first, against (STATS: a part of) the keys that they see; a warp has four tokens' rows.
 // ---------------------------------------------------------------------------
-constexpr int PROMPT_SMEM = (ROWS * D + 4 * TILE) * 4;
-constexpr int STAT_SMEM = (ROWS * D + 2 * TILE) * 4;
+constexpr int PROMPT_SMEM = (2 * ROWS * D + 4 * TILE) * 4;
+constexpr int STAT_SMEM = (2 * ROWS * D + 2 * TILE) * 4;
 
 template <bool STATS>
-__global__ void __launch_bounds__(THREADS) prompt_f32_kernel(Dev d, int layer, const float* __restrict__ q,
+__global__ void __launch_bounds__(THREADS, CTAS) prompt_f32_kernel(Dev d, int layer, const float* __restrict__ q,
                                                              float* __restrict__ out, float scale, int parts,
                                                              float2* __restrict__ stats) {
   extern __shared__ __align__(16) float sm[];
   __shared__ int s_group[GROUPS + 1];
   __shared__ Item s_item;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3, H = d.kv_heads;
-  float *s_q = sm, *s_k = sm + ROWS * D, *s_v = s_k + 2 * TILE;
+  float *s_q = sm, *s_k = sm + 2 * ROWS * D, *s_v = s_k + 2 * TILE;
   pdl_wait();
   pdl_launch_dependents();
   const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;  // (no units: the append failed)
@@ -241,36 +280,37 @@ __global__ void __launch_bounds__(THREADS) prompt_f32_kernel(Dev d, int layer, c
     const int t0 = ((si.t + TOKENS - 1) / TOKENS - 1 - it.in / H / parts) * TOKENS;
     const int nb = blocks_seen(si, min(t0 + TOKENS, si.t) - 1), all = (nb + PAGES - 1) / PAGES;
     const int j0 = (int)((int64_t)all * part / parts), j1 = (int)((int64_t)all * (part + 1) / parts);
+    int pages[PAGES];  // of the next tile to load
+    look_up(d, si, PAGES * j0, nb, pages);
     auto load = [&](int j) {
-      load_pages(d, si, layer, head, PAGES * j, PAGES, nb, s_k + (j & 1) * TILE, STATS ? nullptr : s_v + (j & 1) * TILE);
+      load_pages(d, layer, head, pages, s_k + (j & 1) * TILE, STATS ? nullptr : s_v + (j & 1) * TILE);
       cp_async_commit();
+      look_up(d, si, PAGES * (j + 1), nb, pages);
     };
     if (j0 < j1) load(j0);
-    stage_rows(d, si, head, t0, ROWS, q, scale, s_q);
+    stage_rows<ROWS>(d, si, head, t0, q, scale, s_q, ROWS * D);
     // This lane's rows: 16 warp + g and + 8, of tokens two apart.
     const int tok0 = t0 + 4 * warp + g / G, q_log0 = si.n_hist + si.n_live - si.t;
     const int q_log[2] = {q_log0 + tok0, q_log0 + tok0 + 2};
     const int q_first = q_log0 + t0 + 4 * warp;            // the warp's first token
     const int nb_warp = blocks_seen(si, min(t0 + 4 * warp + 3, si.t - 1));
-    RowFrag rows;
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
     float o[8][4] = {};                                     // [4 h + j]: see above
     for (int j = j0; j < j1; ++j) {
       const float *kt = s_k + (j & 1) * TILE, *vt = s_v + (j & 1) * TILE;
       cp_async_wait_all();
       const bool odd = __syncthreads_or(odd_pages(PAGES, kt, STATS ? nullptr : vt));
-      if (j == j0) rows.load(s_q, 16 * warp, lane);
       if (j + 1 < j1) load(j + 1);
       if (PAGES * j >= nb_warp) continue;                   // behind all tokens of the warp
-      float s[8][4];
+      float s[NT][4];
       if (!odd) {
-        rows.products(kt, lane, s);
+        products(s_q, ROWS * D, 16 * warp, kt, lane, s);
       } else {
 #pragma unroll
-        for (int n = 0; n < 8; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            s[n][i] = plain_product(s_q, 16 * warp + g + (i >> 1) * 8, kt, 8 * n + 2 * t + (i & 1));
+            s[n][i] = plain_product(s_q, ROWS * D, 16 * warp + g + (i >> 1) * 8, kt, 8 * n + 2 * t + (i & 1));
       }
       uint32_t seen[2][PAGES];                              // slots of the pages that the rows see
       bool whole = true;
@@ -285,7 +325,7 @@ __global__ void __launch_bounds__(THREADS) prompt_f32_kernel(Dev d, int layer, c
 #pragma unroll
           for (int h = 0; h < 2; ++h) seen[h][p] = slots_seen(si, PAGES * j + p, nb, q_log[h]);
 #pragma unroll
-        for (int n = 0; n < 8; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             if (!(seen[i >> 1][n >> 1] >> (8 * (n & 1) + 2 * t + (i & 1)) & 1)) s[n][i] = -INFINITY;
@@ -295,7 +335,7 @@ __global__ void __launch_bounds__(THREADS) prompt_f32_kernel(Dev d, int layer, c
       for (int h = 0; h < 2; ++h) {
         float mx = -INFINITY;
 #pragma unroll
-        for (int n = 0; n < 8; ++n) mx = fmaxf(mx, fmaxf(s[n][2 * h], s[n][2 * h + 1]));
+        for (int n = 0; n < NT; ++n) mx = fmaxf(mx, fmaxf(s[n][2 * h], s[n][2 * h + 1]));
         mx = fmaxf(mx, __shfl_xor_sync(FULL, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(FULL, mx, 2));
         const float mn = fmaxf(m[h], mx), ref = mn == -INFINITY ? 0.f : mn;
@@ -303,7 +343,7 @@ __global__ void __launch_bounds__(THREADS) prompt_f32_kernel(Dev d, int layer, c
         m[h] = mn;
         float sum = 0.f;
 #pragma unroll
-        for (int n = 0; n < 8; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             s[n][2 * h + e] = ex2(s[n][2 * h + e] - ref);
@@ -313,41 +353,41 @@ __global__ void __launch_bounds__(THREADS) prompt_f32_kernel(Dev d, int layer, c
       }
       if constexpr (!STATS) {
         if (!odd) {
-          float big[8][4] = {}, small[8][4] = {};
+          Pieces p[NT][4];  // A: rows g, g + 8 of key 2 t, then of key 2 t + 1
 #pragma unroll
-          for (int n = 0; n < 8; ++n) {  // 8 keys
-            uint32_t up[4], low[4];
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {  // A: rows g, g + 8 of key 2 t, then of key 2 t + 1
-              const Pieces p = pieces(s[n][(i & 1) * 2 + (i >> 1)]);
-              up[i] = p.up;
-              low[i] = p.low;
-            }
+            for (int i = 0; i < 4; ++i) p[n][i] = pieces(s[n][(i & 1) * 2 + (i >> 1)]);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+          for (int h = 0; h < 2; ++h) {  // 32 dims
+            float big[4][4] = {}, small[4][4] = {};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
               const float4 a = *reinterpret_cast<const float4*>(vt + at_v(8 * n + 2 * t, 8 * h + g));
               const float4 b = *reinterpret_cast<const float4*>(vt + at_v(8 * n + 2 * t + 1, 8 * h + g));
-              const float x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
+              const Pieces p0[4] = {pieces(a.x), pieces(a.y), pieces(a.z), pieces(a.w)};
+              const Pieces p1[4] = {pieces(b.x), pieces(b.y), pieces(b.z), pieces(b.w)};
+              const uint32_t up[4] = {p[n][0].up, p[n][1].up, p[n][2].up, p[n][3].up};
+              const uint32_t dn[4] = {p[n][0].low, p[n][1].low, p[n][2].low, p[n][3].low};
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const Pieces p0 = pieces(x[i]), p1 = pieces(y[i]);
-                mma(big[4 * h + i], up, p0.up, p1.up);
-                mma(small[4 * h + i], up, p0.low, p1.low);
-                mma(small[4 * h + i], low, p0.up, p1.up);
-              }
+              for (int i = 0; i < 4; ++i) mma(big[i], up, p0[i].up, p1[i].up);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) mma(small[i], up, p0[i].low, p1[i].low);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) mma(small[i], dn, p0[i].up, p1[i].up);
             }
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[4 * h + n][i] = fmaf(o[4 * h + n][i], al[i >> 1], big[n][i] + small[n][i]);
           }
-#pragma unroll
-          for (int n = 0; n < 8; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[n][i] = fmaf(o[n][i], al[i >> 1], big[n][i] + small[n][i]);
         } else {
 #pragma unroll
           for (int n = 0; n < 8; ++n)
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[n][i] *= al[i >> 1];
 #pragma unroll
-          for (int n = 0; n < 8; ++n)
+          for (int n = 0; n < NT; ++n)
 #pragma unroll 1
             for (int k = 0; k < 8; ++k) {
               const int from = (lane & ~3) | (k >> 1), slot = 8 * (n & 1) + k;
@@ -399,17 +439,18 @@ __global__ void __launch_bounds__(THREADS) prompt_f32_kernel(Dev d, int layer, c
 // ---------------------------------------------------------------------------
 constexpr int KEYS = 16 * WARPS, KEY_PAGES = KEYS / PS;
 constexpr int STEP_TOKENS = KT / G;
-constexpr int SUMS_SMEM = (KEYS * D + 2 * TILE) * 4;
+constexpr int SUMS_SMEM = (2 * KEYS * D + 2 * TILE) * 4;
 
-__global__ void __launch_bounds__(THREADS) weights_sums_f32_kernel(Dev d, int layer,
+__global__ void __launch_bounds__(THREADS, CTAS) weights_sums_f32_kernel(Dev d, int layer,
                                                                    const float* __restrict__ q, float scale,
                                                                    int parts, int shares, WeightsWork work) {
   extern __shared__ __align__(16) float sm[];
   __shared__ int s_group[GROUPS + 1];
   __shared__ Item s_item;
   __shared__ __align__(8) float s_lse[2][KT];
+  static_assert(KT <= THREADS, "a thread a row");
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3, H = d.kv_heads;
-  float *s_k = sm, *s_q = sm + KEYS * D;
+  float *s_k = sm, *s_q = sm + 2 * KEYS * D;
   pdl_wait();
   pdl_launch_dependents();
   const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;
@@ -426,9 +467,16 @@ __global__ void __launch_bounds__(THREADS) weights_sums_f32_kernel(Dev d, int la
     const int i0 = max((int)((int64_t)steps * share / shares), first);
     const int i1 = max(i0, (int)((int64_t)steps * (share + 1) / shares));
     if (i0 < i1) {
-      load_pages(d, si, layer, head, b0, KEY_PAGES, si.n_blocks, s_k, nullptr);
+      int pages[KEY_PAGES];
+      look_up(d, si, b0, si.n_blocks, pages);
+      load_pages(d, layer, head, pages, s_k, nullptr);
       cp_async_commit();
       cp_async_wait_all();
+      // Into pieces: each thread what it brought.
+      for (int r = tid >> 4; r < KEYS; r += THREADS / 16) {
+        float* at = s_k + at_k(r, tid & 15);
+        put_pieces(*reinterpret_cast<const float4*>(at), at, KEYS * D);
+      }
     }
     // This lane's keys: 16 warp + g and + 8, and the first token that sees each.
     const int blk = b0 + warp;
@@ -440,11 +488,10 @@ __global__ void __launch_bounds__(THREADS) weights_sums_f32_kernel(Dev d, int la
       in[h] = g + 8 * h >= br.lo && g + 8 * h < br.hi;
       from[h] = br.base + g + 8 * h - q_log0;
     }
-    RowFrag rows;
     float sum[2] = {0.f, 0.f}, rest[2] = {0.f, 0.f};  // (rest: what additions to the sums rounded off)
     for (int i = i0; i < i1; ++i) {
       float* tile = s_q + (i & 1) * TILE;
-      stage_rows(d, si, head, i * STEP_TOKENS, KT, q, scale, tile);
+      stage_rows<KT>(d, si, head, i * STEP_TOKENS, q, scale, tile, 0);
       if (tid < KT) {  // rows past the chunk draw nothing
         const int tok = i * STEP_TOKENS + tid / G;
         float m = INFINITY, l = 1.f;
@@ -462,11 +509,10 @@ __global__ void __launch_bounds__(THREADS) weights_sums_f32_kernel(Dev d, int la
         s_lse[i & 1][tid] = m + log2f(l);
       }
       __syncthreads();
-      if (i == i0) rows.load(s_k, 16 * warp, lane);
-      float s[8][4], add[2] = {0.f, 0.f};
-      rows.products(tile, lane, s);
+      float s[NT][4], add[2] = {0.f, 0.f};
+      products(s_k, KEYS * D, 16 * warp, tile, lane, s);
 #pragma unroll
-      for (int n = 0; n < 8; ++n) {
+      for (int n = 0; n < NT; ++n) {
         const float2 lse = *reinterpret_cast<const float2*>(&s_lse[i & 1][8 * n + 2 * t]);
         const int tok = i * STEP_TOKENS + (8 * n + 2 * t) / G;
 #pragma unroll
@@ -510,7 +556,7 @@ cudaError_t prompt_f32_attributes() {
 
 cudaError_t launch_prompt_f32(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
                               cudaStream_t s) {
-  return launch_ex(&prompt_f32_kernel<false>, dim3(lim.sms), dim3(THREADS), PROMPT_SMEM, s, true, d, layer,
+  return launch_ex(&prompt_f32_kernel<false>, dim3(lim.sms * CTAS), dim3(THREADS), PROMPT_SMEM, s, true, d, layer,
                    static_cast<const float*>(q), static_cast<float*>(out), score_scale(), 1,
                    static_cast<float2*>(nullptr));
 }
@@ -519,11 +565,11 @@ cudaError_t launch_weights_f32(const Dev& d, const Limits& lim, int layer, const
                                const WeightsWork& work, int parts, int shares, cudaStream_t s,
                                int64_t* launches) {
   const float* qf = static_cast<const float*>(q);
-  cudaError_t e = launch_ex(&prompt_f32_kernel<true>, dim3(lim.sms * 2), dim3(THREADS), STAT_SMEM, s, true, d,
+  cudaError_t e = launch_ex(&prompt_f32_kernel<true>, dim3(lim.sms * CTAS), dim3(THREADS), STAT_SMEM, s, true, d,
                             layer, qf, static_cast<float*>(nullptr), score_scale(), parts, work.stats);
   *launches += e == cudaSuccess;
   if (e != cudaSuccess) return e;
-  e = launch_ex(&weights_sums_f32_kernel, dim3(lim.sms * 2), dim3(THREADS), SUMS_SMEM, s, true, d, layer, qf,
+  e = launch_ex(&weights_sums_f32_kernel, dim3(lim.sms * CTAS), dim3(THREADS), SUMS_SMEM, s, true, d, layer, qf,
                 score_scale(), parts, shares, work);
   *launches += e == cudaSuccess;
   return e;

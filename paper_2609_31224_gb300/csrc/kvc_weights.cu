@@ -91,7 +91,7 @@ cudaError_t launch_attn_weights(const Dev& d, const Limits& lim, int layer, cons
   if (max_t == 1) return launch_weights_token(d, lim, layer, q, weights, w, n_seq, early, s, launches);
   // Where the chunk's rows alone are too few items (64 tokens of a KV head, or 32), the keys are cut into
   // parts; where the keys are (256, or 128), the tokens into shares.
-  const int64_t tokens = d.esz == 2 ? 64 : 32, pages = d.esz == 2 ? 16 : 8, ctas = lim.sms * (d.esz == 2 ? 1 : 2);
+  const int64_t tokens = d.esz == 2 ? 64 : 32, pages = d.esz == 2 ? 16 : 8, ctas = lim.sms;
   const int64_t rows = ((int64_t)total + (tokens - 1) * n_seq) / tokens * d.kv_heads;
   const int64_t stats = (int64_t)d.max_tokens * d.q_heads + WEIGHTS_STATS;
   int64_t parts = std::max<int64_t>(1, std::min<int64_t>(2 * ctas / rows, (pages_max + 7) / 8));
