@@ -434,7 +434,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
       const int tiles = it.t0 + TOKENS < it.si.t ? 2 : 1;
       for (int x = 0; x < tiles; ++x, ++q_no) {
         const int slot = q_no % Q_SLOTS;
-        stage_q<1, G>(d, it.si, it.head, it.t0 + x * TOKENS, q, qk_scale, s_q + slot * SLOT, ts,
+        stage_q<1, 128>(d, it.si, it.head, it.t0 + x * TOKENS, q, qk_scale, s_q + slot * SLOT, ts,
                       [&] { return q_no < Q_SLOTS || wait(B_Q_EMPTY + slot, ((q_no / Q_SLOTS) & 1) ^ 1); });
         if (!ok) break;
         fence_proxy_async_smem();

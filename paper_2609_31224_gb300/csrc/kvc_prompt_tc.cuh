@@ -94,26 +94,26 @@ __device__ inline EdgeSteps edge_steps(const SeqInfo& si, int t0) {
           (si.n_hist % PS) ? (nhp - 1) / PAGES : -1, si.live_head ? nhp / PAGES : -1};
 }
 
-// Query rows of tokens [t0, t0 + TOKENS) of one KV head by the 128 threads `ts`: rotated, scaled and
+// Query rows of tokens [t0, t0 + TOKENS) of one KV head by the N threads `ts`: rotated, scaled and
 // rounded into the swizzled tile at `to`; PIECES = 2: what rounding left, rounded too, into the tile
 // behind it.  Rows past the chunk are zero.  `free` waits until the tile may be written (false: give up).
-// A thread takes 16-byte chunks c and c + 8 (which rotate together) of a token's G rows, HEADS at a time.
-template <int PIECES, int HEADS, typename FreeFn>
+// A thread takes 16-byte chunks c and c + 8 (which rotate together) of a token's G rows.
+template <int PIECES, int N, typename FreeFn>
 __device__ inline void stage_q(const Dev& d, const SeqInfo& si, int head, int t0, const __nv_bfloat16* q,
                                float qk_scale, uint8_t* to, int ts, FreeFn free) {
   const int c = ts & 7;
 #pragma unroll 1
-  for (int step = 0; step < 2 * G / HEADS; ++step) {
-    const int tl = (ts >> 3) + 16 * (step / (G / HEADS)), g0 = step % (G / HEADS) * HEADS, tok = t0 + tl;
-    uint4 a[HEADS], b[HEADS];
+  for (int step = 0; step < TOKENS * 8 / N; ++step) {
+    const int tl = (ts >> 3) + N / 8 * step, tok = t0 + tl;
+    uint4 a[G], b[G];
     float4 cs[4];
     const bool in = tok < si.t;
     if (in) {
       const uint4* row = reinterpret_cast<const uint4*>(
-          q + ((size_t)(si.q_row0 + tok) * d.q_heads + head * G + g0) * D) + c;
+          q + ((size_t)(si.q_row0 + tok) * d.q_heads + head * G) * D) + c;
       const float4* t4 = reinterpret_cast<const float4*>(d.rope + (size_t)(si.pos_first + tok) * (D / 2) + c * 8);
 #pragma unroll
-      for (int g = 0; g < HEADS; ++g) {
+      for (int g = 0; g < G; ++g) {
         a[g] = row[g * 16];
         b[g] = row[g * 16 + 8];
       }
@@ -122,7 +122,7 @@ __device__ inline void stage_q(const Dev& d, const SeqInfo& si, int head, int t0
     }
     if (step == 0 && !free()) return;
 #pragma unroll
-    for (int g = 0; g < HEADS; ++g) {
+    for (int g = 0; g < G; ++g) {
       uint32_t ya[PIECES][4] = {}, yb[PIECES][4] = {};
       if (in) {
         const uint32_t ua[4] = {a[g].x, a[g].y, a[g].z, a[g].w};
@@ -142,7 +142,7 @@ __device__ inline void stage_q(const Dev& d, const SeqInfo& si, int head, int t0
           }
         }
       }
-      const int r = tl * G + g0 + g;
+      const int r = tl * G + g;
 #pragma unroll
       for (int p = 0; p < PIECES; ++p) {
         uint8_t* at = to + p * SLOT + tile_at(r, c);

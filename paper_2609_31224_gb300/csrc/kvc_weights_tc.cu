@@ -11,8 +11,9 @@
 //                         sum crosses threads
 // The sums of heads and shares are added up by weights_add_kernel (kvc_weights.cu) in their order.
 // Both are bound by the products, 2 x 512 cycles a tile of 128 x 128; its exponentials take half of that.
-// Warp roles as in kvc_prompt_tc.cu: warp 0 items and K by TMA, warp 1 the products, warps 4-7 query
-// tiles, warps 8-15 what becomes of the scores.  All waits are bounded.
+// Warp roles as in kvc_prompt_tc.cu: warp 0 items and K by TMA, warp 1 the products, warps 4-11
+// query tiles (with four warps they were what the products waited for), warps 12-19 what becomes of the
+// scores.  All waits are bounded.
 #include <cuda.h>
 
 #include <cmath>
@@ -24,9 +25,10 @@ namespace kvc {
 
 namespace {
 
-constexpr int TC_THREADS = 512;
-// Registers a thread of the issuing and query warps, and of the last 256 threads (512 x 128 together).
-constexpr int FEW_REGS = 96, MANY_REGS = 160;
+constexpr int Q_WARPS = 8, Q_THREADS = Q_WARPS * 32;
+constexpr int TC_THREADS = 128 + Q_THREADS + 256;
+constexpr int CHUNK = 32;                          // columns that a row takes at a time
+constexpr float SUM_LIMIT = 1048576.f;              // 2^20, see below
 constexpr int K_RING = 3;
 constexpr int LSE_RING = 4;                        // query tiles whose lse is kept
 constexpr int ALL_COLS = 512;                      // two tiles' scores, twice each: 4 x 128 columns
@@ -52,7 +54,7 @@ enum {
   N_BARS = B_FINAL + 1
 };
 static_assert(N_BARS * 8 <= OFF_ITEM, "barriers fit");
-constexpr int ITEM_READERS = 1 + 4 + 8;
+constexpr int ITEM_READERS = 1 + Q_WARPS + 8;
 
 struct Item {
   SeqInfo si;
@@ -67,7 +69,7 @@ static_assert(sizeof(Item) == 128, "Item size");
 
 __device__ inline void init_barriers(uint64_t* bars) {
   for (int i = 0; i < N_BARS; ++i) {
-    const int count = i >= B_Q_FULL && i < B_Q_EMPTY         ? 4
+    const int count = i >= B_Q_FULL && i < B_Q_EMPTY         ? Q_WARPS
                       : i >= B_S_EMPTY && i < B_ITEM         ? 4
                       : i >= B_ITEM_EMPTY && i < B_LSE_EMPTY ? ITEM_READERS
                       : i >= B_LSE_EMPTY && i < B_FINAL      ? 8
@@ -129,7 +131,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
   };
 
   if (warp < 4) {
-    set_registers<128, FEW_REGS>();
     if (warp == 0) {
       const int total = s_group[GROUPS];
         uint32_t k_no = 0;
@@ -221,8 +222,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
         mbar_wait(d, &bars[B_FINAL], 0);
       }
     }
-  } else if (warp < 8) {
-    set_registers<128, FEW_REGS>();
+  } else if (warp < 4 + Q_WARPS) {
     const int ts = tid - 4 * 32;
     uint32_t q_no[2] = {0, 0};
     for (int n = 0; ok; ++n) {
@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
       if (!it.valid) break;
       const int tiles = it.at + TOKENS < it.si.t ? 2 : 1;
       for (int x = 0; x < tiles && ok && it.begin < it.end; ++x) {
-        stage_q<2, G>(d, it.si, it.head, it.at + x * TOKENS, q, qk_scale, s_q + 2 * x * SLOT, ts,
+        stage_q<2, Q_THREADS>(d, it.si, it.head, it.at + x * TOKENS, q, qk_scale, s_q + 2 * x * SLOT, ts,
                    [&] { return q_no[x] == 0 || wait_warp(B_Q_EMPTY + x, (q_no[x] - 1) & 1); });
         if (!ok) break;
         ++q_no[x];
@@ -243,8 +243,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
       if (lane == 0) mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
     }
   } else {
-    set_registers<128, MANY_REGS>();
-    const int x = (warp - 8) >> 2, r = (warp & 3) * 32 + lane;
+    const int x = (warp - 4 - Q_WARPS) >> 2, r = (warp & 3) * 32 + lane;
     const uint32_t trow = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     uint32_t s_no = 0;
     for (int n = 0; ok; ++n) {
@@ -262,40 +261,59 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
           const int b = 2 * x + (s_no & 1);
           if (!wait_warp(B_S + b, (s_no >> 1) & 1)) break;
           tc_fence_after();
-          float s[KEYS];
-          tmem_ld64(trow + b * KEYS, s);
-          tmem_ld64(trow + b * KEYS + 64, s + 64);
+          // The reference is the maximum of the first keys, until a sum against it passes the limit (or is
+          // NaN); sums and roundings do not depend on its scale.
+          const bool masks = edge.at(j);
+          float add = 0.f;
+#pragma unroll 1
+          for (int c = 0; c < KEYS / CHUNK; ++c) {
+            uint32_t w[CHUNK];
+            tmem_ld32_begin(trow + b * KEYS + CHUNK * c, w);
+            tmem_ld32_wait(w);
+            if (masks) {
+#pragma unroll
+              for (int p = 0; p < CHUNK / PS; ++p) {
+                const uint32_t seen = slots_seen(si, PAGES * j + CHUNK / PS * c + p, nb, q_log);
+#pragma unroll
+                for (int i = 0; i < PS; ++i) w[p * PS + i] = (seen >> i & 1) ? w[p * PS + i] : 0xFF800000u;
+              }
+            }
+            auto most = [&] {
+              float a[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) a[i] = __uint_as_float(w[i]);
+#pragma unroll
+              for (int i = 4; i < CHUNK; i += 4)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) a[k] = fmaxf(a[k], __uint_as_float(w[i + k]));
+              return fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]));
+            };
+            auto sum_of = [&] {
+              const float ref = m == -INFINITY ? 0.f : m;  // (a row that has seen no key yet)
+              const float2 nref = make_float2(-ref, -ref);
+              float2 rs[4] = {};
+#pragma unroll
+              for (int i = 0; i < CHUNK; i += 2) {
+                const float2 y = __fadd2_rn(make_float2(__uint_as_float(w[i]), __uint_as_float(w[i + 1])), nref);
+                rs[(i / 2) & 3] = __fadd2_rn(rs[(i / 2) & 3], make_float2(ex2(y.x), ex2(y.y)));
+              }
+              const float2 r2 = __fadd2_rn(__fadd2_rn(rs[0], rs[1]), __fadd2_rn(rs[2], rs[3]));
+              return r2.x + r2.y;
+            };
+            float sum = m == -INFINITY ? INFINITY : sum_of();
+            if (!__all_sync(FULL, sum < SUM_LIMIT)) {
+              const float to = fmaxf(m, most()), f = m == -INFINITY ? 0.f : exp2f(m - to);
+              l *= f;
+              add *= f;
+              m = to;
+              sum = sum_of();
+            }
+            add += sum;
+          }
+          l += add;
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(&bars[B_S_EMPTY + b]);
-          if (edge.at(j)) {
-#pragma unroll
-            for (int p = 0; p < PAGES; ++p) {
-              const uint32_t seen = slots_seen(si, PAGES * j + p, nb, q_log);
-#pragma unroll
-              for (int i = 0; i < PS; ++i) s[p * PS + i] = (seen >> i & 1) ? s[p * PS + i] : -INFINITY;
-            }
-          }
-          float m8[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) m8[i] = s[i];
-#pragma unroll
-          for (int i = 8; i < KEYS; i += 8)
-#pragma unroll
-            for (int c = 0; c < 8; ++c) m8[c] = fmaxf(m8[c], s[i + c]);
-          const float mx = fmaxf(fmaxf(fmaxf(m8[0], m8[1]), fmaxf(m8[2], m8[3])),
-                                 fmaxf(fmaxf(m8[4], m8[5]), fmaxf(m8[6], m8[7])));
-          const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.f : mn;
-          const float2 nref = make_float2(-ref, -ref);
-          float2 rs[4] = {};
-#pragma unroll
-          for (int i = 0; i < KEYS; i += 2) {
-            const float2 y = __fadd2_rn(make_float2(s[i], s[i + 1]), nref);
-            rs[(i / 2) & 3] = __fadd2_rn(rs[(i / 2) & 3], make_float2(ex2(y.x), ex2(y.y)));
-          }
-          const float2 r2 = __fadd2_rn(__fadd2_rn(rs[0], rs[1]), __fadd2_rn(rs[2], rs[3]));
-          l = l * exp2_safe(m, ref) + (r2.x + r2.y);
-          m = mn;
         }
         if (ok && tok < si.t)
           work.stats[((size_t)it.part * d.g->total_tokens + si.q_row0 + tok) * d.q_heads + it.head * G + r % G] =
@@ -358,7 +376,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
   };
 
   if (warp < 4) {
-    set_registers<128, FEW_REGS>();
     if (warp == 0) {
       const int total = s_group[GROUPS];
         uint32_t k_no = 0;
@@ -448,8 +465,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
         mbar_wait(d, &bars[B_FINAL], 0);
       }
     }
-  } else if (warp < 8) {
-    set_registers<128, FEW_REGS>();
+  } else if (warp < 4 + Q_WARPS) {
     const int ts = tid - 4 * 32;
     uint32_t q_no = 0;
     const int total = d.g->total_tokens;
@@ -462,7 +478,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
         // Row ts of the tile: its parts' (max, sum) joined; rows past the chunk draw nothing.
         const int tok = i * TOKENS + ts / G;
         float m = INFINITY, l = 1.f;
-        if (tok < si.t) {
+        if (ts < M && tok < si.t) {
           const float2* row = work.stats + (size_t)(si.q_row0 + tok) * d.q_heads + it.head * G + ts % G;
           m = row->x;
           l = row->y;
@@ -473,11 +489,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
             m = mn;
           }
         }
-        stage_q<2, G>(d, si, it.head, i * TOKENS, q, qk_scale, s_q + (q_no & 1) * 2 * SLOT, ts,
+        stage_q<2, Q_THREADS>(d, si, it.head, i * TOKENS, q, qk_scale, s_q + (q_no & 1) * 2 * SLOT, ts,
                    [&] { return q_no < 2 || wait_warp(B_Q_EMPTY + (q_no & 1), ((q_no >> 1) & 1) ^ 1); });
         if (!ok) break;
         if (q_no >= LSE_RING && !wait_warp(B_LSE_EMPTY + q_no % LSE_RING, ((q_no / LSE_RING) & 1) ^ 1)) break;
-        s_lse[(q_no % LSE_RING) * M + ts] = m + log2f(l);
+        if (ts < M) s_lse[(q_no % LSE_RING) * M + ts] = m + log2f(l);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars[B_Q_FULL + (q_no & 1)]);
@@ -486,8 +502,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
       if (lane == 0) mbar_arrive(&bars[B_ITEM_EMPTY + (n & 1)]);
     }
   } else {
-    set_registers<128, MANY_REGS>();
-    const int x = (warp - 8) >> 2, r = (warp & 3) * 32 + lane;
+    const int x = (warp - 4 - Q_WARPS) >> 2, r = (warp & 3) * 32 + lane;
     const uint32_t trow = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     uint32_t s_no = 0, q_no = 0;
     for (int n = 0; ok; ++n) {
