@@ -464,8 +464,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) weights_sums_f32_kernel(Dev d, 
     const int head = it.in % H, share = it.in / H % shares, b0 = it.in / H / shares * KEY_PAGES;
     const int steps = (si.t + STEP_TOKENS - 1) / STEP_TOKENS, q_log0 = si.n_hist + si.n_live - si.t;
     const int first = max(0, block_range(si, b0).base - q_log0) / STEP_TOKENS;
-    const int i0 = max((int)((int64_t)steps * share / shares), first);
-    const int i1 = max(i0, (int)((int64_t)steps * (share + 1) / shares));
+    const int i0 = first + (int)((int64_t)(steps - first) * share / shares);
+    const int i1 = first + (int)((int64_t)(steps - first) * (share + 1) / shares);
     if (i0 < i1) {
       int pages[KEY_PAGES];
       look_up(d, si, b0, si.n_blocks, pages);

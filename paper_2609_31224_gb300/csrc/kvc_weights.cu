@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(THREADS) weights_add_kernel(Dev d, int planes,
                                 d.live_pt + (size_t)si.sid * d.max_pages_per_session, at / PS);
     const int gs = page * PS + at % PS;
     float w = 0.f;
-#pragma unroll 8
+#pragma unroll 16
     for (int h = 0; h < planes; ++h) w += work.scores[h * plane + gs];
     weights[(size_t)si.sid * d.max_positions + d.meta_pos[gs]] += w;
   }

@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_stat_kernel(
   if (warp < 4) {
     if (warp == 0) {
       const int total = s_group[GROUPS];
-        uint32_t k_no = 0;
+      uint32_t k_no = 0;
       for (int n = 0; ok; ++n) {
         Item* it = items + (n & 1);
         if (n >= 2 && !wait_warp(B_ITEM_EMPTY + (n & 1), ((n >> 1) & 1) ^ 1)) break;
@@ -378,7 +378,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
   if (warp < 4) {
     if (warp == 0) {
       const int total = s_group[GROUPS];
-        uint32_t k_no = 0;
+      uint32_t k_no = 0;
       for (int n = 0; ok; ++n) {
         Item* it = items + (n & 1);
         if (n >= 2 && !wait_warp(B_ITEM_EMPTY + (n & 1), ((n >> 1) & 1) ^ 1)) break;
@@ -401,8 +401,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) weights_sums_kernel(
         const int head = in % H, share = in / H % shares, b0 = in / H / shares * 2 * PAGES;
         const int n_t = (si.t + TOKENS - 1) / TOKENS, q_log0 = si.n_hist + si.n_live - si.t;
         const int first = max(0, block_range(si, b0).base - q_log0) / TOKENS;
-        const int i0 = max((int)((int64_t)n_t * share / shares), first);
-        const int i1 = max(i0, (int)((int64_t)n_t * (share + 1) / shares));
+        // (The tokens that see a key of the tile, shared out evenly: long items come first.)
+        const int i0 = first + (int)((int64_t)(n_t - first) * share / shares);
+        const int i1 = first + (int)((int64_t)(n_t - first) * (share + 1) / shares);
         if (lane == 0) {
           it->valid = 1;
           it->head = head;
