@@ -466,11 +466,23 @@ __global__ void __launch_bounds__(THREADS, CTAS) weights_sums_f32_kernel(Dev d, 
     const int first = max(0, block_range(si, b0).base - q_log0) / STEP_TOKENS;
     const int i0 = first + (int)((int64_t)(steps - first) * share / shares);
     const int i1 = first + (int)((int64_t)(steps - first) * (share + 1) / shares);
+    auto stage = [&](int i) {
+      stage_rows<KT>(d, si, head, i * STEP_TOKENS, q, scale, s_q + (i & 1) * TILE, 0);
+      if (tid < KT) {  // rows past the chunk draw nothing
+        const int tok = i * STEP_TOKENS + tid / G;
+        float lse = INFINITY;
+        if (tok < si.t)
+          lse = row_lse(work.stats + (size_t)(si.q_row0 + tok) * d.q_heads + head * G + tid % G,
+                        (size_t)total * d.q_heads, parts);
+        s_lse[i & 1][tid] = lse;
+      }
+    };
     if (i0 < i1) {
       int pages[KEY_PAGES];
       look_up(d, si, b0, si.n_blocks, pages);
       load_pages(d, layer, head, pages, s_k, nullptr);
       cp_async_commit();
+      stage(i0);
       cp_async_wait_all();
       // Into pieces: each thread what it brought.
       for (int r = tid >> 4; r < KEYS; r += THREADS / 16) {
@@ -490,24 +502,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) weights_sums_f32_kernel(Dev d, 
     }
     float sum[2] = {0.f, 0.f}, rest[2] = {0.f, 0.f};  // (rest: what additions to the sums rounded off)
     for (int i = i0; i < i1; ++i) {
-      float* tile = s_q + (i & 1) * TILE;
-      stage_rows<KT>(d, si, head, i * STEP_TOKENS, q, scale, tile, 0);
-      if (tid < KT) {  // rows past the chunk draw nothing
-        const int tok = i * STEP_TOKENS + tid / G;
-        float m = INFINITY, l = 1.f;
-        if (tok < si.t) {
-          const float2* row = work.stats + (size_t)(si.q_row0 + tok) * d.q_heads + head * G + tid % G;
-          m = row->x;
-          l = row->y;
-          for (int p = 1; p < parts; ++p) {
-            const float2 o = row[(size_t)p * total * d.q_heads];
-            const float mn = fmaxf(m, o.x);
-            l = l * exp2_safe(m, mn) + o.y * exp2_safe(o.x, mn);
-            m = mn;
-          }
-        }
-        s_lse[i & 1][tid] = m + log2f(l);
-      }
+      const float* tile = s_q + (i & 1) * TILE;
+      if (i > i0) stage(i);
       __syncthreads();
       float s[NT][4], add[2] = {0.f, 0.f};
       products(s_k, KEYS * D, 16 * warp, tile, lane, s);

@@ -18,30 +18,47 @@ namespace {
 constexpr int THREADS = 256;
 
 // The planes' sums of each resident position, added to what it weighs: blockIdx.y is the session of the
-// call.
+// call.  SPLIT threads have every SPLIT-th plane of a position, so that few loads follow one another (one
+// thread took 22 us for 64 planes of 4,000 positions); their sums are joined in order.
+constexpr int SPLIT = 4, POSITIONS = THREADS / SPLIT;
+
 __global__ void __launch_bounds__(THREADS) weights_add_kernel(Dev d, int planes, WeightsWork work,
                                                               float* weights) {
+  __shared__ float s_sum[SPLIT][POSITIONS];
+  const int x = threadIdx.x % POSITIONS, part = threadIdx.x / POSITIONS;
   pdl_wait();
   pdl_launch_dependents();
   if (d.g->n_units == 0) return;
   const SeqInfo si = d.seq[blockIdx.y];
   const size_t plane = (size_t)d.n_pages * PS;
-  for (int at = blockIdx.x * THREADS + threadIdx.x; at < si.n_blocks * PS; at += gridDim.x * THREADS) {
-    const BlockRange br = block_range(si, at / PS);
-    if (at % PS < br.lo || at % PS >= br.hi) continue;
-    const int page = block_page(si, d.hist_pt + (size_t)si.sid * d.max_pages_per_session,
-                                d.live_pt + (size_t)si.sid * d.max_pages_per_session, at / PS);
-    const int gs = page * PS + at % PS;
+  for (int at0 = blockIdx.x * POSITIONS; at0 < si.n_blocks * PS; at0 += gridDim.x * POSITIONS) {
+    const int at = at0 + x, blk = at / PS, slot = at % PS;
+    const BlockRange br = blk < si.n_blocks ? block_range(si, blk) : BlockRange{0, 0, 0};
+    const bool in = slot >= br.lo && slot < br.hi;
     float w = 0.f;
+    int gs = 0;
+    float* to = nullptr;
+    if (in) {
+      gs = block_page(si, d.hist_pt + (size_t)si.sid * d.max_pages_per_session,
+                      d.live_pt + (size_t)si.sid * d.max_pages_per_session, blk) * PS + slot;
+      if (part == 0) to = weights + (size_t)si.sid * d.max_positions + d.meta_pos[gs];
 #pragma unroll 16
-    for (int h = 0; h < planes; ++h) w += work.scores[h * plane + gs];
-    weights[(size_t)si.sid * d.max_positions + d.meta_pos[gs]] += w;
+      for (int h = part; h < planes; h += SPLIT) w += work.scores[h * plane + gs];
+    }
+    s_sum[part][x] = w;
+    __syncthreads();
+    if (to) {
+#pragma unroll
+      for (int p = 1; p < SPLIT; ++p) w += s_sum[p][x];
+      *to += w;
+    }
+    __syncthreads();
   }
 }
 
 cudaError_t launch_add(const Dev& d, const Limits& lim, int planes, const WeightsWork& work, float* weights,
                        int n_seq, cudaStream_t s, int64_t* launches) {
-  const dim3 grid(std::max(1, std::min(64, 8 * lim.sms / n_seq)), n_seq);
+  const dim3 grid(std::max(1, std::min(256, 8 * lim.sms / n_seq)), n_seq);
   const cudaError_t e = launch_ex(&weights_add_kernel, grid, dim3(THREADS), 0, s, true, d, planes, work,
                                   weights);
   *launches += e == cudaSuccess;
@@ -56,7 +73,7 @@ size_t lay_out(uint8_t* base, int64_t n_pages, int q_heads, int max_tokens, int 
     off += (bytes + 255) / 256 * 256;
     return p;
   };
-  uint8_t* scores = take((size_t)n_pages * PS * q_heads * sizeof(float));
+  uint8_t* scores = take((size_t)n_pages * PS * q_heads * 2 * sizeof(float));
   uint8_t* stats = take(((size_t)max_tokens * q_heads + WEIGHTS_STATS) * sizeof(float2));
   uint8_t* whole = take((size_t)max_seq * q_heads * sizeof(float2));
   uint8_t* parts = take((size_t)WEIGHTS_PARTS * 4 * sizeof(float2));
@@ -90,8 +107,8 @@ cudaError_t launch_attn_weights(const Dev& d, const Limits& lim, int layer, cons
   order->launched(layer, false);
   if (max_t == 1) return launch_weights_token(d, lim, layer, q, weights, w, n_seq, early, s, launches);
   // Where the chunk's rows alone are too few items (64 tokens of a KV head, or 32), the keys are cut into
-  // parts; where the keys are (256, or 128), the tokens into shares.
-  const int64_t tokens = d.esz == 2 ? 64 : 32, pages = d.esz == 2 ? 16 : 8, ctas = lim.sms;
+  // parts; where the keys are (512, or 128), the tokens into shares.
+  const int64_t tokens = d.esz == 2 ? 64 : 32, pages = d.esz == 2 ? 32 : 8, ctas = lim.sms;
   const int64_t rows = ((int64_t)total + (tokens - 1) * n_seq) / tokens * d.kv_heads;
   const int64_t stats = (int64_t)d.max_tokens * d.q_heads + WEIGHTS_STATS;
   int64_t parts = std::max<int64_t>(1, std::min<int64_t>(2 * ctas / rows, (pages_max + 7) / 8));

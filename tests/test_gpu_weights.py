@@ -58,6 +58,21 @@ def test_weights_of_chunks(dtype, heads, lens):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens, history", [([1100, 600], 0), ([1057, 1, 300], 520), ([2113], 33)])
+def test_weights_of_chunks_in_shares(dtype, lens, history):
+    """Chunks whose tokens are shared out: shares that see some tiles of an item's keys alone, or none."""
+    from tests import prompt_reference as R
+    rng = np.random.default_rng(lens[0])
+    n = len(lens)
+    cache = R.make_cache(n, dtype=dtype, heads=2, pages=300, positions=2304)
+    work = cache.make_weights_workspace()
+    if history:
+        R.feed(cache, list(range(n)), [history] * n, rng)
+    R.feed(cache, list(range(n)), lens, rng)
+    check(cache, list(range(n)), lens, rng, work)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("lens", [[1, 1], [9, 31], [70, 5]])
 def test_weights_over_evicted_sessions(dtype, lens):
     from tests import prompt_reference as R
