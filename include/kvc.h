@@ -56,7 +56,8 @@ enum { KVC_F32 = 0, KVC_BF16 = 1 };
  * at the finest, 9344 at most, and codes c = x / s rounded to an integer of -7 .. 7 (ties to even).
  * It stands for s * c: elements beyond 65408 are held as 65408, groups below 3.5 * 2^-20 as 0.  A
  * group that holds an infinity or a NaN stands for NaN.
- * Every call takes such a context but kvc_attn_decode_noalloc, which returns KVC_EINVAL.  Attention
+ * Every call takes such a context but kvc_attn_decode_noalloc, kvc_attn_weights and, for chunks of
+ * more than 32 tokens, kvc_attn_prompt, which return KVC_EINVAL.  Attention
  * runs over the numbers that the codes stand for, in binary32 with exact K and V operands.  For the
  * tensor cores q is scaled by a power of two: for bfloat16 P, and in chunks of several tokens q, are
  * rounded to binary16 (single tokens keep q in two such pieces), for binary32 both are split into
@@ -291,8 +292,9 @@ int kvc_attn_decode_noalloc(kvc_ctx* ctx, int layer, const void* d_q, void* d_ou
 /* GQA attention of one layer for the queries of the last append, chunks of any length (a system
  * prompt, a document, a session fed back from its tokens): query t of a session sees every resident
  * key at or before its own position.  Calls of single tokens, and of chunks of at most 32, are
- * kvc_attn_decode and kvc_attn_prefill_chunk.  Longer bfloat16 chunks run on tensor cores with q and P
- * rounded to bfloat16, binary32 accumulation and softmax; binary32 ones stay in binary32 on CUDA cores.
+ * kvc_attn_decode and kvc_attn_prefill_chunk.  Longer bfloat16 chunks run with q and P rounded to
+ * bfloat16, binary32 accumulation and softmax; binary32 ones with products of operands in two TF32
+ * pieces (off by less than 2^-21 of a product), accumulation and softmax in binary32.
  *   d_q, d_out  device [total][Hq][D], as for kvc_attn_prefill_chunk
  * KVC_EINVAL with KVC_KV4 for chunks of more than 32 tokens. */
 int kvc_attn_prompt(kvc_ctx* ctx, int layer, const void* d_q, void* d_out, void* stream);

@@ -20,9 +20,9 @@ SOURCES = ["kvc_api.cu", "kvc_meta.cu", "kvc_attn_decode.cu", "kvc_attn_decode_s
            "kvc_decode_dispatch.cu",
            "kvc_attn_prefill.cu", "kvc_attn_prefill_tc.cu", "kvc_attn_prefill_f32.cu",
            "kvc_noalloc.cu", "kvc_kv4_rows.cu", "kvc_kv4_attn.cu", "kvc_kv4_prefill_f32.cu",
-           "kvc_kv4_decode.cu", "kvc_kv4_prefill_tc.cu", "kvc_prompt.cu", "kvc_prompt_tc.cu", "kvc_prompt_f32.cu", "kvc_weights.cu",
-           "kvc_weights_token.cu", "kvc_weights_tc.cu",
-           "kvc_evict_weighted.cu"]
+           "kvc_kv4_decode.cu", "kvc_kv4_prefill_tc.cu",
+           "kvc_prompt.cu", "kvc_prompt_tc.cu", "kvc_prompt_f32.cu",
+           "kvc_weights.cu", "kvc_weights_tc.cu", "kvc_weights_token.cu", "kvc_evict_weighted.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

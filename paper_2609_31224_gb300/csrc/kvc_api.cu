@@ -196,6 +196,7 @@ struct kvc_ctx {
   // Last append (queries of the following attention calls).
   bool attn_valid = false;
   int last_n_seq = 0, last_total = 0, last_max_t = 0;
+  int last_tiles = 0;      // items of attention over its long chunks, for each KV head
   // Estimates of its sessions' resident pages (largest, sum), for the choice of the attention's
   // split only.
   int est_pages_max = 0;
@@ -442,12 +443,13 @@ int kvc_append_chunk(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, const i
     return fail(KVC_EINVAL, "d_k / d_v must be 16-byte aligned");
   if (h_cu_tokens[0] != 0) return fail(KVC_EINVAL, "h_cu_tokens[0] must be 0");
   int64_t need = 0;
-  int max_t = 0;
+  int max_t = 0, tiles = 0;
   bool single = true;
   for (int i = 0; i < n_seq; ++i) {
     const int t = h_cu_tokens[i + 1] - h_cu_tokens[i];
     if (t < 1) return fail(KVC_EINVAL, "session %d gets %d tokens (must be >= 1)", h_sessions[i], t);
     max_t = std::max(max_t, t);
+    tiles += (t + prompt_tokens(ctx->d) - 1) / prompt_tokens(ctx->d);
     single = single && t == 1;
     const int sid = h_sessions[i];
     if ((int64_t)ctx->pos_next[sid] + t > ctx->cfg.max_positions)
@@ -495,6 +497,7 @@ int kvc_append_chunk(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, const i
   ctx->last_n_seq = n_seq;
   ctx->last_total = total;
   ctx->last_max_t = max_t;
+  ctx->last_tiles = tiles;
   ctx->last_single = single;
   return KVC_OK;
 }
@@ -732,8 +735,9 @@ int kvc_attn_prompt(kvc_ctx* ctx, int layer, const void* d_q, void* d_out, void*
   if (ctx->kv4)
     return fail(KVC_EINVAL, "chunks of more than %d tokens over rows held in 4 bits (KVC_KV4)",
                 PF_MAX_TOKENS);
-  KVC_CUDA(launch_attn_prompt(ctx->d, ctx->lim, layer, d_q, d_out, &ctx->order,
-                              static_cast<cudaStream_t>(stream), &ctx->launches));
+  // (While capturing, too, the pages of now: the split, and with it the last bits, stay those of a call.)
+  KVC_CUDA(launch_attn_prompt(ctx->d, ctx->lim, layer, d_q, d_out, ctx->last_tiles, page_hint(ctx, false).max,
+                              &ctx->order, static_cast<cudaStream_t>(stream), &ctx->launches));
   return KVC_OK;
 }
 

@@ -15,6 +15,11 @@
 //                        one to go by four 8-bit radix passes; the last CTA allocates
 //   weigh_apply_kernel   a CTA per session: moves, tags, page lists, state, mask
 //   weigh_copy_kernel    a CTA per session and (layer, K or V, head): the rows, ascending
+//
+// Bound by the rows that move, each read and written once.  4,099 positions of 32 layers thinned out to
+// 2,048: select 13-19 us, apply 9-13, copy 92 (537 MB, 5.8 TB/s); 16 sessions of 16 layers to 700 each:
+// copy 235 us.  Select and apply are one CTA's latencies a session: radix passes of 8 bits over keys in
+// shared memory (four passes; a sort would move the positions too, which need not be in order).
 #include <climits>
 #include <type_traits>
 

@@ -208,18 +208,21 @@ bool pool_tensor_maps(const Dev& d, CUtensorMap* lo, CUtensorMap* hi);
 // A 4-D view whose boxes are the 4 KiB of a (page, layer, K or V, head) in one copy: 8-row groups of 1 KiB,
 // 128-byte swizzle, columns 0-63 and 64-127 of a group side by side.  Coordinates (0, 0, 0, row / 8).
 bool pool_tile_map(const Dev& d, CUtensorMap* tiles);
-// Whole prompts (kvc_prompt.cu): chunks of any length, rows in the element type.
-cudaError_t launch_attn_prompt(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
-                               LaunchOrder* order, cudaStream_t s, int64_t* launches);
-// Attention weights of the last append's queries, added to weights (kvc_weights.cu).  work: bytes as
-// weights_work_bytes says.
-size_t weights_work_bytes(const kvc_config& c);
+// Whole prompts (kvc_prompt.cu): chunks of any length, rows in the element type.  pages_max: an estimate of
+// the longest session's pages, for the split alone.  tiles: of prompt_tokens tokens, all sessions'.
+inline int prompt_tokens(const Dev& d) { return d.esz == 2 ? 64 : 32; }
+cudaError_t launch_attn_prompt(const Dev& d, const Limits& lim, int layer, const void* q, void* out, int tiles,
+                               int pages_max, LaunchOrder* order, cudaStream_t s, int64_t* launches);
 // Attributes of the kernels of both, in the current CUDA context.
 cudaError_t prompt_attributes(const Dev& d);
 cudaError_t weights_attributes(const Dev& d);
+// Attention weights of the last append's queries, added to weights (kvc_weights.cu).  work: bytes as
+// weights_work_bytes says.  pages_max, pages_sum: estimates of the sessions' pages, for the split alone.
+size_t weights_work_bytes(const kvc_config& c);
 cudaError_t launch_attn_weights(const Dev& d, const Limits& lim, int layer, const void* q,
                                 float* weights, void* work, int n_seq, int total, int max_t,
-                                int pages_max, int64_t pages_sum, LaunchOrder* order, cudaStream_t s, int64_t* launches);
+                                int pages_max, int64_t pages_sum, LaunchOrder* order, cudaStream_t s,
+                                int64_t* launches);
 int noalloc_max_pairs();
 cudaError_t launch_attn_decode_noalloc(const Dev& d, int layer, const void* q, void* out,
                                        int n_seq, cudaStream_t s);

@@ -9,18 +9,26 @@
 // Three products for one: a third of the TF32 rate of mma.sync (300 TFLOP/s measured), 100 against the
 // 76 TFLOP/s of the FMA pipes, which a kernel on them reaches a quarter to a half of.
 //
-// A tile is rows of 64 floats in shared memory.  A warp has 16 rows as the A operand, whose pieces lie in
-// shared memory, and meets a tile of 64 rows as B, which it takes apart itself.  Dims are taken in an order that makes every fragment a 16-byte load: dims
-// 16 c + 4 t .. + 3 of a row are lane t's for the steps 2c (first two) and 2c + 1 of the products; of P V
-// the keys 8 s + 2 t, + 1 are lane t's for step s, as the scores' fragments hold them, and output dims
-// 32 h + 4 g .. + 3 are column g of four products.
+// A tile is rows of 64 floats in shared memory.  A warp has 16 rows as the A operand, whose pieces lie
+// in shared memory, and meets a tile of 64 rows as B, which it takes apart itself.  Dims are taken in an
+// order that makes every fragment a 16-byte load: dims 16 c + 4 t .. + 3 of a row are lane t's for the
+// steps 2c (first two) and 2c + 1 of the products; of P V the keys 8 s + 2 t, + 1 are lane t's for step
+// s, as the scores' fragments hold them, and output dims 32 h + 4 g .. + 3 are column g of four products.
+//
+// Measured: three prompts of up to 1,501 tokens, 4 KV heads, 198 us a layer (531 on the FMA pipes); bound
+// by the products and the operands' taking apart (16 rows a warp leave each B row's pieces to be formed by
+// eight warps), and by items: 32 tokens of a KV head, last ones first, on 152 SMs.  Weights of three units
+// of 17 tokens behind 1,100 positions 29.5 us a layer (102 on the FMA pipes), which is three launches and
+// their chains of latencies; one after the other instead of together, the nine parts of a row's statistics
+// were 3 us of it.
 //
 // Tiles with a number that is not finite (in a slot that holds nothing as well) go a slow way in plain
 // binary32 arithmetic, where a key that a row does not see takes no part.
+#include <algorithm>
 #include <cmath>
 
 #include "kvc_prompt.h"
-#include "kvc_prompt_list.cuh"
+#include "kvc_prompt_merge.cuh"
 #include "kvc_rope.cuh"
 #include "kvc_weights.h"
 
@@ -236,6 +244,7 @@ __device__ inline bool odd_pages(int n_pg, const float* k, const float* v) {
 // An item, as every thread has it.
 struct Item {
   int seq, in;  // session of the call, and which of its items; seq < 0: no more
+  int at;       // of all
 };
 template <typename CountFn>
 __device__ inline Item next_item(const Dev& d, int n_seq, const int* s_group, Item* s_item, CountFn count) {
@@ -245,7 +254,7 @@ __device__ inline Item next_item(const Dev& d, int n_seq, const int* s_group, It
     if (threadIdx.x == 0) at = take_item(d);
     at = __shfl_sync(FULL, at, 0);
     const int seq = at < s_group[GROUPS] ? find_item(n_seq, threadIdx.x, s_group, at, count, &in) : -1;
-    if (threadIdx.x == 0) *s_item = {seq, in};
+    if (threadIdx.x == 0) *s_item = {seq, in, at};
   }
   __syncthreads();
   return *s_item;
@@ -276,8 +285,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) prompt_f32_kernel(Dev d, int la
     const Item it = next_item(d, n_seq, s_group, &s_item, items_of);
     if (it.seq < 0) break;
     const SeqInfo si = d.seq[it.seq];
-    const int head = it.in % H, part = it.in / H % parts;
-    const int t0 = ((si.t + TOKENS - 1) / TOKENS - 1 - it.in / H / parts) * TOKENS;
+    const int part = it.in % parts, head = it.in / parts % H;
+    const int t0 = ((si.t + TOKENS - 1) / TOKENS - 1 - it.in / parts / H) * TOKENS;
     const int nb = blocks_seen(si, min(t0 + TOKENS, si.t) - 1), all = (nb + PAGES - 1) / PAGES;
     const int j0 = (int)((int64_t)all * part / parts), j1 = (int)((int64_t)all * (part + 1) / parts);
     int pages[PAGES];  // of the next tile to load
@@ -419,6 +428,18 @@ __global__ void __launch_bounds__(THREADS, CTAS) prompt_f32_kernel(Dev d, int la
       if constexpr (STATS) {
         if (t == 0) stats[(size_t)part * d.g->total_tokens * d.q_heads + row] = make_float2(m[h], l[h]);
       } else {
+        if (parts > 1) {
+          const int r = 16 * warp + g + 8 * h;
+          float4* to = part_rows<D>(d, it.at) + r;
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              to[(2 * t + 8 * c + e) * PART_ROWS] = make_float4(o[4 * c][2 * h + e], o[4 * c + 1][2 * h + e],
+                                                                o[4 * c + 2][2 * h + e], o[4 * c + 3][2 * h + e]);
+          if (t == 0) part_sums<D>(d, it.at)[r] = make_float2(m[h], l[h]);
+          continue;
+        }
         const float inv = 1.f / l[h];
         float4* to = reinterpret_cast<float4*>(out + row * D + 8 * t);
 #pragma unroll
@@ -535,6 +556,10 @@ __global__ void __launch_bounds__(THREADS, CTAS) weights_sums_f32_kernel(Dev d, 
   if (tid == 0) leave_counters(d);
 }
 
+__global__ void __launch_bounds__(MERGE_THREADS) prompt_merge_f32_kernel(Dev d, float* out, int parts) {
+  merge_parts<float, D, 1>(d, out, parts, [](const SeqInfo&, int, int) { return false; });
+}
+
 template <typename K>
 cudaError_t most_smem(K* kernel, int bytes) {
   return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
@@ -550,11 +575,17 @@ cudaError_t prompt_f32_attributes() {
   return e != cudaSuccess ? e : most_smem(weights_sums_f32_kernel, SUMS_SMEM);
 }
 
-cudaError_t launch_prompt_f32(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
-                              cudaStream_t s) {
-  return launch_ex(&prompt_f32_kernel<false>, dim3(lim.sms * CTAS), dim3(THREADS), PROMPT_SMEM, s, true, d, layer,
-                   static_cast<const float*>(q), static_cast<float*>(out), score_scale(), 1,
-                   static_cast<float2*>(nullptr));
+cudaError_t launch_prompt_f32(const Dev& d, const Limits& lim, int layer, const void* q, void* out, int parts,
+                              int64_t items, cudaStream_t s, int64_t* launches) {
+  float* to = static_cast<float*>(out);
+  cudaError_t e = launch_ex(&prompt_f32_kernel<false>, dim3(lim.sms * CTAS), dim3(THREADS), PROMPT_SMEM, s, true,
+                            d, layer, static_cast<const float*>(q), to, score_scale(), parts,
+                            static_cast<float2*>(nullptr));
+  *launches += e == cudaSuccess;
+  if (e != cudaSuccess || parts == 1) return e;
+  e = launch_ex(&prompt_merge_f32_kernel, dim3(merge_grid(items, D)), dim3(MERGE_THREADS), 0, s, true, d, to, parts);
+  *launches += e == cudaSuccess;
+  return e;
 }
 
 cudaError_t launch_weights_f32(const Dev& d, const Limits& lim, int layer, const void* q,

@@ -6,9 +6,21 @@
 // pages) a step.  Items go to the CTAs (one per SM) from a counter, a session's last tokens, which see
 // most, first.  A step has four products of 128^3: S_A, S_B (Q K^T) and O_A, O_B += P V; while the
 // softmax of one tile runs, the tensor cores have the other tile's.
+//
+// Work and bound: 4 D flops a query row and key, 2.2 TFLOP for one prompt of 16,384 tokens and 8 KV
+// heads; 1,811 us, 1,210 TFLOP/s, 64 % of what the tensor cores were measured to do in a library
+// product.  Products and copies alone, without a softmax to wait for, take 1,294 us at one CTA's N = 128.
+// Beyond them a step is bound by the softmax, about 550 cycles for 32 keys of two rows' warps on a
+// scheduler, whose warps are short of instructions as often as they issue one.  K and V are read once per
+// item, 745 us of copies that run beside.  Also: 4,099 tokens 147 us a layer (938 TFLOP/s), eight
+// prompts of up to 2,500 tokens 183 us, four of up to 700 behind 4,096 positions 171 us, one of 250
+// tokens 14.0 us, which is latency: a launch, an item's set-up, two steps one after the other.
+// Measured and not taken: P of the second half in shared memory with scores of 128 keys a product (a
+// third fewer products; 16,384 tokens 1,826 us, 4,099 155 us), one product for both halves' scores
+// (1,970 us), 16 warps of softmax, two a row (1,970 us).
 // Warp roles (512 threads):
 //   warp 0      items from the counter; K and V by TMA, a page's 4 KiB of a head a copy (twice as many of
-//               2 KiB took 2,600 cycles a step for 1,900), into a ring of five 32 KiB stages in turn
+//               2 KiB took 2,600 cycles a step for 1,900), into a ring of four 32 KiB stages in turn
 //   warps 1, 2  one thread each issues the products of a tile
 //   warp 3      V rows that have to be zero (below)
 //   warps 4-7   query rows, rotated, scaled and rounded, into three tiles of shared memory: an item's
@@ -25,14 +37,16 @@
 // A key that no row of a product may see has P = 0, but 0 times a value that is not finite is not 0.  So
 // the V rows of slots that hold no resident position are zeroed in shared memory, and those of the
 // chunk's own tokens that some rows of the item see and others do not, where they are not finite: the
-// rows that do see such a one add it by themselves at the end (add_odd_values).
+// rows that do see such a one add it by themselves at the end (odd_value).
 //
 // All waits are bounded; a timeout records KVC_DERR_WAIT and the CTA stops.
 #include <cuda.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "kvc_prompt.h"
+#include "kvc_prompt_merge.cuh"
 #include "kvc_prompt_tc.cuh"
 
 namespace kvc {
@@ -74,7 +88,9 @@ struct Item {
   SeqInfo si;
   int32_t head, t0, steps;       // steps = 0: no more items
   int32_t odd;                   // some V row was zeroed because it is not finite
-  int32_t pad[12];
+  int32_t first;                 // step that it starts with
+  int32_t slot;                  // of its first tile's part, -1: the item has all keys
+  int32_t pad[10];
 };
 static_assert(sizeof(Item) == 128, "Item size");
 
@@ -92,6 +108,13 @@ static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of a CTA");
 __device__ inline int page_of(const Dev& d, int sid, int nhp, int b) {
   const size_t row = (size_t)sid * d.max_pages_per_session;
   return b < nhp ? d.hist_pt[row + b] : d.live_pt[row + b - nhp];
+}
+
+// Steps [*j0, *j1) of a part of an item's keys, of `all`.  Each part but an empty one starts with keys that
+// all rows of the item see (its first token, on which the rest of the rows follow, is in step `diag`).
+__device__ inline void part_steps(int all, int diag, int part, int parts, int* j0, int* j1) {
+  *j0 = min(all * part / parts, diag);
+  *j1 = part == parts - 1 ? all : min(all * (part + 1) / parts, diag);
 }
 
 __device__ inline bool not_finite(uint32_t two) {
@@ -132,7 +155,7 @@ __device__ __noinline__ void odd_value(const Dev& d, const SeqInfo& si, int laye
 __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
     Dev d, int layer, const __grid_constant__ CUtensorMap map,
     const __nv_bfloat16* __restrict__ q,
-    __nv_bfloat16* __restrict__ out, float qk_scale) {
+    __nv_bfloat16* __restrict__ out, float qk_scale, int parts) {
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + OFF_BARS);
   Item* items = reinterpret_cast<Item*>(smem + OFF_ITEM);
@@ -159,8 +182,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
     fence_mbar_init();
     *stop = 0;
   }
-  // Items of a session: 64-token tiles of its chunk, for each KV head.
-  auto items_of = [&](int i) { return (d.seq[i].t + 2 * TOKENS - 1) / (2 * TOKENS) * H; };
+  // Items of a session: 64-token tiles of its chunk, for each KV head, and parts of their keys.
+  auto items_of = [&](int i) { return (d.seq[i].t + 2 * TOKENS - 1) / (2 * TOKENS) * H * parts; };
   if (warp == 3) list_items(n_seq, lane, s_group, items_of);
   __syncwarp();
   if (warp == 1) tmem_alloc(tmem_slot, ALL_COLS);
@@ -181,27 +204,33 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
       };
       // The next item, taken from the counter and looked up while the stages of the one before are on
       // their way.  (word: lane i has word i of its session's info.)
-      int word, sid, nhp, head, t0, nb, steps, pid, pid_next;
+      int word, sid, nhp, head, t0, nb, first, slot, steps, pid, pid_next;
       EdgeSteps edge;
       auto fetch = [&] {
-        int at = 0, in;
-        if (lane == 0) at = take_item(d);
-        at = __shfl_sync(FULL, at, 0);
-        steps = 0;
-        if (at >= total) return;
-        const int seq = find_item(n_seq, lane, s_group, at, items_of, &in);
-        word = lane < 16 ? reinterpret_cast<const int*>(d.seq + seq)[lane] : 0;
-        const SeqInfo& si = d.seq[seq];
-        sid = si.sid;
-        nhp = si.n_hist_pages;
-        head = in % H;
-        t0 = ((si.t + 2 * TOKENS - 1) / (2 * TOKENS) - 1 - in / H) * 2 * TOKENS;
-        nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1);
-        steps = (nb + PAGES - 1) / PAGES;
-        edge = edge_steps(si, t0);
+        for (steps = 0; steps == 0;) {
+          int at = 0, in;
+          if (lane == 0) at = take_item(d);
+          at = __shfl_sync(FULL, at, 0);
+          if (at >= total) return;
+          const int seq = find_item(n_seq, lane, s_group, at, items_of, &in);
+          word = lane < 16 ? reinterpret_cast<const int*>(d.seq + seq)[lane] : 0;
+          const SeqInfo& si = d.seq[seq];
+          const int part = in % parts;
+          in /= parts;
+          sid = si.sid;
+          nhp = si.n_hist_pages;
+          head = in % H;
+          t0 = ((si.t + 2 * TOKENS - 1) / (2 * TOKENS) - 1 - in / H) * 2 * TOKENS;
+          nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1);
+          edge = edge_steps(si, t0);
+          part_steps((nb + PAGES - 1) / PAGES, edge.diag, part, parts, &first, &steps);
+          steps -= first;
+          edge.from(first);
+          slot = parts > 1 ? 2 * at : -1;
+        }
         auto page_at = [&](int b) { return b < nb ? page_of(d, sid, nhp, b) : 0; };
-        pid = page_at(lane);
-        pid_next = page_at(32 + lane);
+        pid = page_at(PAGES * first + lane);
+        pid_next = page_at(PAGES * first + 32 + lane);
       };
       auto publish = [&](int n) {
         Item* it = items + (n & 1);
@@ -211,6 +240,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
           it->t0 = t0;
           it->steps = steps;
           it->odd = 0;
+          it->first = first;
+          it->slot = slot;
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars[B_ITEM + (n & 1)]);
@@ -218,7 +249,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
       fetch();
       publish(0);
       for (int n = 0; ok && steps > 0; ++n) {
-        const int c_sid = sid, c_nhp = nhp, c_head = head, c_nb = nb, c_steps = steps;
+        const int c_sid = sid, c_nhp = nhp, c_head = head, c_nb = nb, c_steps = steps, c_first = first;
         const EdgeSteps c_edge = edge;
         int c_pid = pid, c_pid_next = pid_next;
         const int next_bar = B_ITEM_EMPTY + ((n + 1) & 1);
@@ -227,11 +258,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
         for (int j = 0; j < c_steps && ok; ++j) {
           if (j > 0 && (j & 3) == 0) {
             c_pid = c_pid_next;
-            const int b = PAGES * j + 32 + lane;
+            const int b = PAGES * (c_first + j) + 32 + lane;
             c_pid_next = b < c_nb ? page_of(d, c_sid, c_nhp, b) : 0;
           }
           const int page = __shfl_sync(FULL, c_pid, PAGES * (j & 3) + (lane & 7));
-          const int n_pg = min(PAGES, c_nb - PAGES * j);
+          const int n_pg = min(PAGES, c_nb - PAGES * (c_first + j));
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv, ++seq_no) {
             const int st = seq_no % RING;
@@ -316,7 +347,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
         if (steps > 0) begin(items[0], x < tiles);
         for (int n = 0; ok && steps > 0; ++n) {
           const Item& it = items[n & 1];
-          const EdgeSteps edge = edge_steps(it.si, it.t0);
+          EdgeSteps edge = edge_steps(it.si, it.t0);
+          edge.from(it.first);
           const bool mine = x < tiles;
           q_no += tiles;
           for (int j = 0; j < steps && ok; ++j) {
@@ -382,14 +414,15 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
         const SeqInfo& si = it.si;
         const int t0 = it.t0, steps = it.steps, q_log0 = si.n_hist + si.n_live - si.t;
         const int nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1);
-        const EdgeSteps edge = edge_steps(si, t0);
+        EdgeSteps edge = edge_steps(si, t0);
+        edge.from(it.first);
         for (int j = 0; j < steps && ok; ++j) {
           if (!edge.at(j)) continue;
           uint8_t* tile = s_ring + (stages + 2 * j + 1) % RING * SLOT;
           if (!wait(B_EDGE + edges % EDGES, (edges / EDGES) & 1)) break;
 #pragma unroll 1
           for (int r = lane; r < KEYS; r += 32) {
-            const int b = PAGES * j + r / PS;
+            const int b = PAGES * (it.first + j) + r / PS;
             const uint32_t bit = 1u << (r % PS);
             bool zero = !(slots_seen(si, b, nb, q_log0 + si.t) & bit);
             if (!zero && !(slots_seen(si, b, nb, q_log0 + t0) & bit)) {  // some rows see it
@@ -468,7 +501,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
       if (t0 + x * TOKENS < si.t) {
         const int nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1);
         const int q_log = si.n_hist + si.n_live - si.t + tok;
-        const EdgeSteps edge = edge_steps(si, t0);
+        EdgeSteps edge = edge_steps(si, t0);
+        edge.from(it.first);
         float m = 0.f, l = 0.f;
         for (int j = 0; ok && j < steps; ++j) {
           const bool masks = edge.at(j);
@@ -478,7 +512,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
             if (masks) {
 #pragma unroll
               for (int p = 0; p < CHUNK / PS; ++p) {
-                const uint32_t seen = slots_seen(si, PAGES * j + CHUNK / PS * c + p, nb, q_log);
+                const uint32_t seen = slots_seen(si, PAGES * (it.first + j) + CHUNK / PS * c + p, nb, q_log);
 #pragma unroll
                 for (int i = 0; i < PS; ++i) w[p * PS + i] = (seen >> i & 1) ? w[p * PS + i] : 0xFF800000u;
               }
@@ -570,6 +604,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
         ++o_no;
         tc_fence_after();
         const float inv = 1.f / l;
+        const int slot = it.slot + x;
+        const bool partly = it.slot >= 0;
+        if (partly) part_sums<D>(d, slot)[r] = make_float2(m, l);
         const bool odd = *reinterpret_cast<volatile const int*>(&it.odd) != 0;
         __nv_bfloat16* row = out + ((size_t)(si.q_row0 + tok) * d.q_heads + it.head * G + r % G) * D;
 #pragma unroll 1
@@ -582,7 +619,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
 #pragma unroll
             for (int i = 0; i < 32; ++i) o[i] += more[i];
           }
-          if (tok < si.t) {
+          if (partly) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4)
+              part_rows<D>(d, slot)[(c + i) / 4 * PART_ROWS + r] =
+                  make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+          } else if (tok < si.t) {
 #pragma unroll
             for (int i = 0; i < 32; i += 8)
               *reinterpret_cast<uint4*>(row + c + i) =
@@ -607,6 +649,15 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
   if (tid == 0) leave_counters(d);
 }
 
+__global__ void __launch_bounds__(MERGE_THREADS) prompt_merge_kernel(Dev d, __nv_bfloat16* out, int parts) {
+  merge_parts<__nv_bfloat16, D, 2>(d, out, parts, [&](const SeqInfo& si, int t0, int part) {
+    const int nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1);
+    int j0, j1;
+    part_steps((nb + PAGES - 1) / PAGES, edge_steps(si, t0).diag, part, parts, &j0, &j1);
+    return j0 == j1;
+  });
+}
+
 }  // namespace
 
 cudaError_t prompt_tc_attributes() {
@@ -614,13 +665,19 @@ cudaError_t prompt_tc_attributes() {
                               SMEM_BYTES);
 }
 
-cudaError_t launch_prompt_tc(const Dev& d, const Limits& lim, int layer, const void* q, void* out,
-                             cudaStream_t s) {
+cudaError_t launch_prompt_tc(const Dev& d, const Limits& lim, int layer, const void* q, void* out, int parts,
+                             int64_t items, cudaStream_t s, int64_t* launches) {
   CUtensorMap map;
   if (!pool_tile_map(d, &map)) return cudaErrorInvalidValue;
-  return launch_ex(&prompt_tc_kernel, dim3(lim.sms), dim3(TC_THREADS), SMEM_BYTES, s, true, d,
-                   layer, map, static_cast<const __nv_bfloat16*>(q), static_cast<__nv_bfloat16*>(out),
-                   LOG2E / sqrtf((float)D));
+  __nv_bfloat16* to = static_cast<__nv_bfloat16*>(out);
+  cudaError_t e = launch_ex(&prompt_tc_kernel, dim3(lim.sms), dim3(TC_THREADS), SMEM_BYTES, s, true, d, layer,
+                            map, static_cast<const __nv_bfloat16*>(q), to, LOG2E / sqrtf((float)D), parts);
+  *launches += e == cudaSuccess;
+  if (e != cudaSuccess || parts == 1) return e;
+  e = launch_ex(&prompt_merge_kernel, dim3(merge_grid(2 * items, D)), dim3(MERGE_THREADS), 0, s, true, d, to,
+                parts);
+  *launches += e == cudaSuccess;
+  return e;
 }
 
 }  // namespace kvc

@@ -60,13 +60,6 @@ __device__ inline void tma_load_tile(void* dst, const CUtensorMap* map, int grou
       "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(group), "r"(smem_u32(bar))
       : "memory");
 }
-// To N registers a thread from the launch's BASE (a whole warpgroup).
-template <int BASE, int N>
-__device__ inline void set_registers() {
-  if constexpr (N < BASE) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
-  if constexpr (N > BASE) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
-}
-
 // Bounded wait that also ends when another warp has given up.
 __device__ inline bool wait_or_stop(const Dev& d, uint64_t* bar, uint32_t parity, volatile int* stop) {
   if (mbar_try_wait(bar, parity)) return true;
@@ -87,6 +80,12 @@ __device__ inline bool wait_or_stop(const Dev& d, uint64_t* bar, uint32_t parity
 struct EdgeSteps {
   int diag, hist, live;
   __device__ bool at(int j) const { return j >= diag || j == hist || j == live; }
+  // Counted from a step on (those before it are below 0).
+  __device__ void from(int j) {
+    diag -= j;
+    hist -= j;
+    live -= j;
+  }
 };
 __device__ inline EdgeSteps edge_steps(const SeqInfo& si, int t0) {
   const int nhp = si.n_hist_pages;

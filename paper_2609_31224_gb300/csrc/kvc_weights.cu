@@ -99,7 +99,8 @@ cudaError_t weights_attributes(const Dev& d) {
 
 cudaError_t launch_attn_weights(const Dev& d, const Limits& lim, int layer, const void* q,
                                 float* weights, void* work, int n_seq, int total, int max_t,
-                                int pages_max, int64_t pages_sum, LaunchOrder* order, cudaStream_t s, int64_t* launches) {
+                                int pages_max, int64_t pages_sum, LaunchOrder* order, cudaStream_t s,
+                                int64_t* launches) {
   WeightsWork w;
   lay_out(static_cast<uint8_t*>(work), d.n_pages, d.q_heads, d.max_tokens, d.max_seq, &w);
   // (Each kernel but an early one waits for the one before it before it lets the next one start.)
@@ -107,11 +108,16 @@ cudaError_t launch_attn_weights(const Dev& d, const Limits& lim, int layer, cons
   order->launched(layer, false);
   if (max_t == 1) return launch_weights_token(d, lim, layer, q, weights, w, n_seq, early, s, launches);
   // Where the chunk's rows alone are too few items (64 tokens of a KV head, or 32), the keys are cut into
-  // parts; where the keys are (512, or 128), the tokens into shares.
+  // parts of 32 pages or more (binary32: eight), two items an SM in all.  One session, 4,096 positions, 8 KV
+  // heads (4), us a layer, against one part: a chunk of 8 tokens 51 -> 25 (256 -> 26), of 64 tokens
+  // 70 -> 35 (268 -> 53); with bfloat16 parts of eight pages 29 and 47.
+  // Where the keys are too few items (512, or 128), the tokens are cut into shares of at least four tiles: two
+  // prompts of 3,001 and 940 tokens, 72 items, took 264, 206 and 175 us a layer with 2, 4 and 8 shares.
   const int64_t tokens = d.esz == 2 ? 64 : 32, pages = d.esz == 2 ? 32 : 8, ctas = lim.sms;
   const int64_t rows = ((int64_t)total + (tokens - 1) * n_seq) / tokens * d.kv_heads;
+  const int64_t part = d.esz == 2 ? 32 : 8;
   const int64_t stats = (int64_t)d.max_tokens * d.q_heads + WEIGHTS_STATS;
-  int64_t parts = std::max<int64_t>(1, std::min<int64_t>(2 * ctas / rows, (pages_max + 7) / 8));
+  int64_t parts = std::max<int64_t>(1, std::min<int64_t>(2 * ctas / rows, (pages_max + part - 1) / part));
   parts = std::max<int64_t>(1, std::min(parts, stats / ((int64_t)total * d.q_heads)));
   const int64_t keys = (pages_sum / pages + n_seq) * d.kv_heads;
   int shares = 1;

@@ -67,6 +67,42 @@ def test_prompts_behind_evicted_histories(dtype, lens, before):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads", [1, 4])
+@pytest.mark.parametrize("lens, before, evicts", [
+    ([33], [5000], False), ([64], [4097], True), ([65], [1531], True), ([100, 40], [3000, 17], True),
+    ([40, 33, 70], [900, 2600, 16], False), ([300], [2047], True), ([130, 1], [1, 4000], True)])
+def test_short_chunks_behind_long_histories(dtype, heads, lens, before, evicts):
+    """Too few rows for all SMs: an item's keys are cut into parts, some of them empty."""
+    from tests import prompt_reference as R
+    rng = np.random.default_rng([heads, lens[0], before[0]])
+    n = len(lens)
+    cache = R.make_cache(n, dtype=dtype, heads=heads, budget=max(before) - 300 if evicts else -1, pages=360,
+                         positions=8192, tokens=8192)
+    R.feed(cache, range(n), before, rng)
+    if evicts:
+        cache.evict(list(range(n)))
+        R.feed(cache, range(n), [9] * n, rng)
+        cache.evict(list(range(n)))
+    R.feed(cache, range(n), lens, rng)
+    a = check(cache, range(n), lens, rng, q=(q := R.queries(cache, sum(lens), rng)))
+    assert torch.equal(a, check(cache, range(n), lens, rng, q=q))    # bit for bit
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_values_behind_a_token_in_parts(dtype):
+    """V that is not finite in a chunk's own keys reaches the tokens at and behind it alone."""
+    from tests import prompt_reference as R
+    rng = np.random.default_rng(5)
+    cache = R.make_cache(1, dtype=dtype, heads=2, pages=360, positions=8192)
+    R.feed(cache, [0], [4000], rng)
+    k, v = R.rows(cache, 70, rng), R.rows(cache, 70, rng)
+    v[:, 37] = torch.nan
+    v[:, 69] = torch.inf
+    cache.append_chunk([0], [0, 70], torch.zeros(70, dtype=torch.uint8, device="cuda"), k, v)
+    check(cache, [0], [70], rng)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_a_prompt_of_one_session_among_many(dtype):
     from tests import prompt_reference as R
     rng = np.random.default_rng(2)
