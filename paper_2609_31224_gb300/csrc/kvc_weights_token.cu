@@ -10,8 +10,8 @@
 //             upper and lower bfloat16 piece, whose products are added in binary32: q keeps 16 bits or
 //             more at the price of one
 //   binary32  eight lanes a key, an eighth of the query rows in the registers of each
-// Bound by the keys' bytes for many sessions: 64 sessions of 4,100 positions, 8 KV heads, 100 us a layer
-// for 79 us at the copy bandwidth (5.3 TB/s).  One session, 9.2 us for 1.3, is two launches' latencies:
+// Bound by the keys' bytes for many sessions: 64 sessions of 4,100 positions, 8 KV heads, 96 us a layer
+// for 79 us at the copy bandwidth (5.6 TB/s).  One session, 8.2 us for 1.3, is two launches' latencies:
 // their release, q or the parts, a ring's first tiles, then the scores' way back through L2.
 #include <cmath>
 
@@ -23,8 +23,9 @@ namespace kvc {
 
 namespace {
 
-constexpr int TOKEN_WARPS = 4, TOKEN_THREADS = TOKEN_WARPS * 32;
-constexpr int TOKEN_STAGES = 6;                    // 4 KiB each, a warp
+constexpr int TOKEN_WARPS = 8, TOKEN_THREADS = TOKEN_WARPS * 32;
+constexpr int TOKEN_STAGES = 2;                    // 4 KiB each, a warp (16 warps an SM hide the latency of a unit's
+                                                   // chain: 4 warps of 6 stages took 9.4 and 100 us, see above)
 constexpr int UNIT_BYTES = 4096;                   // the keys of a unit, in either type
 constexpr int TOKEN_SMEM = TOKEN_WARPS * TOKEN_STAGES * UNIT_BYTES + 1024;
 constexpr int TOKEN_MIN_UNITS = 4;                 // of a CTA, at least
