@@ -761,13 +761,10 @@ int kvc_attn_weights(kvc_ctx* ctx, int layer, const void* d_q, float* d_weights,
     return fail(KVC_EINVAL, "d_work must be a 256-byte aligned device pointer");
   const size_t need = weights_work_bytes(ctx->cfg);
   if (work_bytes < need) return fail(KVC_EINVAL, "work_bytes %zu < required %zu", work_bytes, need);
-  const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  bool capturing = false;
-  KVC_CUDA(is_capturing(s, &capturing));
-  const PageHint pages = page_hint(ctx, capturing);
+  const PageHint pages = page_hint(ctx, false);  // (as for kvc_attn_prompt)
   KVC_CUDA(launch_attn_weights(ctx->d, ctx->lim, layer, d_q, d_weights, d_work, ctx->last_n_seq,
-                               ctx->last_total, ctx->last_max_t, pages.max, pages.sum, &ctx->order, s,
-                               &ctx->launches));
+                               ctx->last_total, ctx->last_max_t, pages.max, pages.sum, &ctx->order,
+                               static_cast<cudaStream_t>(stream), &ctx->launches));
   return KVC_OK;
 }
 

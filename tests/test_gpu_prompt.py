@@ -103,6 +103,44 @@ def test_values_behind_a_token_in_parts(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scores_far_apart_in_parts(dtype):
+    """Parts whose scores differ by so much that all but one of them weigh nothing, and the other way round."""
+    from tests import prompt_reference as R
+    rng = np.random.default_rng(9)
+    cache = R.make_cache(1, dtype=dtype, layers=1, heads=1, pages=200, positions=4096)
+    t = 3000
+    k, v = R.rows(cache, t, rng), R.rows(cache, t, rng)
+    size = torch.ones(t, device="cuda")
+    size[:900], size[2000:2600] = 0.0, 20.0
+    k = (k.float() * size[None, :, None, None]).to(k.dtype)
+    cache.append_chunk([0], [0, t], torch.zeros(t, dtype=torch.uint8, device="cuda"), k, v)
+    R.feed(cache, [0], [50], rng)
+    q = R.queries(cache, 50, rng)
+    if dtype == "bf16":
+        q = (q.float() / 10).to(q.dtype)
+    out = torch.zeros_like(q)
+    cache.attn_prompt(0, q[0], out[0])
+    hk, hv = R.held(cache, 0)
+    want = R.attention(cache, 0, q[0], hk[0], hv[0])[0]
+    d = (out[0].double() - want).norm() / want.norm()
+    # scores of size up to 2 * 5 (bfloat16) or 20 * 5 (binary32): errors grow with them
+    assert d < (10 * 3e-3 if dtype == "bf16" else 100 * 1e-6)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_sessions_of_long_chunks(dtype):
+    from tests import prompt_reference as R
+    rng = np.random.default_rng(4)
+    n = 130
+    cache = R.make_cache(n, dtype=dtype, layers=1, heads=1, pages=16, tokens=16384)
+    lens = [int(x) for x in rng.integers(1, 80, size=n)]
+    R.feed(cache, range(n), [int(x) for x in rng.integers(1, 100, size=n)], rng)
+    order = [int(x) for x in rng.permutation(n)]
+    R.feed(cache, order, lens, rng)
+    check(cache, order, lens, rng)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_a_prompt_of_one_session_among_many(dtype):
     from tests import prompt_reference as R
     rng = np.random.default_rng(2)

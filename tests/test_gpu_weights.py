@@ -153,3 +153,55 @@ def test_captured_and_replayed():
         graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(w, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens, before", [([5], [4500]), ([64], [4095]), ([2, 33], [40, 3001])])
+def test_weights_of_short_chunks_behind_long_histories(dtype, lens, before):
+    """Row statistics in parts of the keys, more of them than are read at once."""
+    from tests import prompt_reference as R
+    rng = np.random.default_rng(lens[0])
+    n = len(lens)
+    cache = R.make_cache(n, dtype=dtype, heads=1, pages=300, positions=4608, tokens=8192)
+    work = cache.make_weights_workspace()
+    R.feed(cache, list(range(n)), before, rng)
+    R.feed(cache, list(range(n)), lens, rng)
+    check(cache, list(range(n)), lens, rng, work)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("most", [1, 40])
+def test_weights_of_many_sessions(dtype, most):
+    from tests import prompt_reference as R
+    rng = np.random.default_rng(most)
+    n = 150
+    cache = R.make_cache(n, dtype=dtype, layers=1, heads=1, pages=12, tokens=8192)
+    work = cache.make_weights_workspace()
+    lens = [int(x) for x in rng.integers(1, most + 1, size=n)]
+    R.feed(cache, list(range(n)), [int(x) for x in rng.integers(1, 100, size=n)], rng)
+    order = [int(x) for x in rng.permutation(n)]
+    R.feed(cache, order, lens, rng)
+    check(cache, order, lens, rng, work)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_chunk_captured_and_replayed(dtype):
+    """With a scratch of its own, while an eager call uses another: the same bits."""
+    from tests import prompt_reference as R
+    rng = np.random.default_rng(3)
+    cache = R.make_cache(2, dtype=dtype, pages=120)
+    R.feed(cache, [0, 1], [1200, 30], rng)
+    R.feed(cache, [0, 1], [40, 9], rng)
+    q = R.queries(cache, 49, rng)
+    want, w = cache.make_weights(), cache.make_weights()
+    cache.attn_weights(1, q[1], want, cache.make_weights_workspace())
+    work = cache.make_weights_workspace()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        cache.attn_weights(1, q[1], w, work)
+    for _ in range(2):
+        w.zero_()
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(w, want)
