@@ -298,7 +298,8 @@ class KVCache:
 
     # -- attention weights and eviction by them --------------------------------------
     def make_weights(self):
-        """Zeros [n_sessions][max_positions]: what each position of each session weighs so far."""
+        """Zeros [n_sessions][max_positions], filled on the current stream: what each position of each
+        session weighs so far."""
         import torch
         return torch.zeros((self.cfg.n_sessions, self.cfg.max_positions), dtype=torch.float32,
                            device=self.pool.device)
@@ -322,6 +323,8 @@ class KVCache:
         queries in one layer; `work`: make_weights_workspace."""
         import torch
         self._check_by_position("weights", weights, self.cfg.n_sessions, torch.float32)
+        if not work.is_contiguous() or work.device != self.pool.device:
+            raise ValueError(f"work must be contiguous on {self.pool.device}")
         _check(self.lib.kvc_attn_weights(self.ctx, layer, q.data_ptr(), weights.data_ptr(),
                                          work.data_ptr(), work.numel() * work.element_size(),
                                          _stream(stream)))

@@ -262,7 +262,7 @@ __device__ inline Item next_item(const Dev& d, int n_seq, const int* s_group, It
 
 // ---------------------------------------------------------------------------
 // Attention, and (STATS) the rows' (max, sum) alone.  An item is 32 tokens of one session and KV head,
-// the last ones first, against (STATS: a part of) the keys that they see; a warp has four tokens' rows.
+// the last ones first, against (a part of) the keys that they see; a warp has four tokens' rows.
 // ---------------------------------------------------------------------------
 constexpr int PROMPT_SMEM = (2 * ROWS * D + 4 * TILE) * 4;
 constexpr int STAT_SMEM = (2 * ROWS * D + 2 * TILE) * 4;
@@ -583,7 +583,8 @@ cudaError_t launch_prompt_f32(const Dev& d, const Limits& lim, int layer, const 
                             static_cast<float2*>(nullptr));
   *launches += e == cudaSuccess;
   if (e != cudaSuccess || parts == 1) return e;
-  e = launch_ex(&prompt_merge_f32_kernel, dim3(merge_grid(items, D)), dim3(MERGE_THREADS), 0, s, true, d, to, parts);
+  e = launch_ex(&prompt_merge_f32_kernel, dim3(merge_grid(items, D)), dim3(MERGE_THREADS), 0, s, true, d, to,
+                parts);
   *launches += e == cudaSuccess;
   return e;
 }

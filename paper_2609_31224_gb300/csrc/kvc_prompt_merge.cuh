@@ -2,8 +2,9 @@
 //
 // A part's rows (128 of an item's tile) leave their sums of P V, not divided, and (reference, sum) of P:
 // [slot][D / 4][128 rows][4] and [slot][128], in the prefill's partial slots (of binary32 contexts, which
-// have none, the decode's).  The parts of a tile have the slots (item * parts + part) * TILES + tile.  With M = max m_p a row is sum_p O_p 2^(m_p - M) divided by
-// sum_p l_p 2^(m_p - M), in the order of the parts, so that results repeat.
+// have none, the decode's).  The parts of a tile have the slots (item * parts + part) * TILES + tile.
+// With M = max m_p a row is sum_p O_p 2^(m_p - M) divided by sum_p l_p 2^(m_p - M), in the order of the
+// parts, so that results repeat.  The parts come from L2: 5 us a layer, mostly the launch.
 #pragma once
 
 #include "kvc_prompt_list.cuh"

@@ -4,20 +4,22 @@
 // An item is 64 tokens of one session and KV head: two tiles A and B of 32 tokens x G = 4 query heads =
 // 128 rows each, against the session's pages up to the last one that its last token sees, 128 keys (8
 // pages) a step.  Items go to the CTAs (one per SM) from a counter, a session's last tokens, which see
-// most, first.  A step has four products of 128^3: S_A, S_B (Q K^T) and O_A, O_B += P V; while the
-// softmax of one tile runs, the tensor cores have the other tile's.
+// most, first; few items have their keys cut into parts (kvc_prompt.cu).  A step has four products of
+// 128^3: S_A, S_B (Q K^T) and O_A, O_B += P V; while the softmax of one tile runs, the tensor cores have
+// the other tile's.
 //
 // Work and bound: 4 D flops a query row and key, 2.2 TFLOP for one prompt of 16,384 tokens and 8 KV
-// heads; 1,811 us, 1,210 TFLOP/s, 64 % of what the tensor cores were measured to do in a library
-// product.  Products and copies alone, without a softmax to wait for, take 1,294 us at one CTA's N = 128.
-// Beyond them a step is bound by the softmax, about 550 cycles for 32 keys of two rows' warps on a
-// scheduler, whose warps are short of instructions as often as they issue one.  K and V are read once per
-// item, 745 us of copies that run beside.  Also: 4,099 tokens 147 us a layer (938 TFLOP/s), eight
-// prompts of up to 2,500 tokens 183 us, four of up to 700 behind 4,096 positions 171 us, one of 250
-// tokens 14.0 us, which is latency: a launch, an item's set-up, two steps one after the other.
-// Measured and not taken: P of the second half in shared memory with scores of 128 keys a product (a
-// third fewer products; 16,384 tokens 1,826 us, 4,099 155 us), one product for both halves' scores
-// (1,970 us), 16 warps of softmax, two a row (1,970 us).
+// heads; 1,790 us, 1,230 TFLOP/s, 65 % of what the tensor cores were measured to do in a library
+// product.  A product instruction takes 77 cycles, 128 columns wide or 64: the 48 of a step, whose scores
+// come in halves (below), 3,700 of its 3,900 cycles.  With scores of 128 keys a product they would be 2,470
+// (1,294 us without a softmax to wait for), but then the softmax is what a step waits for, 550 cycles for
+// 32 keys of a row: measured with both halves' scores in one product (1,970 us; 16 warps of softmax, two a
+// row, the same) and with P of the second half in shared memory, so that the next scores can start early
+// (1,826 us; 4,099 tokens 155 us a layer).  K and V are read once per item, 745 us of copies that run
+// beside.  Also: 4,099 tokens 147 us a layer (938 TFLOP/s), eight prompts of up to 2,500 tokens 184 us,
+// four of up to 700 behind 4,096 positions 170 us, one of 250 tokens 14.5 us, which is latency: a launch,
+// an item's set-up, two steps one after the other.
+//
 // Warp roles (512 threads):
 //   warp 0      items from the counter; K and V by TMA, a page's 4 KiB of a head a copy (twice as many of
 //               2 KiB took 2,600 cycles a step for 1,900), into a ring of four 32 KiB stages in turn
