@@ -68,11 +68,13 @@ enum {
   B_EMPTY = B_FULL + RING,       // [RING] and was read
   B_Q_FULL = B_EMPTY + RING,     // [Q_SLOTS] a tile's query rows are there
   B_Q_EMPTY = B_Q_FULL + Q_SLOTS,  // [Q_SLOTS] and its last scores complete
-  // Halves of a step's keys: [2 tiles][2].  The first half's scores have one phase more an item, for
-  // the last step's first half of O += P V.
+  // Halves of a step's keys: [2 tiles][2].
   B_S = B_Q_EMPTY + Q_SLOTS,     // scores complete (and every product before them)
   B_P = B_S + 4,                 // P written, O rescaled
-  B_O = B_P + 4,                 // [2] the item's output complete
+  // (A phase of its own, not one more of B_S: the next item's first scores do not wait for the softmax, and
+  // a warp that finds two phases complete takes the first for one to come.)
+  B_LAST = B_P + 4,              // [2] the last step's first half of O += P V complete
+  B_O = B_LAST + 2,              // [2] the item's output complete
   B_O_EMPTY = B_O + 2,           // [2] and read
   // V stages of edge steps land here instead (their B_FULL phase completes at once), and have their
   // rows zeroed: the e-th such stage of the CTA, at e % EDGES.  A ring holds fewer.
@@ -175,7 +177,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
     for (int i = 0; i < N_BARS; ++i) {
       const int count = (i >= B_EMPTY && i < B_Q_FULL) || i == B_FINAL ? 2
                         : i >= B_Q_FULL && i < B_Q_EMPTY             ? 4
-                        : i >= B_P && i < B_O          ? 4
+                        : i >= B_P && i < B_LAST       ? 4
                         : i >= B_O_EMPTY && i < B_EDGE ? 4
                         : i >= B_ITEM_EMPTY && i < B_FINAL ? ITEM_READERS
                                                            : 1;
@@ -376,8 +378,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
                   tc_mma_ts(t_o, t_s + h * HALF + kk * 8, desc_at(vd, (h * (HALF / 16) + kk) * 2 * ROW_GROUP), ID_O,
                             j > 0 || h > 0 || kk > 0);
                 if (!last) scores(h);
-                if (!last || h == 0) tc_commit(&bars[B_S + 2 * x + h]);
-                else tc_commit(&bars[B_O + x]);
+                tc_commit(&bars[!last ? B_S + 2 * x + h : h == 0 ? B_LAST + x : B_O + x]);
               }
               ++p_no;
               if (j + 2 == steps) tc_commit(&bars[B_Q_EMPTY + q_slot]);
@@ -555,7 +556,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
               l *= f;
               add *= f;
               const int h = c / 2;
-              wait(B_S + 2 * x + (h ^ 1), (h == 0 ? s1_no : s0_no) & 1);
+              if (h == 1 && j == steps - 1) wait(B_LAST + x, o_no & 1);
+              else wait(B_S + 2 * x + (h ^ 1), (h == 0 ? s1_no : s0_no) & 1);
               tc_fence_after();
               tmem_st_wait();
 #pragma unroll 1
@@ -601,8 +603,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
           }
           l += add;
         }
-        wait(B_S + 2 * x, s0_no++ & 1);
-        if (!ok || !wait(B_O + x, o_no & 1)) break;
+        if (!ok || !wait(B_LAST + x, o_no & 1) || !wait(B_O + x, o_no & 1)) break;
         ++o_no;
         tc_fence_after();
         const float inv = 1.f / l;
