@@ -173,19 +173,17 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
   pdl_wait();
   pdl_launch_dependents();
   const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;  // (no units: the append failed)
-  if (tid == 0) {
-    for (int i = 0; i < N_BARS; ++i) {
-      const int count = (i >= B_EMPTY && i < B_Q_FULL) || i == B_FINAL ? 2
-                        : i >= B_Q_FULL && i < B_Q_EMPTY             ? 4
-                        : i >= B_P && i < B_LAST       ? 4
-                        : i >= B_O_EMPTY && i < B_EDGE ? 4
-                        : i >= B_ITEM_EMPTY && i < B_FINAL ? ITEM_READERS
-                                                           : 1;
-      mbar_init(&bars[i], count);
-    }
+  if (tid < N_BARS) {  // (by one thread they took 2.5 us of a short prompt's 17.5)
+    const int count = (tid >= B_EMPTY && tid < B_Q_FULL) || tid == B_FINAL ? 2
+                      : tid >= B_Q_FULL && tid < B_Q_EMPTY                 ? 4
+                      : tid >= B_P && tid < B_LAST                         ? 4
+                      : tid >= B_O_EMPTY && tid < B_EDGE                   ? 4
+                      : tid >= B_ITEM_EMPTY && tid < B_FINAL               ? ITEM_READERS
+                                                                           : 1;
+    mbar_init(&bars[tid], count);
     fence_mbar_init();
-    *stop = 0;
   }
+  if (tid == 0) *stop = 0;
   // Items of a session: 64-token tiles of its chunk, for each KV head, and parts of their keys.
   auto items_of = [&](int i) { return (d.seq[i].t + 2 * TOKENS - 1) / (2 * TOKENS) * H * parts; };
   if (warp == 3) list_items(n_seq, lane, s_group, items_of);
@@ -556,8 +554,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
               l *= f;
               add *= f;
               const int h = c / 2;
-              if (h == 1 && j == steps - 1) wait(B_LAST + x, o_no & 1);
-              else wait(B_S + 2 * x + (h ^ 1), (h == 0 ? s1_no : s0_no) & 1);
+              const bool end = h == 1 && j == steps - 1;
+              wait(end ? B_LAST + x : B_S + 2 * x + (h ^ 1), (end ? o_no : h == 0 ? s1_no : s0_no) & 1);
               tc_fence_after();
               tmem_st_wait();
 #pragma unroll 1
@@ -603,7 +601,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
           }
           l += add;
         }
-        if (!ok || !wait(B_LAST + x, o_no & 1) || !wait(B_O + x, o_no & 1)) break;
+        if (!ok || !wait(B_O + x, o_no & 1)) break;  // (B_LAST's phase is complete then, too)
         ++o_no;
         tc_fence_after();
         const float inv = 1.f / l;

@@ -88,19 +88,18 @@ struct Item {
 };
 static_assert(sizeof(Item) == 128, "Item size");
 
-__device__ inline void init_barriers(uint64_t* bars, bool sums) {
-  const int q_warps = sums ? SUMS_Q_WARPS : STAT_Q_WARPS;
-  for (int i = 0; i < N_BARS; ++i) {
-    const int count = i >= B_Q_FULL && i < B_Q_EMPTY         ? q_warps
-                      : i >= B_S_EMPTY && i < B_ITEM         ? 4
-                      : i >= B_ITEM_EMPTY && i < B_LSE_EMPTY ? ITEM_READERS + q_warps + sums
-                      : i >= B_LSE_EMPTY && i < B_LSE        ? 8
-                      : i >= B_KT && i < B_TURN              ? 4
-                      : i >= B_EMPTY && i < B_Q_FULL           ? (sums ? 4 : 2)
-                      : i >= B_Q_EMPTY && i < B_S && sums    ? 2
-                                                             : 1;
-    mbar_init(&bars[i], count);
-  }
+__device__ inline void init_barriers(uint64_t* bars, bool sums) {  // a thread a barrier
+  const int q_warps = sums ? SUMS_Q_WARPS : STAT_Q_WARPS, i = threadIdx.x;
+  if (i >= N_BARS) return;
+  const int count = i >= B_EMPTY && i < B_Q_FULL           ? (sums ? 4 : 2)
+                    : i >= B_Q_FULL && i < B_Q_EMPTY       ? q_warps
+                    : i >= B_Q_EMPTY && i < B_S && sums    ? 2
+                    : i >= B_S_EMPTY && i < B_ITEM         ? 4
+                    : i >= B_ITEM_EMPTY && i < B_LSE_EMPTY ? ITEM_READERS + q_warps + sums
+                    : i >= B_LSE_EMPTY && i < B_LSE        ? 8
+                    : i >= B_KT && i < B_TURN              ? 4
+                                                           : 1;
+  mbar_init(&bars[i], count);
   fence_mbar_init();
 }
 
@@ -137,10 +136,8 @@ __global__ void __launch_bounds__(STAT_THREADS, 1) weights_stat_kernel(
   pdl_wait();
   pdl_launch_dependents();
   const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;
-  if (tid == 0) {
-    init_barriers(bars, false);
-    *stop = 0;
-  }
+  init_barriers(bars, false);
+  if (tid == 0) *stop = 0;
   auto items_of = [&](int i) { return (d.seq[i].t + 2 * TOKENS - 1) / (2 * TOKENS) * H * parts; };
   if (warp == 2) list_items(n_seq, lane, s_group, items_of);
   __syncwarp();
@@ -384,10 +381,8 @@ __global__ void __launch_bounds__(SUMS_THREADS, 1) weights_sums_kernel(
   auto items_of = [&](int i) {
     return (d.seq[i].n_blocks + KEY_TILES * PAGES - 1) / (KEY_TILES * PAGES) * H * shares;
   };
-  if (tid == 0) {
-    init_barriers(bars, true);
-    *stop = 0;
-  }
+  init_barriers(bars, true);
+  if (tid == 0) *stop = 0;
   if (warp == 2) list_items(n_seq, lane, s_group, items_of);
   __syncwarp();
   if (warp == 1) tmem_alloc(tmem_slot, ALL_COLS);
