@@ -141,6 +141,31 @@ def test_many_sessions_of_long_chunks(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_items_a_cta(dtype):
+    """Items of one and two tiles and of one to three steps behind one another, time and again: the same bits."""
+    from tests import prompt_reference as R
+    rng = np.random.default_rng(14)
+    n = 200
+    cache = R.make_cache(n, dtype=dtype, layers=1, heads=8, pages=24, tokens=32768)
+    lens = [int(x) for x in rng.integers(1, 150, size=n)]
+    R.feed(cache, range(n), [int(x) for x in rng.integers(1, 200, size=n)], rng)
+    R.feed(cache, range(n), lens, rng)
+    q = R.queries(cache, sum(lens), rng)
+    want = check(cache, range(n), lens, rng, q=q)[0, :sum(lens)]
+    out = torch.zeros_like(q[0])
+    work, w = cache.make_weights_workspace(), [cache.make_weights() for _ in range(2)]
+    for _ in range(30):
+        out.zero_()
+        cache.attn_prompt(0, q[0], out)
+        assert torch.equal(out, want)
+        for x in w:
+            x.zero_()
+            cache.attn_weights(0, q[0], x, work)
+        assert torch.equal(w[0], w[1])
+    assert cache.device_status()[1] == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_a_prompt_of_one_session_among_many(dtype):
     from tests import prompt_reference as R
     rng = np.random.default_rng(2)
