@@ -27,8 +27,7 @@ cudaError_t launch_attn_prompt(const Dev& d, const Limits& lim, int layer, const
   const int64_t most = tc ? steps / 4 : std::max(steps / 4, std::min<int64_t>(steps / 2, 8));
   int64_t parts = lim.sms / items;
   if (parts == 1 && 2 * lim.sms / items > 2) parts = 3;
-  const int64_t slots = tc ? d.pf_slots / 2 : d.dec_slots * 4 / 128;  // (kvc_prompt_merge.cuh)
-  parts = std::max<int64_t>(1, std::min({parts, most, slots / items}));
+  parts = std::max<int64_t>(1, std::min({parts, most, part_items(d) / items}));
   // (All kernels wait for the one before them before they let the next one start.)
   order->launched(layer, false);
   return tc ? launch_prompt_tc(d, lim, layer, q, out, (int)parts, items, s, launches)

@@ -5,6 +5,16 @@
 
 namespace kvc {
 
+// Items of one part that the partial slots hold (kvc_prompt_merge.cuh).
+__host__ __device__ inline int part_items(const Dev& d) {
+  return d.esz == 2 ? d.pf_slots / 2 : d.dec_slots * 4 / 128;
+}
+// Parts of `items` items of a launch made for `parts`.  All its kernels take it from the items that are there:
+// a captured launch may be replayed behind a longer chunk, whose parts the slots would not hold.
+__device__ inline int parts_now(const Dev& d, int parts, int items) {
+  return max(1, min(parts, part_items(d) / max(1, items)));
+}
+
 cudaError_t prompt_tc_attributes();
 cudaError_t launch_prompt_tc(const Dev& d, const Limits& lim, int layer, const void* q, void* out, int parts,
                              int64_t items, cudaStream_t s, int64_t* launches);

@@ -241,20 +241,21 @@ __device__ inline bool odd_pages(int n_pg, const float* k, const float* v) {
   return odd;
 }
 
-// An item, as every thread has it.
+// An item, as every thread has it: one of `parts` of one of those that count() counts.
 struct Item {
   int seq, in;  // session of the call, and which of its items; seq < 0: no more
   int at;       // of all
 };
 template <typename CountFn>
-__device__ inline Item next_item(const Dev& d, int n_seq, const int* s_group, Item* s_item, CountFn count) {
+__device__ inline Item next_item(const Dev& d, int n_seq, int parts, const int* s_group, Item* s_item, CountFn count) {
   __syncthreads();
   if (threadIdx.x < 32) {
     int at = 0, in = 0;
     if (threadIdx.x == 0) at = take_item(d);
     at = __shfl_sync(FULL, at, 0);
-    const int seq = at < s_group[GROUPS] ? find_item(n_seq, threadIdx.x, s_group, at, count, &in) : -1;
-    if (threadIdx.x == 0) *s_item = {seq, in, at};
+    const int seq =
+        at < s_group[GROUPS] * parts ? find_item(n_seq, threadIdx.x, s_group, at / parts, count, &in) : -1;
+    if (threadIdx.x == 0) *s_item = {seq, in * parts + at % parts, at};
   }
   __syncthreads();
   return *s_item;
@@ -269,7 +270,7 @@ constexpr int STAT_SMEM = (2 * ROWS * D + 2 * TILE) * 4;
 
 template <bool STATS>
 __global__ void __launch_bounds__(THREADS, CTAS) prompt_f32_kernel(Dev d, int layer, const float* __restrict__ q,
-                                                             float* __restrict__ out, float scale, int parts,
+                                                             float* __restrict__ out, float scale, int most_parts,
                                                              float2* __restrict__ stats) {
   extern __shared__ __align__(16) float sm[];
   __shared__ int s_group[GROUPS + 1];
@@ -279,10 +280,12 @@ __global__ void __launch_bounds__(THREADS, CTAS) prompt_f32_kernel(Dev d, int la
   pdl_wait();
   pdl_launch_dependents();
   const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;  // (no units: the append failed)
-  auto items_of = [&](int i) { return (d.seq[i].t + TOKENS - 1) / TOKENS * H * parts; };
+  auto items_of = [&](int i) { return (d.seq[i].t + TOKENS - 1) / TOKENS * H; };
   if (warp == 0) list_items(n_seq, lane, s_group, items_of);
+  __syncthreads();
+  const int parts = STATS ? most_parts : parts_now(d, most_parts, s_group[GROUPS]);
   for (;;) {
-    const Item it = next_item(d, n_seq, s_group, &s_item, items_of);
+    const Item it = next_item(d, n_seq, parts, s_group, &s_item, items_of);
     if (it.seq < 0) break;
     const SeqInfo si = d.seq[it.seq];
     const int part = it.in % parts, head = it.in / parts % H;
@@ -479,7 +482,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) weights_sums_f32_kernel(Dev d, 
   auto items_of = [&](int i) { return (d.seq[i].n_blocks + KEY_PAGES - 1) / KEY_PAGES * H * shares; };
   if (warp == 0) list_items(n_seq, lane, s_group, items_of);
   for (;;) {
-    const Item it = next_item(d, n_seq, s_group, &s_item, items_of);
+    const Item it = next_item(d, n_seq, 1, s_group, &s_item, items_of);
     if (it.seq < 0) break;
     const SeqInfo si = d.seq[it.seq];
     const int head = it.in % H, share = it.in / H % shares, b0 = it.in / H / shares * KEY_PAGES;
@@ -557,7 +560,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) weights_sums_f32_kernel(Dev d, 
 }
 
 __global__ void __launch_bounds__(MERGE_THREADS) prompt_merge_f32_kernel(Dev d, float* out, int parts) {
-  merge_parts<float, D, 1>(d, out, parts, [](const SeqInfo&, int, int) { return false; });
+  merge_parts<float, D, 1>(d, out, parts, [](const SeqInfo&, int, int, int) { return false; });
 }
 
 template <typename K>

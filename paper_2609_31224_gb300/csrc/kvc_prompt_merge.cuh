@@ -7,6 +7,7 @@
 // parts, so that results repeat.  The parts come from L2: 5 us a layer, mostly the launch.
 #pragma once
 
+#include "kvc_prompt.h"
 #include "kvc_prompt_list.cuh"
 
 namespace kvc {
@@ -36,10 +37,10 @@ __device__ inline void put_row(__nv_bfloat16* to, const float (&v)[8]) {
 }
 
 // A CTA joins 16 dims of a tile's rows: a thread has 8 dims of one row.  Items are TILES tiles of 32 tokens
-// of one session and KV head, last ones first; empty(si, t0, part) says which parts left nothing.
+// of one session and KV head, last ones first; empty(si, t0, part, parts) says which of the parts left nothing.
 constexpr int MERGE_THREADS = 2 * PART_ROWS;
 template <typename T, int DIMS, int TILES, typename EmptyFn>
-__device__ inline void merge_parts(const Dev& d, T* out, int parts, EmptyFn empty) {
+__device__ inline void merge_parts(const Dev& d, T* out, int most_parts, EmptyFn empty) {
   constexpr int TOKENS_ = 32, HEADS_ = PART_ROWS / TOKENS_, SLICES = DIMS / 16;
   __shared__ int s_group[GROUPS + 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = d.kv_heads;
@@ -49,6 +50,8 @@ __device__ inline void merge_parts(const Dev& d, T* out, int parts, EmptyFn empt
   auto items_of = [&](int i) { return (d.seq[i].t + TILES * TOKENS_ - 1) / (TILES * TOKENS_) * H; };
   if (warp == 0) list_items(n_seq, lane, s_group, items_of);
   __syncthreads();
+  const int parts = parts_now(d, most_parts, s_group[GROUPS]);
+  if (parts == 1) return;  // (the items wrote their rows themselves)
   const int total = s_group[GROUPS] * TILES * SLICES;
   for (int at = blockIdx.x; at < total; at += gridDim.x) {
     const int item = at / (TILES * SLICES), x = at / SLICES % TILES, slice = at % SLICES;
@@ -61,7 +64,7 @@ __device__ inline void merge_parts(const Dev& d, T* out, int parts, EmptyFn empt
     const int quad = 4 * slice + 2 * (threadIdx.x / PART_ROWS);
     float m = -INFINITY, l = 0.f, o[8] = {};
     for (int p = 0; p < parts; ++p) {
-      if (empty(si, t0, p)) continue;
+      if (empty(si, t0, p, parts)) continue;
       const int slot = (item * parts + p) * TILES + x;
       const float2 ml = part_sums<DIMS>(d, slot)[r];
       const float4* row = part_rows<DIMS>(d, slot) + (size_t)quad * PART_ROWS + r;

@@ -161,7 +161,7 @@ __device__ __noinline__ void odd_value(const Dev& d, const SeqInfo& si, int laye
 __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
     Dev d, int layer, const __grid_constant__ CUtensorMap map,
     const __nv_bfloat16* __restrict__ q,
-    __nv_bfloat16* __restrict__ out, float qk_scale, int parts) {
+    __nv_bfloat16* __restrict__ out, float qk_scale, int most_parts) {
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + OFF_BARS);
   Item* items = reinterpret_cast<Item*>(smem + OFF_ITEM);
@@ -186,8 +186,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
     fence_mbar_init();
   }
   if (tid == 0) *stop = 0;
-  // Items of a session: 64-token tiles of its chunk, for each KV head, and parts of their keys.
-  auto items_of = [&](int i) { return (d.seq[i].t + 2 * TOKENS - 1) / (2 * TOKENS) * H * parts; };
+  // Items of a session: 64-token tiles of its chunk, for each KV head (and parts of their keys).
+  auto items_of = [&](int i) { return (d.seq[i].t + 2 * TOKENS - 1) / (2 * TOKENS) * H; };
   if (warp == 3) list_items(n_seq, lane, s_group, items_of);
   __syncwarp();
   if (warp == 1) tmem_alloc(tmem_slot, ALL_COLS);
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
   if (warp < 4) {
     if (warp == 0) {
       // ---------------- items, K and V ----------------
-      const int total = s_group[GROUPS];
+      const int parts = parts_now(d, most_parts, s_group[GROUPS]), total = s_group[GROUPS] * parts;
       uint32_t seq_no = 0, edges = 0;  // stages so far, and V stages of edge steps
       bool ok = true;
       auto wait = [&](int bar, uint32_t parity) {
@@ -216,11 +216,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
           if (lane == 0) at = take_item(d);
           at = __shfl_sync(FULL, at, 0);
           if (at >= total) return;
-          const int seq = find_item(n_seq, lane, s_group, at, items_of, &in);
+          const int seq = find_item(n_seq, lane, s_group, at / parts, items_of, &in), part = at % parts;
           word = lane < 16 ? reinterpret_cast<const int*>(d.seq + seq)[lane] : 0;
           const SeqInfo& si = d.seq[seq];
-          const int part = in % parts;
-          in /= parts;
           sid = si.sid;
           nhp = si.n_hist_pages;
           head = in % H;
@@ -652,8 +650,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
   if (tid == 0) leave_counters(d);
 }
 
-__global__ void __launch_bounds__(MERGE_THREADS) prompt_merge_kernel(Dev d, __nv_bfloat16* out, int parts) {
-  merge_parts<__nv_bfloat16, D, 2>(d, out, parts, [&](const SeqInfo& si, int t0, int part) {
+__global__ void __launch_bounds__(MERGE_THREADS) prompt_merge_kernel(Dev d, __nv_bfloat16* out, int most_parts) {
+  merge_parts<__nv_bfloat16, D, 2>(d, out, most_parts, [](const SeqInfo& si, int t0, int part, int parts) {
     const int nb = blocks_seen(si, min(t0 + 2 * TOKENS, si.t) - 1);
     int j0, j1;
     part_steps((nb + PAGES - 1) / PAGES, edge_steps(si, t0).diag, part, parts, &j0, &j1);
