@@ -247,7 +247,8 @@ struct Item {
   int at;       // of all
 };
 template <typename CountFn>
-__device__ inline Item next_item(const Dev& d, int n_seq, int parts, const int* s_group, Item* s_item, CountFn count) {
+__device__ inline Item next_item(const Dev& d, int n_seq, int parts, const int* s_group, Item* s_item,
+                                 CountFn count) {
   __syncthreads();
   if (threadIdx.x < 32) {
     int at = 0, in = 0;
@@ -283,7 +284,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) prompt_f32_kernel(Dev d, int la
   auto items_of = [&](int i) { return (d.seq[i].t + TOKENS - 1) / TOKENS * H; };
   if (warp == 0) list_items(n_seq, lane, s_group, items_of);
   __syncthreads();
-  const int parts = STATS ? most_parts : parts_now(d, most_parts, s_group[GROUPS]);
+  const int parts =
+      STATS ? stat_parts(d, most_parts, d.g->total_tokens) : parts_now(d, most_parts, s_group[GROUPS]);
   for (;;) {
     const Item it = next_item(d, n_seq, parts, s_group, &s_item, items_of);
     if (it.seq < 0) break;
@@ -467,7 +469,7 @@ constexpr int SUMS_SMEM = (2 * KEYS * D + 2 * TILE) * 4;
 
 __global__ void __launch_bounds__(THREADS, CTAS) weights_sums_f32_kernel(Dev d, int layer,
                                                                    const float* __restrict__ q, float scale,
-                                                                   int parts, int shares, WeightsWork work) {
+                                                                   int most_parts, int shares, WeightsWork work) {
   extern __shared__ __align__(16) float sm[];
   __shared__ int s_group[GROUPS + 1];
   __shared__ Item s_item;
@@ -478,7 +480,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) weights_sums_f32_kernel(Dev d, 
   pdl_wait();
   pdl_launch_dependents();
   const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;
-  const int total = d.g->total_tokens;
+  const int total = d.g->total_tokens, parts = stat_parts(d, most_parts, total);
   auto items_of = [&](int i) { return (d.seq[i].n_blocks + KEY_PAGES - 1) / KEY_PAGES * H * shares; };
   if (warp == 0) list_items(n_seq, lane, s_group, items_of);
   for (;;) {

@@ -116,9 +116,8 @@ cudaError_t launch_attn_weights(const Dev& d, const Limits& lim, int layer, cons
   const int64_t tokens = d.esz == 2 ? 64 : 32, pages = d.esz == 2 ? 32 : 8, ctas = lim.sms;
   const int64_t rows = ((int64_t)total + (tokens - 1) * n_seq) / tokens * d.kv_heads;
   const int64_t part = d.esz == 2 ? 32 : 8;
-  const int64_t stats = (int64_t)d.max_tokens * d.q_heads + WEIGHTS_STATS;
   int64_t parts = std::max<int64_t>(1, std::min<int64_t>(2 * ctas / rows, (pages_max + part - 1) / part));
-  parts = std::max<int64_t>(1, std::min(parts, stats / ((int64_t)total * d.q_heads)));
+  parts = stat_parts(d, (int)parts, total);
   const int64_t keys = (pages_sum / pages + n_seq) * d.kv_heads;
   int shares = 1;
   while (shares < WEIGHTS_SHARES && keys * shares < 4 * ctas && max_t / 32 > 4 * shares) shares *= 2;

@@ -18,6 +18,14 @@ constexpr int WEIGHTS_PARTS = 4096;  // parts of single tokens, at least twice t
 constexpr int WEIGHTS_STATS = 1 << 18;  // (max, sum) pairs beyond those of one part
 constexpr int WEIGHTS_SHARES = 8;    // of a chunk's tokens, at most (planes of a KV head)
 
+// Parts of the keys for `tokens` rows of a launch made for `parts`, as far as the pairs hold.  All its kernels
+// take it from the tokens that are there: a captured launch may be replayed behind a longer chunk.
+__host__ __device__ inline int stat_parts(const Dev& d, int parts, int tokens) {
+  const int64_t pairs = (int64_t)d.max_tokens * d.q_heads + WEIGHTS_STATS;
+  const int64_t most = pairs / ((int64_t)(tokens > 0 ? tokens : 1) * d.q_heads);
+  return most < parts ? (most > 1 ? (int)most : 1) : parts;
+}
+
 // log2 of a row's denominator from its parts' (max, sum), eight of them read at once (one after the other,
 // nine parts held up a step of few items by 3 us).
 __device__ inline float row_lse(const float2* row, size_t stride, int parts) {

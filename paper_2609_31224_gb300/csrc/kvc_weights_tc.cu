@@ -123,7 +123,7 @@ __device__ inline void piece_products(uint32_t to, uint32_t a, uint32_t a_step, 
 __global__ void __launch_bounds__(STAT_THREADS, 1) weights_stat_kernel(
     Dev d, int layer, const __grid_constant__ CUtensorMap map,
     const __nv_bfloat16* __restrict__ q, float qk_scale,
-    int parts, WeightsWork work) {
+    int most_parts, WeightsWork work) {
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem);
   Item* items = reinterpret_cast<Item*>(smem + OFF_ITEM);
@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(STAT_THREADS, 1) weights_stat_kernel(
   uint8_t* s_k = s_q + 4 * SLOT;
   pdl_wait();
   pdl_launch_dependents();
-  const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;
+  const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0, parts = stat_parts(d, most_parts, d.g->total_tokens);
   init_barriers(bars, false);
   if (tid == 0) *stop = 0;
   auto items_of = [&](int i) { return (d.seq[i].t + 2 * TOKENS - 1) / (2 * TOKENS) * H * parts; };
@@ -364,7 +364,7 @@ static_assert((GROUPS + 1) * 4 <= 136 && OFF_LSE % 16 == 0 && OFF_LSE + LSE_RING
 __global__ void __launch_bounds__(SUMS_THREADS, 1) weights_sums_kernel(
     Dev d, int layer, const __grid_constant__ CUtensorMap map,
     const __nv_bfloat16* __restrict__ q, float qk_scale,
-    int parts, int shares, WeightsWork work) {
+    int most_parts, int shares, WeightsWork work) {
   extern __shared__ __align__(1024) uint8_t smem[];
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem);
   Item* items = reinterpret_cast<Item*>(smem + OFF_ITEM);
@@ -518,6 +518,7 @@ __global__ void __launch_bounds__(SUMS_THREADS, 1) weights_sums_kernel(
       }
     } else {  // four rows of a query tile each lane: their denominators; rows past the chunk draw nothing
       uint32_t q_no = 0;
+      const int parts = stat_parts(d, most_parts, d.g->total_tokens);
       const size_t stride = (size_t)d.g->total_tokens * d.q_heads;
       for (int n = 0; ok; ++n) {
         if (!wait_warp(B_ITEM + (n & 1), (n >> 1) & 1)) break;

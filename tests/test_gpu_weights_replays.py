@@ -1,0 +1,68 @@
+"""Attention weights captured behind one append and replayed behind others: what a replay adds is drawn by
+the queries of the append that is the last one then.  Tolerances as in test_gpu_weights.py."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+REL = 6e-5
+
+
+def workspace(cache):
+    """Scratch with a guard behind it, and the check that the guard is as it was."""
+    need = cache.make_weights_workspace().numel()
+    room = torch.full((need + (1 << 22),), 0x5A, dtype=torch.uint8, device="cuda")
+    return room[:need], lambda: bool((room[need:] == 0x5A).all())
+
+
+def holds(cache, sessions, lens, q, w):
+    """w, from zeros, against 64 bits; what is not resident in these sessions, and others, untouched."""
+    from tests import prompt_reference as R
+    at = 0
+    touched = torch.zeros_like(w, dtype=torch.bool)
+    for s, t in zip(sessions, lens):
+        k, v = R.held(cache, s)
+        pos = torch.as_tensor(cache.export_state(s)["pos"], device="cuda")
+        want = sum(R.attention(cache, s, q[layer, at:at + t], k[layer], v[layer])[1]
+                   for layer in range(cache.cfg.layers))
+        assert torch.allclose(w[s, pos].double(), want, rtol=REL, atol=1e-12), (s, t)
+        touched[s, pos] = True
+        at += t
+    assert bool((w[~touched] == 0.0).all())
+
+
+def replays(cache, first, others, rng):
+    from tests import prompt_reference as R
+    most = max(sum(x[1]) for x in [first] + others)
+    q = R.queries(cache, most, rng)
+    w = cache.make_weights()
+    work, whole = workspace(cache)
+    R.feed(cache, *first, rng)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        for layer in range(cache.cfg.layers):
+            cache.attn_weights(layer, q[layer], w, work)
+    for sessions, lens in [first] + others:
+        if (sessions, lens) != first:
+            R.feed(cache, sessions, lens, rng)
+        w.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert cache.device_status()[1] == 0
+        holds(cache, sessions, lens, q, w)
+        assert whole()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 2])
+def test_a_short_chunk_replayed_behind_long_ones(dtype, n):
+    """The row statistics of a long chunk in as many parts as the short one's would not fit."""
+    from tests import prompt_reference as R
+    rng = np.random.default_rng(n)
+    cache = R.make_cache(n, dtype=dtype, heads=4, layers=1, pages=1000, positions=14000, tokens=7100)
+    every = list(range(n))
+    R.feed(cache, every, [7000] + [50] * (n - 1), rng)
+    replays(cache, (every, [20] * n), [(every, [4000] + [33] * (n - 1)), (every, [2] * n),
+                                       (every, [900] + [1] * (n - 1))], rng)
