@@ -100,7 +100,8 @@ enum {
   KVC_DERR_PAGE_TABLE = 2,   /* a session's page list is full */
   KVC_DERR_POSITION = 4,     /* position beyond max_positions */
   KVC_DERR_MOVES = 8,        /* eviction move list full */
-  KVC_DERR_WAIT = 16         /* a pipeline wait gave up (bounded spin) */
+  KVC_DERR_WAIT = 16,        /* a pipeline wait gave up (bounded spin) */
+  KVC_DERR_CHUNK = 32        /* a captured launch was replayed behind longer chunks than it takes */
 };
 
 typedef struct kvc_config {

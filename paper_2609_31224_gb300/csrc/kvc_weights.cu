@@ -18,7 +18,7 @@ namespace {
 constexpr int THREADS = 256;
 
 // The planes' sums of each resident position, added to what it weighs: blockIdx.y is the session of the
-// call.  SPLIT threads have every SPLIT-th plane of a position, so that few loads follow one another (one
+// call (the first of some, where a captured launch is replayed behind more of them).  SPLIT threads have every SPLIT-th plane of a position, so that few loads follow one another (one
 // thread took 22 us for 64 planes of 4,000 positions); their sums are joined in order.
 constexpr int SPLIT = 4, POSITIONS = THREADS / SPLIT;
 
@@ -28,31 +28,33 @@ __global__ void __launch_bounds__(THREADS) weights_add_kernel(Dev d, int planes,
   const int x = threadIdx.x % POSITIONS, part = threadIdx.x / POSITIONS;
   pdl_wait();
   pdl_launch_dependents();
-  if (d.g->n_units == 0) return;
-  const SeqInfo si = d.seq[blockIdx.y];
+  const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;
   const size_t plane = (size_t)d.n_pages * PS;
-  for (int at0 = blockIdx.x * POSITIONS; at0 < si.n_blocks * PS; at0 += gridDim.x * POSITIONS) {
-    const int at = at0 + x, blk = at / PS, slot = at % PS;
-    const BlockRange br = blk < si.n_blocks ? block_range(si, blk) : BlockRange{0, 0, 0};
-    const bool in = slot >= br.lo && slot < br.hi;
-    float w = 0.f;
-    int gs = 0;
-    float* to = nullptr;
-    if (in) {
-      gs = block_page(si, d.hist_pt + (size_t)si.sid * d.max_pages_per_session,
-                      d.live_pt + (size_t)si.sid * d.max_pages_per_session, blk) * PS + slot;
-      if (part == 0) to = weights + (size_t)si.sid * d.max_positions + d.meta_pos[gs];
+  for (int seq = blockIdx.y; seq < n_seq; seq += gridDim.y) {
+    const SeqInfo si = d.seq[seq];
+    for (int at0 = blockIdx.x * POSITIONS; at0 < si.n_blocks * PS; at0 += gridDim.x * POSITIONS) {
+      const int at = at0 + x, blk = at / PS, slot = at % PS;
+      const BlockRange br = blk < si.n_blocks ? block_range(si, blk) : BlockRange{0, 0, 0};
+      const bool in = slot >= br.lo && slot < br.hi;
+      float w = 0.f;
+      int gs = 0;
+      float* to = nullptr;
+      if (in) {
+        gs = block_page(si, d.hist_pt + (size_t)si.sid * d.max_pages_per_session,
+                        d.live_pt + (size_t)si.sid * d.max_pages_per_session, blk) * PS + slot;
+        if (part == 0) to = weights + (size_t)si.sid * d.max_positions + d.meta_pos[gs];
 #pragma unroll 16
-      for (int h = part; h < planes; h += SPLIT) w += work.scores[h * plane + gs];
-    }
-    s_sum[part][x] = w;
-    __syncthreads();
-    if (to) {
+        for (int h = part; h < planes; h += SPLIT) w += work.scores[h * plane + gs];
+      }
+      s_sum[part][x] = w;
+      __syncthreads();
+      if (to) {
 #pragma unroll
-      for (int p = 1; p < SPLIT; ++p) w += s_sum[p][x];
-      *to += w;
+        for (int p = 1; p < SPLIT; ++p) w += s_sum[p][x];
+        *to += w;
+      }
+      __syncthreads();
     }
-    __syncthreads();
   }
 }
 

@@ -66,3 +66,43 @@ def test_a_short_chunk_replayed_behind_long_ones(dtype, n):
     R.feed(cache, every, [7000] + [50] * (n - 1), rng)
     replays(cache, (every, [20] * n), [(every, [4000] + [33] * (n - 1)), (every, [2] * n),
                                        (every, [900] + [1] * (n - 1))], rng)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tokens", [1, 7, 70])
+def test_replayed_behind_other_sessions(dtype, tokens):
+    """Fewer sessions (nothing of those before them counts), more, and in another order."""
+    from tests import prompt_reference as R
+    rng = np.random.default_rng(tokens)
+    cache = R.make_cache(6, dtype=dtype, heads=2, layers=2, pages=64, positions=1000)
+    R.feed(cache, range(6), [300, 17, 150, 1, 64, 90], rng)
+    replays(cache, ([4, 1, 0], [tokens] * 3), [
+        ([2], [tokens]), ([5, 3, 0, 1, 2, 4], [tokens] * 6), ([0, 1], [tokens] * 2),
+        ([3, 4, 5, 0], [tokens] * 4)], rng)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_single_tokens_replayed_behind_a_chunk_are_refused(dtype):
+    """Captured for a token of each session, replayed behind several: the error word says so, and nothing
+    is added."""
+    from tests import prompt_reference as R
+    rng = np.random.default_rng(3)
+    cache = R.make_cache(2, dtype=dtype)
+    work, w = cache.make_weights_workspace(), cache.make_weights()
+    R.feed(cache, [0, 1], [100, 30], rng)
+    R.feed(cache, [0, 1], [1, 1], rng)
+    q = R.queries(cache, 40, rng)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        cache.attn_weights(0, q[0], w, work)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert cache.device_status()[1] == 0 and bool((w != 0).any())
+    for lens in ([1, 2], [40]):
+        R.feed(cache, range(len(lens)), lens, rng)
+        before = w.clone()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(w, before)
+    assert cache.device_status()[1] == 32
