@@ -29,6 +29,10 @@
  *    reports the recorded code).
  *  - Layouts are row-major and contiguous.  The element type (binary32 or
  *    bfloat16) is fixed at creation for K, V, q and out alike.
+ *  - A captured attention call (CUDA graphs) takes sessions, lengths, positions and
+ *    pages from the append that is the last one when it is replayed; d_q and d_out
+ *    then hold that append's rows.  It is for appends that the call would take, with as
+ *    many sessions as the captured one.  (kvc_attn_prompt and kvc_attn_weights say more.)
  *  - One context serves one host thread and one stream at a time: its
  *    launches share the context's scratch (split-K slots, arrival counters)
  *    and its host mirrors, so calls on it must be ordered on one stream (or
@@ -297,6 +301,9 @@ int kvc_attn_decode_noalloc(kvc_ctx* ctx, int layer, const void* d_q, void* d_ou
  * bfloat16, binary32 accumulation and softmax; binary32 ones with products of operands in two TF32
  * pieces (off by less than 2^-21 of a product), accumulation and softmax in binary32.
  *   d_q, d_out  device [total][Hq][D], as for kvc_attn_prefill_chunk
+ * Captured behind chunks of more than 32 tokens it may be replayed behind chunks of any length and any
+ * number of sessions; behind chunks of 2 to 32 tokens, behind such chunks (behind longer ones it writes
+ * nothing and the error word says KVC_DERR_CHUNK); behind single tokens, behind single tokens.
  * KVC_EINVAL with KVC_KV4 for chunks of more than 32 tokens. */
 int kvc_attn_prompt(kvc_ctx* ctx, int layer, const void* d_q, void* d_out, void* stream);
 
@@ -310,6 +317,9 @@ int kvc_attn_prompt(kvc_ctx* ctx, int layer, const void* d_q, void* d_out, void*
  *              aligned; the caller clears a session's row when it ends (kvc_release)
  *   d_work     device scratch of at least kvc_weights_workspace bytes, 256-byte aligned; its
  *              contents need not last between calls, calls that share it must be ordered
+ * Captured behind chunks it may be replayed behind chunks of any length, behind single tokens only behind
+ * such (behind others it adds nothing and the error word says KVC_DERR_CHUNK); the number of sessions may
+ * be another in both.
  * KVC_EINVAL with KVC_KV4. */
 int kvc_attn_weights(kvc_ctx* ctx, int layer, const void* d_q, float* d_weights, void* d_work,
                      size_t work_bytes, void* stream);

@@ -116,7 +116,8 @@ __global__ void __launch_bounds__(THREADS, 2) attn_prefill_f32_kernel(
   const int slice = blockIdx.x % k, rb = blockIdx.x / k % n_rb, pair = blockIdx.x / k / n_rb;
   const int H = d.kv_heads, seq = pair / H, head = pair % H;
   if (!early) pdl_wait();  // the first call after an append waits for it
-  if (d.g->n_units == 0) {  // the append failed: the whole grid has nothing to do
+  if (d.g->n_units == 0) {  // the append failed, or its chunks are too long: the whole grid has nothing to do
+    if (blockIdx.x == 0 && tid == 0) note_long_chunks(d);
     pdl_wait();
     return;
   }

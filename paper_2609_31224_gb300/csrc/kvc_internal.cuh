@@ -55,7 +55,8 @@ struct DevGlobals {
   int32_t err;
   int32_t n_seq;
   int64_t pages_used;
-  int32_t n_units;
+  int32_t n_units;    // (session, KV head, page) units of the last append for the kernels of chunks of up to
+                      // PF_MAX_TOKENS tokens: 0 where one is longer (or the append failed)
   int32_t free_word;  // no page below bitmap word free_word is free
   int32_t n_moves;
   int32_t total_tokens;
@@ -236,6 +237,12 @@ __device__ inline int block_page(const SeqInfo& si, const int32_t* hist_row,
 }
 
 __device__ inline void set_error(const Dev& d, int bits) { atomicOr(&d.g->err, bits); }
+
+// What a launch of the kernels of short chunks records that finds no units (one thread): captured behind such
+// chunks, it was replayed behind longer ones.  Behind a failed append, whose error is recorded, nothing.
+__device__ inline void note_long_chunks(const Dev& d) {
+  if (d.g->total_tokens > 0) set_error(d, KVC_DERR_CHUNK);
+}
 
 // Tagged partial states.  A CTA writes each value of its partial state as one
 // 64-bit word, (tag << 32) | binary32 bits, and arrives with a relaxed atomic: no

@@ -18,6 +18,7 @@ template <int N>
 struct AppendArgsT {
   int32_t n_seq;
   int32_t total;
+  int32_t max_t;  // longest chunk
   int32_t sessions[N];
   int32_t cu[N + 1];
 };

@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(META_THREADS) append_plan_kernel(Dev d, Append
   if (i == 0) {
     d.g->n_seq = n_seq;
     d.g->total_tokens = a.total;
-    d.g->n_units = s_total_dec;
+    d.g->n_units = a.max_t > PF_MAX_TOKENS ? 0 : s_total_dec;
     d.g->pages_used += total_need;
   }
 }
@@ -1039,6 +1039,7 @@ cudaError_t launch_append(const Dev& d, bool kv4, const AppendArgs& a, const uin
     AppendArgsT<FEW> few;
     few.n_seq = a.n_seq;
     few.total = a.total;
+    few.max_t = a.max_t;
     for (int i = 0; i < a.n_seq; ++i) few.sessions[i] = a.sessions[i];
     for (int i = 0; i <= a.n_seq; ++i) few.cu[i] = a.cu[i];
     e = launch_ex(&append_plan_kernel<FEW>, dim3(1), dim3(META_THREADS), 0, s, true, d, few, types);

@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) prompt_f32_kernel(Dev d, int la
   float *s_q = sm, *s_k = sm + 2 * ROWS * D, *s_v = s_k + 2 * TILE;
   pdl_wait();
   pdl_launch_dependents();
-  const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;  // (no units: the append failed)
+  const int n_seq = d.g->total_tokens > 0 ? d.g->n_seq : 0;  // (no tokens: the append failed)
   auto items_of = [&](int i) { return (d.seq[i].t + TOKENS - 1) / TOKENS * H; };
   if (warp == 0) list_items(n_seq, lane, s_group, items_of);
   __syncthreads();
@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) weights_sums_f32_kernel(Dev d, 
   float *s_k = sm, *s_q = sm + 2 * KEYS * D;
   pdl_wait();
   pdl_launch_dependents();
-  const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;
+  const int n_seq = d.g->total_tokens > 0 ? d.g->n_seq : 0;
   const int total = d.g->total_tokens, parts = stat_parts(d, most_parts, total);
   auto items_of = [&](int i) { return (d.seq[i].n_blocks + KEY_PAGES - 1) / KEY_PAGES * H * shares; };
   if (warp == 0) list_items(n_seq, lane, s_group, items_of);

@@ -46,7 +46,7 @@ __device__ inline void merge_parts(const Dev& d, T* out, int most_parts, EmptyFn
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, H = d.kv_heads;
   pdl_wait();
   pdl_launch_dependents();
-  const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;
+  const int n_seq = d.g->total_tokens > 0 ? d.g->n_seq : 0;
   auto items_of = [&](int i) { return (d.seq[i].t + TILES * TOKENS_ - 1) / (TILES * TOKENS_) * H; };
   if (warp == 0) list_items(n_seq, lane, s_group, items_of);
   __syncthreads();

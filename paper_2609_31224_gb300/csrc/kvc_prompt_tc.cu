@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
   uint8_t* s_ring = s_q + Q_SLOTS * SLOT;
   pdl_wait();
   pdl_launch_dependents();
-  const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;  // (no units: the append failed)
+  const int n_seq = d.g->total_tokens > 0 ? d.g->n_seq : 0;  // (no tokens: the append failed)
   if (tid < N_BARS) {  // (by one thread they took 2.5 us of a short prompt's 17.5)
     const int count = (tid >= B_EMPTY && tid < B_Q_FULL) || tid == B_FINAL ? 2
                       : tid >= B_Q_FULL && tid < B_Q_EMPTY                 ? 4

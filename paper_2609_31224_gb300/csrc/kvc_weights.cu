@@ -28,7 +28,7 @@ __global__ void __launch_bounds__(THREADS) weights_add_kernel(Dev d, int planes,
   const int x = threadIdx.x % POSITIONS, part = threadIdx.x / POSITIONS;
   pdl_wait();
   pdl_launch_dependents();
-  const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;
+  const int n_seq = d.g->total_tokens > 0 ? d.g->n_seq : 0;
   const size_t plane = (size_t)d.n_pages * PS;
   for (int seq = blockIdx.y; seq < n_seq; seq += gridDim.y) {
     const SeqInfo si = d.seq[seq];

@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(STAT_THREADS, 1) weights_stat_kernel(
   uint8_t* s_k = s_q + 4 * SLOT;
   pdl_wait();
   pdl_launch_dependents();
-  const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0, parts = stat_parts(d, most_parts, d.g->total_tokens);
+  const int n_seq = d.g->total_tokens > 0 ? d.g->n_seq : 0, parts = stat_parts(d, most_parts, d.g->total_tokens);
   init_barriers(bars, false);
   if (tid == 0) *stop = 0;
   auto items_of = [&](int i) { return (d.seq[i].t + 2 * TOKENS - 1) / (2 * TOKENS) * H * parts; };
@@ -377,7 +377,7 @@ __global__ void __launch_bounds__(SUMS_THREADS, 1) weights_sums_kernel(
   uint8_t* s_q = s_k + 2 * SLOT;        // two tiles of two pieces
   pdl_wait();
   pdl_launch_dependents();
-  const int n_seq = d.g->n_units > 0 ? d.g->n_seq : 0;
+  const int n_seq = d.g->total_tokens > 0 ? d.g->n_seq : 0;
   auto items_of = [&](int i) {
     return (d.seq[i].n_blocks + KEY_TILES * PAGES - 1) / (KEY_TILES * PAGES) * H * shares;
   };

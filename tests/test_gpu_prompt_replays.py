@@ -54,3 +54,32 @@ def test_replayed_behind_other_chunks(dtype, heads, first, others):
         torch.cuda.synchronize()
         assert cache.device_status()[1] == 0
         holds(cache, range(len(lens)), lens, q, out)
+
+
+@pytest.mark.parametrize("dtype, kv_bits", [("bf16", None), ("f32", None), ("bf16", 4), ("f32", 4)])
+@pytest.mark.parametrize("n, tokens", [(1, 17), (1, 32), (3, 17), (40, 20)])
+def test_short_chunks_replayed_behind_long_ones_are_refused(dtype, kv_bits, n, tokens):
+    """The kernels of chunks of up to 32 tokens do nothing behind longer ones, and the error word says so."""
+    from tests import prompt_reference as R
+    rng = np.random.default_rng(n)
+    cache = R.make_cache(n, dtype=dtype, kv_bits=kv_bits, layers=1, pages=80)
+    every = list(range(n))
+    R.feed(cache, every, [50] * n, rng)
+    R.feed(cache, every, [tokens] * n, rng)
+    q = R.queries(cache, 4000, rng)
+    out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        cache.attn_prompt(0, q[0], out[0])
+    graph.replay()
+    R.feed(cache, every, [2] * n, rng)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert cache.device_status()[1] == 0 and bool((out[0, :tokens * n] != 7.0).any())
+    R.feed(cache, every, [33] + [3] * (n - 1), rng)
+    out.fill_(7.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert cache.device_status()[1] == 32
+    assert bool((out == 7.0).all())
