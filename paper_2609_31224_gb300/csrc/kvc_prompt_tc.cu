@@ -64,6 +64,8 @@ constexpr int S_COL = 0, O_COL = 256, ALL_COLS = 512;
 constexpr int HALF = KEYS / 2;                     // of a step's keys
 constexpr int CHUNK = 32;                          // keys that a row takes at a time
 constexpr float SUM_LIMIT = 1048576.f;              // of a chunk's P in a row: 2^20
+constexpr float NO_KEY = -3.402823466e38f;          // reference of a row whose keys so far all score -infinity
+constexpr float ALL_UP = 200.f;                     // a rise of the reference behind which nothing is left of P
 
 enum {
   B_FULL = 0,                    // [RING] a stage has landed
@@ -547,10 +549,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
             // then it rises by a whole number, so that what was written of P scales exactly.  O may be
             // rescaled behind the last O += P V: the other half's scores come after it, of the same step
             // behind the second half's of the step before, of the next one behind the first half's.
-            if (j == 0 && c == 0) m = most();
+            // A first chunk all at -infinity leaves a finite reference, under which every other score's P is
+            // infinite, and -infinity's 0.
+            if (j == 0 && c == 0) m = fmaxf(most(), NO_KEY);
             float sum = sum_of();
             if (!__all_sync(FULL, sum < SUM_LIMIT)) {
-              const float up = fmaxf(ceilf(most() - m), 0.f), f = exp2f(-up);
+              const float top = most(), up = fmaxf(ceilf(top - m), 0.f), f = exp2f(-up);
               l *= f;
               add *= f;
               const int h = c / 2;
@@ -576,7 +580,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
                   to[i] = pack_bf16(bf16lo(__float_as_uint(o[i])) * f, bf16hi(__float_as_uint(o[i])) * f);
                 tmem_st16(t_s + h * HALF, to);
               }
-              m += up;
+              m = up > ALL_UP ? top : m + up;  // (far scores have no whole numbers between them)
               sum = sum_of();
             }
             add += sum;
