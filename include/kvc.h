@@ -105,7 +105,7 @@ enum {
   KVC_DERR_POSITION = 4,     /* position beyond max_positions */
   KVC_DERR_MOVES = 8,        /* eviction move list full */
   KVC_DERR_WAIT = 16,        /* a pipeline wait gave up (bounded spin) */
-  KVC_DERR_CHUNK = 32        /* a captured launch was replayed behind longer chunks than it takes */
+  KVC_DERR_CHUNK = 32        /* a captured call was replayed behind chunks that it does not take */
 };
 
 typedef struct kvc_config {
@@ -317,9 +317,9 @@ int kvc_attn_prompt(kvc_ctx* ctx, int layer, const void* d_q, void* d_out, void*
  *              aligned; the caller clears a session's row when it ends (kvc_release)
  *   d_work     device scratch of at least kvc_weights_workspace bytes, 256-byte aligned; its
  *              contents need not last between calls, calls that share it must be ordered
- * Captured behind chunks it may be replayed behind chunks of any length, behind single tokens only behind
- * such (behind others it adds nothing and the error word says KVC_DERR_CHUNK); the number of sessions may
- * be another in both.
+ * Captured behind chunks it may be replayed behind chunks of any length and any number of sessions; behind
+ * single tokens, behind single tokens of as many sessions (behind others it adds nothing and the error word
+ * says KVC_DERR_CHUNK).
  * KVC_EINVAL with KVC_KV4. */
 int kvc_attn_weights(kvc_ctx* ctx, int layer, const void* d_q, float* d_weights, void* d_work,
                      size_t work_bytes, void* stream);

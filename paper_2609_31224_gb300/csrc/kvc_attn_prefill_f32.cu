@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(THREADS, 2) attn_prefill_f32_kernel(
   const int H = d.kv_heads, seq = pair / H, head = pair % H;
   if (!early) pdl_wait();  // the first call after an append waits for it
   if (d.g->n_units == 0) {  // the append failed, or its chunks are too long: the whole grid has nothing to do
-    if (blockIdx.x == 0 && tid == 0) note_long_chunks(d);
+    if (blockIdx.x == 0 && tid == 0) note_other_chunks(d);
     pdl_wait();
     return;
   }

@@ -320,7 +320,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_prefill_tc_kernel(
   // The first call after an append waits for it (and lets nothing else start before that).
   if (!early) pdl_wait();
   if (CLUSTER && d.g->n_units == 0) {  // the append failed, or its chunks are too long: nothing to do for any CTA
-    if (blockIdx.x == 0 && tid == 0) note_long_chunks(d);
+    if (blockIdx.x == 0 && tid == 0) note_other_chunks(d);
     pdl_wait();
     return;
   }
@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_prefill_tc_kernel(
     u_end = seg.end;
   } else {
     us = unit_split(d, gridDim.x, PF_MIN_UNITS, PF_MAX_PARTS);
-    if (us.U == 0 && cta == 0 && tid == 0) note_long_chunks(d);
+    if (us.U == 0 && cta == 0 && tid == 0) note_other_chunks(d);
     const bool active = cta < us.n_cta;
     u_begin = active ? us.start_of(cta) : 0;
     u_end = active ? us.start_of(cta + 1) : 0;

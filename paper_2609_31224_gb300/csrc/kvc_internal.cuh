@@ -238,9 +238,9 @@ __device__ inline int block_page(const SeqInfo& si, const int32_t* hist_row,
 
 __device__ inline void set_error(const Dev& d, int bits) { atomicOr(&d.g->err, bits); }
 
-// What a launch of the kernels of short chunks records that finds no units (one thread): captured behind such
-// chunks, it was replayed behind longer ones.  Behind a failed append, whose error is recorded, nothing.
-__device__ inline void note_long_chunks(const Dev& d) {
+// What a launch records that finds no units (one thread): it was captured, and replayed behind chunks that it does
+// not take.  Behind a failed append, whose error is recorded, nothing.
+__device__ inline void note_other_chunks(const Dev& d) {
   if (d.g->total_tokens > 0) set_error(d, KVC_DERR_CHUNK);
 }
 

@@ -498,7 +498,7 @@ __global__ void __launch_bounds__(384, 1) prefill_kv4_f32_kernel(
   const SeqInfo si = d.seq[seq];
   const int parts = min(k_slices, si.n_blocks);
   if (d.g->n_units == 0 || slice >= parts) {  // the append failed, too long chunks; no page left for this CTA
-    if (d.g->n_units == 0 && blockIdx.x == 0 && threadIdx.x == 0) note_long_chunks(d);
+    if (d.g->n_units == 0 && blockIdx.x == 0 && threadIdx.x == 0) note_other_chunks(d);
     pdl_wait();
     return;
   }

@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(THREADS, 1) prefill_kv4_kernel(
   // The first call after an append waits for it (and lets nothing else start before that).
   if (early == EARLY_NONE) pdl_wait();
   if (d.g->n_units == 0) {  // the append failed, or its chunks are too long: nothing to do for any CTA
-    if (blockIdx.x == 0 && tid == 0) note_long_chunks(d);
+    if (blockIdx.x == 0 && tid == 0) note_other_chunks(d);
     pdl_wait();
     return;
   }

@@ -12,7 +12,7 @@ __host__ __device__ inline int part_items(const Dev& d) {
 // Parts of `items` items of a launch made for `parts`.  All its kernels take it from the items that are there:
 // a captured launch may be replayed behind a longer chunk, whose parts the slots would not hold.
 __device__ inline int parts_now(const Dev& d, int parts, int items) {
-  return max(1, min(parts, part_items(d) / max(1, items)));
+  return parts * items <= part_items(d) ? parts : max(1, part_items(d) / items);
 }
 
 cudaError_t prompt_tc_attributes();

@@ -28,10 +28,11 @@ __global__ void __launch_bounds__(THREADS) weights_add_kernel(Dev d, int planes,
   const int x = threadIdx.x % POSITIONS, part = threadIdx.x / POSITIONS;
   pdl_wait();
   pdl_launch_dependents();
+  SeqInfo si = d.seq[blockIdx.y];  // (asked for together with the counts)
   const int n_seq = d.g->total_tokens > 0 ? d.g->n_seq : 0;
   const size_t plane = (size_t)d.n_pages * PS;
   for (int seq = blockIdx.y; seq < n_seq; seq += gridDim.y) {
-    const SeqInfo si = d.seq[seq];
+    if (seq >= (int)gridDim.y) si = d.seq[seq];
     for (int at0 = blockIdx.x * POSITIONS; at0 < si.n_blocks * PS; at0 += gridDim.x * POSITIONS) {
       const int at = at0 + x, blk = at / PS, slot = at % PS;
       const BlockRange br = blk < si.n_blocks ? block_range(si, blk) : BlockRange{0, 0, 0};

@@ -21,9 +21,9 @@ constexpr int WEIGHTS_SHARES = 8;    // of a chunk's tokens, at most (planes of 
 // Parts of the keys for `tokens` rows of a launch made for `parts`, as far as the pairs hold.  All its kernels
 // take it from the tokens that are there: a captured launch may be replayed behind a longer chunk.
 __host__ __device__ inline int stat_parts(const Dev& d, int parts, int tokens) {
-  const int64_t pairs = (int64_t)d.max_tokens * d.q_heads + WEIGHTS_STATS;
-  const int64_t most = pairs / ((int64_t)(tokens > 0 ? tokens : 1) * d.q_heads);
-  return most < parts ? (most > 1 ? (int)most : 1) : parts;
+  const int64_t pairs = (int64_t)d.max_tokens * d.q_heads + WEIGHTS_STATS, rows = (int64_t)tokens * d.q_heads;
+  if (parts * rows <= pairs) return parts;
+  return (int)(pairs / rows);  // (one part of max_tokens tokens always fits)
 }
 
 // log2 of a row's denominator from its parts' (max, sum), eight of them read at once (one after the other,

@@ -89,11 +89,11 @@ __device__ inline void join(float& m, float& l, float mo, float lo) {
   m = mn;
 }
 
-// The units of the call: none where the last append gave a session more than one token (a captured launch,
-// replayed; its weights would be those of the first token alone).
-__device__ inline UnitSplit token_split(const Dev& d, int grid) {
+// The units of a launch made for n_launch single tokens; none where the last append is of other chunks (the launch
+// was captured, and d_q holds other rows).
+__device__ inline UnitSplit token_split(const Dev& d, int grid, int n_launch) {
   UnitSplit us = unit_split(d, grid, TOKEN_MIN_UNITS, TOKEN_NO_LIMIT);
-  if (d.g->total_tokens > d.g->n_seq) us.U = 0;
+  if (d.g->total_tokens != n_launch || d.g->n_seq != n_launch) us.U = 0;
   return us;
 }
 
@@ -101,7 +101,7 @@ template <typename T, int D>
 __global__ void __launch_bounds__(TOKEN_THREADS) weights_token_kernel(
     Dev d, int layer, const __grid_constant__ CUtensorMap map_lo,
     const __grid_constant__ CUtensorMap map_hi, const T* __restrict__ q, float qk_scale,
-    WeightsWork work, int early) {
+    WeightsWork work, int n_launch, int early) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* tiles = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   __shared__ uint64_t s_bars[TOKEN_WARPS * TOKEN_STAGES];
@@ -119,10 +119,10 @@ __global__ void __launch_bounds__(TOKEN_THREADS) weights_token_kernel(
   if (!early) pdl_wait();  // (the first call after an append waits before it lets others start)
   pdl_launch_dependents();
   bool waited = false;
-  const UnitSplit us = token_split(d, gridDim.x);
+  const UnitSplit us = token_split(d, gridDim.x, n_launch);
   const int cta = blockIdx.x;
   if (us.U == 0 || cta >= us.n_cta) {
-    if (cta == 0 && tid == 0 && d.g->total_tokens > d.g->n_seq) set_error(d, KVC_DERR_CHUNK);
+    if (us.U == 0 && cta == 0 && tid == 0) note_other_chunks(d);
     pdl_wait();
     return;
   }
@@ -292,105 +292,100 @@ __global__ void __launch_bounds__(TOKEN_THREADS) weights_token_kernel(
   }
 }
 
-// Pages of one session, eight at a time: blockIdx.y is the session of the call (the first of some, where a
-// captured launch is replayed behind more of them).  (Everything that the append wrote is complete before the
-// kernel in front lets this one start.)
+// Pages of one session, eight at a time: blockIdx.y is the session of the call.  (Everything that the
+// append wrote is complete before the kernel in front lets this one start.)
 __global__ void __launch_bounds__(TOKEN_THREADS) weights_token_add_kernel(Dev d, int grid,
                                                                           WeightsWork work,
                                                                           float* weights) {
   __shared__ __align__(16) float s_lse[64 * G];
   constexpr int AT_ONCE = TOKEN_THREADS / PS, HEADS = 8;  // pages; heads' scores on their way
-  const int tid = threadIdx.x, H = d.kv_heads;
+  const int tid = threadIdx.x, H = d.kv_heads, seq = blockIdx.y;
   pdl_launch_dependents();
-  const UnitSplit us = token_split(d, grid);
-  const int n_seq = us.U > 0 ? d.g->n_seq : 0;
-  bool waited = false;
-  for (int seq = blockIdx.y; seq < n_seq; seq += gridDim.y) {
-    const SeqInfo si = d.seq[seq];
-    const int nb = si.n_blocks, slot = tid % PS;
-    if ((int)blockIdx.x * AT_ONCE >= nb) continue;
-    const int32_t* hrow = d.hist_pt + (size_t)si.sid * d.max_pages_per_session;
-    const int32_t* lrow = d.live_pt + (size_t)si.sid * d.max_pages_per_session;
-    int b = blockIdx.x * AT_ONCE + tid / PS, page = 0, pos = 0;
-    bool in = false;
-    auto find = [&] {  // this thread's slot of its page b
-      in = false;
-      if (b >= nb) return;
-      const BlockRange br = block_range(si, b);
-      in = slot >= br.lo && slot < br.hi;
-      if (!in) return;
-      page = block_page(si, hrow, lrow, b);
-      pos = d.meta_pos[page * PS + slot];
-    };
-    find();
-    const int lane = tid & 31;
-    // A row of lse, eight lanes to its parts.
-    int r = min(tid / 8, H * G - 1), start = si.unit_base + r / G * nb;
-    int cf = us.owner(start), cl = us.owner(start + nb - 1), first = us.slot_of(cf, cf, start);
-    if (!waited) pdl_wait();
-    else __syncthreads();  // (the last session's lse were read)
-    waited = true;
-    float4 x[HEADS];
-    float before = 0.f;
-    const float4* scores = reinterpret_cast<const float4*>(work.scores) + slot;
-    auto fetch = [&](int h0) {
+  const UnitSplit us = token_split(d, grid, gridDim.y);
+  const SeqInfo si = d.seq[seq];
+  const int nb = si.n_blocks, slot = tid % PS;
+  if (us.U == 0 || (int)blockIdx.x * AT_ONCE >= nb) {
+    pdl_wait();
+    return;
+  }
+  const int32_t* hrow = d.hist_pt + (size_t)si.sid * d.max_pages_per_session;
+  const int32_t* lrow = d.live_pt + (size_t)si.sid * d.max_pages_per_session;
+  int b = blockIdx.x * AT_ONCE + tid / PS, page = 0, pos = 0;
+  bool in = false;
+  auto find = [&] {  // this thread's slot of its page b
+    in = false;
+    if (b >= nb) return;
+    const BlockRange br = block_range(si, b);
+    in = slot >= br.lo && slot < br.hi;
+    if (!in) return;
+    page = block_page(si, hrow, lrow, b);
+    pos = d.meta_pos[page * PS + slot];
+  };
+  find();
+  const int lane = tid & 31;
+  // A row of lse, eight lanes to its parts.
+  int r = min(tid / 8, H * G - 1), start = si.unit_base + r / G * nb;
+  int cf = us.owner(start), cl = us.owner(start + nb - 1), first = us.slot_of(cf, cf, start);
+  pdl_wait();
+  float4 x[HEADS];
+  float before = 0.f;
+  const float4* scores = reinterpret_cast<const float4*>(work.scores) + slot;
+  auto fetch = [&](int h0) {
+#pragma unroll
+    for (int h = 0; h < HEADS; ++h)
+      if (in && h0 + h < H) x[h] = scores[((size_t)page * H + h0 + h) * PS];
+  };
+  float* at = weights + (size_t)si.sid * d.max_positions;
+  fetch(0);
+  if (in) before = at[pos];
+  for (int r0 = 0;;) {
+    float2 a = make_float2(-INFINITY, 0.f);
+    if (cf == cl) {
+      if (lane % 8 == 0) a = work.whole[(size_t)seq * H * G + r];
+    } else {
+      for (int c = cf + lane % 8; c <= cl; c += 32) {  // four loads in flight
+        float2 o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          o[i] = c + 8 * i <= cl ? work.parts[(size_t)(c + 8 * i == cf ? first : 2 * (c + 8 * i)) * G + r % G]
+                                 : make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) join(a.x, a.y, o[i].x, o[i].y);
+      }
+    }
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1)
+      join(a.x, a.y, __shfl_xor_sync(FULL, a.x, o), __shfl_xor_sync(FULL, a.y, o));
+    if (lane % 8 == 0) s_lse[r] = a.x + log2f(a.y);
+    r0 += TOKEN_THREADS / 8;
+    if (r0 >= H * G) break;
+    r = min(r0 + tid / 8, H * G - 1);
+    start = si.unit_base + r / G * nb;
+    cf = us.owner(start);
+    cl = us.owner(start + nb - 1);
+    first = us.slot_of(cf, cf, start);
+  }
+  __syncthreads();
+  for (;;) {
+    float w = 0.f;
+    for (int h0 = 0;;) {
 #pragma unroll
       for (int h = 0; h < HEADS; ++h)
-        if (in && h0 + h < H) x[h] = scores[((size_t)page * H + h0 + h) * PS];
-    };
-    float* at = weights + (size_t)si.sid * d.max_positions;
+        if (h0 + h < H) {
+          const float4 lse = reinterpret_cast<const float4*>(s_lse)[h0 + h];
+          w += (exp2f(x[h].x - lse.x) + exp2f(x[h].y - lse.y)) + (exp2f(x[h].z - lse.z) + exp2f(x[h].w - lse.w));
+        }
+      h0 += HEADS;
+      if (h0 >= H) break;
+      fetch(h0);
+    }
+    if (in) at[pos] = before + w;
+    b += gridDim.x * AT_ONCE;
+    if (b - tid / PS >= nb) break;
+    find();
     fetch(0);
     if (in) before = at[pos];
-    for (int r0 = 0;;) {
-      float2 a = make_float2(-INFINITY, 0.f);
-      if (cf == cl) {
-        if (lane % 8 == 0) a = work.whole[(size_t)seq * H * G + r];
-      } else {
-        for (int c = cf + lane % 8; c <= cl; c += 32) {  // four loads in flight
-          float2 o[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            o[i] = c + 8 * i <= cl ? work.parts[(size_t)(c + 8 * i == cf ? first : 2 * (c + 8 * i)) * G + r % G]
-                                   : make_float2(-INFINITY, 0.f);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) join(a.x, a.y, o[i].x, o[i].y);
-        }
-      }
-#pragma unroll
-      for (int o = 4; o > 0; o >>= 1)
-        join(a.x, a.y, __shfl_xor_sync(FULL, a.x, o), __shfl_xor_sync(FULL, a.y, o));
-      if (lane % 8 == 0) s_lse[r] = a.x + log2f(a.y);
-      r0 += TOKEN_THREADS / 8;
-      if (r0 >= H * G) break;
-      r = min(r0 + tid / 8, H * G - 1);
-      start = si.unit_base + r / G * nb;
-      cf = us.owner(start);
-      cl = us.owner(start + nb - 1);
-      first = us.slot_of(cf, cf, start);
-    }
-    __syncthreads();
-    for (;;) {
-      float w = 0.f;
-      for (int h0 = 0;;) {
-#pragma unroll
-        for (int h = 0; h < HEADS; ++h)
-          if (h0 + h < H) {
-            const float4 lse = reinterpret_cast<const float4*>(s_lse)[h0 + h];
-            w += (exp2f(x[h].x - lse.x) + exp2f(x[h].y - lse.y)) + (exp2f(x[h].z - lse.z) + exp2f(x[h].w - lse.w));
-          }
-        h0 += HEADS;
-        if (h0 >= H) break;
-        fetch(h0);
-      }
-      if (in) at[pos] = before + w;
-      b += gridDim.x * AT_ONCE;
-      if (b - tid / PS >= nb) break;
-      find();
-      fetch(0);
-      if (in) before = at[pos];
-    }
   }
-  if (!waited) pdl_wait();
 }
 
 template <typename T, int D>
@@ -401,7 +396,7 @@ cudaError_t launch(const Dev& d, const Limits& lim, int layer, const void* q, fl
   const int grid = lim.sms * 2;
   cudaError_t e = launch_ex(&weights_token_kernel<T, D>, dim3(grid), dim3(TOKEN_THREADS), TOKEN_SMEM, s,
                             true, d, layer, lo, hi, static_cast<const T*>(q), LOG2E / sqrtf((float)D),
-                            work, (int)early);
+                            work, n_seq, (int)early);
   *launches += e == cudaSuccess;
   if (e != cudaSuccess) return e;
   const int per = max(1, min(64, 16 * lim.sms / n_seq));

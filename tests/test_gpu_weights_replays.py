@@ -69,7 +69,7 @@ def test_a_short_chunk_replayed_behind_long_ones(dtype, n):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("tokens", [1, 7, 70])
+@pytest.mark.parametrize("tokens", [7, 70])
 def test_replayed_behind_other_sessions(dtype, tokens):
     """Fewer sessions (nothing of those before them counts), more, and in another order."""
     from tests import prompt_reference as R
@@ -82,14 +82,25 @@ def test_replayed_behind_other_sessions(dtype, tokens):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_single_tokens_replayed_behind_a_chunk_are_refused(dtype):
-    """Captured for a token of each session, replayed behind several: the error word says so, and nothing
-    is added."""
+def test_single_tokens_replayed_behind_other_sessions(dtype):
+    from tests import prompt_reference as R
+    rng = np.random.default_rng(1)
+    cache = R.make_cache(6, dtype=dtype, heads=2, layers=2, pages=64, positions=1000)
+    R.feed(cache, range(6), [300, 17, 150, 1, 64, 90], rng)
+    replays(cache, ([4, 1, 0], [1] * 3), [([5, 0, 2], [1] * 3), ([0, 1, 2], [1] * 3)], rng)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sessions, lens", [([0, 1], [1, 2]), ([0], [40]), ([0], [2]), ([1], [1]),
+                                            ([2, 1, 0], [1, 1, 1])])
+def test_single_tokens_replayed_behind_other_chunks_are_refused(dtype, sessions, lens):
+    """Captured for a token of each of two sessions, replayed behind others: the error word says so, and
+    nothing is added."""
     from tests import prompt_reference as R
     rng = np.random.default_rng(3)
-    cache = R.make_cache(2, dtype=dtype)
+    cache = R.make_cache(3, dtype=dtype)
     work, w = cache.make_weights_workspace(), cache.make_weights()
-    R.feed(cache, [0, 1], [100, 30], rng)
+    R.feed(cache, [0, 1, 2], [100, 30, 500], rng)
     R.feed(cache, [0, 1], [1, 1], rng)
     q = R.queries(cache, 40, rng)
     torch.cuda.synchronize()
@@ -99,10 +110,9 @@ def test_single_tokens_replayed_behind_a_chunk_are_refused(dtype):
     graph.replay()
     torch.cuda.synchronize()
     assert cache.device_status()[1] == 0 and bool((w != 0).any())
-    for lens in ([1, 2], [40]):
-        R.feed(cache, range(len(lens)), lens, rng)
-        before = w.clone()
-        graph.replay()
-        torch.cuda.synchronize()
-        assert torch.equal(w, before)
+    R.feed(cache, sessions, lens, rng)
+    before = w.clone()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(w, before)
     assert cache.device_status()[1] == 32
