@@ -30,7 +30,7 @@
 #include "kvc_prompt.h"
 #include "kvc_prompt_merge.cuh"
 #include "kvc_rope.cuh"
-#include "kvc_weights.h"
+#include "kvc_weights_plain.cuh"
 
 namespace kvc {
 
@@ -555,6 +555,12 @@ __global__ void __launch_bounds__(THREADS, CTAS) weights_sums_f32_kernel(Dev d, 
       if (t != 0 || !in[h]) continue;
       const int page = block_page(si, d.hist_pt + (size_t)si.sid * d.max_pages_per_session,
                                   d.live_pt + (size_t)si.sid * d.max_pages_per_session, blk);
+      if (isnan(sum[h])) {
+        const Dev dev = d;  // (copies, so that only this branch has them in memory)
+        const SeqInfo info = si;
+        sum[h] = plain_sum<float, D>(dev, info, layer, head, page, g + 8 * h, max(i0 * STEP_TOKENS, from[h]),
+                                     min(i1 * STEP_TOKENS, si.t), q, scale, work.stats, parts);
+      }
       work.scores[((size_t)(head * shares + share) * d.n_pages + page) * PS + g + 8 * h] = sum[h];
     }
   }

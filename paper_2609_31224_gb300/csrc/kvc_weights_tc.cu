@@ -29,7 +29,7 @@
 #include <cmath>
 
 #include "kvc_prompt_tc.cuh"
-#include "kvc_weights.h"
+#include "kvc_weights_plain.cuh"
 
 namespace kvc {
 
@@ -337,6 +337,12 @@ __global__ void __launch_bounds__(STAT_THREADS, 1) weights_stat_kernel(
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(&bars[B_S_EMPTY + b]);
+        }
+        if (ok && tok < si.t && isnan(l)) {
+          const float2 again = plain_stat<__nv_bfloat16, D>(d, si, layer, it.head, tok, r % G, q, qk_scale,
+                                                            PAGES * it.begin, PAGES * it.end, nb);
+          m = again.x;
+          l = again.y;
         }
         if (ok && tok < si.t)
           work.stats[((size_t)it.part * d.g->total_tokens + si.q_row0 + tok) * d.q_heads + it.head * G + r % G] =
@@ -660,6 +666,12 @@ __global__ void __launch_bounds__(SUMS_THREADS, 1) weights_sums_kernel(
       }
       if (!ok) break;
       q_no += i1 - i0;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (in[h] && isnan(sum[h]))
+          sum[h] = plain_sum<__nv_bfloat16, D>(d, si, layer, it.head, page[h], slot, max(i0 * TOKENS, seen_from[h]),
+                                               min(i1 * TOKENS, si.t), q, qk_scale, work.stats,
+                                               stat_parts(d, most_parts, d.g->total_tokens));
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         if (in[h]) work.scores[((size_t)(it.head * shares + it.part) * d.n_pages + page[h]) * PS + slot] = sum[h];

@@ -17,7 +17,7 @@
 
 #include "kvc_decode_common.cuh"
 #include "kvc_rope.cuh"
-#include "kvc_weights.h"
+#include "kvc_weights_plain.cuh"
 
 namespace kvc {
 
@@ -89,12 +89,52 @@ __device__ inline void join(float& m, float& l, float mo, float lo) {
   m = mn;
 }
 
+// The scores of a warp's units of a segment again in plain arithmetic (kvc_weights_plain.cuh), and their
+// (max, sum) to ml: lane i has key i % 16 and the query heads 2 (i / 16) and + 1.
+__device__ __noinline__ void score_again(const Dev& d, const SeqInfo& si, int layer, int head, int first,
+                                         int count, const __nv_bfloat16* q, float qk_scale, float* scores,
+                                         float2* ml, int lane) {
+  const int32_t* hrow = d.hist_pt + (size_t)si.sid * d.max_pages_per_session;
+  const int32_t* lrow = d.live_pt + (size_t)si.sid * d.max_pages_per_session;
+  const int key = lane % PS, g = lane / PS * 2;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  for (int k = 0; k < count; ++k) {
+    const int blk = first + k * TOKEN_WARPS, page = block_page(si, hrow, lrow, blk);
+    const BlockRange br = block_range(si, blk);
+    if (key < br.lo || key >= br.hi) continue;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const float s = plain_score<__nv_bfloat16, 128>(d, si, layer, head, 0, g + r, q, qk_scale, page, key);
+      scores[((size_t)page * d.kv_heads + head) * (PS * G) + key * G + g + r] = s;
+      join(m[r], l[r], s, s == s ? 1.f : s);
+    }
+  }
+  __syncwarp();
+#pragma unroll
+  for (int r = 0; r < 2; ++r)
+#pragma unroll
+    for (int o = 1; o < PS; o <<= 1)
+      join(m[r], l[r], __shfl_xor_sync(FULL, m[r], o), __shfl_xor_sync(FULL, l[r], o));
+  if (key == 0) {
+    ml[g] = make_float2(m[0], l[0]);
+    ml[g + 1] = make_float2(m[1], l[1]);
+  }
+}
+
 // The units of a launch made for n_launch single tokens; none where the last append is of other chunks (the launch
 // was captured, and d_q holds other rows).
 __device__ inline UnitSplit token_split(const Dev& d, int grid, int n_launch) {
   UnitSplit us = unit_split(d, grid, TOKEN_MIN_UNITS, TOKEN_NO_LIMIT);
   if (d.g->total_tokens != n_launch || d.g->n_seq != n_launch) us.U = 0;
   return us;
+}
+
+// Two scores into a running (max, sum); -infinity adds nothing, a NaN makes the sum one (in front of all other
+// keys as well, where the maximum is still -infinity).
+__device__ inline void add_two(float& m, float& l, float x, float y) {
+  const float mn = fmaxf(m, fmaxf(x, y)), ref = mn == -INFINITY ? 0.f : mn;
+  l = l * exp2f(m - ref) + exp2f(x - ref) + exp2f(y - ref);
+  m = mn;
 }
 
 template <typename T, int D>
@@ -203,9 +243,7 @@ __global__ void __launch_bounds__(TOKEN_THREADS) weights_token_kernel(
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const float x = in0 ? c[r] : -INFINITY, y = in1 ? c[2 + r] : -INFINITY;
-          const float mn = fmaxf(m[r], fmaxf(x, y));
-          l[r] = l[r] * exp2_safe(m[r], mn) + exp2_safe(x, mn) + exp2_safe(y, mn);
-          m[r] = mn;
+          add_two(m[r], l[r], x, y);
         }
       } else {
         // Key 4 i + j of lane group j = lane / 8; lane c of it ends up with row c % 4.
@@ -236,9 +274,7 @@ __global__ void __launch_bounds__(TOKEN_THREADS) weights_token_kernel(
           z += __shfl_xor_sync(FULL, z, 4);
           if (c < 4) to[key * G + c] = z;
           const float sc = key >= br.lo && key < br.hi ? z : -INFINITY;
-          const float mn = fmaxf(m[0], sc);
-          l[0] = l[0] * exp2_safe(m[0], mn) + exp2_safe(sc, mn);
-          m[0] = mn;
+          add_two(m[0], l[0], sc, -INFINITY);
         }
       }
       __syncwarp();
@@ -257,7 +293,15 @@ __global__ void __launch_bounds__(TOKEN_THREADS) weights_token_kernel(
     }
     if (failed_at >= 0 && lane == 0) s_abort = 1;
     // This warp's state: lanes of the same rows together.
-    if constexpr (sizeof(T) == 2) {
+    bool again = false;
+    if constexpr (sizeof(T) == 2) again = __any_sync(FULL, isnan(l[0] + l[1])) && failed_at < 0;
+    if (again) {
+      if constexpr (sizeof(T) == 2) {
+        const Dev dev = d;  // (copies, so that only this branch has them in memory)
+        const SeqInfo info = si;
+        score_again(dev, info, layer, head, b0 + warp, mine, q, qk_scale, work.scores, s_ml + warp * G, lane);
+      }
+    } else if constexpr (sizeof(T) == 2) {
 #pragma unroll
       for (int r = 0; r < 2; ++r)
 #pragma unroll
