@@ -22,8 +22,8 @@
 // their chains of latencies; one after the other instead of together, the nine parts of a row's statistics
 // were 3 us of it.
 //
-// Tiles with a number that is not finite (in a slot that holds nothing as well) go a slow way in plain
-// binary32 arithmetic, where a key that a row does not see takes no part.
+// Tiles with a number that is not finite, or whose upper piece is not (in a slot that holds nothing as well), go a
+// slow way in plain binary32 arithmetic, where a key that a row does not see takes no part.
 #include <algorithm>
 #include <cmath>
 
@@ -224,14 +224,15 @@ __device__ inline void load_pages(const Dev& d, int layer, int head, const int (
   }
 }
 
-// Whether one of the numbers that this thread brought is not finite.
+// Whether one of the numbers that this thread brought is not finite, or so large that rounded to TF32 it is not
+// (its upper piece would be infinite, the product NaN).
 __device__ inline bool odd_pages(int n_pg, const float* k, const float* v) {
   const int c = threadIdx.x & 15;
   bool odd = false;
   auto look = [&](const float* x) {
     const uint4 w = *reinterpret_cast<const uint4*>(x);
-    const uint32_t e = 0x7F800000u;
-    odd |= (w.x & e) == e || (w.y & e) == e || (w.z & e) == e || (w.w & e) == e;
+    const uint32_t e = 0x7FFFFFFFu, most = 0x7F7FEFFFu;
+    odd |= (w.x & e) > most || (w.y & e) > most || (w.z & e) > most || (w.w & e) > most;
   };
 #pragma unroll 4
   for (int r = threadIdx.x >> 4; r < n_pg * PS; r += THREADS / 16) {
