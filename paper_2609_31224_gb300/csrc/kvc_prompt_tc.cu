@@ -30,9 +30,10 @@
 //   warps 4-7   query rows, rotated, scaled and rounded, into three tiles of shared memory: an item's
 //               first one while the item before still runs
 //   warps 8-15  softmax, four warps a tile: a thread has one row of S, 32 keys at a time, and writes P over
-//               it.  P is taken against the maximum of the row's first keys, for as long as a sum of 32
-//               stays below 2^20 (sums and roundings do not depend on the scale): later ones look for no
-//               maximum, and O is rescaled in tensor memory only when a sum passes that
+//               it.  P is taken against a reference 20 above the maximum of the row's first keys, for as long
+//               as a sum of 32 stays below 1 (sums and roundings do not depend on the scale, and P <= 1 keeps
+//               its products with the largest V finite): later ones look for no maximum, and O is rescaled in
+//               tensor memory only when a sum passes that
 // A step's keys come in halves, each with scores of its own: while the softmax of one half runs, the
 // tensor cores have the other half's O += P V and next scores, so that a row's warp need not wait.
 // Tensor memory: S_A, S_B (two halves each, P over the first part of a half), O_A, O_B, 128 columns each:
@@ -63,7 +64,8 @@ constexpr int TC_THREADS = 512;
 constexpr int S_COL = 0, O_COL = 256, ALL_COLS = 512;
 constexpr int HALF = KEYS / 2;                     // of a step's keys
 constexpr int CHUNK = 32;                          // keys that a row takes at a time
-constexpr float SUM_LIMIT = 1048576.f;              // of a chunk's P in a row: 2^20
+constexpr float ROOM = 20.f;                        // by which a reference lies above the maximum it is taken from
+constexpr float SUM_LIMIT = 1.f;                    // of a chunk's P in a row, 2^ROOM times what it starts with
 constexpr float NO_KEY = -3.402823466e38f;          // reference of a row whose keys so far all score -infinity
 constexpr float ALL_UP = 200.f;                     // a rise of the reference behind which nothing is left of P
 
@@ -520,7 +522,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
                 for (int i = 0; i < PS; ++i) w[p * PS + i] = (seen >> i & 1) ? w[p * PS + i] : 0xFF800000u;
               }
             }
-            auto most = [&] {
+            auto most = [&] {  // a reference for these keys
               float a[4];
 #pragma unroll
               for (int i = 0; i < 4; ++i) a[i] = __uint_as_float(w[i]);
@@ -528,7 +530,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
               for (int i = 4; i < CHUNK; i += 4)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) a[k] = fmaxf(a[k], __uint_as_float(w[i + k]));
-              return fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3]));
+              return fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])) + ROOM;
             };
             uint32_t pw[CHUNK / 2];
             auto sum_of = [&] {
@@ -544,7 +546,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) prompt_tc_kernel(
               const float2 r2 = __fadd2_rn(rs[0], rs[1]);
               return r2.x + r2.y;
             };
-            // The reference is the maximum of the row's first chunk (which holds position 0 of what is
+            // The reference goes by the maximum of the row's first chunk (which holds position 0 of what is
             // resident, so that each row sees a key of it), until a sum passes the limit (or is NaN):
             // then it rises by a whole number, so that what was written of P scales exactly.  O may be
             // rescaled behind the last O += P V: the other half's scores come after it, of the same step
