@@ -207,6 +207,9 @@ int kvc_attn_decode_kv(kvc_ctx* ctx, int layer, const void* d_k, const void* d_v
  * call decided form a prefix of the live region: its survivors move (all
  * layers, 16-byte copies) to the compacted region in position order, and
  * consumed live pages are freed.
+ * (Sessions that kvc_evict_weighted has thinned out hold such positions in the compacted region as well; the
+ * rule is the same for them, and the rows move as there.  Capture the call behind the first
+ * kvc_evict_weighted of the context: captured before, it looks at live positions alone.)
  *   d_resident_out  optional device [n_seq] int64: resident count afterwards
  * Invalidates the last append's queries for attention. */
 int kvc_evict(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, int64_t* d_resident_out,

@@ -186,6 +186,10 @@ struct kvc_ctx {
   std::vector<int32_t> tail_mod;  // (live_head + n_live) % PS, exact
   std::vector<int32_t> pos_next;  // exact
   std::vector<ResidentEstimate> resident;
+  // Sessions that an eviction by weight may have left evictable positions of among the compacted ones
+  // (bit 0; bit 1: a graph holds the call and may be replayed at any time).
+  std::vector<uint8_t> thinned;
+  bool any_thinned = false;
   int64_t used_ub = 0;            // upper bound of pages in use after enqueued work
   int64_t delta_since_readback = 0;
   bool readback_pending = false;
@@ -395,6 +399,7 @@ int kvc_create(kvc_ctx** out, const kvc_config* cfg, void* d_pool, size_t pool_b
   ctx->tail_mod.assign(cfg->n_sessions, 0);
   ctx->pos_next.assign(cfg->n_sessions, 0);
   ctx->resident.assign(cfg->n_sessions, ResidentEstimate());
+  ctx->thinned.assign(cfg->n_sessions, 0);
   auto cleanup = [&](int code) {
     if (ctx->ev) cudaEventDestroy(ctx->ev);
     if (ctx->h_readback) cudaFreeHost(ctx->h_readback);
@@ -530,8 +535,21 @@ int kvc_evict(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, int64_t* d_res
   a.n_seq = n_seq;
   for (int i = 0; i < n_seq; ++i) a.sessions[i] = h_sessions[i];
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  KVC_CUDA(launch_evict(ctx->d, ctx->kv4, a, d_resident_out, ctx->h_readback, ctx->lim.sms, s));
-  ctx->launches += 2;  // plan and copy
+  bool capturing = false, thinned = false;
+  if (ctx->any_thinned) {
+    KVC_CUDA(is_capturing(s, &capturing));
+    for (int i = 0; i < n_seq; ++i) thinned = thinned || capturing || ctx->thinned[h_sessions[i]];
+  }
+  if (thinned) {
+    WeighArgs w = {};
+    w.n_seq = n_seq;
+    for (int i = 0; i < n_seq; ++i) w.sessions[i] = h_sessions[i];
+    KVC_CUDA(launch_evict_weighted(ctx->d, ctx->weigh, ctx->kv4, w, nullptr, d_resident_out, nullptr,
+                                   ctx->h_readback, s, &ctx->launches));
+  } else {
+    KVC_CUDA(launch_evict(ctx->d, ctx->kv4, a, d_resident_out, ctx->h_readback, ctx->lim.sms, s));
+    ctx->launches += 2;  // plan and copy
+  }
   for (int i = 0; i < n_seq; ++i) ctx->resident[h_sessions[i]].evict(ctx->cfg);
   ctx->used_ub += n_seq;  // an evict adds at most one page per session, net
   ctx->delta_since_readback += n_seq;
@@ -563,9 +581,15 @@ int kvc_evict_weighted(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, const
     a.keep[i] = h_keep[i];
   }
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  bool capturing = false;
+  KVC_CUDA(is_capturing(s, &capturing));
   KVC_CUDA(launch_evict_weighted(ctx->d, ctx->weigh, ctx->kv4, a, d_weights, d_resident_out, d_kept,
                                  ctx->h_readback, s, &ctx->launches));
-  for (int i = 0; i < n_seq; ++i) ctx->resident[h_sessions[i]].thin(h_keep[i]);
+  ctx->any_thinned = true;
+  for (int i = 0; i < n_seq; ++i) {
+    ctx->resident[h_sessions[i]].thin(h_keep[i]);
+    ctx->thinned[h_sessions[i]] |= capturing ? 3 : 1;
+  }
   ctx->used_ub += n_seq;  // an evict adds at most one page per session, net
   ctx->delta_since_readback += n_seq;
   enqueue_readback(ctx, s);
@@ -588,6 +612,7 @@ int kvc_release(kvc_ctx* ctx, int n_seq, const int32_t* h_sessions, void* stream
     ctx->tail_mod[h_sessions[i]] = 0;
     ctx->pos_next[h_sessions[i]] = 0;
     ctx->resident[h_sessions[i]].release();
+    ctx->thinned[h_sessions[i]] &= 2;
   }
   enqueue_readback(ctx, s);
   ctx->attn_valid = false;

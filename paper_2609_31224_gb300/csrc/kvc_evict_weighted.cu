@@ -16,6 +16,9 @@
 //   weigh_apply_kernel   a CTA per session: moves, tags, page lists, state, mask
 //   weigh_copy_kernel    a CTA per session and (layer, K or V, head): the rows, ascending
 //
+// kvc_evict takes this way too, with the rule of its policy in place of the weights, for sessions that were
+// thinned out by weight: what it may drop then lies among the compacted positions as well.
+//
 // Bound by the rows that move, each read and written once.  4,099 positions of 32 layers thinned out to
 // 2,048: select 13-19 us, apply 9-13, copy 92 (537 MB, 5.8 TB/s); 16 sessions of 16 layers to 700 each:
 // copy 235 us.  Select and apply are one CTA's latencies a session: radix passes of 8 bits over keys in
@@ -66,7 +69,16 @@ __device__ inline int64_t list_base(const Dev& d, const int32_t* sessions, int q
   return total;  // (all positions of a pool are fewer than 2^31)
 }
 
-template <int N>
+// Whether kvc_evict may drop a position: by the rule of Sec. 3.3 and its position-granular variant, or by the
+// sink + recent variant.
+__device__ inline bool rule_takes(const Dev& d, const SessState& st, int type, int unit, int pos) {
+  if (d.policy == KVC_POLICY_SINK_RECENT) return pos >= d.sink && pos < st.pos_next - d.recent;
+  return unit >= 0 && unit <= st.unit_cur - d.window && (type == KVC_ACOUSTIC || type == KVC_ASR_DELIM);
+}
+
+// RULE: by the context's policy instead of weights, kinds and counts to keep; of the candidates, in position
+// order, the first ones go: as many as the budget wants, and the rest of the last one's unit (KVC_POLICY_UNIT).
+template <int N, bool RULE>
 __global__ void __launch_bounds__(META_THREADS) weigh_select_kernel(Dev d, WeighDev w,
                                                                     WeighArgsT<N> a,
                                                                     const float* weights,
@@ -93,22 +105,54 @@ __global__ void __launch_bounds__(META_THREADS) weigh_select_kernel(Dev d, Weigh
   for (int j = tid; j < n; j += META_THREADS) {
     const int gs = retained_slot(st, hrow, lrow, j);
     const int type = d.meta_type[gs], pos = d.meta_pos[gs];
-    const bool cand = type < 32 && (a.kinds >> type & 1) && pos >= a.sink && pos < st.pos_next - a.recent;
-    const uint32_t k = cand ? weight_key(heavy[pos]) : NO_KEY;
+    const bool cand = RULE ? rule_takes(d, st, type, d.meta_unit[gs], pos)
+                           : type < 32 && (a.kinds >> type & 1) && pos >= a.sink && pos < st.pos_next - a.recent;
+    const uint32_t k = !cand ? NO_KEY : RULE ? 0u : weight_key(heavy[pos]);
     list[j] = make_uint2(k, (uint32_t)gs);
     if (j < CACHED_KEYS) s_keys[j] = k;
     n_cand += cand;
   }
   int cands;
   block_exclusive_scan(n_cand, &cands, s_warp);
-  const int drop = min(max(0, n - a.keep[q]), cands);
+  int64_t over = n - a.keep[q];
+  if (RULE) over = d.policy == KVC_POLICY_SINK_RECENT ? n : d.budget < 0 ? 0 : n - d.budget;
+  int drop = (int)min(max((int64_t)0, over), (int64_t)cands);
 
+  // Index of the rank-th position of a key.
+  auto nth = [&](uint32_t key, int rank) {
+    int seen = 0;
+    for (int j0 = 0; j0 < n; j0 += META_THREADS) {
+      const int j = j0 + tid;
+      const int is = j < n && key_at(j) == key;
+      int total;
+      const int before = seen + block_exclusive_scan(is, &total, s_warp);
+      if (is && before == rank - 1) s_found[3] = j;
+      seen += total;
+      if (seen >= rank) break;
+    }
+    __syncthreads();
+    return s_found[3];
+  };
   WeighPlan p = {};
-  p.drop = drop;
   p.key = 0;
   p.tie_last = -1;
   if (drop > 0 && drop == cands) {
     p.key = NO_KEY;  // all that may
+  } else if (RULE && drop > 0) {
+    p.tie_last = nth(0, drop);
+    if (d.policy == KVC_POLICY_UNIT) {
+      const int unit = d.meta_unit[list[p.tie_last].y];
+      int rest = 0, last = p.tie_last;
+      for (int j = p.tie_last + 1 + tid; j < n; j += META_THREADS)
+        if (key_at(j) == 0 && d.meta_unit[list[j].y] == unit) {
+          ++rest;
+          last = j;
+        }
+      int more;
+      block_exclusive_scan(rest, &more, s_warp);
+      drop += more;
+      p.tie_last = block_max(last, s_warp);
+    }
   } else if (drop > 0) {
     // The drop-th smallest key, digit by digit: `rank` of it among the keys that share the digits
     // found so far.
@@ -140,21 +184,9 @@ __global__ void __launch_bounds__(META_THREADS) weigh_select_kernel(Dev d, Weigh
     p.key = prefix;
     // Of the keys equal to it the first `rank` go.
     p.tie_last = n;
-    if (rank < equal) {
-      int seen = 0;
-      for (int j0 = 0; j0 < n; j0 += META_THREADS) {
-        const int j = j0 + tid;
-        const int is = j < n && key_at(j) == prefix;
-        int total;
-        const int before = seen + block_exclusive_scan(is, &total, s_warp);
-        if (is && before == rank - 1) s_found[3] = j;
-        seen += total;
-        if (seen >= rank) break;
-      }
-      __syncthreads();
-      p.tie_last = s_found[3];
-    }
+    if (rank < equal) p.tie_last = nth(prefix, rank);
   }
+  p.drop = drop;
   // The first and the last position that go.
   int first = INT_MAX, last = -1;
   if (drop > 0)
@@ -409,7 +441,7 @@ __global__ void __launch_bounds__(COPY_THREADS) weigh_copy_kv4_kernel(Dev d, Wei
   }
 }
 
-template <int N>
+template <int N, bool RULE>
 cudaError_t launch_plan(const Dev& d, const WeighDev& w, const WeighArgs& all, const float* weights,
                         int64_t* resident_out, uint8_t* kept, int64_t* used_out, cudaStream_t s, int64_t* launches) {
   WeighArgsT<N> a;
@@ -421,7 +453,7 @@ cudaError_t launch_plan(const Dev& d, const WeighDev& w, const WeighArgs& all, c
     a.sessions[i] = all.sessions[i];
     a.keep[i] = all.keep[i];
   }
-  cudaError_t e = launch_ex(&weigh_select_kernel<N>, dim3(a.n_seq), dim3(META_THREADS),
+  cudaError_t e = launch_ex(&weigh_select_kernel<N, RULE>, dim3(a.n_seq), dim3(META_THREADS),
                             CACHED_KEYS * 4, s, true, d, w, a, weights, used_out);
   if (e != cudaSuccess) return e;
   ++*launches;
@@ -436,9 +468,9 @@ cudaError_t launch_plan(const Dev& d, const WeighDev& w, const WeighArgs& all, c
 cudaError_t launch_evict_weighted(const Dev& d, const WeighDev& w, bool kv4, const WeighArgs& a,
                                   const float* weights, int64_t* resident_out, uint8_t* kept,
                                   int64_t* used_out, cudaStream_t s, int64_t* launches) {
-  cudaError_t e = a.n_seq <= FEW
-                      ? launch_plan<FEW>(d, w, a, weights, resident_out, kept, used_out, s, launches)
-                      : launch_plan<MAX_SEQ>(d, w, a, weights, resident_out, kept, used_out, s, launches);
+  auto plan = a.n_seq <= FEW ? (weights ? launch_plan<FEW, false> : launch_plan<FEW, true>)
+                             : (weights ? launch_plan<MAX_SEQ, false> : launch_plan<MAX_SEQ, true>);
+  cudaError_t e = plan(d, w, a, weights, resident_out, kept, used_out, s, launches);
   if (e != cudaSuccess) return e;
   const dim3 grid(d.layers * 2 * d.kv_heads, a.n_seq);
   if (!kv4)

@@ -115,6 +115,7 @@ cudaError_t launch_append_layers(const Dev& d, int total, int layer0, int n_laye
                                  const void* v, bool after_plan, cudaStream_t s);
 cudaError_t launch_evict(const Dev& d, bool kv4, const SeqArgs& a, int64_t* resident_out,
                          int64_t* used_out, int sms, cudaStream_t s);
+// (No weights: by the context's policy.)
 cudaError_t launch_evict_weighted(const Dev& d, const WeighDev& wd, bool kv4, const WeighArgs& a,
                                   const float* weights, int64_t* resident_out, uint8_t* kept,
                                   int64_t* used_out, cudaStream_t s, int64_t* launches);
