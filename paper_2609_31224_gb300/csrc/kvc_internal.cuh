@@ -238,12 +238,6 @@ __device__ inline int block_page(const SeqInfo& si, const int32_t* hist_row,
 
 __device__ inline void set_error(const Dev& d, int bits) { atomicOr(&d.g->err, bits); }
 
-// What a launch records that finds no units (one thread): it was captured, and replayed behind chunks that it does
-// not take.  Behind a failed append, whose error is recorded, nothing.
-__device__ inline void note_other_chunks(const Dev& d) {
-  if (d.g->total_tokens > 0) set_error(d, KVC_DERR_CHUNK);
-}
-
 // Tagged partial states.  A CTA writes each value of its partial state as one
 // 64-bit word, (tag << 32) | binary32 bits, and arrives with a relaxed atomic: no
 // release fence waits for its stores.  The last CTA to arrive reads each word

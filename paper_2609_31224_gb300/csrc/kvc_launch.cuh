@@ -8,6 +8,12 @@
 
 namespace kvc {
 
+// What a launch records that finds no units (one thread): it was captured, and replayed behind chunks that it does
+// not take.  Behind a failed append, whose error is recorded, nothing.
+__device__ inline void note_other_chunks(const Dev& d) {
+  if (d.g->total_tokens > 0) set_error(d, KVC_DERR_CHUNK);
+}
+
 // ---------------------------------------------------------------------------
 // Launchers (defined in the .cu files).
 // ---------------------------------------------------------------------------
