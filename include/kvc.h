@@ -319,7 +319,9 @@ int kvc_attn_prompt(kvc_ctx* ctx, int layer, const void* d_q, void* d_out, void*
  *   d_weights  device [n_sessions][max_positions] binary32, by session id and position, 16-byte
  *              aligned; the caller clears a session's row when it ends (kvc_release)
  *   d_work     device scratch of at least kvc_weights_workspace bytes, 256-byte aligned; its
- *              contents need not last between calls, calls that share it must be ordered
+ *              contents need not last between calls.  Calls of several contexts that share it must be
+ *              ordered; those of one context must be whatever their scratch (work lists and counters
+ *              are the context's)
  * Captured behind chunks it may be replayed behind chunks of any length and any number of sessions; behind
  * single tokens, behind single tokens of as many sessions (behind others it adds nothing and the error word
  * says KVC_DERR_CHUNK).

@@ -305,7 +305,8 @@ class KVCache:
                            device=self.pool.device)
 
     def make_weights_workspace(self):
-        """Scratch for attn_weights; one for each set of calls that are not ordered."""
+        """Scratch for attn_weights.  One is enough: calls on a cache, and replays of graphs that hold
+        them, are ordered whatever their scratch.  (Two caches need one each unless they are ordered, too.)"""
         import torch
         out = ctypes.c_size_t()
         _check(self.lib.kvc_weights_workspace(ctypes.byref(self.cfg), ctypes.byref(out)))
