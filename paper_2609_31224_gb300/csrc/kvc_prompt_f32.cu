@@ -18,9 +18,10 @@
 // Measured: three prompts of up to 1,501 tokens, 4 KV heads, 198 us a layer (531 on the FMA pipes); bound
 // by the products and the operands' taking apart (16 rows a warp leave each B row's pieces to be formed by
 // eight warps), and by items: 32 tokens of a KV head, last ones first, on 152 SMs.  Weights of three units
-// of 17 tokens behind 1,100 positions 29.5 us a layer (102 on the FMA pipes), which is three launches and
+// of 17 tokens behind 1,100 positions 30 us a layer (102 on the FMA pipes), which is three launches and
 // their chains of latencies; one after the other instead of together, the nine parts of a row's statistics
-// were 3 us of it.
+// were 3 us of it.  Weights of long chunks: the three prompts 234 us a layer, 4,099 tokens 855 (15 and
+// 20 TFLOP/s of scores formed once; they are formed twice).
 //
 // Tiles with a number that is not finite, or whose upper piece is not (in a slot that holds nothing as well), go a
 // slow way in plain binary32 arithmetic, where a key that a row does not see takes no part.

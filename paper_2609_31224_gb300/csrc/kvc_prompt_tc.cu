@@ -9,18 +9,29 @@
 // the other tile's.
 //
 // Work and bound: 4 D flops a query row and key, 2.2 TFLOP for one prompt of 16,384 tokens and 8 KV
-// heads; 1,596 us, 1,378 TFLOP/s, 73 % of what the tensor cores were measured to do in a library
-// product.  A product instruction takes 77 cycles, 128 columns wide or 64: the 48 of a step, whose scores
+// heads; 1,660 to 1,690 us, 1,310 TFLOP/s, 69 % of what the tensor cores were measured to do in a library
+// product (figures that steps are compared by here are of one machine, where it took 1,596).  A product instruction takes 77 cycles, 128 columns wide or 64: the 48 of a step, whose scores
 // come in halves (below), 3,700 of its 3,800 cycles.  With scores of 128 keys a product they would be 2,470,
 // but then the softmax is what a step waits for, 450 cycles and more for 32 keys of a row: measured with P
 // of the second half in shared memory, so that the next scores can start early (16,384 tokens 1,608 us,
 // 4,099 135 a layer, 250 14.9), and earlier, at 1,811 us, with both halves' scores in one product (1,970 us;
 // 16 warps of softmax, two a row, the same).  Code counts as much: the loop of a wait out of line took
 // 1,657 us to 1,617; a softmax with one copy of its arithmetic instead of two spills (2,076 us).
-// K and V are read once per item, 745 us of copies that run beside.  Also: 4,099 tokens 138 us a layer
-// (998 TFLOP/s), eight prompts of up to 2,500 tokens 174 us, four of up to 700 behind 4,096 positions
-// 157 us, one of 250 tokens 14.0 us, which is latency: a launch, an item's set-up, two steps one after
-// the other.
+// K and V are read once per item, 745 us of copies that run beside.
+//
+// Shorter prompts are bound by what stands between steps: with the busiest SM's steps and items counted off
+// the lists (61, 61 and 872 steps; 3.4, 7.8 and 13.5 items an SM), 4,099 tokens (140 us a layer, 980
+// TFLOP/s), eight prompts of up to 2,500 (175 us) and 16,384 tokens come out at 1.7 us a step, some 8 us
+// an item and 6 us a launch.  An item has an edge step whose V rows one warp looks through, a last softmax
+// and product with nothing beside them, and an output that the softmax warps write before the next
+// item's first scores.  Four prompts of up to 700 tokens behind 4,096 positions, 157 us: 72 steps on the
+// busiest SM for a mean of 62, since whole items go to the SMs.  One of 250 tokens, 15 to 16 us: 32 items for
+// 152 SMs, a launch, an item's set-up, two steps one after the other.
+//
+// q and P are rounded to bfloat16 once each, as over short chunks (kvc_attn_prefill_tc.cu), since a product of
+// bfloat16 K or V takes no wider operand: 2.4e-3 to 2.9e-3 of the outputs' norm, of which their own
+// rounding is 1.6e-3.  Two pieces of either would be half as many products again (of 128 x 128 x 128 four a
+// step, two of them scores).
 //
 // Warp roles (512 threads):
 //   warp 0      items from the counter; K and V by TMA, a page's 4 KiB of a head a copy (twice as many of

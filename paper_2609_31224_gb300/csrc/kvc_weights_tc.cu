@@ -361,7 +361,7 @@ __global__ void __launch_bounds__(STAT_THREADS, 1) weights_stat_kernel(
 }
 
 // ---------------------------------------------------------------------------
-// Sums by key: an item is 256 keys (tiles A and B) of one (session, KV head) and a share of the tokens.
+// Sums by key: an item is 512 keys (four tiles) of one (session, KV head) and a share of the tokens.
 // ---------------------------------------------------------------------------
 constexpr int OFF_LSE = OFF_GROUP + 136;
 static_assert((GROUPS + 1) * 4 <= 136 && OFF_LSE % 16 == 0 && OFF_LSE + LSE_RING * M * 4 <= OFF_TILES,

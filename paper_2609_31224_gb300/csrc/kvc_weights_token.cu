@@ -11,8 +11,9 @@
 //             more at the price of one
 //   binary32  eight lanes a key, an eighth of the query rows in the registers of each
 // Bound by the keys' bytes for many sessions: 64 sessions of 4,100 positions, 8 KV heads, 96 us a layer
-// for 79 us at the copy bandwidth (5.6 TB/s).  One session, 8.2 us for 1.3, is two launches' latencies:
-// their release, q or the parts, a ring's first tiles, then the scores' way back through L2.
+// for 79 us at the copy bandwidth (5.6 TB/s); binary32, 4 KV heads, 57 us for 40.  One session, 7.9 us for 1.3
+// (binary32 8.6), is two launches' latencies: their release, q or the parts, a ring's first tiles, then the
+// scores' way back through L2.
 #include <cmath>
 
 #include "kvc_decode_common.cuh"
