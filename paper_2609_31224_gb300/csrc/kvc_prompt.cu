@@ -28,10 +28,11 @@ cudaError_t launch_attn_prompt(const Dev& d, const Limits& lim, int layer, const
   int64_t parts = lim.sms / items;
   if (parts == 1 && 2 * lim.sms / items > 2) parts = 3;
   parts = std::max<int64_t>(1, std::min({parts, most, part_items(d) / items}));
+  const cudaError_t e = tc ? launch_prompt_tc(d, lim, layer, q, out, (int)parts, items, s, launches)
+                           : launch_prompt_f32(d, lim, layer, q, out, (int)parts, items, s, launches);
   // (All kernels wait for the one before them before they let the next one start.)
-  order->launched(layer, false);
-  return tc ? launch_prompt_tc(d, lim, layer, q, out, (int)parts, items, s, launches)
-            : launch_prompt_f32(d, lim, layer, q, out, (int)parts, items, s, launches);
+  if (e == cudaSuccess) order->launched(layer, false);
+  return e;
 }
 
 }  // namespace kvc

@@ -107,9 +107,12 @@ cudaError_t launch_attn_weights(const Dev& d, const Limits& lim, int layer, cons
   WeightsWork w;
   lay_out(static_cast<uint8_t*>(work), d.n_pages, d.q_heads, d.max_tokens, d.max_seq, &w);
   // (Each kernel but an early one waits for the one before it before it lets the next one start.)
-  const bool early = order->early(layer, false);
-  order->launched(layer, false);
-  if (max_t == 1) return launch_weights_token(d, lim, layer, q, weights, w, n_seq, early, s, launches);
+  if (max_t == 1) {
+    const bool early = order->early(layer, false);
+    const cudaError_t e = launch_weights_token(d, lim, layer, q, weights, w, n_seq, early, s, launches);
+    if (e == cudaSuccess) order->launched(layer, false);
+    return e;
+  }
   // Where the chunk's rows alone are too few items (64 tokens of a KV head, or 32), the keys are cut into
   // parts of 32 pages or more (binary32: eight), two items an SM in all.  One session, 4,096 positions, 8 KV
   // heads (4), us a layer, against one part: a chunk of 8 tokens 51 -> 25 (256 -> 26), of 64 tokens
@@ -124,10 +127,11 @@ cudaError_t launch_attn_weights(const Dev& d, const Limits& lim, int layer, cons
   const int64_t keys = (pages_sum / pages + n_seq) * d.kv_heads;
   int shares = 1;
   while (shares < WEIGHTS_SHARES && keys * shares < 4 * ctas && max_t / 32 > 4 * shares) shares *= 2;
-  const cudaError_t e = d.esz == 2
-                            ? launch_weights_tc(d, lim, layer, q, w, (int)parts, shares, s, launches)
-                            : launch_weights_f32(d, lim, layer, q, w, (int)parts, shares, s, launches);
-  return e != cudaSuccess ? e : launch_add(d, lim, d.kv_heads * shares, w, weights, n_seq, s, launches);
+  cudaError_t e = d.esz == 2 ? launch_weights_tc(d, lim, layer, q, w, (int)parts, shares, s, launches)
+                             : launch_weights_f32(d, lim, layer, q, w, (int)parts, shares, s, launches);
+  if (e == cudaSuccess) e = launch_add(d, lim, d.kv_heads * shares, w, weights, n_seq, s, launches);
+  if (e == cudaSuccess) order->launched(layer, false);
+  return e;
 }
 
 }  // namespace kvc
