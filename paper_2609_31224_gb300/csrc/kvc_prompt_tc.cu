@@ -120,7 +120,7 @@ constexpr int OFF_ITEM = 512;                      // [2]
 constexpr int OFF_TMEM = OFF_ITEM + 2 * 128;
 constexpr int OFF_STOP = OFF_TMEM + 4;
 constexpr int OFF_GROUP = OFF_STOP + 4;            // the work list
-constexpr int OFF_TILES = 3072;                    // query tiles, then the ring
+constexpr int OFF_TILES = 3 * 1024;                // query tiles, then the ring
 constexpr int SMEM_BYTES = OFF_TILES + (Q_SLOTS + RING) * SLOT;
 static_assert(N_BARS * 8 <= OFF_ITEM && OFF_GROUP + (GROUPS + 1) * 4 <= OFF_TILES, "header fits");
 static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of a CTA");

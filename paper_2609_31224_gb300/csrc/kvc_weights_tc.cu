@@ -52,7 +52,7 @@ constexpr int OFF_ITEM = 512;                      // [2]
 constexpr int OFF_TMEM = OFF_ITEM + 2 * 128;
 constexpr int OFF_STOP = OFF_TMEM + 4;
 constexpr int OFF_GROUP = OFF_STOP + 4;            // the work list
-constexpr int OFF_TILES = 3072;
+constexpr int OFF_TILES = 3 * 1024;
 constexpr int SMEM_BYTES = OFF_TILES + 7 * SLOT;
 static_assert(SMEM_BYTES <= 227 * 1024, "shared memory of a CTA");
 
